@@ -426,6 +426,80 @@ typedef struct {
 int ht_gat_epoch(ht_ctx *ctx, const ht_graph *g, const ht_gat_model *model, const ht_tensor *X,
                  const int32_t *labels, float *loss_out, ht_stats *stats);
 
+/* ------------------------------------------------- models over ids: their ends */
+
+/* For programs that compose layers themselves: rows for vertices (tokens, items)
+ * that have an id instead of features, and losses over many classes.  All
+ * tensors in HBM, values fp32, ids int32; an id < 0 stands for none.  Results do
+ * not depend on the order in which the GPU runs things: the same bits from call
+ * to call.  The calls are asynchronous on the context's stream.  A program may
+ * record them (HIP graphs) after it has made the same calls once: a recorded
+ * call allocates nothing, and is refused with HT_ESTATE where it would have to.
+ * Calls and replays on one context share its scratch memory and must not overlap
+ * in time. */
+
+/* H[i] = scale * table[ids[i]] for the rows of H [n x d]; ids: device, n.
+ * An id < 0 gives a row of zeros, one that is not below table's rows a row of
+ * NaN (it cannot be refused: it is on the GPU).  H may not share memory with
+ * table. */
+int ht_embed_fwd(ht_ctx *ctx, const ht_tensor *table, const int32_t *ids, float scale, ht_tensor *H);
+/* The gradient of that: d_table[t] = scale * sum of dH[i] over ids[i] = t, 0 for
+ * ids that do not occur; with accumulate the sum is added to what is there, and
+ * only rows whose id occurs are touched (with scale * -lr and the table itself:
+ * its SGD step).  Ids outside the table count nowhere. */
+int ht_embed_bwd(ht_ctx *ctx, const ht_tensor *dH, const int32_t *ids, float scale, int32_t accumulate, ht_tensor *d_table);
+
+/* How a head's weights lie: [d x C], as a layer's W, or [C x d], as a table whose
+ * rows are the classes' (the one that ht_embed_fwd reads, say).  Their row pitch
+ * may be any number of floats from the columns on. */
+enum { HT_W_IN_OUT = 0, HT_W_OUT_IN = 1 };
+enum { HT_REDUCE_MEAN = 0, HT_REDUCE_SUM = 1 };
+enum { HT_HEAD_MAX_WIDTH = 65536, HT_HEAD_MAX_CLASSES = 1 << 24 };
+typedef struct {
+  int32_t d, n_classes;
+  int32_t w_form;        /* HT_W_*                                                   */
+  int32_t reduction;     /* HT_REDUCE_MEAN: N = labelled rows; HT_REDUCE_SUM: N = 1  */
+  int32_t accumulate_dW; /* 1: dW is added to what is there                          */
+  int32_t reserved;
+} ht_head_desc;
+
+/* Softmax cross entropy of a linear layer over n_classes, and its gradients:
+ *   x_v = H_v W ;  l_v = log sum_c exp(x_vc) - x_v,labels[v] ;  loss = sum u_v l_v / N
+ * over the rows with a label (labels[v] >= 0; the others cost nothing but their
+ * label), u = row_weight (device, nullable: 1).  The logits are not kept: scratch
+ * memory is 8 bytes a weight, and up to some 5 GiB for pieces of rows and classes.
+ * loss: device float.  row_loss, row_lse (device [V], nullable): l_v, and log sum
+ * exp; 0 without a label.  dH [V x d], dW (as W; both nullable) are the gradients
+ * of loss: dH is overwritten, 0 in rows without a label, dW overwritten or, with
+ * accumulate_dW, added to.  With no labelled row the loss and the gradients are 0.
+ * A label that is not below n_classes makes its row's loss NaN.  Products have
+ * fp32 precision; where H or W are not finite, what they reach is NaN. */
+int ht_head_loss(ht_ctx *ctx, const ht_head_desc *desc, const ht_tensor *H, const ht_tensor *W, const int32_t *labels,
+                 const float *row_weight, float *loss, float *row_loss, float *row_lse, ht_tensor *dH, ht_tensor *dW);
+
+enum { HT_DISTILL_MAX_K = 256 };
+typedef struct {
+  int32_t n_classes;
+  int32_t k;           /* a row's entries of the teacher, 1 .. HT_DISTILL_MAX_K       */
+  int32_t reduction;   /* HT_REDUCE_MEAN: N = rows with a teacher; HT_REDUCE_SUM: N = 1 */
+  float temperature;   /* T > 0                                                       */
+} ht_distill_desc;
+
+/* Distillation from a teacher's top logits.  A row's entries are top_ids[v*k ..]
+ * and top_logits[v*k ..] (device, [V x k] dense); those with an id < 0 or a logit
+ * of -inf are not there.  With q = softmax of the entries' logits / T among
+ * themselves and p = softmax(logits_v / T) over all classes,
+ *   l_v = T^2 sum_k q_k (log q_k - log p_id(k)) ;  loss = sum u_v l_v / N
+ * over rows with entries; others have l_v = 0 and no gradient.  dlogits (nullable,
+ * may be logits itself) = u_v T (p_c - sum of q_k with id(k) = c) / N.  An id may
+ * occur more than once.  A logit of -inf has p = 0; a row of nothing else has
+ * p = 0 in all of them.  A term with q_k = 0 is 0, one with p = 0 < q_k is +inf.
+ * An id that is not below n_classes makes its row's loss NaN and has no gradient.
+ * loss: device float; row_loss: device [V], nullable; row_weight u: device,
+ * nullable. */
+int ht_distill_loss(ht_ctx *ctx, const ht_distill_desc *desc, const ht_tensor *logits, const int32_t *top_ids,
+                    const float *top_logits, const float *row_weight, float *loss, float *row_loss, ht_tensor *dlogits);
+
 /* -------------------------------------------------------------------- epoch */
 
 /* HT_INTER_AUTO picks per the byte budget; MASK keeps h^{l+1} in HBM and reads

@@ -30,6 +30,10 @@ HT_RES_AUTO, HT_RES_HBM, HT_RES_HOST = 0, 1, 2
 HT_STATS_ALL, HT_STATS_AGG_FWD = 0, 1
 HT_INTER_AUTO, HT_INTER_MASK, HT_INTER_HYBRID, HT_INTER_RECOMPUTE = 0, 1, 2, 3
 HT_BUF_H, HT_BUF_A, HT_BUF_GH, HT_BUF_DW = 0, 1, 2, 3
+HT_W_IN_OUT, HT_W_OUT_IN = 0, 1
+HT_REDUCE_MEAN, HT_REDUCE_SUM = 0, 1
+HT_HEAD_MAX_WIDTH, HT_HEAD_MAX_CLASSES = 65536, 1 << 24
+HT_DISTILL_MAX_K = 256
 HT_MAX_LAYERS = 8
 
 
@@ -110,10 +114,20 @@ class ht_plan_opts(C.Structure):
                 ("reserved", C.c_int32)]
 
 
+class ht_head_desc(C.Structure):
+    _fields_ = [("d", C.c_int32), ("n_classes", C.c_int32), ("w_form", C.c_int32), ("reduction", C.c_int32),
+                ("accumulate_dW", C.c_int32), ("reserved", C.c_int32)]
+
+
+class ht_distill_desc(C.Structure):
+    _fields_ = [("n_classes", C.c_int32), ("k", C.c_int32), ("reduction", C.c_int32), ("temperature", C.c_float)]
+
+
 EXPORTS = ["ht_ctx_create", "ht_ctx_destroy", "ht_sync", "ht_ctx_set_hbm_budget", "ht_ctx_graph_launches", "ht_tensor_zero", "ht_strerror", "ht_last_error",
            "ht_partition", "ht_graph_destroy", "ht_graph_info_get", "ht_graph_chunk_info", "ht_graph_export_chunk",
            "ht_graph_export_csc", "ht_graph_chunk_order", "ht_graph_reorganize", "ht_layer_fwd", "ht_layer_fwd_static", "ht_layer_bwd", "ht_epoch", "ht_epoch_buffer", "ht_tensor_to_host", "ht_memory_model",
-           "ht_chunk_rows_model", "ht_gat_layer_fwd", "ht_gat_layer_bwd", "ht_gat_epoch", "ht_comm_cost_model"]
+           "ht_chunk_rows_model", "ht_gat_layer_fwd", "ht_gat_layer_bwd", "ht_gat_epoch", "ht_comm_cost_model",
+           "ht_embed_fwd", "ht_embed_bwd", "ht_head_loss", "ht_distill_loss"]
 
 _lib = None
 
@@ -176,6 +190,12 @@ def load():
                                      C.POINTER(ht_tensor), C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(ht_stats)]
     lib.ht_gat_epoch.argtypes = [C.c_void_p, C.c_void_p, C.POINTER(ht_gat_model), C.POINTER(ht_tensor), C.c_void_p,
                                  C.POINTER(C.c_float), C.POINTER(ht_stats)]
+    lib.ht_embed_fwd.argtypes = [C.c_void_p, C.POINTER(ht_tensor), C.c_void_p, C.c_float, C.POINTER(ht_tensor)]
+    lib.ht_embed_bwd.argtypes = [C.c_void_p, C.POINTER(ht_tensor), C.c_void_p, C.c_float, C.c_int32, C.POINTER(ht_tensor)]
+    lib.ht_head_loss.argtypes = [C.c_void_p, C.POINTER(ht_head_desc), C.POINTER(ht_tensor), C.POINTER(ht_tensor), C.c_void_p,
+                                 C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(ht_tensor), C.POINTER(ht_tensor)]
+    lib.ht_distill_loss.argtypes = [C.c_void_p, C.POINTER(ht_distill_desc), C.POINTER(ht_tensor), C.c_void_p, C.c_void_p,
+                                    C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(ht_tensor)]
     _lib = lib
     return lib
 
@@ -427,6 +447,67 @@ def ht_gat_epoch(ctx, g, dims: Sequence[int], Ws: List[torch.Tensor], a_dst: Lis
     _check(load().ht_gat_epoch(ctx, g, C.byref(model), C.byref(x), C.c_void_p(labels.data_ptr()), C.byref(loss),
                                C.byref(st) if st is not None else None), ctx)
     return loss.value, st
+
+
+# ------------------------------------------------- models over ids: their ends
+
+def _dev(t: Optional[torch.Tensor], dtype, shape, name: str):
+    """Address of a dense device tensor of this type and shape (None: null)."""
+    if t is None:
+        return None
+    assert t.is_cuda and t.dtype == dtype and t.is_contiguous() and tuple(t.shape) == tuple(shape), f"{name}: {dtype} {tuple(shape)} on the GPU"
+    return C.c_void_p(t.data_ptr())
+
+
+def _ref(t: Optional[torch.Tensor], cols: int):
+    return None if t is None else C.byref(tensor_view(t, cols))
+
+
+def ht_embed_fwd(ctx, d: int, table: torch.Tensor, ids: torch.Tensor, H: torch.Tensor, scale: float = 1.0, sync: bool = True):
+    """H[i] = scale * table[ids[i]]; sync=False leaves the order with work on other streams than the context's to the caller."""
+    ids_p = _dev(ids, torch.int32, (H.shape[0],), "ids")
+    if sync:
+        torch.cuda.synchronize()
+    _check(load().ht_embed_fwd(ctx, _ref(table, d), ids_p, scale, _ref(H, d)), ctx)
+
+
+def ht_embed_bwd(ctx, d: int, dH: torch.Tensor, ids: torch.Tensor, d_table: torch.Tensor, scale: float = 1.0,
+                 accumulate: bool = False, sync: bool = True):
+    """d_table[t] (+)= scale * sum of dH[i] over ids[i] == t."""
+    ids_p = _dev(ids, torch.int32, (dH.shape[0],), "ids")
+    if sync:
+        torch.cuda.synchronize()
+    _check(load().ht_embed_bwd(ctx, _ref(dH, d), ids_p, scale, int(accumulate), _ref(d_table, d)), ctx)
+
+
+def ht_head_loss(ctx, d: int, n_classes: int, H: torch.Tensor, W: torch.Tensor, labels: torch.Tensor, loss: torch.Tensor,
+                 row_weight: Optional[torch.Tensor] = None, row_loss: Optional[torch.Tensor] = None,
+                 row_lse: Optional[torch.Tensor] = None, dH: Optional[torch.Tensor] = None, dW: Optional[torch.Tensor] = None,
+                 w_form: int = HT_W_IN_OUT, reduction: int = HT_REDUCE_MEAN, accumulate_dW: bool = False, sync: bool = True):
+    """Softmax cross entropy of the logits H W and its gradients, without the logits; loss: device tensor of one float."""
+    V, cols = H.shape[0], n_classes if w_form == HT_W_IN_OUT else d
+    desc = ht_head_desc(d, n_classes, w_form, reduction, int(accumulate_dW), 0)
+    args = [_dev(labels, torch.int32, (V,), "labels"), _dev(row_weight, torch.float32, (V,), "row_weight"),
+            _dev(loss, torch.float32, (1,), "loss"), _dev(row_loss, torch.float32, (V,), "row_loss"),
+            _dev(row_lse, torch.float32, (V,), "row_lse")]
+    if sync:
+        torch.cuda.synchronize()
+    _check(load().ht_head_loss(ctx, C.byref(desc), _ref(H, d), _ref(W, cols), *args, _ref(dH, d), _ref(dW, cols)), ctx)
+
+
+def ht_distill_loss(ctx, n_classes: int, logits: torch.Tensor, top_ids: torch.Tensor, top_logits: torch.Tensor, loss: torch.Tensor,
+                    temperature: float = 1.0, row_weight: Optional[torch.Tensor] = None, row_loss: Optional[torch.Tensor] = None,
+                    dlogits: Optional[torch.Tensor] = None, reduction: int = HT_REDUCE_MEAN, sync: bool = True):
+    """Distillation from a teacher's top logits (top_ids, top_logits: [V x k]); loss: device tensor of one float."""
+    V = logits.shape[0]
+    k = top_ids.shape[1]
+    desc = ht_distill_desc(n_classes, k, reduction, temperature)
+    args = [_dev(top_ids, torch.int32, (V, k), "top_ids"), _dev(top_logits, torch.float32, (V, k), "top_logits"),
+            _dev(row_weight, torch.float32, (V,), "row_weight"), _dev(loss, torch.float32, (1,), "loss"),
+            _dev(row_loss, torch.float32, (V,), "row_loss")]
+    if sync:
+        torch.cuda.synchronize()
+    _check(load().ht_distill_loss(ctx, C.byref(desc), _ref(logits, n_classes), *args, _ref(dlogits, n_classes)), ctx)
 
 
 # -------------------------------------------------------------------- epoch

@@ -234,7 +234,8 @@ int ht_scratch(ht_ctx* ctx, int slot, size_t bytes, void** out) {
     if (ctx->scratch[slot]) {
       if (slot == HT_S_TNPART) HT_TRY(ht_flush_products(ctx, ctx->stream));   // (sums that were left to the end of the epoch are in there)
       HT_HIP(ctx, hipStreamSynchronize(ctx->stream));
-      dev_free(ctx, ctx->scratch[slot], ctx->scratch_bytes[slot], !ctx->recorded);
+      if (ht_slot_stays(ctx, slot)) ctx->retired.emplace_back(ctx->scratch[slot], ctx->scratch_bytes[slot]);
+      else dev_free(ctx, ctx->scratch[slot], ctx->scratch_bytes[slot], !ctx->recorded);
       ctx->scratch[slot] = nullptr;
       ctx->scratch_bytes[slot] = 0;
     }
@@ -249,7 +250,7 @@ int ht_scratch(ht_ctx* ctx, int slot, size_t bytes, void** out) {
 }
 
 int ht_scratch_release(ht_ctx* ctx, int slot) {
-  if (ctx->static_mode || !ctx->scratch[slot]) return HT_OK;
+  if (ctx->static_mode || !ctx->scratch[slot] || ht_slot_stays(ctx, slot)) return HT_OK;
   if (slot == HT_S_TNPART) HT_TRY(ht_flush_products(ctx, ctx->stream));
   HT_HIP(ctx, hipStreamSynchronize(ctx->stream));
   dev_free(ctx, ctx->scratch[slot], ctx->scratch_bytes[slot], !ctx->recorded);
@@ -257,6 +258,44 @@ int ht_scratch_release(ht_ctx* ctx, int slot) {
   ctx->scratch_bytes[slot] = 0;
   ++ctx->scratch_gen;
   return HT_OK;
+}
+
+int OpsBlock::take(ht_ctx* ctx, size_t rsort, size_t scan) {
+  const std::pair<int, size_t> want[3] = {{HT_S_OPS, bytes}, {HT_S_RSORT, rsort}, {HT_S_SCAN, scan}};
+  for (const auto& w : want)
+    if (w.second > ctx->scratch_bytes[w.first] && ht_caller_captures(ctx))
+      return ht_set_err(ctx, HT_ESTATE, "a recorded pass needs %zu bytes of scratch memory and finds %zu: make the call once before it is recorded", w.second,
+                        ctx->scratch_bytes[w.first]);
+  for (const auto& w : want) {
+    void* q = nullptr;
+    if (w.second > 0) HT_TRY(ht_scratch(ctx, w.first, w.second, &q));
+    if (w.first == HT_S_OPS) p = (char*)q;
+  }
+  return HT_OK;
+}
+
+int ht_check_rows(ht_ctx* ctx, const ht_tensor* t, int64_t rows, int32_t cols, const char* name) {
+  HT_TRY(ht_check_weights(ctx, t, rows, cols, name));
+  if (t->ld & 3) return ht_set_err(ctx, HT_ESHAPE, "%s: row pitch %lld must be a multiple of 4", name, (long long)t->ld);
+  if ((uintptr_t)t->ptr & 15) return ht_set_err(ctx, HT_ESHAPE, "%s: base pointer must be 16-byte aligned", name);
+  return HT_OK;
+}
+
+int ht_check_weights(ht_ctx* ctx, const ht_tensor* t, int64_t rows, int32_t cols, const char* name) {
+  if (rows < 0 || rows > INT32_MAX) return ht_set_err(ctx, HT_ESHAPE, "%s: %lld rows", name, (long long)rows);
+  if (!t->ptr && t->rows > 0) return ht_set_err(ctx, HT_EINVAL, "%s: null tensor", name);
+  if (t->rows != rows || t->cols != cols)
+    return ht_set_err(ctx, HT_ESHAPE, "%s: shape [%lld x %d], expected [%lld x %d]", name, (long long)t->rows, t->cols, (long long)rows, cols);
+  if (t->ld < t->cols) return ht_set_err(ctx, HT_ESHAPE, "%s: row pitch %lld below the %d columns", name, (long long)t->ld, t->cols);
+  if (t->loc != HT_LOC_DEVICE) return ht_set_err(ctx, HT_ESHAPE, "%s: must be in HBM", name);
+  if ((uintptr_t)t->ptr & 3) return ht_set_err(ctx, HT_ESHAPE, "%s: base pointer must be 4-byte aligned", name);
+  return HT_OK;
+}
+
+bool ht_overlap(const ht_tensor* a, const ht_tensor* b) {
+  if (a->rows <= 0 || b->rows <= 0) return false;
+  const float *a1 = a->ptr + (a->rows - 1) * a->ld + a->cols, *b1 = b->ptr + (b->rows - 1) * b->ld + b->cols;
+  return a->ptr < b1 && b->ptr < a1;
 }
 
 int64_t ht_device_free(ht_ctx* ctx) {
@@ -483,6 +522,7 @@ int ht_ctx_destroy(ht_ctx* ctx) {
   for (ht_graph* g : ctx->graphs) g->ctx = nullptr;
   for (int i = 0; i < HT_N_SCRATCH; ++i)
     if (ctx->scratch[i]) dev_free(ctx, ctx->scratch[i], ctx->scratch_bytes[i], false);
+  for (const auto& r : ctx->retired) dev_free(ctx, r.first, r.second, false);
   ht_kept_release(ctx);
   for (int i = 0; i < HT_N_HS; ++i)
     if (ctx->hscratch[i]) (void)hipHostFree(ctx->hscratch[i]);

@@ -1,0 +1,750 @@
+// Softmax cross entropy of a linear head over many classes, with its gradients, the logits never kept:
+//   x_vc = h_v . w_c ;  lse_v = log sum_c exp(x_vc) ;  loss = sum_v u_v (lse_v - x_vy) / N
+//   dx_vc = (u_v / N) (exp(x_vc - lse_v) - [c = y_v]) ;  dH = dx W^T ;  dW = H^T dx
+// Labelled rows are first listed, and only they are computed with.  Rows go in pieces: a pass over all classes gives lse; then, class piece
+// by class piece, the logits are computed again and leave as exp(x - lse) - [c = y], once grouped along classes (for dH) and once
+// along rows (for dW).  Four products of 2 n d C flops, the fewest possible without keeping n x C numbers.
+//
+// All of them are k_split_nt's: fp32 products on the fp16 matrix cores.  A value is split into two fp16 numbers, x = x0 + x1 (x0 its
+// rounding, x1 the rounding of what is left: |x - x0 - x1| <= 2^-22 |x|), after each row of an operand was scaled by a power of two
+// that brings its largest value to [2^14, 2^15); x0 y0 + x0 y1 + x1 y0 are added in fp32.  What is left out is at most 3 x 2^-22 of a
+// product, typically (the roundings are independent) 2^-24 of it, what fp32 loses in rounding it; values below 2^-17 of their row's
+// largest keep fewer bits, down to 2^-39 of it.  Three fp16 steps take 96 clocks where an fp32 product takes 512.
+#include <algorithm>
+
+#include "ht_internal.h"
+
+namespace {
+
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef float v2f __attribute__((ext_vector_type(2)));
+
+// Operands lie in fragments, what a matrix instruction reads of them: 32 rows x 16 values of the reduction of one plane (x0 or x1), 1 KiB.
+// Lane l + 32 h holds row l and the values 8 (t / 4) + 4 h + t % 4, t = 0 .. 7: the order in which a lane of a product's result holds
+// its rows, so that results become operands without leaving their lanes (any order will do that both operands have).  Fragment (row block,
+// step, plane) is number (block * KS + step) * 2 + plane.
+constexpr int FRAG = 512;
+constexpr int TM = 256, TN = 128;      // tile of a block: rows of A x rows of B
+constexpr float LOG2E = 1.44269504088896340736f;
+constexpr int P_EXP = 15;              // gradients of logits are held times 2^15
+constexpr size_t HEAD_BYTES = (size_t)4 << 30, HEAD_LEAN = (size_t)64 << 20;   // of what a piece's rows take
+constexpr int64_t HEAD_CLASSES = 8192;             // of a piece
+
+__host__ __device__ constexpr int64_t up_to(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
+
+// exp(x - m).  (The difference first: products with log2 e of logits of 10^9 are rounded by more than 1.)
+__device__ __forceinline__ float exp_less(float x, float m) { return __builtin_amdgcn_exp2f((x - m) * LOG2E); }
+
+// The power of two that brings a row whose largest absolute value has these bits to [2^14, 2^15), and its inverse.
+__device__ __forceinline__ uint32_t scale_exp(uint32_t bits) {
+  if (bits == 0 || bits >= 0x7f800000u) return 127;
+  const uint32_t e = 268 - (bits >> 23);
+  return e > 253 ? 253 : e;
+}
+__device__ __forceinline__ float scale_of(uint32_t bits) { return __uint_as_float(scale_exp(bits) << 23); }
+__device__ __forceinline__ float unscale_of(uint32_t bits) { return __uint_as_float((254 - scale_exp(bits)) << 23); }
+
+// ---------------------------------------------------------------- labelled rows
+
+constexpr int ROW_BLOCKS = 4096;
+
+__global__ void __launch_bounds__(256) k_head_count(const int32_t* __restrict__ labels, int64_t V, int64_t rpb, int32_t* __restrict__ cnt) {
+  __shared__ int sh[4];
+  int n = 0;
+  const int64_t v0 = (int64_t)blockIdx.x * rpb, v1 = v0 + rpb < V ? v0 + rpb : V;
+  for (int64_t v = v0 + threadIdx.x; v < v1; v += 256) n += labels[v] >= 0;
+  for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = n;
+  __syncthreads();
+  if (threadIdx.x == 0) cnt[blockIdx.x] = sh[0] + sh[1] + sh[2] + sh[3];
+}
+
+// idx, lab: the labelled rows in order, and their labels; *total: how many.  Rows without a label get their zeros here.
+__global__ void __launch_bounds__(256) k_head_place(const int32_t* __restrict__ labels, int64_t V, int64_t rpb, const int32_t* __restrict__ cnt,
+                                                    int32_t* __restrict__ idx, int32_t* __restrict__ lab, int64_t* __restrict__ total,
+                                                    float* __restrict__ row_loss, float* __restrict__ row_lse, float* __restrict__ dH, int64_t ld, int d) {
+  __shared__ int64_t sh64[4];
+  __shared__ int sh[4];
+  __shared__ uint64_t have[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int64_t at = 0;
+  for (int b = threadIdx.x; b < (int)blockIdx.x; b += 256) at += cnt[b];
+  for (int o = 32; o > 0; o >>= 1) at += __shfl_xor(at, o, 64);
+  if (lane == 0) sh64[wave] = at;
+  __syncthreads();
+  at = sh64[0] + sh64[1] + sh64[2] + sh64[3];
+  const int64_t v0 = (int64_t)blockIdx.x * rpb, v1 = v0 + rpb < V ? v0 + rpb : V;
+  for (int64_t w0 = v0; w0 < v1; w0 += 256) {
+    const int64_t v = w0 + threadIdx.x;
+    const int32_t y = v < v1 ? labels[v] : -1;
+    const uint64_t mask = __ballot(y >= 0);
+    __syncthreads();
+    if (lane == 0) sh[wave] = __popcll(mask), have[wave] = mask;
+    __syncthreads();
+    int before = __popcll(mask & ((1ull << lane) - 1)), all = 0;
+    for (int w = 0; w < 4; ++w) before += w < wave ? sh[w] : 0, all += sh[w];
+    if (y >= 0) {
+      idx[at + before] = (int32_t)v;
+      lab[at + before] = y;
+    } else if (v < v1) {
+      if (row_loss) row_loss[v] = 0.f;
+      if (row_lse) row_lse[v] = 0.f;
+    }
+    at += all;
+    if (dH) {
+      const int64_t rows = v1 - w0 < 256 ? v1 - w0 : 256;
+      for (int r = wave; r < rows; r += 4)
+        if (!((have[r >> 6] >> (r & 63)) & 1))
+          for (int c = lane * 4; c < d; c += 256) *reinterpret_cast<float4*>(dH + (w0 + r) * ld + c) = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+  }
+  if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) *total = at;
+}
+
+// Rows of a piece: what is left of the list from r0 on, at most `most`.
+__device__ __forceinline__ int64_t piece_rows(const int64_t* total, int64_t r0, int64_t most) {
+  const int64_t left = *total - r0;
+  return left < 0 ? 0 : left < most ? left : most;
+}
+
+// ---------------------------------------------------------------- operands
+
+// A matrix [rows x cols], pitch ld, its rows as they are or those that idx names, each times weight[idx[r]].
+struct Source {
+  const float* p;
+  int64_t ld, rows, cols;
+  const int32_t* idx;            // null: all rows, as they are
+  const float* weight;           // (with idx; null: 1)
+  const int64_t* total;          // with idx: rows = piece_rows(total, r0, rows)
+  int64_t r0;
+  __device__ __forceinline__ int64_t n() const { return idx ? piece_rows(total, r0, rows) : rows; }
+  __device__ __forceinline__ int64_t row(int64_t r) const { return idx ? (int64_t)idx[r0 + r] : r; }
+};
+
+// Largest absolute values of rows, and of columns (of weighted rows), as bits, into arrays that hold zeros.  (Maxima do not depend on their order.)
+constexpr int AMAX_COLS = 1024;
+__global__ void __launch_bounds__(256) k_amax(Source s, uint32_t* __restrict__ rmax, uint32_t* __restrict__ cmax) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t n = s.n(), r0 = (int64_t)blockIdx.x * 64 + wave * 16, c0 = (int64_t)blockIdx.y * AMAX_COLS;
+  if ((int64_t)blockIdx.x * 64 >= n) return;
+  const float* p[16];
+  float w[16];
+  uint32_t rm[16];
+#pragma unroll
+  for (int q = 0; q < 16; ++q) {
+    const int64_t r = r0 + q < n ? r0 + q : n - 1, v = s.row(r);
+    p[q] = s.p + v * s.ld;
+    w[q] = s.weight ? s.weight[v] : 1.f;
+    rm[q] = 0;
+  }
+  const int64_t c1 = c0 + AMAX_COLS < s.cols ? c0 + AMAX_COLS : s.cols;
+  for (int64_t c = c0 + lane; c < c1; c += 64) {
+    uint32_t cm = 0;
+#pragma unroll
+    for (int q = 0; q < 16; ++q) {
+      const float x = p[q][c];
+      rm[q] = max(rm[q], __float_as_uint(fabsf(x)));
+      cm = max(cm, __float_as_uint(fabsf(x * w[q])));
+    }
+    if (cmax) atomicMax(cmax + c, cm);
+  }
+#pragma unroll
+  for (int q = 0; q < 16; ++q) {
+    uint32_t m = rm[q];
+    for (int o = 32; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
+    if (lane == 0 && r0 + q < n) atomicMax(rmax + r0 + q, m);
+  }
+}
+
+__device__ __forceinline__ void split2(float x, _Float16* hi, _Float16* lo) {
+  *hi = (_Float16)x;
+  *lo = (_Float16)(x - (float)*hi);
+}
+
+// Fragments of the matrix by rows (reduction along columns: KS steps) and by columns (reduction along rows, weighted: KS_t steps), zeros behind
+// the last row and column, a 64 x 64 tile a block.
+__global__ void __launch_bounds__(256) k_pack(Source s, const uint32_t* __restrict__ rmax, const uint32_t* __restrict__ cmax,
+                                              _Float16* __restrict__ R, int64_t KS, _Float16* __restrict__ T, int64_t KS_t, int64_t row_tile, unsigned col_tiles) {
+  __shared__ float sh[64][65];
+  __shared__ float wt[64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, half = lane >> 5;
+  const int64_t n = s.n(), r0 = (int64_t)(blockIdx.x / col_tiles) * 64, c0 = (int64_t)(blockIdx.x % col_tiles) * 64;
+  if (r0 >= up_to(n, row_tile)) return;
+#pragma unroll
+  for (int q = 0; q < 16; ++q) {
+    const int r = wave * 16 + q;
+    float x = 0.f, w = 0.f;
+    if (r0 + r < n) {
+      const int64_t v = s.row(r0 + r);
+      if (c0 + lane < s.cols) x = s.p[v * s.ld + c0 + lane];
+      w = s.weight ? s.weight[v] : 1.f;
+    }
+    sh[r][lane] = x;
+    if (lane == 0) wt[r] = w;
+  }
+  __syncthreads();
+  auto put = [&](_Float16* to, int64_t frag, const float* x) {
+    v8h hi, lo;
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      _Float16 a, b;
+      split2(x[t], &a, &b);
+      hi[t] = a;
+      lo[t] = b;
+    }
+    *reinterpret_cast<v8h*>(to + frag * 2 * FRAG + lane * 8) = hi;
+    *reinterpret_cast<v8h*>(to + frag * 2 * FRAG + FRAG + lane * 8) = lo;
+  };
+  const int b = wave >> 1;                        // row block of the tile; a wave takes two of its four steps
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int ks = (wave & 1) * 2 + u, k = ks * 16 + half * 4;
+    float x[8];
+    if (R && c0 / 16 + ks < KS) {
+      const int r = b * 32 + l32;
+      const float f = scale_of(r0 + r < n ? rmax[r0 + r] : 0u);
+#pragma unroll
+      for (int t = 0; t < 8; ++t) x[t] = sh[r][k + (t >> 2) * 8 + (t & 3)] * f;
+      put(R, (r0 / 32 + b) * KS + c0 / 16 + ks, x);
+    }
+    if (T && r0 / 16 + ks < KS_t) {
+      const int c = b * 32 + l32;
+      const float f = scale_of(c0 + c < s.cols ? cmax[c0 + c] : 0u);
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        const int r = k + (t >> 2) * 8 + (t & 3);
+        x[t] = sh[r][c] * wt[r] * f;
+      }
+      put(T, (c0 / 32 + b) * KS_t + r0 / 16 + ks, x);
+    }
+  }
+}
+
+// ---------------------------------------------------------------- products
+
+enum { LOSS, GRAD, SUMS };
+struct NtArgs {
+  const _Float16 *A, *B;          // fragments; row blocks KSA, KSB steps apart
+  int64_t KSA, KSB;
+  int64_t ksb0;                   // first step of B
+  int64_t mt, nt;                 // tiles
+  int64_t steps;                  // steps of the reduction (a multiple of 2); < 0: up to the piece's rows
+  int splits;                     // parts of it, each with sums of its own
+  // the piece
+  const int64_t* total;
+  int64_t r0, most;
+  int rows_are;                   // which operand's rows are the piece's: 0 none, 1 A's, 2 B's
+  // LOSS, GRAD: A's rows are classes from c0 on, B's rows of the piece
+  int64_t c0, C;
+  const uint32_t *cmax, *hmax;    // their largest values
+  const int32_t* lab;
+  float2* part;                   // LOSS: [class tile][most]: largest logit, sum of exponentials less it
+  float* xlab;                    // LOSS: the label's logit
+  const float* lse;               // GRAD
+  _Float16 *P, *PT;               // GRAD: fragments by rows (KSP steps), by classes (KST steps)
+  int64_t KSP, KST;
+  // SUMS
+  float* out;                     // [split][out_m x out_n]
+  int64_t out_m, out_n;
+  int add;
+};
+
+// What a wave's lanes have written to LDS is there for its other lanes, and what they have read may be overwritten.
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
+constexpr int KT = 2;             // steps of a stage
+template <int EPI>
+__global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
+  constexpr int STAGE = TN / 32 * KT * 2 * FRAG;        // halfs
+  constexpr int TR_PITCH = 40;                          // dwords between classes in a transposed 32 x 32 tile
+  __shared__ __attribute__((aligned(16))) _Float16 Bs[2 * STAGE];
+  static_assert(4 * 32 * TR_PITCH * 4 <= sizeof(Bs), "the waves' transposed tiles fit where B was");
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
+  // each XCD takes a contiguous part of the tiles, eight tiles of A over all of B after eight others
+  const int64_t tiles = a.mt * a.nt, per = (tiles + 7) / 8, t = (int64_t)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  if ((int64_t)(blockIdx.x >> 3) >= per || t >= tiles) return;
+  const int64_t g = t / (8 * a.nt), gm = a.mt - g * 8 < 8 ? a.mt - g * 8 : 8, q = t - g * 8 * a.nt;
+  const int64_t m0 = (g * 8 + q % gm) * TM, n0 = q / gm * TN;
+  const int64_t rows = piece_rows(a.total, a.r0, a.most);
+  if ((a.rows_are == 1 && m0 >= rows) || (a.rows_are == 2 && n0 >= rows)) return;
+  const int64_t all = a.steps >= 0 ? a.steps : up_to(rows, 16 * KT) / 16, stages = all / KT;
+  const int64_t s0 = stages * blockIdx.y / a.splits, s1 = stages * (blockIdx.y + 1) / a.splits;
+
+  v16f acc[2][4];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+
+  const _Float16* Ap[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) Ap[i] = a.A + (m0 / 32 + wave * 2 + i) * a.KSA * 2 * FRAG + lane * 8;
+  const _Float16* Bp = a.B + ((n0 / 32 + wave) * a.KSB + a.ksb0) * 2 * FRAG + lane * 8;     // a wave brings one of the four row blocks
+  v8h ra[2][2][2], rb[KT * 2];    // [step in turn][row block][plane]
+  auto fetch_a = [&](int64_t ks, int to) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int p = 0; p < 2; ++p) ra[to][i][p] = *reinterpret_cast<const v8h*>(Ap[i] + (ks * 2 + p) * FRAG);
+  };
+  auto fetch_b = [&](int64_t s) {
+#pragma unroll
+    for (int u = 0; u < KT * 2; ++u) rb[u] = *reinterpret_cast<const v8h*>(Bp + (s * KT * 2 + u) * FRAG);
+  };
+  auto stash_b = [&](int to) {
+#pragma unroll
+    for (int u = 0; u < KT * 2; ++u) *reinterpret_cast<v8h*>(Bs + to * STAGE + (wave * KT * 2 + u) * FRAG + lane * 8) = rb[u];
+  };
+  if (s0 < s1) {
+    fetch_b(s0);
+    fetch_a(s0 * KT, 0);
+    stash_b(0);
+    __syncthreads();
+  }
+  for (int64_t s = s0; s < s1; ++s) {
+    const int cur = (int)(s - s0) & 1;
+    if (s + 1 < s1) fetch_b(s + 1);
+#pragma unroll
+    for (int u = 0; u < KT; ++u) {
+      const int64_t ks = s * KT + u, nx = ks + 1 < s1 * KT ? ks + 1 : ks;
+      fetch_a(nx, (u + 1) & 1);
+      const v8h (&x)[2][2] = ra[u & 1];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const _Float16* f = Bs + cur * STAGE + (j * KT * 2 + u * 2) * FRAG + lane * 8;
+        const v8h b0 = *reinterpret_cast<const v8h*>(f), b1 = *reinterpret_cast<const v8h*>(f + FRAG);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][1], b0, acc[i][j], 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][0], b1, acc[i][j], 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][0], b0, acc[i][j], 0, 0, 0);
+      }
+    }
+    if (s + 1 < s1) stash_b(cur ^ 1);
+    __syncthreads();
+  }
+
+  // lane l32 + 32 half of a 32 x 32 tile has column l32 and the rows 8 (e / 4) + 4 half + e % 4
+  const int64_t mw = m0 + wave * 64;
+  if constexpr (EPI == SUMS) {
+    float* out = a.out + (int64_t)blockIdx.y * a.out_m * a.out_n;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int64_t n = n0 + j * 32 + l32;
+      if (n >= a.out_n) continue;
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int64_t m = mw + i * 32 + (e >> 2) * 8 + half * 4 + (e & 3);
+          if (m >= a.out_m) continue;
+          float* o = out + m * a.out_n + n;
+          *o = a.add ? *o + acc[i][j][e] : acc[i][j][e];
+        }
+    }
+    return;
+  }
+  float cs[2][16];                 // what undoes the classes' scaling
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int64_t c = a.c0 + mw + i * 32 + (e >> 2) * 8 + half * 4 + (e & 3);
+      cs[i][e] = unscale_of(c < a.C ? a.cmax[c] : 0u);
+    }
+  const bool whole = a.c0 + mw + 64 <= a.C;
+  auto inside = [&](int i, int e) { return whole || a.c0 + mw + i * 32 + (e >> 2) * 8 + half * 4 + (e & 3) < a.C; };
+  if constexpr (EPI == LOSS) {
+    float2* red = reinterpret_cast<float2*>(Bs);      // [wave][column]
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int64_t v = n0 + j * 32 + l32;
+      const bool there = v < rows;
+      const float hs = unscale_of(there ? a.hmax[v] : 0u);
+      float m = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          acc[i][j][e] = inside(i, e) ? acc[i][j][e] * hs * cs[i][e] : -INFINITY;
+          m = fmaxf(m, acc[i][j][e]);
+        }
+      m = fmaxf(m, __shfl_xor(m, 32, 64));
+      float z = 0.f;
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) z += inside(i, e) ? exp_less(acc[i][j][e], m) : 0.f;
+      z += __shfl_xor(z, 32, 64);
+      if (half == 0) red[wave * TN + j * 32 + l32] = make_float2(m, z);
+      const int64_t off = there ? a.lab[a.r0 + v] - (a.c0 + mw) : -1;
+      const bool mine = off >= 0 && off < 64 && ((off >> 2) & 1) == half;
+      if (__ballot(mine)) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (mine && off == i * 32 + (e >> 2) * 8 + half * 4 + (e & 3)) a.xlab[v] = acc[i][j][e];
+      }
+    }
+    __syncthreads();
+    if (tid < TN && n0 + tid < rows) {
+      float m = -INFINITY, z = 0.f;
+      for (int w = 0; w < 4; ++w) m = fmaxf(m, red[w * TN + tid].x);
+      for (int w = 0; w < 4; ++w) {
+        const float2 p = red[w * TN + tid];
+        z += p.x == -INFINITY ? p.y : p.y * exp_less(p.x, m);
+      }
+      a.part[m0 / TM * a.most + n0 + tid] = make_float2(m, z);
+    }
+    return;
+  }
+  if constexpr (EPI == GRAD) {
+    uint32_t* tr = reinterpret_cast<uint32_t*>(Bs) + wave * 32 * TR_PITCH;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int64_t v = n0 + j * 32 + l32;
+      const bool there = v < rows;
+      const float hs = unscale_of(there ? a.hmax[v] : 0u);
+      const float lse = there ? a.lse[v] : 0.f;
+      const int64_t off = there ? a.lab[a.r0 + v] - (a.c0 + mw) : -1;
+      const bool mine = off >= 0 && off < 64 && ((off >> 2) & 1) == half;
+      const bool any = __ballot(mine);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float p[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          p[e] = __builtin_amdgcn_exp2f(fmaf(fmaf(acc[i][j][e] * hs, cs[i][e], -lse), LOG2E, P_EXP));
+          if (!there || !inside(i, e)) p[e] = 0.f;
+        }
+        if (any) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (mine && off == i * 32 + (e >> 2) * 8 + half * 4 + (e & 3)) p[e] -= (float)(1 << P_EXP);
+        }
+        uint32_t both[16];
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+          v8h hi, lo;
+#pragma unroll
+          for (int u = 0; u < 8; ++u) {
+            _Float16 x, y;
+            split2(p[ks * 8 + u], &x, &y);
+            hi[u] = x;
+            lo[u] = y;
+            both[ks * 8 + u] = (uint32_t)__builtin_bit_cast(uint16_t, x) | (uint32_t)__builtin_bit_cast(uint16_t, y) << 16;
+          }
+          _Float16* to = a.P + (((n0 / 32 + j) * a.KSP + (mw + i * 32) / 16 + ks) * 2) * FRAG + lane * 8;
+          *reinterpret_cast<v8h*>(to) = hi;
+          *reinterpret_cast<v8h*>(to + FRAG) = lo;
+        }
+        // the same 32 x 32 values with a class in each lane
+        wave_sync();
+#pragma unroll
+        for (int e = 0; e < 16; ++e) tr[((e >> 2) * 8 + half * 4 + (e & 3)) * TR_PITCH + l32] = both[e];
+        wave_sync();
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+          v8h hi, lo;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint4 x = *reinterpret_cast<const uint4*>(tr + l32 * TR_PITCH + ks * 16 + h * 8 + half * 4);
+            const uint32_t y[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              hi[h * 4 + u] = __builtin_bit_cast(_Float16, (uint16_t)y[u]);
+              lo[h * 4 + u] = __builtin_bit_cast(_Float16, (uint16_t)(y[u] >> 16));
+            }
+          }
+          _Float16* to = a.PT + (((mw / 32 + i) * a.KST + (n0 + j * 32) / 16 + ks) * 2) * FRAG + lane * 8;
+          *reinterpret_cast<v8h*>(to) = hi;
+          *reinterpret_cast<v8h*>(to + FRAG) = lo;
+        }
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------- what the products leave
+
+// Blocks of 64 rows, 16 parts of the class tiles each.  part_loss[block] = sum of its rows' weighted losses.
+__global__ void __launch_bounds__(1024) k_head_join(const float2* __restrict__ part, int64_t tiles, int64_t most, const int64_t* __restrict__ total, int64_t r0,
+                                                    const int32_t* __restrict__ idx, const int32_t* __restrict__ lab, int64_t C,
+                                                    const float* __restrict__ weight, const float* __restrict__ xlab, float* __restrict__ lse_of,
+                                                    float* __restrict__ row_loss, float* __restrict__ row_lse, double* __restrict__ part_loss) {
+  __shared__ float2 sh[16][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t rows = piece_rows(total, r0, most);
+  double mine = 0.0;
+  for (int64_t v0 = (int64_t)blockIdx.x * 64; v0 < rows; v0 += (int64_t)gridDim.x * 64) {
+    const int64_t v = v0 + lane;
+    float m = -INFINITY, z = 0.f;
+    if (v < rows)
+#pragma unroll 4
+      for (int64_t t = wave; t < tiles; t += 16) {
+        const float2 p = part[t * most + v];
+        const float n = fmaxf(m, p.x);
+        z = (m == -INFINITY ? 0.f : z * exp_less(m, n)) + (p.x == -INFINITY ? p.y : p.y * exp_less(p.x, n));
+        m = n;
+      }
+    sh[wave][lane] = make_float2(m, z);
+    __syncthreads();
+    if (wave == 0) {
+      m = -INFINITY;
+      for (int w = 0; w < 16; ++w) m = fmaxf(m, sh[w][lane].x);
+      z = 0.f;
+      for (int w = 0; w < 16; ++w) z += sh[w][lane].x == -INFINITY ? sh[w][lane].y : sh[w][lane].y * exp_less(sh[w][lane].x, m);
+      if (v < rows) {
+        const float lse = m + logf(z);
+        const float l = lab[r0 + v] < C ? lse - xlab[v] : NAN;
+        lse_of[v] = lse;
+        const int64_t at = idx[r0 + v];
+        if (row_loss) row_loss[at] = l;
+        if (row_lse) row_lse[at] = lse;
+        mine += weight ? (double)weight[at] * (double)l : (double)l;
+      }
+    }
+    __syncthreads();
+  }
+  if (wave != 0) return;
+  for (int o = 32; o > 0; o >>= 1) mine += __shfl_xor(mine, o, 64);
+  if (lane == 0) part_loss[blockIdx.x] = mine;
+}
+
+__global__ void __launch_bounds__(256) k_head_loss(const double* __restrict__ part, int64_t n, const int64_t* __restrict__ total, int mean, float* __restrict__ loss) {
+  __shared__ double sh[256];
+  double s = 0.0;
+  for (int64_t i = threadIdx.x; i < n; i += 256) s += part[i];
+  sh[threadIdx.x] = s;
+  __syncthreads();
+  for (int o = 128; o > 0; o >>= 1) {
+    if ((int)threadIdx.x < o) sh[threadIdx.x] += sh[threadIdx.x + o];
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) *loss = *total > 0 ? (float)(sh[0] / (mean ? (double)*total : 1.0)) : 0.f;
+}
+
+__device__ __forceinline__ float inv_count(const int64_t* total, int mean) { return mean ? 1.f / (float)(*total > 0 ? *total : 1) : 1.f; }
+
+// dH rows of a piece: the splits' sums, scaled
+__global__ void __launch_bounds__(256) k_head_dh(const float* __restrict__ sums, int splits, int64_t most, int64_t pitch, const int64_t* __restrict__ total,
+                                                 int64_t r0, const int32_t* __restrict__ idx, const float* __restrict__ weight, int mean,
+                                                 const uint32_t* __restrict__ wmax, float* __restrict__ dH, int64_t ld, int d) {
+  const int64_t rows = piece_rows(total, r0, most);
+  const int nv = (d + 3) / 4;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, v = i / nv;
+  if (v >= rows) return;
+  const int c = (int)(i % nv) * 4;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int k = 0; k < splits; ++k) {
+    const float4 x = *reinterpret_cast<const float4*>(sums + ((int64_t)k * most + v) * pitch + c);
+    s.x += x.x, s.y += x.y, s.z += x.z, s.w += x.w;
+  }
+  const int64_t at = idx[r0 + v];
+  const float f = inv_count(total, mean) * (weight ? weight[at] : 1.f) * (1.f / (1 << P_EXP));
+  auto out = [&](float x, int k) { return c + k < d ? x * unscale_of(wmax[c + k]) * f : 0.f; };
+  *reinterpret_cast<float4*>(dH + at * ld + c) = make_float4(out(s.x, 0), out(s.y, 1), out(s.z, 2), out(s.w, 3));
+}
+
+// dW's part [rows x cols] at out (pitch ld): the splits' sums (pitch cols_p, rows_p rows each), scaled by what undoes hmax along rows or columns
+__global__ void __launch_bounds__(256) k_head_dw(const float* __restrict__ sums, int splits, int64_t rows_p, int64_t cols_p, int64_t rows, int64_t cols,
+                                                 const uint32_t* __restrict__ hmax, int along_rows, const int64_t* __restrict__ total, int64_t r0, int mean, int add,
+                                                 float* __restrict__ out, int64_t ld) {
+  if (r0 > 0 && *total <= r0) return;             // (nothing to add)
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, r = i / cols, c = i - r * cols;
+  if (r >= rows) return;
+  float s = 0.f;
+  for (int k = 0; k < splits; ++k) s += sums[((int64_t)k * rows_p + r) * cols_p + c];
+  s *= unscale_of(hmax[along_rows ? r : c]) * (1.f / (1 << P_EXP)) * inv_count(total, mean);
+  float* o = out + r * ld + c;
+  *o = add ? *o + s : s;
+}
+
+struct HeadPlan {
+  int64_t Cp, Rp, KSd;               // classes and rows of a piece, steps of a reduction over d
+  int64_t Cpad, dpad;
+  int splits_h, splits_w;
+};
+
+HeadPlan head_plan(int64_t V, int64_t d, int64_t C, bool in_out, size_t bytes) {
+  HeadPlan p{};
+  p.KSd = up_to(d, 16 * KT) / 16;
+  p.Cpad = up_to(C, TM);
+  p.dpad = up_to(d, TM);
+  p.Cp = std::min<int64_t>(p.Cpad, HEAD_CLASSES);
+  // a row takes 4 bytes a value of its own, by rows and by features, and of its gradient, 8 a class of the piece, and 8 a tile of classes
+  p.Rp = (int64_t)(bytes / (size_t)(8 * p.Cp + 12 * p.dpad + 8 * (p.Cpad / TM))) / TM * TM;
+  p.Rp = std::max<int64_t>(TM, std::min(p.Rp, up_to(V, TM)));
+  auto splits = [](int64_t tiles, int64_t steps) {      // parts of a reduction: two blocks a CU, and 512 values each at least
+    return (int)std::max<int64_t>(1, std::min<int64_t>({512 / std::max<int64_t>(tiles, 1), steps / 32, 32}));
+  };
+  p.splits_h = splits(p.Rp / TM * (up_to(d, TN) / TN), p.Cp / 16);
+  p.splits_w = splits(in_out ? p.dpad / TM * (p.Cp / TN) : p.Cp / TM * (up_to(d, TN) / TN), p.Rp / 16);
+  return p;
+}
+
+int split_nt(ht_ctx* ctx, hipStream_t st, int epi, const NtArgs& a) {
+  const int64_t blocks = (a.mt * a.nt + 7) / 8 * 8;
+  if (blocks >= (1 << 24)) return ht_set_err(ctx, HT_ESHAPE, "head: %lld tiles in one product", (long long)blocks);
+  const dim3 grid((unsigned)blocks, (unsigned)(epi == SUMS ? a.splits : 1));
+  if (epi == LOSS) k_split_nt<LOSS><<<grid, 256, 0, st>>>(a);
+  else if (epi == GRAD) k_split_nt<GRAD><<<grid, 256, 0, st>>>(a);
+  else k_split_nt<SUMS><<<grid, 256, 0, st>>>(a);
+  HT_LAUNCH_CHECK(ctx);
+  return HT_OK;
+}
+
+int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_tensor* W, const int32_t* labels, const float* weight,
+             float* loss, float* row_loss, float* row_lse, const ht_tensor* dH, const ht_tensor* dW, size_t bytes) {
+  const int64_t V = H->rows, d = D->d, C = D->n_classes;
+  const bool in_out = D->w_form == HT_W_IN_OUT, grad = dH || dW;
+  const int mean = D->reduction == HT_REDUCE_MEAN;
+  hipStream_t st = ctx->stream;
+  const HeadPlan p = head_plan(V, d, C, in_out, bytes);
+  const int64_t pieces = std::max<int64_t>(1, ceil_div64(V, p.Rp)), ct = p.Cpad / TM;
+  const int64_t rpb = std::max<int64_t>(256, up_to(ceil_div64(std::max<int64_t>(V, 1), ROW_BLOCKS), 256)), rb = std::max<int64_t>(1, ceil_div64(V, rpb));
+  const int64_t jb = std::min<int64_t>(p.Rp / 64, 1024);   // blocks of k_head_join a piece
+  const int64_t KSC = p.Cpad / 16, KSR = p.Rp / 16;
+
+  OpsBlock m;
+  const auto cnt = m.add<int32_t>(rb);
+  const auto idx = m.add<int32_t>(V), lab = m.add<int32_t>(V);
+  const auto total = m.add<int64_t>(1);
+  const auto wc = m.add<uint32_t>(p.Cpad + p.dpad);              // W's largest values by class, by feature
+  const auto hm = m.add<uint32_t>(p.Rp + p.dpad);                // H's by row, by feature
+  const auto Wf = m.add<_Float16>(p.Cpad * p.KSd * 32);
+  const auto Hf = m.add<_Float16>(p.Rp * p.KSd * 32);
+  const auto part = m.add<float2>(ct * p.Rp);
+  const auto xlab = m.add<float>(p.Rp), lse = m.add<float>(p.Rp);
+  const auto ploss = m.add<double>(pieces * jb);
+  const auto Wt = m.add<_Float16>(dH ? p.dpad * KSC * 32 : 0);
+  const auto Ht = m.add<_Float16>(dW ? p.dpad * KSR * 32 : 0);
+  const auto P = m.add<_Float16>(grad ? p.Rp * p.Cp * 2 : 0), PT = m.add<_Float16>(grad ? p.Rp * p.Cp * 2 : 0);
+  const auto sh = m.add<float>(dH ? p.splits_h * p.Rp * p.dpad : 0);
+  const auto sw = m.add<float>(dW ? p.splits_w * p.Cp * p.dpad : 0);
+  HT_TRY(m.take(ctx));
+
+  k_head_count<<<(unsigned)rb, 256, 0, st>>>(labels, V, rpb, m.at(cnt));
+  HT_LAUNCH_CHECK(ctx);
+  k_head_place<<<(unsigned)rb, 256, 0, st>>>(labels, V, rpb, m.at(cnt), m.at(idx), m.at(lab), m.at(total), row_loss, row_lse,
+                                             dH ? dH->ptr : nullptr, dH ? dH->ld : 0, (int)d);
+  HT_LAUNCH_CHECK(ctx);
+  uint32_t *wmax_c = m.at(wc), *wmax_j = wmax_c + p.Cpad, *hmax_v = m.at(hm), *hmax_j = hmax_v + p.Rp;
+  HT_TRY(ht_fill_zero(ctx, st, wmax_c, (size_t)(p.Cpad + p.dpad) * 4));
+  {
+    const Source s{W->ptr, W->ld, W->rows, W->cols, nullptr, nullptr, nullptr, 0};
+    uint32_t *r = in_out ? wmax_j : wmax_c, *c = in_out ? wmax_c : wmax_j;
+    k_amax<<<dim3((unsigned)ceil_div64(s.rows, 64), (unsigned)ceil_div64(s.cols, AMAX_COLS)), 256, 0, st>>>(s, r, c);
+    HT_LAUNCH_CHECK(ctx);
+    _Float16* wt = dH ? m.at(Wt) : nullptr;
+    const int64_t rt = up_to(s.rows, in_out ? 64 : TM) / 64, cols_t = up_to(s.cols, in_out ? TM : 64) / 64;
+    k_pack<<<(unsigned)(rt * cols_t), 256, 0, st>>>(s, r, c, in_out ? wt : m.at(Wf), in_out ? KSC : p.KSd, in_out ? m.at(Wf) : wt, in_out ? p.KSd : KSC,
+                                                    in_out ? 64 : TM, (unsigned)cols_t);
+    HT_LAUNCH_CHECK(ctx);
+  }
+  for (int64_t k = 0; k < pieces; ++k) {
+    const int64_t r0 = k * p.Rp;
+    HT_TRY(ht_fill_zero(ctx, st, hmax_v, (size_t)(p.Rp + p.dpad) * 4));
+    const Source s{H->ptr, H->ld, p.Rp, d, m.at(idx), weight, m.at(total), r0};
+    k_amax<<<dim3((unsigned)(p.Rp / 64), (unsigned)ceil_div64(d, AMAX_COLS)), 256, 0, st>>>(s, hmax_v, hmax_j);
+    HT_LAUNCH_CHECK(ctx);
+    k_pack<<<(unsigned)(p.Rp / 64 * ceil_div64(d, 64)), 256, 0, st>>>(s, hmax_v, hmax_j, m.at(Hf), p.KSd, dW ? m.at(Ht) : nullptr, KSR, TN,
+                                                                     (unsigned)ceil_div64(d, 64));
+    HT_LAUNCH_CHECK(ctx);
+    NtArgs a{};
+    a.total = m.at(total), a.r0 = r0, a.most = p.Rp;
+    a.splits = 1;
+    a.C = C, a.cmax = wmax_c, a.hmax = hmax_v, a.lab = m.at(lab), a.part = m.at(part), a.xlab = m.at(xlab), a.lse = m.at(lse);
+    a.A = m.at(Wf), a.KSA = p.KSd, a.B = m.at(Hf), a.KSB = p.KSd;
+    a.mt = ct, a.nt = p.Rp / TN, a.steps = p.KSd, a.rows_are = 2;
+    HT_TRY(split_nt(ctx, st, LOSS, a));
+    k_head_join<<<(unsigned)jb, 1024, 0, st>>>(m.at(part), ct, p.Rp, m.at(total), r0, m.at(idx), m.at(lab), C, weight, m.at(xlab), m.at(lse), row_loss, row_lse,
+                                               m.at(ploss) + k * jb);
+    HT_LAUNCH_CHECK(ctx);
+    if (!grad) continue;
+    for (int64_t c0 = 0; c0 < p.Cpad; c0 += p.Cp) {
+      const int64_t cp = std::min(p.Cp, p.Cpad - c0);
+      NtArgs g = a;
+      g.c0 = c0, g.A = m.at(Wf) + c0 * p.KSd * 32, g.mt = cp / TM;
+      g.P = m.at(P), g.KSP = p.Cp / 16, g.PT = m.at(PT), g.KST = KSR;
+      HT_TRY(split_nt(ctx, st, GRAD, g));
+      if (dH) {
+        NtArgs h{};
+        h.total = m.at(total), h.r0 = r0, h.most = p.Rp, h.rows_are = 1;
+        h.A = m.at(P), h.KSA = p.Cp / 16, h.B = m.at(Wt), h.KSB = KSC, h.ksb0 = c0 / 16;
+        h.mt = p.Rp / TM, h.nt = up_to(d, TN) / TN, h.steps = cp / 16, h.splits = p.splits_h;
+        h.out = m.at(sh), h.out_m = p.Rp, h.out_n = p.dpad, h.add = c0 > 0;
+        HT_TRY(split_nt(ctx, st, SUMS, h));
+      }
+      if (dW) {
+        NtArgs w{};
+        w.total = m.at(total), w.r0 = r0, w.most = p.Rp, w.steps = -1, w.splits = p.splits_w;
+        w.out = m.at(sw);
+        if (in_out) {
+          w.A = m.at(Ht), w.B = m.at(PT), w.KSA = w.KSB = KSR;
+          w.mt = p.dpad / TM, w.nt = cp / TN, w.out_m = p.dpad, w.out_n = p.Cp;
+        } else {
+          w.A = m.at(PT), w.B = m.at(Ht), w.KSA = w.KSB = KSR;
+          w.mt = cp / TM, w.nt = up_to(d, TN) / TN, w.out_m = p.Cp, w.out_n = p.dpad;
+        }
+        HT_TRY(split_nt(ctx, st, SUMS, w));
+        const int64_t cls = std::min(cp, C - c0), rows = in_out ? d : cls, cols = in_out ? cls : d;
+        float* out = dW->ptr + (in_out ? c0 : c0 * dW->ld);
+        k_head_dw<<<(unsigned)ceil_div64(rows * cols, 256), 256, 0, st>>>(m.at(sw), p.splits_w, w.out_m, w.out_n, rows, cols, hmax_j, in_out, m.at(total), r0, mean,
+                                                                          k > 0 || D->accumulate_dW, out, dW->ld);
+        HT_LAUNCH_CHECK(ctx);
+      }
+    }
+    if (dH) {
+      k_head_dh<<<(unsigned)ceil_div64(p.Rp * ((d + 3) / 4), 256), 256, 0, st>>>(m.at(sh), p.splits_h, p.Rp, p.dpad, m.at(total), r0, m.at(idx), weight, mean, wmax_j,
+                                                                                 dH->ptr, dH->ld, (int)d);
+      HT_LAUNCH_CHECK(ctx);
+    }
+  }
+  k_head_loss<<<1, 256, 0, st>>>(m.at(ploss), pieces * jb, m.at(total), mean, loss);
+  HT_LAUNCH_CHECK(ctx);
+  return HT_OK;
+}
+
+}  // namespace
+
+extern "C" int ht_head_loss(ht_ctx* ctx, const ht_head_desc* desc, const ht_tensor* H, const ht_tensor* W, const int32_t* labels,
+                            const float* row_weight, float* loss, float* row_loss, float* row_lse, ht_tensor* dH, ht_tensor* dW) {
+  if (!ctx) return HT_EINVAL;
+  if (!desc || !H || !W || (!labels && H->rows > 0) || !loss) return ht_set_err(ctx, HT_EINVAL, "ht_head_loss: null argument");
+  if (desc->d <= 0 || desc->n_classes <= 0) return ht_set_err(ctx, HT_ESHAPE, "ht_head_loss: width and number of classes must be positive");
+  if (desc->d > HT_HEAD_MAX_WIDTH || desc->n_classes > HT_HEAD_MAX_CLASSES)
+    return ht_set_err(ctx, HT_ESHAPE, "ht_head_loss: %d x %d weights, at most %d x %d", desc->d, desc->n_classes, HT_HEAD_MAX_WIDTH, HT_HEAD_MAX_CLASSES);
+  if (desc->w_form != HT_W_IN_OUT && desc->w_form != HT_W_OUT_IN) return ht_set_err(ctx, HT_EINVAL, "ht_head_loss: unknown form of W %d", desc->w_form);
+  if (desc->reduction != HT_REDUCE_MEAN && desc->reduction != HT_REDUCE_SUM)
+    return ht_set_err(ctx, HT_EINVAL, "ht_head_loss: unknown reduction %d", desc->reduction);
+  const int64_t wr = desc->w_form == HT_W_IN_OUT ? desc->d : desc->n_classes;
+  const int32_t wcols = desc->w_form == HT_W_IN_OUT ? desc->n_classes : desc->d;
+  HT_TRY(ht_check_rows(ctx, H, H->rows, desc->d, "ht_head_loss: H"));
+  HT_TRY(ht_check_weights(ctx, W, wr, wcols, "ht_head_loss: W"));
+  if (dH) {
+    HT_TRY(ht_check_rows(ctx, dH, H->rows, desc->d, "ht_head_loss: dH"));
+    if (ht_overlap(dH, H) || ht_overlap(dH, W)) return ht_set_err(ctx, HT_EINVAL, "ht_head_loss: dH shares memory with an input");
+  }
+  if (dW) {
+    HT_TRY(ht_check_weights(ctx, dW, wr, wcols, "ht_head_loss: dW"));
+    if (ht_overlap(dW, H) || ht_overlap(dW, W) || (dH && ht_overlap(dW, dH)))
+      return ht_set_err(ctx, HT_EINVAL, "ht_head_loss: dW shares memory with another tensor");
+  }
+  HT_HIP(ctx, hipSetDevice(ctx->device));
+  return ht_with_room(ctx, [&]() -> int {
+    auto run = [&](size_t bytes) { return head_run(ctx, desc, H, W, labels, row_weight, loss, row_loss, row_lse, dH, dW, bytes); };
+    const int rc = ht_may_spend(ctx) ? run(HEAD_BYTES) : (int)HT_ENOMEM;
+    return rc == HT_ENOMEM ? run(HEAD_LEAN) : rc;      // (nothing has been launched by a call that is refused memory)
+  });
+}

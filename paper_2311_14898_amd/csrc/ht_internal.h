@@ -4,10 +4,12 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <chrono>
 #include <cstdio>
 #include <string>
 #include <unordered_map>
+#include <utility>
 #include <vector>
 
 #include "../../include/hongtu.h"
@@ -33,7 +35,7 @@ struct ht_graph;
 enum {
   HT_S_PACKW = 0, HT_S_TNPART, HT_S_LOSS, HT_S_ACHUNK, HT_S_OCHUNK, HT_S_ZCHUNK, HT_S_DZCHUNK, HT_S_DACHUNK,
   HT_S_NBUF, HT_S_SPART, HT_S_LEAVE, HT_S_MISC, HT_S_TFULL, HT_S_TFULL2, HT_S_GATV, HT_S_GATE, HT_S_GATWS, HT_S_GATP, HT_S_GATKEEP,
-  HT_S_LINK0, HT_S_LINK1, HT_S_LINK2, HT_S_SCAN, HT_S_RSORT, HT_S_TNTAB, HT_S_LIST, HT_S_DENSE, HT_N_SCRATCH
+  HT_S_LINK0, HT_S_LINK1, HT_S_LINK2, HT_S_SCAN, HT_S_RSORT, HT_S_TNTAB, HT_S_LIST, HT_S_DENSE, HT_S_OPS, HT_N_SCRATCH
 };
 
 constexpr int HT_HS_READBACK = 3, HT_HS_LOSS = 4, HT_N_HS = 5;
@@ -101,6 +103,7 @@ struct ht_ctx {
   int64_t tight_room = -1;     // room that was left after the last such call (-1: none since memory was plentiful)
   size_t gat_keep_limit = 0;   // a GAT epoch that kept this many bytes between its passes ran out of memory (0: none did) ...
   int64_t gat_keep_room = 0;   // ... and had this much room without them
+  std::vector<std::pair<void*, size_t>> retired;   // blocks of slots that a recorded pass works in, outgrown since (freed with the context)
   bool recorded = false;       // the owner of the stream has recorded a pass, which may be replayed for as long as it likes
   int64_t refuse_alloc = 0;    // HT_REFUSE_ALLOC=k: the context's k-th allocation is refused; -k: its k-th hipMalloc fails (tests)
   int64_t device_bytes = 0;    // HT_DEVICE_BYTES: plan as if the device had no more memory than this for the context (0: as it reports)
@@ -149,6 +152,10 @@ void ht_free_orphan(ht_graph* g);   // a graph whose context is gone
 int ht_scratch(ht_ctx* ctx, int slot, size_t bytes, void** out);
 // Gives a slot's memory back (after the work in flight).
 int ht_scratch_release(ht_ctx* ctx, int slot);
+// Slots whose blocks stay until the context's end once a caller has recorded a pass: replays of the operators below find them there.
+inline bool ht_slot_stays(const ht_ctx* ctx, int slot) {
+  return ctx->recorded && (slot == HT_S_OPS || slot == HT_S_RSORT || slot == HT_S_SCAN);
+}
 // What the device reports free.
 int64_t ht_device_free(ht_ctx* ctx);
 // Bytes that can still be allocated: by the byte budget and by the device's free memory.
@@ -264,6 +271,28 @@ struct DevBlock {
   void release() { mem.release(); planned = taken = 0; }
 };
 
+// Arrays of one call in the slot HT_S_OPS: add() every one, take() the memory, at() gives their addresses (256-byte aligned).  A pass that its
+// caller records takes what an earlier one has left, or is refused: nothing can be allocated there.
+struct OpsBlock {
+  template <typename T>
+  struct At { size_t off; };
+  size_t bytes = 0;
+  char* p = nullptr;
+  template <typename T>
+  At<T> add(int64_t count) {
+    const At<T> a{bytes};
+    bytes += ((size_t)std::max<int64_t>(count, 0) * sizeof(T) + 255) & ~(size_t)255;
+    return a;
+  }
+  int take(ht_ctx* ctx, size_t rsort = 0, size_t scan = 0);   // (with these bytes of the sort's and the scan's slots beside it)
+  template <typename T>
+  T* at(At<T> a) const { return reinterpret_cast<T*>(p + a.off); }
+};
+// Checks of operators' arguments: rows of vertex tensors in HBM (pitch and base as everywhere), weights (any pitch >= cols, 4-byte aligned).
+int ht_check_rows(ht_ctx* ctx, const ht_tensor* t, int64_t rows, int32_t cols, const char* name);
+int ht_check_weights(ht_ctx* ctx, const ht_tensor* t, int64_t rows, int32_t cols, const char* name);
+bool ht_overlap(const ht_tensor* a, const ht_tensor* b);
+
 static inline int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // ---- primitives (ht_prims.hip) -------------------------------------------------------
@@ -294,6 +323,8 @@ int ht_scan_i64(ht_ctx* ctx, const int64_t* in, int64_t* out, int64_t n, bool wa
 // have n entries; returns in *sorted which of the two holds the result.
 int ht_radix_sort_u64(ht_ctx* ctx, uint64_t* keys, uint64_t* tmp, int64_t n, int bit_lo, int bit_hi,
                       uint64_t** sorted);
+// Bytes of the slots HT_S_RSORT and HT_S_SCAN that a sort of n keys works in.
+void ht_radix_wants(int64_t n, size_t* rsort, size_t* scan);
 // Edges as keys (destination << bits) | source, a self-loop per vertex behind them where n > E; an id outside [0, V) raises the flag and becomes 0, so that
 // nothing later leaves its array.
 struct EdgeKeys {

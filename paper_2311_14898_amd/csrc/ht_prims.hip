@@ -413,6 +413,16 @@ int sort_any(ht_ctx* ctx, const EdgeKeys* edges, uint64_t* keys, uint64_t* tmp, 
 
 }  // namespace
 
+void ht_radix_wants(int64_t n, size_t* rsort, size_t* scan) {
+  *rsort = *scan = 0;
+  if (n <= 1) return;
+  const bool brief = n <= RS_SHORT_BLOCKS * RadixShape<RS_SHORT>::tile;
+  const int64_t cells = brief ? RadixShape<RS_SHORT>::bins * ceil_div64(n, RadixShape<RS_SHORT>::tile) : RadixShape<RS_LONG>::bins * ceil_div64(n, RadixShape<RS_LONG>::tile);
+  *rsort = (size_t)cells * 12 + 16;
+  if (brief) return;
+  for (int64_t m = ceil_div64(cells, SCAN_TILE); m > 1; m = ceil_div64(m, SCAN_TILE)) *scan += (size_t)m * sizeof(int64_t);
+}
+
 int ht_radix_sort_u64(ht_ctx* ctx, uint64_t* keys, uint64_t* tmp, int64_t n, int bit_lo, int bit_hi,
                       uint64_t** sorted) {
   *sorted = keys;
