@@ -29,7 +29,7 @@ constexpr int FRAG = 512;
 constexpr int TM = 256, TN = 128;      // tile of a block: rows of A x rows of B
 constexpr float LOG2E = 1.44269504088896340736f;
 constexpr int P_EXP = 15;              // gradients of logits are held times 2^15
-constexpr size_t HEAD_BYTES = (size_t)4 << 30, HEAD_LEAN = (size_t)64 << 20;   // of what a piece's rows take
+constexpr size_t HEAD_BYTES = (size_t)6 << 30, HEAD_LEAN = (size_t)64 << 20;   // of what a piece's rows take
 constexpr int64_t HEAD_CLASSES = 8192;             // of a piece
 
 __host__ __device__ constexpr int64_t up_to(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
@@ -124,38 +124,50 @@ struct Source {
 };
 
 // Largest absolute values of rows, and of columns (of weighted rows), as bits, into arrays that hold zeros.  (Maxima do not depend on their order.)
-constexpr int AMAX_COLS = 1024;
+// A block takes groups of 64 rows by AMAX_COLS columns; columns are joined once a block.
+constexpr int AMAX_COLS = 512;
 __global__ void __launch_bounds__(256) k_amax(Source s, uint32_t* __restrict__ rmax, uint32_t* __restrict__ cmax) {
+  constexpr int Q = AMAX_COLS / 64;
+  __shared__ uint32_t sh[4][AMAX_COLS];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t n = s.n(), r0 = (int64_t)blockIdx.x * 64 + wave * 16, c0 = (int64_t)blockIdx.y * AMAX_COLS;
-  if ((int64_t)blockIdx.x * 64 >= n) return;
-  const float* p[16];
-  float w[16];
-  uint32_t rm[16];
+  const int64_t n = s.n(), c0 = (int64_t)blockIdx.y * AMAX_COLS + lane;
+  uint32_t cm[Q];
 #pragma unroll
-  for (int q = 0; q < 16; ++q) {
-    const int64_t r = r0 + q < n ? r0 + q : n - 1, v = s.row(r);
-    p[q] = s.p + v * s.ld;
-    w[q] = s.weight ? s.weight[v] : 1.f;
-    rm[q] = 0;
-  }
-  const int64_t c1 = c0 + AMAX_COLS < s.cols ? c0 + AMAX_COLS : s.cols;
-  for (int64_t c = c0 + lane; c < c1; c += 64) {
-    uint32_t cm = 0;
-#pragma unroll
+  for (int k = 0; k < Q; ++k) cm[k] = 0;
+  for (int64_t g0 = (int64_t)blockIdx.x * 64; g0 < n; g0 += (int64_t)gridDim.x * 64) {
+    const int64_t r0 = g0 + wave * 16;
+#pragma unroll 4
     for (int q = 0; q < 16; ++q) {
-      const float x = p[q][c];
-      rm[q] = max(rm[q], __float_as_uint(fabsf(x)));
-      cm = max(cm, __float_as_uint(fabsf(x * w[q])));
+      const int64_t r = r0 + q < n ? r0 + q : n - 1, v = s.row(r);
+      const float* p = s.p + v * s.ld;
+      const float w = s.weight ? s.weight[v] : 1.f;
+      uint32_t rm = 0;
+#pragma unroll
+      for (int k = 0; k < Q; ++k) {
+        const float x = c0 + k * 64 < s.cols ? p[c0 + k * 64] : 0.f;
+        rm = max(rm, __float_as_uint(fabsf(x)));
+        cm[k] = max(cm[k], __float_as_uint(fabsf(x * w)));
+      }
+      for (int o = 32; o > 0; o >>= 1) rm = max(rm, (uint32_t)__shfl_xor((int)rm, o, 64));
+      if (lane == 0) {
+        if (gridDim.y == 1) rmax[r] = rm;
+        else atomicMax(rmax + r, rm);
+      }
     }
-    if (cmax) atomicMax(cmax + c, cm);
   }
 #pragma unroll
-  for (int q = 0; q < 16; ++q) {
-    uint32_t m = rm[q];
-    for (int o = 32; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
-    if (lane == 0 && r0 + q < n) atomicMax(rmax + r0 + q, m);
+  for (int k = 0; k < Q; ++k) sh[wave][k * 64 + lane] = cm[k];
+  __syncthreads();
+  for (int k = threadIdx.x; k < AMAX_COLS; k += 256) {
+    const int64_t c = (int64_t)blockIdx.y * AMAX_COLS + k;
+    const uint32_t m = max(max(sh[0][k], sh[1][k]), max(sh[2][k], sh[3][k]));
+    if (c < s.cols && m) atomicMax(cmax + c, m);
   }
+}
+constexpr int64_t AMAX_BLOCKS = 1024;
+void launch_amax(hipStream_t st, const Source& s, uint32_t* rmax, uint32_t* cmax) {
+  const int64_t gy = ceil_div64(s.cols, AMAX_COLS), gx = std::max<int64_t>(1, std::min(ceil_div64(s.rows, 64), AMAX_BLOCKS / gy));
+  k_amax<<<dim3((unsigned)gx, (unsigned)gy), 256, 0, st>>>(s, rmax, cmax);
 }
 
 __device__ __forceinline__ void split2(float x, _Float16* hi, _Float16* lo) {
@@ -230,7 +242,7 @@ struct NtArgs {
   int64_t KSA, KSB;
   int64_t ksb0;                   // first step of B
   int64_t mt, nt;                 // tiles
-  int64_t steps;                  // steps of the reduction (a multiple of 2); < 0: up to the piece's rows
+  int64_t steps;                  // steps of the reduction (a multiple of 4); < 0: up to the piece's rows
   int splits;                     // parts of it, each with sums of its own
   // the piece
   const int64_t* total;
@@ -258,7 +270,9 @@ __device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 
-constexpr int KT = 2;             // steps of a stage
+constexpr int KT = 2, PAIR = 32 * KT;   // steps of a stage; values of the reduction in two stages, which go together
+// C = A B^T of fragments, 256 x 128 a block, 64 x 128 a wave.  A wave reads its own rows of A straight into registers, a stage ahead, and the four
+// waves share B through LDS, which is filled a stage ahead as well; two blocks a CU.
 template <int EPI>
 __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
   constexpr int STAGE = TN / 32 * KT * 2 * FRAG;        // halfs
@@ -266,15 +280,16 @@ __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
   __shared__ __attribute__((aligned(16))) _Float16 Bs[2 * STAGE];
   static_assert(4 * 32 * TR_PITCH * 4 <= sizeof(Bs), "the waves' transposed tiles fit where B was");
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
+  const int64_t rows = a.total ? piece_rows(a.total, a.r0, a.most) : 0;
+  const int64_t mt = a.rows_are == 1 ? up_to(rows, TM) / TM : a.mt, nt = a.rows_are == 2 ? up_to(rows, TN) / TN : a.nt;
   // each XCD takes a contiguous part of the tiles, eight tiles of A over all of B after eight others
-  const int64_t tiles = a.mt * a.nt, per = (tiles + 7) / 8, t = (int64_t)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  const int64_t tiles = mt * nt, per = (tiles + 7) / 8, t = (int64_t)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
   if ((int64_t)(blockIdx.x >> 3) >= per || t >= tiles) return;
-  const int64_t g = t / (8 * a.nt), gm = a.mt - g * 8 < 8 ? a.mt - g * 8 : 8, q = t - g * 8 * a.nt;
+  const int64_t g = t / (8 * nt), gm = mt - g * 8 < 8 ? mt - g * 8 : 8, q = t - g * 8 * nt;
   const int64_t m0 = (g * 8 + q % gm) * TM, n0 = q / gm * TN;
-  const int64_t rows = piece_rows(a.total, a.r0, a.most);
-  if ((a.rows_are == 1 && m0 >= rows) || (a.rows_are == 2 && n0 >= rows)) return;
-  const int64_t all = a.steps >= 0 ? a.steps : up_to(rows, 16 * KT) / 16, stages = all / KT;
-  const int64_t s0 = stages * blockIdx.y / a.splits, s1 = stages * (blockIdx.y + 1) / a.splits;
+  const int64_t pairs = (a.steps >= 0 ? a.steps : up_to(rows, PAIR) / 16) / (2 * KT);
+  const int64_t s0 = pairs * blockIdx.y / a.splits * 2;                     // its first stage
+  int todo = __builtin_amdgcn_readfirstlane((int)(pairs * (blockIdx.y + 1) / a.splits - s0 / 2));
 
   v16f acc[2][4];
 #pragma unroll
@@ -284,106 +299,126 @@ __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
-  const _Float16* Ap[2];
+  const _Float16 *Ap0 = a.A + ((m0 / 32 + wave * 2) * a.KSA + s0 * KT) * 2 * FRAG + lane * 8, *Ap1 = Ap0 + a.KSA * 2 * FRAG;
+  const _Float16* Bp = a.B + ((n0 / 32 + wave) * a.KSB + a.ksb0 + s0 * KT) * 2 * FRAG + lane * 8;     // a wave brings one of the four row blocks
+  v8h ra[2][KT][2][2], rb[KT * 2];    // [stage in turn][step][row block][plane]
+  auto fetch = [&](int to) {          // of the stage that the pointers have come to
 #pragma unroll
-  for (int i = 0; i < 2; ++i) Ap[i] = a.A + (m0 / 32 + wave * 2 + i) * a.KSA * 2 * FRAG + lane * 8;
-  const _Float16* Bp = a.B + ((n0 / 32 + wave) * a.KSB + a.ksb0) * 2 * FRAG + lane * 8;     // a wave brings one of the four row blocks
-  v8h ra[2][2][2], rb[KT * 2];    // [step in turn][row block][plane]
-  auto fetch_a = [&](int64_t ks, int to) {
+    for (int u = 0; u < KT * 2; ++u) rb[u] = *reinterpret_cast<const v8h*>(Bp + u * FRAG);
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int u = 0; u < KT; ++u)
 #pragma unroll
-      for (int p = 0; p < 2; ++p) ra[to][i][p] = *reinterpret_cast<const v8h*>(Ap[i] + (ks * 2 + p) * FRAG);
+      for (int p = 0; p < 2; ++p) {
+        ra[to][u][0][p] = *reinterpret_cast<const v8h*>(Ap0 + (u * 2 + p) * FRAG);
+        ra[to][u][1][p] = *reinterpret_cast<const v8h*>(Ap1 + (u * 2 + p) * FRAG);
+      }
+    Ap0 += KT * 2 * FRAG, Ap1 += KT * 2 * FRAG, Bp += KT * 2 * FRAG;
   };
-  auto fetch_b = [&](int64_t s) {
-#pragma unroll
-    for (int u = 0; u < KT * 2; ++u) rb[u] = *reinterpret_cast<const v8h*>(Bp + (s * KT * 2 + u) * FRAG);
-  };
-  auto stash_b = [&](int to) {
+  auto stash = [&](int to) {
 #pragma unroll
     for (int u = 0; u < KT * 2; ++u) *reinterpret_cast<v8h*>(Bs + to * STAGE + (wave * KT * 2 + u) * FRAG + lane * 8) = rb[u];
   };
-  if (s0 < s1) {
-    fetch_b(s0);
-    fetch_a(s0 * KT, 0);
-    stash_b(0);
-    __syncthreads();
-  }
-  for (int64_t s = s0; s < s1; ++s) {
-    const int cur = (int)(s - s0) & 1;
-    if (s + 1 < s1) fetch_b(s + 1);
+  auto read_b = [&](v8h* b, int cur, int k) {          // k: step * 4 + row block
+    const _Float16* f = Bs + cur * STAGE + ((k & 3) * KT * 2 + (k >> 2) * 2) * FRAG + lane * 8;
+    b[0] = *reinterpret_cast<const v8h*>(f);
+    b[1] = *reinterpret_cast<const v8h*>(f + FRAG);
+  };
+  // (Loads have no condition, so that waits count only the loads that they wait for: the last stage fetches itself again.  The barriers to scheduling
+  // keep them where they stand; they would be moved down to where they are used.)
+  auto stage = [&](int cur, bool more) {
+    if (!more) Ap0 -= KT * 2 * FRAG, Ap1 -= KT * 2 * FRAG, Bp -= KT * 2 * FRAG;
+    v8h b[2][2];
+    read_b(b[0], cur, 0);
+    fetch(cur ^ 1);
 #pragma unroll
-    for (int u = 0; u < KT; ++u) {
-      const int64_t ks = s * KT + u, nx = ks + 1 < s1 * KT ? ks + 1 : ks;
-      fetch_a(nx, (u + 1) & 1);
-      const v8h (&x)[2][2] = ra[u & 1];
+    for (int k = 0; k < 4 * KT; ++k) {
+      const v8h (&x)[2][2] = ra[cur][k >> 2];
+      const v8h (&y)[2] = b[k & 1];
+      if (k + 1 < 4 * KT) read_b(b[(k + 1) & 1], cur, k + 1);
+      __builtin_amdgcn_sched_barrier(0);
+      const int j = k & 3;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const _Float16* f = Bs + cur * STAGE + (j * KT * 2 + u * 2) * FRAG + lane * 8;
-        const v8h b0 = *reinterpret_cast<const v8h*>(f), b1 = *reinterpret_cast<const v8h*>(f + FRAG);
+      for (int i = 0; i < 2; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][1], y[0], acc[i][j], 0, 0, 0);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][1], b0, acc[i][j], 0, 0, 0);
+      for (int i = 0; i < 2; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][0], y[1], acc[i][j], 0, 0, 0);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][0], b1, acc[i][j], 0, 0, 0);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][0], b0, acc[i][j], 0, 0, 0);
-      }
+      for (int i = 0; i < 2; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][0], y[0], acc[i][j], 0, 0, 0);
     }
-    if (s + 1 < s1) stash_b(cur ^ 1);
+    __builtin_amdgcn_sched_barrier(0);
+    stash(cur ^ 1);
     __syncthreads();
+  };
+  if (todo > 0) {
+    fetch(0);
+    stash(0);
+    __syncthreads();
+    do {
+      stage(0, true);
+      stage(1, --todo > 0);
+    } while (todo > 0);
   }
 
   // lane l32 + 32 half of a 32 x 32 tile has column l32 and the rows 8 (e / 4) + 4 half + e % 4
   const int64_t mw = m0 + wave * 64;
-  if constexpr (EPI == SUMS) {
-    float* out = a.out + (int64_t)blockIdx.y * a.out_m * a.out_n;
+  if constexpr (EPI == SUMS) {         // (whole tiles: what lies behind the last row and column is not looked at)
+    float* out = a.out + ((int64_t)blockIdx.y * a.out_m + mw + half * 4) * a.out_n + n0 + l32;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int64_t n = n0 + j * 32 + l32;
-      if (n >= a.out_n) continue;
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int j = 0; j < 4; ++j) {
+        float was[16];
+        if (a.add) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int64_t m = mw + i * 32 + (e >> 2) * 8 + half * 4 + (e & 3);
-          if (m >= a.out_m) continue;
-          float* o = out + m * a.out_n + n;
-          *o = a.add ? *o + acc[i][j][e] : acc[i][j][e];
+          for (int e = 0; e < 16; ++e) was[e] = out[(i * 32 + (e >> 2) * 8 + (e & 3)) * a.out_n + j * 32];
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) was[e] = 0.f;
         }
-    }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) out[(i * 32 + (e >> 2) * 8 + (e & 3)) * a.out_n + j * 32] = was[e] + acc[i][j][e];
+      }
     return;
   }
-  float cs[2][16];                 // what undoes the classes' scaling
+  float cs[2][16];                 // what undoes the classes' scaling (cmax is there for whole tiles)
 #pragma unroll
   for (int i = 0; i < 2; ++i)
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const int64_t c = a.c0 + mw + i * 32 + (e >> 2) * 8 + half * 4 + (e & 3);
-      cs[i][e] = unscale_of(c < a.C ? a.cmax[c] : 0u);
+    for (int k = 0; k < 4; ++k) {
+      const uint4 x = *reinterpret_cast<const uint4*>(a.cmax + a.c0 + mw + i * 32 + k * 8 + half * 4);
+      cs[i][k * 4] = unscale_of(x.x), cs[i][k * 4 + 1] = unscale_of(x.y), cs[i][k * 4 + 2] = unscale_of(x.z), cs[i][k * 4 + 3] = unscale_of(x.w);
     }
-  const bool whole = a.c0 + mw + 64 <= a.C;
-  auto inside = [&](int i, int e) { return whole || a.c0 + mw + i * 32 + (e >> 2) * 8 + half * 4 + (e & 3) < a.C; };
+  const int64_t left = a.C - a.c0 - mw;                              // classes of the wave's 64
+  const int lim = (left >= 64 ? 64 : left < 0 ? 0 : (int)left) - half * 4;
   if constexpr (EPI == LOSS) {
     float2* red = reinterpret_cast<float2*>(Bs);      // [wave][column]
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int64_t v = n0 + j * 32 + l32;
       const bool there = v < rows;
-      const float hs = unscale_of(there ? a.hmax[v] : 0u);
+      const float hs = unscale_of(a.hmax[v]);
       float m = -INFINITY;
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          acc[i][j][e] = inside(i, e) ? acc[i][j][e] * hs * cs[i][e] : -INFINITY;
-          m = fmaxf(m, acc[i][j][e]);
-        }
+        for (int e = 0; e < 16; ++e) acc[i][j][e] *= hs * cs[i][e];
+      if (left < 64) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (i * 32 + (e >> 2) * 8 + (e & 3) >= lim) acc[i][j][e] = -INFINITY;
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) m = fmaxf(m, acc[i][j][e]);
       m = fmaxf(m, __shfl_xor(m, 32, 64));
+      const float m1 = m == -INFINITY ? 0.f : m;      // (a wave behind the last class: exp(-inf) throughout)
       float z = 0.f;
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) z += inside(i, e) ? exp_less(acc[i][j][e], m) : 0.f;
+        for (int e = 0; e < 16; ++e) z += exp_less(acc[i][j][e], m1);
       z += __shfl_xor(z, 32, 64);
       if (half == 0) red[wave * TN + j * 32 + l32] = make_float2(m, z);
       const int64_t off = there ? a.lab[a.r0 + v] - (a.c0 + mw) : -1;
@@ -414,7 +449,7 @@ __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
     for (int j = 0; j < 4; ++j) {
       const int64_t v = n0 + j * 32 + l32;
       const bool there = v < rows;
-      const float hs = unscale_of(there ? a.hmax[v] : 0u);
+      const float hs = unscale_of(a.hmax[v]);
       const float lse = there ? a.lse[v] : 0.f;
       const int64_t off = there ? a.lab[a.r0 + v] - (a.c0 + mw) : -1;
       const bool mine = off >= 0 && off < 64 && ((off >> 2) & 1) == half;
@@ -423,9 +458,11 @@ __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
       for (int i = 0; i < 2; ++i) {
         float p[16];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          p[e] = __builtin_amdgcn_exp2f(fmaf(fmaf(acc[i][j][e] * hs, cs[i][e], -lse), LOG2E, P_EXP));
-          if (!there || !inside(i, e)) p[e] = 0.f;
+        for (int e = 0; e < 16; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(fmaf(acc[i][j][e], hs * cs[i][e], -lse), LOG2E, P_EXP));
+        if (left < 64 || n0 + TN > rows) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (!there || i * 32 + (e >> 2) * 8 + (e & 3) >= lim) p[e] = 0.f;
         }
         if (any) {
 #pragma unroll
@@ -537,13 +574,14 @@ __global__ void __launch_bounds__(256) k_head_loss(const double* __restrict__ pa
 __device__ __forceinline__ float inv_count(const int64_t* total, int mean) { return mean ? 1.f / (float)(*total > 0 ? *total : 1) : 1.f; }
 
 // dH rows of a piece: the splits' sums, scaled
+constexpr int64_t DH_BLOCKS = 8192;
 __global__ void __launch_bounds__(256) k_head_dh(const float* __restrict__ sums, int splits, int64_t most, int64_t pitch, const int64_t* __restrict__ total,
                                                  int64_t r0, const int32_t* __restrict__ idx, const float* __restrict__ weight, int mean,
                                                  const uint32_t* __restrict__ wmax, float* __restrict__ dH, int64_t ld, int d) {
   const int64_t rows = piece_rows(total, r0, most);
   const int nv = (d + 3) / 4;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, v = i / nv;
-  if (v >= rows) return;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * nv; i += (int64_t)gridDim.x * 256) {
+  const int64_t v = i / nv;
   const int c = (int)(i % nv) * 4;
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int k = 0; k < splits; ++k) {
@@ -554,6 +592,7 @@ __global__ void __launch_bounds__(256) k_head_dh(const float* __restrict__ sums,
   const float f = inv_count(total, mean) * (weight ? weight[at] : 1.f) * (1.f / (1 << P_EXP));
   auto out = [&](float x, int k) { return c + k < d ? x * unscale_of(wmax[c + k]) * f : 0.f; };
   *reinterpret_cast<float4*>(dH + at * ld + c) = make_float4(out(s.x, 0), out(s.y, 1), out(s.z, 2), out(s.w, 3));
+  }
 }
 
 // dW's part [rows x cols] at out (pitch ld): the splits' sums (pitch cols_p, rows_p rows each), scaled by what undoes hmax along rows or columns
@@ -578,7 +617,7 @@ struct HeadPlan {
 
 HeadPlan head_plan(int64_t V, int64_t d, int64_t C, bool in_out, size_t bytes) {
   HeadPlan p{};
-  p.KSd = up_to(d, 16 * KT) / 16;
+  p.KSd = up_to(d, PAIR) / 16;
   p.Cpad = up_to(C, TM);
   p.dpad = up_to(d, TM);
   p.Cp = std::min<int64_t>(p.Cpad, HEAD_CLASSES);
@@ -644,7 +683,7 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
   {
     const Source s{W->ptr, W->ld, W->rows, W->cols, nullptr, nullptr, nullptr, 0};
     uint32_t *r = in_out ? wmax_j : wmax_c, *c = in_out ? wmax_c : wmax_j;
-    k_amax<<<dim3((unsigned)ceil_div64(s.rows, 64), (unsigned)ceil_div64(s.cols, AMAX_COLS)), 256, 0, st>>>(s, r, c);
+    launch_amax(st, s, r, c);
     HT_LAUNCH_CHECK(ctx);
     _Float16* wt = dH ? m.at(Wt) : nullptr;
     const int64_t rt = up_to(s.rows, in_out ? 64 : TM) / 64, cols_t = up_to(s.cols, in_out ? TM : 64) / 64;
@@ -656,7 +695,7 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
     const int64_t r0 = k * p.Rp;
     HT_TRY(ht_fill_zero(ctx, st, hmax_v, (size_t)(p.Rp + p.dpad) * 4));
     const Source s{H->ptr, H->ld, p.Rp, d, m.at(idx), weight, m.at(total), r0};
-    k_amax<<<dim3((unsigned)(p.Rp / 64), (unsigned)ceil_div64(d, AMAX_COLS)), 256, 0, st>>>(s, hmax_v, hmax_j);
+    launch_amax(st, s, hmax_v, hmax_j);
     HT_LAUNCH_CHECK(ctx);
     k_pack<<<(unsigned)(p.Rp / 64 * ceil_div64(d, 64)), 256, 0, st>>>(s, hmax_v, hmax_j, m.at(Hf), p.KSd, dW ? m.at(Ht) : nullptr, KSR, TN,
                                                                      (unsigned)ceil_div64(d, 64));
@@ -706,7 +745,7 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
       }
     }
     if (dH) {
-      k_head_dh<<<(unsigned)ceil_div64(p.Rp * ((d + 3) / 4), 256), 256, 0, st>>>(m.at(sh), p.splits_h, p.Rp, p.dpad, m.at(total), r0, m.at(idx), weight, mean, wmax_j,
+      k_head_dh<<<(unsigned)std::min(ceil_div64(p.Rp * ((d + 3) / 4), 256), DH_BLOCKS), 256, 0, st>>>(m.at(sh), p.splits_h, p.Rp, p.dpad, m.at(total), r0, m.at(idx), weight, mean, wmax_j,
                                                                                  dH->ptr, dH->ld, (int)d);
       HT_LAUNCH_CHECK(ctx);
     }
