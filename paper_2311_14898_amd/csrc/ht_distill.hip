@@ -123,9 +123,10 @@ typedef float V4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ float4 zero4() { return make_float4(0.f, 0.f, 0.f, 0.f); }
 
 // T threads a row, NV float4 of it in each thread's registers; what goes beyond (MORE) is read once more for the gradient, the last read first, while some of
-// it is still in the caches.  Rows of T x NV x 4 classes.
+// it is still in the caches.  Rows of T x NV x 4 classes.  Short rows want waves (at most 72 registers: 100,003 rows x 172 56.7 -> 53.2 us); long rows
+// past the caches, loads and stores that are not for them (4,096 x 131,072, where 49,152 classes stay in registers: 1.15 ms, with such stores 1.08, with loads too 1.05).
 template <int T, int NV, bool MORE>
-__global__ void __launch_bounds__(T < 256 ? 256 : T) k_distill(DistillArgs a, const unsigned long long* __restrict__ cnt, int n_cnt, double* __restrict__ part) {
+__global__ void __launch_bounds__(T < 256 ? 256 : T, T < 256 ? 7 : 1) k_distill(DistillArgs a, const unsigned long long* __restrict__ cnt, int n_cnt, double* __restrict__ part) {
   constexpr int B = T < 256 ? 256 : T, R = B / T;
   extern __shared__ float entries[];             // [R][K] ids, [R][K] q
   __shared__ float2 red[B / 64];
@@ -157,7 +158,14 @@ __global__ void __launch_bounds__(T < 256 ? 256 : T) k_distill(DistillArgs a, co
       return y;
     };
 #pragma unroll
-    for (int u = 0; u < NV; ++u) keep[u] = read(u);
+    for (int u = 0; u < NV; ++u) {
+      if (MORE) {                                // (read once: behind none of it is the last class)
+        const V4 y = __builtin_nontemporal_load(reinterpret_cast<const V4*>(x + (u * T + l) * 4));
+        keep[u] = make_float4(y.x, y.y, y.z, y.w);
+      } else {
+        keep[u] = read(u);
+      }
+    }
     const float tmax = load_entries<T>(a, v, l, sid, sq);
     float xm = -INFINITY, z = 0.f;
 #pragma unroll

@@ -5,40 +5,95 @@
 
 namespace {
 
-// ---- H[i] = scale * table[ids[i]]: LPR lanes a row, a float4 each, four rows of a group at once.
-template <int LPR>
+typedef float V4 __attribute__((ext_vector_type(4)));
+
+// ---- H[i] = scale * table[ids[i]]: a float4 a thread and turn, rows one after the other without lanes that idle at their ends, four turns in flight.
+// What bounds it is writing H.
+constexpr int EMBED_TURNS = 4;
+// Bytes of H from which it is written past the L2s, which hold 32 MiB and then keep the table.  Through them | past them: 232,965 rows of 301 floats of a table
+// of 60 MB 82 | 57 us, 65,000 of 300 19.5 | 17.7, 35,000 11.5 | 9.7.  Less than that may still be there for whoever reads H next.
+constexpr int64_t EMBED_PAST = (int64_t)32 << 20;
+template <bool PAST>
 __global__ void __launch_bounds__(256) k_embed(const float* __restrict__ table, int64_t ld, int64_t V, const int32_t* __restrict__ ids, int64_t n, float scale,
-                                               float* __restrict__ H, int64_t ld_h, int nv) {
-  constexpr int U = 4, G = 256 / LPR;
-  const int l = threadIdx.x % LPR;
-  const int64_t i0 = ((int64_t)blockIdx.x * G + threadIdx.x / LPR) * U;
-  int32_t id[U];
+                                               float* __restrict__ H, int64_t ld_h, uint32_t nv) {
+  // a block's first float4 as row and column, in 64 bits once; from there on 32 bits do
+  const int64_t first = (int64_t)blockIdx.x * (256 * EMBED_TURNS), r0 = first / nv;
+  const uint32_t c0 = (uint32_t)(first - r0 * nv) + threadIdx.x;
+  int64_t row[EMBED_TURNS];
+  uint32_t c[EMBED_TURNS];
+  int32_t id[EMBED_TURNS];
+  float4 x[EMBED_TURNS];
 #pragma unroll
-  for (int u = 0; u < U; ++u) id[u] = i0 + u < n ? ids[i0 + u] : -1;
-  for (int c = l; c < nv; c += LPR) {
-    float4 x[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const float no = id[u] < 0 ? 0.f : NAN;
-      x[u] = make_float4(no, no, no, no);
-      if (id[u] >= 0 && id[u] < V) x[u] = *reinterpret_cast<const float4*>(table + id[u] * ld + c * 4);
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (i0 + u < n) *reinterpret_cast<float4*>(H + (i0 + u) * ld_h + c * 4) = make_float4(x[u].x * scale, x[u].y * scale, x[u].z * scale, x[u].w * scale);
+  for (int u = 0; u < EMBED_TURNS; ++u) {
+    const uint32_t at = c0 + u * 256, r = at / nv;
+    c[u] = (at - r * nv) * 4;
+    row[u] = r0 + r;
+    id[u] = row[u] < n ? ids[row[u]] : -1;
   }
+#pragma unroll
+  for (int u = 0; u < EMBED_TURNS; ++u) {
+    const float no = id[u] < 0 ? 0.f : NAN;
+    x[u] = make_float4(no, no, no, no);
+    if (id[u] >= 0 && id[u] < V) x[u] = *reinterpret_cast<const float4*>(table + id[u] * ld + c[u]);
+  }
+#pragma unroll
+  for (int u = 0; u < EMBED_TURNS; ++u)
+    if (row[u] < n) {
+      const V4 y{x[u].x * scale, x[u].y * scale, x[u].z * scale, x[u].w * scale};
+      V4* to = reinterpret_cast<V4*>(H + row[u] * ld_h + c[u]);
+      if (PAST) __builtin_nontemporal_store(y, to);
+      else *to = y;
+    }
 }
 
-// ---- the gradient.  (id, position) pairs are sorted by id; a tile of TS sorted entries is summed by one group of lanes, in order.  What begins and ends
-// in a tile is written; the sums of an id that goes on into other tiles are left, as the tile's first or last, to k_embed_join, which adds
-// them in the order of the tiles.
-constexpr int TS = 32;
+// ---- the gradient.  (id, position) pairs are sorted by id; a tile of sorted entries is summed by one group of LPR lanes, in order, and the groups of a
+// block join the sums of ids that go on from tile to tile in LDS.  What begins and ends in a block is written; the rest is left, as the
+// block's first or last sum, to k_embed_join, which adds it in the order of the blocks.
+constexpr int GROUPS = 16;                 // of a block
+constexpr int TILE = 32, TILE_FEW = 8;     // entries of a tile
 
-__global__ void __launch_bounds__(256) k_embed_keys(const int32_t* __restrict__ ids, int64_t n, int64_t V, uint64_t* __restrict__ keys) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= n) return;
+// A table's rows are cleared by blocks of the launch that makes the keys (the first `key_blocks` of it), which leave the memory idle.
+struct EmbedClear {
+  float* p;                      // 16-byte aligned
+  int64_t words;                 // (0: nothing to clear)
+  __device__ __forceinline__ void run(int64_t block, int64_t blocks) const {
+    const int64_t n4 = words >> 2, stride = blocks * 256;
+    for (int64_t i = block * 256 + threadIdx.x; i < n4; i += stride) reinterpret_cast<float4*>(p)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (block == 0 && threadIdx.x < (words & 3)) p[n4 * 4 + threadIdx.x] = 0.f;
+  }
+};
+__device__ __forceinline__ uint64_t embed_key(const int32_t* ids, int64_t i, int64_t V) {      // (ids of no row: behind the others)
   const int32_t id = ids[i];
-  keys[i] = (uint64_t)(id >= 0 && id < V ? (uint32_t)id : (uint32_t)V) << 32 | (uint32_t)i;      // (ids of no row: behind the others)
+  return (uint64_t)(id >= 0 && id < V ? (uint32_t)id : (uint32_t)V) << 32 | (uint32_t)i;
+}
+__global__ void __launch_bounds__(256) k_embed_keys(const int32_t* __restrict__ ids, int64_t n, int64_t V, uint64_t* __restrict__ keys, unsigned key_blocks,
+                                                    EmbedClear clear) {
+  if (blockIdx.x >= key_blocks) return clear.run(blockIdx.x - key_blocks, gridDim.x - key_blocks);
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i < n) keys[i] = embed_key(ids, i, V);
+}
+// Few entries are put in order in the same launch: an entry's place is the number of entries before it, which it counts.  us, counted | sorted: 6,000 entries
+// of 1,000 ids 27 | 32, 10,000 of 131,000 56 | 67, 16,000 of either 95 | 37 and 126 | 68.
+constexpr int EMBED_FEW = 8192;
+__global__ void __launch_bounds__(256) k_embed_rank(const int32_t* __restrict__ ids, int n, int64_t V, uint64_t* __restrict__ keys, unsigned key_blocks,
+                                                    EmbedClear clear) {
+  if (blockIdx.x >= key_blocks) return clear.run(blockIdx.x - key_blocks, gridDim.x - key_blocks);
+  // 16 lanes an entry, each compares with every 16th four of the others
+  extern __shared__ __attribute__((aligned(16))) uint32_t sh[];      // [n, up to the next 4]
+  const int n4 = (n + 3) / 4;
+  for (int i = threadIdx.x; i < n4 * 4; i += 256) sh[i] = i < n ? (uint32_t)(embed_key(ids, i, V) >> 32) : 0xffffffffu;
+  __syncthreads();
+  const int l = threadIdx.x & 15, i = blockIdx.x * 16 + (threadIdx.x >> 4);
+  const uint32_t mine = i < n ? sh[i] : 0;
+  int before = 0;
+  for (int q = l; q < n4; q += 16) {
+    const uint4 x = *reinterpret_cast<const uint4*>(sh + q * 4);
+    const int j = q * 4;
+    before += (x.x < mine || (x.x == mine && j < i)) + (x.y < mine || (x.y == mine && j + 1 < i)) + (x.z < mine || (x.z == mine && j + 2 < i)) +
+              (x.w < mine || (x.w == mine && j + 3 < i));
+  }
+  for (int o = 8; o > 0; o >>= 1) before += __shfl_xor(before, o, 64);
+  if (l == 0 && i < n) keys[before] = (uint64_t)mine << 32 | (uint32_t)i;
 }
 
 struct EmbedOut {
@@ -54,75 +109,113 @@ struct EmbedOut {
   }
 };
 
-// edge: [tile][first, last][4 nv] floats
-template <int LPR>
-__global__ void __launch_bounds__(256) k_embed_sum(const uint64_t* __restrict__ keys, int64_t n, const float* __restrict__ dH, int64_t ld_h, EmbedOut out,
-                                                   float4* __restrict__ edge) {
-  constexpr int G = 256 / LPR, U = 8;
-  const int64_t tile = (int64_t)blockIdx.x * G + threadIdx.x / LPR, p0 = tile * TS;
-  const int c = blockIdx.y * LPR + threadIdx.x % LPR;
-  if (p0 >= n || c >= out.nv) return;
-  const int64_t p1 = p0 + TS < n ? p0 + TS : n;
-  const bool goes_on = p1 < n && (uint32_t)(keys[p1] >> 32) == (uint32_t)(keys[p1 - 1] >> 32);
-  bool first = p0 > 0 && (uint32_t)(keys[p0 - 1] >> 32) == (uint32_t)(keys[p0] >> 32);      // the run has begun before this tile
-  uint32_t id = (uint32_t)(keys[p0] >> 32);
-  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-  auto end = [&](bool last) {
-    if (first) edge[(tile * 2) * out.nv + c] = s;
-    else if (last) edge[(tile * 2 + 1) * out.nv + c] = s;
-    else out.put(id, c, s);
-    first = false;
-  };
-  for (int64_t p = p0; p < p1; p += U) {
-    uint64_t k[U];
-    float4 x[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) k[u] = keys[p + u < p1 ? p + u : p1 - 1];
-#pragma unroll
-    for (int u = 0; u < U; ++u) x[u] = *reinterpret_cast<const float4*>(dH + (int64_t)(uint32_t)k[u] * ld_h + c * 4);
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (p + u >= p1) break;
-      const uint32_t t = (uint32_t)(k[u] >> 32);
-      if (t != id) {
-        end(false);
-        id = t;
-        s = make_float4(0.f, 0.f, 0.f, 0.f);
-      }
-      s.x += x[u].x, s.y += x[u].y, s.z += x[u].z, s.w += x[u].w;
-    }
+// edge: [block][first, last][nv]
+template <int LPR, int TS>
+__global__ void __launch_bounds__(LPR * GROUPS) k_embed_sum(const uint64_t* __restrict__ keys, int64_t n, const float* __restrict__ dH, int64_t ld_h, EmbedOut out,
+                                                            float4* __restrict__ edge) {
+  constexpr int B = LPR * GROUPS, E = GROUPS * TS, U = 8;
+  __shared__ uint32_t id[E + 2], pos[E];   // id[e + 1]: of entry e; before and behind them their neighbours
+  __shared__ float4 sums[GROUPS][LPR][2];  // of a tile's first run where it has begun before, of its last where it goes on
+  const int64_t e0 = (int64_t)blockIdx.x * E;
+  const int here = n - e0 < E ? (int)(n - e0) : E;
+  constexpr uint32_t NONE = 0xffffffffu;   // (no id: ids are below 2^31)
+  for (int e = (int)threadIdx.x - 1; e < E + 1; e += B) {
+    const int64_t p = e0 + e;
+    const uint64_t k = p >= 0 && p < n ? keys[p] : (uint64_t)NONE << 32;
+    id[e + 1] = (uint32_t)(k >> 32);
+    if (e >= 0 && e < E) pos[e] = (uint32_t)k;
   }
-  end(goes_on);
+  __syncthreads();
+  const int g = threadIdx.x / LPR, l = threadIdx.x % LPR, c = blockIdx.y * LPR + l;
+  const int a = g * TS, b = a + TS < here ? a + TS : here;
+  const bool works = a < here && c < out.nv;
+  if (works) {
+    bool first = id[a + 1] == id[a];       // the run has begun before this tile
+    uint32_t t = id[a + 1];
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto end = [&](bool last) {
+      if (first) sums[g][l][0] = s;
+      else if (last) sums[g][l][1] = s;
+      else out.put(t, c, s);
+      first = false;
+    };
+    for (int e = a; e < b; e += U) {
+      float4 x[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) x[u] = *reinterpret_cast<const float4*>(dH + (int64_t)pos[e + u < b ? e + u : b - 1] * ld_h + c * 4);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (e + u >= b) break;
+        const uint32_t i = id[e + u + 1];
+        if (i != t) {
+          end(false);
+          t = i;
+          s = make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        s.x += x[u].x, s.y += x[u].y, s.z += x[u].z, s.w += x[u].w;
+      }
+    }
+    end(id[b + 1] == t);
+  }
+  __syncthreads();
+  if (!works) return;
+  auto goes_on = [&](int k) {              // tile k's last run does
+    const int z = (k + 1) * TS < here ? (k + 1) * TS : here;
+    return id[z] == id[z + 1];
+  };
+  auto one_run = [&](int k) {
+    const int z = (k + 1) * TS < here ? (k + 1) * TS : here;
+    return id[k * TS + 1] == id[z];
+  };
+  // the sum from tile k's first run on, until the run ends; true: in this block
+  auto follow = [&](int k, float4* s) {
+    for (; k * TS < here; ++k) {
+      const float4 x = sums[k][l][0];
+      s->x += x.x, s->y += x.y, s->z += x.z, s->w += x.w;
+      if (!one_run(k) || !goes_on(k)) return true;
+    }
+    return false;
+  };
+  const bool begun = id[a + 1] == id[a];
+  if (g == 0 && begun) {
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    (void)follow(0, &s);
+    edge[(int64_t)blockIdx.x * 2 * out.nv + c] = s;
+  }
+  if (goes_on(g) && !(begun && one_run(g))) {
+    float4 s = sums[g][l][1];
+    if (follow(g + 1, &s)) out.put(id[b], c, s);
+    else edge[((int64_t)blockIdx.x * 2 + 1) * out.nv + c] = s;
+  }
 }
 
-// A block a tile: if a run begins in it and goes on, its last sum and the first ones of the tiles that the run reaches.
+// A block each: if a run begins in block `blockIdx.x` of k_embed_sum's (E entries each) and goes on, its last sum and the first ones of those that the run reaches.
 template <int LPR>
-__global__ void __launch_bounds__(256) k_embed_join(const uint64_t* __restrict__ keys, int64_t n, EmbedOut out, const float4* __restrict__ edge) {
+__global__ void __launch_bounds__(256) k_embed_join(const uint64_t* __restrict__ keys, int64_t n, int E, EmbedOut out, const float4* __restrict__ edge) {
   constexpr int G = 256 / LPR;
   __shared__ float4 sh[256];
-  const int64_t tile = blockIdx.x, p0 = tile * TS, p1 = p0 + TS;
-  if (p1 >= n) return;
+  const int64_t block = blockIdx.x, p0 = block * E, p1 = p0 + E;
   const uint32_t id = (uint32_t)(keys[p1 - 1] >> 32);
   if ((uint32_t)(keys[p1] >> 32) != id) return;
   if (p0 > 0 && (uint32_t)(keys[p0 - 1] >> 32) == id) return;       // (sorted: the run has begun before)
-  // the run's end, by bisection over the tiles' first entries, then the tiles after this one that it reaches
-  int64_t lo = tile + 1, hi = (n + TS - 1) / TS;
+  // the last block that the run reaches, by bisection over the blocks' first entries
+  int64_t lo = block + 1, hi = (n + E - 1) / E;
   while (hi - lo > 1) {
     const int64_t mid = (lo + hi) / 2;
-    if ((uint32_t)(keys[mid * TS] >> 32) == id) lo = mid;
+    if ((uint32_t)(keys[mid * E] >> 32) == id) lo = mid;
     else hi = mid;
   }
-  const int64_t m = lo - tile;
+  const int64_t m = lo - block;
   const int g = threadIdx.x / LPR;
   for (int c0 = 0; c0 < out.nv; c0 += LPR) {
     const int c = c0 + threadIdx.x % LPR;
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
     if (c < out.nv) {
-      if (g == 0) s = edge[(tile * 2 + 1) * out.nv + c];
+      if (g == 0) s = edge[(block * 2 + 1) * out.nv + c];
       const int64_t a = m * g / G, b = m * (g + 1) / G;
 #pragma unroll 8
       for (int64_t t = a; t < b; ++t) {
-        const float4 x = edge[((tile + 1 + t) * 2) * out.nv + c];
+        const float4 x = edge[((block + 1 + t) * 2) * out.nv + c];
         s.x += x.x, s.y += x.y, s.z += x.z, s.w += x.w;
       }
     }
@@ -159,16 +252,18 @@ extern "C" int ht_embed_fwd(ht_ctx* ctx, const ht_tensor* table, const int32_t* 
   HT_TRY(ht_check_rows(ctx, H, H->rows, table->cols, "ht_embed_fwd: H"));
   if (ht_overlap(H, table)) return ht_set_err(ctx, HT_EINVAL, "ht_embed_fwd: H shares memory with table");
   HT_HIP(ctx, hipSetDevice(ctx->device));
-  const int nv = (table->cols + 3) / 4;
-  const int64_t n = H->rows;
-  with_lanes(nv, [&](auto lanes) {
-    constexpr int LPR = decltype(lanes)::value;
-    const int64_t rows = 256 / LPR * 4;
-    if (n > 0)
-      k_embed<LPR><<<(unsigned)ceil_div64(n, rows), 256, 0, ctx->stream>>>(table->ptr, table->ld, table->rows, ids, n, scale, H->ptr, H->ld, nv);
+  const int64_t nv = (table->cols + 3) / 4, n = H->rows;
+  if (n == 0) return HT_OK;
+  const bool past = n * nv * 16 >= EMBED_PAST;
+  // (a launch takes less than 2^32 threads)
+  return ht_in_launches(n, std::max<int64_t>(1, HT_LAUNCH_WAVES * 64 * EMBED_TURNS / nv), [&](int64_t i, int64_t m) {
+    const unsigned blocks = (unsigned)ceil_div64(m * nv, 256 * EMBED_TURNS);
+    float* to = H->ptr + i * H->ld;
+    if (past) k_embed<true><<<blocks, 256, 0, ctx->stream>>>(table->ptr, table->ld, table->rows, ids + i, m, scale, to, H->ld, (uint32_t)nv);
+    else k_embed<false><<<blocks, 256, 0, ctx->stream>>>(table->ptr, table->ld, table->rows, ids + i, m, scale, to, H->ld, (uint32_t)nv);
+    HT_LAUNCH_CHECK(ctx);
+    return (int)HT_OK;
   });
-  HT_LAUNCH_CHECK(ctx);
-  return HT_OK;
 }
 
 extern "C" int ht_embed_bwd(ht_ctx* ctx, const ht_tensor* dH, const int32_t* ids, float scale, int32_t accumulate, ht_tensor* dT) {
@@ -180,28 +275,35 @@ extern "C" int ht_embed_bwd(ht_ctx* ctx, const ht_tensor* dH, const int32_t* ids
   if (ht_overlap(dH, dT)) return ht_set_err(ctx, HT_EINVAL, "ht_embed_bwd: d_table shares memory with dH");
   HT_HIP(ctx, hipSetDevice(ctx->device));
   const int nv = (dT->cols + 3) / 4;
-  const int64_t n = dH->rows, V = dT->rows, tiles = ceil_div64(n, TS);
+  const int64_t n = dH->rows, V = dT->rows;
   int bits = 1;
   while (((int64_t)1 << bits) <= V) ++bits;
   return ht_with_room(ctx, [&]() -> int {
     OpsBlock m;
-    const auto keys = m.add<uint64_t>(n), tmp = m.add<uint64_t>(n);
-    const auto edge = m.add<float4>(tiles * 2 * nv);
+    const bool few = n <= EMBED_FEW;
+    const auto keys = m.add<uint64_t>(n), tmp = m.add<uint64_t>(few ? 0 : n);
+    const int E = GROUPS * (few ? TILE_FEW : TILE);
+    const int64_t blocks = ceil_div64(n, E);
+    const auto edge = m.add<float4>(blocks * 2 * nv);
     size_t rsort = 0, scan = 0;
-    ht_radix_wants(n, &rsort, &scan);
+    if (!few) ht_radix_wants(n, &rsort, &scan);
     HT_TRY(m.take(ctx, rsort, scan));
-    if (!accumulate && V > 0) HT_TRY(ht_fill_zero(ctx, ctx->stream, dT->ptr, (size_t)((V - 1) * dT->ld + dT->cols) * 4));
-    if (n == 0 || V == 0) return HT_OK;
-    k_embed_keys<<<(unsigned)ceil_div64(n, 256), 256, 0, ctx->stream>>>(ids, n, V, m.at(keys));
+    const EmbedClear clear{dT->ptr, accumulate || V == 0 ? 0 : (V - 1) * dT->ld + dT->cols};
+    const unsigned key_blocks = (unsigned)ceil_div64(n, few ? 16 : 256), clear_blocks = (unsigned)std::min<int64_t>(ceil_div64(clear.words, 1024), 4096);
+    if (key_blocks + clear_blocks == 0) return HT_OK;
+    uint64_t* sorted = m.at(keys);
+    if (few) k_embed_rank<<<key_blocks + clear_blocks, 256, (size_t)ceil_div64(n, 4) * 16, ctx->stream>>>(ids, (int)n, V, m.at(keys), key_blocks, clear);
+    else k_embed_keys<<<key_blocks + clear_blocks, 256, 0, ctx->stream>>>(ids, n, V, m.at(keys), key_blocks, clear);
     HT_LAUNCH_CHECK(ctx);
-    uint64_t* sorted = nullptr;
-    HT_TRY(ht_radix_sort_u64(ctx, m.at(keys), m.at(tmp), n, 32, 32 + bits, &sorted));
+    if (n == 0 || V == 0) return HT_OK;
+    if (!few) HT_TRY(ht_radix_sort_u64(ctx, m.at(keys), m.at(tmp), n, 32, 32 + bits, &sorted));
     const EmbedOut out{dT->ptr, dT->ld, V, scale, accumulate, nv};
     with_lanes(nv, [&](auto lanes) {
       constexpr int LPR = decltype(lanes)::value;
-      k_embed_sum<LPR><<<dim3((unsigned)ceil_div64(tiles, 256 / LPR), (unsigned)((nv + LPR - 1) / LPR)), 256, 0, ctx->stream>>>(sorted, n, dH->ptr, dH->ld, out,
-                                                                                                                            m.at(edge));
-      if (tiles > 1) k_embed_join<LPR><<<(unsigned)tiles, 256, 0, ctx->stream>>>(sorted, n, out, m.at(edge));
+      const dim3 grid((unsigned)blocks, (unsigned)((nv + LPR - 1) / LPR));
+      if (few) k_embed_sum<LPR, TILE_FEW><<<grid, LPR * GROUPS, 0, ctx->stream>>>(sorted, n, dH->ptr, dH->ld, out, m.at(edge));
+      else k_embed_sum<LPR, TILE><<<grid, LPR * GROUPS, 0, ctx->stream>>>(sorted, n, dH->ptr, dH->ld, out, m.at(edge));
+      if (blocks > 1) k_embed_join<LPR><<<(unsigned)(blocks - 1), 256, 0, ctx->stream>>>(sorted, n, E, out, m.at(edge));
     });
     HT_LAUNCH_CHECK(ctx);
     return HT_OK;
