@@ -783,6 +783,10 @@ extern "C" int ht_head_loss(ht_ctx* ctx, const ht_head_desc* desc, const ht_tens
   HT_HIP(ctx, hipSetDevice(ctx->device));
   return ht_with_room(ctx, [&]() -> int {
     auto run = [&](size_t bytes) { return head_run(ctx, desc, H, W, labels, row_weight, loss, row_loss, row_lse, dH, dW, bytes); };
+    if (H->rows > 0 && H->rows <= HT_HEAD_FEW && ht_may_spend(ctx)) {
+      const int rc = ht_head_few(ctx, desc, H, W, labels, row_weight, loss, row_loss, row_lse, dH, dW);
+      if (rc != HT_ENOMEM) return rc;
+    }
     const int rc = ht_may_spend(ctx) ? run(HEAD_BYTES) : (int)HT_ENOMEM;
     return rc == HT_ENOMEM ? run(HEAD_LEAN) : rc;      // (nothing has been launched by a call that is refused memory)
   });

@@ -1,0 +1,458 @@
+// ht_head_loss for at most 64 rows, where all there is to do is read W (twice for dH) and write dW: fp32 matrix instructions on W as it lies, no
+// copies of it.  The logits are at most a quarter of W's size and are kept between the launches (64 rows, 256 features): logits with each
+// block's maximum and sum | log sum exp, losses | gradients, a part of dH per block | dH.
+//
+// v_mfma_f32_16x16x4 takes 16 rows of either operand, lane l + 16 q value q of row l.  Which of a reduction's (or of an output's) values are value 0, 1, 2, 3 is
+// free as long as both operands agree, so that a lane can load four neighbours at once and use them in four instructions.
+#include <algorithm>
+#include <type_traits>
+
+#include "ht_internal.h"
+
+namespace {
+
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef float v4u __attribute__((ext_vector_type(4), aligned(4)));      // anywhere: weights need no alignment
+
+constexpr int KC = 128, HP = KC + 4;         // features of H in LDS at a time, and their pitch
+constexpr int CT = 64, PP = CT + 4;          // classes of a tile of gradients, and its pitch
+constexpr int JT = 256;                      // features of a block's gradients
+constexpr float LOG2E = 1.44269504088896340736f;
+
+__device__ __forceinline__ float exp_less(float x, float m) { return __builtin_amdgcn_exp2f((x - m) * LOG2E); }
+
+// The labelled rows among V <= 64, found by every wave for itself.
+struct FewRows {
+  uint64_t mask;
+  int n;
+  __device__ __forceinline__ FewRows(const int32_t* labels, int64_t V, int* idx, int32_t* lab) {
+    const int lane = threadIdx.x & 63;
+    const int32_t y = lane < V ? labels[lane] : -1;
+    mask = __ballot(y >= 0);
+    n = __popcll(mask);
+    if (threadIdx.x < 64) {
+      idx[lane] = 0, lab[lane] = -1;
+      __builtin_amdgcn_wave_barrier();
+      if (y >= 0) {
+        const int at = __popcll(mask & ((1ull << lane) - 1));
+        idx[at] = lane, lab[at] = y;
+      }
+    }
+    __syncthreads();
+  }
+};
+
+// W's values at p[0 .. 3], of which `left` are there; the others are 0.
+__device__ __forceinline__ v4f load4(const float* p, int left) {
+  if (left >= 4) return *reinterpret_cast<const v4u*>(p);
+  v4f x = {0.f, 0.f, 0.f, 0.f};
+  if (left > 0) x[0] = p[0];
+  if (left > 1) x[1] = p[1];
+  if (left > 2) x[2] = p[2];
+  return x;
+}
+__device__ __forceinline__ void store4(float* p, v4f x, int left, int add) {
+  if (left >= 4) {
+    v4u* to = reinterpret_cast<v4u*>(p);
+    if (add) x += *to;
+    *to = x;
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 3; ++i)
+    if (i < left) p[i] = add ? p[i] + x[i] : x[i];
+}
+
+struct FewArgs {
+  const float* H;
+  int64_t ldh, V;
+  int d, C;
+  const float* W;
+  int64_t ldw;
+  const int32_t* labels;
+  float* X;                        // [NB * 16][ldx] logits (null: not wanted)
+  int64_t ldx;
+  float2* part;                    // [row][blocks]
+  int blocks;
+  float* xlab;                     // [row]
+};
+
+// 256 classes a block, 64 a wave, NB * 16 rows.  OUT_IN: four tiles of 16 neighbouring classes; else tile t has the classes 4 m + t.
+template <int NB, bool OUT_IN>
+__global__ void __launch_bounds__(256) k_few_logits(FewArgs a) {
+  __shared__ float Hs[NB * 16][HP];
+  __shared__ int idx[64];
+  __shared__ int32_t lab[64];
+  __shared__ float2 red[4][NB * 16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 15, q = lane >> 4;
+  const FewRows rows(a.labels, a.V, idx, lab);
+  const int64_t c0 = (int64_t)blockIdx.x * 256 + wave * 64;
+  v4f acc[4][NB];
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+#pragma unroll
+    for (int b = 0; b < NB; ++b) acc[t][b] = v4f{0.f, 0.f, 0.f, 0.f};
+  const float* Wp[4];
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    const int64_t c = c0 + t * 16 + l;
+    Wp[t] = a.W + (c < a.C ? c : a.C - 1) * a.ldw;
+  }
+  const int64_t cw = c0 + 4 * l, cl = a.C - cw;
+  const int cleft = cl >= 4 ? 4 : (int)cl;                 // (!OUT_IN)
+  for (int k0 = 0; k0 < a.d; k0 += KC) {
+    const int kc = a.d - k0 < KC ? a.d - k0 : KC;
+    if (k0 > 0) __syncthreads();
+    for (int i = threadIdx.x; i < NB * 16 * KC; i += 256) {
+      const int r = i / KC, k = i % KC;
+      Hs[r][k] = r < rows.n && k < kc ? a.H[idx[r] * a.ldh + k0 + k] : 0.f;
+    }
+    __syncthreads();
+    if (OUT_IN) {
+      auto step = [&](int s, const v4f* w) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          const v4f h = *reinterpret_cast<const v4f*>(&Hs[b * 16 + l][s * 16 + 4 * q]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) acc[t][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[t][i], h[i], acc[t][b], 0, 0, 0);
+        }
+      };
+      int s = 0;
+      for (; (s + 4) * 16 <= kc; s += 4) {
+        v4f w[4][4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+          for (int t = 0; t < 4; ++t) w[u][t] = *reinterpret_cast<const v4u*>(Wp[t] + k0 + (s + u) * 16 + 4 * q);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) step(s + u, w[u]);
+      }
+      for (; s * 16 < kc; ++s) {
+        v4f w[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) w[t] = load4(Wp[t] + k0 + s * 16 + 4 * q, kc - s * 16 - 4 * q);
+        step(s, w);
+      }
+    } else {
+      for (int s0 = 0; s0 * 4 < kc; s0 += 16) {
+        v4f w[16];
+#pragma unroll
+        for (int u = 0; u < 16; ++u) {
+          const int k = (s0 + u) * 4 + q;
+          w[u] = k < kc ? load4(a.W + (int64_t)(k0 + k) * a.ldw + cw, cleft) : v4f{0.f, 0.f, 0.f, 0.f};
+        }
+#pragma unroll
+        for (int u = 0; u < 16; ++u) {
+          if ((s0 + u) * 4 >= kc) break;
+#pragma unroll
+          for (int b = 0; b < NB; ++b) {
+            const float h = Hs[b * 16 + l][(s0 + u) * 4 + q];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) acc[t][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[u][t], h, acc[t][b], 0, 0, 0);
+          }
+        }
+      }
+    }
+  }
+  // a lane has row b * 16 + l and of each tile the classes number 4 q + r
+  auto cls = [&](int t, int r) { return OUT_IN ? c0 + t * 16 + 4 * q + r : c0 + 4 * (4 * q + r) + t; };
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    const int v = b * 16 + l;
+    float m = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        if (cls(t, r) >= a.C) acc[t][b][r] = -INFINITY;
+        m = fmaxf(m, acc[t][b][r]);
+      }
+    m = fmaxf(m, __shfl_xor(m, 16, 64));
+    m = fmaxf(m, __shfl_xor(m, 32, 64));
+    const float m1 = m == -INFINITY ? 0.f : m;
+    float z = 0.f;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) z += exp_less(acc[t][b][r], m1);
+    z += __shfl_xor(z, 16, 64);
+    z += __shfl_xor(z, 32, 64);
+    if (q == 0) red[wave][v] = make_float2(m, z);
+    if (v < rows.n) {
+      const int32_t y = lab[v];
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (cls(t, r) == y) a.xlab[v] = acc[t][b][r];
+      if (a.X) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const v4f x = OUT_IN ? acc[k][b] : v4f{acc[0][b][k], acc[1][b][k], acc[2][b][k], acc[3][b][k]};
+          *reinterpret_cast<v4f*>(a.X + v * a.ldx + (OUT_IN ? c0 + k * 16 + 4 * q : c0 + 16 * q + 4 * k)) = x;
+        }
+      }
+    }
+  }
+  __syncthreads();
+  if ((int)threadIdx.x < rows.n) {
+    const int v = threadIdx.x;
+    float m = -INFINITY, z = 0.f;
+    for (int w = 0; w < 4; ++w) m = fmaxf(m, red[w][v].x);
+    for (int w = 0; w < 4; ++w) z += red[w][v].x == -INFINITY ? red[w][v].y : red[w][v].y * exp_less(red[w][v].x, m);
+    a.part[(int64_t)v * a.blocks + blockIdx.x] = make_float2(m, z);
+  }
+}
+
+// One block: a wave a row.  lse: of the labelled rows in order.
+__global__ void __launch_bounds__(1024) k_few_join(FewArgs a, const float* __restrict__ weight, int mean, float* __restrict__ lse_of, float* __restrict__ row_loss,
+                                                   float* __restrict__ row_lse, float* __restrict__ loss) {
+  __shared__ int idx[64];
+  __shared__ int32_t lab[64];
+  __shared__ double sh[16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const FewRows rows(a.labels, a.V, idx, lab);
+  if (wave == 0 && lane < a.V && !((rows.mask >> lane) & 1)) {
+    if (row_loss) row_loss[lane] = 0.f;
+    if (row_lse) row_lse[lane] = 0.f;
+  }
+  double mine = 0.0;
+  for (int v = wave; v < rows.n; v += 16) {
+    float m = -INFINITY, z = 0.f;
+#pragma unroll 4
+    for (int t = lane; t < a.blocks; t += 64) {
+      const float2 p = a.part[(int64_t)v * a.blocks + t];
+      const float n = fmaxf(m, p.x);
+      z = (m == -INFINITY ? z : z * exp_less(m, n)) + (p.x == -INFINITY ? p.y : p.y * exp_less(p.x, n));
+      m = n;
+    }
+    float all = m;
+    for (int o = 32; o > 0; o >>= 1) all = fmaxf(all, __shfl_xor(all, o, 64));
+    z = m == -INFINITY ? z : z * exp_less(m, all);
+    for (int o = 32; o > 0; o >>= 1) z += __shfl_xor(z, o, 64);
+    const float lse = all + logf(z), l = lab[v] < a.C ? lse - a.xlab[v] : NAN;
+    if (lane == 0) {
+      lse_of[v] = lse;
+      if (row_loss) row_loss[idx[v]] = l;
+      if (row_lse) row_lse[idx[v]] = lse;
+      mine += weight ? (double)weight[idx[v]] * (double)l : (double)l;
+    }
+  }
+  if (lane == 0) sh[wave] = mine;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    double s = 0.0;
+    for (int w = 0; w < 16; ++w) s += sh[w];
+    *loss = rows.n > 0 ? (float)(s / (mean ? (double)rows.n : 1.0)) : 0.f;
+  }
+}
+
+struct FewGrad {
+  const float* weight;
+  const float* lse;
+  int mean, add;
+  float* dW;                       // (null: not wanted), pitch ldd
+  int64_t ldd;
+  float* part;                     // [block][NB * 16][d] of dH (null: not wanted)
+  int tiles;                       // of CT classes
+};
+
+// Classes in tiles of CT, a contiguous part of them a block; JT features, 64 a wave.
+template <int NB, bool OUT_IN>
+__global__ void __launch_bounds__(256) k_few_grad(FewArgs a, FewGrad g) {
+  __shared__ float Ps[NB * 16][PP];
+  __shared__ int idx[64];
+  __shared__ int32_t lab[64];
+  __shared__ float lse[64], scale[64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 15, q = lane >> 4;
+  const FewRows rows(a.labels, a.V, idx, lab);
+  if (threadIdx.x < 64) {
+    const int v = threadIdx.x;
+    const bool there = v < rows.n;
+    lse[v] = there ? g.lse[v] : 0.f;
+    scale[v] = there ? (g.weight ? g.weight[idx[v]] : 1.f) * (g.mean ? 1.f / (float)rows.n : 1.f) : 0.f;
+  }
+  const int j0 = blockIdx.y * JT + wave * 64, jl = j0 + 4 * l, jleft = a.d - jl;      // the lane's four features, and how many of them there are
+  v4f h[NB * 4];                   // row 4 s + q
+#pragma unroll
+  for (int s = 0; s < NB * 4; ++s) {
+    const int v = s * 4 + q;
+    h[s] = g.dW && v < rows.n ? load4(a.H + idx[v] * a.ldh + jl, jleft) : v4f{0.f, 0.f, 0.f, 0.f};
+  }
+  v4f sum[4][NB];
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+#pragma unroll
+    for (int b = 0; b < NB; ++b) sum[t][b] = v4f{0.f, 0.f, 0.f, 0.f};
+  const int t0 = (int)((int64_t)g.tiles * blockIdx.x / gridDim.x), t1 = (int)((int64_t)g.tiles * (blockIdx.x + 1) / gridDim.x);
+  for (int tile = t0; tile < t1; ++tile) {
+    const int64_t c0 = (int64_t)tile * CT;
+    // W for dH: OUT_IN four rows of a step of 16 classes; else four columns of a step, of each of four tiles of 16 features
+    v4f w[4][4];
+    auto fetch = [&](int s) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (OUT_IN) {
+          const int64_t c = c0 + s * 16 + 4 * q + k;
+          w[s & 3][k] = c < a.C ? load4(a.W + c * a.ldw + jl, jleft) : v4f{0.f, 0.f, 0.f, 0.f};
+        } else {
+          const int j = j0 + k * 16 + l;
+          const int64_t c = c0 + s * 16 + 4 * q, left = a.C - c;
+          w[s & 3][k] = j < a.d ? load4(a.W + (int64_t)j * a.ldw + c, left >= 4 ? 4 : (int)left) : v4f{0.f, 0.f, 0.f, 0.f};
+        }
+      }
+    };
+    if (g.part) {
+#pragma unroll
+      for (int s = 0; s < 4; ++s) fetch(s);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < NB * 16 * (CT / 4); i += 256) {
+      const int v = i / (CT / 4), c = i % (CT / 4) * 4;
+      v4f p = {0.f, 0.f, 0.f, 0.f};
+      if (v < rows.n) {
+        const v4f x = *reinterpret_cast<const v4f*>(a.X + v * a.ldx + c0 + c);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (c0 + c + k < a.C) p[k] = (exp_less(x[k], lse[v]) - (c0 + c + k == lab[v] ? 1.f : 0.f)) * scale[v];
+      }
+      *reinterpret_cast<v4f*>(&Ps[v][c]) = p;
+    }
+    __syncthreads();
+    if (g.dW) {
+      if (OUT_IN) {
+#pragma unroll
+        for (int ct = 0; ct < 4; ++ct) {
+          v4f o[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[i] = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int s = 0; s < NB * 4; ++s) {
+            const float p = Ps[s * 4 + q][ct * 16 + l];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(p, h[s][i], o[i], 0, 0, 0);
+          }
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int64_t c = c0 + ct * 16 + 4 * q + r;
+            if (c < a.C && jleft > 0) store4(g.dW + c * g.ldd + jl, v4f{o[0][r], o[1][r], o[2][r], o[3][r]}, jleft, g.add);
+          }
+        }
+      } else {
+        const int64_t cl = a.C - c0 - 4 * l;
+        const int cleft = cl >= 4 ? 4 : (int)cl;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {          // features 4 m + i
+          v4f o[4];
+#pragma unroll
+          for (int t = 0; t < 4; ++t) o[t] = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int s = 0; s < NB * 4; ++s) {
+            const v4f p = *reinterpret_cast<const v4f*>(&Ps[s * 4 + q][4 * l]);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) o[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(h[s][i], p[t], o[t], 0, 0, 0);
+          }
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int j = j0 + 4 * (4 * q + r) + i;
+            if (j < a.d && cleft > 0) store4(g.dW + (int64_t)j * g.ldd + c0 + 4 * l, v4f{o[0][r], o[1][r], o[2][r], o[3][r]}, cleft, g.add);
+          }
+        }
+      }
+    }
+    if (g.part) {
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          const v4f p = *reinterpret_cast<const v4f*>(&Ps[b * 16 + l][s * 16 + 4 * q]);
+#pragma unroll
+          for (int k = 0; k < 4; ++k)          // value k of the lane's four classes
+#pragma unroll
+            for (int t = 0; t < 4; ++t) sum[t][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(p[k], OUT_IN ? w[s][k][t] : w[s][t][k], sum[t][b], 0, 0, 0);
+        }
+    }
+  }
+  if (!g.part) return;
+  // a lane has the rows b * 16 + 4 q + r and a feature of each tile: OUT_IN 4 l + t, else t * 16 + l
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int v = b * 16 + 4 * q + r;
+      if (v >= rows.n) continue;
+      float* o = g.part + ((int64_t)blockIdx.x * (NB * 16) + v) * a.d;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const int j = OUT_IN ? jl + t : j0 + t * 16 + l;
+        if (j < a.d) o[j] = sum[t][b][r];
+      }
+    }
+}
+
+// dH: rows of 64 features a block, 16 parts of the blocks' sums each
+__global__ void __launch_bounds__(1024) k_few_dh(FewArgs a, const float* __restrict__ part, int blocks, int rows16, float* __restrict__ dH, int64_t ld) {
+  __shared__ int idx[64];
+  __shared__ int32_t lab[64];
+  __shared__ float sh[16][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const FewRows rows(a.labels, a.V, idx, lab);
+  const int v = blockIdx.x, j = blockIdx.y * 64 + lane;
+  if (!((rows.mask >> v) & 1)) {
+    if (wave == 0 && j < a.d) dH[v * ld + j] = 0.f;
+    return;
+  }
+  const int at = __popcll(rows.mask & ((1ull << v) - 1));
+  float s = 0.f;
+  if (j < a.d)
+#pragma unroll 8
+    for (int k = blocks * wave / 16; k < blocks * (wave + 1) / 16; ++k) s += part[((int64_t)k * rows16 + at) * a.d + j];
+  sh[wave][lane] = s;
+  __syncthreads();
+  if (wave == 0 && j < a.d) {
+    for (int w = 1; w < 16; ++w) s += sh[w][lane];
+    dH[v * ld + j] = s;
+  }
+}
+
+}  // namespace
+
+int ht_head_few(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_tensor* W, const int32_t* labels, const float* weight, float* loss, float* row_loss,
+                float* row_lse, const ht_tensor* dH, const ht_tensor* dW) {
+  const bool out_in = D->w_form == HT_W_OUT_IN, grad = dH || dW;
+  const int mean = D->reduction == HT_REDUCE_MEAN, d = D->d, C = D->n_classes;
+  const int NB = H->rows <= 16 ? 1 : H->rows <= 32 ? 2 : 4;
+  const int blocks = (int)ceil_div64(C, 256), tiles = (int)ceil_div64(C, CT);
+  const int64_t ldx = (int64_t)blocks * 256;
+  const int gy = (int)ceil_div64(d, JT), gx = (int)std::min<int64_t>(tiles, std::max(64, 512 / gy));
+  hipStream_t st = ctx->stream;
+  OpsBlock m;
+  const auto X = m.add<float>(grad ? NB * 16 * ldx : 0);
+  const auto part = m.add<float2>((int64_t)64 * blocks);
+  const auto xlab = m.add<float>(64), lse = m.add<float>(64);
+  const auto ph = m.add<float>(dH ? (int64_t)gx * NB * 16 * d : 0);
+  HT_TRY(m.take(ctx));
+  const FewArgs a{H->ptr, H->ld, H->rows, d, C, W->ptr, W->ld, labels, grad ? m.at(X) : nullptr, ldx, m.at(part), blocks, m.at(xlab)};
+  const FewGrad g{weight, m.at(lse), mean, D->accumulate_dW, dW ? dW->ptr : nullptr, dW ? dW->ld : 0, dH ? m.at(ph) : nullptr, tiles};
+  auto run = [&](auto nb, auto form) -> int {
+    constexpr int N = decltype(nb)::value;
+    constexpr bool F = decltype(form)::value;
+    k_few_logits<N, F><<<(unsigned)blocks, 256, 0, st>>>(a);
+    HT_LAUNCH_CHECK(ctx);
+    k_few_join<<<1, 1024, 0, st>>>(a, weight, mean, m.at(lse), row_loss, row_lse, loss);
+    HT_LAUNCH_CHECK(ctx);
+    if (!grad) return HT_OK;
+    k_few_grad<N, F><<<dim3((unsigned)gx, (unsigned)gy), 256, 0, st>>>(a, g);
+    HT_LAUNCH_CHECK(ctx);
+    return HT_OK;
+  };
+  auto with_form = [&](auto nb) { return out_in ? run(nb, std::true_type()) : run(nb, std::false_type()); };
+  HT_TRY(NB == 1 ? with_form(std::integral_constant<int, 1>()) : NB == 2 ? with_form(std::integral_constant<int, 2>()) : with_form(std::integral_constant<int, 4>()));
+  if (dH) {
+    k_few_dh<<<dim3((unsigned)H->rows, (unsigned)ceil_div64(d, 64)), 1024, 0, st>>>(a, m.at(ph), gx, NB * 16, dH->ptr, dH->ld);
+    HT_LAUNCH_CHECK(ctx);
+  }
+  return HT_OK;
+}

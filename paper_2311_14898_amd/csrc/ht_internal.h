@@ -675,6 +675,11 @@ size_t ht_gemm_groups_bytes(int32_t K, int32_t N, const std::vector<int64_t>& gr
 int ht_agg_update_fused(ht_ctx* ctx, hipStream_t st, const ht_graph* g, const ChunkMeta& c, const float* H_in, int64_t in_ld,
                         int32_t d_in, const float* W, int32_t d_out, int relu, float* H_out, int64_t out_ld);
 
+// ht_head_loss of at most HT_HEAD_FEW rows (ht_head_few.hip)
+constexpr int HT_HEAD_FEW = 64;
+int ht_head_few(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_tensor* W, const int32_t* labels, const float* weight, float* loss, float* row_loss,
+                float* row_lse, const ht_tensor* dH, const ht_tensor* dW);
+
 // Elementwise / loss (ht_elem.hip)
 // dz = dh * [ref > 0]
 int ht_relu_mask(ht_ctx* ctx, hipStream_t st, const float* dh, int64_t ld_dh, const float* ref, int64_t ld_ref,
