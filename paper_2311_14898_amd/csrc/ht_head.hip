@@ -30,7 +30,10 @@ constexpr int TM = 256, TN = 128;      // tile of a block: rows of A x rows of B
 constexpr float LOG2E = 1.44269504088896340736f;
 constexpr int P_EXP = 15;              // gradients of logits are held times 2^15
 constexpr size_t HEAD_BYTES = (size_t)6 << 30, HEAD_LEAN = (size_t)64 << 20;   // of what a piece's rows take
-constexpr int64_t HEAD_CLASSES = 8192;             // of a piece
+// Bytes of a piece's gradients of logits, at most.  us with pieces of 8,192 classes | 16,384 | 32,768 | of 2 GiB | 6 GiB: 8,192 rows x 131,072 classes x 256 8,152 | 7,708 | 7,502 | 7,538
+// | 7,795; 2,048 x 32,768 685 | 687 | 607 | 605 | 606; 2,100 of 7,001 rows x 50,003 x 602 2,691 | 2,521 | 2,339 | 2,322 | 2,302; 128 x 131,072 x 256 1,394 | | | 640 | 640.
+constexpr size_t HEAD_PIECE = (size_t)2 << 30;
+constexpr int64_t HEAD_CLASSES = 8192;             // of a piece at least, where a row's share of the memory is settled
 
 __host__ __device__ constexpr int64_t up_to(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
@@ -620,10 +623,12 @@ HeadPlan head_plan(int64_t V, int64_t d, int64_t C, bool in_out, size_t bytes) {
   p.KSd = up_to(d, PAIR) / 16;
   p.Cpad = up_to(C, TM);
   p.dpad = up_to(d, TM);
-  p.Cp = std::min<int64_t>(p.Cpad, HEAD_CLASSES);
   // a row takes 4 bytes a value of its own, by rows and by features, and of its gradient, 8 a class of the piece, and 8 a tile of classes
-  p.Rp = (int64_t)(bytes / (size_t)(8 * p.Cp + 12 * p.dpad + 8 * (p.Cpad / TM))) / TM * TM;
+  const int64_t own = 12 * p.dpad + 8 * (p.Cpad / TM), least = std::min<int64_t>(p.Cpad, HEAD_CLASSES);
+  p.Rp = (int64_t)bytes / (8 * least + own) / TM * TM;
   p.Rp = std::max<int64_t>(TM, std::min(p.Rp, up_to(V, TM)));
+  // ... and as many classes as memory allows: every piece of them reads and writes the sums that dH is made of
+  p.Cp = std::max(least, std::min<int64_t>(p.Cpad, (int64_t)std::min(bytes, HEAD_PIECE) / (8 * p.Rp) / TM * TM));
   auto splits = [](int64_t tiles, int64_t steps) {      // parts of a reduction: two blocks a CU, and 512 values each at least
     return (int)std::max<int64_t>(1, std::min<int64_t>({512 / std::max<int64_t>(tiles, 1), steps / 32, 32}));
   };
