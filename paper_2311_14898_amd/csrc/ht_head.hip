@@ -17,9 +17,8 @@
 namespace {
 
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
-typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 typedef float v16f __attribute__((ext_vector_type(16)));
-typedef float v2f __attribute__((ext_vector_type(2)));
+typedef float V4 __attribute__((ext_vector_type(4)));
 
 // Operands lie in fragments, what a matrix instruction reads of them: 32 rows x 16 values of the reduction of one plane (x0 or x1), 1 KiB.
 // Lane l + 32 h holds row l and the values 8 (t / 4) + 4 h + t % 4, t = 0 .. 7: the order in which a lane of a product's result holds
@@ -52,9 +51,16 @@ __device__ __forceinline__ float unscale_of(uint32_t bits) { return __uint_as_fl
 // ---------------------------------------------------------------- labelled rows
 
 constexpr int ROW_BLOCKS = 4096;
+constexpr int64_t CLEAR_BLOCKS = 8192;
 
-__global__ void __launch_bounds__(256) k_head_count(const int32_t* __restrict__ labels, int64_t V, int64_t rpb, int32_t* __restrict__ cnt) {
+// Labelled rows of the first `blocks` blocks' shares; the other blocks clear n4 fours of words.
+__global__ void __launch_bounds__(256) k_head_count(const int32_t* __restrict__ labels, int64_t V, int64_t rpb, int32_t* __restrict__ cnt, unsigned blocks,
+                                                    uint4* __restrict__ clear, int64_t n4) {
   __shared__ int sh[4];
+  if (blockIdx.x >= blocks) {
+    for (int64_t i = (int64_t)(blockIdx.x - blocks) * 256 + threadIdx.x; i < n4; i += (int64_t)(gridDim.x - blocks) * 256) clear[i] = make_uint4(0, 0, 0, 0);
+    return;
+  }
   int n = 0;
   const int64_t v0 = (int64_t)blockIdx.x * rpb, v1 = v0 + rpb < V ? v0 + rpb : V;
   for (int64_t v = v0 + threadIdx.x; v < v1; v += 256) n += labels[v] >= 0;
@@ -64,13 +70,25 @@ __global__ void __launch_bounds__(256) k_head_count(const int32_t* __restrict__ 
   if (threadIdx.x == 0) cnt[blockIdx.x] = sh[0] + sh[1] + sh[2] + sh[3];
 }
 
-// idx, lab: the labelled rows in order, and their labels; *total: how many.  Rows without a label get their zeros here.
+// Zeros in dH's rows without a label, a wave 64 rows at a time.
+__global__ void __launch_bounds__(256) k_head_clear(const int32_t* __restrict__ labels, int64_t V, float* __restrict__ dH, int64_t ld, int d) {
+  const int lane = threadIdx.x & 63;
+  for (int64_t v0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * 64; v0 < V; v0 += (int64_t)gridDim.x * 256) {
+    uint64_t none = __ballot(v0 + lane < V && labels[v0 + lane < V ? v0 + lane : V - 1] < 0);
+    while (none) {
+      const int r = __builtin_ctzll(none);
+      none &= none - 1;
+      for (int c = lane * 4; c < d; c += 256) __builtin_nontemporal_store(V4{0.f, 0.f, 0.f, 0.f}, reinterpret_cast<V4*>(dH + (v0 + r) * ld + c));
+    }
+  }
+}
+
+// idx, lab: the labelled rows in order, and their labels; *total: how many.  Losses of rows without a label are cleared here.
 __global__ void __launch_bounds__(256) k_head_place(const int32_t* __restrict__ labels, int64_t V, int64_t rpb, const int32_t* __restrict__ cnt,
                                                     int32_t* __restrict__ idx, int32_t* __restrict__ lab, int64_t* __restrict__ total,
-                                                    float* __restrict__ row_loss, float* __restrict__ row_lse, float* __restrict__ dH, int64_t ld, int d) {
+                                                    float* __restrict__ row_loss, float* __restrict__ row_lse) {
   __shared__ int64_t sh64[4];
   __shared__ int sh[4];
-  __shared__ uint64_t have[4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int64_t at = 0;
   for (int b = threadIdx.x; b < (int)blockIdx.x; b += 256) at += cnt[b];
@@ -84,7 +102,7 @@ __global__ void __launch_bounds__(256) k_head_place(const int32_t* __restrict__ 
     const int32_t y = v < v1 ? labels[v] : -1;
     const uint64_t mask = __ballot(y >= 0);
     __syncthreads();
-    if (lane == 0) sh[wave] = __popcll(mask), have[wave] = mask;
+    if (lane == 0) sh[wave] = __popcll(mask);
     __syncthreads();
     int before = __popcll(mask & ((1ull << lane) - 1)), all = 0;
     for (int w = 0; w < 4; ++w) before += w < wave ? sh[w] : 0, all += sh[w];
@@ -96,12 +114,6 @@ __global__ void __launch_bounds__(256) k_head_place(const int32_t* __restrict__ 
       if (row_lse) row_lse[v] = 0.f;
     }
     at += all;
-    if (dH) {
-      const int64_t rows = v1 - w0 < 256 ? v1 - w0 : 256;
-      for (int r = wave; r < rows; r += 4)
-        if (!((have[r >> 6] >> (r & 63)) & 1))
-          for (int c = lane * 4; c < d; c += 256) *reinterpret_cast<float4*>(dH + (w0 + r) * ld + c) = make_float4(0.f, 0.f, 0.f, 0.f);
-    }
   }
   if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) *total = at;
 }
@@ -127,20 +139,21 @@ struct Source {
 };
 
 // Largest absolute values of rows, and of columns (of weighted rows), as bits, into arrays that hold zeros.  (Maxima do not depend on their order.)
-// A block takes groups of 64 rows by AMAX_COLS columns; columns are joined once a block.
+// A wave takes RW rows at a time, a block AMAX_COLS columns of them; columns are joined once a block.
 constexpr int AMAX_COLS = 512;
+template <int RW>
 __global__ void __launch_bounds__(256) k_amax(Source s, uint32_t* __restrict__ rmax, uint32_t* __restrict__ cmax) {
   constexpr int Q = AMAX_COLS / 64;
-  __shared__ uint32_t sh[4][AMAX_COLS];
+  __shared__ uint32_t sh[4][AMAX_COLS], shr[4 * RW];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t n = s.n(), c0 = (int64_t)blockIdx.y * AMAX_COLS + lane;
   uint32_t cm[Q];
 #pragma unroll
   for (int k = 0; k < Q; ++k) cm[k] = 0;
-  for (int64_t g0 = (int64_t)blockIdx.x * 64; g0 < n; g0 += (int64_t)gridDim.x * 64) {
-    const int64_t r0 = g0 + wave * 16;
+  for (int64_t g0 = (int64_t)blockIdx.x * (4 * RW); g0 < n; g0 += (int64_t)gridDim.x * (4 * RW)) {
+    const int64_t r0 = g0 + wave * RW;
 #pragma unroll 4
-    for (int q = 0; q < 16; ++q) {
+    for (int q = 0; q < RW; ++q) {
       const int64_t r = r0 + q < n ? r0 + q : n - 1, v = s.row(r);
       const float* p = s.p + v * s.ld;
       const float w = s.weight ? s.weight[v] : 1.f;
@@ -152,11 +165,15 @@ __global__ void __launch_bounds__(256) k_amax(Source s, uint32_t* __restrict__ r
         cm[k] = max(cm[k], __float_as_uint(fabsf(x * w)));
       }
       for (int o = 32; o > 0; o >>= 1) rm = max(rm, (uint32_t)__shfl_xor((int)rm, o, 64));
-      if (lane == 0) {
-        if (gridDim.y == 1) rmax[r] = rm;
-        else atomicMax(rmax + r, rm);
-      }
+      if (lane == 0) shr[wave * RW + q] = rm;
     }
+    // one request for the block's rows (one for every row: 256 x 131,072 107 us, like this 38)
+    __syncthreads();
+    if (threadIdx.x < 4 * RW && g0 + threadIdx.x < n) {
+      if (gridDim.y == 1) rmax[g0 + threadIdx.x] = shr[threadIdx.x];
+      else atomicMax(rmax + g0 + threadIdx.x, shr[threadIdx.x]);
+    }
+    __syncthreads();
   }
 #pragma unroll
   for (int k = 0; k < Q; ++k) sh[wave][k * 64 + lane] = cm[k];
@@ -164,13 +181,15 @@ __global__ void __launch_bounds__(256) k_amax(Source s, uint32_t* __restrict__ r
   for (int k = threadIdx.x; k < AMAX_COLS; k += 256) {
     const int64_t c = (int64_t)blockIdx.y * AMAX_COLS + k;
     const uint32_t m = max(max(sh[0][k], sh[1][k]), max(sh[2][k], sh[3][k]));
-    if (c < s.cols && m) atomicMax(cmax + c, m);
+    if (c < s.cols) atomicMax(cmax + c, m);
   }
 }
 constexpr int64_t AMAX_BLOCKS = 1024;
 void launch_amax(hipStream_t st, const Source& s, uint32_t* rmax, uint32_t* cmax) {
-  const int64_t gy = ceil_div64(s.cols, AMAX_COLS), gx = std::max<int64_t>(1, std::min(ceil_div64(s.rows, 64), AMAX_BLOCKS / gy));
-  k_amax<<<dim3((unsigned)gx, (unsigned)gy), 256, 0, st>>>(s, rmax, cmax);
+  const int64_t gy = ceil_div64(s.cols, AMAX_COLS), most = std::max<int64_t>(1, AMAX_BLOCKS / gy);
+  // (listed rows may be far fewer than there could be)
+  if (s.idx || ceil_div64(s.rows, 16) <= most) k_amax<4><<<dim3((unsigned)std::max<int64_t>(1, std::min(ceil_div64(s.rows, 16), most)), (unsigned)gy), 256, 0, st>>>(s, rmax, cmax);
+  else k_amax<16><<<dim3((unsigned)std::max<int64_t>(1, std::min(ceil_div64(s.rows, 64), most)), (unsigned)gy), 256, 0, st>>>(s, rmax, cmax);
 }
 
 __device__ __forceinline__ void split2(float x, _Float16* hi, _Float16* lo) {
@@ -185,8 +204,9 @@ __global__ void __launch_bounds__(256) k_pack(Source s, const uint32_t* __restri
   __shared__ float sh[64][65];
   __shared__ float wt[64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, half = lane >> 5;
-  const int64_t n = s.n(), r0 = (int64_t)(blockIdx.x / col_tiles) * 64, c0 = (int64_t)(blockIdx.x % col_tiles) * 64;
-  if (r0 >= up_to(n, row_tile)) return;
+  const int64_t n = s.n(), tiles = up_to(n, row_tile) / 64 * col_tiles;
+  for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+  const int64_t r0 = tile / col_tiles * 64, c0 = tile % col_tiles * 64;
 #pragma unroll
   for (int q = 0; q < 16; ++q) {
     const int r = wave * 16 + q;
@@ -235,11 +255,25 @@ __global__ void __launch_bounds__(256) k_pack(Source s, const uint32_t* __restri
       put(T, (c0 / 32 + b) * KS_t + r0 / 16 + ks, x);
     }
   }
+  __syncthreads();
+  }
 }
+constexpr int64_t PACK_BLOCKS = 16384;
 
 // ---------------------------------------------------------------- products
 
-enum { LOSS, GRAD, SUMS };
+enum { LOSS, GRAD, SUMS, DIRECT };
+// The sums of dH: as many parts of the reduction as there are blocks for, by the rows that there are, which the host does not know.
+struct HeadSplits {
+  int64_t blocks;                 // blocks of the launch, tiles of which have room in the sums
+  int64_t nt;                     // tiles along the features
+  int most;
+  __device__ __forceinline__ int splits(int64_t rows) const {
+    const int64_t tiles = up_to(rows, TM) / TM * nt, s = tiles > 0 ? blocks / tiles : 1;
+    return (int)(s < 1 ? 1 : s < most ? s : most);
+  }
+};
+__device__ __forceinline__ float inv_count(const int64_t* total, int mean) { return mean ? 1.f / (float)(*total > 0 ? *total : 1) : 1.f; }
 struct NtArgs {
   const _Float16 *A, *B;          // fragments; row blocks KSA, KSB steps apart
   int64_t KSA, KSB;
@@ -264,6 +298,11 @@ struct NtArgs {
   float* out;                     // [split][out_m x out_n]
   int64_t out_m, out_n;
   int add;
+  HeadSplits by_rows;             // rows_are 1: how often the reduction is split, and out_m, follow from the number of rows
+  // DIRECT: a part of dW, finished: [m_end x n_end] at out, pitch out_n
+  int64_t m_end, n_end;
+  const uint32_t* fmax;           // H's largest values by feature
+  int features_are_rows, mean;
 };
 
 // What a wave's lanes have written to LDS is there for its other lanes, and what they have read may be overwritten.
@@ -285,14 +324,17 @@ __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
   const int64_t rows = a.total ? piece_rows(a.total, a.r0, a.most) : 0;
   const int64_t mt = a.rows_are == 1 ? up_to(rows, TM) / TM : a.mt, nt = a.rows_are == 2 ? up_to(rows, TN) / TN : a.nt;
+  if (EPI == DIRECT && a.r0 > 0 && rows == 0) return;                      // (nothing to add)
+  const int splits = a.rows_are == 1 ? a.by_rows.splits(rows) : a.splits;
   // each XCD takes a contiguous part of the tiles, eight tiles of A over all of B after eight others
-  const int64_t tiles = mt * nt, per = (tiles + 7) / 8, t = (int64_t)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
-  if ((int64_t)(blockIdx.x >> 3) >= per || t >= tiles) return;
+  const int64_t tiles = mt * nt, per = (tiles * splits + 7) / 8, ts = (int64_t)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  if ((int64_t)(blockIdx.x >> 3) >= per || ts >= tiles * splits) return;
+  const int64_t split = ts / tiles, t = ts - split * tiles;
   const int64_t g = t / (8 * nt), gm = mt - g * 8 < 8 ? mt - g * 8 : 8, q = t - g * 8 * nt;
   const int64_t m0 = (g * 8 + q % gm) * TM, n0 = q / gm * TN;
   const int64_t pairs = (a.steps >= 0 ? a.steps : up_to(rows, PAIR) / 16) / (2 * KT);
-  const int64_t s0 = pairs * blockIdx.y / a.splits * 2;                     // its first stage
-  int todo = __builtin_amdgcn_readfirstlane((int)(pairs * (blockIdx.y + 1) / a.splits - s0 / 2));
+  const int64_t s0 = pairs * split / splits * 2;                     // its first stage
+  int todo = __builtin_amdgcn_readfirstlane((int)(pairs * (split + 1) / splits - s0 / 2));
 
   v16f acc[2][4];
 #pragma unroll
@@ -364,7 +406,7 @@ __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
   // lane l32 + 32 half of a 32 x 32 tile has column l32 and the rows 8 (e / 4) + 4 half + e % 4
   const int64_t mw = m0 + wave * 64;
   if constexpr (EPI == SUMS) {         // (whole tiles: what lies behind the last row and column is not looked at)
-    float* out = a.out + ((int64_t)blockIdx.y * a.out_m + mw + half * 4) * a.out_n + n0 + l32;
+    float* out = a.out + (split * (a.rows_are == 1 ? mt * TM : a.out_m) + mw + half * 4) * a.out_n + n0 + l32;
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -379,6 +421,42 @@ __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
         }
 #pragma unroll
         for (int e = 0; e < 16; ++e) out[(i * 32 + (e >> 2) * 8 + (e & 3)) * a.out_n + j * 32] = was[e] + acc[i][j][e];
+      }
+    return;
+  }
+  if constexpr (EPI == DIRECT) {
+    const float f = inv_count(a.total, a.mean) * (1.f / (1 << P_EXP));
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int64_t n = n0 + j * 32 + l32;
+        if (n >= a.n_end) continue;
+        float fs[16];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          if (a.features_are_rows) {
+            const uint4 x = *reinterpret_cast<const uint4*>(a.fmax + mw + i * 32 + k * 8 + half * 4);       // (whole tiles of them are there)
+            fs[k * 4] = unscale_of(x.x), fs[k * 4 + 1] = unscale_of(x.y), fs[k * 4 + 2] = unscale_of(x.z), fs[k * 4 + 3] = unscale_of(x.w);
+          } else {
+            fs[k * 4] = fs[k * 4 + 1] = fs[k * 4 + 2] = fs[k * 4 + 3] = unscale_of(a.fmax[n]);
+          }
+        }
+        float* out = a.out + (mw + i * 32 + half * 4) * a.out_n + n;
+        const int64_t left = a.m_end - (mw + i * 32 + half * 4);
+        if (left >= 28) {
+          float was[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) was[e] = a.add ? out[((e >> 2) * 8 + (e & 3)) * a.out_n] : 0.f;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) out[((e >> 2) * 8 + (e & 3)) * a.out_n] = was[e] + acc[i][j][e] * fs[e] * f;
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int r = (e >> 2) * 8 + (e & 3);
+            if (r < left) out[r * a.out_n] = (a.add ? out[r * a.out_n] : 0.f) + acc[i][j][e] * fs[e] * f;
+          }
+        }
       }
     return;
   }
@@ -574,21 +652,21 @@ __global__ void __launch_bounds__(256) k_head_loss(const double* __restrict__ pa
   if (threadIdx.x == 0) *loss = *total > 0 ? (float)(sh[0] / (mean ? (double)*total : 1.0)) : 0.f;
 }
 
-__device__ __forceinline__ float inv_count(const int64_t* total, int mean) { return mean ? 1.f / (float)(*total > 0 ? *total : 1) : 1.f; }
-
 // dH rows of a piece: the splits' sums, scaled
 constexpr int64_t DH_BLOCKS = 8192;
-__global__ void __launch_bounds__(256) k_head_dh(const float* __restrict__ sums, int splits, int64_t most, int64_t pitch, const int64_t* __restrict__ total,
+__global__ void __launch_bounds__(256) k_head_dh(const float* __restrict__ sums, HeadSplits by_rows, int64_t most, int64_t pitch, const int64_t* __restrict__ total,
                                                  int64_t r0, const int32_t* __restrict__ idx, const float* __restrict__ weight, int mean,
                                                  const uint32_t* __restrict__ wmax, float* __restrict__ dH, int64_t ld, int d) {
   const int64_t rows = piece_rows(total, r0, most);
-  const int nv = (d + 3) / 4;
+  const int nv = (d + 3) / 4, splits = by_rows.splits(rows);
+  const int64_t part = up_to(rows, TM) * pitch;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * nv; i += (int64_t)gridDim.x * 256) {
   const int64_t v = i / nv;
   const int c = (int)(i % nv) * 4;
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
   for (int k = 0; k < splits; ++k) {
-    const float4 x = *reinterpret_cast<const float4*>(sums + ((int64_t)k * most + v) * pitch + c);
+    const float4 x = *reinterpret_cast<const float4*>(sums + k * part + v * pitch + c);
     s.x += x.x, s.y += x.y, s.z += x.z, s.w += x.w;
   }
   const int64_t at = idx[r0 + v];
@@ -615,7 +693,9 @@ __global__ void __launch_bounds__(256) k_head_dw(const float* __restrict__ sums,
 struct HeadPlan {
   int64_t Cp, Rp, KSd;               // classes and rows of a piece, steps of a reduction over d
   int64_t Cpad, dpad;
-  int splits_h, splits_w;
+  int splits_w;
+  HeadSplits by_rows;
+  int64_t sum_rows;                  // of dH's sums
 };
 
 HeadPlan head_plan(int64_t V, int64_t d, int64_t C, bool in_out, size_t bytes) {
@@ -629,20 +709,23 @@ HeadPlan head_plan(int64_t V, int64_t d, int64_t C, bool in_out, size_t bytes) {
   p.Rp = std::max<int64_t>(TM, std::min(p.Rp, up_to(V, TM)));
   // ... and as many classes as memory allows: every piece of them reads and writes the sums that dH is made of
   p.Cp = std::max(least, std::min<int64_t>(p.Cpad, (int64_t)std::min(bytes, HEAD_PIECE) / (8 * p.Rp) / TM * TM));
-  auto splits = [](int64_t tiles, int64_t steps) {      // parts of a reduction: two blocks a CU, and 512 values each at least
-    return (int)std::max<int64_t>(1, std::min<int64_t>({512 / std::max<int64_t>(tiles, 1), steps / 32, 32}));
-  };
-  p.splits_h = splits(p.Rp / TM * (up_to(d, TN) / TN), p.Cp / 16);
-  p.splits_w = splits(in_out ? p.dpad / TM * (p.Cp / TN) : p.Cp / TM * (up_to(d, TN) / TN), p.Rp / 16);
+  // parts of a reduction: two blocks a CU, and 512 values each at least
+  auto splits = [](int64_t tiles, int64_t steps, int64_t most) { return (int)std::max<int64_t>(1, std::min({512 / std::max<int64_t>(tiles, 1), steps / 32, most})); };
+  const int64_t nt = up_to(d, TN) / TN, mt = p.Rp / TM;
+  p.splits_w = splits(in_out ? p.dpad / TM * (p.Cp / TN) : p.Cp / TM * nt, p.Rp / 16, 32);
+  const int most = splits(nt, p.Cp / 16, 128);                        // (of one tile of rows)
+  p.by_rows = HeadSplits{std::max<int64_t>(mt * nt, std::min<int64_t>(512 / nt, mt * most) * nt), nt, most};
+  p.sum_rows = p.by_rows.blocks / nt * TM;
   return p;
 }
 
 int split_nt(ht_ctx* ctx, hipStream_t st, int epi, const NtArgs& a) {
-  const int64_t blocks = (a.mt * a.nt + 7) / 8 * 8;
+  const int64_t blocks = up_to(a.rows_are == 1 ? a.by_rows.blocks : a.mt * a.nt * a.splits, 8);
   if (blocks >= (1 << 24)) return ht_set_err(ctx, HT_ESHAPE, "head: %lld tiles in one product", (long long)blocks);
-  const dim3 grid((unsigned)blocks, (unsigned)(epi == SUMS ? a.splits : 1));
+  const unsigned grid = (unsigned)blocks;
   if (epi == LOSS) k_split_nt<LOSS><<<grid, 256, 0, st>>>(a);
   else if (epi == GRAD) k_split_nt<GRAD><<<grid, 256, 0, st>>>(a);
+  else if (epi == DIRECT) k_split_nt<DIRECT><<<grid, 256, 0, st>>>(a);
   else k_split_nt<SUMS><<<grid, 256, 0, st>>>(a);
   HT_LAUNCH_CHECK(ctx);
   return HT_OK;
@@ -664,8 +747,8 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
   const auto cnt = m.add<int32_t>(rb);
   const auto idx = m.add<int32_t>(V), lab = m.add<int32_t>(V);
   const auto total = m.add<int64_t>(1);
-  const auto wc = m.add<uint32_t>(p.Cpad + p.dpad);              // W's largest values by class, by feature
-  const auto hm = m.add<uint32_t>(p.Rp + p.dpad);                // H's by row, by feature
+  const int64_t n_max = p.Cpad + p.Rp + 2 * p.dpad;
+  const auto wc = m.add<uint32_t>(n_max);                        // W's largest values by class, by feature, H's by row, by feature
   const auto Wf = m.add<_Float16>(p.Cpad * p.KSd * 32);
   const auto Hf = m.add<_Float16>(p.Rp * p.KSd * 32);
   const auto part = m.add<float2>(ct * p.Rp);
@@ -674,17 +757,20 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
   const auto Wt = m.add<_Float16>(dH ? p.dpad * KSC * 32 : 0);
   const auto Ht = m.add<_Float16>(dW ? p.dpad * KSR * 32 : 0);
   const auto P = m.add<_Float16>(grad ? p.Rp * p.Cp * 2 : 0), PT = m.add<_Float16>(grad ? p.Rp * p.Cp * 2 : 0);
-  const auto sh = m.add<float>(dH ? p.splits_h * p.Rp * p.dpad : 0);
-  const auto sw = m.add<float>(dW ? p.splits_w * p.Cp * p.dpad : 0);
+  const auto sh = m.add<float>(dH ? p.sum_rows * p.dpad : 0);
+  const auto sw = m.add<float>(dW && p.splits_w > 1 ? p.splits_w * p.Cp * p.dpad : 0);
   HT_TRY(m.take(ctx));
 
-  k_head_count<<<(unsigned)rb, 256, 0, st>>>(labels, V, rpb, m.at(cnt));
+  uint32_t *wmax_c = m.at(wc), *wmax_j = wmax_c + p.Cpad, *hmax_v = wmax_j + p.dpad, *hmax_j = hmax_v + p.Rp;
+  const unsigned clear_blocks = (unsigned)std::min<int64_t>(ceil_div64(n_max, 4096), 1024);
+  k_head_count<<<(unsigned)rb + clear_blocks, 256, 0, st>>>(labels, V, rpb, m.at(cnt), (unsigned)rb, (uint4*)wmax_c, n_max / 4);
   HT_LAUNCH_CHECK(ctx);
-  k_head_place<<<(unsigned)rb, 256, 0, st>>>(labels, V, rpb, m.at(cnt), m.at(idx), m.at(lab), m.at(total), row_loss, row_lse,
-                                             dH ? dH->ptr : nullptr, dH ? dH->ld : 0, (int)d);
+  k_head_place<<<(unsigned)rb, 256, 0, st>>>(labels, V, rpb, m.at(cnt), m.at(idx), m.at(lab), m.at(total), row_loss, row_lse);
   HT_LAUNCH_CHECK(ctx);
-  uint32_t *wmax_c = m.at(wc), *wmax_j = wmax_c + p.Cpad, *hmax_v = m.at(hm), *hmax_j = hmax_v + p.Rp;
-  HT_TRY(ht_fill_zero(ctx, st, wmax_c, (size_t)(p.Cpad + p.dpad) * 4));
+  if (dH && V > 0) {
+    k_head_clear<<<(unsigned)std::min<int64_t>(ceil_div64(V, 256), CLEAR_BLOCKS), 256, 0, st>>>(labels, V, dH->ptr, dH->ld, (int)d);
+    HT_LAUNCH_CHECK(ctx);
+  }
   {
     const Source s{W->ptr, W->ld, W->rows, W->cols, nullptr, nullptr, nullptr, 0};
     uint32_t *r = in_out ? wmax_j : wmax_c, *c = in_out ? wmax_c : wmax_j;
@@ -692,17 +778,17 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
     HT_LAUNCH_CHECK(ctx);
     _Float16* wt = dH ? m.at(Wt) : nullptr;
     const int64_t rt = up_to(s.rows, in_out ? 64 : TM) / 64, cols_t = up_to(s.cols, in_out ? TM : 64) / 64;
-    k_pack<<<(unsigned)(rt * cols_t), 256, 0, st>>>(s, r, c, in_out ? wt : m.at(Wf), in_out ? KSC : p.KSd, in_out ? m.at(Wf) : wt, in_out ? p.KSd : KSC,
+    k_pack<<<(unsigned)std::min(rt * cols_t, PACK_BLOCKS), 256, 0, st>>>(s, r, c, in_out ? wt : m.at(Wf), in_out ? KSC : p.KSd, in_out ? m.at(Wf) : wt, in_out ? p.KSd : KSC,
                                                     in_out ? 64 : TM, (unsigned)cols_t);
     HT_LAUNCH_CHECK(ctx);
   }
   for (int64_t k = 0; k < pieces; ++k) {
     const int64_t r0 = k * p.Rp;
-    HT_TRY(ht_fill_zero(ctx, st, hmax_v, (size_t)(p.Rp + p.dpad) * 4));
+    if (k > 0) HT_TRY(ht_fill_zero(ctx, st, hmax_v, (size_t)(p.Rp + p.dpad) * 4));
     const Source s{H->ptr, H->ld, p.Rp, d, m.at(idx), weight, m.at(total), r0};
     launch_amax(st, s, hmax_v, hmax_j);
     HT_LAUNCH_CHECK(ctx);
-    k_pack<<<(unsigned)(p.Rp / 64 * ceil_div64(d, 64)), 256, 0, st>>>(s, hmax_v, hmax_j, m.at(Hf), p.KSd, dW ? m.at(Ht) : nullptr, KSR, TN,
+    k_pack<<<(unsigned)std::min(p.Rp / 64 * ceil_div64(d, 64), PACK_BLOCKS / 8), 256, 0, st>>>(s, hmax_v, hmax_j, m.at(Hf), p.KSd, dW ? m.at(Ht) : nullptr, KSR, TN,
                                                                      (unsigned)ceil_div64(d, 64));
     HT_LAUNCH_CHECK(ctx);
     NtArgs a{};
@@ -726,14 +812,14 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
         NtArgs h{};
         h.total = m.at(total), h.r0 = r0, h.most = p.Rp, h.rows_are = 1;
         h.A = m.at(P), h.KSA = p.Cp / 16, h.B = m.at(Wt), h.KSB = KSC, h.ksb0 = c0 / 16;
-        h.mt = p.Rp / TM, h.nt = up_to(d, TN) / TN, h.steps = cp / 16, h.splits = p.splits_h;
+        h.mt = p.Rp / TM, h.nt = up_to(d, TN) / TN, h.steps = cp / 16, h.by_rows = p.by_rows;
         h.out = m.at(sh), h.out_m = p.Rp, h.out_n = p.dpad, h.add = c0 > 0;
         HT_TRY(split_nt(ctx, st, SUMS, h));
       }
       if (dW) {
         NtArgs w{};
         w.total = m.at(total), w.r0 = r0, w.most = p.Rp, w.steps = -1, w.splits = p.splits_w;
-        w.out = m.at(sw);
+        w.out = p.splits_w > 1 ? m.at(sw) : nullptr;
         if (in_out) {
           w.A = m.at(Ht), w.B = m.at(PT), w.KSA = w.KSB = KSR;
           w.mt = p.dpad / TM, w.nt = cp / TN, w.out_m = p.dpad, w.out_n = p.Cp;
@@ -741,16 +827,22 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
           w.A = m.at(PT), w.B = m.at(Ht), w.KSA = w.KSB = KSR;
           w.mt = cp / TM, w.nt = up_to(d, TN) / TN, w.out_m = p.Cp, w.out_n = p.dpad;
         }
-        HT_TRY(split_nt(ctx, st, SUMS, w));
         const int64_t cls = std::min(cp, C - c0), rows = in_out ? d : cls, cols = in_out ? cls : d;
         float* out = dW->ptr + (in_out ? c0 : c0 * dW->ld);
+        if (p.splits_w == 1) {
+          w.out = out, w.out_n = dW->ld, w.m_end = rows, w.n_end = cols, w.fmax = hmax_j, w.features_are_rows = in_out, w.mean = mean;
+          w.add = k > 0 || D->accumulate_dW;
+          HT_TRY(split_nt(ctx, st, DIRECT, w));
+          continue;
+        }
+        HT_TRY(split_nt(ctx, st, SUMS, w));
         k_head_dw<<<(unsigned)ceil_div64(rows * cols, 256), 256, 0, st>>>(m.at(sw), p.splits_w, w.out_m, w.out_n, rows, cols, hmax_j, in_out, m.at(total), r0, mean,
                                                                           k > 0 || D->accumulate_dW, out, dW->ld);
         HT_LAUNCH_CHECK(ctx);
       }
     }
     if (dH) {
-      k_head_dh<<<(unsigned)std::min(ceil_div64(p.Rp * ((d + 3) / 4), 256), DH_BLOCKS), 256, 0, st>>>(m.at(sh), p.splits_h, p.Rp, p.dpad, m.at(total), r0, m.at(idx), weight, mean, wmax_j,
+      k_head_dh<<<(unsigned)std::min(ceil_div64(p.Rp * ((d + 3) / 4), 256), DH_BLOCKS), 256, 0, st>>>(m.at(sh), p.by_rows, p.Rp, p.dpad, m.at(total), r0, m.at(idx), weight, mean, wmax_j,
                                                                                  dH->ptr, dH->ld, (int)d);
       HT_LAUNCH_CHECK(ctx);
     }
