@@ -2,8 +2,7 @@
 //   x_vc = h_v . w_c ;  lse_v = log sum_c exp(x_vc) ;  loss = sum_v u_v (lse_v - x_vy) / N
 //   dx_vc = (u_v / N) (exp(x_vc - lse_v) - [c = y_v]) ;  dH = dx W^T ;  dW = H^T dx
 // Labelled rows are first listed, and only they are computed with.  Rows go in pieces: a pass over all classes gives lse; then, class piece
-// by class piece, the logits are computed again and leave as exp(x - lse) - [c = y], once grouped along classes (for dH) and once
-// along rows (for dW).  Four products of 2 n d C flops, the fewest possible without keeping n x C numbers.
+// by class piece, the logits are computed again and leave as exp(x - lse) - [c = y], which dH and dW are made of.  Four products of 2 n d C flops, the fewest possible without keeping n x C numbers.
 //
 // All of them are k_split_nt's: fp32 products on the fp16 matrix cores.  A value is split into two fp16 numbers, x = x0 + x1 (x0 its
 // rounding, x1 the rounding of what is left: |x - x0 - x1| <= 2^-22 |x|), after each row of an operand was scaled by a power of two
@@ -19,6 +18,7 @@ namespace {
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef float V4 __attribute__((ext_vector_type(4)));
+typedef float V4u __attribute__((ext_vector_type(4), aligned(4)));      // weights need no alignment
 
 // Operands lie in fragments, what a matrix instruction reads of them: 32 rows x 16 values of the reduction of one plane (x0 or x1), 1 KiB.
 // Lane l + 32 h holds row l and the values 8 (t / 4) + 4 h + t % 4, t = 0 .. 7: the order in which a lane of a product's result holds
@@ -292,35 +292,38 @@ struct NtArgs {
   float2* part;                   // LOSS: [class tile][most]: largest logit, sum of exponentials less it
   float* xlab;                    // LOSS: the label's logit
   const float* lse;               // GRAD
-  _Float16 *P, *PT;               // GRAD: fragments by rows (KSP steps), by classes (KST steps)
-  int64_t KSP, KST;
+  _Float16* P;                    // GRAD: fragments by rows (KSP steps)
+  int64_t KSP;
   // SUMS
-  float* out;                     // [split][out_m x out_n]
-  int64_t out_m, out_n;
+  float* out;                     // [split], split_part floats apart; row m of A and row n of B at m ms + n ns
+  int64_t split_part, ms, ns;
   int add;
-  HeadSplits by_rows;             // rows_are 1: how often the reduction is split, and out_m, follow from the number of rows
-  // DIRECT: a part of dW, finished: [m_end x n_end] at out, pitch out_n
+  HeadSplits by_rows;             // rows_are 1: how often the reduction is split follows from the number of rows, and split_part
+  // DIRECT: a part of dW, finished: m_end features by n_end classes
   int64_t m_end, n_end;
   const uint32_t* fmax;           // H's largest values by feature
-  int features_are_rows, mean;
+  int mean;
 };
 
-// What a wave's lanes have written to LDS is there for its other lanes, and what they have read may be overwritten.
-__device__ __forceinline__ void wave_sync() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+// Column `lane % 16` of four rows of 16, each 16 lanes for themselves, which name four of a row each.
+typedef _Float16 v4h __attribute__((ext_vector_type(4)));
+typedef short v4s __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ v4h turned(const _Float16* p) {
+  return __builtin_bit_cast(v4h, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)p));
 }
 
 constexpr int KT = 2, PAIR = 32 * KT;   // steps of a stage; values of the reduction in two stages, which go together
 // C = A B^T of fragments, 256 x 128 a block, 64 x 128 a wave.  A wave reads its own rows of A straight into registers, a stage ahead, and the four
 // waves share B through LDS, which is filled a stage ahead as well; two blocks a CU.
-template <int EPI>
+//
+// TURN: B is the transpose of what its fragments hold, rows of the reduction by 16s of its own rows (gradients of logits, rows by classes, for dW).  A stage is 32 rows of the
+// reduction by 128, and lies in LDS as in memory; ds_read_tr gives 16 lanes the columns of four rows of 16.  (Each half of a fragment starts 640 bytes after
+// the one before, so that what a quarter of the lanes reads lies in other banks than what the others do.)
+constexpr int TURN_HALF = 320;    // halfs
+template <int EPI, bool TURN>
 __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
-  constexpr int STAGE = TN / 32 * KT * 2 * FRAG;        // halfs
-  constexpr int TR_PITCH = 40;                          // dwords between classes in a transposed 32 x 32 tile
+  constexpr int STAGE = TURN ? TN / 16 * 4 * TURN_HALF : TN / 32 * KT * 2 * FRAG;        // halfs
   __shared__ __attribute__((aligned(16))) _Float16 Bs[2 * STAGE];
-  static_assert(4 * 32 * TR_PITCH * 4 <= sizeof(Bs), "the waves' transposed tiles fit where B was");
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
   const int64_t rows = a.total ? piece_rows(a.total, a.r0, a.most) : 0;
   const int64_t mt = a.rows_are == 1 ? up_to(rows, TM) / TM : a.mt, nt = a.rows_are == 2 ? up_to(rows, TN) / TN : a.nt;
@@ -345,7 +348,9 @@ __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
   const _Float16 *Ap0 = a.A + ((m0 / 32 + wave * 2) * a.KSA + s0 * KT) * 2 * FRAG + lane * 8, *Ap1 = Ap0 + a.KSA * 2 * FRAG;
-  const _Float16* Bp = a.B + ((n0 / 32 + wave) * a.KSB + a.ksb0 + s0 * KT) * 2 * FRAG + lane * 8;     // a wave brings one of the four row blocks
+  // a wave brings one of the four row blocks, or two of the eight 16s
+  const _Float16* Bp = a.B + (TURN ? s0 * a.KSB + n0 / 16 + wave * 2 : (n0 / 32 + wave) * a.KSB + a.ksb0 + s0 * KT) * 2 * FRAG + lane * 8;
+  const int64_t b_step = (TURN ? a.KSB : KT) * 2 * FRAG;
   v8h ra[2][KT][2][2], rb[KT * 2];    // [stage in turn][step][row block][plane]
   auto fetch = [&](int to) {          // of the stage that the pointers have come to
 #pragma unroll
@@ -357,13 +362,24 @@ __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
         ra[to][u][0][p] = *reinterpret_cast<const v8h*>(Ap0 + (u * 2 + p) * FRAG);
         ra[to][u][1][p] = *reinterpret_cast<const v8h*>(Ap1 + (u * 2 + p) * FRAG);
       }
-    Ap0 += KT * 2 * FRAG, Ap1 += KT * 2 * FRAG, Bp += KT * 2 * FRAG;
+    Ap0 += KT * 2 * FRAG, Ap1 += KT * 2 * FRAG, Bp += b_step;
   };
   auto stash = [&](int to) {
 #pragma unroll
-    for (int u = 0; u < KT * 2; ++u) *reinterpret_cast<v8h*>(Bs + to * STAGE + (wave * KT * 2 + u) * FRAG + lane * 8) = rb[u];
+    for (int u = 0; u < KT * 2; ++u)
+      *reinterpret_cast<v8h*>(Bs + to * STAGE + (TURN ? ((wave * 4 + u) * 2 + half) * TURN_HALF + l32 * 8 : (wave * KT * 2 + u) * FRAG + lane * 8)) = rb[u];
   };
   auto read_b = [&](v8h* b, int cur, int k) {          // k: step * 4 + row block
+    if (TURN) {
+      const int i = lane & 15, sixteen = (k & 3) * 2 + ((lane >> 4) & 1);
+      const _Float16* f = Bs + cur * STAGE + (sixteen * 4 + (i & 1)) * TURN_HALF + ((k >> 2) * 16 + half * 4 + (i >> 2)) * 8 + ((i >> 1) & 1) * 4;
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        const v4h lo = turned(f + p * 2 * TURN_HALF), hi = turned(f + p * 2 * TURN_HALF + 64);
+        b[p] = v8h{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      }
+      return;
+    }
     const _Float16* f = Bs + cur * STAGE + ((k & 3) * KT * 2 + (k >> 2) * 2) * FRAG + lane * 8;
     b[0] = *reinterpret_cast<const v8h*>(f);
     b[1] = *reinterpret_cast<const v8h*>(f + FRAG);
@@ -371,7 +387,7 @@ __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
   // (Loads have no condition, so that waits count only the loads that they wait for: the last stage fetches itself again.  The barriers to scheduling
   // keep them where they stand; they would be moved down to where they are used.)
   auto stage = [&](int cur, bool more) {
-    if (!more) Ap0 -= KT * 2 * FRAG, Ap1 -= KT * 2 * FRAG, Bp -= KT * 2 * FRAG;
+    if (!more) Ap0 -= KT * 2 * FRAG, Ap1 -= KT * 2 * FRAG, Bp -= b_step;
     v8h b[2][2];
     read_b(b[0], cur, 0);
     fetch(cur ^ 1);
@@ -406,58 +422,73 @@ __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
   // lane l32 + 32 half of a 32 x 32 tile has column l32 and the rows 8 (e / 4) + 4 half + e % 4
   const int64_t mw = m0 + wave * 64;
   if constexpr (EPI == SUMS) {         // (whole tiles: what lies behind the last row and column is not looked at)
-    float* out = a.out + (split * (a.rows_are == 1 ? mt * TM : a.out_m) + mw + half * 4) * a.out_n + n0 + l32;
+    float* out = a.out + split * (a.rows_are == 1 ? mt * TM * a.ms : a.split_part) + (mw + half * 4) * a.ms + (n0 + l32) * a.ns;
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        float was[16];
-        if (a.add) {
+        float* o = out + i * 32 * a.ms + j * 32 * a.ns;
+        if (a.ms == 1) {               // (fours of a lane's rows are neighbours)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) was[e] = out[(i * 32 + (e >> 2) * 8 + (e & 3)) * a.out_n + j * 32];
-        } else {
-#pragma unroll
-          for (int e = 0; e < 16; ++e) was[e] = 0.f;
+          for (int k = 0; k < 4; ++k) {
+            V4 x{acc[i][j][k * 4], acc[i][j][k * 4 + 1], acc[i][j][k * 4 + 2], acc[i][j][k * 4 + 3]};
+            if (a.add) x += *reinterpret_cast<const V4*>(o + k * 8);
+            *reinterpret_cast<V4*>(o + k * 8) = x;
+          }
+          continue;
         }
+        float was[16];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) out[(i * 32 + (e >> 2) * 8 + (e & 3)) * a.out_n + j * 32] = was[e] + acc[i][j][e];
+        for (int e = 0; e < 16; ++e) was[e] = a.add ? o[((e >> 2) * 8 + (e & 3)) * a.ms] : 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[((e >> 2) * 8 + (e & 3)) * a.ms] = was[e] + acc[i][j][e];
       }
     return;
   }
-  if constexpr (EPI == DIRECT) {
+  if constexpr (EPI == DIRECT) {       // m: features, n: classes
     const float f = inv_count(a.total, a.mean) * (1.f / (1 << P_EXP));
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < 2; ++i) {
+      const int64_t m = mw + i * 32 + half * 4, left = a.m_end - m;
+      float fs[16];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {    // (whole tiles of them are there)
+        const uint4 x = *reinterpret_cast<const uint4*>(a.fmax + m + k * 8);
+        fs[k * 4] = unscale_of(x.x), fs[k * 4 + 1] = unscale_of(x.y), fs[k * 4 + 2] = unscale_of(x.z), fs[k * 4 + 3] = unscale_of(x.w);
+      }
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int64_t n = n0 + j * 32 + l32;
         if (n >= a.n_end) continue;
-        float fs[16];
+        float* o = a.out + m * a.ms + n * a.ns;
+        if (a.ms == 1) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          if (a.features_are_rows) {
-            const uint4 x = *reinterpret_cast<const uint4*>(a.fmax + mw + i * 32 + k * 8 + half * 4);       // (whole tiles of them are there)
-            fs[k * 4] = unscale_of(x.x), fs[k * 4 + 1] = unscale_of(x.y), fs[k * 4 + 2] = unscale_of(x.z), fs[k * 4 + 3] = unscale_of(x.w);
-          } else {
-            fs[k * 4] = fs[k * 4 + 1] = fs[k * 4 + 2] = fs[k * 4 + 3] = unscale_of(a.fmax[n]);
+          for (int k = 0; k < 4; ++k) {
+            V4 x{acc[i][j][k * 4] * fs[k * 4] * f, acc[i][j][k * 4 + 1] * fs[k * 4 + 1] * f, acc[i][j][k * 4 + 2] * fs[k * 4 + 2] * f, acc[i][j][k * 4 + 3] * fs[k * 4 + 3] * f};
+            if (k * 8 + 4 <= left) {
+              if (a.add) x += *reinterpret_cast<const V4u*>(o + k * 8);
+              *reinterpret_cast<V4u*>(o + k * 8) = x;
+            } else {
+#pragma unroll
+              for (int e = 0; e < 3; ++e)
+                if (k * 8 + e < left) o[k * 8 + e] = (a.add ? o[k * 8 + e] : 0.f) + x[e];
+            }
           }
-        }
-        float* out = a.out + (mw + i * 32 + half * 4) * a.out_n + n;
-        const int64_t left = a.m_end - (mw + i * 32 + half * 4);
-        if (left >= 28) {
+        } else if (left >= 28) {
           float was[16];
 #pragma unroll
-          for (int e = 0; e < 16; ++e) was[e] = a.add ? out[((e >> 2) * 8 + (e & 3)) * a.out_n] : 0.f;
+          for (int e = 0; e < 16; ++e) was[e] = a.add ? o[((e >> 2) * 8 + (e & 3)) * a.ms] : 0.f;
 #pragma unroll
-          for (int e = 0; e < 16; ++e) out[((e >> 2) * 8 + (e & 3)) * a.out_n] = was[e] + acc[i][j][e] * fs[e] * f;
+          for (int e = 0; e < 16; ++e) o[((e >> 2) * 8 + (e & 3)) * a.ms] = was[e] + acc[i][j][e] * fs[e] * f;
         } else {
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             const int r = (e >> 2) * 8 + (e & 3);
-            if (r < left) out[r * a.out_n] = (a.add ? out[r * a.out_n] : 0.f) + acc[i][j][e] * fs[e] * f;
+            if (r < left) o[r * a.ms] = (a.add ? o[r * a.ms] : 0.f) + acc[i][j][e] * fs[e] * f;
           }
         }
       }
+    }
     return;
   }
   float cs[2][16];                 // what undoes the classes' scaling (cmax is there for whole tiles)
@@ -525,7 +556,6 @@ __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
     return;
   }
   if constexpr (EPI == GRAD) {
-    uint32_t* tr = reinterpret_cast<uint32_t*>(Bs) + wave * 32 * TR_PITCH;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int64_t v = n0 + j * 32 + l32;
@@ -550,7 +580,6 @@ __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
           for (int e = 0; e < 16; ++e)
             if (mine && off == i * 32 + (e >> 2) * 8 + half * 4 + (e & 3)) p[e] -= (float)(1 << P_EXP);
         }
-        uint32_t both[16];
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
           v8h hi, lo;
@@ -560,31 +589,8 @@ __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
             split2(p[ks * 8 + u], &x, &y);
             hi[u] = x;
             lo[u] = y;
-            both[ks * 8 + u] = (uint32_t)__builtin_bit_cast(uint16_t, x) | (uint32_t)__builtin_bit_cast(uint16_t, y) << 16;
           }
           _Float16* to = a.P + (((n0 / 32 + j) * a.KSP + (mw + i * 32) / 16 + ks) * 2) * FRAG + lane * 8;
-          *reinterpret_cast<v8h*>(to) = hi;
-          *reinterpret_cast<v8h*>(to + FRAG) = lo;
-        }
-        // the same 32 x 32 values with a class in each lane
-        wave_sync();
-#pragma unroll
-        for (int e = 0; e < 16; ++e) tr[((e >> 2) * 8 + half * 4 + (e & 3)) * TR_PITCH + l32] = both[e];
-        wave_sync();
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-          v8h hi, lo;
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const uint4 x = *reinterpret_cast<const uint4*>(tr + l32 * TR_PITCH + ks * 16 + h * 8 + half * 4);
-            const uint32_t y[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              hi[h * 4 + u] = __builtin_bit_cast(_Float16, (uint16_t)y[u]);
-              lo[h * 4 + u] = __builtin_bit_cast(_Float16, (uint16_t)(y[u] >> 16));
-            }
-          }
-          _Float16* to = a.PT + (((mw / 32 + i) * a.KST + (n0 + j * 32) / 16 + ks) * 2) * FRAG + lane * 8;
           *reinterpret_cast<v8h*>(to) = hi;
           *reinterpret_cast<v8h*>(to + FRAG) = lo;
         }
@@ -703,30 +709,31 @@ HeadPlan head_plan(int64_t V, int64_t d, int64_t C, bool in_out, size_t bytes) {
   p.KSd = up_to(d, PAIR) / 16;
   p.Cpad = up_to(C, TM);
   p.dpad = up_to(d, TM);
-  // a row takes 4 bytes a value of its own, by rows and by features, and of its gradient, 8 a class of the piece, and 8 a tile of classes
+  // a row takes 4 bytes a value of its own, by rows and by features, and of its gradient, 4 a class of the piece, and 8 a tile of classes
   const int64_t own = 12 * p.dpad + 8 * (p.Cpad / TM), least = std::min<int64_t>(p.Cpad, HEAD_CLASSES);
-  p.Rp = (int64_t)bytes / (8 * least + own) / TM * TM;
+  p.Rp = (int64_t)bytes / (4 * least + own) / TM * TM;
   p.Rp = std::max<int64_t>(TM, std::min(p.Rp, up_to(V, TM)));
   // ... and as many classes as memory allows: every piece of them reads and writes the sums that dH is made of
-  p.Cp = std::max(least, std::min<int64_t>(p.Cpad, (int64_t)std::min(bytes, HEAD_PIECE) / (8 * p.Rp) / TM * TM));
+  p.Cp = std::max(least, std::min<int64_t>(p.Cpad, (int64_t)std::min(bytes, HEAD_PIECE) / (4 * p.Rp) / TM * TM));
   // parts of a reduction: two blocks a CU, and 512 values each at least
   auto splits = [](int64_t tiles, int64_t steps, int64_t most) { return (int)std::max<int64_t>(1, std::min({512 / std::max<int64_t>(tiles, 1), steps / 32, most})); };
   const int64_t nt = up_to(d, TN) / TN, mt = p.Rp / TM;
-  p.splits_w = splits(in_out ? p.dpad / TM * (p.Cp / TN) : p.Cp / TM * nt, p.Rp / 16, 32);
+  p.splits_w = splits(p.dpad / TM * (p.Cp / TN), p.Rp / 16, 32);
   const int most = splits(nt, p.Cp / 16, 128);                        // (of one tile of rows)
   p.by_rows = HeadSplits{std::max<int64_t>(mt * nt, std::min<int64_t>(512 / nt, mt * most) * nt), nt, most};
   p.sum_rows = p.by_rows.blocks / nt * TM;
   return p;
 }
 
-int split_nt(ht_ctx* ctx, hipStream_t st, int epi, const NtArgs& a) {
+int split_nt(ht_ctx* ctx, hipStream_t st, int epi, const NtArgs& a, bool turn = false) {
   const int64_t blocks = up_to(a.rows_are == 1 ? a.by_rows.blocks : a.mt * a.nt * a.splits, 8);
   if (blocks >= (1 << 24)) return ht_set_err(ctx, HT_ESHAPE, "head: %lld tiles in one product", (long long)blocks);
   const unsigned grid = (unsigned)blocks;
-  if (epi == LOSS) k_split_nt<LOSS><<<grid, 256, 0, st>>>(a);
-  else if (epi == GRAD) k_split_nt<GRAD><<<grid, 256, 0, st>>>(a);
-  else if (epi == DIRECT) k_split_nt<DIRECT><<<grid, 256, 0, st>>>(a);
-  else k_split_nt<SUMS><<<grid, 256, 0, st>>>(a);
+  if (epi == LOSS) k_split_nt<LOSS, false><<<grid, 256, 0, st>>>(a);
+  else if (epi == GRAD) k_split_nt<GRAD, false><<<grid, 256, 0, st>>>(a);
+  else if (epi == DIRECT) k_split_nt<DIRECT, true><<<grid, 256, 0, st>>>(a);
+  else if (turn) k_split_nt<SUMS, true><<<grid, 256, 0, st>>>(a);
+  else k_split_nt<SUMS, false><<<grid, 256, 0, st>>>(a);
   HT_LAUNCH_CHECK(ctx);
   return HT_OK;
 }
@@ -756,7 +763,7 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
   const auto ploss = m.add<double>(pieces * jb);
   const auto Wt = m.add<_Float16>(dH ? p.dpad * KSC * 32 : 0);
   const auto Ht = m.add<_Float16>(dW ? p.dpad * KSR * 32 : 0);
-  const auto P = m.add<_Float16>(grad ? p.Rp * p.Cp * 2 : 0), PT = m.add<_Float16>(grad ? p.Rp * p.Cp * 2 : 0);
+  const auto P = m.add<_Float16>(grad ? p.Rp * p.Cp * 2 : 0);
   const auto sh = m.add<float>(dH ? p.sum_rows * p.dpad : 0);
   const auto sw = m.add<float>(dW && p.splits_w > 1 ? p.splits_w * p.Cp * p.dpad : 0);
   HT_TRY(m.take(ctx));
@@ -806,38 +813,34 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
       const int64_t cp = std::min(p.Cp, p.Cpad - c0);
       NtArgs g = a;
       g.c0 = c0, g.A = m.at(Wf) + c0 * p.KSd * 32, g.mt = cp / TM;
-      g.P = m.at(P), g.KSP = p.Cp / 16, g.PT = m.at(PT), g.KST = KSR;
+      g.P = m.at(P), g.KSP = p.Cp / 16;
       HT_TRY(split_nt(ctx, st, GRAD, g));
       if (dH) {
         NtArgs h{};
         h.total = m.at(total), h.r0 = r0, h.most = p.Rp, h.rows_are = 1;
         h.A = m.at(P), h.KSA = p.Cp / 16, h.B = m.at(Wt), h.KSB = KSC, h.ksb0 = c0 / 16;
         h.mt = p.Rp / TM, h.nt = up_to(d, TN) / TN, h.steps = cp / 16, h.by_rows = p.by_rows;
-        h.out = m.at(sh), h.out_m = p.Rp, h.out_n = p.dpad, h.add = c0 > 0;
+        h.out = m.at(sh), h.ms = p.dpad, h.ns = 1, h.add = c0 > 0;
         HT_TRY(split_nt(ctx, st, SUMS, h));
       }
       if (dW) {
         NtArgs w{};
         w.total = m.at(total), w.r0 = r0, w.most = p.Rp, w.steps = -1, w.splits = p.splits_w;
-        w.out = p.splits_w > 1 ? m.at(sw) : nullptr;
-        if (in_out) {
-          w.A = m.at(Ht), w.B = m.at(PT), w.KSA = w.KSB = KSR;
-          w.mt = p.dpad / TM, w.nt = cp / TN, w.out_m = p.dpad, w.out_n = p.Cp;
-        } else {
-          w.A = m.at(PT), w.B = m.at(Ht), w.KSA = w.KSB = KSR;
-          w.mt = cp / TM, w.nt = up_to(d, TN) / TN, w.out_m = p.Cp, w.out_n = p.dpad;
-        }
+        w.A = m.at(Ht), w.KSA = KSR, w.B = m.at(P), w.KSB = p.Cp / 16;
+        w.mt = p.dpad / TM, w.nt = cp / TN;
         const int64_t cls = std::min(cp, C - c0), rows = in_out ? d : cls, cols = in_out ? cls : d;
+        const int add = k > 0 || D->accumulate_dW;
         float* out = dW->ptr + (in_out ? c0 : c0 * dW->ld);
         if (p.splits_w == 1) {
-          w.out = out, w.out_n = dW->ld, w.m_end = rows, w.n_end = cols, w.fmax = hmax_j, w.features_are_rows = in_out, w.mean = mean;
-          w.add = k > 0 || D->accumulate_dW;
+          w.out = out, w.ms = in_out ? dW->ld : 1, w.ns = in_out ? 1 : dW->ld, w.m_end = d, w.n_end = cls, w.fmax = hmax_j, w.mean = mean, w.add = add;
           HT_TRY(split_nt(ctx, st, DIRECT, w));
           continue;
         }
-        HT_TRY(split_nt(ctx, st, SUMS, w));
-        k_head_dw<<<(unsigned)ceil_div64(rows * cols, 256), 256, 0, st>>>(m.at(sw), p.splits_w, w.out_m, w.out_n, rows, cols, hmax_j, in_out, m.at(total), r0, mean,
-                                                                          k > 0 || D->accumulate_dW, out, dW->ld);
+        const int64_t rows_p = in_out ? p.dpad : p.Cp, cols_p = in_out ? p.Cp : p.dpad;
+        w.out = m.at(sw), w.split_part = rows_p * cols_p, w.ms = in_out ? cols_p : 1, w.ns = in_out ? 1 : cols_p;
+        HT_TRY(split_nt(ctx, st, SUMS, w, true));
+        k_head_dw<<<(unsigned)ceil_div64(rows * cols, 256), 256, 0, st>>>(m.at(sw), p.splits_w, rows_p, cols_p, rows, cols, hmax_j, in_out, m.at(total), r0, mean, add,
+                                                                          out, dW->ld);
         HT_LAUNCH_CHECK(ctx);
       }
     }
