@@ -14,7 +14,6 @@ namespace {
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v4u __attribute__((ext_vector_type(4), aligned(4)));      // anywhere: weights need no alignment
 
-constexpr int KC = 128, HP = KC + 4;         // features of H in LDS at a time, and their pitch
 constexpr int CT = 64, PP = CT + 4;          // classes of a tile of gradients, and its pitch
 constexpr int JT = 256;                      // features of a block's gradients
 constexpr float LOG2E = 1.44269504088896340736f;
@@ -75,99 +74,95 @@ struct FewArgs {
   float2* part;                    // [row][blocks]
   int blocks;
   float* xlab;                     // [row]
+  unsigned* ticket;
 };
 
-// 256 classes a block, 64 a wave, NB * 16 rows.  OUT_IN: four tiles of 16 neighbouring classes; else tile t has the classes 4 m + t.
+// CT classes a block, NB * 16 rows, a quarter of the features a wave, in steps of 16: lane l + 16 q has features 4 q .. 4 q + 3 of a step, of row l of H, and of W OUT_IN the
+// same features of class t * 16 + l for each tile t, else of those features the classes 4 l + t.  U steps are loaded together; H comes out of the caches.
 template <int NB, bool OUT_IN>
 __global__ void __launch_bounds__(256) k_few_logits(FewArgs a) {
-  __shared__ float Hs[NB * 16][HP];
+  constexpr int U = 2;
+  __shared__ float sums[3][NB][16][64];    // of the waves that do not own the 16 rows
   __shared__ int idx[64];
   __shared__ int32_t lab[64];
-  __shared__ float2 red[4][NB * 16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 15, q = lane >> 4;
   const FewRows rows(a.labels, a.V, idx, lab);
-  const int64_t c0 = (int64_t)blockIdx.x * 256 + wave * 64;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.ticket = 0;
+  const int64_t c0 = (int64_t)blockIdx.x * CT;
   v4f acc[4][NB];
 #pragma unroll
   for (int t = 0; t < 4; ++t)
 #pragma unroll
     for (int b = 0; b < NB; ++b) acc[t][b] = v4f{0.f, 0.f, 0.f, 0.f};
-  const float* Wp[4];
+  const float *Wp[4], *Hp[NB];
+  int wleft = 4;                           // (!OUT_IN: classes of the lane that there are)
 #pragma unroll
   for (int t = 0; t < 4; ++t) {
     const int64_t c = c0 + t * 16 + l;
-    Wp[t] = a.W + (c < a.C ? c : a.C - 1) * a.ldw;
+    Wp[t] = OUT_IN ? a.W + (c < a.C ? c : a.C - 1) * a.ldw + 4 * q : a.W + (int64_t)(4 * q + t) * a.ldw + c0 + 4 * l;
   }
-  const int64_t cw = c0 + 4 * l, cl = a.C - cw;
-  const int cleft = cl >= 4 ? 4 : (int)cl;                 // (!OUT_IN)
-  for (int k0 = 0; k0 < a.d; k0 += KC) {
-    const int kc = a.d - k0 < KC ? a.d - k0 : KC;
-    if (k0 > 0) __syncthreads();
-    for (int i = threadIdx.x; i < NB * 16 * KC; i += 256) {
-      const int r = i / KC, k = i % KC;
-      Hs[r][k] = r < rows.n && k < kc ? a.H[idx[r] * a.ldh + k0 + k] : 0.f;
+  if (!OUT_IN) wleft = a.C - c0 - 4 * l >= 4 ? 4 : (int)(a.C - c0 - 4 * l);
+#pragma unroll
+  for (int b = 0; b < NB; ++b) Hp[b] = a.H + idx[b * 16 + l] * a.ldh + 4 * q;      // (rows that are not there: the first, whose products nobody looks at)
+  const int S = (a.d + 15) / 16, s0 = S * wave / 4, s1 = S * (wave + 1) / 4, whole = a.d / 16;
+  auto multiply = [&](const v4f (&w)[4], const v4f (&h)[NB]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) acc[t][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(OUT_IN ? w[t][i] : w[i][t], h[b][i], acc[t][b], 0, 0, 0);
+  };
+  int s = s0;
+  const int end = OUT_IN || c0 + CT <= a.C ? (s1 < whole ? s1 : whole) : s0;       // (steps without an edge)
+  for (; s + U <= end; s += U) {
+    v4f w[U][4], h[U][NB];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) w[u][t] = *reinterpret_cast<const v4u*>(OUT_IN ? Wp[t] + (s + u) * 16 : Wp[t] + (int64_t)(s + u) * 16 * a.ldw);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) h[u][b] = *reinterpret_cast<const v4f*>(Hp[b] + (s + u) * 16);
     }
-    __syncthreads();
-    if (OUT_IN) {
-      auto step = [&](int s, const v4f* w) {
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-          const v4f h = *reinterpret_cast<const v4f*>(&Hs[b * 16 + l][s * 16 + 4 * q]);
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int t = 0; t < 4; ++t) acc[t][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[t][i], h[i], acc[t][b], 0, 0, 0);
-        }
-      };
-      int s = 0;
-      for (; (s + 4) * 16 <= kc; s += 4) {
-        v4f w[4][4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-#pragma unroll
-          for (int t = 0; t < 4; ++t) w[u][t] = *reinterpret_cast<const v4u*>(Wp[t] + k0 + (s + u) * 16 + 4 * q);
-#pragma unroll
-        for (int u = 0; u < 4; ++u) step(s + u, w[u]);
-      }
-      for (; s * 16 < kc; ++s) {
-        v4f w[4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) w[t] = load4(Wp[t] + k0 + s * 16 + 4 * q, kc - s * 16 - 4 * q);
-        step(s, w);
-      }
-    } else {
-      for (int s0 = 0; s0 * 4 < kc; s0 += 16) {
-        v4f w[16];
-#pragma unroll
-        for (int u = 0; u < 16; ++u) {
-          const int k = (s0 + u) * 4 + q;
-          w[u] = k < kc ? load4(a.W + (int64_t)(k0 + k) * a.ldw + cw, cleft) : v4f{0.f, 0.f, 0.f, 0.f};
-        }
-#pragma unroll
-        for (int u = 0; u < 16; ++u) {
-          if ((s0 + u) * 4 >= kc) break;
-#pragma unroll
-          for (int b = 0; b < NB; ++b) {
-            const float h = Hs[b * 16 + l][(s0 + u) * 4 + q];
-#pragma unroll
-            for (int t = 0; t < 4; ++t) acc[t][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[u][t], h, acc[t][b], 0, 0, 0);
-          }
-        }
-      }
-    }
+    for (int u = 0; u < U; ++u) multiply(w[u], h[u]);
   }
+  for (; s < s1; ++s) {
+    const int left = a.d - s * 16 - 4 * q;           // the lane's features that there are
+    v4f w[4], h[NB];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) w[t] = OUT_IN ? load4(Wp[t] + s * 16, left) : load4(Wp[t] + (int64_t)s * 16 * a.ldw, t < left ? wleft : 0);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) h[b] = load4(Hp[b] + s * 16, left);
+    multiply(w, h);
+  }
+  // 16 rows b belong to wave b
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+    if (b != wave) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sums[(wave - b + 3) & 3][b][t * 4 + r][lane] = acc[t][b][r];
+    }
+  __syncthreads();
   // a lane has row b * 16 + l and of each tile the classes number 4 q + r
   auto cls = [&](int t, int r) { return OUT_IN ? c0 + t * 16 + 4 * q + r : c0 + 4 * (4 * q + r) + t; };
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
+    if (b != wave) continue;
     const int v = b * 16 + l;
     float m = -INFINITY;
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        if (cls(t, r) >= a.C) acc[t][b][r] = -INFINITY;
-        m = fmaxf(m, acc[t][b][r]);
+        float x = acc[t][b][r];
+#pragma unroll
+        for (int k = 0; k < 3; ++k) x += sums[k][b][t * 4 + r][lane];
+        if (cls(t, r) >= a.C) x = -INFINITY;
+        acc[t][b][r] = x;
+        m = fmaxf(m, x);
       }
     m = fmaxf(m, __shfl_xor(m, 16, 64));
     m = fmaxf(m, __shfl_xor(m, 32, 64));
@@ -179,50 +174,42 @@ __global__ void __launch_bounds__(256) k_few_logits(FewArgs a) {
       for (int r = 0; r < 4; ++r) z += exp_less(acc[t][b][r], m1);
     z += __shfl_xor(z, 16, 64);
     z += __shfl_xor(z, 32, 64);
-    if (q == 0) red[wave][v] = make_float2(m, z);
-    if (v < rows.n) {
-      const int32_t y = lab[v];
+    if (v >= rows.n) continue;
+    if (q == 0) a.part[(int64_t)v * a.blocks + blockIdx.x] = make_float2(m, z);
+    const int32_t y = lab[v];
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
+    for (int t = 0; t < 4; ++t)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (cls(t, r) == y) a.xlab[v] = acc[t][b][r];
-      if (a.X) {
+      for (int r = 0; r < 4; ++r)
+        if (cls(t, r) == y) a.xlab[v] = acc[t][b][r];
+    if (a.X) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const v4f x = OUT_IN ? acc[k][b] : v4f{acc[0][b][k], acc[1][b][k], acc[2][b][k], acc[3][b][k]};
-          *reinterpret_cast<v4f*>(a.X + v * a.ldx + (OUT_IN ? c0 + k * 16 + 4 * q : c0 + 16 * q + 4 * k)) = x;
-        }
+      for (int k = 0; k < 4; ++k) {
+        const v4f x = OUT_IN ? acc[k][b] : v4f{acc[0][b][k], acc[1][b][k], acc[2][b][k], acc[3][b][k]};
+        *reinterpret_cast<v4f*>(a.X + v * a.ldx + (OUT_IN ? c0 + k * 16 + 4 * q : c0 + 16 * q + 4 * k)) = x;
       }
     }
   }
-  __syncthreads();
-  if ((int)threadIdx.x < rows.n) {
-    const int v = threadIdx.x;
-    float m = -INFINITY, z = 0.f;
-    for (int w = 0; w < 4; ++w) m = fmaxf(m, red[w][v].x);
-    for (int w = 0; w < 4; ++w) z += red[w][v].x == -INFINITY ? red[w][v].y : red[w][v].y * exp_less(red[w][v].x, m);
-    a.part[(int64_t)v * a.blocks + blockIdx.x] = make_float2(m, z);
-  }
 }
 
-// One block: a wave a row.  lse: of the labelled rows in order.
-__global__ void __launch_bounds__(1024) k_few_join(FewArgs a, const float* __restrict__ weight, int mean, float* __restrict__ lse_of, float* __restrict__ row_loss,
-                                                   float* __restrict__ row_lse, float* __restrict__ loss) {
+// A block a row; the last of them to come to an end adds up the losses.  lse_of, l_of: of the labelled rows in order.
+__global__ void __launch_bounds__(256) k_few_join(FewArgs a, const float* __restrict__ weight, int mean, float* __restrict__ lse_of, float* __restrict__ l_of,
+                                                  float* __restrict__ row_loss, float* __restrict__ row_lse, float* __restrict__ loss) {
   __shared__ int idx[64];
   __shared__ int32_t lab[64];
-  __shared__ double sh[16];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  __shared__ float2 sh[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, at = blockIdx.x;
   const FewRows rows(a.labels, a.V, idx, lab);
-  if (wave == 0 && lane < a.V && !((rows.mask >> lane) & 1)) {
-    if (row_loss) row_loss[lane] = 0.f;
-    if (row_lse) row_lse[lane] = 0.f;
-  }
-  double mine = 0.0;
-  for (int v = wave; v < rows.n; v += 16) {
+  if (!((rows.mask >> at) & 1)) {
+    if (threadIdx.x == 0) {
+      if (row_loss) row_loss[at] = 0.f;
+      if (row_lse) row_lse[at] = 0.f;
+    }
+  } else {
+    const int v = __popcll(rows.mask & ((1ull << at) - 1));
     float m = -INFINITY, z = 0.f;
-#pragma unroll 4
-    for (int t = lane; t < a.blocks; t += 64) {
+#pragma unroll 8
+    for (int t = threadIdx.x; t < a.blocks; t += 256) {
       const float2 p = a.part[(int64_t)v * a.blocks + t];
       const float n = fmaxf(m, p.x);
       z = (m == -INFINITY ? z : z * exp_less(m, n)) + (p.x == -INFINITY ? p.y : p.y * exp_less(p.x, n));
@@ -232,21 +219,26 @@ __global__ void __launch_bounds__(1024) k_few_join(FewArgs a, const float* __res
     for (int o = 32; o > 0; o >>= 1) all = fmaxf(all, __shfl_xor(all, o, 64));
     z = m == -INFINITY ? z : z * exp_less(m, all);
     for (int o = 32; o > 0; o >>= 1) z += __shfl_xor(z, o, 64);
-    const float lse = all + logf(z), l = lab[v] < a.C ? lse - a.xlab[v] : NAN;
-    if (lane == 0) {
+    if (lane == 0) sh[wave] = make_float2(all, z);
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      m = fmaxf(fmaxf(sh[0].x, sh[1].x), fmaxf(sh[2].x, sh[3].x));
+      z = 0.f;
+      for (int w = 0; w < 4; ++w) z += sh[w].x == -INFINITY ? sh[w].y : sh[w].y * exp_less(sh[w].x, m);
+      const float lse = m + logf(z), l = lab[v] < a.C ? lse - a.xlab[v] : NAN;
       lse_of[v] = lse;
-      if (row_loss) row_loss[idx[v]] = l;
-      if (row_lse) row_lse[idx[v]] = lse;
-      mine += weight ? (double)weight[idx[v]] * (double)l : (double)l;
+      __hip_atomic_store(l_of + v, weight ? weight[at] * l : l, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (row_loss) row_loss[at] = l;
+      if (row_lse) row_lse[at] = lse;
     }
   }
-  if (lane == 0) sh[wave] = mine;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    double s = 0.0;
-    for (int w = 0; w < 16; ++w) s += sh[w];
-    *loss = rows.n > 0 ? (float)(s / (mean ? (double)rows.n : 1.0)) : 0.f;
-  }
+  if (wave != 0) return;
+  unsigned ended = 0;
+  if (lane == 0) ended = __hip_atomic_fetch_add(a.ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+  if (__builtin_amdgcn_readfirstlane((int)ended) != (int)gridDim.x - 1) return;
+  double s = lane < rows.n ? (double)__hip_atomic_load(l_of + lane, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0;
+  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+  if (lane == 0) *loss = rows.n > 0 ? (float)(s / (mean ? (double)rows.n : 1.0)) : 0.f;
 }
 
 struct FewGrad {
@@ -287,40 +279,51 @@ __global__ void __launch_bounds__(256) k_few_grad(FewArgs a, FewGrad g) {
 #pragma unroll
     for (int b = 0; b < NB; ++b) sum[t][b] = v4f{0.f, 0.f, 0.f, 0.f};
   const int t0 = (int)((int64_t)g.tiles * blockIdx.x / gridDim.x), t1 = (int)((int64_t)g.tiles * (blockIdx.x + 1) / gridDim.x);
-  for (int tile = t0; tile < t1; ++tile) {
+  // of the next tile: W for dH, OUT_IN four rows of a step of 16 classes, else four columns of a step, of each of four tiles of 16 features; and the logits
+  v4f w[4][4], x[NB];
+  auto fetch_w = [&](int tile) {
     const int64_t c0 = (int64_t)tile * CT;
-    // W for dH: OUT_IN four rows of a step of 16 classes; else four columns of a step, of each of four tiles of 16 features
-    v4f w[4][4];
-    auto fetch = [&](int s) {
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         if (OUT_IN) {
           const int64_t c = c0 + s * 16 + 4 * q + k;
-          w[s & 3][k] = c < a.C ? load4(a.W + c * a.ldw + jl, jleft) : v4f{0.f, 0.f, 0.f, 0.f};
+          w[s][k] = c < a.C ? load4(a.W + c * a.ldw + jl, jleft) : v4f{0.f, 0.f, 0.f, 0.f};
         } else {
           const int j = j0 + k * 16 + l;
           const int64_t c = c0 + s * 16 + 4 * q, left = a.C - c;
-          w[s & 3][k] = j < a.d ? load4(a.W + (int64_t)j * a.ldw + c, left >= 4 ? 4 : (int)left) : v4f{0.f, 0.f, 0.f, 0.f};
+          w[s][k] = j < a.d ? load4(a.W + (int64_t)j * a.ldw + c, left >= 4 ? 4 : (int)left) : v4f{0.f, 0.f, 0.f, 0.f};
         }
       }
-    };
-    if (g.part) {
+  };
+  auto fetch_x = [&](int tile) {
 #pragma unroll
-      for (int s = 0; s < 4; ++s) fetch(s);
+    for (int b = 0; b < NB; ++b) {
+      const int v = b * 16 + threadIdx.x / 16;
+      x[b] = v < rows.n ? *reinterpret_cast<const v4f*>(a.X + v * a.ldx + (int64_t)tile * CT + threadIdx.x % 16 * 4) : v4f{0.f, 0.f, 0.f, 0.f};
     }
-    __syncthreads();
-    for (int i = threadIdx.x; i < NB * 16 * (CT / 4); i += 256) {
-      const int v = i / (CT / 4), c = i % (CT / 4) * 4;
+  };
+  if (t0 < t1) {
+    fetch_x(t0);
+    if (g.part) fetch_w(t0);
+  }
+  __syncthreads();                         // (lse, scale)
+  for (int tile = t0; tile < t1; ++tile) {
+    const int64_t c0 = (int64_t)tile * CT;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const int v = b * 16 + threadIdx.x / 16, c = threadIdx.x % 16 * 4;
       v4f p = {0.f, 0.f, 0.f, 0.f};
       if (v < rows.n) {
-        const v4f x = *reinterpret_cast<const v4f*>(a.X + v * a.ldx + c0 + c);
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-          if (c0 + c + k < a.C) p[k] = (exp_less(x[k], lse[v]) - (c0 + c + k == lab[v] ? 1.f : 0.f)) * scale[v];
+          if (c0 + c + k < a.C) p[k] = (exp_less(x[b][k], lse[v]) - (c0 + c + k == lab[v] ? 1.f : 0.f)) * scale[v];
       }
       *reinterpret_cast<v4f*>(&Ps[v][c]) = p;
     }
     __syncthreads();
+    if (tile + 1 < t1) fetch_x(tile + 1);
     if (g.dW) {
       if (OUT_IN) {
 #pragma unroll
@@ -373,7 +376,9 @@ __global__ void __launch_bounds__(256) k_few_grad(FewArgs a, FewGrad g) {
 #pragma unroll
             for (int t = 0; t < 4; ++t) sum[t][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(p[k], OUT_IN ? w[s][k][t] : w[s][t][k], sum[t][b], 0, 0, 0);
         }
+      if (tile + 1 < t1) fetch_w(tile + 1);
     }
+    __syncthreads();
   }
   if (!g.part) return;
   // a lane has the rows b * 16 + 4 q + r and a feature of each tile: OUT_IN 4 l + t, else t * 16 + l
@@ -424,24 +429,25 @@ int ht_head_few(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht
   const bool out_in = D->w_form == HT_W_OUT_IN, grad = dH || dW;
   const int mean = D->reduction == HT_REDUCE_MEAN, d = D->d, C = D->n_classes;
   const int NB = H->rows <= 16 ? 1 : H->rows <= 32 ? 2 : 4;
-  const int blocks = (int)ceil_div64(C, 256), tiles = (int)ceil_div64(C, CT);
-  const int64_t ldx = (int64_t)blocks * 256;
+  const int blocks = (int)ceil_div64(C, CT), tiles = blocks;
+  const int64_t ldx = (int64_t)blocks * CT;
   const int gy = (int)ceil_div64(d, JT), gx = (int)std::min<int64_t>(tiles, std::max(64, 512 / gy));
   hipStream_t st = ctx->stream;
   OpsBlock m;
   const auto X = m.add<float>(grad ? NB * 16 * ldx : 0);
   const auto part = m.add<float2>((int64_t)64 * blocks);
-  const auto xlab = m.add<float>(64), lse = m.add<float>(64);
+  const auto xlab = m.add<float>(64), lse = m.add<float>(64), lrow = m.add<float>(64);
+  const auto ticket = m.add<unsigned>(1);
   const auto ph = m.add<float>(dH ? (int64_t)gx * NB * 16 * d : 0);
   HT_TRY(m.take(ctx));
-  const FewArgs a{H->ptr, H->ld, H->rows, d, C, W->ptr, W->ld, labels, grad ? m.at(X) : nullptr, ldx, m.at(part), blocks, m.at(xlab)};
+  const FewArgs a{H->ptr, H->ld, H->rows, d, C, W->ptr, W->ld, labels, grad ? m.at(X) : nullptr, ldx, m.at(part), blocks, m.at(xlab), m.at(ticket)};
   const FewGrad g{weight, m.at(lse), mean, D->accumulate_dW, dW ? dW->ptr : nullptr, dW ? dW->ld : 0, dH ? m.at(ph) : nullptr, tiles};
   auto run = [&](auto nb, auto form) -> int {
     constexpr int N = decltype(nb)::value;
     constexpr bool F = decltype(form)::value;
     k_few_logits<N, F><<<(unsigned)blocks, 256, 0, st>>>(a);
     HT_LAUNCH_CHECK(ctx);
-    k_few_join<<<1, 1024, 0, st>>>(a, weight, mean, m.at(lse), row_loss, row_lse, loss);
+    k_few_join<<<(unsigned)H->rows, 256, 0, st>>>(a, weight, mean, m.at(lse), m.at(lrow), row_loss, row_lse, loss);
     HT_LAUNCH_CHECK(ctx);
     if (!grad) return HT_OK;
     k_few_grad<N, F><<<dim3((unsigned)gx, (unsigned)gy), 256, 0, st>>>(a, g);
