@@ -5,10 +5,10 @@
 // by class piece, the logits are computed again and leave as exp(x - lse) - [c = y], which dH and dW are made of.  Four products of 2 n d C flops, the fewest possible without keeping n x C numbers.
 //
 // All of them are k_split_nt's: fp32 products on the fp16 matrix cores.  A value is split into two fp16 numbers, x = x0 + x1 (x0 its
-// rounding, x1 the rounding of what is left: |x - x0 - x1| <= 2^-22 |x|), after each row of an operand was scaled by a power of two
-// that brings its largest value to [2^14, 2^15); x0 y0 + x0 y1 + x1 y0 are added in fp32.  What is left out is at most 3 x 2^-22 of a
-// product, typically (the roundings are independent) 2^-24 of it, what fp32 loses in rounding it; values below 2^-17 of their row's
-// largest keep fewer bits, down to 2^-39 of it.  Three fp16 steps take 96 clocks where an fp32 product takes 512.
+// rounding, x1 the rounding of what is left: |x - x0 - x1| <= 2^-22 |x|), after W, each row of H, and each weighted column of H for dW were
+// scaled by a power of two that brings the largest value to [2^14, 2^15); x0 y0 + x0 y1 + x1 y0 are added in fp32.  What is left out is at most 3 x 2^-22 of a
+// product, typically (the roundings are independent) 2^-24 of it, what fp32 loses in rounding it; values below 2^-17 of the
+// largest that they are scaled by keep fewer bits, down to 2^-39 of it.  Three fp16 steps take 96 clocks where an fp32 product takes 512.
 #include <algorithm>
 
 #include "ht_internal.h"
@@ -140,8 +140,7 @@ struct Source {
 
 // Largest absolute values of rows, and of columns (of weighted rows), as bits, into arrays that hold zeros.  (Maxima do not depend on their order.)
 // A wave takes RW rows at a time, a block AMAX_COLS columns of them; columns are joined once a block.
-constexpr int AMAX_COLS = 512;
-template <int RW>
+constexpr int AMAX_COLS = 512, RW = 4;
 __global__ void __launch_bounds__(256) k_amax(Source s, uint32_t* __restrict__ rmax, uint32_t* __restrict__ cmax) {
   constexpr int Q = AMAX_COLS / 64;
   __shared__ uint32_t sh[4][AMAX_COLS], shr[4 * RW];
@@ -152,7 +151,7 @@ __global__ void __launch_bounds__(256) k_amax(Source s, uint32_t* __restrict__ r
   for (int k = 0; k < Q; ++k) cm[k] = 0;
   for (int64_t g0 = (int64_t)blockIdx.x * (4 * RW); g0 < n; g0 += (int64_t)gridDim.x * (4 * RW)) {
     const int64_t r0 = g0 + wave * RW;
-#pragma unroll 4
+#pragma unroll
     for (int q = 0; q < RW; ++q) {
       const int64_t r = r0 + q < n ? r0 + q : n - 1, v = s.row(r);
       const float* p = s.p + v * s.ld;
@@ -167,7 +166,7 @@ __global__ void __launch_bounds__(256) k_amax(Source s, uint32_t* __restrict__ r
       for (int o = 32; o > 0; o >>= 1) rm = max(rm, (uint32_t)__shfl_xor((int)rm, o, 64));
       if (lane == 0) shr[wave * RW + q] = rm;
     }
-    // one request for the block's rows (one for every row: 256 x 131,072 107 us, like this 38)
+    // (one request for the block's rows, not one for each)
     __syncthreads();
     if (threadIdx.x < 4 * RW && g0 + threadIdx.x < n) {
       if (gridDim.y == 1) rmax[g0 + threadIdx.x] = shr[threadIdx.x];
@@ -184,12 +183,36 @@ __global__ void __launch_bounds__(256) k_amax(Source s, uint32_t* __restrict__ r
     if (c < s.cols) atomicMax(cmax + c, m);
   }
 }
-constexpr int64_t AMAX_BLOCKS = 1024;
+constexpr int64_t AMAX_BLOCKS = 1024, ABSMAX_BLOCKS = 1024;   // (as many requests to one word: 2,048 of them take 27 us)
 void launch_amax(hipStream_t st, const Source& s, uint32_t* rmax, uint32_t* cmax) {
-  const int64_t gy = ceil_div64(s.cols, AMAX_COLS), most = std::max<int64_t>(1, AMAX_BLOCKS / gy);
-  // (listed rows may be far fewer than there could be)
-  if (s.idx || ceil_div64(s.rows, 16) <= most) k_amax<4><<<dim3((unsigned)std::max<int64_t>(1, std::min(ceil_div64(s.rows, 16), most)), (unsigned)gy), 256, 0, st>>>(s, rmax, cmax);
-  else k_amax<16><<<dim3((unsigned)std::max<int64_t>(1, std::min(ceil_div64(s.rows, 64), most)), (unsigned)gy), 256, 0, st>>>(s, rmax, cmax);
+  const int64_t gy = ceil_div64(s.cols, AMAX_COLS), gx = std::min(ceil_div64(s.rows, 4 * RW), std::max<int64_t>(1, AMAX_BLOCKS / gy));
+  k_amax<<<dim3((unsigned)std::max<int64_t>(1, gx), (unsigned)gy), 256, 0, st>>>(s, rmax, cmax);
+}
+
+// The largest absolute value of a matrix, as bits.
+__global__ void __launch_bounds__(256) k_absmax(const float* __restrict__ p, int64_t ld, int64_t rows, int64_t cols, uint32_t* __restrict__ out) {
+  __shared__ uint32_t sh[4];
+  constexpr int U = 16;                  // units of 256 columns of a row, at a time
+  const uint32_t parts = (uint32_t)((cols + 255) / 256);
+  const int64_t n = rows * parts;
+  uint32_t m = 0;
+  for (int64_t i = (int64_t)blockIdx.x * U; i < n; i += (int64_t)gridDim.x * U) {
+    const int64_t r0 = i / parts;
+    const uint32_t q0 = (uint32_t)(i - r0 * parts);
+    float x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t q = (q0 + u) / parts;
+      const int64_t r = r0 + q, c = (int64_t)(q0 + u - q * parts) * 256 + threadIdx.x;
+      x[u] = p[(r < rows ? r : rows - 1) * ld + (c < cols ? c : cols - 1)];       // (behind the last ones: those again)
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) m = max(m, __float_as_uint(fabsf(x[u])));
+  }
+  for (int o = 32; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = m;
+  __syncthreads();
+  if (threadIdx.x == 0) atomicMax(out, max(max(sh[0], sh[1]), max(sh[2], sh[3])));
 }
 
 __device__ __forceinline__ void split2(float x, _Float16* hi, _Float16* lo) {
@@ -199,7 +222,8 @@ __device__ __forceinline__ void split2(float x, _Float16* hi, _Float16* lo) {
 
 // Fragments of the matrix by rows (reduction along columns: KS steps) and by columns (reduction along rows, weighted: KS_t steps), zeros behind
 // the last row and column, a 64 x 64 tile a block.
-__global__ void __launch_bounds__(256) k_pack(Source s, const uint32_t* __restrict__ rmax, const uint32_t* __restrict__ cmax,
+// `all`: the largest value of everything, where it is scaled by one factor.
+__global__ void __launch_bounds__(256) k_pack(Source s, const uint32_t* __restrict__ rmax, const uint32_t* __restrict__ cmax, const uint32_t* __restrict__ all,
                                               _Float16* __restrict__ R, int64_t KS, _Float16* __restrict__ T, int64_t KS_t, int64_t row_tile, unsigned col_tiles) {
   __shared__ float sh[64][65];
   __shared__ float wt[64];
@@ -239,14 +263,14 @@ __global__ void __launch_bounds__(256) k_pack(Source s, const uint32_t* __restri
     float x[8];
     if (R && c0 / 16 + ks < KS) {
       const int r = b * 32 + l32;
-      const float f = scale_of(r0 + r < n ? rmax[r0 + r] : 0u);
+      const float f = scale_of(all ? *all : r0 + r < n ? rmax[r0 + r] : 0u);
 #pragma unroll
       for (int t = 0; t < 8; ++t) x[t] = sh[r][k + (t >> 2) * 8 + (t & 3)] * f;
       put(R, (r0 / 32 + b) * KS + c0 / 16 + ks, x);
     }
     if (T && r0 / 16 + ks < KS_t) {
       const int c = b * 32 + l32;
-      const float f = scale_of(c0 + c < s.cols ? cmax[c0 + c] : 0u);
+      const float f = scale_of(all ? *all : c0 + c < s.cols ? cmax[c0 + c] : 0u);
 #pragma unroll
       for (int t = 0; t < 8; ++t) {
         const int r = k + (t >> 2) * 8 + (t & 3);
@@ -277,7 +301,7 @@ __device__ __forceinline__ float inv_count(const int64_t* total, int mean) { ret
 struct NtArgs {
   const _Float16 *A, *B;          // fragments; row blocks KSA, KSB steps apart
   int64_t KSA, KSB;
-  int64_t ksb0;                   // first step of B
+  int64_t b0;                     // first step of B, or (turned) first row block
   int64_t mt, nt;                 // tiles
   int64_t steps;                  // steps of the reduction (a multiple of 4); < 0: up to the piece's rows
   int splits;                     // parts of it, each with sums of its own
@@ -287,7 +311,7 @@ struct NtArgs {
   int rows_are;                   // which operand's rows are the piece's: 0 none, 1 A's, 2 B's
   // LOSS, GRAD: A's rows are classes from c0 on, B's rows of the piece
   int64_t c0, C;
-  const uint32_t *cmax, *hmax;    // their largest values
+  const uint32_t *wmax, *hmax;    // the largest values of W, of each row of H
   const int32_t* lab;
   float2* part;                   // LOSS: [class tile][most]: largest logit, sum of exponentials less it
   float* xlab;                    // LOSS: the label's logit
@@ -316,7 +340,8 @@ constexpr int KT = 2, PAIR = 32 * KT;   // steps of a stage; values of the reduc
 // C = A B^T of fragments, 256 x 128 a block, 64 x 128 a wave.  A wave reads its own rows of A straight into registers, a stage ahead, and the four
 // waves share B through LDS, which is filled a stage ahead as well; two blocks a CU.
 //
-// TURN: B is the transpose of what its fragments hold, rows of the reduction by 16s of its own rows (gradients of logits, rows by classes, for dW).  A stage is 32 rows of the
+// TURN: B is the transpose of what its fragments hold, rows of the reduction by 16s of its own rows (for dH W's classes by features, for dW
+// the gradients' rows by classes).  A stage is 32 rows of the
 // reduction by 128, and lies in LDS as in memory; ds_read_tr gives 16 lanes the columns of four rows of 16.  (Each half of a fragment starts 640 bytes after
 // the one before, so that what a quarter of the lanes reads lies in other banks than what the others do.)
 constexpr int TURN_HALF = 320;    // halfs
@@ -349,7 +374,7 @@ __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
 
   const _Float16 *Ap0 = a.A + ((m0 / 32 + wave * 2) * a.KSA + s0 * KT) * 2 * FRAG + lane * 8, *Ap1 = Ap0 + a.KSA * 2 * FRAG;
   // a wave brings one of the four row blocks, or two of the eight 16s
-  const _Float16* Bp = a.B + (TURN ? s0 * a.KSB + n0 / 16 + wave * 2 : (n0 / 32 + wave) * a.KSB + a.ksb0 + s0 * KT) * 2 * FRAG + lane * 8;
+  const _Float16* Bp = a.B + (TURN ? (a.b0 + s0) * a.KSB + n0 / 16 + wave * 2 : (n0 / 32 + wave) * a.KSB + a.b0 + s0 * KT) * 2 * FRAG + lane * 8;
   const int64_t b_step = (TURN ? a.KSB : KT) * 2 * FRAG;
   v8h ra[2][KT][2][2], rb[KT * 2];    // [stage in turn][step][row block][plane]
   auto fetch = [&](int to) {          // of the stage that the pointers have come to
@@ -491,14 +516,7 @@ __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
     }
     return;
   }
-  float cs[2][16];                 // what undoes the classes' scaling (cmax is there for whole tiles)
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const uint4 x = *reinterpret_cast<const uint4*>(a.cmax + a.c0 + mw + i * 32 + k * 8 + half * 4);
-      cs[i][k * 4] = unscale_of(x.x), cs[i][k * 4 + 1] = unscale_of(x.y), cs[i][k * 4 + 2] = unscale_of(x.z), cs[i][k * 4 + 3] = unscale_of(x.w);
-    }
+  const float ws = unscale_of(*a.wmax);
   const int64_t left = a.C - a.c0 - mw;                              // classes of the wave's 64
   const int lim = (left >= 64 ? 64 : left < 0 ? 0 : (int)left) - half * 4;
   if constexpr (EPI == LOSS) {
@@ -507,12 +525,12 @@ __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
     for (int j = 0; j < 4; ++j) {
       const int64_t v = n0 + j * 32 + l32;
       const bool there = v < rows;
-      const float hs = unscale_of(a.hmax[v]);
+      const float hs = unscale_of(a.hmax[v]) * ws;
       float m = -INFINITY;
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) acc[i][j][e] *= hs * cs[i][e];
+        for (int e = 0; e < 16; ++e) acc[i][j][e] *= hs;
       if (left < 64) {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -560,7 +578,7 @@ __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
     for (int j = 0; j < 4; ++j) {
       const int64_t v = n0 + j * 32 + l32;
       const bool there = v < rows;
-      const float hs = unscale_of(a.hmax[v]);
+      const float hs = unscale_of(a.hmax[v]) * ws;
       const float lse = there ? a.lse[v] : 0.f;
       const int64_t off = there ? a.lab[a.r0 + v] - (a.c0 + mw) : -1;
       const bool mine = off >= 0 && off < 64 && ((off >> 2) & 1) == half;
@@ -569,7 +587,7 @@ __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
       for (int i = 0; i < 2; ++i) {
         float p[16];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(fmaf(acc[i][j][e], hs * cs[i][e], -lse), LOG2E, P_EXP));
+        for (int e = 0; e < 16; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(fmaf(acc[i][j][e], hs, -lse), LOG2E, P_EXP));
         if (left < 64 || n0 + TN > rows) {
 #pragma unroll
           for (int e = 0; e < 16; ++e)
@@ -677,8 +695,8 @@ __global__ void __launch_bounds__(256) k_head_dh(const float* __restrict__ sums,
     s.x += x.x, s.y += x.y, s.z += x.z, s.w += x.w;
   }
   const int64_t at = idx[r0 + v];
-  const float f = inv_count(total, mean) * (weight ? weight[at] : 1.f) * (1.f / (1 << P_EXP));
-  auto out = [&](float x, int k) { return c + k < d ? x * unscale_of(wmax[c + k]) * f : 0.f; };
+  const float f = inv_count(total, mean) * (weight ? weight[at] : 1.f) * (1.f / (1 << P_EXP)), ws = unscale_of(*wmax);
+  auto out = [&](float x, int k) { return c + k < d ? x * ws * f : 0.f; };
   *reinterpret_cast<float4*>(dH + at * ld + c) = make_float4(out(s.x, 0), out(s.y, 1), out(s.z, 2), out(s.w, 3));
   }
 }
@@ -698,7 +716,8 @@ __global__ void __launch_bounds__(256) k_head_dw(const float* __restrict__ sums,
 }
 
 struct HeadPlan {
-  int64_t Cp, Rp, KSd;               // classes and rows of a piece, steps of a reduction over d
+  int64_t Cp, Rp;                    // classes and rows of a piece
+  int64_t KSd, steps_d;              // steps over d as operands hold them, and of a reduction
   int64_t Cpad, dpad;
   int splits_w;
   HeadSplits by_rows;
@@ -707,7 +726,8 @@ struct HeadPlan {
 
 HeadPlan head_plan(int64_t V, int64_t d, int64_t C, bool in_out, size_t bytes) {
   HeadPlan p{};
-  p.KSd = up_to(d, PAIR) / 16;
+  p.KSd = up_to(d, TN) / 16;
+  p.steps_d = up_to(d, PAIR) / 16;
   p.Cpad = up_to(C, TM);
   p.dpad = up_to(d, TM);
   // a row takes 4 bytes a value of its own, by rows and by features, and of its gradient, 4 a class of the piece, and 8 a tile of classes
@@ -726,15 +746,14 @@ HeadPlan head_plan(int64_t V, int64_t d, int64_t C, bool in_out, size_t bytes) {
   return p;
 }
 
-int split_nt(ht_ctx* ctx, hipStream_t st, int epi, const NtArgs& a, bool turn = false) {
+int split_nt(ht_ctx* ctx, hipStream_t st, int epi, const NtArgs& a) {
   const int64_t blocks = up_to(a.rows_are == 1 ? a.by_rows.blocks : a.mt * a.nt * a.splits, 8);
   if (blocks >= (1 << 24)) return ht_set_err(ctx, HT_ESHAPE, "head: %lld tiles in one product", (long long)blocks);
   const unsigned grid = (unsigned)blocks;
   if (epi == LOSS) k_split_nt<LOSS, false><<<grid, 256, 0, st>>>(a);
   else if (epi == GRAD) k_split_nt<GRAD, false><<<grid, 256, 0, st>>>(a);
   else if (epi == DIRECT) k_split_nt<DIRECT, true><<<grid, 256, 0, st>>>(a);
-  else if (turn) k_split_nt<SUMS, true><<<grid, 256, 0, st>>>(a);
-  else k_split_nt<SUMS, false><<<grid, 256, 0, st>>>(a);
+  else k_split_nt<SUMS, true><<<grid, 256, 0, st>>>(a);
   HT_LAUNCH_CHECK(ctx);
   return HT_OK;
 }
@@ -749,29 +768,28 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
   const int64_t pieces = std::max<int64_t>(1, ceil_div64(V, p.Rp)), ct = p.Cpad / TM;
   const int64_t rpb = std::max<int64_t>(256, up_to(ceil_div64(std::max<int64_t>(V, 1), ROW_BLOCKS), 256)), rb = std::max<int64_t>(1, ceil_div64(V, rpb));
   const int64_t jb = std::min<int64_t>(p.Rp / 64, 1024);   // blocks of k_head_join a piece
-  const int64_t KSC = p.Cpad / 16, KSR = p.Rp / 16;
+  const int64_t KSR = p.Rp / 16;
 
   OpsBlock m;
   const auto cnt = m.add<int32_t>(rb);
   const auto idx = m.add<int32_t>(V), lab = m.add<int32_t>(V);
   const auto total = m.add<int64_t>(1);
-  const int64_t n_max = p.Cpad + p.Rp + 2 * p.dpad;
-  const auto wc = m.add<uint32_t>(n_max);                        // W's largest values by class, by feature, H's by row, by feature
+  const int64_t n_max = 4 + p.Rp + p.dpad;
+  const auto mx = m.add<uint32_t>(n_max);                        // the largest values: of W (and three words), of H by row, by feature
   const auto Wf = m.add<_Float16>(p.Cpad * p.KSd * 32);
   const auto Hf = m.add<_Float16>(p.Rp * p.KSd * 32);
   const auto part = m.add<float2>(ct * p.Rp);
   const auto xlab = m.add<float>(p.Rp), lse = m.add<float>(p.Rp);
   const auto ploss = m.add<double>(pieces * jb);
-  const auto Wt = m.add<_Float16>(dH ? p.dpad * KSC * 32 : 0);
   const auto Ht = m.add<_Float16>(dW ? p.dpad * KSR * 32 : 0);
   const auto P = m.add<_Float16>(grad ? p.Rp * p.Cp * 2 : 0);
   const auto sh = m.add<float>(dH ? p.sum_rows * p.dpad : 0);
   const auto sw = m.add<float>(dW && p.splits_w > 1 ? p.splits_w * p.Cp * p.dpad : 0);
   HT_TRY(m.take(ctx));
 
-  uint32_t *wmax_c = m.at(wc), *wmax_j = wmax_c + p.Cpad, *hmax_v = wmax_j + p.dpad, *hmax_j = hmax_v + p.Rp;
+  uint32_t *wmax = m.at(mx), *hmax_v = wmax + 4, *hmax_j = hmax_v + p.Rp;
   const unsigned clear_blocks = (unsigned)std::min<int64_t>(ceil_div64(n_max, 4096), 1024);
-  k_head_count<<<(unsigned)rb + clear_blocks, 256, 0, st>>>(labels, V, rpb, m.at(cnt), (unsigned)rb, (uint4*)wmax_c, n_max / 4);
+  k_head_count<<<(unsigned)rb + clear_blocks, 256, 0, st>>>(labels, V, rpb, m.at(cnt), (unsigned)rb, (uint4*)wmax, n_max / 4);
   HT_LAUNCH_CHECK(ctx);
   k_head_place<<<(unsigned)rb, 256, 0, st>>>(labels, V, rpb, m.at(cnt), m.at(idx), m.at(lab), m.at(total), row_loss, row_lse);
   HT_LAUNCH_CHECK(ctx);
@@ -781,13 +799,12 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
   }
   {
     const Source s{W->ptr, W->ld, W->rows, W->cols, nullptr, nullptr, nullptr, 0};
-    uint32_t *r = in_out ? wmax_j : wmax_c, *c = in_out ? wmax_c : wmax_j;
-    launch_amax(st, s, r, c);
+    k_absmax<<<(unsigned)std::min<int64_t>(ceil_div64(s.rows * ceil_div64(s.cols, 256), 64), ABSMAX_BLOCKS), 256, 0, st>>>(s.p, s.ld, s.rows, s.cols, wmax);
     HT_LAUNCH_CHECK(ctx);
-    _Float16* wt = dH ? m.at(Wt) : nullptr;
-    const int64_t rt = up_to(s.rows, in_out ? 64 : TM) / 64, cols_t = up_to(s.cols, in_out ? TM : 64) / 64;
-    k_pack<<<(unsigned)std::min(rt * cols_t, PACK_BLOCKS), 256, 0, st>>>(s, r, c, in_out ? wt : m.at(Wf), in_out ? KSC : p.KSd, in_out ? m.at(Wf) : wt, in_out ? p.KSd : KSC,
-                                                    in_out ? 64 : TM, (unsigned)cols_t);
+    // by classes: W's rows, or its columns
+    const int64_t rt = up_to(s.rows, in_out ? 64 : TM) / 64, ct64 = up_to(s.cols, in_out ? TM : 64) / 64;
+    k_pack<<<(unsigned)std::min(rt * ct64, PACK_BLOCKS), 256, 0, st>>>(s, nullptr, nullptr, wmax, in_out ? nullptr : m.at(Wf), p.KSd, in_out ? m.at(Wf) : nullptr, p.KSd,
+                                                                      in_out ? 64 : TM, (unsigned)ct64);
     HT_LAUNCH_CHECK(ctx);
   }
   for (int64_t k = 0; k < pieces; ++k) {
@@ -796,15 +813,15 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
     const Source s{H->ptr, H->ld, p.Rp, d, m.at(idx), weight, m.at(total), r0};
     launch_amax(st, s, hmax_v, hmax_j);
     HT_LAUNCH_CHECK(ctx);
-    k_pack<<<(unsigned)std::min(p.Rp / 64 * ceil_div64(d, 64), PACK_BLOCKS / 8), 256, 0, st>>>(s, hmax_v, hmax_j, m.at(Hf), p.KSd, dW ? m.at(Ht) : nullptr, KSR, TN,
+    k_pack<<<(unsigned)std::min(p.Rp / 64 * ceil_div64(d, 64), PACK_BLOCKS / 8), 256, 0, st>>>(s, hmax_v, hmax_j, nullptr, m.at(Hf), p.KSd, dW ? m.at(Ht) : nullptr, KSR, TN,
                                                                      (unsigned)ceil_div64(d, 64));
     HT_LAUNCH_CHECK(ctx);
     NtArgs a{};
     a.total = m.at(total), a.r0 = r0, a.most = p.Rp;
     a.splits = 1;
-    a.C = C, a.cmax = wmax_c, a.hmax = hmax_v, a.lab = m.at(lab), a.part = m.at(part), a.xlab = m.at(xlab), a.lse = m.at(lse);
+    a.C = C, a.wmax = wmax, a.hmax = hmax_v, a.lab = m.at(lab), a.part = m.at(part), a.xlab = m.at(xlab), a.lse = m.at(lse);
     a.A = m.at(Wf), a.KSA = p.KSd, a.B = m.at(Hf), a.KSB = p.KSd;
-    a.mt = ct, a.nt = p.Rp / TN, a.steps = p.KSd, a.rows_are = 2;
+    a.mt = ct, a.nt = p.Rp / TN, a.steps = p.steps_d, a.rows_are = 2;
     HT_TRY(split_nt(ctx, st, LOSS, a));
     k_head_join<<<(unsigned)jb, 1024, 0, st>>>(m.at(part), ct, p.Rp, m.at(total), r0, m.at(idx), m.at(lab), C, weight, m.at(xlab), m.at(lse), row_loss, row_lse,
                                                m.at(ploss) + k * jb);
@@ -819,7 +836,7 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
       if (dH) {
         NtArgs h{};
         h.total = m.at(total), h.r0 = r0, h.most = p.Rp, h.rows_are = 1;
-        h.A = m.at(P), h.KSA = p.Cp / 16, h.B = m.at(Wt), h.KSB = KSC, h.ksb0 = c0 / 16;
+        h.A = m.at(P), h.KSA = p.Cp / 16, h.B = m.at(Wf), h.KSB = p.KSd, h.b0 = c0 / 32;
         h.mt = p.Rp / TM, h.nt = up_to(d, TN) / TN, h.steps = cp / 16, h.by_rows = p.by_rows;
         h.out = m.at(sh), h.ms = p.dpad, h.ns = 1, h.add = c0 > 0;
         HT_TRY(split_nt(ctx, st, SUMS, h));
@@ -839,14 +856,14 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
         }
         const int64_t rows_p = in_out ? p.dpad : p.Cp, cols_p = in_out ? p.Cp : p.dpad;
         w.out = m.at(sw), w.split_part = rows_p * cols_p, w.ms = in_out ? cols_p : 1, w.ns = in_out ? 1 : cols_p;
-        HT_TRY(split_nt(ctx, st, SUMS, w, true));
+        HT_TRY(split_nt(ctx, st, SUMS, w));
         k_head_dw<<<(unsigned)ceil_div64(rows * cols, 256), 256, 0, st>>>(m.at(sw), p.splits_w, rows_p, cols_p, rows, cols, hmax_j, in_out, m.at(total), r0, mean, add,
                                                                           out, dW->ld);
         HT_LAUNCH_CHECK(ctx);
       }
     }
     if (dH) {
-      k_head_dh<<<(unsigned)std::min(ceil_div64(p.Rp * ((d + 3) / 4), 256), DH_BLOCKS), 256, 0, st>>>(m.at(sh), p.by_rows, p.Rp, p.dpad, m.at(total), r0, m.at(idx), weight, mean, wmax_j,
+      k_head_dh<<<(unsigned)std::min(ceil_div64(p.Rp * ((d + 3) / 4), 256), DH_BLOCKS), 256, 0, st>>>(m.at(sh), p.by_rows, p.Rp, p.dpad, m.at(total), r0, m.at(idx), weight, mean, wmax,
                                                                                  dH->ptr, dH->ld, (int)d);
       HT_LAUNCH_CHECK(ctx);
     }
