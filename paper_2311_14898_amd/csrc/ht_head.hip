@@ -2,7 +2,8 @@
 //   x_vc = h_v . w_c ;  lse_v = log sum_c exp(x_vc) ;  loss = sum_v u_v (lse_v - x_vy) / N
 //   dx_vc = (u_v / N) (exp(x_vc - lse_v) - [c = y_v]) ;  dH = dx W^T ;  dW = H^T dx
 // Labelled rows are first listed, and only they are computed with.  Rows go in pieces: a pass over all classes gives lse; then, class piece
-// by class piece, the logits are computed again and leave as exp(x - lse) - [c = y], which dH and dW are made of.  Four products of 2 n d C flops, the fewest possible without keeping n x C numbers.
+// by class piece, the logits are computed again and leave as exp(x - lse) - [c = y], which dH and dW are made of.  Four products of
+// 2 n d C flops, the fewest possible without keeping n x C numbers.
 //
 // All of them are k_split_nt's: fp32 products on the fp16 matrix cores.  A value is split into two fp16 numbers, x = x0 + x1 (x0 its
 // rounding, x1 the rounding of what is left: |x - x0 - x1| <= 2^-22 |x|), after W, each row of H, and each weighted column of H for dW were
@@ -230,56 +231,56 @@ __global__ void __launch_bounds__(256) k_pack(Source s, const uint32_t* __restri
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, half = lane >> 5;
   const int64_t n = s.n(), tiles = up_to(n, row_tile) / 64 * col_tiles;
   for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-  const int64_t r0 = tile / col_tiles * 64, c0 = tile % col_tiles * 64;
+    const int64_t r0 = tile / col_tiles * 64, c0 = tile % col_tiles * 64;
 #pragma unroll
-  for (int q = 0; q < 16; ++q) {
-    const int r = wave * 16 + q;
-    float x = 0.f, w = 0.f;
-    if (r0 + r < n) {
-      const int64_t v = s.row(r0 + r);
-      if (c0 + lane < s.cols) x = s.p[v * s.ld + c0 + lane];
-      w = s.weight ? s.weight[v] : 1.f;
+    for (int q = 0; q < 16; ++q) {
+      const int r = wave * 16 + q;
+      float x = 0.f, w = 0.f;
+      if (r0 + r < n) {
+        const int64_t v = s.row(r0 + r);
+        if (c0 + lane < s.cols) x = s.p[v * s.ld + c0 + lane];
+        w = s.weight ? s.weight[v] : 1.f;
+      }
+      sh[r][lane] = x;
+      if (lane == 0) wt[r] = w;
     }
-    sh[r][lane] = x;
-    if (lane == 0) wt[r] = w;
-  }
-  __syncthreads();
-  auto put = [&](_Float16* to, int64_t frag, const float* x) {
-    v8h hi, lo;
-#pragma unroll
-    for (int t = 0; t < 8; ++t) {
-      _Float16 a, b;
-      split2(x[t], &a, &b);
-      hi[t] = a;
-      lo[t] = b;
-    }
-    *reinterpret_cast<v8h*>(to + frag * 2 * FRAG + lane * 8) = hi;
-    *reinterpret_cast<v8h*>(to + frag * 2 * FRAG + FRAG + lane * 8) = lo;
-  };
-  const int b = wave >> 1;                        // row block of the tile; a wave takes two of its four steps
-#pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    const int ks = (wave & 1) * 2 + u, k = ks * 16 + half * 4;
-    float x[8];
-    if (R && c0 / 16 + ks < KS) {
-      const int r = b * 32 + l32;
-      const float f = scale_of(all ? *all : r0 + r < n ? rmax[r0 + r] : 0u);
-#pragma unroll
-      for (int t = 0; t < 8; ++t) x[t] = sh[r][k + (t >> 2) * 8 + (t & 3)] * f;
-      put(R, (r0 / 32 + b) * KS + c0 / 16 + ks, x);
-    }
-    if (T && r0 / 16 + ks < KS_t) {
-      const int c = b * 32 + l32;
-      const float f = scale_of(all ? *all : c0 + c < s.cols ? cmax[c0 + c] : 0u);
+    __syncthreads();
+    auto put = [&](_Float16* to, int64_t frag, const float* x) {
+      v8h hi, lo;
 #pragma unroll
       for (int t = 0; t < 8; ++t) {
-        const int r = k + (t >> 2) * 8 + (t & 3);
-        x[t] = sh[r][c] * wt[r] * f;
+        _Float16 a, b;
+        split2(x[t], &a, &b);
+        hi[t] = a;
+        lo[t] = b;
       }
-      put(T, (c0 / 32 + b) * KS_t + r0 / 16 + ks, x);
+      *reinterpret_cast<v8h*>(to + frag * 2 * FRAG + lane * 8) = hi;
+      *reinterpret_cast<v8h*>(to + frag * 2 * FRAG + FRAG + lane * 8) = lo;
+    };
+    const int b = wave >> 1;                        // row block of the tile; a wave takes two of its four steps
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int ks = (wave & 1) * 2 + u, k = ks * 16 + half * 4;
+      float x[8];
+      if (R && c0 / 16 + ks < KS) {
+        const int r = b * 32 + l32;
+        const float f = scale_of(all ? *all : r0 + r < n ? rmax[r0 + r] : 0u);
+#pragma unroll
+        for (int t = 0; t < 8; ++t) x[t] = sh[r][k + (t >> 2) * 8 + (t & 3)] * f;
+        put(R, (r0 / 32 + b) * KS + c0 / 16 + ks, x);
+      }
+      if (T && r0 / 16 + ks < KS_t) {
+        const int c = b * 32 + l32;
+        const float f = scale_of(all ? *all : c0 + c < s.cols ? cmax[c0 + c] : 0u);
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+          const int r = k + (t >> 2) * 8 + (t & 3);
+          x[t] = sh[r][c] * wt[r] * f;
+        }
+        put(T, (c0 / 32 + b) * KS_t + r0 / 16 + ks, x);
+      }
     }
-  }
-  __syncthreads();
+    __syncthreads();
   }
 }
 constexpr int64_t PACK_BLOCKS = 16384;
@@ -315,7 +316,7 @@ struct NtArgs {
   const int32_t* lab;
   float2* part;                   // LOSS: [class tile][most]: largest logit, sum of exponentials less it
   float* xlab;                    // LOSS: the label's logit
-  const float* lse;               // GRAD
+  const float2* norm;             // GRAD: of each row the largest logit m and P_EXP - log2 of the sum of exp(x - m): exp(x - lse) without a rounding of lse
   _Float16* P;                    // GRAD: fragments by rows (KSP steps)
   int64_t KSP;
   // SUMS
@@ -341,9 +342,9 @@ constexpr int KT = 2, PAIR = 32 * KT;   // steps of a stage; values of the reduc
 // waves share B through LDS, which is filled a stage ahead as well; two blocks a CU.
 //
 // TURN: B is the transpose of what its fragments hold, rows of the reduction by 16s of its own rows (for dH W's classes by features, for dW
-// the gradients' rows by classes).  A stage is 32 rows of the
-// reduction by 128, and lies in LDS as in memory; ds_read_tr gives 16 lanes the columns of four rows of 16.  (Each half of a fragment starts 640 bytes after
-// the one before, so that what a quarter of the lanes reads lies in other banks than what the others do.)
+// the gradients' rows by classes).  A stage is 32 rows of the reduction by 128, and lies in LDS as in memory; ds_read_tr gives 16 lanes the
+// columns of four rows of 16.  (Each half of a fragment starts 640 bytes after the one before, so that what a quarter of the lanes reads
+// lies in other banks than what the others do.)
 constexpr int TURN_HALF = 320;    // halfs
 template <int EPI, bool TURN>
 __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
@@ -579,7 +580,7 @@ __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
       const int64_t v = n0 + j * 32 + l32;
       const bool there = v < rows;
       const float hs = unscale_of(a.hmax[v]) * ws;
-      const float lse = there ? a.lse[v] : 0.f;
+      const float2 nm = there ? a.norm[v] : make_float2(0.f, 0.f);
       const int64_t off = there ? a.lab[a.r0 + v] - (a.c0 + mw) : -1;
       const bool mine = off >= 0 && off < 64 && ((off >> 2) & 1) == half;
       const bool any = __ballot(mine);
@@ -587,7 +588,7 @@ __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
       for (int i = 0; i < 2; ++i) {
         float p[16];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(fmaf(acc[i][j][e], hs, -lse), LOG2E, P_EXP));
+        for (int e = 0; e < 16; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(fmaf(acc[i][j][e], hs, -nm.x), LOG2E, nm.y));
         if (left < 64 || n0 + TN > rows) {
 #pragma unroll
           for (int e = 0; e < 16; ++e)
@@ -623,7 +624,7 @@ __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
 // Blocks of 64 rows, 16 parts of the class tiles each.  part_loss[block] = sum of its rows' weighted losses.
 __global__ void __launch_bounds__(1024) k_head_join(const float2* __restrict__ part, int64_t tiles, int64_t most, const int64_t* __restrict__ total, int64_t r0,
                                                     const int32_t* __restrict__ idx, const int32_t* __restrict__ lab, int64_t C,
-                                                    const float* __restrict__ weight, const float* __restrict__ xlab, float* __restrict__ lse_of,
+                                                    const float* __restrict__ weight, const float* __restrict__ xlab, float2* __restrict__ norm,
                                                     float* __restrict__ row_loss, float* __restrict__ row_lse, double* __restrict__ part_loss) {
   __shared__ float2 sh[16][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -637,7 +638,7 @@ __global__ void __launch_bounds__(1024) k_head_join(const float2* __restrict__ p
       for (int64_t t = wave; t < tiles; t += 16) {
         const float2 p = part[t * most + v];
         const float n = fmaxf(m, p.x);
-        z = (m == -INFINITY ? 0.f : z * exp_less(m, n)) + (p.x == -INFINITY ? p.y : p.y * exp_less(p.x, n));
+        z = (m == -INFINITY ? z : z * exp_less(m, n)) + (p.x == -INFINITY ? p.y : p.y * exp_less(p.x, n));      // (0 or NaN of what has no maximum)
         m = n;
       }
     sh[wave][lane] = make_float2(m, z);
@@ -650,7 +651,7 @@ __global__ void __launch_bounds__(1024) k_head_join(const float2* __restrict__ p
       if (v < rows) {
         const float lse = m + logf(z);
         const float l = lab[r0 + v] < C ? lse - xlab[v] : NAN;
-        lse_of[v] = lse;
+        norm[v] = make_float2(m, P_EXP - log2f(z));
         const int64_t at = idx[r0 + v];
         if (row_loss) row_loss[at] = l;
         if (row_lse) row_lse[at] = lse;
@@ -686,18 +687,18 @@ __global__ void __launch_bounds__(256) k_head_dh(const float* __restrict__ sums,
   const int nv = (d + 3) / 4, splits = by_rows.splits(rows);
   const int64_t part = up_to(rows, TM) * pitch;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * nv; i += (int64_t)gridDim.x * 256) {
-  const int64_t v = i / nv;
-  const int c = (int)(i % nv) * 4;
-  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    const int64_t v = i / nv;
+    const int c = (int)(i % nv) * 4;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 8
-  for (int k = 0; k < splits; ++k) {
-    const float4 x = *reinterpret_cast<const float4*>(sums + k * part + v * pitch + c);
-    s.x += x.x, s.y += x.y, s.z += x.z, s.w += x.w;
-  }
-  const int64_t at = idx[r0 + v];
-  const float f = inv_count(total, mean) * (weight ? weight[at] : 1.f) * (1.f / (1 << P_EXP)), ws = unscale_of(*wmax);
-  auto out = [&](float x, int k) { return c + k < d ? x * ws * f : 0.f; };
-  *reinterpret_cast<float4*>(dH + at * ld + c) = make_float4(out(s.x, 0), out(s.y, 1), out(s.z, 2), out(s.w, 3));
+    for (int k = 0; k < splits; ++k) {
+      const float4 x = *reinterpret_cast<const float4*>(sums + k * part + v * pitch + c);
+      s.x += x.x, s.y += x.y, s.z += x.z, s.w += x.w;
+    }
+    const int64_t at = idx[r0 + v];
+    const float f = inv_count(total, mean) * (weight ? weight[at] : 1.f) * (1.f / (1 << P_EXP)), ws = unscale_of(*wmax);
+    auto out = [&](float x, int k) { return c + k < d ? x * ws * f : 0.f; };
+    *reinterpret_cast<float4*>(dH + at * ld + c) = make_float4(out(s.x, 0), out(s.y, 1), out(s.z, 2), out(s.w, 3));
   }
 }
 
@@ -779,7 +780,8 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
   const auto Wf = m.add<_Float16>(p.Cpad * p.KSd * 32);
   const auto Hf = m.add<_Float16>(p.Rp * p.KSd * 32);
   const auto part = m.add<float2>(ct * p.Rp);
-  const auto xlab = m.add<float>(p.Rp), lse = m.add<float>(p.Rp);
+  const auto xlab = m.add<float>(p.Rp);
+  const auto norm = m.add<float2>(p.Rp);
   const auto ploss = m.add<double>(pieces * jb);
   const auto Ht = m.add<_Float16>(dW ? p.dpad * KSR * 32 : 0);
   const auto P = m.add<_Float16>(grad ? p.Rp * p.Cp * 2 : 0);
@@ -819,11 +821,11 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
     NtArgs a{};
     a.total = m.at(total), a.r0 = r0, a.most = p.Rp;
     a.splits = 1;
-    a.C = C, a.wmax = wmax, a.hmax = hmax_v, a.lab = m.at(lab), a.part = m.at(part), a.xlab = m.at(xlab), a.lse = m.at(lse);
+    a.C = C, a.wmax = wmax, a.hmax = hmax_v, a.lab = m.at(lab), a.part = m.at(part), a.xlab = m.at(xlab), a.norm = m.at(norm);
     a.A = m.at(Wf), a.KSA = p.KSd, a.B = m.at(Hf), a.KSB = p.KSd;
     a.mt = ct, a.nt = p.Rp / TN, a.steps = p.steps_d, a.rows_are = 2;
     HT_TRY(split_nt(ctx, st, LOSS, a));
-    k_head_join<<<(unsigned)jb, 1024, 0, st>>>(m.at(part), ct, p.Rp, m.at(total), r0, m.at(idx), m.at(lab), C, weight, m.at(xlab), m.at(lse), row_loss, row_lse,
+    k_head_join<<<(unsigned)jb, 1024, 0, st>>>(m.at(part), ct, p.Rp, m.at(total), r0, m.at(idx), m.at(lab), C, weight, m.at(xlab), m.at(norm), row_loss, row_lse,
                                                m.at(ploss) + k * jb);
     HT_LAUNCH_CHECK(ctx);
     if (!grad) continue;

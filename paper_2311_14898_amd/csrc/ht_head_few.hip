@@ -192,8 +192,8 @@ __global__ void __launch_bounds__(256) k_few_logits(FewArgs a) {
   }
 }
 
-// A block a row; the last of them to come to an end adds up the losses.  lse_of, l_of: of the labelled rows in order.
-__global__ void __launch_bounds__(256) k_few_join(FewArgs a, const float* __restrict__ weight, int mean, float* __restrict__ lse_of, float* __restrict__ l_of,
+// A block a row; the last of them to come to an end adds up the losses.  norm (largest logit m, 1 / sum of exp(x - m)), l_of: of the labelled rows in order.
+__global__ void __launch_bounds__(256) k_few_join(FewArgs a, const float* __restrict__ weight, int mean, float2* __restrict__ norm, float* __restrict__ l_of,
                                                   float* __restrict__ row_loss, float* __restrict__ row_lse, float* __restrict__ loss) {
   __shared__ int idx[64];
   __shared__ int32_t lab[64];
@@ -226,7 +226,7 @@ __global__ void __launch_bounds__(256) k_few_join(FewArgs a, const float* __rest
       z = 0.f;
       for (int w = 0; w < 4; ++w) z += sh[w].x == -INFINITY ? sh[w].y : sh[w].y * exp_less(sh[w].x, m);
       const float lse = m + logf(z), l = lab[v] < a.C ? lse - a.xlab[v] : NAN;
-      lse_of[v] = lse;
+      norm[v] = make_float2(m, 1.f / z);
       __hip_atomic_store(l_of + v, weight ? weight[at] * l : l, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       if (row_loss) row_loss[at] = l;
       if (row_lse) row_lse[at] = lse;
@@ -243,7 +243,7 @@ __global__ void __launch_bounds__(256) k_few_join(FewArgs a, const float* __rest
 
 struct FewGrad {
   const float* weight;
-  const float* lse;
+  const float2* norm;
   int mean, add;
   float* dW;                       // (null: not wanted), pitch ldd
   int64_t ldd;
@@ -257,13 +257,14 @@ __global__ void __launch_bounds__(256) k_few_grad(FewArgs a, FewGrad g) {
   __shared__ float Ps[NB * 16][PP];
   __shared__ int idx[64];
   __shared__ int32_t lab[64];
-  __shared__ float lse[64], scale[64];
+  __shared__ float2 norm[64];
+  __shared__ float scale[64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 15, q = lane >> 4;
   const FewRows rows(a.labels, a.V, idx, lab);
   if (threadIdx.x < 64) {
     const int v = threadIdx.x;
     const bool there = v < rows.n;
-    lse[v] = there ? g.lse[v] : 0.f;
+    norm[v] = there ? g.norm[v] : make_float2(0.f, 0.f);
     scale[v] = there ? (g.weight ? g.weight[idx[v]] : 1.f) * (g.mean ? 1.f / (float)rows.n : 1.f) : 0.f;
   }
   const int j0 = blockIdx.y * JT + wave * 64, jl = j0 + 4 * l, jleft = a.d - jl;      // the lane's four features, and how many of them there are
@@ -308,7 +309,7 @@ __global__ void __launch_bounds__(256) k_few_grad(FewArgs a, FewGrad g) {
     fetch_x(t0);
     if (g.part) fetch_w(t0);
   }
-  __syncthreads();                         // (lse, scale)
+  __syncthreads();                         // (norm, scale)
   for (int tile = t0; tile < t1; ++tile) {
     const int64_t c0 = (int64_t)tile * CT;
 #pragma unroll
@@ -318,7 +319,7 @@ __global__ void __launch_bounds__(256) k_few_grad(FewArgs a, FewGrad g) {
       if (v < rows.n) {
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-          if (c0 + c + k < a.C) p[k] = (exp_less(x[b][k], lse[v]) - (c0 + c + k == lab[v] ? 1.f : 0.f)) * scale[v];
+          if (c0 + c + k < a.C) p[k] = (exp_less(x[b][k], norm[v].x) * norm[v].y - (c0 + c + k == lab[v] ? 1.f : 0.f)) * scale[v];
       }
       *reinterpret_cast<v4f*>(&Ps[v][c]) = p;
     }
@@ -436,18 +437,19 @@ int ht_head_few(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht
   OpsBlock m;
   const auto X = m.add<float>(grad ? NB * 16 * ldx : 0);
   const auto part = m.add<float2>((int64_t)64 * blocks);
-  const auto xlab = m.add<float>(64), lse = m.add<float>(64), lrow = m.add<float>(64);
+  const auto xlab = m.add<float>(64), lrow = m.add<float>(64);
+  const auto norm = m.add<float2>(64);
   const auto ticket = m.add<unsigned>(1);
   const auto ph = m.add<float>(dH ? (int64_t)gx * NB * 16 * d : 0);
   HT_TRY(m.take(ctx));
   const FewArgs a{H->ptr, H->ld, H->rows, d, C, W->ptr, W->ld, labels, grad ? m.at(X) : nullptr, ldx, m.at(part), blocks, m.at(xlab), m.at(ticket)};
-  const FewGrad g{weight, m.at(lse), mean, D->accumulate_dW, dW ? dW->ptr : nullptr, dW ? dW->ld : 0, dH ? m.at(ph) : nullptr, tiles};
+  const FewGrad g{weight, m.at(norm), mean, D->accumulate_dW, dW ? dW->ptr : nullptr, dW ? dW->ld : 0, dH ? m.at(ph) : nullptr, tiles};
   auto run = [&](auto nb, auto form) -> int {
     constexpr int N = decltype(nb)::value;
     constexpr bool F = decltype(form)::value;
     k_few_logits<N, F><<<(unsigned)blocks, 256, 0, st>>>(a);
     HT_LAUNCH_CHECK(ctx);
-    k_few_join<<<(unsigned)H->rows, 256, 0, st>>>(a, weight, mean, m.at(lse), m.at(lrow), row_loss, row_lse, loss);
+    k_few_join<<<(unsigned)H->rows, 256, 0, st>>>(a, weight, mean, m.at(norm), m.at(lrow), row_loss, row_lse, loss);
     HT_LAUNCH_CHECK(ctx);
     if (!grad) return HT_OK;
     k_few_grad<N, F><<<dim3((unsigned)gx, (unsigned)gy), 256, 0, st>>>(a, g);

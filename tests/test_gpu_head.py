@@ -190,6 +190,42 @@ def test_labels_beyond_the_classes_and_values_that_are_not_finite(ctx):
         assert (out["row_loss"][rest] == good["row_loss"][rest]).all() and (out["dH"][rest] == good["dH"][rest]).all()
 
 
+@pytest.mark.parametrize("n", [40, 70])
+@pytest.mark.parametrize("first,last", [(0, 300), (300, 600), (599, 600)])
+def test_weights_that_are_not_numbers_reach_every_row(ctx, n, first, last):
+    """Whole tiles of classes without a largest logit, before and behind others."""
+    H, W, y = _inputs(n, 32, 600, np.random.default_rng(14))
+    W[5, first:last] = np.nan
+    for form in (B.HT_W_IN_OUT, B.HT_W_OUT_IN):
+        out = call(ctx, H, W, y, form)
+        assert np.isnan(out["loss"]) and np.isnan(out["row_loss"]).all() and np.isnan(out["row_lse"]).all()
+        assert np.isnan(out["dH"]).all() and np.isnan(out["dW"]).all()
+
+
+@pytest.mark.parametrize("n", [8, 90])
+def test_logits_of_millions(ctx, n):
+    """Far from 0 the rows' own differences count: integers, whose logits are exact, so that tolerances have no part of the products' errors."""
+    rng = np.random.default_rng(15)
+    d, C = 4, 700
+    H = rng.integers(1, 5, (n, d)).astype(np.float32)
+    W = (rng.integers(-3, 4, (d, C)) + np.array([[1 << 20], [0], [0], [0]])).astype(np.float32)
+    y = rng.integers(0, C, n)
+    x = H.astype(np.float64) @ W.astype(np.float64)
+    p = np.exp(x - x.max(axis=1, keepdims=True))
+    p /= p.sum(axis=1, keepdims=True)
+    g = p.copy()
+    g[np.arange(n), y] -= 1.0
+    out = call(ctx, H, W, y, B.HT_W_IN_OUT, mean=False)
+    # p: the exponential's argument (up to 100) in half steps, two steps of its own, the sum of 700 terms; products and their sums as above
+    rel = 2.0 ** -24 * (100 + 4) + 20 * STEP
+    pe = p * rel + 2.0 ** -39
+    pe[np.arange(n), y] += 2 * STEP
+    terms = 3 * 2.0 ** -22 + (3 * C / 16 + 64) * STEP
+    assert (np.abs(out["dW"] - H.T.astype(np.float64) @ g) <= H.T @ pe + terms * (H.T @ np.abs(g))).all()
+    # dH = sum over classes of g W, where each row's g has the sum 0: W's common part, 2^20, multiplies what rounding leaves of it
+    assert (np.abs(out["dH"] - g @ W.T.astype(np.float64)) <= pe @ np.abs(W).T + terms * (np.abs(g) @ np.abs(W).T)).all()
+
+
 def test_differences(ctx):
     """Gradients against central differences of the loss in 64 bits at the same point, and of the call's own loss."""
     rng = np.random.default_rng(11)
