@@ -123,7 +123,7 @@ typedef float V4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ float4 zero4() { return make_float4(0.f, 0.f, 0.f, 0.f); }
 
 // T threads a row, NV float4 of it in each thread's registers; what goes beyond (MORE) is read once more for the gradient, the last read first, while some of
-// it is still in the caches.  Rows of T x NV x 4 classes.  Short rows want waves (at most 72 registers: 100,003 rows x 172 56.7 -> 53.2 us); long rows
+// it is still in the caches.  Rows of T x NV x 4 classes.  Short rows want waves (at most 72 registers: 100,003 rows x 172 56.7 -> 53.2 us, with three float4s a thread for four 51.3); long rows
 // past the caches, loads and stores that are not for them (4,096 x 131,072, where 49,152 classes stay in registers: 1.15 ms, with such stores 1.08, with loads too 1.05).
 template <int T, int NV, bool MORE>
 __global__ void __launch_bounds__(T < 256 ? 256 : T, T < 256 ? 7 : 1) k_distill(DistillArgs a, const unsigned long long* __restrict__ cnt, int n_cnt, double* __restrict__ part) {
@@ -250,6 +250,7 @@ __global__ void __launch_bounds__(T < 256 ? 256 : T, T < 256 ? 7 : 1) k_distill(
 #pragma unroll
     for (int u2 = 0; u2 < NV; ++u2) put(u2, keep[u2]);
     row.sync();
+    if (l < (-a.C & 3)) g[a.C + l] = 0.f;        // (NaN until here where the row's weight is not finite)
 #pragma unroll
     for (int e = 0; e < EK; ++e) {
       const int k = e * T + l;
@@ -443,6 +444,7 @@ void with_shape(int C, F&& f) {
   using std::integral_constant;
   if (C <= 64) go(integral_constant<int, 16>(), integral_constant<int, 1>());
   else if (C <= 128) go(integral_constant<int, 16>(), integral_constant<int, 2>());
+  else if (C <= 192) go(integral_constant<int, 16>(), integral_constant<int, 3>());
   else if (C <= 256) go(integral_constant<int, 16>(), integral_constant<int, 4>());
   else if (C <= 512) go(integral_constant<int, 64>(), integral_constant<int, 2>());
   else if (C <= 1024) go(integral_constant<int, 64>(), integral_constant<int, 4>());

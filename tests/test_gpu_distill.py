@@ -197,3 +197,29 @@ def test_refusals(ctx):
     refused(B.HT_EINVAL, X=big[:4], dlogits=big[1:])
     with pytest.raises(AssertionError):
         B.ht_distill_loss(ctx, 8, X, ids.long(), top, loss)
+
+
+@pytest.mark.parametrize("inplace", [False, True])
+@pytest.mark.parametrize("n,C,K", [(70, 66_003, 40), (65, 131_073, 256)])
+def test_rows_past_the_registers(ctx, n, C, K, inplace):
+    X, ids, top = _inputs(n, C, K, np.random.default_rng(n), missing=0.1)
+    X[1, ::3] = -np.inf
+    ids[1] = np.where(ids[1] % 3 == 0, -1, ids[1])
+    ids[2, 1::2] = ids[2, 0]
+    ref, tol = reference(X, ids, top, 2.0, None, True)
+    check(call(ctx, X, ids, top, 2.0, inplace=inplace), ref, tol)
+
+
+@pytest.mark.parametrize("n,C", [(3, 5), (40, 70), (5, 190), (6, 301), (3, 5_001), (66, 5_001), (65, 66_003)])
+def test_what_lies_behind_the_last_class(ctx, n, C):
+    X, ids, top = _inputs(n, C, 4, np.random.default_rng(C), missing=0.0)
+    ids[n - 1] = -1
+    u = np.full(n, np.inf, np.float32)
+    u[0] = np.nan
+    wide = (C + 3) // 4 * 4
+    Xd = torch.full((n, wide), float("nan"), device="cuda")
+    Xd[:, :C] = torch.from_numpy(X).cuda()
+    dX = torch.full_like(Xd, 7.0)
+    loss = torch.zeros(1, device="cuda")
+    B.ht_distill_loss(ctx, C, Xd, torch.from_numpy(ids.astype(np.int32)).cuda(), torch.from_numpy(top).cuda(), loss, row_weight=torch.from_numpy(u).cuda(), dlogits=dX)
+    assert (dX[:, C:] == 0).all() and dX[0, :C].isnan().all() and (dX[n - 1] == 0).all() and not dX[1:n - 1, :C].isfinite().all()
