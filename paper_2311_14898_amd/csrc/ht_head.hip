@@ -119,6 +119,48 @@ __global__ void __launch_bounds__(256) k_head_place(const int32_t* __restrict__ 
   if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) *total = at;
 }
 
+// All of that in one launch for up to LIST_ROWS rows: blocks of 256 rows, each counting what lies before it, then clear_blocks that clear n4
+// fours of words.  us of a call, so | in three launches: 80 rows x 256 features x 131,072 classes 322 | 328, 5,000 x 64 x 500 134 | 138, 8,000 x 100 x 30,000 4 less.
+constexpr int64_t LIST_ROWS = 16384;
+__global__ void __launch_bounds__(256) k_head_list(const int32_t* __restrict__ labels, int64_t V, unsigned blocks, int32_t* __restrict__ idx, int32_t* __restrict__ lab,
+                                                   int64_t* __restrict__ total, float* __restrict__ row_loss, float* __restrict__ row_lse, float* __restrict__ dH,
+                                                   int64_t ld, int d, uint4* __restrict__ clear, int64_t n4) {
+  __shared__ int sh[4], here[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (blockIdx.x >= blocks) {
+    for (int64_t i = (int64_t)(blockIdx.x - blocks) * 256 + threadIdx.x; i < n4; i += (int64_t)(gridDim.x - blocks) * 256) clear[i] = make_uint4(0, 0, 0, 0);
+    return;
+  }
+  const int v0 = blockIdx.x * 256;
+  int before = 0;
+#pragma unroll 8
+  for (int v = threadIdx.x; v < v0; v += 256) before += labels[v] >= 0;
+  for (int o = 32; o > 0; o >>= 1) before += __shfl_xor(before, o, 64);
+  const int64_t v = v0 + threadIdx.x;
+  const int32_t y = v < V ? labels[v] : -1;
+  const uint64_t mask = __ballot(y >= 0);
+  if (lane == 0) sh[wave] = before, here[wave] = __popcll(mask);
+  __syncthreads();
+  int at = sh[0] + sh[1] + sh[2] + sh[3], all = 0;
+  for (int w = 0; w < 4; ++w) at += w < wave ? here[w] : 0, all += here[w];
+  if (y >= 0) {
+    const int k = at + __popcll(mask & ((1ull << lane) - 1));
+    idx[k] = (int32_t)v;
+    lab[k] = y;
+  } else if (v < V) {
+    if (row_loss) row_loss[v] = 0.f;
+    if (row_lse) row_lse[v] = 0.f;
+  }
+  if (blockIdx.x == blocks - 1 && threadIdx.x == 0) *total = sh[0] + sh[1] + sh[2] + sh[3] + all;
+  if (!dH) return;
+  uint64_t none = __ballot(y < 0 && v < V);
+  while (none) {
+    const int r = __builtin_ctzll(none);
+    none &= none - 1;
+    for (int c = lane * 4; c < d; c += 256) *reinterpret_cast<float4*>(dH + (v0 + wave * 64 + r) * ld + c) = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+}
+
 // Rows of a piece: what is left of the list from r0 on, at most `most`.
 __device__ __forceinline__ int64_t piece_rows(const int64_t* total, int64_t r0, int64_t most) {
   const int64_t left = *total - r0;
@@ -528,10 +570,6 @@ __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
       const bool there = v < rows;
       const float hs = unscale_of(a.hmax[v]) * ws;
       float m = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) acc[i][j][e] *= hs;
       if (left < 64) {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -543,13 +581,13 @@ __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
       for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int e = 0; e < 16; ++e) m = fmaxf(m, acc[i][j][e]);
-      m = fmaxf(m, __shfl_xor(m, 32, 64));
+      m = fmaxf(m, __shfl_xor(m, 32, 64)) * hs;
       const float m1 = m == -INFINITY ? 0.f : m;      // (a wave behind the last class: exp(-inf) throughout)
       float z = 0.f;
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) z += exp_less(acc[i][j][e], m1);
+        for (int e = 0; e < 16; ++e) z += __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], hs, -m1) * LOG2E);
       z += __shfl_xor(z, 32, 64);
       if (half == 0) red[wave * TN + j * 32 + l32] = make_float2(m, z);
       const int64_t off = there ? a.lab[a.r0 + v] - (a.c0 + mw) : -1;
@@ -559,7 +597,7 @@ __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
         for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int e = 0; e < 16; ++e)
-            if (mine && off == i * 32 + (e >> 2) * 8 + half * 4 + (e & 3)) a.xlab[v] = acc[i][j][e];
+            if (mine && off == i * 32 + (e >> 2) * 8 + half * 4 + (e & 3)) a.xlab[v] = acc[i][j][e] * hs;
       }
     }
     __syncthreads();
@@ -791,13 +829,20 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
 
   uint32_t *wmax = m.at(mx), *hmax_v = wmax + 4, *hmax_j = hmax_v + p.Rp;
   const unsigned clear_blocks = (unsigned)std::min<int64_t>(ceil_div64(n_max, 4096), 1024);
-  k_head_count<<<(unsigned)rb + clear_blocks, 256, 0, st>>>(labels, V, rpb, m.at(cnt), (unsigned)rb, (uint4*)wmax, n_max / 4);
-  HT_LAUNCH_CHECK(ctx);
-  k_head_place<<<(unsigned)rb, 256, 0, st>>>(labels, V, rpb, m.at(cnt), m.at(idx), m.at(lab), m.at(total), row_loss, row_lse);
-  HT_LAUNCH_CHECK(ctx);
-  if (dH && V > 0) {
-    k_head_clear<<<(unsigned)std::min<int64_t>(ceil_div64(V, 256), CLEAR_BLOCKS), 256, 0, st>>>(labels, V, dH->ptr, dH->ld, (int)d);
+  if (V <= LIST_ROWS) {
+    const unsigned blocks = (unsigned)std::max<int64_t>(1, ceil_div64(V, 256));
+    k_head_list<<<blocks + clear_blocks, 256, 0, st>>>(labels, V, blocks, m.at(idx), m.at(lab), m.at(total), row_loss, row_lse, dH ? dH->ptr : nullptr, dH ? dH->ld : 0,
+                                                       (int)d, (uint4*)wmax, n_max / 4);
     HT_LAUNCH_CHECK(ctx);
+  } else {
+    k_head_count<<<(unsigned)rb + clear_blocks, 256, 0, st>>>(labels, V, rpb, m.at(cnt), (unsigned)rb, (uint4*)wmax, n_max / 4);
+    HT_LAUNCH_CHECK(ctx);
+    k_head_place<<<(unsigned)rb, 256, 0, st>>>(labels, V, rpb, m.at(cnt), m.at(idx), m.at(lab), m.at(total), row_loss, row_lse);
+    HT_LAUNCH_CHECK(ctx);
+    if (dH) {
+      k_head_clear<<<(unsigned)std::min<int64_t>(ceil_div64(V, 256), CLEAR_BLOCKS), 256, 0, st>>>(labels, V, dH->ptr, dH->ld, (int)d);
+      HT_LAUNCH_CHECK(ctx);
+    }
   }
   {
     const Source s{W->ptr, W->ld, W->rows, W->cols, nullptr, nullptr, nullptr, 0};
