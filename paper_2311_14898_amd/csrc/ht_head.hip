@@ -71,19 +71,6 @@ __global__ void __launch_bounds__(256) k_head_count(const int32_t* __restrict__ 
   if (threadIdx.x == 0) cnt[blockIdx.x] = sh[0] + sh[1] + sh[2] + sh[3];
 }
 
-// Zeros in dH's rows without a label, a wave 64 rows at a time.
-__global__ void __launch_bounds__(256) k_head_clear(const int32_t* __restrict__ labels, int64_t V, float* __restrict__ dH, int64_t ld, int d) {
-  const int lane = threadIdx.x & 63;
-  for (int64_t v0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * 64; v0 < V; v0 += (int64_t)gridDim.x * 256) {
-    uint64_t none = __ballot(v0 + lane < V && labels[v0 + lane < V ? v0 + lane : V - 1] < 0);
-    while (none) {
-      const int r = __builtin_ctzll(none);
-      none &= none - 1;
-      for (int c = lane * 4; c < d; c += 256) __builtin_nontemporal_store(V4{0.f, 0.f, 0.f, 0.f}, reinterpret_cast<V4*>(dH + (v0 + r) * ld + c));
-    }
-  }
-}
-
 // idx, lab: the labelled rows in order, and their labels; *total: how many.  Losses of rows without a label are cleared here.
 __global__ void __launch_bounds__(256) k_head_place(const int32_t* __restrict__ labels, int64_t V, int64_t rpb, const int32_t* __restrict__ cnt,
                                                     int32_t* __restrict__ idx, int32_t* __restrict__ lab, int64_t* __restrict__ total,
@@ -181,30 +168,57 @@ struct Source {
   __device__ __forceinline__ int64_t row(int64_t r) const { return idx ? (int64_t)idx[r0 + r] : r; }
 };
 
-// Largest absolute values of rows, and of columns (of weighted rows), as bits, into arrays that hold zeros.  (Maxima do not depend on their order.)
+// One launch finds the largest absolute values (as bits; maxima do not depend on their order) that a piece's operands are scaled by, and clears what has no
+// gradient: blocks for H, blocks for W, blocks for dH, all of which the first piece has.  Memory is idle otherwise while so few blocks look for the values
+// of a few labelled rows of many (1,000,000 rows x 256 features, 1 % of them labelled, 172 classes: 330 us, in launches of their own 358; 5,000 x 64 x 500 118 | 134).
+struct HeadTop {
+  // H: largest values of rows, and of columns (of weighted rows), into arrays that hold zeros
+  Source s;
+  uint32_t *rmax, *cmax;
+  unsigned gx, gy;               // blocks along rows, along columns
+  // W: of all of it
+  const float* W;
+  int64_t ldw, wrows, wcols;
+  uint32_t* wmax;
+  unsigned w_blocks;             // (0: it is known)
+  // dH: its rows without a label
+  const int32_t* labels;
+  int64_t V;
+  float* dH;
+  int64_t ld;
+  int d;
+  unsigned clear_blocks;         // (0: nothing to clear)
+};
+
 // A wave takes RW rows at a time, a block AMAX_COLS columns of them; columns are joined once a block.
 constexpr int AMAX_COLS = 512, RW = 4;
-__global__ void __launch_bounds__(256) k_amax(Source s, uint32_t* __restrict__ rmax, uint32_t* __restrict__ cmax) {
+__device__ __forceinline__ void amax_of_h(const HeadTop& a, int bx, int by) {
   constexpr int Q = AMAX_COLS / 64;
   __shared__ uint32_t sh[4][AMAX_COLS], shr[4 * RW];
+  const Source& s = a.s;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t n = s.n(), c0 = (int64_t)blockIdx.y * AMAX_COLS + lane;
+  const int64_t n = s.n(), c0 = (int64_t)by * AMAX_COLS + lane;
   uint32_t cm[Q];
 #pragma unroll
   for (int k = 0; k < Q; ++k) cm[k] = 0;
-  for (int64_t g0 = (int64_t)blockIdx.x * (4 * RW); g0 < n; g0 += (int64_t)gridDim.x * (4 * RW)) {
+  for (int64_t g0 = (int64_t)bx * (4 * RW); g0 < n; g0 += (int64_t)a.gx * (4 * RW)) {
     const int64_t r0 = g0 + wave * RW;
+    float x[RW][Q], w[RW];
 #pragma unroll
     for (int q = 0; q < RW; ++q) {
       const int64_t r = r0 + q < n ? r0 + q : n - 1, v = s.row(r);
       const float* p = s.p + v * s.ld;
-      const float w = s.weight ? s.weight[v] : 1.f;
+      w[q] = s.weight ? s.weight[v] : 1.f;
+#pragma unroll
+      for (int k = 0; k < Q; ++k) x[q][k] = p[c0 + k * 64 < s.cols ? c0 + k * 64 : s.cols - 1];       // (behind the last column: that once more)
+    }
+#pragma unroll
+    for (int q = 0; q < RW; ++q) {
       uint32_t rm = 0;
 #pragma unroll
       for (int k = 0; k < Q; ++k) {
-        const float x = c0 + k * 64 < s.cols ? p[c0 + k * 64] : 0.f;
-        rm = max(rm, __float_as_uint(fabsf(x)));
-        cm[k] = max(cm[k], __float_as_uint(fabsf(x * w)));
+        rm = max(rm, __float_as_uint(fabsf(x[q][k])));
+        cm[k] = max(cm[k], __float_as_uint(fabsf(x[q][k] * w[q])));
       }
       for (int o = 32; o > 0; o >>= 1) rm = max(rm, (uint32_t)__shfl_xor((int)rm, o, 64));
       if (lane == 0) shr[wave * RW + q] = rm;
@@ -212,8 +226,8 @@ __global__ void __launch_bounds__(256) k_amax(Source s, uint32_t* __restrict__ r
     // (one request for the block's rows, not one for each)
     __syncthreads();
     if (threadIdx.x < 4 * RW && g0 + threadIdx.x < n) {
-      if (gridDim.y == 1) rmax[g0 + threadIdx.x] = shr[threadIdx.x];
-      else atomicMax(rmax + g0 + threadIdx.x, shr[threadIdx.x]);
+      if (a.gy == 1) a.rmax[g0 + threadIdx.x] = shr[threadIdx.x];
+      else atomicMax(a.rmax + g0 + threadIdx.x, shr[threadIdx.x]);
     }
     __syncthreads();
   }
@@ -221,25 +235,20 @@ __global__ void __launch_bounds__(256) k_amax(Source s, uint32_t* __restrict__ r
   for (int k = 0; k < Q; ++k) sh[wave][k * 64 + lane] = cm[k];
   __syncthreads();
   for (int k = threadIdx.x; k < AMAX_COLS; k += 256) {
-    const int64_t c = (int64_t)blockIdx.y * AMAX_COLS + k;
+    const int64_t c = (int64_t)by * AMAX_COLS + k;
     const uint32_t m = max(max(sh[0][k], sh[1][k]), max(sh[2][k], sh[3][k]));
-    if (c < s.cols) atomicMax(cmax + c, m);
+    if (c < s.cols) atomicMax(a.cmax + c, m);
   }
 }
 constexpr int64_t AMAX_BLOCKS = 1024, ABSMAX_BLOCKS = 1024;   // (as many requests to one word: 2,048 of them take 27 us)
-void launch_amax(hipStream_t st, const Source& s, uint32_t* rmax, uint32_t* cmax) {
-  const int64_t gy = ceil_div64(s.cols, AMAX_COLS), gx = std::min(ceil_div64(s.rows, 4 * RW), std::max<int64_t>(1, AMAX_BLOCKS / gy));
-  k_amax<<<dim3((unsigned)std::max<int64_t>(1, gx), (unsigned)gy), 256, 0, st>>>(s, rmax, cmax);
-}
 
-// The largest absolute value of a matrix, as bits.
-__global__ void __launch_bounds__(256) k_absmax(const float* __restrict__ p, int64_t ld, int64_t rows, int64_t cols, uint32_t* __restrict__ out) {
+__device__ __forceinline__ void amax_of_w(const HeadTop& a, unsigned block) {
   __shared__ uint32_t sh[4];
   constexpr int U = 16;                  // units of 256 columns of a row, at a time
-  const uint32_t parts = (uint32_t)((cols + 255) / 256);
-  const int64_t n = rows * parts;
+  const uint32_t parts = (uint32_t)((a.wcols + 255) / 256);
+  const int64_t n = a.wrows * parts;
   uint32_t m = 0;
-  for (int64_t i = (int64_t)blockIdx.x * U; i < n; i += (int64_t)gridDim.x * U) {
+  for (int64_t i = (int64_t)block * U; i < n; i += (int64_t)a.w_blocks * U) {
     const int64_t r0 = i / parts;
     const uint32_t q0 = (uint32_t)(i - r0 * parts);
     float x[U];
@@ -247,7 +256,7 @@ __global__ void __launch_bounds__(256) k_absmax(const float* __restrict__ p, int
     for (int u = 0; u < U; ++u) {
       const uint32_t q = (q0 + u) / parts;
       const int64_t r = r0 + q, c = (int64_t)(q0 + u - q * parts) * 256 + threadIdx.x;
-      x[u] = p[(r < rows ? r : rows - 1) * ld + (c < cols ? c : cols - 1)];       // (behind the last ones: those again)
+      x[u] = a.W[(r < a.wrows ? r : a.wrows - 1) * a.ldw + (c < a.wcols ? c : a.wcols - 1)];       // (behind the last ones: those again)
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) m = max(m, __float_as_uint(fabsf(x[u])));
@@ -255,7 +264,28 @@ __global__ void __launch_bounds__(256) k_absmax(const float* __restrict__ p, int
   for (int o = 32; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
   if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = m;
   __syncthreads();
-  if (threadIdx.x == 0) atomicMax(out, max(max(sh[0], sh[1]), max(sh[2], sh[3])));
+  if (threadIdx.x == 0) atomicMax(a.wmax, max(max(sh[0], sh[1]), max(sh[2], sh[3])));
+}
+
+// A wave 64 rows at a time.
+__device__ __forceinline__ void clear_rows(const HeadTop& a, unsigned block) {
+  const int lane = threadIdx.x & 63;
+  for (int64_t v0 = ((int64_t)block * 4 + (threadIdx.x >> 6)) * 64; v0 < a.V; v0 += (int64_t)a.clear_blocks * 256) {
+    uint64_t none = __ballot(v0 + lane < a.V && a.labels[v0 + lane < a.V ? v0 + lane : a.V - 1] < 0);
+    while (none) {
+      const int r = __builtin_ctzll(none);
+      none &= none - 1;
+      for (int c = lane * 4; c < a.d; c += 256) __builtin_nontemporal_store(V4{0.f, 0.f, 0.f, 0.f}, reinterpret_cast<V4*>(a.dH + (v0 + r) * a.ld + c));
+    }
+  }
+}
+
+__global__ void __launch_bounds__(256) k_head_top(HeadTop a) {
+  unsigned block = blockIdx.x;
+  if (block < a.gx * a.gy) return amax_of_h(a, (int)(block / a.gy), (int)(block % a.gy));
+  block -= a.gx * a.gy;
+  if (block < a.w_blocks) return amax_of_w(a, block);
+  clear_rows(a, block - a.w_blocks);
 }
 
 __device__ __forceinline__ void split2(float x, _Float16* hi, _Float16* lo) {
@@ -266,13 +296,30 @@ __device__ __forceinline__ void split2(float x, _Float16* hi, _Float16* lo) {
 // Fragments of the matrix by rows (reduction along columns: KS steps) and by columns (reduction along rows, weighted: KS_t steps), zeros behind
 // the last row and column, a 64 x 64 tile a block.
 // `all`: the largest value of everything, where it is scaled by one factor.
-__global__ void __launch_bounds__(256) k_pack(Source s, const uint32_t* __restrict__ rmax, const uint32_t* __restrict__ cmax, const uint32_t* __restrict__ all,
-                                              _Float16* __restrict__ R, int64_t KS, _Float16* __restrict__ T, int64_t KS_t, int64_t row_tile, unsigned col_tiles) {
+struct Pack {
+  Source s;
+  const uint32_t *rmax, *cmax, *all;
+  _Float16* R;
+  int64_t KS;
+  _Float16* T;
+  int64_t KS_t, row_tile;
+  unsigned col_tiles, blocks;
+};
+// (H's, in the first blocks, and then W's, with the first piece of rows: W's blocks keep the memory busy that H's few do not)
+__global__ void __launch_bounds__(256) k_pack(Pack first, Pack second) {
+  const bool is_first = blockIdx.x < first.blocks;
+  const Pack& a = is_first ? first : second;
+  const unsigned block = is_first ? blockIdx.x : blockIdx.x - first.blocks;
+  const Source s = a.s;
+  const uint32_t *__restrict__ rmax = a.rmax, *__restrict__ cmax = a.cmax, *__restrict__ all = a.all;
+  _Float16 *__restrict__ R = a.R, *__restrict__ T = a.T;
+  const int64_t KS = a.KS, KS_t = a.KS_t, row_tile = a.row_tile;
+  const unsigned col_tiles = a.col_tiles;
   __shared__ float sh[64][65];
   __shared__ float wt[64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, half = lane >> 5;
   const int64_t n = s.n(), tiles = up_to(n, row_tile) / 64 * col_tiles;
-  for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+  for (int64_t tile = block; tile < tiles; tile += a.blocks) {
     const int64_t r0 = tile / col_tiles * 64, c0 = tile % col_tiles * 64;
 #pragma unroll
     for (int q = 0; q < 16; ++q) {
@@ -839,29 +886,29 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
     HT_LAUNCH_CHECK(ctx);
     k_head_place<<<(unsigned)rb, 256, 0, st>>>(labels, V, rpb, m.at(cnt), m.at(idx), m.at(lab), m.at(total), row_loss, row_lse);
     HT_LAUNCH_CHECK(ctx);
-    if (dH) {
-      k_head_clear<<<(unsigned)std::min<int64_t>(ceil_div64(V, 256), CLEAR_BLOCKS), 256, 0, st>>>(labels, V, dH->ptr, dH->ld, (int)d);
-      HT_LAUNCH_CHECK(ctx);
-    }
   }
-  {
-    const Source s{W->ptr, W->ld, W->rows, W->cols, nullptr, nullptr, nullptr, 0};
-    k_absmax<<<(unsigned)std::min<int64_t>(ceil_div64(s.rows * ceil_div64(s.cols, 256), 64), ABSMAX_BLOCKS), 256, 0, st>>>(s.p, s.ld, s.rows, s.cols, wmax);
-    HT_LAUNCH_CHECK(ctx);
-    // by classes: W's rows, or its columns
-    const int64_t rt = up_to(s.rows, in_out ? 64 : TM) / 64, ct64 = up_to(s.cols, in_out ? TM : 64) / 64;
-    k_pack<<<(unsigned)std::min(rt * ct64, PACK_BLOCKS), 256, 0, st>>>(s, nullptr, nullptr, wmax, in_out ? nullptr : m.at(Wf), p.KSd, in_out ? m.at(Wf) : nullptr, p.KSd,
-                                                                      in_out ? 64 : TM, (unsigned)ct64);
-    HT_LAUNCH_CHECK(ctx);
-  }
+  const Source w{W->ptr, W->ld, W->rows, W->cols, nullptr, nullptr, nullptr, 0};
+  HeadTop t{};
+  t.rmax = hmax_v, t.cmax = hmax_j;
+  t.gy = (unsigned)ceil_div64(d, AMAX_COLS), t.gx = (unsigned)std::max<int64_t>(1, std::min(p.Rp / (4 * RW), std::max<int64_t>(1, AMAX_BLOCKS / t.gy)));
+  t.W = w.p, t.ldw = w.ld, t.wrows = w.rows, t.wcols = w.cols, t.wmax = wmax;
+  t.labels = labels, t.V = V, t.dH = dH ? dH->ptr : nullptr, t.ld = dH ? dH->ld : 0, t.d = (int)d;
   for (int64_t k = 0; k < pieces; ++k) {
     const int64_t r0 = k * p.Rp;
     if (k > 0) HT_TRY(ht_fill_zero(ctx, st, hmax_v, (size_t)(p.Rp + p.dpad) * 4));
     const Source s{H->ptr, H->ld, p.Rp, d, m.at(idx), weight, m.at(total), r0};
-    launch_amax(st, s, hmax_v, hmax_j);
+    t.s = s;
+    t.w_blocks = k > 0 ? 0 : (unsigned)std::min<int64_t>(ceil_div64(w.rows * ceil_div64(w.cols, 256), 64), ABSMAX_BLOCKS);
+    t.clear_blocks = k > 0 || !dH || V <= LIST_ROWS ? 0 : (unsigned)std::min<int64_t>(ceil_div64(V, 256), CLEAR_BLOCKS);
+    k_head_top<<<t.gx * t.gy + t.w_blocks + t.clear_blocks, 256, 0, st>>>(t);
     HT_LAUNCH_CHECK(ctx);
-    k_pack<<<(unsigned)std::min(p.Rp / 64 * ceil_div64(d, 64), PACK_BLOCKS / 8), 256, 0, st>>>(s, hmax_v, hmax_j, nullptr, m.at(Hf), p.KSd, dW ? m.at(Ht) : nullptr, KSR, TN,
-                                                                     (unsigned)ceil_div64(d, 64));
+    const unsigned hc = (unsigned)ceil_div64(d, 64);
+    const Pack ph{s, hmax_v, hmax_j, nullptr, m.at(Hf), p.KSd, dW ? m.at(Ht) : nullptr, KSR, TN, hc, (unsigned)std::min(p.Rp / 64 * hc, PACK_BLOCKS / 8)};
+    // by classes: W's rows, or its columns
+    const int64_t rt = up_to(w.rows, in_out ? 64 : TM) / 64, wc = up_to(w.cols, in_out ? TM : 64) / 64;
+    const Pack pw{w, nullptr, nullptr, wmax, in_out ? nullptr : m.at(Wf), p.KSd, in_out ? m.at(Wf) : nullptr, p.KSd, in_out ? 64 : TM, (unsigned)wc,
+                  k > 0 ? 0 : (unsigned)std::min(rt * wc, PACK_BLOCKS)};
+    k_pack<<<ph.blocks + pw.blocks, 256, 0, st>>>(ph, pw);
     HT_LAUNCH_CHECK(ctx);
     NtArgs a{};
     a.total = m.at(total), a.r0 = r0, a.most = p.Rp;
