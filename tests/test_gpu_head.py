@@ -327,3 +327,19 @@ def test_refusals(ctx):
         B.ht_head_loss(ctx, 8, 5, H, W, y.long(), loss)
     with pytest.raises(AssertionError):
         B.ht_head_loss(ctx, 8, 5, H, W, y, loss, row_weight=torch.zeros(5, device="cuda"))
+
+
+@pytest.mark.parametrize("n", [16_384, 16_385, 70_001])
+def test_few_labels_among_many_rows(ctx, n):
+    rng = np.random.default_rng(n)
+    d, C = 35, 300
+    H, W, y = _inputs(n, d, C, rng)
+    y[rng.random(n) < 0.98] = -1
+    y[[0, n - 1]] = [-1, 7]
+    H[y < 0] = np.nan                                      # nothing of these rows is read
+    has = y >= 0
+    ref, tol = reference(H[has], W, y[has], None, True)
+    for form in (B.HT_W_IN_OUT, B.HT_W_OUT_IN):
+        out = call(ctx, H, W, y, form)
+        assert (out["dH"][~has] == 0).all() and (out["row_loss"][~has] == 0).all() and (out["row_lse"][~has] == 0).all()
+        check({k: v[has] if k in ("dH", "row_loss", "row_lse") else v for k, v in out.items()}, ref, tol)
