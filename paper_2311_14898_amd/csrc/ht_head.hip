@@ -378,13 +378,16 @@ constexpr int64_t PACK_BLOCKS = 16384;
 
 enum { LOSS, GRAD, SUMS, DIRECT };
 // The sums of dH: as many parts of the reduction as there are blocks for, by the rows that there are, which the host does not know.
+constexpr int64_t LONG_PART = 32, SHORT_PART = 8, ONE_EACH = 256;
 struct HeadSplits {
   int64_t blocks;                 // blocks of the launch, tiles of which have room in the sums
   int64_t nt;                     // tiles along the features
-  int most;
+  int most, most_short;           // parts of LONG_PART and of SHORT_PART steps
   __device__ __forceinline__ int splits(int64_t rows) const {
-    const int64_t tiles = up_to(rows, TM) / TM * nt, s = tiles > 0 ? blocks / tiles : 1;
-    return (int)(s < 1 ? 1 : s < most ? s : most);
+    const int64_t tiles = up_to(rows, TM) / TM * nt;
+    if (tiles == 0) return 1;
+    const int64_t s = blocks / tiles < most ? blocks / tiles : most, t = ONE_EACH / tiles < most_short ? ONE_EACH / tiles : most_short;
+    return (int)(s > t ? s : t > 1 ? t : 1);
   }
 };
 __device__ __forceinline__ float inv_count(const int64_t* total, int mean) { return mean ? 1.f / (float)(*total > 0 ? *total : 1) : 1.f; }
@@ -822,12 +825,14 @@ HeadPlan head_plan(int64_t V, int64_t d, int64_t C, bool in_out, size_t bytes) {
   p.Rp = std::max<int64_t>(TM, std::min(p.Rp, up_to(V, TM)));
   // ... and as many classes as memory allows: every piece of them reads and writes the sums that dH is made of
   p.Cp = std::max(least, std::min<int64_t>(p.Cpad, (int64_t)std::min(bytes, HEAD_PIECE) / (4 * p.Rp) / TM * TM));
-  // parts of a reduction, of 512 values each at least: for dH two blocks a CU; for dW one (what is not split needs no sums: 2,048 rows x 32,768 classes 602 | 593 us)
-  auto splits = [](int64_t tiles, int64_t steps, int64_t most, int64_t blocks) { return (int)std::max<int64_t>(1, std::min({blocks / std::max<int64_t>(tiles, 1), steps / 32, most})); };
-  const int64_t nt = up_to(d, TN) / TN, mt = p.Rp / TM;
-  p.splits_w = splits(p.dpad / TM * (p.Cp / TN), p.Rp / 16, 32, 256);
-  const int most = splits(nt, p.Cp / 16, 128, 512);                        // (of one tile of rows)
-  p.by_rows = HeadSplits{std::max<int64_t>(mt * nt, std::min<int64_t>(512 / nt, mt * most) * nt), nt, most};
+  // Parts of a reduction: for dH of 512 values each at least while there are blocks for two a CU, and of 128 while there are for one (a block that is alone on its CU
+  // waits for its loads, 3 us for 64 values); for dW of 128, one block a CU (what is not split needs no sums: 2,048 rows x 32,768 classes 602 | 593 us).  us of a call
+  // with such short parts, and without: 100 rows x 64 features x 300 classes 73 | 85, 1,000 x 256 x 1,000 105 | 123, 3,000 x 256 x 5,000 174 | 173 (two short ones a CU: 188).
+  const int64_t nt = up_to(d, TN) / TN, mt = p.Rp / TM, steps = p.Cp / 16, tiles_w = p.dpad / TM * (p.Cp / TN);
+  auto parts = [](int64_t a, int64_t b, int64_t most) { return (int)std::max<int64_t>(1, std::min({a, b, most})); };
+  p.splits_w = parts(ONE_EACH / tiles_w, p.Rp / 16 / SHORT_PART, 32);
+  const int most = parts(2 * ONE_EACH / nt, steps / LONG_PART, 128), most_short = parts(ONE_EACH / nt, steps / SHORT_PART, 128);       // (of one tile of rows)
+  p.by_rows = HeadSplits{std::max<int64_t>(mt * nt, std::min<int64_t>(2 * ONE_EACH / nt, mt * std::max(most, most_short)) * nt), nt, most, most_short};
   p.sum_rows = p.by_rows.blocks / nt * TM;
   return p;
 }
