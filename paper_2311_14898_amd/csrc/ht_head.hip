@@ -190,57 +190,56 @@ struct HeadTop {
   unsigned clear_blocks;         // (0: nothing to clear)
 };
 
-// A wave takes RW rows at a time, a block AMAX_COLS columns of them; columns are joined once a block.
-constexpr int AMAX_COLS = 512, RW = 4;
+// lpr lanes take a row's AMAX_COLS columns, four each, and a wave RW rows of each of its groups of lanes at a time; columns are joined once a block.
+constexpr int AMAX_COLS = 256, RW = 8;
+__host__ __device__ __forceinline__ int amax_lanes(int64_t cols) { return cols > 128 ? 64 : cols > 64 ? 32 : 16; }
+__device__ __forceinline__ uint32_t max4(uint4 x) { return max(max(x.x, x.y), max(x.z, x.w)); }
 __device__ __forceinline__ void amax_of_h(const HeadTop& a, int bx, int by) {
-  constexpr int Q = AMAX_COLS / 64;
-  __shared__ uint32_t sh[4][AMAX_COLS], shr[4 * RW];
+  __shared__ __attribute__((aligned(16))) uint32_t sh[4][AMAX_COLS];
+  __shared__ uint32_t shr[4 * RW * 4];
   const Source& s = a.s;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t n = s.n(), c0 = (int64_t)by * AMAX_COLS + lane;
-  uint32_t cm[Q];
-#pragma unroll
-  for (int k = 0; k < Q; ++k) cm[k] = 0;
-  for (int64_t g0 = (int64_t)bx * (4 * RW); g0 < n; g0 += (int64_t)a.gx * (4 * RW)) {
-    const int64_t r0 = g0 + wave * RW;
-    float x[RW][Q], w[RW];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lpr = amax_lanes(s.cols), l = lane & (lpr - 1), groups = 64 / lpr, g = lane / lpr;
+  const int here = 4 * RW * groups;                         // rows of a block at a time
+  const int64_t n = s.n(), c = (int64_t)by * AMAX_COLS + l * 4;
+  const bool there = c < s.cols;
+  uint4 cm = make_uint4(0, 0, 0, 0);
+  for (int64_t r0 = (int64_t)bx * here; r0 < n; r0 += (int64_t)a.gx * here) {
+    float4 x[RW];
+    float w[RW];
 #pragma unroll
     for (int q = 0; q < RW; ++q) {
-      const int64_t r = r0 + q < n ? r0 + q : n - 1, v = s.row(r);
-      const float* p = s.p + v * s.ld;
+      const int64_t at = r0 + (wave * RW + q) * groups + g, v = s.row(at < n ? at : n - 1);
+      x[q] = *reinterpret_cast<const float4*>(s.p + v * s.ld + (there ? c : 0));
       w[q] = s.weight ? s.weight[v] : 1.f;
-#pragma unroll
-      for (int k = 0; k < Q; ++k) x[q][k] = p[c0 + k * 64 < s.cols ? c0 + k * 64 : s.cols - 1];       // (behind the last column: that once more)
     }
 #pragma unroll
     for (int q = 0; q < RW; ++q) {
-      uint32_t rm = 0;
-#pragma unroll
-      for (int k = 0; k < Q; ++k) {
-        rm = max(rm, __float_as_uint(fabsf(x[q][k])));
-        cm[k] = max(cm[k], __float_as_uint(fabsf(x[q][k] * w[q])));
-      }
-      for (int o = 32; o > 0; o >>= 1) rm = max(rm, (uint32_t)__shfl_xor((int)rm, o, 64));
-      if (lane == 0) shr[wave * RW + q] = rm;
+      if (c + 1 >= s.cols) x[q].y = x[q].x;                 // (pad columns, and lanes behind the last column: once more what is there)
+      if (c + 2 >= s.cols) x[q].z = x[q].x;
+      if (c + 3 >= s.cols) x[q].w = x[q].x;
+      auto bits = [](float y) { return __float_as_uint(fabsf(y)); };
+      uint32_t rm = max4(make_uint4(bits(x[q].x), bits(x[q].y), bits(x[q].z), bits(x[q].w)));
+      cm = make_uint4(max(cm.x, bits(x[q].x * w[q])), max(cm.y, bits(x[q].y * w[q])), max(cm.z, bits(x[q].z * w[q])), max(cm.w, bits(x[q].w * w[q])));
+      for (int o = lpr / 2; o > 0; o >>= 1) rm = max(rm, (uint32_t)__shfl_xor((int)rm, o, 64));
+      if (l == 0) shr[(wave * RW + q) * groups + g] = rm;
     }
     // (one request for the block's rows, not one for each)
     __syncthreads();
-    if (threadIdx.x < 4 * RW && g0 + threadIdx.x < n) {
-      if (a.gy == 1) a.rmax[g0 + threadIdx.x] = shr[threadIdx.x];
-      else atomicMax(a.rmax + g0 + threadIdx.x, shr[threadIdx.x]);
+    if ((int)threadIdx.x < here && r0 + threadIdx.x < n) {
+      if (a.gy == 1) a.rmax[r0 + threadIdx.x] = shr[threadIdx.x];
+      else atomicMax(a.rmax + r0 + threadIdx.x, shr[threadIdx.x]);
     }
     __syncthreads();
   }
-#pragma unroll
-  for (int k = 0; k < Q; ++k) sh[wave][k * 64 + lane] = cm[k];
+  for (int o = lpr; o < 64; o <<= 1)
+    cm = make_uint4(max(cm.x, (uint32_t)__shfl_xor((int)cm.x, o, 64)), max(cm.y, (uint32_t)__shfl_xor((int)cm.y, o, 64)),
+                    max(cm.z, (uint32_t)__shfl_xor((int)cm.z, o, 64)), max(cm.w, (uint32_t)__shfl_xor((int)cm.w, o, 64)));
+  if (g == 0) *reinterpret_cast<uint4*>(&sh[wave][l * 4]) = cm;
   __syncthreads();
-  for (int k = threadIdx.x; k < AMAX_COLS; k += 256) {
-    const int64_t c = (int64_t)by * AMAX_COLS + k;
-    const uint32_t m = max(max(sh[0][k], sh[1][k]), max(sh[2][k], sh[3][k]));
-    if (c < s.cols) atomicMax(a.cmax + c, m);
-  }
+  const int64_t k = threadIdx.x, col = (int64_t)by * AMAX_COLS + k;
+  if (k < lpr * 4 && col < s.cols) atomicMax(a.cmax + col, max(max(sh[0][k], sh[1][k]), max(sh[2][k], sh[3][k])));
 }
-constexpr int64_t AMAX_BLOCKS = 1024, ABSMAX_BLOCKS = 1024;   // (as many requests to one word: 2,048 of them take 27 us)
+constexpr int64_t AMAX_BLOCKS = 512, ABSMAX_BLOCKS = 1024;    // (as many requests to one word: 2,048 of them take 27 us)
 
 __device__ __forceinline__ void amax_of_w(const HeadTop& a, unsigned block) {
   __shared__ uint32_t sh[4];
@@ -390,6 +389,11 @@ struct HeadSplits {
     return (int)(s > t ? s : t > 1 ? t : 1);
   }
 };
+// The sums of dW: at most `most` parts of the rows that there are.
+__device__ __forceinline__ int row_parts(int most, int64_t rows) {
+  const int64_t s = rows / (SHORT_PART * 16);
+  return (int)(s < 1 ? 1 : s < most ? s : most);
+}
 __device__ __forceinline__ float inv_count(const int64_t* total, int mean) { return mean ? 1.f / (float)(*total > 0 ? *total : 1) : 1.f; }
 struct NtArgs {
   const _Float16 *A, *B;          // fragments; row blocks KSA, KSB steps apart
@@ -446,7 +450,7 @@ __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
   const int64_t rows = a.total ? piece_rows(a.total, a.r0, a.most) : 0;
   const int64_t mt = a.rows_are == 1 ? up_to(rows, TM) / TM : a.mt, nt = a.rows_are == 2 ? up_to(rows, TN) / TN : a.nt;
   if (EPI == DIRECT && a.r0 > 0 && rows == 0) return;                      // (nothing to add)
-  const int splits = a.rows_are == 1 ? a.by_rows.splits(rows) : a.splits;
+  const int splits = a.rows_are == 1 ? a.by_rows.splits(rows) : a.steps < 0 ? row_parts(a.splits, rows) : a.splits;
   // each XCD takes a contiguous part of the tiles, eight tiles of A over all of B after eight others
   const int64_t tiles = mt * nt, per = (tiles * splits + 7) / 8, ts = (int64_t)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
   if ((int64_t)(blockIdx.x >> 3) >= per || ts >= tiles * splits) return;
@@ -791,13 +795,15 @@ __global__ void __launch_bounds__(256) k_head_dh(const float* __restrict__ sums,
 }
 
 // dW's part [rows x cols] at out (pitch ld): the splits' sums (pitch cols_p, rows_p rows each), scaled by what undoes hmax along rows or columns
-__global__ void __launch_bounds__(256) k_head_dw(const float* __restrict__ sums, int splits, int64_t rows_p, int64_t cols_p, int64_t rows, int64_t cols,
+__global__ void __launch_bounds__(256) k_head_dw(const float* __restrict__ sums, int most_parts, int64_t most, int64_t rows_p, int64_t cols_p, int64_t rows, int64_t cols,
                                                  const uint32_t* __restrict__ hmax, int along_rows, const int64_t* __restrict__ total, int64_t r0, int mean, int add,
                                                  float* __restrict__ out, int64_t ld) {
   if (r0 > 0 && *total <= r0) return;             // (nothing to add)
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, r = i / cols, c = i - r * cols;
   if (r >= rows) return;
+  const int splits = row_parts(most_parts, piece_rows(total, r0, most));
   float s = 0.f;
+#pragma unroll 16
   for (int k = 0; k < splits; ++k) s += sums[((int64_t)k * rows_p + r) * cols_p + c];
   s *= unscale_of(hmax[along_rows ? r : c]) * (1.f / (1 << P_EXP)) * inv_count(total, mean);
   float* o = out + r * ld + c;
@@ -830,7 +836,7 @@ HeadPlan head_plan(int64_t V, int64_t d, int64_t C, bool in_out, size_t bytes) {
   // with such short parts, and without: 100 rows x 64 features x 300 classes 73 | 85, 1,000 x 256 x 1,000 105 | 123, 3,000 x 256 x 5,000 174 | 173 (two short ones a CU: 188).
   const int64_t nt = up_to(d, TN) / TN, mt = p.Rp / TM, steps = p.Cp / 16, tiles_w = p.dpad / TM * (p.Cp / TN);
   auto parts = [](int64_t a, int64_t b, int64_t most) { return (int)std::max<int64_t>(1, std::min({a, b, most})); };
-  p.splits_w = parts(ONE_EACH / tiles_w, p.Rp / 16 / SHORT_PART, 32);
+  p.splits_w = parts(ONE_EACH / tiles_w, p.Rp / 16 / SHORT_PART, 128);
   const int most = parts(2 * ONE_EACH / nt, steps / LONG_PART, 128), most_short = parts(ONE_EACH / nt, steps / SHORT_PART, 128);       // (of one tile of rows)
   p.by_rows = HeadSplits{std::max<int64_t>(mt * nt, std::min<int64_t>(2 * ONE_EACH / nt, mt * std::max(most, most_short)) * nt), nt, most, most_short};
   p.sum_rows = p.by_rows.blocks / nt * TM;
@@ -895,7 +901,7 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
   const Source w{W->ptr, W->ld, W->rows, W->cols, nullptr, nullptr, nullptr, 0};
   HeadTop t{};
   t.rmax = hmax_v, t.cmax = hmax_j;
-  t.gy = (unsigned)ceil_div64(d, AMAX_COLS), t.gx = (unsigned)std::max<int64_t>(1, std::min(p.Rp / (4 * RW), std::max<int64_t>(1, AMAX_BLOCKS / t.gy)));
+  t.gy = (unsigned)ceil_div64(d, AMAX_COLS), t.gx = (unsigned)std::max<int64_t>(1, std::min(ceil_div64(p.Rp, 4 * RW * (64 / amax_lanes(d))), std::max<int64_t>(1, AMAX_BLOCKS / t.gy)));
   t.W = w.p, t.ldw = w.ld, t.wrows = w.rows, t.wcols = w.cols, t.wmax = wmax;
   t.labels = labels, t.V = V, t.dH = dH ? dH->ptr : nullptr, t.ld = dH ? dH->ld : 0, t.d = (int)d;
   for (int64_t k = 0; k < pieces; ++k) {
@@ -956,7 +962,7 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
         const int64_t rows_p = in_out ? p.dpad : p.Cp, cols_p = in_out ? p.Cp : p.dpad;
         w.out = m.at(sw), w.split_part = rows_p * cols_p, w.ms = in_out ? cols_p : 1, w.ns = in_out ? 1 : cols_p;
         HT_TRY(split_nt(ctx, st, SUMS, w));
-        k_head_dw<<<(unsigned)ceil_div64(rows * cols, 256), 256, 0, st>>>(m.at(sw), p.splits_w, rows_p, cols_p, rows, cols, hmax_j, in_out, m.at(total), r0, mean, add,
+        k_head_dw<<<(unsigned)ceil_div64(rows * cols, 256), 256, 0, st>>>(m.at(sw), p.splits_w, p.Rp, rows_p, cols_p, rows, cols, hmax_j, in_out, m.at(total), r0, mean, add,
                                                                           out, dW->ld);
         HT_LAUNCH_CHECK(ctx);
       }
