@@ -395,6 +395,27 @@ __device__ __forceinline__ int row_parts(int most, int64_t rows) {
   return (int)(s < 1 ? 1 : s < most ? s : most);
 }
 __device__ __forceinline__ float inv_count(const int64_t* total, int mean) { return mean ? 1.f / (float)(*total > 0 ? *total : 1) : 1.f; }
+// Where a piece's dH goes, and what undoes its scales.
+struct DhOut {
+  float* dH;                      // (null: nowhere)
+  int64_t ld;
+  int d, mean;
+  const int64_t* total;
+  int64_t r0;
+  const int32_t* idx;
+  const float* weight;
+  const uint32_t* wmax;
+};
+struct DhRow {
+  float *p, ws, f;
+  __device__ __forceinline__ DhRow(const DhOut& o, int64_t v) {
+    const int64_t at = o.idx[o.r0 + v];
+    p = o.dH + at * o.ld;
+    ws = unscale_of(*o.wmax);
+    f = inv_count(o.total, o.mean) * (o.weight ? o.weight[at] : 1.f) * (1.f / (1 << P_EXP));
+  }
+  __device__ __forceinline__ float operator()(float x) const { return x * ws * f; }
+};
 struct NtArgs {
   const _Float16 *A, *B;          // fragments; row blocks KSA, KSB steps apart
   int64_t KSA, KSB;
@@ -420,6 +441,7 @@ struct NtArgs {
   int64_t split_part, ms, ns;
   int add;
   HeadSplits by_rows;             // rows_are 1: how often the reduction is split follows from the number of rows, and split_part
+  DhOut dh;                       // ... and where it is not split (and `add` is 0), its sums go here
   // DIRECT: a part of dW, finished: m_end features by n_end classes
   int64_t m_end, n_end;
   const uint32_t* fmax;           // H's largest values by feature
@@ -544,6 +566,23 @@ __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
   // lane l32 + 32 half of a 32 x 32 tile has column l32 and the rows 8 (e / 4) + 4 half + e % 4
   const int64_t mw = m0 + wave * 64;
   if constexpr (EPI == SUMS) {         // (whole tiles: what lies behind the last row and column is not looked at)
+    if (a.dh.dH && splits == 1) {      // nothing to add up: rows of dH
+      const int64_t n_end = (a.dh.d + 3) / 4 * 4;
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int64_t v = mw + i * 32 + (e >> 2) * 8 + half * 4 + (e & 3);
+          if (v >= rows) continue;
+          const DhRow to(a.dh, v);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int64_t n = n0 + j * 32 + l32;
+            if (n < n_end) to.p[n] = n < a.dh.d ? to(acc[i][j][e]) : 0.f;
+          }
+        }
+      return;
+    }
     float* out = a.out + split * (a.rows_are == 1 ? mt * TM * a.ms : a.split_part) + (mw + half * 4) * a.ms + (n0 + l32) * a.ns;
 #pragma unroll
     for (int i = 0; i < 2; ++i)
@@ -757,57 +796,98 @@ __global__ void __launch_bounds__(1024) k_head_join(const float2* __restrict__ p
   if (lane == 0) part_loss[blockIdx.x] = mine;
 }
 
-__global__ void __launch_bounds__(256) k_head_loss(const double* __restrict__ part, int64_t n, const int64_t* __restrict__ total, int mean, float* __restrict__ loss) {
+// ---- What comes after a piece's products, in one launch: the loss (a block), dH and dW from the sums of their splits.
+struct LossArgs {
+  const double* part;
+  int64_t n;
+  const int64_t* total;
+  int mean;
+  float* loss;                   // (null: later)
+};
+__device__ __forceinline__ void head_loss(const LossArgs& a) {
   __shared__ double sh[256];
   double s = 0.0;
-  for (int64_t i = threadIdx.x; i < n; i += 256) s += part[i];
+  for (int64_t i = threadIdx.x; i < a.n; i += 256) s += a.part[i];
   sh[threadIdx.x] = s;
   __syncthreads();
   for (int o = 128; o > 0; o >>= 1) {
     if ((int)threadIdx.x < o) sh[threadIdx.x] += sh[threadIdx.x + o];
     __syncthreads();
   }
-  if (threadIdx.x == 0) *loss = *total > 0 ? (float)(sh[0] / (mean ? (double)*total : 1.0)) : 0.f;
+  if (threadIdx.x == 0) *a.loss = *a.total > 0 ? (float)(sh[0] / (a.mean ? (double)*a.total : 1.0)) : 0.f;
 }
 
-// dH rows of a piece: the splits' sums, scaled
 constexpr int64_t DH_BLOCKS = 8192;
-__global__ void __launch_bounds__(256) k_head_dh(const float* __restrict__ sums, HeadSplits by_rows, int64_t most, int64_t pitch, const int64_t* __restrict__ total,
-                                                 int64_t r0, const int32_t* __restrict__ idx, const float* __restrict__ weight, int mean,
-                                                 const uint32_t* __restrict__ wmax, float* __restrict__ dH, int64_t ld, int d) {
-  const int64_t rows = piece_rows(total, r0, most);
-  const int nv = (d + 3) / 4, splits = by_rows.splits(rows);
-  const int64_t part = up_to(rows, TM) * pitch;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * nv; i += (int64_t)gridDim.x * 256) {
+struct DhArgs {
+  DhOut to;
+  const float* sums;
+  HeadSplits by_rows;
+  int64_t most, pitch;
+  int in_place;                  // what is not split is there already
+  unsigned blocks;
+};
+__device__ __forceinline__ void head_dh(const DhArgs& a, unsigned block) {
+  const int64_t rows = piece_rows(a.to.total, a.to.r0, a.most);
+  const int nv = (a.to.d + 3) / 4, splits = a.by_rows.splits(rows);
+  if (a.in_place && splits == 1) return;
+  const int64_t part = up_to(rows, TM) * a.pitch;
+  for (int64_t i = (int64_t)block * 256 + threadIdx.x; i < rows * nv; i += (int64_t)a.blocks * 256) {
     const int64_t v = i / nv;
     const int c = (int)(i % nv) * 4;
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 8
     for (int k = 0; k < splits; ++k) {
-      const float4 x = *reinterpret_cast<const float4*>(sums + k * part + v * pitch + c);
+      const float4 x = *reinterpret_cast<const float4*>(a.sums + k * part + v * a.pitch + c);
       s.x += x.x, s.y += x.y, s.z += x.z, s.w += x.w;
     }
-    const int64_t at = idx[r0 + v];
-    const float f = inv_count(total, mean) * (weight ? weight[at] : 1.f) * (1.f / (1 << P_EXP)), ws = unscale_of(*wmax);
-    auto out = [&](float x, int k) { return c + k < d ? x * ws * f : 0.f; };
-    *reinterpret_cast<float4*>(dH + at * ld + c) = make_float4(out(s.x, 0), out(s.y, 1), out(s.z, 2), out(s.w, 3));
+    const DhRow to(a.to, v);
+    auto out = [&](float x, int k) { return c + k < a.to.d ? to(x) : 0.f; };
+    *reinterpret_cast<float4*>(to.p + c) = make_float4(out(s.x, 0), out(s.y, 1), out(s.z, 2), out(s.w, 3));
   }
 }
 
 // dW's part [rows x cols] at out (pitch ld): the splits' sums (pitch cols_p, rows_p rows each), scaled by what undoes hmax along rows or columns
-__global__ void __launch_bounds__(256) k_head_dw(const float* __restrict__ sums, int most_parts, int64_t most, int64_t rows_p, int64_t cols_p, int64_t rows, int64_t cols,
-                                                 const uint32_t* __restrict__ hmax, int along_rows, const int64_t* __restrict__ total, int64_t r0, int mean, int add,
-                                                 float* __restrict__ out, int64_t ld) {
-  if (r0 > 0 && *total <= r0) return;             // (nothing to add)
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, r = i / cols, c = i - r * cols;
-  if (r >= rows) return;
-  const int splits = row_parts(most_parts, piece_rows(total, r0, most));
+struct DwArgs {
+  const float* sums;
+  int most_parts;
+  int64_t most, rows_p, cols_p, rows, cols;
+  const uint32_t* hmax;
+  int along_rows;
+  const int64_t* total;
+  int64_t r0;
+  int mean, add;
+  float* out;
+  int64_t ld;
+  unsigned blocks;
+};
+__device__ __forceinline__ void head_dw(const DwArgs& a, unsigned block) {
+  if (a.r0 > 0 && *a.total <= a.r0) return;       // (nothing to add)
+  const int64_t i = (int64_t)block * 256 + threadIdx.x, r = i / a.cols, c = i - r * a.cols;
+  if (r >= a.rows) return;
+  const int splits = row_parts(a.most_parts, piece_rows(a.total, a.r0, a.most));
   float s = 0.f;
 #pragma unroll 16
-  for (int k = 0; k < splits; ++k) s += sums[((int64_t)k * rows_p + r) * cols_p + c];
-  s *= unscale_of(hmax[along_rows ? r : c]) * (1.f / (1 << P_EXP)) * inv_count(total, mean);
-  float* o = out + r * ld + c;
-  *o = add ? *o + s : s;
+  for (int k = 0; k < splits; ++k) s += a.sums[((int64_t)k * a.rows_p + r) * a.cols_p + c];
+  s *= unscale_of(a.hmax[a.along_rows ? r : c]) * (1.f / (1 << P_EXP)) * inv_count(a.total, a.mean);
+  float* o = a.out + r * a.ld + c;
+  *o = a.add ? *o + s : s;
+}
+
+__global__ void __launch_bounds__(256) k_head_end(LossArgs loss, DhArgs dh, DwArgs dw) {
+  unsigned block = blockIdx.x;
+  if (loss.loss) {
+    if (block == 0) return head_loss(loss);
+    --block;
+  }
+  if (block < dh.blocks) return head_dh(dh, block);
+  head_dw(dw, block - dh.blocks);
+}
+int head_end(ht_ctx* ctx, hipStream_t st, const LossArgs& loss, const DhArgs& dh, const DwArgs& dw) {
+  const unsigned blocks = (loss.loss ? 1 : 0) + dh.blocks + dw.blocks;
+  if (blocks == 0) return HT_OK;
+  k_head_end<<<blocks, 256, 0, st>>>(loss, dh, dw);
+  HT_LAUNCH_CHECK(ctx);
+  return HT_OK;
 }
 
 struct HeadPlan {
@@ -931,7 +1011,14 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
     k_head_join<<<(unsigned)jb, 1024, 0, st>>>(m.at(part), ct, p.Rp, m.at(total), r0, m.at(idx), m.at(lab), C, weight, m.at(xlab), m.at(norm), row_loss, row_lse,
                                                m.at(ploss) + k * jb);
     HT_LAUNCH_CHECK(ctx);
-    if (!grad) continue;
+    // (with the last piece's)
+    const LossArgs last{m.at(ploss), pieces * jb, m.at(total), mean, k == pieces - 1 ? loss : nullptr};
+    if (!grad) {
+      HT_TRY(head_end(ctx, st, last, DhArgs{}, DwArgs{}));
+      continue;
+    }
+    const DhOut to{dH ? dH->ptr : nullptr, dH ? dH->ld : 0, (int)d, mean, m.at(total), r0, m.at(idx), weight, wmax};
+    DwArgs dw{};
     for (int64_t c0 = 0; c0 < p.Cpad; c0 += p.Cp) {
       const int64_t cp = std::min(p.Cp, p.Cpad - c0);
       NtArgs g = a;
@@ -944,6 +1031,7 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
         h.A = m.at(P), h.KSA = p.Cp / 16, h.B = m.at(Wf), h.KSB = p.KSd, h.b0 = c0 / 32;
         h.mt = p.Rp / TM, h.nt = up_to(d, TN) / TN, h.steps = cp / 16, h.by_rows = p.by_rows;
         h.out = m.at(sh), h.ms = p.dpad, h.ns = 1, h.add = c0 > 0;
+        if (p.Cp == p.Cpad) h.dh = to;
         HT_TRY(split_nt(ctx, st, SUMS, h));
       }
       if (dW) {
@@ -962,19 +1050,14 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
         const int64_t rows_p = in_out ? p.dpad : p.Cp, cols_p = in_out ? p.Cp : p.dpad;
         w.out = m.at(sw), w.split_part = rows_p * cols_p, w.ms = in_out ? cols_p : 1, w.ns = in_out ? 1 : cols_p;
         HT_TRY(split_nt(ctx, st, SUMS, w));
-        k_head_dw<<<(unsigned)ceil_div64(rows * cols, 256), 256, 0, st>>>(m.at(sw), p.splits_w, p.Rp, rows_p, cols_p, rows, cols, hmax_j, in_out, m.at(total), r0, mean, add,
-                                                                          out, dW->ld);
-        HT_LAUNCH_CHECK(ctx);
+        const DwArgs part{m.at(sw), p.splits_w, p.Rp, rows_p, cols_p, rows, cols, hmax_j, in_out, m.at(total), r0, mean, add, out, dW->ld, (unsigned)ceil_div64(rows * cols, 256)};
+        if (c0 + p.Cp < p.Cpad) HT_TRY(head_end(ctx, st, LossArgs{}, DhArgs{}, part));
+        else dw = part;
       }
     }
-    if (dH) {
-      k_head_dh<<<(unsigned)std::min(ceil_div64(p.Rp * ((d + 3) / 4), 256), DH_BLOCKS), 256, 0, st>>>(m.at(sh), p.by_rows, p.Rp, p.dpad, m.at(total), r0, m.at(idx), weight, mean, wmax,
-                                                                                 dH->ptr, dH->ld, (int)d);
-      HT_LAUNCH_CHECK(ctx);
-    }
+    const unsigned dh_blocks = dH ? (unsigned)std::min(ceil_div64(p.Rp * ((d + 3) / 4), 256), DH_BLOCKS) : 0;
+    HT_TRY(head_end(ctx, st, last, DhArgs{to, m.at(sh), p.by_rows, p.Rp, p.dpad, p.Cp == p.Cpad, dh_blocks}, dw));
   }
-  k_head_loss<<<1, 256, 0, st>>>(m.at(ploss), pieces * jb, m.at(total), mean, loss);
-  HT_LAUNCH_CHECK(ctx);
   return HT_OK;
 }
 
