@@ -193,6 +193,10 @@ struct HeadTop {
 // lpr lanes take a row's AMAX_COLS columns, four each, and a wave RW rows of each of its groups of lanes at a time; columns are joined once a block.
 constexpr int AMAX_COLS = 256, RW = 8;
 __host__ __device__ __forceinline__ int amax_lanes(int64_t cols) { return cols > 128 ? 64 : cols > 64 ? 32 : 16; }
+// (Most blocks find a word as large as it need be: requests to one word wait for each other.)
+__device__ __forceinline__ void raise(uint32_t* word, uint32_t m) {
+  if (__hip_atomic_load(word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) < m) atomicMax(word, m);
+}
 __device__ __forceinline__ uint32_t max4(uint4 x) { return max(max(x.x, x.y), max(x.z, x.w)); }
 __device__ __forceinline__ void amax_of_h(const HeadTop& a, int bx, int by) {
   __shared__ __attribute__((aligned(16))) uint32_t sh[4][AMAX_COLS];
@@ -237,9 +241,9 @@ __device__ __forceinline__ void amax_of_h(const HeadTop& a, int bx, int by) {
   if (g == 0) *reinterpret_cast<uint4*>(&sh[wave][l * 4]) = cm;
   __syncthreads();
   const int64_t k = threadIdx.x, col = (int64_t)by * AMAX_COLS + k;
-  if (k < lpr * 4 && col < s.cols) atomicMax(a.cmax + col, max(max(sh[0][k], sh[1][k]), max(sh[2][k], sh[3][k])));
+  if (k < lpr * 4 && col < s.cols) raise(a.cmax + col, max(max(sh[0][k], sh[1][k]), max(sh[2][k], sh[3][k])));
 }
-constexpr int64_t AMAX_BLOCKS = 512, ABSMAX_BLOCKS = 1024;    // (as many requests to one word: 2,048 of them take 27 us)
+constexpr int64_t AMAX_BLOCKS = 1024, ABSMAX_BLOCKS = 1024;
 
 __device__ __forceinline__ void amax_of_w(const HeadTop& a, unsigned block) {
   __shared__ uint32_t sh[4];
@@ -263,7 +267,7 @@ __device__ __forceinline__ void amax_of_w(const HeadTop& a, unsigned block) {
   for (int o = 32; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
   if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = m;
   __syncthreads();
-  if (threadIdx.x == 0) atomicMax(a.wmax, max(max(sh[0], sh[1]), max(sh[2], sh[3])));
+  if (threadIdx.x == 0) raise(a.wmax, max(max(sh[0], sh[1]), max(sh[2], sh[3])));
 }
 
 // A wave 64 rows at a time.
@@ -320,17 +324,28 @@ __global__ void __launch_bounds__(256) k_pack(Pack first, Pack second) {
   const int64_t n = s.n(), tiles = up_to(n, row_tile) / 64 * col_tiles;
   for (int64_t tile = block; tile < tiles; tile += a.blocks) {
     const int64_t r0 = tile / col_tiles * 64, c0 = tile % col_tiles * 64;
+    // four rows of 16 lanes at a time
+    V4 y[4];
+    float w[4];
+    const int c4 = (lane & 15) * 4, rq = wave * 16 + (lane >> 4);
 #pragma unroll
-    for (int q = 0; q < 16; ++q) {
-      const int r = wave * 16 + q;
-      float x = 0.f, w = 0.f;
-      if (r0 + r < n) {
-        const int64_t v = s.row(r0 + r);
-        if (c0 + lane < s.cols) x = s.p[v * s.ld + c0 + lane];
-        w = s.weight ? s.weight[v] : 1.f;
+    for (int q = 0; q < 4; ++q) {
+      const int64_t r = r0 + rq + q * 4, v = s.row(r < n ? r : n - 1);
+      const float* at = s.p + v * s.ld + c0 + c4;
+      if (c0 + 64 <= s.cols) {
+        y[q] = *reinterpret_cast<const V4u*>(at);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) y[q][k] = c0 + c4 + k < s.cols ? at[k] : 0.f;
       }
-      sh[r][lane] = x;
-      if (lane == 0) wt[r] = w;
+      w[q] = s.weight ? s.weight[v] : 1.f;
+      if (r >= n) y[q] = V4{0.f, 0.f, 0.f, 0.f}, w[q] = 0.f;
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) sh[rq + q * 4][c4 + k] = y[q][k];
+      if ((lane & 15) == 0) wt[rq + q * 4] = w[q];
     }
     __syncthreads();
     auto put = [&](_Float16* to, int64_t frag, const float* x) {
@@ -994,7 +1009,7 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
     k_head_top<<<t.gx * t.gy + t.w_blocks + t.clear_blocks, 256, 0, st>>>(t);
     HT_LAUNCH_CHECK(ctx);
     const unsigned hc = (unsigned)ceil_div64(d, 64);
-    const Pack ph{s, hmax_v, hmax_j, nullptr, m.at(Hf), p.KSd, dW ? m.at(Ht) : nullptr, KSR, TN, hc, (unsigned)std::min(p.Rp / 64 * hc, PACK_BLOCKS / 8)};
+    const Pack ph{s, hmax_v, hmax_j, nullptr, m.at(Hf), p.KSd, dW ? m.at(Ht) : nullptr, KSR, TN, hc, (unsigned)std::min(p.Rp / 64 * hc, PACK_BLOCKS / 2)};
     // by classes: W's rows, or its columns
     const int64_t rt = up_to(w.rows, in_out ? 64 : TM) / 64, wc = up_to(w.cols, in_out ? TM : 64) / 64;
     const Pack pw{w, nullptr, nullptr, wmax, in_out ? nullptr : m.at(Wf), p.KSd, in_out ? m.at(Wf) : nullptr, p.KSd, in_out ? 64 : TM, (unsigned)wc,
