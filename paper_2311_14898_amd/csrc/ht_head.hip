@@ -390,7 +390,7 @@ constexpr int64_t PACK_BLOCKS = 16384;
 
 // ---------------------------------------------------------------- products
 
-enum { LOSS, GRAD, SUMS, DIRECT };
+enum { LOSS, GRAD, SUMS, DIRECT, WHOLE };       // WHOLE: LOSS and GRAD, and what is in between, where one tile has all classes
 // The sums of dH: as many parts of the reduction as there are blocks for, by the rows that there are, which the host does not know.
 constexpr int64_t LONG_PART = 32, SHORT_PART = 8, ONE_EACH = 256;
 struct HeadSplits {
@@ -451,6 +451,11 @@ struct NtArgs {
   const float2* norm;             // GRAD: of each row the largest logit m and P_EXP - log2 of the sum of exp(x - m): exp(x - lse) without a rounding of lse
   _Float16* P;                    // GRAD: fragments by rows (KSP steps)
   int64_t KSP;
+  // WHOLE
+  const int32_t* idx;
+  const float* weight;
+  float *row_loss, *row_lse;
+  double* part_loss;              // [row tile]
   // SUMS
   float* out;                     // [split], split_part floats apart; row m of A and row n of B at m ms + n ns
   int64_t split_part, ms, ns;
@@ -462,6 +467,15 @@ struct NtArgs {
   const uint32_t* fmax;           // H's largest values by feature
   int mean;
 };
+
+// Of a row's maximum and sum of exponentials: what its probabilities are made of, and its loss.
+__device__ __forceinline__ float2 norm_of(float m, float z) { return make_float2(m, P_EXP - log2f(z)); }
+__device__ __forceinline__ float row_end(float m, float z, float xlab, int64_t at, float* row_loss, float* row_lse) {
+  const float lse = m + logf(z), l = lse - xlab;
+  if (row_loss) row_loss[at] = l;
+  if (row_lse) row_lse[at] = lse;
+  return l;
+}
 
 // Column `lane % 16` of four rows of 16, each 16 lanes for themselves, which name four of a row each.
 typedef _Float16 v4h __attribute__((ext_vector_type(4)));
@@ -670,8 +684,51 @@ __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
   const float ws = unscale_of(*a.wmax);
   const int64_t left = a.C - a.c0 - mw;                              // classes of the wave's 64
   const int lim = (left >= 64 ? 64 : left < 0 ? 0 : (int)left) - half * 4;
-  if constexpr (EPI == LOSS) {
+  // rows of the gradients of logits from norm: the gradients times 2^P_EXP, as fragments
+  auto put_grad = [&](int j, float2 nm) {
+    const int64_t v = n0 + j * 32 + l32;
+    const bool there = v < rows;
+    const float hs = unscale_of(a.hmax[v]) * ws;
+    const int64_t off = there ? a.lab[a.r0 + v] - (a.c0 + mw) : -1;
+    const bool mine = off >= 0 && off < 64 && ((off >> 2) & 1) == half;
+    const bool any = __ballot(mine);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      float p[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(fmaf(acc[i][j][e], hs, -nm.x), LOG2E, nm.y));
+      if (left < 64 || n0 + TN > rows) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (!there || i * 32 + (e >> 2) * 8 + (e & 3) >= lim) p[e] = 0.f;
+      }
+      if (any) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (mine && off == i * 32 + (e >> 2) * 8 + half * 4 + (e & 3)) p[e] -= (float)(1 << P_EXP);
+      }
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        v8h hi, lo;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          _Float16 x, y;
+          split2(p[ks * 8 + u], &x, &y);
+          hi[u] = x;
+          lo[u] = y;
+        }
+        _Float16* to = a.P + (((n0 / 32 + j) * a.KSP + (mw + i * 32) / 16 + ks) * 2) * FRAG + lane * 8;
+        // (past the caches, which have W and H to keep: 8,192 rows x 131,072 classes 6.80 -> 6.52 ms)
+        __builtin_nontemporal_store(hi, reinterpret_cast<v8h*>(to));
+        __builtin_nontemporal_store(lo, reinterpret_cast<v8h*>(to + FRAG));
+      }
+    }
+  };
+  if constexpr (EPI == LOSS || EPI == WHOLE) {
     float2* red = reinterpret_cast<float2*>(Bs);      // [wave][column]
+    float2* norm = red + 4 * TN;                      // WHOLE: [column]
+    float* xlab = reinterpret_cast<float*>(norm + TN);
+    double* sums = reinterpret_cast<double*>(xlab + TN);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int64_t v = n0 + j * 32 + l32;
@@ -705,10 +762,11 @@ __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
         for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int e = 0; e < 16; ++e)
-            if (mine && off == i * 32 + (e >> 2) * 8 + half * 4 + (e & 3)) a.xlab[v] = acc[i][j][e] * hs;
+            if (mine && off == i * 32 + (e >> 2) * 8 + half * 4 + (e & 3)) (EPI == WHOLE ? xlab[j * 32 + l32] : a.xlab[v]) = acc[i][j][e] * hs;
       }
     }
     __syncthreads();
+    float l = 0.f;
     if (tid < TN && n0 + tid < rows) {
       float m = -INFINITY, z = 0.f;
       for (int w = 0; w < 4; ++w) m = fmaxf(m, red[w * TN + tid].x);
@@ -716,52 +774,32 @@ __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
         const float2 p = red[w * TN + tid];
         z += p.x == -INFINITY ? p.y : p.y * exp_less(p.x, m);
       }
-      a.part[m0 / TM * a.most + n0 + tid] = make_float2(m, z);
+      if constexpr (EPI == LOSS) {
+        a.part[m0 / TM * a.most + n0 + tid] = make_float2(m, z);
+      } else {
+        norm[tid] = norm_of(m, z);
+        const int64_t r = a.r0 + n0 + tid, at = a.idx[r];
+        l = row_end(m, z, a.lab[r] < a.C ? xlab[tid] : NAN, at, a.row_loss, a.row_lse);
+      }
+    }
+    if constexpr (EPI == WHOLE) {
+      // (in 64 bits)
+      double mine = 0.0;
+      if (tid < TN && n0 + tid < rows) mine = a.weight ? (double)a.weight[a.idx[a.r0 + n0 + tid]] * (double)l : (double)l;
+      for (int o = 32; o > 0; o >>= 1) mine += __shfl_xor(mine, o, 64);
+      if (lane == 0 && wave < 2) sums[wave] = mine;
+      __syncthreads();
+      if (tid == 0) a.part_loss[n0 / TN] = sums[0] + sums[1];
+      if (a.P) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) put_grad(j, n0 + j * 32 + l32 < rows ? norm[j * 32 + l32] : make_float2(0.f, 0.f));
+      }
     }
     return;
   }
   if constexpr (EPI == GRAD) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int64_t v = n0 + j * 32 + l32;
-      const bool there = v < rows;
-      const float hs = unscale_of(a.hmax[v]) * ws;
-      const float2 nm = there ? a.norm[v] : make_float2(0.f, 0.f);
-      const int64_t off = there ? a.lab[a.r0 + v] - (a.c0 + mw) : -1;
-      const bool mine = off >= 0 && off < 64 && ((off >> 2) & 1) == half;
-      const bool any = __ballot(mine);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        float p[16];
-#pragma unroll
-        for (int e = 0; e < 16; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(fmaf(acc[i][j][e], hs, -nm.x), LOG2E, nm.y));
-        if (left < 64 || n0 + TN > rows) {
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (!there || i * 32 + (e >> 2) * 8 + (e & 3) >= lim) p[e] = 0.f;
-        }
-        if (any) {
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (mine && off == i * 32 + (e >> 2) * 8 + half * 4 + (e & 3)) p[e] -= (float)(1 << P_EXP);
-        }
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-          v8h hi, lo;
-#pragma unroll
-          for (int u = 0; u < 8; ++u) {
-            _Float16 x, y;
-            split2(p[ks * 8 + u], &x, &y);
-            hi[u] = x;
-            lo[u] = y;
-          }
-          _Float16* to = a.P + (((n0 / 32 + j) * a.KSP + (mw + i * 32) / 16 + ks) * 2) * FRAG + lane * 8;
-          // (past the caches, which have W and H to keep: 8,192 rows x 131,072 classes 6.80 -> 6.52 ms)
-          __builtin_nontemporal_store(hi, reinterpret_cast<v8h*>(to));
-          __builtin_nontemporal_store(lo, reinterpret_cast<v8h*>(to + FRAG));
-        }
-      }
-    }
+    for (int j = 0; j < 4; ++j) put_grad(j, n0 + j * 32 + l32 < rows ? a.norm[n0 + j * 32 + l32] : make_float2(0.f, 0.f));
   }
 }
 
@@ -795,12 +833,9 @@ __global__ void __launch_bounds__(1024) k_head_join(const float2* __restrict__ p
       z = 0.f;
       for (int w = 0; w < 16; ++w) z += sh[w][lane].x == -INFINITY ? sh[w][lane].y : sh[w][lane].y * exp_less(sh[w][lane].x, m);
       if (v < rows) {
-        const float lse = m + logf(z);
-        const float l = lab[r0 + v] < C ? lse - xlab[v] : NAN;
-        norm[v] = make_float2(m, P_EXP - log2f(z));
+        norm[v] = norm_of(m, z);
         const int64_t at = idx[r0 + v];
-        if (row_loss) row_loss[at] = l;
-        if (row_lse) row_lse[at] = lse;
+        const float l = row_end(m, z, lab[r0 + v] < C ? xlab[v] : NAN, at, row_loss, row_lse);
         mine += weight ? (double)weight[at] * (double)l : (double)l;
       }
     }
@@ -814,7 +849,8 @@ __global__ void __launch_bounds__(1024) k_head_join(const float2* __restrict__ p
 // ---- What comes after a piece's products, in one launch: the loss (a block), dH and dW from the sums of their splits.
 struct LossArgs {
   const double* part;
-  int64_t n;
+  int64_t n;                     // parts, per_piece of them a piece of `most` rows; the i-th has a value if there is a row i row_step
+  int64_t per_piece, most, row_step;
   const int64_t* total;
   int mean;
   float* loss;                   // (null: later)
@@ -822,7 +858,10 @@ struct LossArgs {
 __device__ __forceinline__ void head_loss(const LossArgs& a) {
   __shared__ double sh[256];
   double s = 0.0;
-  for (int64_t i = threadIdx.x; i < a.n; i += 256) s += a.part[i];
+  for (int64_t i = threadIdx.x; i < a.n; i += 256) {
+    const int64_t k = i / a.per_piece, r = (i - k * a.per_piece) * a.row_step;
+    if (r < piece_rows(a.total, k * a.most, a.most)) s += a.part[i];
+  }
   sh[threadIdx.x] = s;
   __syncthreads();
   for (int o = 128; o > 0; o >>= 1) {
@@ -942,7 +981,8 @@ int split_nt(ht_ctx* ctx, hipStream_t st, int epi, const NtArgs& a) {
   const int64_t blocks = up_to(a.rows_are == 1 ? a.by_rows.blocks : a.mt * a.nt * a.splits, 8);
   if (blocks >= (1 << 24)) return ht_set_err(ctx, HT_ESHAPE, "head: %lld tiles in one product", (long long)blocks);
   const unsigned grid = (unsigned)blocks;
-  if (epi == LOSS) k_split_nt<LOSS, false><<<grid, 256, 0, st>>>(a);
+  if (epi == WHOLE) k_split_nt<WHOLE, false><<<grid, 256, 0, st>>>(a);
+  else if (epi == LOSS) k_split_nt<LOSS, false><<<grid, 256, 0, st>>>(a);
   else if (epi == GRAD) k_split_nt<GRAD, false><<<grid, 256, 0, st>>>(a);
   else if (epi == DIRECT) k_split_nt<DIRECT, true><<<grid, 256, 0, st>>>(a);
   else k_split_nt<SUMS, true><<<grid, 256, 0, st>>>(a);
@@ -959,7 +999,8 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
   const HeadPlan p = head_plan(V, d, C, in_out, bytes);
   const int64_t pieces = std::max<int64_t>(1, ceil_div64(V, p.Rp)), ct = p.Cpad / TM;
   const int64_t rpb = std::max<int64_t>(256, up_to(ceil_div64(std::max<int64_t>(V, 1), ROW_BLOCKS), 256)), rb = std::max<int64_t>(1, ceil_div64(V, rpb));
-  const int64_t jb = std::min<int64_t>(p.Rp / 64, 1024);   // blocks of k_head_join a piece
+  const bool whole = p.Cpad == TM;                         // all classes in one tile
+  const int64_t row_step = whole ? TN : 64, jb = whole ? p.Rp / TN : std::min<int64_t>(p.Rp / 64, 1024);      // a piece's sums of losses
   const int64_t KSR = p.Rp / 16;
 
   OpsBlock m;
@@ -1022,12 +1063,18 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
     a.C = C, a.wmax = wmax, a.hmax = hmax_v, a.lab = m.at(lab), a.part = m.at(part), a.xlab = m.at(xlab), a.norm = m.at(norm);
     a.A = m.at(Wf), a.KSA = p.KSd, a.B = m.at(Hf), a.KSB = p.KSd;
     a.mt = ct, a.nt = p.Rp / TN, a.steps = p.steps_d, a.rows_are = 2;
-    HT_TRY(split_nt(ctx, st, LOSS, a));
-    k_head_join<<<(unsigned)jb, 1024, 0, st>>>(m.at(part), ct, p.Rp, m.at(total), r0, m.at(idx), m.at(lab), C, weight, m.at(xlab), m.at(norm), row_loss, row_lse,
-                                               m.at(ploss) + k * jb);
-    HT_LAUNCH_CHECK(ctx);
+    if (whole) {
+      a.idx = m.at(idx), a.weight = weight, a.row_loss = row_loss, a.row_lse = row_lse, a.part_loss = m.at(ploss) + k * jb;
+      a.P = grad ? m.at(P) : nullptr, a.KSP = TM / 16;
+      HT_TRY(split_nt(ctx, st, WHOLE, a));
+    } else {
+      HT_TRY(split_nt(ctx, st, LOSS, a));
+      k_head_join<<<(unsigned)jb, 1024, 0, st>>>(m.at(part), ct, p.Rp, m.at(total), r0, m.at(idx), m.at(lab), C, weight, m.at(xlab), m.at(norm), row_loss, row_lse,
+                                                 m.at(ploss) + k * jb);
+      HT_LAUNCH_CHECK(ctx);
+    }
     // (with the last piece's)
-    const LossArgs last{m.at(ploss), pieces * jb, m.at(total), mean, k == pieces - 1 ? loss : nullptr};
+    const LossArgs last{m.at(ploss), pieces * jb, jb, p.Rp, row_step, m.at(total), mean, k == pieces - 1 ? loss : nullptr};
     if (!grad) {
       HT_TRY(head_end(ctx, st, last, DhArgs{}, DwArgs{}));
       continue;
@@ -1039,7 +1086,7 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
       NtArgs g = a;
       g.c0 = c0, g.A = m.at(Wf) + c0 * p.KSd * 32, g.mt = cp / TM;
       g.P = m.at(P), g.KSP = p.Cp / 16;
-      HT_TRY(split_nt(ctx, st, GRAD, g));
+      if (!whole) HT_TRY(split_nt(ctx, st, GRAD, g));
       if (dH) {
         NtArgs h{};
         h.total = m.at(total), h.r0 = r0, h.most = p.Rp, h.rows_are = 1;
