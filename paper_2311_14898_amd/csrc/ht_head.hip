@@ -1082,7 +1082,7 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
     const DhOut to{dH ? dH->ptr : nullptr, dH ? dH->ld : 0, (int)d, mean, m.at(total), r0, m.at(idx), weight, wmax};
     DwArgs dw{};
     for (int64_t c0 = 0; c0 < p.Cpad; c0 += p.Cp) {
-      const int64_t cp = std::min(p.Cp, p.Cpad - c0);
+      const int64_t cp = std::min(p.Cp, p.Cpad - c0), cls = std::min(cp, C - c0);
       NtArgs g = a;
       g.c0 = c0, g.A = m.at(Wf) + c0 * p.KSd * 32, g.mt = cp / TM;
       g.P = m.at(P), g.KSP = p.Cp / 16;
@@ -1091,7 +1091,7 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
         NtArgs h{};
         h.total = m.at(total), h.r0 = r0, h.most = p.Rp, h.rows_are = 1;
         h.A = m.at(P), h.KSA = p.Cp / 16, h.B = m.at(Wf), h.KSB = p.KSd, h.b0 = c0 / 32;
-        h.mt = p.Rp / TM, h.nt = up_to(d, TN) / TN, h.steps = cp / 16, h.by_rows = p.by_rows;
+        h.mt = p.Rp / TM, h.nt = up_to(d, TN) / TN, h.steps = up_to(cls, PAIR) / 16, h.by_rows = p.by_rows;
         h.out = m.at(sh), h.ms = p.dpad, h.ns = 1, h.add = c0 > 0;
         if (p.Cp == p.Cpad) h.dh = to;
         HT_TRY(split_nt(ctx, st, SUMS, h));
@@ -1100,8 +1100,8 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
         NtArgs w{};
         w.total = m.at(total), w.r0 = r0, w.most = p.Rp, w.steps = -1, w.splits = p.splits_w;
         w.A = m.at(Ht), w.KSA = KSR, w.B = m.at(P), w.KSB = p.Cp / 16;
-        w.mt = p.dpad / TM, w.nt = cp / TN;
-        const int64_t cls = std::min(cp, C - c0), rows = in_out ? d : cls, cols = in_out ? cls : d;
+        w.mt = p.dpad / TM, w.nt = ceil_div64(cls, TN);
+        const int64_t rows = in_out ? d : cls, cols = in_out ? cls : d;
         const int add = k > 0 || D->accumulate_dW;
         float* out = dW->ptr + (in_out ? c0 : c0 * dW->ld);
         if (p.splits_w == 1) {
