@@ -685,6 +685,7 @@ __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
   const int64_t left = a.C - a.c0 - mw;                              // classes of the wave's 64
   const int lim = (left >= 64 ? 64 : left < 0 ? 0 : (int)left) - half * 4;
   // rows of the gradients of logits from norm: the gradients times 2^P_EXP, as fragments
+  const bool read = a.c0 + mw < up_to(a.C, TN);                             // (nothing reads what is behind the last TN classes)
   auto put_grad = [&](int j, float2 nm) {
     const int64_t v = n0 + j * 32 + l32;
     const bool there = v < rows;
@@ -790,7 +791,7 @@ __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
       if (lane == 0 && wave < 2) sums[wave] = mine;
       __syncthreads();
       if (tid == 0) a.part_loss[n0 / TN] = sums[0] + sums[1];
-      if (a.P) {
+      if (a.P && read) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) put_grad(j, n0 + j * 32 + l32 < rows ? norm[j * 32 + l32] : make_float2(0.f, 0.f));
       }
@@ -798,6 +799,7 @@ __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
     return;
   }
   if constexpr (EPI == GRAD) {
+    if (!read) return;
 #pragma unroll
     for (int j = 0; j < 4; ++j) put_grad(j, n0 + j * 32 + l32 < rows ? a.norm[n0 + j * 32 + l32] : make_float2(0.f, 0.f));
   }
