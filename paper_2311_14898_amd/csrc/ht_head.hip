@@ -1,11 +1,12 @@
-// Softmax cross entropy of a linear head over many classes, with its gradients, the logits never kept:
+// Softmax cross entropy of a linear head over many classes, with its gradients, of whose logits no more are kept than a piece:
 //   x_vc = h_v . w_c ;  lse_v = log sum_c exp(x_vc) ;  loss = sum_v u_v (lse_v - x_vy) / N
 //   dx_vc = (u_v / N) (exp(x_vc - lse_v) - [c = y_v]) ;  dH = dx W^T ;  dW = H^T dx
-// Labelled rows are first listed, and only they are computed with.  Rows go in pieces: a pass over all classes gives lse; then, class piece
-// by class piece, the logits are computed again and leave as exp(x - lse) - [c = y], which dH and dW are made of.  Four products of
-// 2 n d C flops, the fewest possible without keeping n x C numbers.
+// Labelled rows are first listed, and only they are computed with.  Rows go in pieces: a pass over all classes gives lse, and then the gradients of the
+// logits, exp(x - lse) - [c = y], are what dH and dW are made of.  Up to 256 classes a tile has all of a row's logits, and one launch leaves their
+// gradients.  Of wide rows, and of few logits, the pass keeps its sums, which the gradients take the place of (three products of 2 n d C flops); of others they are
+// computed again, class piece by class piece (four).
 //
-// All of them are k_split_nt's: fp32 products on the fp16 matrix cores.  A value is split into two fp16 numbers, x = x0 + x1 (x0 its
+// All products are k_split_nt's: fp32 products on the fp16 matrix cores.  A value is split into two fp16 numbers, x = x0 + x1 (x0 its
 // rounding, x1 the rounding of what is left: |x - x0 - x1| <= 2^-22 |x|), after W, each row of H, and each weighted column of H for dW were
 // scaled by a power of two that brings the largest value to [2^14, 2^15); x0 y0 + x0 y1 + x1 y0 are added in fp32.  What is left out is at most 3 x 2^-22 of a
 // product, typically (the roundings are independent) 2^-24 of it, what fp32 loses in rounding it; values below 2^-17 of the
@@ -725,6 +726,21 @@ __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
       }
     }
   };
+  if constexpr (EPI == LOSS) {
+    if (a.P && read) {                 // the sums, for k_head_grad, where the gradients will be
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int ks = 0; ks < 2; ++ks) {
+            _Float16* to = a.P + (((n0 / 32 + j) * a.KSP + (mw + i * 32) / 16 + ks) * 2) * FRAG + lane * 8;
+            auto four = [&](int e) { return V4{acc[i][j][e], acc[i][j][e + 1], acc[i][j][e + 2], acc[i][j][e + 3]}; };
+            __builtin_nontemporal_store(four(ks * 8), reinterpret_cast<V4*>(to));
+            __builtin_nontemporal_store(four(ks * 8 + 4), reinterpret_cast<V4*>(to + FRAG));
+          }
+    }
+  }
   if constexpr (EPI == LOSS || EPI == WHOLE) {
     float2* red = reinterpret_cast<float2*>(Bs);      // [wave][column]
     float2* norm = red + 4 * TN;                      // WHOLE: [column]
@@ -848,6 +864,51 @@ __global__ void __launch_bounds__(1024) k_head_join(const float2* __restrict__ p
   if (lane == 0) part_loss[blockIdx.x] = mine;
 }
 
+// The gradients of logits whose sums LOSS has kept in their place.  A wave takes fragments of 32 rows, GRAD_FRAGS of them one after the other.
+// What this costs is 12 bytes a logit, against the product once more in GRAD: from 193 features on (which are 256 in the product) it is less, and where the sums are
+// so few that a product's launch costs more than its work.  us of a call, kept | made again: 2,048 rows x 32,768 classes by 128 features 398 | 384, 256 478 | 497, 602
+// 888 | 1,015, 1,024 1,246 | 1,490; 20,000 x 200 x 3,000 467 | 490; 8,192 x 512 x 131,072 10.7 | 11.8 ms; 300 x 128 x 1,000 (1 MB) 69 | 75, 5,000 x 64 x 500 (10 MB)
+// 80 | 83, 3,000 x 64 x 5,000 (60 MB) 125 | 120.
+constexpr int GRAD_FRAGS = 8;
+constexpr int64_t GRAD_BLOCKS = 16384, KEEP_WIDTH = 193, KEEP_BYTES = (int64_t)16 << 20;
+__global__ void __launch_bounds__(256) k_head_grad(_Float16* __restrict__ P, int64_t KSP, const int64_t* __restrict__ total, int64_t r0, int64_t most, int64_t C,
+                                                   const uint32_t* __restrict__ wmax, const uint32_t* __restrict__ hmax, const int32_t* __restrict__ lab,
+                                                   const float2* __restrict__ norm) {
+  const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
+  const int64_t rows = piece_rows(total, r0, most), KS = up_to(C, TN) / 16, per = (KS + GRAD_FRAGS - 1) / GRAD_FRAGS, all = up_to(rows, TN) / 32 * per;
+  for (int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); t < all; t += (int64_t)gridDim.x * 4) {
+    const int64_t b = t / per, k0 = (t - b * per) * GRAD_FRAGS, v = b * 32 + l32;
+    const bool there = v < rows;
+    _Float16* at = P + (b * KSP + k0) * 2 * FRAG + lane * 8;
+    V4 x[GRAD_FRAGS][2];
+#pragma unroll
+    for (int k = 0; k < GRAD_FRAGS; ++k) {
+      const _Float16* from = at + (k0 + k < KS ? k : 0) * 2 * FRAG;
+      x[k][0] = *reinterpret_cast<const V4*>(from), x[k][1] = *reinterpret_cast<const V4*>(from + FRAG);
+    }
+    const float hs = unscale_of(hmax[v]) * unscale_of(*wmax);
+    const float2 nm = there ? norm[v] : make_float2(0.f, 0.f);
+    const int64_t c0 = k0 * 16 + half * 4, off = there ? lab[r0 + v] - c0 : -1, lim = there ? C - c0 : 0;      // (against the classes of the lane: k 16 + u / 4 8 + u % 4)
+#pragma unroll
+    for (int k = 0; k < GRAD_FRAGS; ++k) {
+      if (k0 + k >= KS) break;
+      v8h hi, lo;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int c = k * 16 + (u >> 2) * 8 + (u & 3);
+        float p = __builtin_amdgcn_exp2f(fmaf(fmaf(x[k][u >> 2][u & 3], hs, -nm.x), LOG2E, nm.y));
+        if (c >= lim) p = 0.f;
+        if (c == off) p -= (float)(1 << P_EXP);
+        _Float16 a, l;
+        split2(p, &a, &l);
+        hi[u] = a, lo[u] = l;
+      }
+      __builtin_nontemporal_store(hi, reinterpret_cast<v8h*>(at + k * 2 * FRAG));
+      __builtin_nontemporal_store(lo, reinterpret_cast<v8h*>(at + k * 2 * FRAG + FRAG));
+    }
+  }
+}
+
 // ---- What comes after a piece's products, in one launch: the loss (a block), dH and dW from the sums of their splits.
 struct LossArgs {
   const double* part;
@@ -965,6 +1026,7 @@ HeadPlan head_plan(int64_t V, int64_t d, int64_t C, bool in_out, size_t bytes) {
   const int64_t own = 12 * p.dpad + 8 * (p.Cpad / TM), least = std::min<int64_t>(p.Cpad, HEAD_CLASSES);
   p.Rp = (int64_t)bytes / (4 * least + own) / TM * TM;
   p.Rp = std::max<int64_t>(TM, std::min(p.Rp, up_to(V, TM)));
+  if (d >= KEEP_WIDTH && (int64_t)HEAD_PIECE / (4 * p.Cpad) >= 2048) p.Rp = std::min<int64_t>(p.Rp, (int64_t)HEAD_PIECE / (4 * p.Cpad) / TM * TM);
   // ... and as many classes as memory allows: every piece of them reads and writes the sums that dH is made of
   p.Cp = std::max(least, std::min<int64_t>(p.Cpad, (int64_t)std::min(bytes, HEAD_PIECE) / (4 * p.Rp) / TM * TM));
   // Parts of a reduction: for dH of 512 values each at least while there are blocks for two a CU, and of 128 while there are for one (a block that is alone on its CU
@@ -1002,6 +1064,7 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
   const int64_t pieces = std::max<int64_t>(1, ceil_div64(V, p.Rp)), ct = p.Cpad / TM;
   const int64_t rpb = std::max<int64_t>(256, up_to(ceil_div64(std::max<int64_t>(V, 1), ROW_BLOCKS), 256)), rb = std::max<int64_t>(1, ceil_div64(V, rpb));
   const bool whole = p.Cpad == TM;                         // all classes in one tile
+  const bool keep = grad && !whole && p.Cp == p.Cpad && (d >= KEEP_WIDTH || p.Rp * p.Cp * 4 <= KEEP_BYTES);
   const int64_t row_step = whole ? TN : 64, jb = whole ? p.Rp / TN : std::min<int64_t>(p.Rp / 64, 1024);      // a piece's sums of losses
   const int64_t KSR = p.Rp / 16;
 
@@ -1070,6 +1133,7 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
       a.P = grad ? m.at(P) : nullptr, a.KSP = TM / 16;
       HT_TRY(split_nt(ctx, st, WHOLE, a));
     } else {
+      if (keep) a.P = m.at(P), a.KSP = p.Cp / 16;
       HT_TRY(split_nt(ctx, st, LOSS, a));
       k_head_join<<<(unsigned)jb, 1024, 0, st>>>(m.at(part), ct, p.Rp, m.at(total), r0, m.at(idx), m.at(lab), C, weight, m.at(xlab), m.at(norm), row_loss, row_lse,
                                                  m.at(ploss) + k * jb);
@@ -1088,7 +1152,13 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
       NtArgs g = a;
       g.c0 = c0, g.A = m.at(Wf) + c0 * p.KSd * 32, g.mt = cp / TM;
       g.P = m.at(P), g.KSP = p.Cp / 16;
-      if (!whole) HT_TRY(split_nt(ctx, st, GRAD, g));
+      if (keep) {
+        const int64_t waves = p.Rp / 32 * ceil_div64(p.Cpad / 16, GRAD_FRAGS);
+        k_head_grad<<<(unsigned)std::min(ceil_div64(waves, 4), GRAD_BLOCKS), 256, 0, st>>>(m.at(P), p.Cp / 16, m.at(total), r0, p.Rp, C, wmax, hmax_v, m.at(lab), m.at(norm));
+        HT_LAUNCH_CHECK(ctx);
+      } else if (!whole) {
+        HT_TRY(split_nt(ctx, st, GRAD, g));
+      }
       if (dH) {
         NtArgs h{};
         h.total = m.at(total), h.r0 = r0, h.most = p.Rp, h.rows_are = 1;

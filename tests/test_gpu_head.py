@@ -343,3 +343,36 @@ def test_few_labels_among_many_rows(ctx, n):
         out = call(ctx, H, W, y, form)
         assert (out["dH"][~has] == 0).all() and (out["row_loss"][~has] == 0).all() and (out["row_lse"][~has] == 0).all()
         check({k: v[has] if k in ("dH", "row_loss", "row_lse") else v for k, v in out.items()}, ref, tol)
+
+
+@pytest.mark.parametrize("n,d,C", [(2_300, 193, 262_144), (300, 256, 70_001), (66, 100, 262_145)])
+def test_many_classes(ctx, n, d, C):
+    """The same formulas and tolerances with the 64-bit sums on the GPU: rows in two pieces whose sums are kept, rows in one, rows whose sums are made again."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(n)
+    H = torch.randn(n, (d + 3) // 4 * 4, generator=g, device="cuda")
+    W = torch.randn(C, d, generator=g, device="cuda") * (2.0 / d ** 0.5)
+    y = torch.randint(0, C, (n,), generator=g, device="cuda", dtype=torch.int32)
+    y[5] = -1
+    loss, row_loss, dH, dW = torch.zeros(1, device="cuda"), torch.zeros(n, device="cuda"), torch.zeros_like(H), torch.zeros_like(W)
+    B.ht_head_loss(ctx, d, C, H, W, y, loss, row_loss=row_loss, dH=dH, dW=dW, w_form=B.HT_W_OUT_IN)
+    H, W, dH = H[:, :d].double(), W.double(), dH[:, :d]
+    has, at, N = y >= 0, (torch.arange(n, device="cuda"), y.clamp(min=0).long()), float((y >= 0).sum())
+    x = H @ W.t().contiguous()
+    e = (H.abs() @ W.abs().t().contiguous()) * (3 * 2.0 ** -22 + (3 * np.ceil(d / 16) + 4) * STEP)
+    lse = torch.logsumexp(x, dim=1)
+    b = e.amax(dim=1) + 4 * STEP * (x.abs().amax(dim=1) + lse.abs() + 1) + 2.0 ** -20
+    l = torch.where(has, lse - x[at], 0.0)
+    le = b + e[at] + 2 * STEP * l.abs()
+    assert ((row_loss - l).abs() <= torch.where(has, le, 0.0)).all()
+    assert abs(float(loss) - float(l.sum()) / N) <= float(torch.where(has, le, 0.0).sum()) / N + STEP * float(l.sum()) / N
+    p = x.sub_(lse[:, None]).exp_()
+    e.add_(b[:, None] + 2.0 ** -20).mul_(p).add_(2.0 ** -39)
+    e[at] += 2 * STEP
+    p[at] -= 1.0
+    f = torch.where(has, 1.0 / N, 0.0).double()[:, None]
+    p.mul_(f), e.mul_(f)
+    terms = 3 * 2.0 ** -22 + (3 * max(n, C) / 16 + 64) * STEP
+    assert ((dH - p @ W).abs() <= e @ W.abs() + terms * (p.abs() @ W.abs())).all()
+    p, e = p.t().contiguous(), e.t().contiguous()
+    assert ((dW - p @ H).abs() <= e @ H.abs() + terms * (p.abs() @ H.abs())).all()
