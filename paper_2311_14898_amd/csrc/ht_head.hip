@@ -31,8 +31,8 @@ constexpr int TM = 256, TN = 128;      // tile of a block: rows of A x rows of B
 constexpr float LOG2E = 1.44269504088896340736f;
 constexpr int P_EXP = 15;              // gradients of logits are held times 2^15
 constexpr size_t HEAD_BYTES = (size_t)6 << 30, HEAD_LEAN = (size_t)64 << 20;   // of what a piece's rows take
-// Bytes of a piece's gradients of logits, at most.  us with pieces of 8,192 classes | 16,384 | 32,768 | of 2 GiB | 6 GiB: 8,192 rows x 131,072 classes x 256 8,152 | 7,708 | 7,502 | 7,538
-// | 7,795; 2,048 x 32,768 685 | 687 | 607 | 605 | 606; 2,100 of 7,001 rows x 50,003 x 602 2,691 | 2,521 | 2,339 | 2,322 | 2,302; 128 x 131,072 x 256 1,394 | | | 640 | 640.
+// Bytes of a piece's gradients of logits, at most.  ms with pieces of 1 GiB | 2 | 6: 8,192 rows x 256 features x 131,072 classes 6.69 | 6.52 | 6.63, 8,192 x 240 x 60,000 3.02 |
+// 2.94 | 2.95, 2,100 labelled rows of 7,001 x 602 x 50,003 1.473 | 1.446 | 1.442.
 constexpr size_t HEAD_PIECE = (size_t)2 << 30;
 constexpr int64_t HEAD_CLASSES = 8192;             // of a piece at least, where a row's share of the memory is settled
 
@@ -108,7 +108,7 @@ __global__ void __launch_bounds__(256) k_head_place(const int32_t* __restrict__ 
 }
 
 // All of that in one launch for up to LIST_ROWS rows: blocks of 256 rows, each counting what lies before it, then clear_blocks that clear n4
-// fours of words.  us of a call, so | in three launches: 80 rows x 256 features x 131,072 classes 322 | 328, 5,000 x 64 x 500 134 | 138, 8,000 x 100 x 30,000 4 less.
+// fours of words.  Instead of three launches: 6 us of a call less by 80 rows x 256 features x 131,072 classes, 3 by 5,000 x 64 x 500, 4 by 2,048 x 256 x 32,768.
 constexpr int64_t LIST_ROWS = 16384;
 __global__ void __launch_bounds__(256) k_head_list(const int32_t* __restrict__ labels, int64_t V, unsigned blocks, int32_t* __restrict__ idx, int32_t* __restrict__ lab,
                                                    int64_t* __restrict__ total, float* __restrict__ row_loss, float* __restrict__ row_lse, float* __restrict__ dH,
@@ -171,7 +171,7 @@ struct Source {
 
 // One launch finds the largest absolute values (as bits; maxima do not depend on their order) that a piece's operands are scaled by, and clears what has no
 // gradient: blocks for H, blocks for W, blocks for dH, all of which the first piece has.  Memory is idle otherwise while so few blocks look for the values
-// of a few labelled rows of many (1,000,000 rows x 256 features, 1 % of them labelled, 172 classes: 330 us, in launches of their own 358; 5,000 x 64 x 500 118 | 134).
+// of a few labelled rows of many (1,000,000 rows x 256 features, 1 % of them labelled, 172 classes: 28 us of a call less than in launches of their own; 5,000 x 64 x 500 16).
 struct HeadTop {
   // H: largest values of rows, and of columns (of weighted rows), into arrays that hold zeros
   Source s;
@@ -865,7 +865,7 @@ __global__ void __launch_bounds__(1024) k_head_join(const float2* __restrict__ p
 }
 
 // The gradients of logits whose sums LOSS has kept in their place.  A wave takes fragments of 32 rows, GRAD_FRAGS of them one after the other.
-// What this costs is 12 bytes a logit, against the product once more in GRAD: from 193 features on (which are 256 in the product) it is less, and where the sums are
+// What this costs is 8 bytes a logit, against the product once more in GRAD: from 193 features on (which are 256 in the product) it is less, and where the sums are
 // so few that a product's launch costs more than its work.  us of a call, kept | made again: 2,048 rows x 32,768 classes by 128 features 398 | 384, 256 478 | 497, 602
 // 888 | 1,015, 1,024 1,246 | 1,490; 20,000 x 200 x 3,000 467 | 490; 8,192 x 512 x 131,072 10.7 | 11.8 ms; 300 x 128 x 1,000 (1 MB) 69 | 75, 5,000 x 64 x 500 (10 MB)
 // 80 | 83, 3,000 x 64 x 5,000 (60 MB) 125 | 120.
@@ -1030,8 +1030,8 @@ HeadPlan head_plan(int64_t V, int64_t d, int64_t C, bool in_out, size_t bytes) {
   // ... and as many classes as memory allows: every piece of them reads and writes the sums that dH is made of
   p.Cp = std::max(least, std::min<int64_t>(p.Cpad, (int64_t)std::min(bytes, HEAD_PIECE) / (4 * p.Rp) / TM * TM));
   // Parts of a reduction: for dH of 512 values each at least while there are blocks for two a CU, and of 128 while there are for one (a block that is alone on its CU
-  // waits for its loads, 3 us for 64 values); for dW of 128, one block a CU (what is not split needs no sums: 2,048 rows x 32,768 classes 602 | 593 us).  us of a call
-  // with such short parts, and without: 100 rows x 64 features x 300 classes 73 | 85, 1,000 x 256 x 1,000 105 | 123, 3,000 x 256 x 5,000 174 | 173 (two short ones a CU: 188).
+  // waits for its loads, 3 us for 64 values); for dW of 128, one block a CU (what is not split needs no sums: 2,048 rows x 32,768 classes 602 | 593 us).  Short
+  // parts take 12 us off a call with 100 rows x 64 features x 300 classes, 18 off 1,000 x 256 x 1,000, none off 3,000 x 256 x 5,000 (two short ones a CU: 15 more).
   const int64_t nt = up_to(d, TN) / TN, mt = p.Rp / TM, steps = p.Cp / 16, tiles_w = p.dpad / TM * (p.Cp / TN);
   auto parts = [](int64_t a, int64_t b, int64_t most) { return (int)std::max<int64_t>(1, std::min({a, b, most})); };
   p.splits_w = parts(ONE_EACH / tiles_w, p.Rp / 16 / SHORT_PART, 128);
