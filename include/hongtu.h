@@ -20,6 +20,13 @@
  *                  Sec. 4.2, a softmax cross-entropy downstream task and an SGD
  *                  parameter update.
  *
+ * Beyond the paper, for models that programs compose of layers themselves:
+ *
+ *   ht_embed_fwd, ht_embed_bwd   rows of a table by id, and the table's gradient;
+ *   ht_head_loss                 softmax cross entropy of a linear layer over
+ *                                many classes, with its gradients;
+ *   ht_distill_loss              distillation from a teacher's top logits.
+ *
  * Conventions
  *   - Every function returns an int status: HT_OK (0) or a negative HT_E* code.
  *     Nothing throws across this boundary.  ht_strerror() names a code;
@@ -90,7 +97,8 @@ int ht_sync(ht_ctx *ctx);
  * need, to run all chunks at once: up to 8 GiB of rows and 4 GiB of partial
  * sums, and on a graph from its first backward pass on its entries grouped by
  * source (4 or 8 bytes each; up to 1 GiB of a destroyed graph's stay for the
- * next one); ht_gat_epoch up to 16 GiB more for rows kept between its passes.
+ * next one); ht_gat_epoch up to 16 GiB more for rows kept between its passes;
+ * ht_head_loss what is said with it.
  *
  * Plans: passes over a graph that are meant to be many (ht_epoch, ht_layer_bwd,
  * ht_layer_fwd with A_ckpt; tensors in HBM) order its entries anew where that
@@ -434,7 +442,8 @@ int ht_gat_epoch(ht_ctx *ctx, const ht_graph *g, const ht_gat_model *model, cons
  * not depend on the order in which the GPU runs things: the same bits from call
  * to call.  The calls are asynchronous on the context's stream.  A program may
  * record them (HIP graphs) after it has made the same calls once: a recorded
- * call allocates nothing, and is refused with HT_ESTATE where it would have to.
+ * call allocates nothing, and is refused with HT_ESTATE where it would have to;
+ * what memory a recording works in stays with the context until its end.
  * Calls and replays on one context share its scratch memory and must not overlap
  * in time. */
 
@@ -466,14 +475,19 @@ typedef struct {
 /* Softmax cross entropy of a linear layer over n_classes, and its gradients:
  *   x_v = H_v W ;  l_v = log sum_c exp(x_vc) - x_v,labels[v] ;  loss = sum u_v l_v / N
  * over the rows with a label (labels[v] >= 0; the others cost nothing but their
- * label), u = row_weight (device, nullable: 1).  The logits are not kept: scratch
- * memory is 8 bytes a weight, and up to some 5 GiB for pieces of rows and classes.
+ * label), u = row_weight (device, nullable: 1).  The logits are not all kept:
+ * scratch memory is 4 bytes a weight, and up to some 8 GiB for pieces of rows and
+ * classes (pieces are smaller where memory is scarce); with at most 64 rows, 4
+ * bytes a logit and up to 1 GiB for the sums of dH.
  * loss: device float.  row_loss, row_lse (device [V], nullable): l_v, and log sum
  * exp; 0 without a label.  dH [V x d], dW (as W; both nullable) are the gradients
  * of loss: dH is overwritten, 0 in rows without a label, dW overwritten or, with
  * accumulate_dW, added to.  With no labelled row the loss and the gradients are 0.
  * A label that is not below n_classes makes its row's loss NaN.  Products have
- * fp32 precision; where H or W are not finite, what they reach is NaN. */
+ * fp32 precision (a value of H counts against the largest of its row, in dW
+ * against the largest of its feature, one of W against the largest of all: those
+ * below 2^-39 of it are 0); where H or W are not finite, what they reach is NaN.
+ * dH and dW may not share memory with an input or with each other. */
 int ht_head_loss(ht_ctx *ctx, const ht_head_desc *desc, const ht_tensor *H, const ht_tensor *W, const int32_t *labels,
                  const float *row_weight, float *loss, float *row_loss, float *row_lse, ht_tensor *dH, ht_tensor *dW);
 
@@ -482,7 +496,7 @@ typedef struct {
   int32_t n_classes;
   int32_t k;           /* a row's entries of the teacher, 1 .. HT_DISTILL_MAX_K       */
   int32_t reduction;   /* HT_REDUCE_MEAN: N = rows with a teacher; HT_REDUCE_SUM: N = 1 */
-  float temperature;   /* T > 0                                                       */
+  float temperature;   /* T > 0, and so large that log2(e) / T is finite in fp32      */
 } ht_distill_desc;
 
 /* Distillation from a teacher's top logits.  A row's entries are top_ids[v*k ..]
