@@ -376,3 +376,22 @@ def test_many_classes(ctx, n, d, C):
     assert ((dH - p @ W).abs() <= e @ W.abs() + terms * (p.abs() @ W.abs())).all()
     p, e = p.t().contiguous(), e.t().contiguous()
     assert ((dW - p @ H).abs() <= e @ H.abs() + terms * (p.abs() @ H.abs())).all()
+
+
+@pytest.mark.parametrize("d,C,budget", [(100, 200, 150 << 20), (200, 1500, 200 << 20)])
+@pytest.mark.parametrize("labelled", ["most", "the first", "none"])
+def test_pieces_of_rows(d, C, budget, labelled):
+    """Rows in pieces whose classes are all in one tile, or whose sums are kept; the last pieces may have no rows."""
+    rng = np.random.default_rng(d)
+    n = 40_000
+    H, W, y = _inputs(n, d, C, rng, unlabelled=0.05)
+    if labelled != "most":
+        y[9_000 if labelled == "the first" else 0:] = -1
+    ref, tol = reference(H, W, y, None, True)
+    ctx = B.ht_ctx_create(0)
+    try:
+        B.ht_ctx_set_hbm_budget(ctx, budget)
+        check(call(ctx, H, W, y, B.HT_W_IN_OUT), ref, tol)
+        check(call(ctx, H, W, y, B.HT_W_OUT_IN, grad=False), ref, tol)
+    finally:
+        B.ht_ctx_destroy(ctx)
