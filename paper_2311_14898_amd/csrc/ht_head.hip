@@ -149,6 +149,34 @@ __global__ void __launch_bounds__(256) k_head_list(const int32_t* __restrict__ l
   }
 }
 
+// Of more rows: zeros in dH's rows v0 .. v1 - 1 that have no label, by `blocks` blocks behind the first `from` of a launch that has other work.  The first piece's launches
+// share them (CLEAR_*: which part of all rows is done after each): where few rows have labels, those launches wait for memory or for each other, and
+// writing dH is what there is to do.  us of a call, shared | all of it in the first launch: 1,000,000 rows x 256 features, 1 % of them labelled, 172 classes 268 | 297, 1,000,000 x
+// 64 x 100 114 | 130, 200,000 x 100 x 300 (80 MB), 30 % labelled, 252 | 261, 1,000,000 x 256 x 172, 30 % labelled, as fast; dH of less than CLEAR_SHARED bytes, which
+// the caches hold, is not shared: 50,000 x 256 x 1,000 (51 MB), 10 % labelled, 124 | 119.
+struct Clear {
+  const int32_t* labels;
+  float* dH;
+  int64_t ld;
+  int d;
+  int64_t v0, v1;
+  unsigned from, blocks;
+};
+constexpr double CLEAR_TOP = 0.3, CLEAR_PACK = 0.4, CLEAR_LOGITS = 0.6, CLEAR_DH = 0.72, CLEAR_DW = 0.85;
+constexpr int64_t CLEAR_SHARED = (int64_t)64 << 20;
+// A wave 64 rows at a time.
+__device__ __forceinline__ void clear_rows(const Clear& a, unsigned block) {
+  const int lane = threadIdx.x & 63;
+  for (int64_t v0 = a.v0 + ((int64_t)block * 4 + (threadIdx.x >> 6)) * 64; v0 < a.v1; v0 += (int64_t)a.blocks * 256) {
+    uint64_t none = __ballot(v0 + lane < a.v1 && a.labels[v0 + lane < a.v1 ? v0 + lane : a.v1 - 1] < 0);
+    while (none) {
+      const int r = __builtin_ctzll(none);
+      none &= none - 1;
+      for (int c = lane * 4; c < a.d; c += 256) __builtin_nontemporal_store(V4{0.f, 0.f, 0.f, 0.f}, reinterpret_cast<V4*>(a.dH + (v0 + r) * a.ld + c));
+    }
+  }
+}
+
 // Rows of a piece: what is left of the list from r0 on, at most `most`.
 __device__ __forceinline__ int64_t piece_rows(const int64_t* total, int64_t r0, int64_t most) {
   const int64_t left = *total - r0;
@@ -169,9 +197,8 @@ struct Source {
   __device__ __forceinline__ int64_t row(int64_t r) const { return idx ? (int64_t)idx[r0 + r] : r; }
 };
 
-// One launch finds the largest absolute values (as bits; maxima do not depend on their order) that a piece's operands are scaled by, and clears what has no
-// gradient: blocks for H, blocks for W, blocks for dH, all of which the first piece has.  Memory is idle otherwise while so few blocks look for the values
-// of a few labelled rows of many (1,000,000 rows x 256 features, 1 % of them labelled, 172 classes: 28 us of a call less than in launches of their own; 5,000 x 64 x 500 16).
+// One launch finds the largest absolute values (as bits; maxima do not depend on their order) that a piece's operands are scaled by: blocks for H, and with the
+// first piece blocks for W.
 struct HeadTop {
   // H: largest values of rows, and of columns (of weighted rows), into arrays that hold zeros
   Source s;
@@ -182,13 +209,7 @@ struct HeadTop {
   int64_t ldw, wrows, wcols;
   uint32_t* wmax;
   unsigned w_blocks;             // (0: it is known)
-  // dH: its rows without a label
-  const int32_t* labels;
-  int64_t V;
-  float* dH;
-  int64_t ld;
-  int d;
-  unsigned clear_blocks;         // (0: nothing to clear)
+  Clear clear;
 };
 
 // lpr lanes take a row's AMAX_COLS columns, four each, and a wave RW rows of each of its groups of lanes at a time; columns are joined once a block.
@@ -271,25 +292,12 @@ __device__ __forceinline__ void amax_of_w(const HeadTop& a, unsigned block) {
   if (threadIdx.x == 0) raise(a.wmax, max(max(sh[0], sh[1]), max(sh[2], sh[3])));
 }
 
-// A wave 64 rows at a time.
-__device__ __forceinline__ void clear_rows(const HeadTop& a, unsigned block) {
-  const int lane = threadIdx.x & 63;
-  for (int64_t v0 = ((int64_t)block * 4 + (threadIdx.x >> 6)) * 64; v0 < a.V; v0 += (int64_t)a.clear_blocks * 256) {
-    uint64_t none = __ballot(v0 + lane < a.V && a.labels[v0 + lane < a.V ? v0 + lane : a.V - 1] < 0);
-    while (none) {
-      const int r = __builtin_ctzll(none);
-      none &= none - 1;
-      for (int c = lane * 4; c < a.d; c += 256) __builtin_nontemporal_store(V4{0.f, 0.f, 0.f, 0.f}, reinterpret_cast<V4*>(a.dH + (v0 + r) * a.ld + c));
-    }
-  }
-}
-
 __global__ void __launch_bounds__(256) k_head_top(HeadTop a) {
   unsigned block = blockIdx.x;
   if (block < a.gx * a.gy) return amax_of_h(a, (int)(block / a.gy), (int)(block % a.gy));
   block -= a.gx * a.gy;
   if (block < a.w_blocks) return amax_of_w(a, block);
-  clear_rows(a, block - a.w_blocks);
+  clear_rows(a.clear, block - a.w_blocks);
 }
 
 __device__ __forceinline__ void split2(float x, _Float16* hi, _Float16* lo) {
@@ -310,7 +318,8 @@ struct Pack {
   unsigned col_tiles, blocks;
 };
 // (H's, in the first blocks, and then W's, with the first piece of rows: W's blocks keep the memory busy that H's few do not)
-__global__ void __launch_bounds__(256) k_pack(Pack first, Pack second) {
+__global__ void __launch_bounds__(256) k_pack(Pack first, Pack second, Clear clear) {
+  if (blockIdx.x >= first.blocks + second.blocks) return clear_rows(clear, blockIdx.x - first.blocks - second.blocks);
   const bool is_first = blockIdx.x < first.blocks;
   const Pack& a = is_first ? first : second;
   const unsigned block = is_first ? blockIdx.x : blockIdx.x - first.blocks;
@@ -433,6 +442,7 @@ struct DhRow {
   __device__ __forceinline__ float operator()(float x) const { return x * ws * f; }
 };
 struct NtArgs {
+  Clear clear;
   const _Float16 *A, *B;          // fragments; row blocks KSA, KSB steps apart
   int64_t KSA, KSB;
   int64_t b0;                     // first step of B, or (turned) first row block
@@ -499,6 +509,7 @@ __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
   constexpr int STAGE = TURN ? TN / 16 * 4 * TURN_HALF : TN / 32 * KT * 2 * FRAG;        // halfs
   __shared__ __attribute__((aligned(16))) _Float16 Bs[2 * STAGE];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
+  if (EPI != GRAD && blockIdx.x >= a.clear.from) return clear_rows(a.clear, blockIdx.x - a.clear.from);
   const int64_t rows = a.total ? piece_rows(a.total, a.r0, a.most) : 0;
   const int64_t mt = a.rows_are == 1 ? up_to(rows, TM) / TM : a.mt, nt = a.rows_are == 2 ? up_to(rows, TN) / TN : a.nt;
   if (EPI == DIRECT && a.r0 > 0 && rows == 0) return;                      // (nothing to add)
@@ -990,7 +1001,8 @@ __device__ __forceinline__ void head_dw(const DwArgs& a, unsigned block) {
   *o = a.add ? *o + s : s;
 }
 
-__global__ void __launch_bounds__(256) k_head_end(LossArgs loss, DhArgs dh, DwArgs dw) {
+__global__ void __launch_bounds__(256) k_head_end(LossArgs loss, DhArgs dh, DwArgs dw, Clear clear) {
+  if (blockIdx.x >= clear.from) return clear_rows(clear, blockIdx.x - clear.from);
   unsigned block = blockIdx.x;
   if (loss.loss) {
     if (block == 0) return head_loss(loss);
@@ -999,10 +1011,10 @@ __global__ void __launch_bounds__(256) k_head_end(LossArgs loss, DhArgs dh, DwAr
   if (block < dh.blocks) return head_dh(dh, block);
   head_dw(dw, block - dh.blocks);
 }
-int head_end(ht_ctx* ctx, hipStream_t st, const LossArgs& loss, const DhArgs& dh, const DwArgs& dw) {
-  const unsigned blocks = (loss.loss ? 1 : 0) + dh.blocks + dw.blocks;
-  if (blocks == 0) return HT_OK;
-  k_head_end<<<blocks, 256, 0, st>>>(loss, dh, dw);
+int head_end(ht_ctx* ctx, hipStream_t st, const LossArgs& loss, const DhArgs& dh, const DwArgs& dw, Clear clear = Clear{}) {
+  clear.from = (loss.loss ? 1 : 0) + dh.blocks + dw.blocks;
+  if (clear.from + clear.blocks == 0) return HT_OK;
+  k_head_end<<<clear.from + clear.blocks, 256, 0, st>>>(loss, dh, dw, clear);
   HT_LAUNCH_CHECK(ctx);
   return HT_OK;
 }
@@ -1041,10 +1053,11 @@ HeadPlan head_plan(int64_t V, int64_t d, int64_t C, bool in_out, size_t bytes) {
   return p;
 }
 
-int split_nt(ht_ctx* ctx, hipStream_t st, int epi, const NtArgs& a) {
+int split_nt(ht_ctx* ctx, hipStream_t st, int epi, NtArgs a) {
   const int64_t blocks = up_to(a.rows_are == 1 ? a.by_rows.blocks : a.mt * a.nt * a.splits, 8);
   if (blocks >= (1 << 24)) return ht_set_err(ctx, HT_ESHAPE, "head: %lld tiles in one product", (long long)blocks);
-  const unsigned grid = (unsigned)blocks;
+  a.clear.from = (unsigned)blocks;
+  const unsigned grid = a.clear.from + a.clear.blocks;
   if (epi == WHOLE) k_split_nt<WHOLE, false><<<grid, 256, 0, st>>>(a);
   else if (epi == LOSS) k_split_nt<LOSS, false><<<grid, 256, 0, st>>>(a);
   else if (epi == GRAD) k_split_nt<GRAD, false><<<grid, 256, 0, st>>>(a);
@@ -1104,15 +1117,22 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
   t.rmax = hmax_v, t.cmax = hmax_j;
   t.gy = (unsigned)ceil_div64(d, AMAX_COLS), t.gx = (unsigned)std::max<int64_t>(1, std::min(ceil_div64(p.Rp, 4 * RW * (64 / amax_lanes(d))), std::max<int64_t>(1, AMAX_BLOCKS / t.gy)));
   t.W = w.p, t.ldw = w.ld, t.wrows = w.rows, t.wcols = w.cols, t.wmax = wmax;
-  t.labels = labels, t.V = V, t.dH = dH ? dH->ptr : nullptr, t.ld = dH ? dH->ld : 0, t.d = (int)d;
+  int64_t cleared = dH && V > LIST_ROWS ? 0 : V;
+  auto clear_to = [&](double part) {
+    if (V * d * 4 < CLEAR_SHARED) part = 1.0;
+    Clear c{labels, dH ? dH->ptr : nullptr, dH ? dH->ld : 0, (int)d, cleared, part >= 1.0 ? V : std::max(cleared, std::min<int64_t>(V, up_to((int64_t)(part * (double)V), 256))), 0, 0};
+    c.blocks = (unsigned)std::min(ceil_div64(c.v1 - c.v0, 256), CLEAR_BLOCKS);
+    cleared = c.v1;
+    return c;
+  };
   for (int64_t k = 0; k < pieces; ++k) {
     const int64_t r0 = k * p.Rp;
     if (k > 0) HT_TRY(ht_fill_zero(ctx, st, hmax_v, (size_t)(p.Rp + p.dpad) * 4));
     const Source s{H->ptr, H->ld, p.Rp, d, m.at(idx), weight, m.at(total), r0};
     t.s = s;
     t.w_blocks = k > 0 ? 0 : (unsigned)std::min<int64_t>(ceil_div64(w.rows * ceil_div64(w.cols, 256), 64), ABSMAX_BLOCKS);
-    t.clear_blocks = k > 0 || !dH || V <= LIST_ROWS ? 0 : (unsigned)std::min<int64_t>(ceil_div64(V, 256), CLEAR_BLOCKS);
-    k_head_top<<<t.gx * t.gy + t.w_blocks + t.clear_blocks, 256, 0, st>>>(t);
+    t.clear = clear_to(CLEAR_TOP);
+    k_head_top<<<t.gx * t.gy + t.w_blocks + t.clear.blocks, 256, 0, st>>>(t);
     HT_LAUNCH_CHECK(ctx);
     const unsigned hc = (unsigned)ceil_div64(d, 64);
     const Pack ph{s, hmax_v, hmax_j, nullptr, m.at(Hf), p.KSd, dW ? m.at(Ht) : nullptr, KSR, TN, hc, (unsigned)std::min(p.Rp / 64 * hc, PACK_BLOCKS / 2)};
@@ -1120,11 +1140,13 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
     const int64_t rt = up_to(w.rows, in_out ? 64 : TM) / 64, wc = up_to(w.cols, in_out ? TM : 64) / 64;
     const Pack pw{w, nullptr, nullptr, wmax, in_out ? nullptr : m.at(Wf), p.KSd, in_out ? m.at(Wf) : nullptr, p.KSd, in_out ? 64 : TM, (unsigned)wc,
                   k > 0 ? 0 : (unsigned)std::min(rt * wc, PACK_BLOCKS)};
-    k_pack<<<ph.blocks + pw.blocks, 256, 0, st>>>(ph, pw);
+    const Clear cp = clear_to(CLEAR_PACK);
+    k_pack<<<ph.blocks + pw.blocks + cp.blocks, 256, 0, st>>>(ph, pw, cp);
     HT_LAUNCH_CHECK(ctx);
     NtArgs a{};
     a.total = m.at(total), a.r0 = r0, a.most = p.Rp;
     a.splits = 1;
+    a.clear = clear_to(CLEAR_LOGITS);
     a.C = C, a.wmax = wmax, a.hmax = hmax_v, a.lab = m.at(lab), a.part = m.at(part), a.xlab = m.at(xlab), a.norm = m.at(norm);
     a.A = m.at(Wf), a.KSA = p.KSd, a.B = m.at(Hf), a.KSB = p.KSd;
     a.mt = ct, a.nt = p.Rp / TN, a.steps = p.steps_d, a.rows_are = 2;
@@ -1150,6 +1172,7 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
     for (int64_t c0 = 0; c0 < p.Cpad; c0 += p.Cp) {
       const int64_t cp = std::min(p.Cp, p.Cpad - c0), cls = std::min(cp, C - c0);
       NtArgs g = a;
+      g.clear = Clear{};
       g.c0 = c0, g.A = m.at(Wf) + c0 * p.KSd * 32, g.mt = cp / TM;
       g.P = m.at(P), g.KSP = p.Cp / 16;
       if (keep) {
@@ -1166,6 +1189,7 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
         h.mt = p.Rp / TM, h.nt = up_to(d, TN) / TN, h.steps = up_to(cls, PAIR) / 16, h.by_rows = p.by_rows;
         h.out = m.at(sh), h.ms = p.dpad, h.ns = 1, h.add = c0 > 0;
         if (p.Cp == p.Cpad) h.dh = to;
+        h.clear = clear_to(CLEAR_DH);
         HT_TRY(split_nt(ctx, st, SUMS, h));
       }
       if (dW) {
@@ -1175,6 +1199,7 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
         w.mt = p.dpad / TM, w.nt = ceil_div64(cls, TN);
         const int64_t rows = in_out ? d : cls, cols = in_out ? cls : d;
         const int add = k > 0 || D->accumulate_dW;
+        w.clear = clear_to(CLEAR_DW);
         float* out = dW->ptr + (in_out ? c0 : c0 * dW->ld);
         if (p.splits_w == 1) {
           w.out = out, w.ms = in_out ? dW->ld : 1, w.ns = in_out ? 1 : dW->ld, w.m_end = d, w.n_end = cls, w.fmax = hmax_j, w.mean = mean, w.add = add;
@@ -1190,7 +1215,7 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
       }
     }
     const unsigned dh_blocks = dH ? (unsigned)std::min(ceil_div64(p.Rp * ((d + 3) / 4), 256), DH_BLOCKS) : 0;
-    HT_TRY(head_end(ctx, st, last, DhArgs{to, m.at(sh), p.by_rows, p.Rp, p.dpad, p.Cp == p.Cpad, dh_blocks}, dw));
+    HT_TRY(head_end(ctx, st, last, DhArgs{to, m.at(sh), p.by_rows, p.Rp, p.dpad, p.Cp == p.Cpad, dh_blocks}, dw, clear_to(1.0)));
   }
   return HT_OK;
 }
