@@ -77,50 +77,58 @@ struct FewArgs {
   unsigned* ticket;
 };
 
-// CT classes a block, NB * 16 rows, a quarter of the features a wave, in steps of 16: lane l + 16 q has features 4 q .. 4 q + 3 of a step, of row l of H, and of W OUT_IN the
+// CT classes a block (T = 4), NB * 16 rows, a quarter of the features a wave, in steps of 16: lane l + 16 q has features 4 q .. 4 q + 3 of a step, of row l of H, and of W OUT_IN the
 // same features of class t * 16 + l for each tile t, else of those features the classes 4 l + t.  U steps are loaded together; H comes out of the caches.
-template <int NB, bool OUT_IN>
+// T = 1: 16 classes a block, of which lane l + 16 q has class l, for few classes (four times as many blocks).
+template <int NB, bool OUT_IN, int T>
 __global__ void __launch_bounds__(256) k_few_logits(FewArgs a) {
   constexpr int U = 2;
-  __shared__ float sums[3][NB][16][64];    // of the waves that do not own the 16 rows
+  constexpr bool BY4 = !OUT_IN && T == 4;  // classes by fours of neighbours
+  __shared__ float sums[3][NB][T * 4][64];    // of the waves that do not own the 16 rows
   __shared__ int idx[64];
   __shared__ int32_t lab[64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 15, q = lane >> 4;
   const FewRows rows(a.labels, a.V, idx, lab);
   if (blockIdx.x == 0 && threadIdx.x == 0) *a.ticket = 0;
-  const int64_t c0 = (int64_t)blockIdx.x * CT;
-  v4f acc[4][NB];
+  const int64_t c0 = (int64_t)blockIdx.x * (T * 16);
+  v4f acc[T][NB];
 #pragma unroll
-  for (int t = 0; t < 4; ++t)
+  for (int t = 0; t < T; ++t)
 #pragma unroll
     for (int b = 0; b < NB; ++b) acc[t][b] = v4f{0.f, 0.f, 0.f, 0.f};
-  const float *Wp[4], *Hp[NB];
+  // of a step, OUT_IN: of T classes four features; else of four features four classes, or one
+  constexpr int L = OUT_IN ? T : 4;
+  const float *Wp[L], *Hp[NB];
   int wleft = 4;                           // (!OUT_IN: classes of the lane that there are)
 #pragma unroll
-  for (int t = 0; t < 4; ++t) {
-    const int64_t c = c0 + t * 16 + l;
-    Wp[t] = OUT_IN ? a.W + (c < a.C ? c : a.C - 1) * a.ldw + 4 * q : a.W + (int64_t)(4 * q + t) * a.ldw + c0 + 4 * l;
+  for (int t = 0; t < L; ++t) {
+    const int64_t c = c0 + (OUT_IN ? t * 16 : 0) + l;
+    Wp[t] = OUT_IN ? a.W + (c < a.C ? c : a.C - 1) * a.ldw + 4 * q : a.W + (int64_t)(4 * q + t) * a.ldw + (BY4 ? c0 + 4 * l : c < a.C ? c : a.C - 1);
   }
-  if (!OUT_IN) wleft = a.C - c0 - 4 * l >= 4 ? 4 : (int)(a.C - c0 - 4 * l);
+  if (BY4) wleft = a.C - c0 - 4 * l >= 4 ? 4 : (int)(a.C - c0 - 4 * l);
 #pragma unroll
   for (int b = 0; b < NB; ++b) Hp[b] = a.H + idx[b * 16 + l] * a.ldh + 4 * q;      // (rows that are not there: the first, whose products nobody looks at)
   const int S = (a.d + 15) / 16, s0 = S * wave / 4, s1 = S * (wave + 1) / 4, whole = a.d / 16;
-  auto multiply = [&](const v4f (&w)[4], const v4f (&h)[NB]) {
+  auto multiply = [&](const v4f (&w)[L], const v4f (&h)[NB]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int t = 0; t < 4; ++t) acc[t][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(OUT_IN ? w[t][i] : w[i][t], h[b][i], acc[t][b], 0, 0, 0);
+        for (int t = 0; t < T; ++t) acc[t][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(OUT_IN ? w[t][i] : w[i][t], h[b][i], acc[t][b], 0, 0, 0);
   };
   int s = s0;
-  const int end = OUT_IN || c0 + CT <= a.C ? (s1 < whole ? s1 : whole) : s0;       // (steps without an edge)
+  const int end = !BY4 || c0 + CT <= a.C ? (s1 < whole ? s1 : whole) : s0;       // (steps without an edge)
   for (; s + U <= end; s += U) {
-    v4f w[U][4], h[U][NB];
+    v4f w[U][L], h[U][NB];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
 #pragma unroll
-      for (int t = 0; t < 4; ++t) w[u][t] = *reinterpret_cast<const v4u*>(OUT_IN ? Wp[t] + (s + u) * 16 : Wp[t] + (int64_t)(s + u) * 16 * a.ldw);
+      for (int t = 0; t < L; ++t) {
+        const float* at = OUT_IN ? Wp[t] + (s + u) * 16 : Wp[t] + (int64_t)(s + u) * 16 * a.ldw;
+        if (OUT_IN || BY4) w[u][t] = *reinterpret_cast<const v4u*>(at);
+        else w[u][t] = v4f{*at, 0.f, 0.f, 0.f};
+      }
 #pragma unroll
       for (int b = 0; b < NB; ++b) h[u][b] = *reinterpret_cast<const v4f*>(Hp[b] + (s + u) * 16);
     }
@@ -129,9 +137,9 @@ __global__ void __launch_bounds__(256) k_few_logits(FewArgs a) {
   }
   for (; s < s1; ++s) {
     const int left = a.d - s * 16 - 4 * q;           // the lane's features that there are
-    v4f w[4], h[NB];
+    v4f w[L], h[NB];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) w[t] = OUT_IN ? load4(Wp[t] + s * 16, left) : load4(Wp[t] + (int64_t)s * 16 * a.ldw, t < left ? wleft : 0);
+    for (int t = 0; t < L; ++t) w[t] = OUT_IN ? load4(Wp[t] + s * 16, left) : load4(Wp[t] + (int64_t)s * 16 * a.ldw, t < left ? (BY4 ? wleft : 1) : 0);
 #pragma unroll
     for (int b = 0; b < NB; ++b) h[b] = load4(Hp[b] + s * 16, left);
     multiply(w, h);
@@ -141,20 +149,20 @@ __global__ void __launch_bounds__(256) k_few_logits(FewArgs a) {
   for (int b = 0; b < NB; ++b)
     if (b != wave) {
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
+      for (int t = 0; t < T; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) sums[(wave - b + 3) & 3][b][t * 4 + r][lane] = acc[t][b][r];
     }
   __syncthreads();
   // a lane has row b * 16 + l and of each tile the classes number 4 q + r
-  auto cls = [&](int t, int r) { return OUT_IN ? c0 + t * 16 + 4 * q + r : c0 + 4 * (4 * q + r) + t; };
+  auto cls = [&](int t, int r) { return BY4 ? c0 + 4 * (4 * q + r) + t : c0 + t * 16 + 4 * q + r; };
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
     if (b != wave) continue;
     const int v = b * 16 + l;
     float m = -INFINITY;
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int t = 0; t < T; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         float x = acc[t][b][r];
@@ -169,7 +177,7 @@ __global__ void __launch_bounds__(256) k_few_logits(FewArgs a) {
     const float m1 = m == -INFINITY ? 0.f : m;
     float z = 0.f;
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int t = 0; t < T; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r) z += exp_less(acc[t][b][r], m1);
     z += __shfl_xor(z, 16, 64);
@@ -178,15 +186,16 @@ __global__ void __launch_bounds__(256) k_few_logits(FewArgs a) {
     if (q == 0) a.part[(int64_t)v * a.blocks + blockIdx.x] = make_float2(m, z);
     const int32_t y = lab[v];
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int t = 0; t < T; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r)
         if (cls(t, r) == y) a.xlab[v] = acc[t][b][r];
     if (a.X) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const v4f x = OUT_IN ? acc[k][b] : v4f{acc[0][b][k], acc[1][b][k], acc[2][b][k], acc[3][b][k]};
-        *reinterpret_cast<v4f*>(a.X + v * a.ldx + (OUT_IN ? c0 + k * 16 + 4 * q : c0 + 16 * q + 4 * k)) = x;
+      for (int k = 0; k < T; ++k) {
+        v4f x = acc[k][b];
+        if constexpr (BY4) x = v4f{acc[0][b][k], acc[1][b][k], acc[2][b][k], acc[3][b][k]};
+        *reinterpret_cast<v4f*>(a.X + v * a.ldx + (BY4 ? c0 + 16 * q + 4 * k : c0 + k * 16 + 4 * q)) = x;
       }
     }
   }
@@ -249,10 +258,11 @@ struct FewGrad {
   int64_t ldd;
   float* part;                     // [block][NB * 16][d] of dH (null: not wanted)
   int tiles;                       // of CT classes
+  int split;                       // blocks that a tile's work is divided among: 1, 2 (dW and dH) or 8 (four each)
 };
 
 // Classes in tiles of CT, a contiguous part of them a block; JT features, 64 a wave.
-template <int NB, bool OUT_IN>
+template <int NB, bool OUT_IN, bool CUT>
 __global__ void __launch_bounds__(256) k_few_grad(FewArgs a, FewGrad g) {
   __shared__ float Ps[NB * 16][PP];
   __shared__ int idx[64];
@@ -260,6 +270,11 @@ __global__ void __launch_bounds__(256) k_few_grad(FewArgs a, FewGrad g) {
   __shared__ float2 norm[64];
   __shared__ float scale[64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 15, q = lane >> 4;
+  // CUT: the block's part: quarters w0 .. w1 - 1 of dW's features (OUT_IN: classes), h0 .. h1 - 1 of dH's classes
+  const int z = blockIdx.z, each = g.split == 8 ? 1 : 4, parts_h = CUT ? 4 / each : 1;
+  const bool for_w = g.dW && (!CUT || z < parts_h), for_h = g.part && (!CUT || z >= parts_h);
+  const int w0 = CUT ? z * each : 0, w1 = CUT ? w0 + each : 4, h0 = CUT ? (z - parts_h) * each : 0, h1 = CUT ? h0 + each : 4;
+  if (CUT && !for_w && !for_h) return;
   const FewRows rows(a.labels, a.V, idx, lab);
   if (threadIdx.x < 64) {
     const int v = threadIdx.x;
@@ -272,7 +287,7 @@ __global__ void __launch_bounds__(256) k_few_grad(FewArgs a, FewGrad g) {
 #pragma unroll
   for (int s = 0; s < NB * 4; ++s) {
     const int v = s * 4 + q;
-    h[s] = g.dW && v < rows.n ? load4(a.H + idx[v] * a.ldh + jl, jleft) : v4f{0.f, 0.f, 0.f, 0.f};
+    h[s] = for_w && v < rows.n ? load4(a.H + idx[v] * a.ldh + jl, jleft) : v4f{0.f, 0.f, 0.f, 0.f};
   }
   v4f sum[4][NB];
 #pragma unroll
@@ -288,6 +303,7 @@ __global__ void __launch_bounds__(256) k_few_grad(FewArgs a, FewGrad g) {
     for (int s = 0; s < 4; ++s)
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
+        if (s < h0 || s >= h1) continue;
         if (OUT_IN) {
           const int64_t c = c0 + s * 16 + 4 * q + k;
           w[s][k] = c < a.C ? load4(a.W + c * a.ldw + jl, jleft) : v4f{0.f, 0.f, 0.f, 0.f};
@@ -307,7 +323,7 @@ __global__ void __launch_bounds__(256) k_few_grad(FewArgs a, FewGrad g) {
   };
   if (t0 < t1) {
     fetch_x(t0);
-    if (g.part) fetch_w(t0);
+    if (for_h) fetch_w(t0);
   }
   __syncthreads();                         // (norm, scale)
   for (int tile = t0; tile < t1; ++tile) {
@@ -325,10 +341,11 @@ __global__ void __launch_bounds__(256) k_few_grad(FewArgs a, FewGrad g) {
     }
     __syncthreads();
     if (tile + 1 < t1) fetch_x(tile + 1);
-    if (g.dW) {
+    if (for_w) {
       if (OUT_IN) {
 #pragma unroll
         for (int ct = 0; ct < 4; ++ct) {
+          if (ct < w0 || ct >= w1) continue;
           v4f o[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) o[i] = v4f{0.f, 0.f, 0.f, 0.f};
@@ -349,6 +366,7 @@ __global__ void __launch_bounds__(256) k_few_grad(FewArgs a, FewGrad g) {
         const int cleft = cl >= 4 ? 4 : (int)cl;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {          // features 4 m + i
+          if (i < w0 || i >= w1) continue;
           v4f o[4];
 #pragma unroll
           for (int t = 0; t < 4; ++t) o[t] = v4f{0.f, 0.f, 0.f, 0.f};
@@ -366,11 +384,12 @@ __global__ void __launch_bounds__(256) k_few_grad(FewArgs a, FewGrad g) {
         }
       }
     }
-    if (g.part) {
+    if (for_h) {
 #pragma unroll
       for (int s = 0; s < 4; ++s)
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
+          if (s < h0 || s >= h1) continue;
           const v4f p = *reinterpret_cast<const v4f*>(&Ps[b * 16 + l][s * 16 + 4 * q]);
 #pragma unroll
           for (int k = 0; k < 4; ++k)          // value k of the lane's four classes
@@ -381,7 +400,7 @@ __global__ void __launch_bounds__(256) k_few_grad(FewArgs a, FewGrad g) {
     }
     __syncthreads();
   }
-  if (!g.part) return;
+  if (!for_h) return;
   // a lane has the rows b * 16 + 4 q + r and a feature of each tile: OUT_IN 4 l + t, else t * 16 + l
 #pragma unroll
   for (int b = 0; b < NB; ++b)
@@ -389,7 +408,7 @@ __global__ void __launch_bounds__(256) k_few_grad(FewArgs a, FewGrad g) {
     for (int r = 0; r < 4; ++r) {
       const int v = b * 16 + 4 * q + r;
       if (v >= rows.n) continue;
-      float* o = g.part + ((int64_t)blockIdx.x * (NB * 16) + v) * a.d;
+      float* o = g.part + (((int64_t)blockIdx.x * parts_h + (CUT ? h0 / each : 0)) * (NB * 16) + v) * a.d;
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
         const int j = OUT_IN ? jl + t : j0 + t * 16 + l;
@@ -425,14 +444,23 @@ __global__ void __launch_bounds__(1024) k_few_dh(FewArgs a, const float* __restr
 
 }  // namespace
 
+// Few tiles leave most CUs without a block, and those that have one with a long chain of instructions (64 rows: 512 of 32 clocks a tile for dW and dH).  Up to FEW_TILES tiles the
+// logits go by 16 classes a block, and up to SPLIT2 blocks of gradients each is divided, dW from dH, up to SPLIT8 those by quarters.  us of a call, so | not: 64 rows x 64
+// features x 500 classes 23 | 34, 40 x 1,000 x 700 37 | 57 (the loss alone 18 | 34), 20 x 180 x 3,600 24 | 28, 64 x 200 x 8,000 37 | 44 (loss 13 | 15); 16 classes a block of 2,048 tiles
+// 240 | 213, eighths of 64 blocks 46 | 37 (40 x 1,000 x 700).
+constexpr int FEW_TILES = 256, SPLIT8 = 32, SPLIT2 = 128;
+
 int ht_head_few(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_tensor* W, const int32_t* labels, const float* weight, float* loss, float* row_loss,
                 float* row_lse, const ht_tensor* dH, const ht_tensor* dW) {
   const bool out_in = D->w_form == HT_W_OUT_IN, grad = dH || dW;
   const int mean = D->reduction == HT_REDUCE_MEAN, d = D->d, C = D->n_classes;
   const int NB = H->rows <= 16 ? 1 : H->rows <= 32 ? 2 : 4;
-  const int blocks = (int)ceil_div64(C, CT), tiles = blocks;
-  const int64_t ldx = (int64_t)blocks * CT;
+  const int tiles = (int)ceil_div64(C, CT);
+  const bool narrow = tiles <= FEW_TILES;
+  const int blocks = narrow ? (int)ceil_div64(C, 16) : tiles;
+  const int64_t ldx = (int64_t)tiles * CT;
   const int gy = (int)ceil_div64(d, JT), gx = (int)std::min<int64_t>(tiles, std::max(64, 512 / gy));
+  const int split = (int64_t)gx * gy <= SPLIT8 ? 8 : (int64_t)gx * gy <= SPLIT2 ? 2 : 1, dh_parts = gx * (split == 8 ? 4 : 1);
   hipStream_t st = ctx->stream;
   OpsBlock m;
   const auto X = m.add<float>(grad ? NB * 16 * ldx : 0);
@@ -440,26 +468,28 @@ int ht_head_few(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht
   const auto xlab = m.add<float>(64), lrow = m.add<float>(64);
   const auto norm = m.add<float2>(64);
   const auto ticket = m.add<unsigned>(1);
-  const auto ph = m.add<float>(dH ? (int64_t)gx * NB * 16 * d : 0);
+  const auto ph = m.add<float>(dH ? (int64_t)dh_parts * NB * 16 * d : 0);
   HT_TRY(m.take(ctx));
   const FewArgs a{H->ptr, H->ld, H->rows, d, C, W->ptr, W->ld, labels, grad ? m.at(X) : nullptr, ldx, m.at(part), blocks, m.at(xlab), m.at(ticket)};
-  const FewGrad g{weight, m.at(norm), mean, D->accumulate_dW, dW ? dW->ptr : nullptr, dW ? dW->ld : 0, dH ? m.at(ph) : nullptr, tiles};
+  const FewGrad g{weight, m.at(norm), mean, D->accumulate_dW, dW ? dW->ptr : nullptr, dW ? dW->ld : 0, dH ? m.at(ph) : nullptr, tiles, split};
   auto run = [&](auto nb, auto form) -> int {
     constexpr int N = decltype(nb)::value;
     constexpr bool F = decltype(form)::value;
-    k_few_logits<N, F><<<(unsigned)blocks, 256, 0, st>>>(a);
+    if (narrow) k_few_logits<N, F, 1><<<(unsigned)blocks, 256, 0, st>>>(a);
+    else k_few_logits<N, F, 4><<<(unsigned)blocks, 256, 0, st>>>(a);
     HT_LAUNCH_CHECK(ctx);
     k_few_join<<<(unsigned)H->rows, 256, 0, st>>>(a, weight, mean, m.at(norm), m.at(lrow), row_loss, row_lse, loss);
     HT_LAUNCH_CHECK(ctx);
     if (!grad) return HT_OK;
-    k_few_grad<N, F><<<dim3((unsigned)gx, (unsigned)gy), 256, 0, st>>>(a, g);
+    if (split > 1) k_few_grad<N, F, true><<<dim3((unsigned)gx, (unsigned)gy, (unsigned)split), 256, 0, st>>>(a, g);
+    else k_few_grad<N, F, false><<<dim3((unsigned)gx, (unsigned)gy), 256, 0, st>>>(a, g);
     HT_LAUNCH_CHECK(ctx);
     return HT_OK;
   };
   auto with_form = [&](auto nb) { return out_in ? run(nb, std::true_type()) : run(nb, std::false_type()); };
   HT_TRY(NB == 1 ? with_form(std::integral_constant<int, 1>()) : NB == 2 ? with_form(std::integral_constant<int, 2>()) : with_form(std::integral_constant<int, 4>()));
   if (dH) {
-    k_few_dh<<<dim3((unsigned)H->rows, (unsigned)ceil_div64(d, 64)), 1024, 0, st>>>(a, m.at(ph), gx, NB * 16, dH->ptr, dH->ld);
+    k_few_dh<<<dim3((unsigned)H->rows, (unsigned)ceil_div64(d, 64)), 1024, 0, st>>>(a, m.at(ph), dh_parts, NB * 16, dH->ptr, dH->ld);
     HT_LAUNCH_CHECK(ctx);
   }
   return HT_OK;
