@@ -505,18 +505,18 @@ constexpr int KT = 2, PAIR = 32 * KT;   // steps of a stage; values of the reduc
 // lies in other banks than what the others do.)
 constexpr int TURN_HALF = 320;    // halfs
 template <int EPI, bool TURN>
-__global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
+__device__ __forceinline__ void split_nt(const NtArgs& a, const unsigned block) {
   constexpr int STAGE = TURN ? TN / 16 * 4 * TURN_HALF : TN / 32 * KT * 2 * FRAG;        // halfs
   __shared__ __attribute__((aligned(16))) _Float16 Bs[2 * STAGE];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
-  if (EPI != GRAD && blockIdx.x >= a.clear.from) return clear_rows(a.clear, blockIdx.x - a.clear.from);
+  if (EPI != GRAD && block >= a.clear.from) return clear_rows(a.clear, block - a.clear.from);
   const int64_t rows = a.total ? piece_rows(a.total, a.r0, a.most) : 0;
   const int64_t mt = a.rows_are == 1 ? up_to(rows, TM) / TM : a.mt, nt = a.rows_are == 2 ? up_to(rows, TN) / TN : a.nt;
   if (EPI == DIRECT && a.r0 > 0 && rows == 0) return;                      // (nothing to add)
   const int splits = a.rows_are == 1 ? a.by_rows.splits(rows) : a.steps < 0 ? row_parts(a.splits, rows) : a.splits;
   // each XCD takes a contiguous part of the tiles, eight tiles of A over all of B after eight others
-  const int64_t tiles = mt * nt, per = (tiles * splits + 7) / 8, ts = (int64_t)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
-  if ((int64_t)(blockIdx.x >> 3) >= per || ts >= tiles * splits) return;
+  const int64_t tiles = mt * nt, per = (tiles * splits + 7) / 8, ts = (int64_t)(block & 7) * per + (block >> 3);
+  if ((int64_t)(block >> 3) >= per || ts >= tiles * splits) return;
   const int64_t split = ts / tiles, t = ts - split * tiles;
   const int64_t g = t / (8 * nt), gm = mt - g * 8 < 8 ? mt - g * 8 : 8, q = t - g * 8 * nt;
   const int64_t m0 = (g * 8 + q % gm) * TM, n0 = q / gm * TN;
@@ -831,6 +831,15 @@ __global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
     for (int j = 0; j < 4; ++j) put_grad(j, n0 + j * 32 + l32 < rows ? a.norm[n0 + j * 32 + l32] : make_float2(0.f, 0.f));
   }
 }
+template <int EPI, bool TURN>
+__global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) { split_nt<EPI, TURN>(a, blockIdx.x); }
+// dH's and dW's sums, which do not wait for each other, the second behind the first `from` blocks, where those have no more tiles than there are CUs.  us of a call, so |
+// in two launches: 100 rows x 64 features x 300 classes 52 | 63, 1,000 x 256 x 1,000 73 | 84, 20,000 x 128 x 300 126 | 131; of more tiles the two take each
+// other's place in the caches: 60,000 x 256 x 172 217 | 210, 233,000 x 256 x 41 605 | 580.
+__global__ void __launch_bounds__(256, 2) k_split_both(NtArgs first, NtArgs second, unsigned from) {
+  if (blockIdx.x < from) return split_nt<SUMS, true>(first, blockIdx.x);
+  split_nt<SUMS, true>(second, blockIdx.x - from);
+}
 
 // ---------------------------------------------------------------- what the products leave
 
@@ -1053,16 +1062,31 @@ HeadPlan head_plan(int64_t V, int64_t d, int64_t C, bool in_out, size_t bytes) {
   return p;
 }
 
-int split_nt(ht_ctx* ctx, hipStream_t st, int epi, NtArgs a) {
-  const int64_t blocks = up_to(a.rows_are == 1 ? a.by_rows.blocks : a.mt * a.nt * a.splits, 8);
+// (and sets a->clear.from)
+int nt_blocks(ht_ctx* ctx, NtArgs* a, unsigned* grid) {
+  const int64_t blocks = up_to(a->rows_are == 1 ? a->by_rows.blocks : a->mt * a->nt * a->splits, 8);
   if (blocks >= (1 << 24)) return ht_set_err(ctx, HT_ESHAPE, "head: %lld tiles in one product", (long long)blocks);
-  a.clear.from = (unsigned)blocks;
-  const unsigned grid = a.clear.from + a.clear.blocks;
+  a->clear.from = (unsigned)blocks;
+  *grid = a->clear.from + a->clear.blocks;
+  return HT_OK;
+}
+int split_nt(ht_ctx* ctx, hipStream_t st, int epi, NtArgs a) {
+  unsigned grid = 0;
+  HT_TRY(nt_blocks(ctx, &a, &grid));
   if (epi == WHOLE) k_split_nt<WHOLE, false><<<grid, 256, 0, st>>>(a);
   else if (epi == LOSS) k_split_nt<LOSS, false><<<grid, 256, 0, st>>>(a);
   else if (epi == GRAD) k_split_nt<GRAD, false><<<grid, 256, 0, st>>>(a);
   else if (epi == DIRECT) k_split_nt<DIRECT, true><<<grid, 256, 0, st>>>(a);
   else k_split_nt<SUMS, true><<<grid, 256, 0, st>>>(a);
+  HT_LAUNCH_CHECK(ctx);
+  return HT_OK;
+}
+int split_both(ht_ctx* ctx, hipStream_t st, NtArgs a, NtArgs b) {
+  unsigned first = 0, second = 0;
+  HT_TRY(nt_blocks(ctx, &a, &first));
+  HT_TRY(nt_blocks(ctx, &b, &second));
+  first = (unsigned)up_to(first, 8);
+  k_split_both<<<first + second, 256, 0, st>>>(a, b, first);
   HT_LAUNCH_CHECK(ctx);
   return HT_OK;
 }
@@ -1182,15 +1206,16 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
       } else if (!whole) {
         HT_TRY(split_nt(ctx, st, GRAD, g));
       }
+      NtArgs h{};
+      const bool both = dH && dW && p.splits_w > 1 && p.Rp / TM * p.by_rows.nt <= ONE_EACH;
       if (dH) {
-        NtArgs h{};
         h.total = m.at(total), h.r0 = r0, h.most = p.Rp, h.rows_are = 1;
         h.A = m.at(P), h.KSA = p.Cp / 16, h.B = m.at(Wf), h.KSB = p.KSd, h.b0 = c0 / 32;
         h.mt = p.Rp / TM, h.nt = up_to(d, TN) / TN, h.steps = up_to(cls, PAIR) / 16, h.by_rows = p.by_rows;
         h.out = m.at(sh), h.ms = p.dpad, h.ns = 1, h.add = c0 > 0;
         if (p.Cp == p.Cpad) h.dh = to;
         h.clear = clear_to(CLEAR_DH);
-        HT_TRY(split_nt(ctx, st, SUMS, h));
+        if (!both) HT_TRY(split_nt(ctx, st, SUMS, h));
       }
       if (dW) {
         NtArgs w{};
@@ -1208,7 +1233,7 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
         }
         const int64_t rows_p = in_out ? p.dpad : p.Cp, cols_p = in_out ? p.Cp : p.dpad;
         w.out = m.at(sw), w.split_part = rows_p * cols_p, w.ms = in_out ? cols_p : 1, w.ns = in_out ? 1 : cols_p;
-        HT_TRY(split_nt(ctx, st, SUMS, w));
+        HT_TRY(both ? split_both(ctx, st, h, w) : split_nt(ctx, st, SUMS, w));
         const DwArgs part{m.at(sw), p.splits_w, p.Rp, rows_p, cols_p, rows, cols, hmax_j, in_out, m.at(total), r0, mean, add, out, dW->ld, (unsigned)ceil_div64(rows * cols, 256)};
         if (c0 + p.Cp < p.Cpad) HT_TRY(head_end(ctx, st, LossArgs{}, DhArgs{}, part));
         else dw = part;
