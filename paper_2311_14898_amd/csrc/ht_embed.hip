@@ -232,6 +232,90 @@ __global__ void __launch_bounds__(256) k_embed_join(const uint64_t* __restrict__
   }
 }
 
+// Very few entries, all in one launch: a block an entry and 64 float4s of it.  The first entry of an id adds up all of them, each wave those in its share of the
+// positions, in order; other blocks clear the rows that none has.  us, so | in order first (three launches): 1,000
+// entries of 10,000 ids x 64 7.2 | 13.0, 500 of 131,072 x 256 19 | 29, 1 of 10,000 x 64 7.9 | 11.0, 1,000 of one id 12.5 | 12.6; 2,000 of 10,000 would take 12 | 16, of one id a chain of twice the rows.
+constexpr int EMBED_ONCE = 1024, ONCE_ROWS = 1024, ONCE_PARTS = 16, ONCE_WAVES = 8;          // entries; rows that a block clears at a time
+__global__ void __launch_bounds__(ONCE_WAVES * 64) k_embed_once(const int32_t* __restrict__ ids, int n, const float* __restrict__ dH, int64_t ld_h, EmbedOut out, unsigned col_blocks) {
+  __shared__ int32_t sid[EMBED_ONCE];
+  __shared__ uint32_t there[ONCE_ROWS / 32];
+  __shared__ float4 sums[ONCE_WAVES][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const unsigned sum_blocks = n * col_blocks;
+  for (int i = threadIdx.x; i < EMBED_ONCE; i += ONCE_WAVES * 64) sid[i] = i < n ? ids[i] : -1;
+  if (blockIdx.x >= sum_blocks) {
+    // ONCE_PARTS blocks clear the same ONCE_ROWS rows
+    const uint32_t block = (blockIdx.x - sum_blocks) / ONCE_PARTS, part = (blockIdx.x - sum_blocks) % ONCE_PARTS, blocks = (gridDim.x - sum_blocks) / ONCE_PARTS;
+    const uint32_t nv = out.nv;
+    for (int64_t r0 = (int64_t)block * ONCE_ROWS; r0 < out.V; r0 += (int64_t)blocks * ONCE_ROWS) {
+      const int rows = out.V - r0 < ONCE_ROWS ? (int)(out.V - r0) : ONCE_ROWS;
+      __syncthreads();
+      for (int i = threadIdx.x; i < ONCE_ROWS / 32; i += ONCE_WAVES * 64) there[i] = 0;
+      __syncthreads();
+      for (int i = threadIdx.x; i < n; i += ONCE_WAVES * 64) {
+        const int64_t r = sid[i] - r0;
+        if (sid[i] >= 0 && r >= 0 && r < rows) atomicOr(&there[r >> 5], 1u << (r & 31));
+      }
+      __syncthreads();
+      const uint32_t per = (rows + ONCE_PARTS - 1) / ONCE_PARTS, r1 = part * per, r2 = r1 + per < (uint32_t)rows ? r1 + per : rows;
+      // (rows one after the other without lanes that idle at their ends)
+      uint32_t r = r1 + threadIdx.x / nv, c = threadIdx.x % nv;
+      for (const uint32_t dr = ONCE_WAVES * 64 / nv, dc = ONCE_WAVES * 64 % nv; r < r2;) {
+        if (!((there[r >> 5] >> (r & 31)) & 1)) *reinterpret_cast<float4*>(out.dT + (r0 + r) * out.ld + c * 4) = make_float4(0.f, 0.f, 0.f, 0.f);
+        r += dr, c += dc;
+        if (c >= nv) c -= nv, ++r;
+      }
+    }
+    return;
+  }
+  __syncthreads();
+  const int e = blockIdx.x / col_blocks, id = __builtin_amdgcn_readfirstlane(sid[e]);
+  if (id < 0 || id >= out.V) return;
+  constexpr int K = EMBED_ONCE / (ONCE_WAVES * 64);      // sets of 64 positions of a wave: every ONCE_WAVES-th
+  bool first = true;
+  for (int k = 0; k * 64 < e; ++k) {
+    const int i = k * 64 + lane;
+    first = first && !__ballot(i < e && sid[i] == id);
+  }
+  if (!first) return;
+  uint64_t same[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) same[k] = __ballot(sid[(k * ONCE_WAVES + wave) * 64 + lane] == id);
+  for (int c0 = blockIdx.x % col_blocks * 64; c0 < out.nv; c0 += col_blocks * 64) {
+    const int c = c0 + lane < out.nv ? c0 + lane : out.nv - 1;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      uint64_t left = same[k];
+      while (left) {
+        constexpr int U = 8;
+        float4 x[U];
+        int at[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          at[u] = left ? (k * ONCE_WAVES + wave) * 64 + __builtin_ctzll(left) : -1;
+          left &= left - 1;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u] = *reinterpret_cast<const float4*>(dH + (at[u] < 0 ? at[0] : at[u]) * ld_h + c * 4);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (at[u] >= 0) s.x += x[u].x, s.y += x[u].y, s.z += x[u].z, s.w += x[u].w;
+      }
+    }
+    __syncthreads();
+    sums[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && c0 + lane < out.nv) {
+      for (int w = 1; w < ONCE_WAVES; ++w) {
+        const float4 x = sums[w][lane];
+        s.x += x.x, s.y += x.y, s.z += x.z, s.w += x.w;
+      }
+      out.put(id, c, s);
+    }
+  }
+}
+
 // f(LPR) with the lanes that a row of nv float4s takes
 template <class F>
 void with_lanes(int nv, F&& f) {
@@ -278,6 +362,14 @@ extern "C" int ht_embed_bwd(ht_ctx* ctx, const ht_tensor* dH, const int32_t* ids
   const int64_t n = dH->rows, V = dT->rows;
   int bits = 1;
   while (((int64_t)1 << bits) <= V) ++bits;
+  const EmbedOut out{dT->ptr, dT->ld, V, scale, accumulate, nv};
+  if (n <= EMBED_ONCE) {
+    if (V == 0 || (n == 0 && accumulate)) return HT_OK;
+    const unsigned col_blocks = (unsigned)std::min(16, (nv + 63) / 64), clear_blocks = accumulate ? 0 : ONCE_PARTS * (unsigned)std::min<int64_t>(ceil_div64(V, ONCE_ROWS), 4096);
+    k_embed_once<<<(unsigned)n * col_blocks + clear_blocks, ONCE_WAVES * 64, 0, ctx->stream>>>(ids, (int)n, dH->ptr, dH->ld, out, col_blocks);
+    HT_LAUNCH_CHECK(ctx);
+    return HT_OK;
+  }
   return ht_with_room(ctx, [&]() -> int {
     OpsBlock m;
     const bool few = n <= EMBED_FEW;
@@ -297,7 +389,6 @@ extern "C" int ht_embed_bwd(ht_ctx* ctx, const ht_tensor* dH, const int32_t* ids
     HT_LAUNCH_CHECK(ctx);
     if (n == 0 || V == 0) return HT_OK;
     if (!few) HT_TRY(ht_radix_sort_u64(ctx, m.at(keys), m.at(tmp), n, 32, 32 + bits, &sorted));
-    const EmbedOut out{dT->ptr, dT->ld, V, scale, accumulate, nv};
     with_lanes(nv, [&](auto lanes) {
       constexpr int LPR = decltype(lanes)::value;
       const dim3 grid((unsigned)blocks, (unsigned)((nv + LPR - 1) / LPR));

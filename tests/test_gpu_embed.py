@@ -168,3 +168,9 @@ def test_refusals(ctx):
         B.ht_embed_fwd(ctx, 8, ok, ids.long(), wide)
     with pytest.raises(AssertionError):
         B.ht_embed_fwd(ctx, 8, ok, ids[:3], wide)
+
+
+@pytest.mark.parametrize("n,V,d,kind", [(1, 3000, 20, "spread"), (64, 2050, 12, "holes"), (65, 5, 300, "hot"), (512, 1025, 2052, "spread"), (513, 70_000, 33, "hot"),
+                                        (1024, 1, 260, "one"), (1024, 200, 8, "none"), (1025, 1, 260, "one"), (8192, 1024, 60, "hot"), (8193, 1024, 60, "hot")])
+def test_few_entries(ctx, n, V, d, kind):
+    test_lookup_and_gradient(ctx, n, V, d, kind)

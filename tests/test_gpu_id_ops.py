@@ -213,6 +213,7 @@ def test_a_recorded_first_call_is_refused():
     try:
         w = Work(ctx)
         x = torch.zeros(8, device="cuda")
+        many, many_ids = w.dH0.repeat(9, 1), w.ids.repeat(9)
         codes = []
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph, stream=s):
@@ -220,14 +221,15 @@ def test_a_recorded_first_call_is_refused():
             for call in (lambda: B.ht_embed_bwd(ctx, w.d, w.dH0, w.ids, w.dT, sync=False),
                          lambda: B.ht_head_loss(ctx, w.d, w.C, w.H, w.W, w.y, w.loss, sync=False),
                          lambda: B.ht_head_loss(ctx, w.d, w.C, w.H[:3], w.W, w.y[:3], w.loss, sync=False),
-                         lambda: B.ht_distill_loss(ctx, w.C, w.X, w.top_ids, w.top, w.lossd, sync=False)):
+                         lambda: B.ht_distill_loss(ctx, w.C, w.X, w.top_ids, w.top, w.lossd, sync=False),
+                         lambda: B.ht_embed_bwd(ctx, w.d, many, many_ids, w.dT, sync=False)):
                 try:
                     call()
                     codes.append(0)
                 except B.HongtuError as e:
                     codes.append(e.code)
             B.ht_embed_fwd(ctx, w.d, w.table, w.ids, w.H, sync=False)     # (needs no scratch memory)
-        assert codes == [B.HT_ESTATE] * 4
+        assert codes == [0] + [B.HT_ESTATE] * 4            # (the gradient of few entries needs no scratch memory either)
         with torch.cuda.stream(s):
             graph.replay()
             graph.replay()
@@ -285,7 +287,8 @@ def test_refused_memory_is_said_and_gone_again():
     try:
         B.ht_ctx_set_hbm_budget(ctx, 4096)
         w = Work(ctx)
-        for call in (lambda: B.ht_embed_bwd(ctx, w.d, w.dH0, w.ids, w.dT), lambda: B.ht_head_loss(ctx, w.d, w.C, w.H, w.W, w.y, w.loss),
+        many, many_ids = w.dH0.repeat(9, 1), w.ids.repeat(9)      # (the gradient of few entries needs no scratch memory)
+        for call in (lambda: B.ht_embed_bwd(ctx, w.d, many, many_ids, w.dT), lambda: B.ht_head_loss(ctx, w.d, w.C, w.H, w.W, w.y, w.loss),
                      lambda: B.ht_head_loss(ctx, w.d, w.C, w.H[:3], w.W, w.y[:3], w.loss), lambda: B.ht_distill_loss(ctx, w.C, w.X, w.top_ids, w.top, w.lossd)):
             with pytest.raises(B.HongtuError) as err:
                 call()
