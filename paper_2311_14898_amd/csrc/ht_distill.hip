@@ -9,7 +9,7 @@
 namespace {
 
 constexpr int DISTILL_COUNTS = 256, DISTILL_BLOCKS = 4096;
-constexpr int FEW_ROWS = 64, FEW_PARTS = 64;      // rows up to which a row is cut among blocks, and into how many parts at most
+constexpr int FEW_ROWS = 64, FEW_PARTS = 64, FEW_CLASSES = 4096;      // rows up to which a row of more classes is cut among blocks, and into how many parts at most
 
 struct DistillArgs {
   const float* x;                  // (may be grad)
@@ -39,6 +39,17 @@ __device__ __forceinline__ bool has_entries(const DistillArgs& a, int64_t v) {
   bool any = false;
   for (int k = 0; k < a.K && !any; ++k) any = a.ids[v * a.K + k] >= 0 && a.top[v * a.K + k] != -INFINITY;
   return any;
+}
+
+// How many of at most FEW_ROWS rows have entries, counted by a block for itself; with[v]: whether row v has.
+__device__ __forceinline__ int count_few(const DistillArgs& a, int* with) {
+  for (int v = threadIdx.x; v < FEW_ROWS; v += blockDim.x) with[v] = 0;
+  __syncthreads();
+  for (int i = threadIdx.x; i < a.V * a.K; i += blockDim.x)
+    if (a.ids[i] >= 0 && a.top[i] != -INFINITY) with[i / a.K] = 1;
+  __syncthreads();
+  static_assert(FEW_ROWS == 64, "a row a lane");
+  return __popcll(__ballot(with[threadIdx.x & 63]));
 }
 
 // Rows with entries, per block.
@@ -125,19 +136,25 @@ __device__ __forceinline__ float4 zero4() { return make_float4(0.f, 0.f, 0.f, 0.
 // T threads a row, NV float4 of it in each thread's registers; what goes beyond (MORE) is read once more for the gradient, the last read first, while some of
 // it is still in the caches.  Rows of T x NV x 4 classes.  Short rows want waves (at most 72 registers: 100,003 rows x 172 56.7 -> 53.2 us, with three float4s a thread for four 51.3); long rows
 // past the caches, loads and stores that are not for them (4,096 x 131,072, where 49,152 classes stay in registers: 1.15 ms, with such stores 1.08, with loads too 1.05).
-template <int T, int NV, bool MORE>
-__global__ void __launch_bounds__(T < 256 ? 256 : T, T < 256 ? 7 : 1) k_distill(DistillArgs a, const unsigned long long* __restrict__ cnt, int n_cnt, double* __restrict__ part) {
+template <int T, int NV, bool MORE, bool FEW>
+__global__ void __launch_bounds__(T < 256 ? 256 : T, T < 256 ? 7 : 1) k_distill(DistillArgs a, unsigned long long* __restrict__ cnt, int n_cnt, double* __restrict__ part) {
   constexpr int B = T < 256 ? 256 : T, R = B / T;
   extern __shared__ float entries[];             // [R][K] ids, [R][K] q
   __shared__ float2 red[B / 64];
   __shared__ double dred[B / 64];
+  __shared__ int with[FEW ? FEW_ROWS : 1];
   const int r = threadIdx.x / T, l = threadIdx.x % T;
   const Row<T> row{red};
   int* sid = reinterpret_cast<int*>(entries) + r * a.K;
   float* sq = entries + R * a.K + r * a.K;
   unsigned long long N = 0;
-  for (int i = threadIdx.x & 63; i < n_cnt; i += 64) N += cnt[i];
-  for (int o = 32; o > 0; o >>= 1) N += __shfl_xor(N, o, 64);
+  if (FEW) {                                     // (at most FEW_ROWS: nobody has counted them, a launch less; k_distill_loss is told)
+    N = count_few(a, with);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *cnt = N;
+  } else {
+    for (int i = threadIdx.x & 63; i < n_cnt; i += 64) N += cnt[i];
+    for (int o = 32; o > 0; o >>= 1) N += __shfl_xor(N, o, 64);
+  }
   const float inv = a.mean ? 1.f / (float)(N > 0 ? N : 1) : 1.f;
   double mine = 0.0;
   for (int64_t v0 = (int64_t)blockIdx.x * R; v0 < a.V; v0 += (int64_t)gridDim.x * R) {
@@ -356,14 +373,7 @@ __global__ void __launch_bounds__(256) k_distill_apply(DistillArgs a, const floa
   const Row<256> row{red};
   const Row<64> wv{nullptr};
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  // how many rows have entries: every block looks for itself
-  for (int v = threadIdx.x; v < FEW_ROWS; v += 256) with[v] = 0;
-  __syncthreads();
-  for (int i = threadIdx.x; i < a.V * a.K; i += 256)
-    if (a.ids[i] >= 0 && a.top[i] != -INFINITY) with[i / a.K] = 1;
-  __syncthreads();
-  const int N = __popcll(__ballot(with[lane]));
-  static_assert(FEW_ROWS == 64, "a row a lane");
+  const int N = count_few(a, with);
   if ((int)blockIdx.x < parts) {
     if (!a.grad) return;
     const int64_t v = blockIdx.y;
@@ -482,7 +492,7 @@ extern "C" int ht_distill_loss(ht_ctx* ctx, const ht_distill_desc* desc, const h
   hipStream_t st = ctx->stream;
   return ht_with_room(ctx, [&]() -> int {
     OpsBlock m;
-    if (a.V >= 1 && a.V <= FEW_ROWS && a.C > 4096) {
+    if (a.V >= 1 && a.V <= FEW_ROWS && a.C > FEW_CLASSES) {
       const auto part = m.add<float2>(FEW_ROWS * FEW_PARTS);
       const auto xe = m.add<float>((int64_t)FEW_ROWS * HT_DISTILL_MAX_K);
       HT_TRY(m.take(ctx));
@@ -498,13 +508,20 @@ extern "C" int ht_distill_loss(ht_ctx* ctx, const ht_distill_desc* desc, const h
     const auto part = m.add<double>(DISTILL_BLOCKS);
     HT_TRY(m.take(ctx));
     const unsigned nc = (unsigned)std::max<int64_t>(1, std::min<int64_t>(DISTILL_COUNTS, ceil_div64(a.V, 256)));
-    k_distill_count<<<nc, 256, 0, st>>>(a, m.at(cnt));
-    HT_LAUNCH_CHECK(ctx);
+    const bool few = a.V <= FEW_ROWS && a.C <= FEW_CLASSES;
+    if (!few) {
+      k_distill_count<<<nc, 256, 0, st>>>(a, m.at(cnt));
+      HT_LAUNCH_CHECK(ctx);
+    }
     unsigned nb = 1;
     with_shape(a.C, [&](auto t, auto nv, auto more) {
       constexpr int T = decltype(t)::value, B = T < 256 ? 256 : T, R = B / T;
       nb = (unsigned)std::max<int64_t>(1, std::min<int64_t>(DISTILL_BLOCKS, ceil_div64(a.V, R)));
-      k_distill<T, decltype(nv)::value, decltype(more)::value><<<nb, B, (size_t)R * a.K * 8, st>>>(a, m.at(cnt), (int)nc, m.at(part));
+      constexpr int NV = decltype(nv)::value;
+      constexpr bool MORE = decltype(more)::value;
+      if constexpr (T * NV * 4 <= FEW_CLASSES && !MORE)
+        if (few) return k_distill<T, NV, MORE, true><<<nb, B, (size_t)R * a.K * 8, st>>>(a, m.at(cnt), 0, m.at(part));
+      k_distill<T, NV, MORE, false><<<nb, B, (size_t)R * a.K * 8, st>>>(a, m.at(cnt), (int)nc, m.at(part));
     });
     HT_LAUNCH_CHECK(ctx);
     k_distill_loss<<<1, 256, 0, st>>>(m.at(part), (int)nb, m.at(cnt), (int)nc, a.mean, loss);

@@ -223,3 +223,15 @@ def test_what_lies_behind_the_last_class(ctx, n, C):
     loss = torch.zeros(1, device="cuda")
     B.ht_distill_loss(ctx, C, Xd, torch.from_numpy(ids.astype(np.int32)).cuda(), torch.from_numpy(top).cuda(), loss, row_weight=torch.from_numpy(u).cuda(), dlogits=dX)
     assert (dX[:, C:] == 0).all() and dX[0, :C].isnan().all() and (dX[n - 1] == 0).all() and not dX[1:n - 1, :C].isfinite().all()
+
+
+@pytest.mark.parametrize("n,C", [(0, 10), (0, 5_000), (0, 70_000), (64, 10), (64, 4_096), (64, 4_097), (65, 4_096)])
+def test_few_rows(ctx, n, C):
+    X, ids, top = _inputs(n, C, 5, np.random.default_rng(C), missing=0.2) if n else (np.ones((0, C), np.float32), np.zeros((0, 5), np.int64), np.zeros((0, 5), np.float32))
+    for mean in (True, False):
+        out = call(ctx, X, ids, top, 1.5, mean=mean)
+        if n:
+            ref, tol = reference(X, ids, top, 1.5, None, mean)
+            check(out, ref, tol)
+        else:
+            assert out["loss"] == 0
