@@ -1005,7 +1005,8 @@ __device__ __forceinline__ void head_dw(const DwArgs& a, unsigned block) {
   float s = 0.f;
 #pragma unroll 16
   for (int k = 0; k < splits; ++k) s += a.sums[((int64_t)k * a.rows_p + r) * a.cols_p + c];
-  s *= unscale_of(a.hmax[a.along_rows ? r : c]) * (1.f / (1 << P_EXP)) * inv_count(a.total, a.mean);
+  // (the inverse scale first: of a feature below 2^-97 it is near the smallest float, and what follows would take it below)
+  s = s * unscale_of(a.hmax[a.along_rows ? r : c]) * ((1.f / (1 << P_EXP)) * inv_count(a.total, a.mean));
   float* o = a.out + r * a.ld + c;
   *o = a.add ? *o + s : s;
 }
