@@ -49,6 +49,9 @@ __device__ __forceinline__ uint32_t scale_exp(uint32_t bits) {
 }
 __device__ __forceinline__ float scale_of(uint32_t bits) { return __uint_as_float(scale_exp(bits) << 23); }
 __device__ __forceinline__ float unscale_of(uint32_t bits) { return __uint_as_float((254 - scale_exp(bits)) << 23); }
+// What makes a logit of a sum: the inverse of both operands' scales, but never 0 (a sum is below 2^47, so that such a row's logits are below 2^-79, and count as
+// 0; the -inf of what lies behind the last class has to stay one).
+__device__ __forceinline__ float logit_scale(uint32_t hbits, float ws) { return fmaxf(unscale_of(hbits) * ws, 0x1p-126f); }
 
 // ---------------------------------------------------------------- labelled rows
 
@@ -701,7 +704,7 @@ __device__ __forceinline__ void split_nt(const NtArgs& a, const unsigned block) 
   auto put_grad = [&](int j, float2 nm) {
     const int64_t v = n0 + j * 32 + l32;
     const bool there = v < rows;
-    const float hs = unscale_of(a.hmax[v]) * ws;
+    const float hs = logit_scale(a.hmax[v], ws);
     const int64_t off = there ? a.lab[a.r0 + v] - (a.c0 + mw) : -1;
     const bool mine = off >= 0 && off < 64 && ((off >> 2) & 1) == half;
     const bool any = __ballot(mine);
@@ -761,7 +764,7 @@ __device__ __forceinline__ void split_nt(const NtArgs& a, const unsigned block) 
     for (int j = 0; j < 4; ++j) {
       const int64_t v = n0 + j * 32 + l32;
       const bool there = v < rows;
-      const float hs = unscale_of(a.hmax[v]) * ws;
+      const float hs = logit_scale(a.hmax[v], ws);
       float m = -INFINITY;
       if (left < 64) {
 #pragma unroll
@@ -906,7 +909,7 @@ __global__ void __launch_bounds__(256) k_head_grad(_Float16* __restrict__ P, int
       const _Float16* from = at + (k0 + k < KS ? k : 0) * 2 * FRAG;
       x[k][0] = *reinterpret_cast<const V4*>(from), x[k][1] = *reinterpret_cast<const V4*>(from + FRAG);
     }
-    const float hs = unscale_of(hmax[v]) * unscale_of(*wmax);
+    const float hs = logit_scale(hmax[v], unscale_of(*wmax));
     const float2 nm = there ? norm[v] : make_float2(0.f, 0.f);
     const int64_t c0 = k0 * 16 + half * 4, off = there ? lab[r0 + v] - c0 : -1, lim = there ? C - c0 : 0;      // (against the classes of the lane: k 16 + u / 4 8 + u % 4)
 #pragma unroll

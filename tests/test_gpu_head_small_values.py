@@ -1,4 +1,4 @@
-"""ht_head_loss of very small values: gradients keep their bits.
+"""ht_head_loss of very small values: gradients keep their bits, and where products of H and W are far below the smallest float logits are 0, not NaN.
 Tolerances as in test_gpu_head."""
 import numpy as np
 import pytest
@@ -22,3 +22,27 @@ def test_small_features(ctx, n, C, h):  # noqa: F811
     if h >= 1e-30:
         ref, tol = reference(H, W, y, None, True)
         check(call(ctx, H, W, y, B.HT_W_OUT_IN), ref, tol)
+
+
+@pytest.mark.parametrize("h,w", [(1e-20, 1e-18), (1e-26, 1e-12), (1e-30, 1e-9), (1e-10, 1e-25)])
+@pytest.mark.parametrize("n,C", [(20, 130), (150, 64), (150, 70), (150, 200), (90, 256), (150, 400), (150, 1001)])
+def test_products_below_the_smallest_float(ctx, n, C, h, w):  # noqa: F811
+    rng = np.random.default_rng(n + C)
+    H, W, y = _inputs(n, 96, C, rng, unlabelled=0.1)
+    H, W = (H * np.float32(h)).astype(np.float32), (W * np.float32(w)).astype(np.float32)
+    ref, tol = reference(H, W, y, None, True)
+    for form in (B.HT_W_IN_OUT, B.HT_W_OUT_IN):
+        out = call(ctx, H, W, y, form)
+        check(out, ref, tol)
+        assert np.abs(out["row_lse"][y >= 0] - np.log(C)).max() <= 1e-5
+
+
+def test_one_small_row_among_others(ctx):  # noqa: F811
+    rng = np.random.default_rng(4)
+    H, W, y = _inputs(100, 40, 333, rng)
+    H[17] *= np.float32(1e-30)
+    W *= np.float32(1e-10)
+    H[:17] *= np.float32(1e10)
+    H[18:] *= np.float32(1e10)
+    ref, tol = reference(H, W, y, None, True)
+    check(call(ctx, H, W, y, B.HT_W_OUT_IN), ref, tol)
