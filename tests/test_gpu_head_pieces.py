@@ -1,0 +1,82 @@
+"""ht_head_loss where memory is short: rows and classes in pieces.
+
+The tolerances are those of test_gpu_head, the 64-bit sums are made on the GPU.  (Of 3,000 rows x 36 features a byte budget of 340 MiB leaves pieces of
+1,792 rows x 9,216 classes.)"""
+import numpy as np
+import pytest
+import torch
+
+from paper_2311_14898_amd import binding as B
+from tests.test_gpu_head import STEP, _inputs, _pad, call, check
+
+pytestmark = pytest.mark.gpu
+BUDGET = 340 << 20
+
+
+def reference(H, W, y, u, mean):
+    """test_gpu_head's, on the GPU."""
+    dev = lambda x, t=torch.float64: torch.from_numpy(np.ascontiguousarray(x)).cuda().to(t)
+    H, W, y = dev(H), dev(W), dev(y, torch.int64)
+    (n, d), C = H.shape, W.shape[1]
+    has = y >= 0
+    N = max(1, int(has.sum())) if mean else 1
+    u = torch.where(has, torch.ones(n, device="cuda", dtype=torch.float64) if u is None else dev(u), 0.0)
+    x = H @ W
+    e = (H.abs() @ W.abs()).mul_(3 * 2.0 ** -22 + (3 * np.ceil(d / 16) + 4) * STEP)
+    lse = torch.logsumexp(x, dim=1)
+    at = torch.arange(n, device="cuda"), y.clamp(min=0)
+    b = e.amax(dim=1) + 4 * STEP * (x.abs().amax(dim=1) + lse.abs() + 1) + 2.0 ** -20
+    l = torch.where(has, lse - x[at], 0.0)
+    le = torch.where(has, b + e[at] + 2 * STEP * l.abs(), 0.0)
+    p = x.sub_(lse[:, None]).exp_()
+    e.add_(b[:, None] + 2.0 ** -20).mul_(p).add_(2.0 ** -39)
+    e[at] += 2 * STEP
+    p[at] -= 1.0
+    f = (u / N)[:, None]
+    p.mul_(f), e.mul_(f.abs())
+    terms = 3 * 2.0 ** -22 + (3 * max(n, C) / 16 + 64) * STEP
+    Wt, Ht = W.t().contiguous(), H.t().contiguous()
+    out = dict(loss=(u * l).sum() / N, row_loss=l, row_lse=torch.where(has, lse, 0.0), dH=p @ Wt, dW=Ht @ p)
+    tol = dict(loss=(u.abs() * le).sum() / N + STEP * (u * l).abs().sum() / N, row_loss=le, row_lse=torch.where(has, b, 0.0),
+               dH=e @ Wt.abs() + terms * (p.abs() @ Wt.abs()), dW=Ht.abs() @ e + terms * (Ht.abs() @ p.abs()))
+    return tuple({k: v.cpu().numpy() for k, v in o.items()} for o in (out, tol))
+
+
+@pytest.fixture
+def small():
+    s = torch.cuda.Stream()
+    c = B.ht_ctx_create(0, s.cuda_stream)
+    B.ht_ctx_set_hbm_budget(c, BUDGET)
+    yield c, s
+    B.ht_ctx_destroy(c)
+
+
+@pytest.mark.parametrize("n,C,labelled", [(3000, 18_433, 0.95), (3000, 20_001, 0.95), (3000, 18_433, 0.02)])      # (18,433: the last piece has one class)
+def test_pieces_of_rows_and_classes(small, n, C, labelled):
+    ctx, _ = small
+    rng = np.random.default_rng(C)
+    d = 36
+    H, W, y = _inputs(n, d, C, rng, unlabelled=1 - labelled)
+    y[:4] = [C - 1, 9_215, 9_216, 0]                       # labels at the pieces' borders
+    u = (rng.random(n) * 2).astype(np.float32)
+    dW0 = rng.standard_normal(W.shape).astype(np.float32) * np.float32(1e-4)
+    ref, tol = reference(H, W, y, None, True)
+    weighted, room = reference(H, W, y, u, False)
+    for form in (B.HT_W_IN_OUT, B.HT_W_OUT_IN):
+        check(call(ctx, H, W, y, form), ref, tol)
+        check(call(ctx, H, W, y, form, grad=False), ref, tol)
+        check(call(ctx, H, W, y, form, u=u, mean=False, dW0=dW0), weighted, room, dW0)
+
+
+def test_classes_in_pieces_with_plenty_of_memory():
+    """28,000 rows of few features: the gradients of 20,000 classes are made in two pieces where nothing limits the memory."""
+    rng = np.random.default_rng(6)
+    n, d, C = 28_000, 36, 20_000
+    H, W, y = _inputs(n, d, C, rng, unlabelled=0.1)
+    ref, tol = reference(H, W, y, None, True)
+    ctx = B.ht_ctx_create(0)
+    try:
+        for form in (B.HT_W_IN_OUT, B.HT_W_OUT_IN):
+            check(call(ctx, H, W, y, form), ref, tol)
+    finally:
+        B.ht_ctx_destroy(ctx)
