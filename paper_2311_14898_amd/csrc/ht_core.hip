@@ -231,15 +231,23 @@ int ht_scratch(ht_ctx* ctx, int slot, size_t bytes, void** out) {
     return HT_OK;
   }
   if (ctx->scratch_bytes[slot] < bytes) {
+    const size_t want = ht_scratch_size(bytes);
+    if (ctx->scratch[slot] && ht_slot_stays(ctx, slot)) {      // (where the larger block is refused, the slot keeps the one that it has)
+      void* larger = nullptr;
+      HT_TRY(ht_dev_alloc(ctx, &larger, want));
+      ctx->retired.emplace_back(ctx->scratch[slot], ctx->scratch_bytes[slot]);
+      ctx->scratch[slot] = *out = larger;
+      ctx->scratch_bytes[slot] = want;
+      ++ctx->scratch_gen;
+      return HT_OK;
+    }
     if (ctx->scratch[slot]) {
       if (slot == HT_S_TNPART) HT_TRY(ht_flush_products(ctx, ctx->stream));   // (sums that were left to the end of the epoch are in there)
       HT_HIP(ctx, hipStreamSynchronize(ctx->stream));
-      if (ht_slot_stays(ctx, slot)) ctx->retired.emplace_back(ctx->scratch[slot], ctx->scratch_bytes[slot]);
-      else dev_free(ctx, ctx->scratch[slot], ctx->scratch_bytes[slot], !ctx->recorded);
+      dev_free(ctx, ctx->scratch[slot], ctx->scratch_bytes[slot], !ctx->recorded);
       ctx->scratch[slot] = nullptr;
       ctx->scratch_bytes[slot] = 0;
     }
-    const size_t want = ht_scratch_size(bytes);
     int rc = ht_dev_alloc(ctx, &ctx->scratch[slot], want);
     if (rc != HT_OK) return rc;
     ctx->scratch_bytes[slot] = want;

@@ -1,4 +1,4 @@
-"""ht_head_loss where memory is short: rows and classes in pieces.
+"""ht_head_loss where memory is short: rows and classes in pieces, and refused calls beside a recording.
 
 The tolerances are those of test_gpu_head, the 64-bit sums are made on the GPU.  (Of 3,000 rows x 36 features a byte budget of 340 MiB leaves pieces of
 1,792 rows x 9,216 classes.)"""
@@ -80,3 +80,39 @@ def test_classes_in_pieces_with_plenty_of_memory():
             check(call(ctx, H, W, y, form), ref, tol)
     finally:
         B.ht_ctx_destroy(ctx)
+
+
+def test_a_block_that_replays_work_in_outlives_a_refusal(small):
+    """A larger call that is refused memory on a context with a recording leaves it what it has."""
+    ctx, s = small
+    B.ht_ctx_set_hbm_budget(ctx, 40 << 20)
+    rng = np.random.default_rng(5)
+    n, d, C = 300, 36, 9000
+    H, W, y = _inputs(n, d, C, rng)
+    Hd, Wd, yd, loss = _pad(H), _pad(W), torch.from_numpy(y.astype(np.int32)).cuda(), torch.zeros(1, device="cuda")
+    big = torch.zeros(36, 1_200_000, device="cuda")        # 614 MB of copies
+    torch.cuda.synchronize()
+
+    def run():
+        B.ht_head_loss(ctx, d, C, Hd, Wd, yd, loss, sync=False)
+
+    run()
+    s.synchronize()
+    want = loss.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        run()
+    for _ in range(20):
+        with pytest.raises(B.HongtuError) as err:
+            B.ht_head_loss(ctx, d, 1_200_000, Hd, big, yd, loss, sync=False)
+        assert err.value.code == B.HT_ENOMEM
+        loss.fill_(7.0)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(s):
+            graph.replay()
+        s.synchronize()
+        assert torch.equal(loss, want)
+        run()
+        s.synchronize()
+        assert torch.equal(loss, want)
+    del graph
