@@ -282,6 +282,17 @@ int OpsBlock::take(ht_ctx* ctx, size_t rsort, size_t scan) {
   return HT_OK;
 }
 
+int OpsBlock::take_if_room(ht_ctx* ctx) {
+  if (ctx->scratch_bytes[HT_S_OPS] < bytes) {
+    if (ctx->recorded && ht_caller_captures(ctx)) return HT_ENOMEM;
+    const int64_t more = (int64_t)ht_scratch_size(bytes) - (ht_slot_stays(ctx, HT_S_OPS) ? 0 : (int64_t)ctx->scratch_bytes[HT_S_OPS]);
+    if (!ht_may_spend(ctx) || more > ht_room(ctx)) return HT_ENOMEM;
+  }
+  const int rc = take(ctx);
+  if (rc == HT_ENOMEM) ctx->tight_room = ht_room(ctx);     // (there was room by the figures, and yet none)
+  return rc;
+}
+
 int ht_check_rows(ht_ctx* ctx, const ht_tensor* t, int64_t rows, int32_t cols, const char* name) {
   HT_TRY(ht_check_weights(ctx, t, rows, cols, name));
   if (t->ld & 3) return ht_set_err(ctx, HT_ESHAPE, "%s: row pitch %lld must be a multiple of 4", name, (long long)t->ld);

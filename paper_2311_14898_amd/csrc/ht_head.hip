@@ -1125,7 +1125,7 @@ int head_run(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht_te
   const auto P = m.add<_Float16>(grad ? p.Rp * p.Cp * 2 : 0);
   const auto sh = m.add<float>(dH ? p.sum_rows * p.dpad : 0);
   const auto sw = m.add<float>(dW && p.splits_w > 1 ? p.splits_w * p.Cp * p.dpad : 0);
-  HT_TRY(m.take(ctx));
+  HT_TRY(bytes > HEAD_LEAN ? m.take_if_room(ctx) : m.take(ctx));
 
   uint32_t *wmax = m.at(mx), *hmax_v = wmax + 4, *hmax_j = hmax_v + p.Rp;
   const unsigned clear_blocks = (unsigned)std::min<int64_t>(ceil_div64(n_max, 4096), 1024);
@@ -1276,12 +1276,9 @@ extern "C" int ht_head_loss(ht_ctx* ctx, const ht_head_desc* desc, const ht_tens
   }
   HT_HIP(ctx, hipSetDevice(ctx->device));
   return ht_with_room(ctx, [&]() -> int {
+    if (H->rows > 0 && H->rows <= HT_HEAD_FEW) return ht_head_few(ctx, desc, H, W, labels, row_weight, loss, row_loss, row_lse, dH, dW);      // (less memory than either of these)
     auto run = [&](size_t bytes) { return head_run(ctx, desc, H, W, labels, row_weight, loss, row_loss, row_lse, dH, dW, bytes); };
-    if (H->rows > 0 && H->rows <= HT_HEAD_FEW && ht_may_spend(ctx)) {
-      const int rc = ht_head_few(ctx, desc, H, W, labels, row_weight, loss, row_loss, row_lse, dH, dW);
-      if (rc != HT_ENOMEM) return rc;
-    }
-    const int rc = ht_may_spend(ctx) ? run(HEAD_BYTES) : (int)HT_ENOMEM;
+    const int rc = run(HEAD_BYTES);
     return rc == HT_ENOMEM ? run(HEAD_LEAN) : rc;      // (nothing has been launched by a call that is refused memory)
   });
 }

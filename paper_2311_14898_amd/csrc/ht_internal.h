@@ -285,6 +285,8 @@ struct OpsBlock {
     return a;
   }
   int take(ht_ctx* ctx, size_t rsort = 0, size_t scan = 0);   // (with these bytes of the sort's and the scan's slots beside it)
+  // For calls that can do with less: HT_ENOMEM, and the slot as it was, where it is too small and there is no room for more of it, or a pass is recorded.
+  int take_if_room(ht_ctx* ctx);
   template <typename T>
   T* at(At<T> a) const { return reinterpret_cast<T*>(p + a.off); }
 };

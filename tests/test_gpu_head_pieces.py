@@ -1,4 +1,4 @@
-"""ht_head_loss where memory is short: rows and classes in pieces, and refused calls beside a recording.
+"""ht_head_loss where memory is short: rows and classes in pieces, recorded, and without taking more from call to call.
 
 The tolerances are those of test_gpu_head, the 64-bit sums are made on the GPU.  (Of 3,000 rows x 36 features a byte budget of 340 MiB leaves pieces of
 1,792 rows x 9,216 classes.)"""
@@ -82,6 +82,52 @@ def test_classes_in_pieces_with_plenty_of_memory():
         B.ht_ctx_destroy(ctx)
 
 
+@pytest.mark.parametrize("grad", [True, False])
+def test_a_small_plan_is_recorded_and_takes_no_more_from_call_to_call(small, grad):
+    ctx, s = small
+    rng = np.random.default_rng(3)
+    n, d, C = (3000, 36, 18_433) if grad else (9000, 300, 60_001)
+    if not grad:
+        B.ht_ctx_set_hbm_budget(ctx, 118 << 20)            # (131 MiB in two pieces of rows, 105 in six)
+    H, W, y = _inputs(n, d, C, rng, unlabelled=0.05)
+    Hd, Wd, yd = _pad(H), _pad(W, C), torch.from_numpy(y.astype(np.int32)).cuda()
+    out = {k: torch.zeros(v, device="cuda") for k, v in (("loss", 1), ("row_loss", n), ("row_lse", n))}
+    if grad:
+        out.update(dH=torch.zeros(n, d, device="cuda"), dW=torch.zeros(d, C, device="cuda"))
+    torch.cuda.synchronize()
+
+    def run():
+        B.ht_head_loss(ctx, d, C, Hd, Wd, yd, sync=False, **out)
+
+    def clear():
+        for o in out.values():
+            o.fill_(7.0)
+        torch.cuda.synchronize()
+
+    for _ in range(3):
+        clear()
+        run()
+        s.synchronize()
+    want = {k: v.clone() for k, v in out.items()}
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        run()
+    for _ in range(3):
+        clear()
+        with torch.cuda.stream(s):
+            graph.replay()
+        s.synchronize()
+        for k in out:
+            assert torch.equal(out[k], want[k]), k
+        for _ in range(4):                                 # (a block more each time would be past the budget with the second)
+            clear()
+            run()
+            s.synchronize()
+            for k in out:
+                assert torch.equal(out[k], want[k]), k
+    del graph
+
+
 def test_a_block_that_replays_work_in_outlives_a_refusal(small):
     """A larger call that is refused memory on a context with a recording leaves it what it has."""
     ctx, s = small
@@ -116,3 +162,27 @@ def test_a_block_that_replays_work_in_outlives_a_refusal(small):
         s.synchronize()
         assert torch.equal(loss, want)
     del graph
+
+
+def test_few_rows_after_a_refusal(monkeypatch):
+    """A context whose device had no memory for a large plan takes small ones from then on; up to 64 rows there is one plan, and one result."""
+    rng = np.random.default_rng(8)
+    n, d, C = 40, 36, 9000
+    H, W, y = _inputs(n, d, C, rng)
+    many = _inputs(500, d, C, rng)
+    own = B.ht_ctx_create(0)
+    want = call(own, H, W, y, B.HT_W_IN_OUT)
+    usual = call(own, *many, B.HT_W_IN_OUT)
+    B.ht_ctx_destroy(own)
+    monkeypatch.setenv("HT_REFUSE_ALLOC", "-1")            # (the first hipMalloc fails)
+    ctx = B.ht_ctx_create(0)
+    monkeypatch.delenv("HT_REFUSE_ALLOC")
+    try:
+        for _ in range(2):
+            got = call(ctx, *many, B.HT_W_IN_OUT)
+            assert all(np.allclose(got[k], usual[k], rtol=1e-4, atol=1e-6) for k in got)
+            got = call(ctx, H, W, y, B.HT_W_IN_OUT)
+            for k in got:
+                assert np.array_equal(got[k], want[k]), k
+    finally:
+        B.ht_ctx_destroy(ctx)
