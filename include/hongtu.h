@@ -110,7 +110,8 @@ int ht_sync(ht_ctx *ctx);
  *
  * A call that is refused memory, by the cap or by the device, gives all of
  * that back and is made again chunk by chunk, so no call fails for memory that
- * an earlier one or a faster pass holds.
+ * an earlier one or a faster pass holds.  What recorded calls of the models over
+ * ids below work in is not given back: their replays need it.
  *
  * Without a cap, blocks of device memory that calls and destroyed graphs free
  * (scratch memory only until a caller has recorded a pass on its stream) are

@@ -236,6 +236,7 @@ int ht_scratch(ht_ctx* ctx, int slot, size_t bytes, void** out) {
       void* larger = nullptr;
       HT_TRY(ht_dev_alloc(ctx, &larger, want));
       ctx->retired.emplace_back(ctx->scratch[slot], ctx->scratch_bytes[slot]);
+      ctx->replayed &= ~((uint64_t)1 << slot);                 // (nothing recorded works in the new one)
       ctx->scratch[slot] = *out = larger;
       ctx->scratch_bytes[slot] = want;
       ++ctx->scratch_gen;
@@ -270,10 +271,14 @@ int ht_scratch_release(ht_ctx* ctx, int slot) {
 
 int OpsBlock::take(ht_ctx* ctx, size_t rsort, size_t scan) {
   const std::pair<int, size_t> want[3] = {{HT_S_OPS, bytes}, {HT_S_RSORT, rsort}, {HT_S_SCAN, scan}};
-  for (const auto& w : want)
-    if (w.second > ctx->scratch_bytes[w.first] && ht_caller_captures(ctx))
-      return ht_set_err(ctx, HT_ESTATE, "a recorded pass needs %zu bytes of scratch memory and finds %zu: make the call once before it is recorded", w.second,
-                        ctx->scratch_bytes[w.first]);
+  if (ctx->recorded && ht_caller_captures(ctx)) {
+    for (const auto& w : want)
+      if (w.second > ctx->scratch_bytes[w.first])
+        return ht_set_err(ctx, HT_ESTATE, "a recorded pass needs %zu bytes of scratch memory and finds %zu: make the call once before it is recorded", w.second,
+                          ctx->scratch_bytes[w.first]);
+    for (const auto& w : want)
+      if (w.second > 0) ctx->replayed |= (uint64_t)1 << w.first;
+  }
   for (const auto& w : want) {
     void* q = nullptr;
     if (w.second > 0) HT_TRY(ht_scratch(ctx, w.first, w.second, &q));

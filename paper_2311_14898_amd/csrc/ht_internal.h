@@ -37,6 +37,7 @@ enum {
   HT_S_NBUF, HT_S_SPART, HT_S_LEAVE, HT_S_MISC, HT_S_TFULL, HT_S_TFULL2, HT_S_GATV, HT_S_GATE, HT_S_GATWS, HT_S_GATP, HT_S_GATKEEP,
   HT_S_LINK0, HT_S_LINK1, HT_S_LINK2, HT_S_SCAN, HT_S_RSORT, HT_S_TNTAB, HT_S_LIST, HT_S_DENSE, HT_S_OPS, HT_N_SCRATCH
 };
+static_assert(HT_N_SCRATCH <= 64, "a bit a slot");
 
 constexpr int HT_HS_READBACK = 3, HT_HS_LOSS = 4, HT_N_HS = 5;
 
@@ -103,7 +104,8 @@ struct ht_ctx {
   int64_t tight_room = -1;     // room that was left after the last such call (-1: none since memory was plentiful)
   size_t gat_keep_limit = 0;   // a GAT epoch that kept this many bytes between its passes ran out of memory (0: none did) ...
   int64_t gat_keep_room = 0;   // ... and had this much room without them
-  std::vector<std::pair<void*, size_t>> retired;   // blocks of slots that a recorded pass works in, outgrown since (freed with the context)
+  std::vector<std::pair<void*, size_t>> retired;   // blocks of such slots (`replayed`), outgrown since (freed with the context)
+  uint64_t replayed = 0;       // scratch slots, a bit each, that a recorded pass works in
   bool recorded = false;       // the owner of the stream has recorded a pass, which may be replayed for as long as it likes
   int64_t refuse_alloc = 0;    // HT_REFUSE_ALLOC=k: the context's k-th allocation is refused; -k: its k-th hipMalloc fails (tests)
   int64_t device_bytes = 0;    // HT_DEVICE_BYTES: plan as if the device had no more memory than this for the context (0: as it reports)
@@ -152,10 +154,8 @@ void ht_free_orphan(ht_graph* g);   // a graph whose context is gone
 int ht_scratch(ht_ctx* ctx, int slot, size_t bytes, void** out);
 // Gives a slot's memory back (after the work in flight).
 int ht_scratch_release(ht_ctx* ctx, int slot);
-// Slots whose blocks stay until the context's end once a caller has recorded a pass: replays of the operators below find them there.
-inline bool ht_slot_stays(const ht_ctx* ctx, int slot) {
-  return ctx->recorded && (slot == HT_S_OPS || slot == HT_S_RSORT || slot == HT_S_SCAN);
-}
+// Slots whose blocks stay until the context's end: a call of the operators below was recorded, and its replays find them there.
+inline bool ht_slot_stays(const ht_ctx* ctx, int slot) { return (ctx->replayed >> slot) & 1; }
 // What the device reports free.
 int64_t ht_device_free(ht_ctx* ctx);
 // Bytes that can still be allocated: by the byte budget and by the device's free memory.
