@@ -144,6 +144,7 @@ __global__ void __launch_bounds__(T < 256 ? 256 : T, T < 256 ? 7 : 1) k_distill(
   __shared__ double dred[B / 64];
   __shared__ int with[FEW ? FEW_ROWS : 1];
   const int r = threadIdx.x / T, l = threadIdx.x % T;
+  const uint32_t C = a.C;                        // (columns are counted in 32 bits without a sign: up to 16,383 behind the last of 2^31 - 1)
   const Row<T> row{red};
   int* sid = reinterpret_cast<int*>(entries) + r * a.K;
   float* sq = entries + R * a.K + r * a.K;
@@ -164,13 +165,13 @@ __global__ void __launch_bounds__(T < 256 ? 256 : T, T < 256 ? 7 : 1) k_distill(
     float* g = a.grad ? a.grad + v * a.ld_g : nullptr;
     float4 keep[NV];
     auto read = [&](int i) {                     // the i-th float4 of the thread; what lies behind the last class counts as -inf
-      const int c = (i * T + l) * 4;
+      const uint32_t c = (uint32_t)(i * T + l) * 4;
       float4 y = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-      if (c < a.C) {
+      if (c < C) {
         y = *reinterpret_cast<const float4*>(x + c);
-        if (c + 1 >= a.C) y.y = -INFINITY;
-        if (c + 2 >= a.C) y.z = -INFINITY;
-        if (c + 3 >= a.C) y.w = -INFINITY;
+        if (c + 1 >= C) y.y = -INFINITY;
+        if (c + 2 >= C) y.z = -INFINITY;
+        if (c + 3 >= C) y.w = -INFINITY;
       }
       return y;
     };
@@ -209,7 +210,7 @@ __global__ void __launch_bounds__(T < 256 ? 256 : T, T < 256 ? 7 : 1) k_distill(
     if (top.x == -INFINITY) {                    // no teacher
       if (l == 0 && a.row_loss) a.row_loss[v] = 0.f;
       if (g)
-        for (int c = l * 4; c < a.C; c += T * 4) *reinterpret_cast<float4*>(g + c) = zero4();
+        for (uint32_t c = l * 4; c < C; c += T * 4) *reinterpret_cast<float4*>(g + c) = zero4();
       continue;
     }
     const bool none = top.y == -INFINITY;        // no class is possible
@@ -248,8 +249,8 @@ __global__ void __launch_bounds__(T < 256 ? 256 : T, T < 256 ? 7 : 1) k_distill(
     }
     row.sync();
     auto put = [&](int i, float4 y) {
-      const int c = (i * T + l) * 4;
-      if (c >= a.C) return;
+      const uint32_t c = (uint32_t)(i * T + l) * 4;
+      if (c >= C) return;
       float4 o = make_float4(exp_of(y.x - xm, a) * wp, exp_of(y.y - xm, a) * wp, exp_of(y.z - xm, a) * wp, exp_of(y.w - xm, a) * wp);
       if (none) o = zero4();
       if (MORE) __builtin_nontemporal_store(V4{o.x, o.y, o.z, o.w}, reinterpret_cast<V4*>(g + c));     // (or it drives out of the caches what is read again)
@@ -308,11 +309,11 @@ __global__ void __launch_bounds__(256) k_distill_loss(const double* __restrict__
 
 // ---- few rows of many classes: a row's classes in `gridDim.x` parts.  The first launch leaves each part's maximum and sum, and the entries'
 // logits (before a gradient can take their place); in the second every block joins its row's parts, and one more makes the losses.
-__device__ __forceinline__ void part_of(int C, int parts, int part, int* c0, int* c1) {      // (whole float4s)
+__device__ __forceinline__ void part_of(int C, int parts, int part, uint32_t* c0, uint32_t* c1) {      // (whole float4s)
   const int64_t n4 = ((int64_t)C + 3) / 4;
-  *c0 = (int)(n4 * part / parts * 4);
+  *c0 = (uint32_t)(n4 * part / parts * 4);
   const int64_t e = n4 * (part + 1) / parts * 4;
-  *c1 = e < C ? (int)e : C;
+  *c1 = e < C ? (uint32_t)e : (uint32_t)C;
 }
 
 __global__ void __launch_bounds__(256) k_distill_part(DistillArgs a, float2* __restrict__ part, float* __restrict__ xe) {
@@ -320,7 +321,8 @@ __global__ void __launch_bounds__(256) k_distill_part(DistillArgs a, float2* __r
   const Row<256> row{red};
   const int64_t v = blockIdx.y;
   const float* x = a.x + v * a.ld;
-  int c0, c1;
+  const uint32_t C = a.C;
+  uint32_t c0, c1;
   part_of(a.C, gridDim.x, blockIdx.x, &c0, &c1);
   if (blockIdx.x == 0)
     for (int k = threadIdx.x; k < a.K; k += 256) {
@@ -328,18 +330,18 @@ __global__ void __launch_bounds__(256) k_distill_part(DistillArgs a, float2* __r
       xe[v * a.K + k] = id >= 0 && id < a.C ? x[id] : NAN;
     }
   float m = -INFINITY, z = 0.f;
-  for (int i = c0 + threadIdx.x * 4; i < c1; i += 4096) {
+  for (uint32_t i = c0 + threadIdx.x * 4; i < c1; i += 4096) {
     float4 y[4];
     float n = m;
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const int c = i + u * 1024;
+      const uint32_t c = i + u * 1024;
       y[u] = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
       if (c >= c1) continue;
       y[u] = *reinterpret_cast<const float4*>(x + c);
-      if (c + 1 >= a.C) y[u].y = -INFINITY;
-      if (c + 2 >= a.C) y[u].z = -INFINITY;
-      if (c + 3 >= a.C) y[u].w = -INFINITY;
+      if (c + 1 >= C) y[u].y = -INFINITY;
+      if (c + 2 >= C) y[u].z = -INFINITY;
+      if (c + 3 >= C) y[u].w = -INFINITY;
       n = fmaxf(n, fmaxf(fmaxf(y[u].x, y[u].y), fmaxf(y[u].z, y[u].w)));
     }
     const float s = n == -INFINITY ? 0.f : n;
@@ -378,10 +380,11 @@ __global__ void __launch_bounds__(256) k_distill_apply(DistillArgs a, const floa
     if (!a.grad) return;
     const int64_t v = blockIdx.y;
     float* g = a.grad + v * a.ld_g;
-    int c0, c1;
+    const uint32_t C = a.C;
+    uint32_t c0, c1;
     part_of(a.C, parts, blockIdx.x, &c0, &c1);
     if (!with[v]) {
-      for (int c = c0 + threadIdx.x * 4; c < c1; c += 1024) *reinterpret_cast<float4*>(g + c) = zero4();
+      for (uint32_t c = c0 + threadIdx.x * 4; c < c1; c += 1024) *reinterpret_cast<float4*>(g + c) = zero4();
     } else {
       const float tmax = row.max(make_float2(load_entries<256>(a, v, threadIdx.x, sid, sq), 0.f)).x;
       bool none;
@@ -394,18 +397,18 @@ __global__ void __launch_bounds__(256) k_distill_apply(DistillArgs a, const floa
       const float u = a.weight ? a.weight[v] : 1.f, w = u * a.temp * (a.mean ? 1.f / (float)N : 1.f), ip = none ? 0.f : 1.f / j.y, wp = w * ip;
       const float* x = a.x + v * a.ld;
 #pragma unroll 4
-      for (int c = c0 + threadIdx.x * 4; c < c1; c += 1024) {
+      for (uint32_t c = c0 + threadIdx.x * 4; c < c1; c += 1024) {
         const float4 y = *reinterpret_cast<const float4*>(x + c);
         float4 o = make_float4(exp_of(y.x - j.x, a) * wp, exp_of(y.y - j.x, a) * wp, exp_of(y.z - j.x, a) * wp, exp_of(y.w - j.x, a) * wp);
         if (none) o = zero4();
-        if (c + 1 >= a.C) o.y = 0.f;
-        if (c + 2 >= a.C) o.z = 0.f;
-        if (c + 3 >= a.C) o.w = 0.f;
+        if (c + 1 >= C) o.y = 0.f;
+        if (c + 2 >= C) o.z = 0.f;
+        if (c + 3 >= C) o.w = 0.f;
         *reinterpret_cast<float4*>(g + c) = o;
       }
       __syncthreads();
       for (int k = threadIdx.x; k < a.K; k += 256)
-        if (sid[k] >= c0 && sid[k] < c1) put_entry(a, sid, sq, k, g, w, none ? 0.f : exp_of(xe[v * a.K + k] - j.x, a) * ip);
+        if (sid[k] >= 0 && (uint32_t)sid[k] >= c0 && (uint32_t)sid[k] < c1) put_entry(a, sid, sq, k, g, w, none ? 0.f : exp_of(xe[v * a.K + k] - j.x, a) * ip);
     }
   }
   if ((int)blockIdx.x < parts || blockIdx.y) return;
