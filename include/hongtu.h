@@ -456,7 +456,8 @@ int ht_embed_fwd(ht_ctx *ctx, const ht_tensor *table, const int32_t *ids, float 
 /* The gradient of that: d_table[t] = scale * sum of dH[i] over ids[i] = t, 0 for
  * ids that do not occur; with accumulate the sum is added to what is there, and
  * only rows whose id occurs are touched (with scale * -lr and the table itself:
- * its SGD step).  Ids outside the table count nowhere. */
+ * its SGD step).  Ids outside the table count nowhere.  With more than 1,024 ids
+ * rows have at most 65,535 * 256 columns (HT_ESHAPE). */
 int ht_embed_bwd(ht_ctx *ctx, const ht_tensor *dH, const int32_t *ids, float scale, int32_t accumulate, ht_tensor *d_table);
 
 /* How a head's weights lie: [d x C], as a layer's W, or [C x d], as a table whose

@@ -336,7 +336,7 @@ extern "C" int ht_embed_fwd(ht_ctx* ctx, const ht_tensor* table, const int32_t* 
   HT_TRY(ht_check_rows(ctx, H, H->rows, table->cols, "ht_embed_fwd: H"));
   if (ht_overlap(H, table)) return ht_set_err(ctx, HT_EINVAL, "ht_embed_fwd: H shares memory with table");
   HT_HIP(ctx, hipSetDevice(ctx->device));
-  const int64_t nv = (table->cols + 3) / 4, n = H->rows;
+  const int64_t nv = ceil_div64(table->cols, 4), n = H->rows;
   if (n == 0) return HT_OK;
   const bool past = n * nv * 16 >= EMBED_PAST;
   // (a launch takes less than 2^32 threads)
@@ -358,8 +358,9 @@ extern "C" int ht_embed_bwd(ht_ctx* ctx, const ht_tensor* dH, const int32_t* ids
   HT_TRY(ht_check_rows(ctx, dH, dH->rows, dT->cols, "ht_embed_bwd: dH"));
   if (ht_overlap(dH, dT)) return ht_set_err(ctx, HT_EINVAL, "ht_embed_bwd: d_table shares memory with dH");
   HT_HIP(ctx, hipSetDevice(ctx->device));
-  const int nv = (dT->cols + 3) / 4;
+  const int nv = (int)ceil_div64(dT->cols, 4);
   const int64_t n = dH->rows, V = dT->rows;
+  if (n > EMBED_ONCE && ceil_div64(nv, 64) > 65535) return ht_set_err(ctx, HT_ESHAPE, "ht_embed_bwd: %d columns are too many for %lld entries", dT->cols, (long long)n);      // (of a grid)
   int bits = 1;
   while (((int64_t)1 << bits) <= V) ++bits;
   const EmbedOut out{dT->ptr, dT->ld, V, scale, accumulate, nv};

@@ -1,0 +1,47 @@
+"""ht_embed_fwd / ht_embed_bwd at the ends of their range: the widest rows that a tensor can have."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2311_14898_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = B.ht_ctx_create(0)
+    yield c
+    B.ht_ctx_destroy(c)
+
+
+@pytest.mark.parametrize("d", [2 ** 31 - 1, 2 ** 31 - 6])
+def test_the_widest_rows(ctx, d):
+    ld = (d + 3) // 4 * 4
+    row = torch.arange(ld, dtype=torch.int32, device="cuda").bitwise_and_(1023).float().view(1, ld)
+    ids = torch.zeros(1, dtype=torch.int32, device="cuda")
+    out = torch.full((ld + 1024,), 7.0, device="cuda")
+    B.ht_embed_fwd(ctx, d, row, ids, out[:ld].view(1, ld), scale=2.0)
+    B.ht_sync(ctx)
+    assert torch.equal(out[:d], row[0, :d].mul_(2.0)) and bool((out[ld:] == 7.0).all())
+    out.fill_(7.0)
+    B.ht_embed_bwd(ctx, d, row, ids, out[:ld].view(1, ld), scale=0.5)
+    B.ht_sync(ctx)
+    assert torch.equal(out[:d], row[0, :d].mul_(0.5)) and bool((out[ld:] == 7.0).all())
+
+
+def test_gradients_of_many_entries_have_a_widest_row(ctx):
+    """Refused before anything is looked at: the tensors are described only."""
+    some, ids = torch.zeros(64, device="cuda"), torch.zeros(1025, dtype=torch.int32, device="cuda")
+    lib = B.load()
+
+    def code(d, n):
+        ld = (d + 3) // 4 * 4
+        dH, dT = B.ht_tensor(some.data_ptr(), n, d, ld, B.HT_LOC_DEVICE), B.ht_tensor(some.data_ptr() + (n + 1) * ld * 4, 3, d, ld, B.HT_LOC_DEVICE)
+        return lib.ht_embed_bwd(ctx, C.byref(dH), C.c_void_p(ids.data_ptr()), 1.0, 0, C.byref(dT))
+
+    for d in (65_535 * 256 + 1, 2 ** 31 - 1):
+        assert code(d, 1025) == B.HT_ESHAPE
+    B.ht_sync(ctx)
+    assert not bool(some.any())
