@@ -213,8 +213,7 @@ __global__ void __launch_bounds__(T < 256 ? 256 : T, T < 256 ? 7 : 1) k_distill(
         for (uint32_t c = l * 4; c < C; c += T * 4) *reinterpret_cast<float4*>(g + c) = zero4();
       continue;
     }
-    const bool none = top.y == -INFINITY;        // no class is possible
-    xm = none ? 0.f : top.y;
+    xm = top.y == -INFINITY ? 0.f : top.y;
 #pragma unroll
     for (int u = 0; u < NV; ++u) z += sum4(keep[u], xm);
     if (MORE && mm != -INFINITY) z += zm * exp_of(mm - xm, a);
@@ -223,6 +222,7 @@ __global__ void __launch_bounds__(T < 256 ? 256 : T, T < 256 ? 7 : 1) k_distill(
     for (int k = l; k < a.K; k += T)
       if (sid[k] >= 0) tz += exp_of(sq[k] - top.x, a);
     const float2 sums = row.sum(make_float2(tz, z));
+    const bool none = top.y == -INFINITY && sums.y == 0.f;             // no class is possible (logits that are all NaN, or NaN and -inf, have no largest either)
     const float mq = a.temp * logf(sums.x), lse = none ? 0.f : a.temp * logf(sums.y), iz = 1.f / sums.x, ip = none ? 0.f : 1.f / sums.y;
     float loss = 0.f;
     for (int k = l; k < a.K; k += T) {
@@ -362,8 +362,9 @@ __device__ __forceinline__ float2 join_parts(const DistillArgs& a, const float2*
   const int lane = threadIdx.x & 63;
   const float2 p = lane < parts ? part[lane] : make_float2(-INFINITY, 0.f);
   const float m = wave.max(p).x;
-  *none = m == -INFINITY;
-  return make_float2(*none ? 0.f : m, wave.sum(make_float2(p.x == -INFINITY ? p.y : p.y * exp_of(p.x - m, a), 0.f)).x);
+  const float z = wave.sum(make_float2(p.x == -INFINITY ? p.y : p.y * exp_of(p.x - m, a), 0.f)).x;
+  *none = m == -INFINITY && z == 0.f;
+  return make_float2(m == -INFINITY ? 0.f : m, z);
 }
 
 __global__ void __launch_bounds__(256) k_distill_apply(DistillArgs a, const float2* __restrict__ part, const float* __restrict__ xe, int parts, float* __restrict__ loss) {
