@@ -39,7 +39,8 @@ __global__ void __launch_bounds__(256) k_embed(const float* __restrict__ table, 
 #pragma unroll
   for (int u = 0; u < EMBED_TURNS; ++u)
     if (row[u] < n) {
-      const V4 y{x[u].x * scale, x[u].y * scale, x[u].z * scale, x[u].w * scale};
+      const float f = id[u] < 0 ? 0.f : scale;             // (zeros whatever the scale)
+      const V4 y{x[u].x * f, x[u].y * f, x[u].z * f, x[u].w * f};
       V4* to = reinterpret_cast<V4*>(H + row[u] * ld_h + c[u]);
       if (PAST) __builtin_nontemporal_store(y, to);
       else *to = y;

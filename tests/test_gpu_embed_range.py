@@ -1,4 +1,4 @@
-"""ht_embed_fwd / ht_embed_bwd at the ends of their range: the widest rows that a tensor can have."""
+"""ht_embed_fwd / ht_embed_bwd at the ends of their range: the widest rows that a tensor can have, scales that are not finite."""
 import ctypes as C
 
 import pytest
@@ -45,3 +45,12 @@ def test_gradients_of_many_entries_have_a_widest_row(ctx):
         assert code(d, 1025) == B.HT_ESHAPE
     B.ht_sync(ctx)
     assert not bool(some.any())
+
+
+@pytest.mark.parametrize("scale", [float("inf"), float("nan"), -2.0, 0.0])
+def test_rows_without_an_id_are_zeros_at_any_scale(ctx, scale):
+    table, ids, H = torch.ones(5, 12, device="cuda"), torch.tensor([3, -1, 5, -2 ** 31], dtype=torch.int32, device="cuda"), torch.full((4, 12), 7.0, device="cuda")
+    B.ht_embed_fwd(ctx, 12, table, ids, H, scale=scale)
+    B.ht_sync(ctx)
+    assert bool((H[1] == 0).all()) and bool((H[3] == 0).all()) and bool(torch.isnan(H[2]).all())
+    assert torch.equal(H[0], torch.full((12,), scale, device="cuda")) or (scale != scale and bool(torch.isnan(H[0]).all()))
