@@ -384,12 +384,11 @@ extern "C" int ht_embed_bwd(ht_ctx* ctx, const ht_tensor* dH, const int32_t* ids
     HT_TRY(m.take(ctx, rsort, scan));
     const EmbedClear clear{dT->ptr, accumulate || V == 0 ? 0 : (V - 1) * dT->ld + dT->cols};
     const unsigned key_blocks = (unsigned)ceil_div64(n, few ? 16 : 256), clear_blocks = (unsigned)std::min<int64_t>(ceil_div64(clear.words, 1024), 4096);
-    if (key_blocks + clear_blocks == 0) return HT_OK;
     uint64_t* sorted = m.at(keys);
     if (few) k_embed_rank<<<key_blocks + clear_blocks, 256, (size_t)ceil_div64(n, 4) * 16, ctx->stream>>>(ids, (int)n, V, m.at(keys), key_blocks, clear);
     else k_embed_keys<<<key_blocks + clear_blocks, 256, 0, ctx->stream>>>(ids, n, V, m.at(keys), key_blocks, clear);
     HT_LAUNCH_CHECK(ctx);
-    if (n == 0 || V == 0) return HT_OK;
+    if (V == 0) return HT_OK;
     if (!few) HT_TRY(ht_radix_sort_u64(ctx, m.at(keys), m.at(tmp), n, 32, 32 + bits, &sorted));
     with_lanes(nv, [&](auto lanes) {
       constexpr int LPR = decltype(lanes)::value;
