@@ -485,10 +485,13 @@ typedef struct {
  * exp; 0 without a label.  dH [V x d], dW (as W; both nullable) are the gradients
  * of loss: dH is overwritten, 0 in rows without a label, dW overwritten or, with
  * accumulate_dW, added to.  With no labelled row the loss and the gradients are 0.
- * A label that is not below n_classes makes its row's loss NaN.  Products have
- * fp32 precision (a value of H counts against the largest of its row, in dW
- * against the largest of its feature, one of W against the largest of all: those
- * below 2^-39 of it are 0); where H or W are not finite, what they reach is NaN.
+ * A label that is not below n_classes makes its row's loss NaN.  Products are
+ * added up in fp32.  With at most 64 rows their factors are fp32 too; with more
+ * they keep 22 bits: a value of H down to 2^-17 of the largest of its row (in dW
+ * of its feature), one of W down to 2^-17 of the largest of all, fewer below
+ * that, and none below 2^-39; a probability down to 2^-30, and 2^-51 of the
+ * product's other factor below that.  Where H or W are not finite, what they
+ * reach is NaN.
  * dH and dW may not share memory with an input or with each other. */
 int ht_head_loss(ht_ctx *ctx, const ht_head_desc *desc, const ht_tensor *H, const ht_tensor *W, const int32_t *labels,
                  const float *row_weight, float *loss, float *row_loss, float *row_lse, ht_tensor *dH, ht_tensor *dW);

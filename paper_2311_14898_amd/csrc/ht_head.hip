@@ -11,6 +11,11 @@
 // scaled by a power of two that brings the largest value to [2^14, 2^15); x0 y0 + x0 y1 + x1 y0 are added in fp32.  What is left out is at most 3 x 2^-22 of a
 // product, typically (the roundings are independent) 2^-24 of it, what fp32 loses in rounding it; values below 2^-17 of the
 // largest that they are scaled by keep fewer bits, down to 2^-39 of it.  Three fp16 steps take 96 clocks where an fp32 product takes 512.
+//
+// Gradients of logits have one scale, 2^15, whatever their class: a row of dW of a class that is no row's label is made of small probabilities alone.  Their
+// x1 is held times 2^12, as far as fp16 goes (it is at most 8), and y0 is taken times 2^-12 where they meet, in registers: 22 bits down to p = 2^-30, where a class of 2^24 equal
+// ones has 2^-24, and 2^-52 (with the x1 y1 that is left out 2^-51) in what is smaller.  Without that factor those are 2^-17 and 2^-39.  What it costs, us with | without: 2,048
+// rows x 256 features x 32,768 classes 489 | 485, 2,100 labelled rows of 7,001 x 602 x 50,003 1,468 | 1,448, 8,192 x 256 x 131,072 6,542 | 6,467.
 #include <algorithm>
 
 #include "ht_internal.h"
@@ -30,6 +35,7 @@ constexpr int FRAG = 512;
 constexpr int TM = 256, TN = 128;      // tile of a block: rows of A x rows of B
 constexpr float LOG2E = 1.44269504088896340736f;
 constexpr int P_EXP = 15;              // gradients of logits are held times 2^15
+constexpr int LOW_EXP = 12;            // ... what their rounding leaves times 2^12 more
 constexpr size_t HEAD_BYTES = (size_t)6 << 30, HEAD_LEAN = (size_t)64 << 20;   // of what a piece's rows take
 // Bytes of a piece's gradients of logits, at most.  ms with pieces of 1 GiB | 2 | 6: 8,192 rows x 256 features x 131,072 classes 6.69 | 6.52 | 6.63, 8,192 x 240 x 60,000 3.02 |
 // 2.94 | 2.95, 2,100 labelled rows of 7,001 x 602 x 50,003 1.473 | 1.446 | 1.442.
@@ -307,6 +313,12 @@ __device__ __forceinline__ void split2(float x, _Float16* hi, _Float16* lo) {
   *hi = (_Float16)x;
   *lo = (_Float16)(x - (float)*hi);
 }
+// Of a gradient of a logit, times 2^P_EXP; lo times 2^LOW_EXP.
+__device__ __forceinline__ void split_grad(float x, _Float16* hi, _Float16* lo) {
+  *hi = (_Float16)x;
+  *lo = (_Float16)((x - (float)*hi) * (float)(1 << LOW_EXP));
+}
+__device__ __forceinline__ v8h lowered(v8h x) { return x * (_Float16)(1.f / (1 << LOW_EXP)); }
 
 // Fragments of the matrix by rows (reduction along columns: KS steps) and by columns (reduction along rows, weighted: KS_t steps), zeros behind
 // the last row and column, a 64 x 64 tile a block.
@@ -404,6 +416,7 @@ constexpr int64_t PACK_BLOCKS = 16384;
 // ---------------------------------------------------------------- products
 
 enum { LOSS, GRAD, SUMS, DIRECT, WHOLE };       // WHOLE: LOSS and GRAD, and what is in between, where one tile has all classes
+enum { NEITHER, IS_A, IS_B };                   // which operand are gradients of logits
 // The sums of dH: as many parts of the reduction as there are blocks for, by the rows that there are, which the host does not know.
 constexpr int64_t LONG_PART = 32, SHORT_PART = 8, ONE_EACH = 256;
 struct HeadSplits {
@@ -507,10 +520,11 @@ constexpr int KT = 2, PAIR = 32 * KT;   // steps of a stage; values of the reduc
 // columns of four rows of 16.  (Each half of a fragment starts 640 bytes after the one before, so that what a quarter of the lanes reads
 // lies in other banks than what the others do.)
 constexpr int TURN_HALF = 320;    // halfs
-template <int EPI, bool TURN>
-__device__ __forceinline__ void split_nt(const NtArgs& a, const unsigned block) {
-  constexpr int STAGE = TURN ? TN / 16 * 4 * TURN_HALF : TN / 32 * KT * 2 * FRAG;        // halfs
-  __shared__ __attribute__((aligned(16))) _Float16 Bs[2 * STAGE];
+constexpr int stage_halfs(bool turn) { return turn ? TN / 16 * 4 * TURN_HALF : TN / 32 * KT * 2 * FRAG; }
+template <int EPI, int GRADS>
+__device__ __forceinline__ void split_nt(const NtArgs& a, const unsigned block, _Float16* Bs) {
+  constexpr bool TURN = GRADS != NEITHER;
+  constexpr int STAGE = stage_halfs(TURN);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
   if (EPI != GRAD && block >= a.clear.from) return clear_rows(a.clear, block - a.clear.from);
   const int64_t rows = a.total ? piece_rows(a.total, a.r0, a.most) : 0;
@@ -586,10 +600,11 @@ __device__ __forceinline__ void split_nt(const NtArgs& a, const unsigned block) 
       if (k + 1 < 4 * KT) read_b(b[(k + 1) & 1], cur, k + 1);
       __builtin_amdgcn_sched_barrier(0);
       const int j = k & 3;
+      const v8h y0 = GRADS == IS_A ? lowered(y[0]) : y[0];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][1], y[0], acc[i][j], 0, 0, 0);
+      for (int i = 0; i < 2; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][1], y0, acc[i][j], 0, 0, 0);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][0], y[1], acc[i][j], 0, 0, 0);
+      for (int i = 0; i < 2; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(GRADS == IS_B ? lowered(x[i][0]) : x[i][0], y[1], acc[i][j], 0, 0, 0);
 #pragma unroll
       for (int i = 0; i < 2; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][0], y[0], acc[i][j], 0, 0, 0);
     }
@@ -729,7 +744,7 @@ __device__ __forceinline__ void split_nt(const NtArgs& a, const unsigned block) 
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
           _Float16 x, y;
-          split2(p[ks * 8 + u], &x, &y);
+          split_grad(p[ks * 8 + u], &x, &y);
           hi[u] = x;
           lo[u] = y;
         }
@@ -834,14 +849,18 @@ __device__ __forceinline__ void split_nt(const NtArgs& a, const unsigned block) 
     for (int j = 0; j < 4; ++j) put_grad(j, n0 + j * 32 + l32 < rows ? a.norm[n0 + j * 32 + l32] : make_float2(0.f, 0.f));
   }
 }
-template <int EPI, bool TURN>
-__global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) { split_nt<EPI, TURN>(a, blockIdx.x); }
+template <int EPI, int GRADS>
+__global__ void __launch_bounds__(256, 2) k_split_nt(NtArgs a) {
+  __shared__ __attribute__((aligned(16))) _Float16 Bs[2 * stage_halfs(GRADS != NEITHER)];
+  split_nt<EPI, GRADS>(a, blockIdx.x, Bs);
+}
 // dH's and dW's sums, which do not wait for each other, the second behind the first `from` blocks, where those have no more tiles than there are CUs.  us of a call, so |
 // in two launches: 100 rows x 64 features x 300 classes 52 | 63, 1,000 x 256 x 1,000 73 | 84, 20,000 x 128 x 300 126 | 131; of more tiles the two take each
 // other's place in the caches: 60,000 x 256 x 172 217 | 210, 233,000 x 256 x 41 605 | 580.
 __global__ void __launch_bounds__(256, 2) k_split_both(NtArgs first, NtArgs second, unsigned from) {
-  if (blockIdx.x < from) return split_nt<SUMS, true>(first, blockIdx.x);
-  split_nt<SUMS, true>(second, blockIdx.x - from);
+  __shared__ __attribute__((aligned(16))) _Float16 Bs[2 * stage_halfs(true)];
+  if (blockIdx.x < from) return split_nt<SUMS, IS_A>(first, blockIdx.x, Bs);
+  split_nt<SUMS, IS_B>(second, blockIdx.x - from, Bs);
 }
 
 // ---------------------------------------------------------------- what the products leave
@@ -923,7 +942,7 @@ __global__ void __launch_bounds__(256) k_head_grad(_Float16* __restrict__ P, int
         if (c >= lim) p = 0.f;
         if (c == off) p -= (float)(1 << P_EXP);
         _Float16 a, l;
-        split2(p, &a, &l);
+        split_grad(p, &a, &l);
         hi[u] = a, lo[u] = l;
       }
       __builtin_nontemporal_store(hi, reinterpret_cast<v8h*>(at + k * 2 * FRAG));
@@ -1077,11 +1096,12 @@ int nt_blocks(ht_ctx* ctx, NtArgs* a, unsigned* grid) {
 int split_nt(ht_ctx* ctx, hipStream_t st, int epi, NtArgs a) {
   unsigned grid = 0;
   HT_TRY(nt_blocks(ctx, &a, &grid));
-  if (epi == WHOLE) k_split_nt<WHOLE, false><<<grid, 256, 0, st>>>(a);
-  else if (epi == LOSS) k_split_nt<LOSS, false><<<grid, 256, 0, st>>>(a);
-  else if (epi == GRAD) k_split_nt<GRAD, false><<<grid, 256, 0, st>>>(a);
-  else if (epi == DIRECT) k_split_nt<DIRECT, true><<<grid, 256, 0, st>>>(a);
-  else k_split_nt<SUMS, true><<<grid, 256, 0, st>>>(a);
+  if (epi == WHOLE) k_split_nt<WHOLE, NEITHER><<<grid, 256, 0, st>>>(a);
+  else if (epi == LOSS) k_split_nt<LOSS, NEITHER><<<grid, 256, 0, st>>>(a);
+  else if (epi == GRAD) k_split_nt<GRAD, NEITHER><<<grid, 256, 0, st>>>(a);
+  else if (epi == DIRECT) k_split_nt<DIRECT, IS_B><<<grid, 256, 0, st>>>(a);
+  else if (a.rows_are == 1) k_split_nt<SUMS, IS_A><<<grid, 256, 0, st>>>(a);
+  else k_split_nt<SUMS, IS_B><<<grid, 256, 0, st>>>(a);
   HT_LAUNCH_CHECK(ctx);
   return HT_OK;
 }
