@@ -441,7 +441,8 @@ int ht_gat_epoch(ht_ctx *ctx, const ht_graph *g, const ht_gat_model *model, cons
  * that have an id instead of features, and losses over many classes.  All
  * tensors in HBM, values fp32, ids int32; an id < 0 stands for none.  Results do
  * not depend on the order in which the GPU runs things: the same bits from call
- * to call.  The calls are asynchronous on the context's stream.  A program may
+ * to call (ht_head_loss of more than 64 rows: as long as the memory that there is
+ * allows the same pieces).  The calls are asynchronous on the context's stream.  A program may
  * record them (HIP graphs) after it has made the same calls once: a recorded
  * call allocates nothing, and is refused with HT_ESTATE where it would have to;
  * what memory a recording works in stays with the context until its end.
@@ -478,9 +479,11 @@ typedef struct {
  *   x_v = H_v W ;  l_v = log sum_c exp(x_vc) - x_v,labels[v] ;  loss = sum u_v l_v / N
  * over the rows with a label (labels[v] >= 0; the others cost nothing but their
  * label), u = row_weight (device, nullable: 1).  The logits are not all kept:
- * scratch memory is 4 bytes a weight, and up to some 8 GiB for pieces of rows and
- * classes (pieces are smaller where memory is scarce); with at most 64 rows, 4
- * bytes a logit and up to 1 GiB for the sums of dH.
+ * scratch memory is 4 bytes a weight, with classes counted in 256s and features in
+ * 128s, and up to some 8 GiB for pieces of rows and classes (pieces are smaller
+ * where memory is scarce, by all rows and not by the labelled ones); with at most
+ * 64 rows, 4 bytes a logit and up to 1 GiB for the sums of dH; and an eighth of
+ * that.
  * loss: device float.  row_loss, row_lse (device [V], nullable): l_v, and log sum
  * exp; 0 without a label.  dH [V x d], dW (as W; both nullable) are the gradients
  * of loss: dH is overwritten, 0 in rows without a label, dW overwritten or, with

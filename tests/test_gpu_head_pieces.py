@@ -186,3 +186,23 @@ def test_few_rows_after_a_refusal(monkeypatch):
                 assert np.array_equal(got[k], want[k]), k
     finally:
         B.ht_ctx_destroy(ctx)
+
+
+@pytest.mark.parametrize("d,C", [(1, 1_000_000), (7, 300_000), (129, 100_000), (256, 50_000)])
+@pytest.mark.parametrize("form", [B.HT_W_IN_OUT, B.HT_W_OUT_IN])
+def test_scratch_memory_is_what_is_said(d, C, form):
+    """The loss alone of 100 rows: 4 bytes a weight, classes counted in 256s and features in 128s, 4 bytes a value of the rows, 8 a row and 256 classes; and an eighth."""
+    up = lambda x, m: (x + m - 1) // m * m
+    rng = np.random.default_rng(d)
+    H, W, y = _inputs(100, d, C, rng)
+    x = H.astype(np.float64) @ W.astype(np.float64)
+    m = x.max(axis=1)
+    lse = np.log(np.exp(x - m[:, None]).sum(axis=1)) + m
+    ctx = B.ht_ctx_create(0)
+    try:
+        bytes_ = 4 * up(C, 256) * up(d, 128) + 256 * (4 * up(d, 128) + 8 * (up(C, 256) // 256)) + (1 << 18)
+        B.ht_ctx_set_hbm_budget(ctx, bytes_ + bytes_ // 8)
+        out = call(ctx, H, W, y, form, grad=False)
+        assert np.abs(out["row_lse"] - lse).max() <= 1e-4
+    finally:
+        B.ht_ctx_destroy(ctx)

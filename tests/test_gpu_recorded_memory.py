@@ -1,4 +1,4 @@
-"""Scratch memory of a context that has recorded something: only what the recorded calls work in stays."""
+"""Scratch memory of a context that has recorded something: what the recorded calls work in stays, and nothing else."""
 import pytest
 import torch
 
@@ -91,3 +91,49 @@ def test_what_replays_work_in_stays_when_memory_is_given_back():
         del graph
     finally:
         B.ht_ctx_destroy(ctx)
+
+
+@pytest.mark.parametrize("n,V", [(262_144, 5000), (262_145, 131_072), (3_000_001, 70_000)])
+def test_long_sorts_recorded_and_replayed(n, V):
+    """Beyond 262,144 entries the sort scans its counts in memory of its own; other ids in the same place before each replay."""
+    s = torch.cuda.Stream()
+    ctx = B.ht_ctx_create(0, s.cuda_stream)
+    other = B.ht_ctx_create(0)
+    try:
+        g = torch.Generator(device="cuda")
+        g.manual_seed(n)
+        dH, ids = torch.randn(n, 8, generator=g, device="cuda"), torch.zeros(n, dtype=torch.int32, device="cuda")
+        dT, want = torch.zeros(V, 8, device="cuda"), torch.zeros(V, 8, device="cuda")
+
+        def renew():
+            ids.copy_(torch.randint(-1, V, (n,), generator=g, device="cuda", dtype=torch.int32))
+            ids[: n // 3] = V // 2
+            B.ht_embed_bwd(other, 8, dH, ids, want)
+            B.ht_sync(other)
+            dT.fill_(7.0)
+            torch.cuda.synchronize()
+
+        renew()
+        B.ht_embed_bwd(ctx, 8, dH, ids, dT, sync=False)
+        s.synchronize()
+        assert torch.equal(dT, want)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            B.ht_embed_bwd(ctx, 8, dH, ids, dT, sync=False)
+        for _ in range(4):
+            renew()
+            with torch.cuda.stream(s):
+                graph.replay()
+            s.synchronize()
+            assert torch.equal(dT, want)
+        src, dst = inputs.rmat_edges(50_000, 1_000_000, seed=2)          # (a partition sorts in the same memory)
+        B.ht_graph_destroy(B.ht_partition(ctx, 50_000, src.cuda(), dst.cuda(), 2))
+        renew()
+        with torch.cuda.stream(s):
+            graph.replay()
+        s.synchronize()
+        assert torch.equal(dT, want)
+        del graph
+    finally:
+        B.ht_ctx_destroy(ctx)
+        B.ht_ctx_destroy(other)
