@@ -500,11 +500,13 @@ int ht_head_loss(ht_ctx *ctx, const ht_head_desc *desc, const ht_tensor *H, cons
                  const float *row_weight, float *loss, float *row_loss, float *row_lse, ht_tensor *dH, ht_tensor *dW);
 
 enum { HT_DISTILL_MAX_K = 256 };
+#define HT_DISTILL_MAX_TEMPERATURE 1e37f
 typedef struct {
   int32_t n_classes;
   int32_t k;           /* a row's entries of the teacher, 1 .. HT_DISTILL_MAX_K       */
   int32_t reduction;   /* HT_REDUCE_MEAN: N = rows with a teacher; HT_REDUCE_SUM: N = 1 */
-  float temperature;   /* T > 0, and so large that log2(e) / T is finite in fp32      */
+  float temperature;   /* T > 0, so large that log2(e) / T is finite in fp32, and at
+                          most HT_DISTILL_MAX_TEMPERATURE                              */
 } ht_distill_desc;
 
 /* Distillation from a teacher's top logits.  A row's entries are top_ids[v*k ..]

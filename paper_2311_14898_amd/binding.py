@@ -33,7 +33,7 @@ HT_BUF_H, HT_BUF_A, HT_BUF_GH, HT_BUF_DW = 0, 1, 2, 3
 HT_W_IN_OUT, HT_W_OUT_IN = 0, 1
 HT_REDUCE_MEAN, HT_REDUCE_SUM = 0, 1
 HT_HEAD_MAX_WIDTH, HT_HEAD_MAX_CLASSES = 65536, 1 << 24
-HT_DISTILL_MAX_K = 256
+HT_DISTILL_MAX_K, HT_DISTILL_MAX_TEMPERATURE = 256, 1e37
 HT_MAX_LAYERS = 8
 
 

@@ -479,7 +479,9 @@ extern "C" int ht_distill_loss(ht_ctx* ctx, const ht_distill_desc* desc, const h
   if (desc->n_classes <= 0) return ht_set_err(ctx, HT_ESHAPE, "ht_distill_loss: number of classes must be positive");
   if (desc->k < 1 || desc->k > HT_DISTILL_MAX_K) return ht_set_err(ctx, HT_ESHAPE, "ht_distill_loss: %d entries a row, at least 1 and at most %d", desc->k, HT_DISTILL_MAX_K);
   if ((!top_ids || !top_logits) && logits->rows > 0) return ht_set_err(ctx, HT_EINVAL, "ht_distill_loss: null argument");
-  if (!(desc->temperature > 0.f) || desc->temperature > 3.0e38f) return ht_set_err(ctx, HT_EINVAL, "ht_distill_loss: temperature must be positive and finite");
+  // (temperature times the logarithm of a sum of up to 2^31 exponentials, below 22, is finite)
+  if (!(desc->temperature > 0.f) || desc->temperature > HT_DISTILL_MAX_TEMPERATURE)
+    return ht_set_err(ctx, HT_EINVAL, "ht_distill_loss: temperature must be positive and at most %g", (double)HT_DISTILL_MAX_TEMPERATURE);
   if (desc->reduction != HT_REDUCE_MEAN && desc->reduction != HT_REDUCE_SUM)
     return ht_set_err(ctx, HT_EINVAL, "ht_distill_loss: unknown reduction %d", desc->reduction);
   HT_TRY(ht_check_rows(ctx, logits, logits->rows, desc->n_classes, "ht_distill_loss: logits"));

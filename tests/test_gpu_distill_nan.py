@@ -1,4 +1,4 @@
-"""ht_distill_loss of rows whose logits have no largest: -inf throughout is a row without a possible class, NaN stays NaN."""
+"""ht_distill_loss of rows whose logits have no largest: -inf throughout is a row without a possible class, NaN stays NaN.  And temperatures at the end of their range."""
 import numpy as np
 import pytest
 import torch
@@ -42,3 +42,25 @@ def test_rows_of_no_numbers(ctx, n, C):
     np.add.at(want, ids[2], -q / q.sum())
     assert np.abs(dX[2] - want).max() <= 1e-6
     assert np.isfinite(row_loss[3:]).all() and np.isfinite(dX[3:]).all()
+
+
+@pytest.mark.parametrize("n,C", [(2, 40), (3, 9001), (70, 300), (70, 70_001)])
+def test_the_largest_temperature(ctx, n, C):
+    rng = np.random.default_rng(1)
+    T, K = 1e37, 200
+    ld = (C + 3) // 4 * 4
+    X = torch.randn(n, ld, device="cuda")
+    ids, top = torch.from_numpy(rng.integers(0, C, (n, K)).astype(np.int32)).cuda(), torch.randn(n, K, device="cuda")
+    loss, row_loss, dX = torch.zeros(1, device="cuda"), torch.zeros(n, device="cuda"), torch.zeros(n, ld, device="cuda")
+    B.ht_distill_loss(ctx, C, X, ids, top, loss, temperature=T, row_loss=row_loss, dlogits=dX, reduction=B.HT_REDUCE_SUM)
+    B.ht_sync(ctx)
+    # p = 1 / C, q = 1 / K: T^2 (log C - log K) is beyond fp32, not NaN
+    sign = np.sign(C - K)
+    assert float(loss) == sign * np.inf and (row_loss.cpu().numpy() == sign * np.inf).all()
+    want = np.full((n, C), 1.0 / C)
+    np.add.at(want, (np.arange(n)[:, None], ids.cpu().numpy()), -1.0 / K)
+    assert np.abs(dX.cpu().numpy()[:, :C].astype(np.float64) / T - want).max() <= 1e-6
+    for t in (1.01e37, 3e38):
+        with pytest.raises(B.HongtuError) as err:
+            B.ht_distill_loss(ctx, C, X, ids, top, loss, temperature=t)
+        assert err.value.code == B.HT_EINVAL
