@@ -171,6 +171,9 @@ struct Clear {
   int64_t v0, v1;
   unsigned from, blocks;
 };
+// Which share each launch takes matters little: the first 45 % | 30 | 17 | 15 (the others in proportion) 275 | 270 | 264 | 267 us by 1,000,000 x 256 x 172 with 1 % labelled,
+// 123 | 116 | 121 | 121 by 1,000,000 x 64 x 100, 351 | 351 | 355 | 352 by 300,000 x 602 x 41 with 10 % (all in the first launch 302, 133, 389); the shares here are
+// roughly those of the launches' times where few rows have labels.
 constexpr double CLEAR_TOP = 0.3, CLEAR_PACK = 0.4, CLEAR_LOGITS = 0.6, CLEAR_DH = 0.72, CLEAR_DW = 0.85;
 constexpr int64_t CLEAR_SHARED = (int64_t)64 << 20;
 // A wave 64 rows at a time.
