@@ -202,7 +202,7 @@ __global__ void __launch_bounds__(256) k_few_logits(FewArgs a) {
 }
 
 // A block a row; the last of them to come to an end adds up the losses.  norm (largest logit m, 1 / sum of exp(x - m)), l_of: of the labelled rows in order.
-__global__ void __launch_bounds__(256) k_few_join(FewArgs a, const float* __restrict__ weight, int mean, float2* __restrict__ norm, float* __restrict__ l_of,
+__global__ void __launch_bounds__(256) k_few_join(FewArgs a, const float* __restrict__ weight, int mean, float2* __restrict__ norm, double* __restrict__ l_of,
                                                   float* __restrict__ row_loss, float* __restrict__ row_lse, float* __restrict__ loss) {
   __shared__ int idx[64];
   __shared__ int32_t lab[64];
@@ -236,7 +236,7 @@ __global__ void __launch_bounds__(256) k_few_join(FewArgs a, const float* __rest
       for (int w = 0; w < 4; ++w) z += sh[w].x == -INFINITY ? sh[w].y : sh[w].y * exp_less(sh[w].x, m);
       const float lse = m + logf(z), l = lab[v] < a.C ? lse - a.xlab[v] : NAN;
       norm[v] = make_float2(m, 1.f / z);
-      __hip_atomic_store(l_of + v, weight ? weight[at] * l : l, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __hip_atomic_store(l_of + v, weight ? (double)weight[at] * (double)l : (double)l, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       if (row_loss) row_loss[at] = l;
       if (row_lse) row_lse[at] = lse;
     }
@@ -245,7 +245,7 @@ __global__ void __launch_bounds__(256) k_few_join(FewArgs a, const float* __rest
   unsigned ended = 0;
   if (lane == 0) ended = __hip_atomic_fetch_add(a.ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
   if (__builtin_amdgcn_readfirstlane((int)ended) != (int)gridDim.x - 1) return;
-  double s = lane < rows.n ? (double)__hip_atomic_load(l_of + lane, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0;
+  double s = lane < rows.n ? __hip_atomic_load(l_of + lane, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0;
   for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
   if (lane == 0) *loss = rows.n > 0 ? (float)(s / (mean ? (double)rows.n : 1.0)) : 0.f;
 }
@@ -465,7 +465,8 @@ int ht_head_few(ht_ctx* ctx, const ht_head_desc* D, const ht_tensor* H, const ht
   OpsBlock m;
   const auto X = m.add<float>(grad ? NB * 16 * ldx : 0);
   const auto part = m.add<float2>((int64_t)64 * blocks);
-  const auto xlab = m.add<float>(64), lrow = m.add<float>(64);
+  const auto xlab = m.add<float>(64);
+  const auto lrow = m.add<double>(64);
   const auto norm = m.add<float2>(64);
   const auto ticket = m.add<unsigned>(1);
   const auto ph = m.add<float>(dH ? (int64_t)dh_parts * NB * 16 * d : 0);

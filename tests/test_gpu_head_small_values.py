@@ -1,4 +1,4 @@
-"""ht_head_loss of very small values: gradients keep their bits, and where products of H and W are far below the smallest float logits are 0, not NaN.
+"""ht_head_loss of very small and very large values: gradients keep their bits, and where products of H and W are far below the smallest float logits are 0, not NaN.
 Tolerances as in test_gpu_head."""
 import numpy as np
 import pytest
@@ -46,3 +46,21 @@ def test_one_small_row_among_others(ctx):  # noqa: F811
     H[18:] *= np.float32(1e10)
     ref, tol = reference(H, W, y, None, True)
     check(call(ctx, H, W, y, B.HT_W_OUT_IN), ref, tol)
+
+
+@pytest.mark.parametrize("n", [1, 40, 64, 65, 200])
+def test_losses_are_weighted_and_added_up_in_64_bits(ctx, n):  # noqa: F811
+    """u l is beyond fp32 for a row, the mean is not; and weights of both signs whose sum is small."""
+    rng = np.random.default_rng(n)
+    H, W, y = _inputs(n, 8, 30, rng, spread=40.0)
+    u = np.zeros(n, np.float32)
+    u[0], y[0] = 3e38, int((H[0].astype(np.float64) @ W).argmin())
+    out = call(ctx, H, W, y, B.HT_W_IN_OUT, u=u, grad=False)
+    l = float(out["row_loss"][0])
+    assert l > 5
+    want = float(u[0]) * l / n
+    assert (abs(out["loss"] - want) <= 2.0 ** -22 * want) if want < 3.4e38 else out["loss"] == np.inf
+    u = np.where(np.arange(n) % 2, -1.0, 1.0).astype(np.float32) * np.float32(1.1)
+    out = call(ctx, H, W, y, B.HT_W_IN_OUT, u=u, mean=False, grad=False)
+    want = (u.astype(np.float64) * out["row_loss"].astype(np.float64)).sum()
+    assert abs(out["loss"] - want) <= 2.0 ** -24 * abs(want) + 1e-12 * np.abs(out["row_loss"]).sum()
