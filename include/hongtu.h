@@ -442,10 +442,10 @@ int ht_gat_epoch(ht_ctx *ctx, const ht_graph *g, const ht_gat_model *model, cons
  * tensors in HBM, values fp32, ids int32; an id < 0 stands for none.  Results do
  * not depend on the order in which the GPU runs things: the same bits from call
  * to call (ht_head_loss of more than 64 rows: as long as the memory that there is
- * allows the same pieces).  The calls are asynchronous on the context's stream.  A program may
- * record them (HIP graphs) after it has made the same calls once: a recorded
- * call allocates nothing, and is refused with HT_ESTATE where it would have to;
- * what memory a recording works in stays with the context until its end.
+ * allows the same pieces).  The calls are asynchronous on the context's stream.  A
+ * program may record them (HIP graphs) after it has made the same calls once: a
+ * recorded call allocates nothing, and is refused with HT_ESTATE where it would
+ * have to; what memory a recording works in stays with the context until its end.
  * Calls and replays on one context share its scratch memory and must not overlap
  * in time. */
 
@@ -494,7 +494,8 @@ typedef struct {
  * of its feature), one of W down to 2^-17 of the largest of all, fewer below
  * that, and none below 2^-39; a probability down to 2^-30, and 2^-51 of the
  * product's other factor below that.  Where H or W are not finite, what they
- * reach is NaN.
+ * reach is NaN (with at most 64 rows a logit of -inf leaves its row's loss the
+ * others').
  * dH and dW may not share memory with an input or with each other. */
 int ht_head_loss(ht_ctx *ctx, const ht_head_desc *desc, const ht_tensor *H, const ht_tensor *W, const int32_t *labels,
                  const float *row_weight, float *loss, float *row_loss, float *row_lse, ht_tensor *dH, ht_tensor *dW);

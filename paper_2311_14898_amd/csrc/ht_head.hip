@@ -13,7 +13,7 @@
 // largest that they are scaled by keep fewer bits, down to 2^-39 of it.  Three fp16 steps take 96 clocks where an fp32 product takes 512.
 //
 // Gradients of logits have one scale, 2^15, whatever their class: a row of dW of a class that is no row's label is made of small probabilities alone.  Their
-// x1 is held times 2^12, as far as fp16 goes (it is at most 8), and y0 is taken times 2^-12 where they meet, in registers: 22 bits down to p = 2^-30, where a class of 2^24 equal
+// x1 is held times 2^12, as far as fp16 goes (it is at most 8: scales are powers of two, so that x - m is exact and no p is rounded beyond 1), and y0 is taken times 2^-12 where they meet, in registers: 22 bits down to p = 2^-30, where a class of 2^24 equal
 // ones has 2^-24, and 2^-52 (with the x1 y1 that is left out 2^-51) in what is smaller.  Without that factor those are 2^-17 and 2^-39.  What it costs, us with | without: 2,048
 // rows x 256 features x 32,768 classes 489 | 485, 2,100 labelled rows of 7,001 x 602 x 50,003 1,468 | 1,448, 8,192 x 256 x 131,072 6,542 | 6,467.
 #include <algorithm>
