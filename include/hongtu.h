@@ -25,7 +25,10 @@
  *   ht_embed_fwd, ht_embed_bwd   rows of a table by id, and the table's gradient;
  *   ht_head_loss                 softmax cross entropy of a linear layer over
  *                                many classes, with its gradients;
- *   ht_distill_loss              distillation from a teacher's top logits.
+ *   ht_distill_loss              distillation from a teacher's top logits;
+ *   ht_ffn_fwd, ht_ffn_bwd       gated feed-forward blocks, and their gradients;
+ *   ht_grad_norm, ht_grad_clip   the norm of many tensors together, and those
+ *                                tensors scaled by what it may be (an SGD step too).
  *
  * Conventions
  *   - Every function returns an int status: HT_OK (0) or a negative HT_E* code.
@@ -524,6 +527,60 @@ typedef struct {
  * nullable. */
 int ht_distill_loss(ht_ctx *ctx, const ht_distill_desc *desc, const ht_tensor *logits, const int32_t *top_ids,
                     const float *top_logits, const float *row_weight, float *loss, float *row_loss, ht_tensor *dlogits);
+
+/* -------------------------------------- models over ids: blocks and their step */
+
+/* The activation of a block's gate: a s(a) with s(a) = 1 / (1 + exp(-a)); a Phi(a)
+ * with the normal distribution Phi; a s(2 sqrt(2 / pi) (a + 0.044715 a^3)), which is
+ * a (1 + tanh(..)) / 2; max(a, 0), whose derivative at 0 is 0; s(a). */
+enum { HT_GATE_SILU = 0, HT_GATE_GELU = 1, HT_GATE_GELU_TANH = 2, HT_GATE_RELU = 3, HT_GATE_SIGMOID = 4 };
+enum { HT_FFN_MAX_WIDTH = 65536 };
+typedef struct {
+  int32_t d_in, d_hidden, d_out;   /* d, f, e below; 1 .. HT_FFN_MAX_WIDTH                   */
+  int32_t act;                     /* HT_GATE_*                                              */
+  int32_t w_form;                  /* HT_W_IN_OUT: Wg, Wu [d x f], Wd [f x e], as a layer's W;
+                                      HT_W_OUT_IN: [f x d], [e x f]                          */
+  int32_t accumulate;              /* 1: Y (dX) is added to what is there                    */
+  int32_t accumulate_dW;           /* 1: dWg, dWu, dWd are added to what is there            */
+  int32_t reserved;
+} ht_ffn_desc;
+
+/* A gated feed-forward block over the rows of X [n x d]:
+ *   A = X Wg ;  B = X Wu ;  Y = (act(A) * B) Wd  [n x e]
+ * All tensors in HBM; row pitches of Wg, Wu, Wd may be any number of floats from the
+ * columns on.  gate, up [n x f] (both or neither): A and B, for the backward pass.
+ * Y, gate and up may not share memory with an input or with each other (columns of
+ * one matrix beside each other do not).  Asynchronous, recorded, and the same bits
+ * from call to call, as the calls above. */
+int ht_ffn_fwd(ht_ctx *ctx, const ht_ffn_desc *desc, const ht_tensor *X, const ht_tensor *Wg, const ht_tensor *Wu, const ht_tensor *Wd,
+               ht_tensor *Y, ht_tensor *gate, ht_tensor *up);
+/* Its gradients from dY: with G = dY Wd^T,
+ *   dA = G * B * act'(A) ;  dB = G * act(A) ;  dX = dA Wg^T + dB Wu^T
+ *   dWg = X^T dA ;  dWu = X^T dB ;  dWd = (act(A) * B)^T dY
+ * gate, up: what ht_ffn_fwd left there, or null: A and B are made again.  Each of
+ * dX [n x d], dWg, dWu, dWd (as the weights) may be null; with n = 0 those of the
+ * weights are 0.  Outputs may not share memory with an input or with each other. */
+int ht_ffn_bwd(ht_ctx *ctx, const ht_ffn_desc *desc, const ht_tensor *X, const ht_tensor *Wg, const ht_tensor *Wu, const ht_tensor *Wd,
+               const ht_tensor *gate, const ht_tensor *up, const ht_tensor *dY, ht_tensor *dX, ht_tensor *dWg, ht_tensor *dWu, ht_tensor *dWd);
+
+/* The norm of the values of n tensors together, in HBM and of any row pitch:
+ *   *norm = sqrt(sum of the squares of them all)
+ * norm: device float.  Squares are added up in 64 bits: no value is too small or
+ * too large for its square, but a norm above the largest float is +inf.  grads is
+ * an array of n on the host, which the call is done with when it returns; n may be
+ * 0 (a norm of 0).  A tensor that is named twice counts twice. */
+int ht_grad_norm(ht_ctx *ctx, int32_t n, const ht_tensor *grads, float *norm);
+/* The same norm, and every tensor scaled so that it is at most max_norm > 0 (+inf: as
+ * it is):
+ *   c = max_norm / norm where the norm is larger, else 1 ;  out_i = scale c grads_i
+ * or, with accumulate, out_i += scale c grads_i (with -lr and the parameters: an SGD
+ * step with clipped gradients in one pass).  out: n tensors of the same shapes, or
+ * null for grads themselves; one of them may be its gradient (in place: the same
+ * pointer and pitch), otherwise out shares no memory with grads or with itself.
+ * norm: device float, nullable: the norm before.  c is taken from the norm in 64
+ * bits.  With a gradient that is NaN all of out is; with infinite ones c is 0, and
+ * out NaN where they are. */
+int ht_grad_clip(ht_ctx *ctx, int32_t n, const ht_tensor *grads, float max_norm, float scale, int32_t accumulate, ht_tensor *out, float *norm);
 
 /* -------------------------------------------------------------------- epoch */
 

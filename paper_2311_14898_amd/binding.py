@@ -114,6 +114,10 @@ class ht_plan_opts(C.Structure):
                 ("reserved", C.c_int32)]
 
 
+HT_GATE_SILU, HT_GATE_GELU, HT_GATE_GELU_TANH, HT_GATE_RELU, HT_GATE_SIGMOID = range(5)
+HT_FFN_MAX_WIDTH = 65536
+
+
 class ht_head_desc(C.Structure):
     _fields_ = [("d", C.c_int32), ("n_classes", C.c_int32), ("w_form", C.c_int32), ("reduction", C.c_int32),
                 ("accumulate_dW", C.c_int32), ("reserved", C.c_int32)]
@@ -123,11 +127,16 @@ class ht_distill_desc(C.Structure):
     _fields_ = [("n_classes", C.c_int32), ("k", C.c_int32), ("reduction", C.c_int32), ("temperature", C.c_float)]
 
 
+class ht_ffn_desc(C.Structure):
+    _fields_ = [("d_in", C.c_int32), ("d_hidden", C.c_int32), ("d_out", C.c_int32), ("act", C.c_int32), ("w_form", C.c_int32),
+                ("accumulate", C.c_int32), ("accumulate_dW", C.c_int32), ("reserved", C.c_int32)]
+
+
 EXPORTS = ["ht_ctx_create", "ht_ctx_destroy", "ht_sync", "ht_ctx_set_hbm_budget", "ht_ctx_graph_launches", "ht_tensor_zero", "ht_strerror", "ht_last_error",
            "ht_partition", "ht_graph_destroy", "ht_graph_info_get", "ht_graph_chunk_info", "ht_graph_export_chunk",
            "ht_graph_export_csc", "ht_graph_chunk_order", "ht_graph_reorganize", "ht_layer_fwd", "ht_layer_fwd_static", "ht_layer_bwd", "ht_epoch", "ht_epoch_buffer", "ht_tensor_to_host", "ht_memory_model",
            "ht_chunk_rows_model", "ht_gat_layer_fwd", "ht_gat_layer_bwd", "ht_gat_epoch", "ht_comm_cost_model",
-           "ht_embed_fwd", "ht_embed_bwd", "ht_head_loss", "ht_distill_loss"]
+           "ht_embed_fwd", "ht_embed_bwd", "ht_head_loss", "ht_distill_loss", "ht_ffn_fwd", "ht_ffn_bwd", "ht_grad_norm", "ht_grad_clip"]
 
 _lib = None
 
@@ -196,6 +205,10 @@ def load():
                                  C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(ht_tensor), C.POINTER(ht_tensor)]
     lib.ht_distill_loss.argtypes = [C.c_void_p, C.POINTER(ht_distill_desc), C.POINTER(ht_tensor), C.c_void_p, C.c_void_p,
                                     C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(ht_tensor)]
+    lib.ht_ffn_fwd.argtypes = [C.c_void_p, C.POINTER(ht_ffn_desc)] + [C.POINTER(ht_tensor)] * 7
+    lib.ht_ffn_bwd.argtypes = [C.c_void_p, C.POINTER(ht_ffn_desc)] + [C.POINTER(ht_tensor)] * 11
+    lib.ht_grad_norm.argtypes = [C.c_void_p, C.c_int32, C.POINTER(ht_tensor), C.c_void_p]
+    lib.ht_grad_clip.argtypes = [C.c_void_p, C.c_int32, C.POINTER(ht_tensor), C.c_float, C.c_float, C.c_int32, C.POINTER(ht_tensor), C.c_void_p]
     _lib = lib
     return lib
 
@@ -508,6 +521,62 @@ def ht_distill_loss(ctx, n_classes: int, logits: torch.Tensor, top_ids: torch.Te
     if sync:
         torch.cuda.synchronize()
     _check(load().ht_distill_loss(ctx, C.byref(desc), _ref(logits, n_classes), *args, _ref(dlogits, n_classes)), ctx)
+
+
+# -------------------------------------- models over ids: blocks and their step
+
+def _ffn_args(d_in, d_hidden, d_out, X, Wg, Wu, Wd, act, w_form, accumulate, accumulate_dW):
+    desc = ht_ffn_desc(d_in, d_hidden, d_out, act, w_form, int(accumulate), int(accumulate_dW), 0)
+    c, cd = (d_hidden, d_out) if w_form == HT_W_IN_OUT else (d_in, d_hidden)
+    return desc, c, cd, [_ref(X, d_in), _ref(Wg, c), _ref(Wu, c), _ref(Wd, cd)]
+
+
+def ht_ffn_fwd(ctx, d_in: int, d_hidden: int, d_out: int, X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: torch.Tensor, Y: torch.Tensor,
+               gate: Optional[torch.Tensor] = None, up: Optional[torch.Tensor] = None, act: int = HT_GATE_SILU, w_form: int = HT_W_IN_OUT,
+               accumulate: bool = False, sync: bool = True):
+    """Y (+)= (act(X Wg) * (X Wu)) Wd; gate, up: X Wg and X Wu, kept for the backward pass."""
+    desc, _, _, args = _ffn_args(d_in, d_hidden, d_out, X, Wg, Wu, Wd, act, w_form, accumulate, False)
+    if sync:
+        torch.cuda.synchronize()
+    _check(load().ht_ffn_fwd(ctx, C.byref(desc), *args, _ref(Y, d_out), _ref(gate, d_hidden), _ref(up, d_hidden)), ctx)
+
+
+def ht_ffn_bwd(ctx, d_in: int, d_hidden: int, d_out: int, X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: torch.Tensor, dY: torch.Tensor,
+               dX: Optional[torch.Tensor] = None, dWg: Optional[torch.Tensor] = None, dWu: Optional[torch.Tensor] = None,
+               dWd: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None, up: Optional[torch.Tensor] = None,
+               act: int = HT_GATE_SILU, w_form: int = HT_W_IN_OUT, accumulate: bool = False, accumulate_dW: bool = False, sync: bool = True):
+    """The gradients of that block that are asked for, from dY."""
+    desc, c, cd, args = _ffn_args(d_in, d_hidden, d_out, X, Wg, Wu, Wd, act, w_form, accumulate, accumulate_dW)
+    if sync:
+        torch.cuda.synchronize()
+    _check(load().ht_ffn_bwd(ctx, C.byref(desc), *args, _ref(gate, d_hidden), _ref(up, d_hidden), _ref(dY, d_out), _ref(dX, d_in), _ref(dWg, c),
+                             _ref(dWu, c), _ref(dWd, cd)), ctx)
+
+
+def _views(tensors: Sequence[torch.Tensor], cols: Optional[Sequence[int]]):
+    """An array of ht_tensor; `cols`: their columns of data (else all of them).  Vectors are single rows."""
+    assert cols is None or len(cols) == len(tensors)
+    rows = [t.unsqueeze(0) if t.dim() == 1 else t for t in tensors]
+    return (ht_tensor * len(rows))(*[tensor_view(t, t.shape[1] if cols is None else cols[i]) for i, t in enumerate(rows)])
+
+
+def ht_grad_norm(ctx, grads: Sequence[torch.Tensor], norm: torch.Tensor, cols: Optional[Sequence[int]] = None, sync: bool = True):
+    """norm (device tensor of one float) = the norm of all values of the tensors together."""
+    views, norm_p = _views(grads, cols), _dev(norm, torch.float32, (1,), "norm")
+    if sync:
+        torch.cuda.synchronize()
+    _check(load().ht_grad_norm(ctx, len(views), views, norm_p), ctx)
+
+
+def ht_grad_clip(ctx, grads: Sequence[torch.Tensor], max_norm: float, out: Optional[Sequence[torch.Tensor]] = None, scale: float = 1.0,
+                 accumulate: bool = False, norm: Optional[torch.Tensor] = None, cols: Optional[Sequence[int]] = None, sync: bool = True):
+    """out (+)= scale * min(1, max_norm / norm) * grads; out: None for grads themselves."""
+    views, norm_p = _views(grads, cols), _dev(norm, torch.float32, (1,), "norm")
+    assert out is None or len(out) == len(grads)
+    out_views = None if out is None else _views(out, cols)
+    if sync:
+        torch.cuda.synchronize()
+    _check(load().ht_grad_clip(ctx, len(views), views, max_norm, scale, int(accumulate), out_views, norm_p), ctx)
 
 
 # -------------------------------------------------------------------- epoch

@@ -322,6 +322,14 @@ bool ht_overlap(const ht_tensor* a, const ht_tensor* b) {
   return a->ptr < b1 && b->ptr < a1;
 }
 
+bool ht_shares(const ht_tensor* a, const ht_tensor* b) {
+  if (!ht_overlap(a, b)) return false;
+  if (a->ld != b->ld || a->rows < 2 || b->rows < 2) return true;
+  int64_t off = (b->ptr - a->ptr) % a->ld;                  // b's first column, in a's rows
+  if (off < 0) off += a->ld;
+  return off < a->cols || off + b->cols > a->ld;
+}
+
 int64_t ht_device_free(ht_ctx* ctx) {
   int64_t room = INT64_MAX;
   size_t free_b = 0, total_b = 0;

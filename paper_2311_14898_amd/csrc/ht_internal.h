@@ -294,6 +294,8 @@ struct OpsBlock {
 int ht_check_rows(ht_ctx* ctx, const ht_tensor* t, int64_t rows, int32_t cols, const char* name);
 int ht_check_weights(ht_ctx* ctx, const ht_tensor* t, int64_t rows, int32_t cols, const char* name);
 bool ht_overlap(const ht_tensor* a, const ht_tensor* b);
+// The same of their columns of data alone: parts of one matrix's columns beside each other share nothing.
+bool ht_shares(const ht_tensor* a, const ht_tensor* b);
 
 static inline int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
