@@ -18,21 +18,10 @@
 // rows x 256 features x 32,768 classes 489 | 485, 2,100 labelled rows of 7,001 x 602 x 50,003 1,468 | 1,448, 8,192 x 256 x 131,072 6,542 | 6,467.
 #include <algorithm>
 
-#include "ht_internal.h"
+#include "ht_split.h"
 
 namespace {
 
-typedef _Float16 v8h __attribute__((ext_vector_type(8)));
-typedef float v16f __attribute__((ext_vector_type(16)));
-typedef float V4 __attribute__((ext_vector_type(4)));
-typedef float V4u __attribute__((ext_vector_type(4), aligned(4)));      // weights need no alignment
-
-// Operands lie in fragments, what a matrix instruction reads of them: 32 rows x 16 values of the reduction of one plane (x0 or x1), 1 KiB.
-// Lane l + 32 h holds row l and the values 8 (t / 4) + 4 h + t % 4, t = 0 .. 7: the order in which a lane of a product's result holds
-// its rows, so that results become operands without leaving their lanes (any order will do that both operands have).  Fragment (row block,
-// step, plane) is number (block * KS + step) * 2 + plane.
-constexpr int FRAG = 512;
-constexpr int TM = 256, TN = 128;      // tile of a block: rows of A x rows of B
 constexpr float LOG2E = 1.44269504088896340736f;
 constexpr int P_EXP = 15;              // gradients of logits are held times 2^15
 constexpr int LOW_EXP = 12;            // ... what their rounding leaves times 2^12 more
@@ -41,8 +30,6 @@ constexpr size_t HEAD_BYTES = (size_t)6 << 30, HEAD_LEAN = (size_t)64 << 20;   /
 // 2.94 | 2.95, 2,100 labelled rows of 7,001 x 602 x 50,003 1.473 | 1.446 | 1.442.
 constexpr size_t HEAD_PIECE = (size_t)2 << 30;
 constexpr int64_t HEAD_CLASSES = 8192;             // of a piece at least, where a row's share of the memory is settled
-
-__host__ __device__ constexpr int64_t up_to(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
 // exp(x - m).  (The difference first: products with log2 e of logits of 10^9 are rounded by more than 1.)
 __device__ __forceinline__ float exp_less(float x, float m) { return __builtin_amdgcn_exp2f((x - m) * LOG2E); }
@@ -312,10 +299,6 @@ __global__ void __launch_bounds__(256) k_head_top(HeadTop a) {
   clear_rows(a.clear, block - a.w_blocks);
 }
 
-__device__ __forceinline__ void split2(float x, _Float16* hi, _Float16* lo) {
-  *hi = (_Float16)x;
-  *lo = (_Float16)(x - (float)*hi);
-}
 // Of a gradient of a logit, times 2^P_EXP; lo times 2^LOW_EXP.
 __device__ __forceinline__ void split_grad(float x, _Float16* hi, _Float16* lo) {
   *hi = (_Float16)x;
@@ -507,23 +490,9 @@ __device__ __forceinline__ float row_end(float m, float z, float xlab, int64_t a
   return l;
 }
 
-// Column `lane % 16` of four rows of 16, each 16 lanes for themselves, which name four of a row each.
-typedef _Float16 v4h __attribute__((ext_vector_type(4)));
-typedef short v4s __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ v4h turned(const _Float16* p) {
-  return __builtin_bit_cast(v4h, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)p));
-}
-
-constexpr int KT = 2, PAIR = 32 * KT;   // steps of a stage; values of the reduction in two stages, which go together
 // C = A B^T of fragments, 256 x 128 a block, 64 x 128 a wave.  A wave reads its own rows of A straight into registers, a stage ahead, and the four
 // waves share B through LDS, which is filled a stage ahead as well; two blocks a CU.
-//
-// TURN: B is the transpose of what its fragments hold, rows of the reduction by 16s of its own rows (for dH W's classes by features, for dW
-// the gradients' rows by classes).  A stage is 32 rows of the reduction by 128, and lies in LDS as in memory; ds_read_tr gives 16 lanes the
-// columns of four rows of 16.  (Each half of a fragment starts 640 bytes after the one before, so that what a quarter of the lanes reads
-// lies in other banks than what the others do.)
-constexpr int TURN_HALF = 320;    // halfs
-constexpr int stage_halfs(bool turn) { return turn ? TN / 16 * 4 * TURN_HALF : TN / 32 * KT * 2 * FRAG; }
+// TURN: for dH W's classes by features, for dW the gradients' rows by classes.
 template <int EPI, int GRADS>
 __device__ __forceinline__ void split_nt(const NtArgs& a, const unsigned block, _Float16* Bs) {
   constexpr bool TURN = GRADS != NEITHER;
