@@ -1,10 +1,18 @@
 // Gated feed-forward blocks:  A = X Wg ;  B = X Wu ;  H = act(A) * B ;  Y = H Wd, and their gradients:
 //   G = dY Wd^T ;  dA = G * B * act'(A) ;  dB = G * act(A) ;  dX = dA Wg^T + dB Wu^T ;  dWg = X^T dA ;  dWu = X^T dB ;  dWd = H^T dY
+//
+// All products are fp32 products on the fp16 matrix cores (ht_split.h).  X, dY and the weights are packed into fragments of split values first: by
+// rows, scaled by the largest of each row (of all of a weight); for the gradients of weights also by columns, scaled by the largest of each column.
+// The hidden columns of Wg and Wu lie interleaved by 32s, so that one product makes A and B of the same column in the same lane, and dA and dB are one operand
+// with a reduction over both.  H, dA and dB are kept in fp32, in the order of fragments, and with the largest values of their rows and columns; the products that
+// read them split them as they load: no pass in between, and either scale as the reduction asks for it.
 #include <algorithm>
 
-#include "ht_internal.h"
+#include "ht_split.h"
 
 namespace {
+
+constexpr int HB = 32;                 // hidden columns of a block: [gate, up] of interleaved operands
 
 // act(a) and its derivative.  exp(-|a|) gives s(a) and s(-a) = 1 - s(a) without cancellation.
 struct Act {
@@ -25,106 +33,731 @@ __device__ __forceinline__ Act act_of(int act, float a) {
   return {a * s, fmaf(a * s, t * du, s)};
 }
 
-// C[m, n] (+)= sum_k A[m, k] B[k, n], each by its strides; 64 x 64 a block.
-struct Product {
-  const float *A, *B;
-  float* C;
-  int64_t am, ak, bk, bn, cm, cn, M, N, K;
+
+// ---------------------------------------------------------------- scales
+
+// The exponent of the power of two that brings what has its largest absolute value in these bits to [2^14, 2^15).  Largest values are those of
+// what is finite: the rest becomes NaN in its split, and takes no bits off the others.  (NONE: there is nothing, or only zeros.)
+constexpr int NONE = 1 << 20;
+__device__ __forceinline__ int scale_exp(uint32_t bits) {
+  if (bits == 0) return NONE;
+  const int e = 141 - (int)(bits >> 23);
+  return e > 126 ? 126 : e;            // (values below 2^-112 come to less)
+}
+__device__ __forceinline__ int exp_or_0(int e) { return e >= NONE ? 0 : e; }
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)((e < -126 ? -126 : e > 126 ? 126 : e) + 127) << 23); }
+__device__ __forceinline__ uint32_t size_bits(float x) {
+  const uint32_t b = __float_as_uint(fabsf(x));
+  return b < 0x7f800000u ? b : 0u;
+}
+__device__ __forceinline__ void raise(uint32_t* word, uint32_t m) {       // (most find a word as large as it need be)
+  if (__hip_atomic_load(word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) < m) atomicMax(word, m);
+}
+
+// ---------------------------------------------------------------- operands
+
+// A matrix [rows x cols], pitch ld, of which the largest values are wanted: of each row, of each column, or of all of it (words that hold zeros).
+struct Top {
+  const float* p;
+  int64_t ld, rows, cols;
+  uint32_t *rmax, *cmax, *all;         // (null: not wanted)
+  unsigned blocks;
+};
+constexpr int TOPS = 5, TOP_ROWS = 32;
+struct Tops {
+  Top top[TOPS];
+  int n;
+};
+// A block takes TOP_ROWS rows by 256 columns, a wave 8 of the rows, four columns a lane.
+__global__ void __launch_bounds__(256) k_ffn_top(Tops tops) {
+  __shared__ uint32_t sh[4][256];
+  unsigned block = blockIdx.x;
+  int k = 0;
+  while (block >= tops.top[k].blocks) block -= tops.top[k++].blocks;
+  const Top& t = tops.top[k];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const unsigned cb = (unsigned)((t.cols + 255) / 256);
+  const int64_t r0 = (int64_t)(block / cb) * TOP_ROWS + wave * 8, c = (int64_t)(block % cb) * 256 + lane * 4;
+  uint4 cm = make_uint4(0, 0, 0, 0);
+  V4 x[8];
+#pragma unroll
+  for (int q = 0; q < 8; ++q) {
+    const int64_t r = r0 + q < t.rows ? r0 + q : t.rows - 1;               // (the last row again, behind it)
+    const float* at = t.p + r * t.ld + c;
+    if (c + 4 <= t.cols) {
+      x[q] = *reinterpret_cast<const V4u*>(at);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[q][i] = c + i < t.cols ? at[i] : 0.f;
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < 8; ++q) {
+    const uint4 b = make_uint4(size_bits(x[q][0]), size_bits(x[q][1]), size_bits(x[q][2]), size_bits(x[q][3]));
+    cm = make_uint4(max(cm.x, b.x), max(cm.y, b.y), max(cm.z, b.z), max(cm.w, b.w));
+    if (t.rmax) {
+      uint32_t m = max(max(b.x, b.y), max(b.z, b.w));
+      for (int o = 32; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
+      if (lane == 0 && r0 + q < t.rows) raise(t.rmax + r0 + q, m);
+    }
+  }
+  *reinterpret_cast<uint4*>(&sh[wave][lane * 4]) = cm;
+  __syncthreads();
+  const uint32_t m = max(max(sh[0][threadIdx.x], sh[1][threadIdx.x]), max(sh[2][threadIdx.x], sh[3][threadIdx.x]));
+  const int64_t col = (int64_t)(block % cb) * 256 + threadIdx.x;
+  if (t.cmax && col < t.cols) raise(t.cmax + col, m);
+  if (t.all) {
+    uint32_t a = m;
+    for (int o = 32; o > 0; o >>= 1) a = max(a, (uint32_t)__shfl_xor((int)a, o, 64));
+    if (lane == 0) raise(t.all, a);
+  }
+}
+
+// Fragments of a matrix by rows (R: reduction along columns, KS steps apart) and by columns (T: reduction along rows), zeros behind the last row and column; a
+// 64 x 64 tile a block.  Row block b of R is number b mul + add (so of T: its column blocks).
+struct Pack {
+  const float* p;
+  int64_t ld, rows, cols;
+  const uint32_t *rmax, *cmax, *all;   // scales: `all` of both, or rows for R and columns for T
+  _Float16 *R, *T;
+  int64_t KS, KS_t;
+  int mul, add;
+  unsigned row_tiles, col_tiles;
+};
+struct Packs {
+  Pack pack[TOPS];
+  int n;
+};
+__global__ void __launch_bounds__(256) k_ffn_pack(Packs packs) {
+  __shared__ float sh[64][65];
+  unsigned block = blockIdx.x;
+  int i = 0;
+  while (block >= packs.pack[i].row_tiles * packs.pack[i].col_tiles) block -= packs.pack[i].row_tiles * packs.pack[i].col_tiles, ++i;
+  const Pack& a = packs.pack[i];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, half = lane >> 5;
+  const int64_t r0 = (int64_t)(block / a.col_tiles) * 64, c0 = (int64_t)(block % a.col_tiles) * 64;
+  const int c4 = (lane & 15) * 4, rq = wave * 16 + (lane >> 4);
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int64_t r = r0 + rq + q * 4;
+    const float* at = a.p + (r < a.rows ? r : a.rows - 1) * a.ld + c0 + c4;
+    V4 y;
+    if (c0 + 64 <= a.cols) {
+      y = *reinterpret_cast<const V4u*>(at);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) y[k] = c0 + c4 + k < a.cols ? at[k] : 0.f;
+    }
+    if (r >= a.rows) y = V4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) sh[rq + q * 4][c4 + k] = y[k];
+  }
+  __syncthreads();
+  auto put = [&](_Float16* to, int64_t frag, const float* x) {
+    v8h hi, lo;
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      _Float16 u, v;
+      split2(x[t], &u, &v);
+      hi[t] = u;
+      lo[t] = v;
+    }
+    *reinterpret_cast<v8h*>(to + frag * 2 * FRAG + lane * 8) = hi;
+    *reinterpret_cast<v8h*>(to + frag * 2 * FRAG + FRAG + lane * 8) = lo;
+  };
+  const int b = wave >> 1;                        // row block of the tile; a wave takes two of its four steps
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int ks = (wave & 1) * 2 + u, k = ks * 16 + half * 4;
+    float x[8];
+    if (a.R && c0 / 16 + ks < a.KS) {
+      const int r = b * 32 + l32;
+      const float f = pow2(exp_or_0(scale_exp(a.all ? *a.all : r0 + r < a.rows ? a.rmax[r0 + r] : 0u)));
+#pragma unroll
+      for (int t = 0; t < 8; ++t) x[t] = sh[r][k + (t >> 2) * 8 + (t & 3)] * f;
+      put(a.R, ((r0 / 32 + b) * a.mul + a.add) * a.KS + c0 / 16 + ks, x);
+    }
+    if (a.T && r0 / 16 + ks < a.KS_t) {
+      const int c = b * 32 + l32;
+      const float f = pow2(exp_or_0(scale_exp(a.all ? *a.all : c0 + c < a.cols ? a.cmax[c0 + c] : 0u)));
+#pragma unroll
+      for (int t = 0; t < 8; ++t) x[t] = sh[k + (t >> 2) * 8 + (t & 3)][c] * f;
+      put(a.T, ((c0 / 32 + b) * a.mul + a.add) * a.KS_t + r0 / 16 + ks, x);
+    }
+  }
+}
+
+// ---------------------------------------------------------------- products
+
+// PROJECT  A's rows: the interleaved hidden columns, B's the rows of X: A and B of the block, H and its largest values
+// BACK     A's rows: the hidden columns of Wd, B's the rows of dY: G, from that and A and B all of H, dA, dB and their largest values
+// ROWS     A: H or [dA dB] by rows, B: a weight turned: Y, dX
+// COLS     A: X or dY by columns, B: [dA dB] or H turned: gradients of weights
+enum { PROJECT, BACK, ROWS, COLS };
+
+struct Out {                           // value (m, n) at m ms + n ns, split_part floats apart
+  float* p;
+  int64_t ms, ns, split_part;
+};
+struct Args {
+  const _Float16 *A, *B;               // fragments; row blocks KSA, KSB steps apart (B turned: of its own)
+  int64_t KSA, KSB;
+  int64_t mt, nt;                      // tiles
+  int64_t pairs;                       // of stages, of the reduction
+  int splits;                          // parts of it
+  int act;
+  int two;                             // an operand is [dA dB]
+  // largest values: of the weights (gate or only one, up), of the rows of X or dY; of what is made or read by rows and by columns (H; or dA and dB)
+  const uint32_t *w0, *w1, *rows_in;
+  uint32_t *h_row, *a_row, *b_row, *h_col, *a_col, *b_col;
+  const uint32_t* m_top;               // COLS: of A's rows
+  int64_t n, f;                        // rows, hidden columns that there are
+  float *H, *D;                        // in the order of fragments (null: not wanted)
+  int64_t KSH, KSD;
+  float *gate, *up;                    // [n x f]
+  int64_t ld_gate, ld_up;
+  Out out[2];                          // ROWS: [0]; COLS of [dA dB]: gate's and up's (null: not wanted)
+  int64_t m_end, n_end;                // (n_end: of hidden columns, for COLS)
   int add;
 };
-__global__ void __launch_bounds__(256) k_ffn_product(Product p) {
-  __shared__ float As[16][65], Bs[16][65];
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const int64_t m0 = (int64_t)blockIdx.x * 64, n0 = (int64_t)blockIdx.y * 64;
-  float acc[4][4] = {};
-  for (int64_t k0 = 0; k0 < p.K; k0 += 16) {
-    for (int i = threadIdx.x; i < 1024; i += 256) {
-      const int64_t k = k0 + (i & 15), m = m0 + (i >> 4), n = n0 + (i >> 4);
-      As[i & 15][i >> 4] = k < p.K && m < p.M ? p.A[m * p.am + k * p.ak] : 0.f;
-      Bs[i & 15][i >> 4] = k < p.K && n < p.N ? p.B[k * p.bk + n * p.bn] : 0.f;
-    }
-    __syncthreads();
-    for (int k = 0; k < 16; ++k)
-      for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(As[k][ty * 4 + i], Bs[k][tx * 4 + j], acc[i][j]);
-    __syncthreads();
+
+__device__ __forceinline__ V4 as_floats(v8h x) { return __builtin_bit_cast(V4, x); }
+// Eight values (t = 0 .. 3 and 4 .. 7 where the planes will be), each times its factor
+template <class F>
+__device__ __forceinline__ void split8(v8h& p0, v8h& p1, F&& factor) {
+  const V4 x = as_floats(p0), y = as_floats(p1);
+  v8h hi, lo;
+#pragma unroll
+  for (int t = 0; t < 8; ++t) {
+    _Float16 u, v;
+    split2((t < 4 ? x[t & 3] : y[t & 3]) * factor(t), &u, &v);
+    hi[t] = u, lo[t] = v;
   }
-  for (int i = 0; i < 4; ++i)
+  p0 = hi, p1 = lo;
+}
+
+// Of eight words a lane (of 16, of which each half of a lane's 32 neighbours keeps one half) ... down to one a lane: the largest of each over l32, word e in the
+// lanes whose bits 4, 3, 2, 1 are e's bits 3, 2, 1, 0.
+__device__ __forceinline__ uint32_t max_over_32(const uint32_t (&x)[16]) {
+  const int l32 = threadIdx.x & 31;
+  uint32_t y[8], z[4], w[2], v;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const uint32_t keep = l32 & 16 ? x[k + 8] : x[k], give = l32 & 16 ? x[k] : x[k + 8];
+    y[k] = max(keep, (uint32_t)__shfl_xor((int)give, 16, 64));
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const uint32_t keep = l32 & 8 ? y[k + 4] : y[k], give = l32 & 8 ? y[k] : y[k + 4];
+    z[k] = max(keep, (uint32_t)__shfl_xor((int)give, 8, 64));
+  }
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const uint32_t keep = l32 & 4 ? z[k + 2] : z[k], give = l32 & 4 ? z[k] : z[k + 2];
+    w[k] = max(keep, (uint32_t)__shfl_xor((int)give, 4, 64));
+  }
+  const uint32_t keep = l32 & 2 ? w[1] : w[0], give = l32 & 2 ? w[0] : w[1];
+  v = max(keep, (uint32_t)__shfl_xor((int)give, 2, 64));
+  return max(v, (uint32_t)__shfl_xor((int)v, 1, 64));
+}
+
+// C = A B^T of fragments, 256 x 128 a block, 64 x 128 a wave.  A wave reads its own rows of A straight into registers, a stage ahead, and the four
+// waves share B through LDS, which is filled a stage ahead as well; two blocks a CU.
+template <int MODE>
+__global__ void __launch_bounds__(256, 2) k_ffn_split(Args a) {
+  constexpr bool TURN = MODE == ROWS || MODE == COLS;
+  constexpr int STAGE = stage_halfs(TURN);
+  __shared__ __attribute__((aligned(16))) _Float16 Bs[2 * STAGE];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
+  // each XCD takes a contiguous part of the tiles, eight tiles of A over all of B after eight others
+  const int64_t tiles = a.mt * a.nt, per = (tiles * a.splits + 7) / 8, ts = (int64_t)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  if ((int64_t)(blockIdx.x >> 3) >= per || ts >= tiles * a.splits) return;
+  const int64_t split = ts / tiles, t = ts - split * tiles;
+  const int64_t g = t / (8 * a.nt), gm = a.mt - g * 8 < 8 ? a.mt - g * 8 : 8, q = t - g * 8 * a.nt;
+  const int64_t m0 = (g * 8 + q % gm) * TM, n0 = q / gm * TN;
+  const int64_t s0 = a.pairs * split / a.splits * 2;                 // its first stage
+  int todo = __builtin_amdgcn_readfirstlane((int)(a.pairs * (split + 1) / a.splits - s0 / 2));
+  const int64_t mw = m0 + wave * 64;
+
+  // exponents of the weights; of the rows of A (ROWS), of the columns that are split on the way to LDS (COLS)
+  const int e0 = exp_or_0(a.w0 ? scale_exp(*a.w0) : NONE), e1 = exp_or_0(a.w1 ? scale_exp(*a.w1) : NONE);
+  // of a row of H or [dA dB], times the weights that it meets: the smallest that its parts allow
+  auto row_exp = [&](int64_t v) {
+    int e = NONE * 2;
+    if (a.two) {
+      const int x = scale_exp(a.a_row[v]), y = scale_exp(a.b_row[v]);
+      if (x < NONE) e = x + e0;
+      if (y < NONE) e = min(e, y + e1);
+    } else {
+      const int x = scale_exp(a.h_row[v]);
+      if (x < NONE) e = x + e0;
+    }
+    return e >= NONE ? 0 : e;
+  };
+  // hidden column of column n of B, and which of the two
+  auto hidden = [&](int64_t n) { return a.two ? n / (2 * HB) * HB + n % HB : n; };
+  auto col_top = [&](int64_t n) -> uint32_t {
+    const int64_t c = hidden(n);
+    if (c >= a.f) return 0u;
+    return !a.two ? a.h_col[c] : (n / HB) & 1 ? a.b_col[c] : a.a_col[c];
+  };
+  float fr[2][2], fc[2][8];
+  if constexpr (MODE == ROWS) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int e = row_exp(mw + i * 32 + l32);
+      fr[i][0] = pow2(e - e0), fr[i][1] = pow2(e - (a.two ? e1 : e0));
+    }
+  }
+  if constexpr (MODE == COLS) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) fc[u][k] = pow2(exp_or_0(scale_exp(col_top(n0 + wave * 32 + u * 16 + (k >> 2) * 8 + half * 4 + (k & 3)))));
+  }
+
+  v16f acc[2][4];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+
+  const _Float16 *Ap0 = a.A + ((m0 / 32 + wave * 2) * a.KSA + s0 * KT) * 2 * FRAG + lane * 8, *Ap1 = Ap0 + a.KSA * 2 * FRAG;
+  // a wave brings one of the four row blocks, or two of the eight 16s
+  const _Float16* Bp = a.B + (TURN ? s0 * a.KSB + n0 / 16 + wave * 2 : (n0 / 32 + wave) * a.KSB + s0 * KT) * 2 * FRAG + lane * 8;
+  const int64_t b_step = (TURN ? a.KSB : KT) * 2 * FRAG;
+  v8h ra[2][KT][2][2], rb[KT * 2];    // [stage in turn][step][row block][plane]
+  auto fetch = [&](int to) {          // of the stage that the pointers have come to
+#pragma unroll
+    for (int u = 0; u < KT * 2; ++u) rb[u] = *reinterpret_cast<const v8h*>(Bp + u * FRAG);
+#pragma unroll
+    for (int u = 0; u < KT; ++u)
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        ra[to][u][0][p] = *reinterpret_cast<const v8h*>(Ap0 + (u * 2 + p) * FRAG);
+        ra[to][u][1][p] = *reinterpret_cast<const v8h*>(Ap1 + (u * 2 + p) * FRAG);
+      }
+    Ap0 += KT * 2 * FRAG, Ap1 += KT * 2 * FRAG, Bp += b_step;
+  };
+  auto stash = [&](int to) {
+    if constexpr (MODE == COLS) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) split8(rb[u * 2], rb[u * 2 + 1], [&](int t) { return fc[u][t]; });
+    }
+#pragma unroll
+    for (int u = 0; u < KT * 2; ++u)
+      *reinterpret_cast<v8h*>(Bs + to * STAGE + (TURN ? ((wave * 4 + u) * 2 + half) * TURN_HALF + l32 * 8 : (wave * KT * 2 + u) * FRAG + lane * 8)) = rb[u];
+  };
+  auto read_b = [&](v8h* b, int cur, int k) {          // k: step * 4 + row block
+    if (TURN) {
+      const int i = lane & 15, sixteen = (k & 3) * 2 + ((lane >> 4) & 1);
+      const _Float16* f = Bs + cur * STAGE + (sixteen * 4 + (i & 1)) * TURN_HALF + ((k >> 2) * 16 + half * 4 + (i >> 2)) * 8 + ((i >> 1) & 1) * 4;
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        const v4h lo = turned(f + p * 2 * TURN_HALF), hi = turned(f + p * 2 * TURN_HALF + 64);
+        b[p] = v8h{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      }
+      return;
+    }
+    const _Float16* f = Bs + cur * STAGE + ((k & 3) * KT * 2 + (k >> 2) * 2) * FRAG + lane * 8;
+    b[0] = *reinterpret_cast<const v8h*>(f);
+    b[1] = *reinterpret_cast<const v8h*>(f + FRAG);
+  };
+  // (Loads have no condition, so that waits count only the loads that they wait for: the last stage fetches itself again.  The barriers to scheduling
+  // keep them where they stand; they would be moved down to where they are used.)  cur is also which half of a hidden block [gate, up] the stage is.
+  auto stage = [&](int cur, bool more) {
+    if (!more) Ap0 -= KT * 2 * FRAG, Ap1 -= KT * 2 * FRAG, Bp -= b_step;
+    v8h b[2][2];
+    read_b(b[0], cur, 0);
+    fetch(cur ^ 1);
+#pragma unroll
+    for (int k = 0; k < 4 * KT; ++k) {
+      v8h (&x)[2][2] = ra[cur][k >> 2];
+      const v8h (&y)[2] = b[k & 1];
+      if (MODE == ROWS && (k & 3) == 0) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) split8(x[i][0], x[i][1], [&](int) { return fr[i][cur]; });
+      }
+      if (k + 1 < 4 * KT) read_b(b[(k + 1) & 1], cur, k + 1);
+      __builtin_amdgcn_sched_barrier(0);
+      const int j = k & 3;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][1], y[0], acc[i][j], 0, 0, 0);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][0], y[1], acc[i][j], 0, 0, 0);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][0], y[0], acc[i][j], 0, 0, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    stash(cur ^ 1);
+    __syncthreads();
+  };
+  if (todo > 0) {
+    fetch(0);
+    stash(0);
+    __syncthreads();
+    do {
+      stage(0, true);
+      stage(1, --todo > 0);
+    } while (todo > 0);
+  }
+
+  // lane l32 + 32 half of a 32 x 32 tile has column l32 and the rows 8 (e / 4) + 4 half + e % 4
+  if constexpr (MODE == ROWS || MODE == COLS) {
+#pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int64_t m = m0 + ty * 4 + i, n = n0 + tx * 4 + j;
-      if (m >= p.M || n >= p.N) continue;
-      float* c = p.C + m * p.cm + n * p.cn;
-      *c = p.add ? *c + acc[i][j] : acc[i][j];
+      const int64_t n = n0 + j * 32 + l32, c = MODE == COLS ? hidden(n) : n;
+      const Out& o = a.out[MODE == COLS && a.two ? j & 1 : 0];
+      if (!o.p || c >= a.n_end) continue;
+      const int en = MODE == COLS ? exp_or_0(scale_exp(col_top(n))) : 0;
+      float* at = o.p + split * o.split_part + c * o.ns;
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int64_t m = mw + i * 32 + k * 8 + half * 4;
+          V4 x;
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            x[e] = m + e < a.m_end ? __builtin_amdgcn_ldexpf(acc[i][j][k * 4 + e], -(MODE == COLS ? exp_or_0(scale_exp(a.m_top[m + e])) + en : row_exp(m + e))) : 0.f;
+          float* to = at + m * o.ms;
+          if (o.ms == 1 && m + 4 <= a.m_end) {
+            if (a.add) x += *reinterpret_cast<const V4u*>(to);
+            *reinterpret_cast<V4u*>(to) = x;
+            continue;
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (m + e < a.m_end) to[e * o.ms] = a.add ? to[e * o.ms] + x[e] : x[e];
+        }
     }
-}
-
-// H = act(A) * B; with dA, dB (G lies in dB): the gradients too.
-__global__ void __launch_bounds__(256) k_ffn_gate(int act, const float* A, int64_t lda, const float* B, int64_t ldb, int64_t n, int64_t f, float* H, float* dA, float* dB) {
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n * f; i += (int64_t)gridDim.x * 256) {
-    const int64_t r = i / f, c = i - r * f;
-    const float a = A[r * lda + c], b = B[r * ldb + c];
-    const Act x = act_of(act, a);
-    H[i] = x.v * b;
-    if (!dA) continue;
-    const float g = dB[i];
-    dA[i] = g * b * x.s;
-    dB[i] = g * x.v;
+    return;
+  }
+  uint32_t* top = reinterpret_cast<uint32_t*>(Bs);      // [wave][which][row]
+  // four values of hidden columns c .. c + 3 to a row of gate or up
+  auto put4 = [&](float* p, int64_t c, V4 x) {
+    if (c + 4 <= a.f) {
+      *reinterpret_cast<V4*>(p + c) = x;
+      return;
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+      if (c + k < a.f) p[c + k] = x[k];
+  };
+  auto get4 = [&](const float* p, int64_t c) {
+    if (c + 4 <= a.f) return *reinterpret_cast<const V4*>(p + c);
+    V4 x{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+      if (c + k < a.f) x[k] = p[c + k];
+    return x;
+  };
+  // four values of a row, in the order of fragments: the k-th four of 16 columns by half
+  auto put_frag = [&](float* p, int64_t KS, int64_t row_block, int64_t step, int k, V4 x) {
+    *reinterpret_cast<V4*>(p + ((row_block * KS + step) * 2 + k) * (FRAG / 2) + lane * 4) = x;
+  };
+  if constexpr (MODE == PROJECT) {
+    const int64_t c0 = mw / 2;                          // the wave's 32 hidden columns
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int64_t v = n0 + j * 32 + l32;
+      const bool there = v < a.n;
+      const int ex = exp_or_0(scale_exp(there ? a.rows_in[v] : 0u));
+      uint32_t m = 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int64_t c = c0 + k * 8 + half * 4;
+        V4 x, y, h;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          x[e] = __builtin_amdgcn_ldexpf(acc[0][j][k * 4 + e], -(ex + e0)), y[e] = __builtin_amdgcn_ldexpf(acc[1][j][k * 4 + e], -(ex + e1));
+          h[e] = there ? act_of(a.act, x[e]).v * y[e] : 0.f;
+          m = max(m, size_bits(h[e]));
+        }
+        if (a.gate && there) put4(a.gate + v * a.ld_gate, c, x), put4(a.up + v * a.ld_up, c, y);
+        if (a.H) put_frag(a.H, a.KSH, n0 / 32 + j, c0 / 16 + (k >> 1), k & 1, h);
+      }
+      m = max(m, (uint32_t)__shfl_xor((int)m, 32, 64));
+      if (half == 0) top[wave * TN + j * 32 + l32] = m;
+    }
+    if (!a.H) return;
+    __syncthreads();
+    if (tid < TN && n0 + tid < a.n) raise(a.h_row + n0 + tid, max(max(top[tid], top[TN + tid]), max(top[2 * TN + tid], top[3 * TN + tid])));
+  }
+  if constexpr (MODE == BACK) {
+    uint32_t ma[4] = {}, mb[4] = {};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int64_t c0 = mw + i * 32;
+      uint32_t ch[16] = {}, ca[16] = {}, cb[16] = {};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int64_t v = n0 + j * 32 + l32;
+        const bool there = v < a.n;
+        const int64_t row = there ? v : a.n - 1;
+        const int ey = exp_or_0(scale_exp(there ? a.rows_in[v] : 0u));
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int64_t c = c0 + k * 8 + half * 4;
+          const V4 x = get4(a.gate + row * a.ld_gate, c), y = get4(a.up + row * a.ld_up, c);
+          V4 h, da, db;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float gr = __builtin_amdgcn_ldexpf(acc[i][j][k * 4 + e], -(ey + e0));
+            const Act s = act_of(a.act, x[e]);
+            const bool in = there && c + e < a.f;
+            h[e] = in ? s.v * y[e] : 0.f;
+            da[e] = in ? gr * y[e] * s.s : 0.f;
+            db[e] = in ? gr * s.v : 0.f;
+            ch[k * 4 + e] = max(ch[k * 4 + e], size_bits(h[e]));
+            ca[k * 4 + e] = max(ca[k * 4 + e], size_bits(da[e]));
+            cb[k * 4 + e] = max(cb[k * 4 + e], size_bits(db[e]));
+            ma[j] = max(ma[j], size_bits(da[e]));
+            mb[j] = max(mb[j], size_bits(db[e]));
+          }
+          const int64_t step = c0 / 16 + (k >> 1);
+          put_frag(a.H, a.KSH, n0 / 32 + j, step, k & 1, h);
+          put_frag(a.D, a.KSD, n0 / 32 + j, c0 / 8 + (k >> 1), k & 1, da);
+          put_frag(a.D, a.KSD, n0 / 32 + j, c0 / 8 + 2 + (k >> 1), k & 1, db);
+        }
+      }
+      const int e = l32 >> 1;
+      const int64_t c = c0 + (e >> 2) * 8 + half * 4 + (e & 3);
+      const uint32_t th = max_over_32(ch), ta = max_over_32(ca), tb = max_over_32(cb);
+      if (!(l32 & 1) && c < a.f) raise(a.h_col + c, th), raise(a.a_col + c, ta), raise(a.b_col + c, tb);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t x = max(ma[j], (uint32_t)__shfl_xor((int)ma[j], 32, 64)), y = max(mb[j], (uint32_t)__shfl_xor((int)mb[j], 32, 64));
+      top[(wave * 2 + half) * TN + j * 32 + l32] = half ? y : x;
+    }
+    __syncthreads();
+    const int which = tid / TN, r = tid % TN;
+    if (n0 + r < a.n) {
+      const uint32_t m = max(max(top[which * TN + r], top[(2 + which) * TN + r]), max(top[(4 + which) * TN + r], top[(6 + which) * TN + r]));
+      raise((which ? a.b_row : a.a_row) + n0 + r, m);
+    }
   }
 }
 
+// What products left in parts, added up in their order: out [rows x cols] (+)= the sum of `parts` blocks of [rows x pitch].
+struct Join {
+  const float* sums;
+  int64_t part, pitch, rows, cols;
+  int parts, add;
+  float* out;
+  int64_t ld;
+  unsigned blocks;
+};
+struct Joins {
+  Join join[3];
+  int n;
+};
+__global__ void __launch_bounds__(256) k_ffn_join(Joins joins) {
+  unsigned block = blockIdx.x;
+  int k = 0;
+  while (block >= joins.join[k].blocks) block -= joins.join[k++].blocks;
+  const Join& a = joins.join[k];
+  const int64_t nv = a.pitch / 4, i = (int64_t)block * 256 + threadIdx.x, r = i / nv, c = (i - r * nv) * 4;
+  if (r >= a.rows || c >= a.cols) return;
+  V4 s{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+  for (int p = 0; p < a.parts; ++p) s += *reinterpret_cast<const V4*>(a.sums + p * a.part + r * a.pitch + c);
+  float* to = a.out + r * a.ld + c;
+  if (c + 4 <= a.cols) {
+    if (a.add) s += *reinterpret_cast<const V4u*>(to);
+    *reinterpret_cast<V4u*>(to) = s;
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 3; ++e)
+    if (c + e < a.cols) to[e] = a.add ? to[e] + s[e] : s[e];
+}
+
+// ---------------------------------------------------------------- plan
+
+constexpr size_t FFN_BYTES = (size_t)4 << 30, FFN_LEAN = (size_t)64 << 20;     // of what a piece's rows take
+constexpr int64_t SLOTS = 512;                     // blocks that run together: two a CU
+constexpr int64_t LEAST_PAIRS = 4;                 // of a part of a reduction
+
+int parts_of(int64_t tiles, int64_t pairs) { return (int)std::max<int64_t>(1, std::min<int64_t>({SLOTS / tiles, pairs / LEAST_PAIRS, 64})); }
+
+// One of ht_ffn_fwd and ht_ffn_bwd
 struct Ffn {
   ht_ctx* ctx;
   const ht_ffn_desc* D;
   const ht_tensor *X, *Wg, *Wu, *Wd;
-  bool in_out() const { return D->w_form == HT_W_IN_OUT; }
-  int product(int64_t M, int64_t N, int64_t K, const float* A, int64_t am, int64_t ak, const float* B, int64_t bk, int64_t bn, float* C, int64_t cm, int64_t cn, int add) const {
-    if (M == 0 || N == 0) return HT_OK;
-    k_ffn_product<<<dim3((unsigned)ceil_div64(M, 64), (unsigned)ceil_div64(N, 64)), 256, 0, ctx->stream>>>(Product{A, B, C, am, ak, bk, bn, cm, cn, M, N, K, add});
+  const ht_tensor *gate = nullptr, *up = nullptr;
+  const ht_tensor *Y = nullptr;                                            // forward
+  const ht_tensor *dY = nullptr, *dX = nullptr, *dWg = nullptr, *dWu = nullptr, *dWd = nullptr;
+
+  int launch(int mode, Args& a) const {
+    const int64_t blocks = up_to(a.mt * a.nt * a.splits, 8);
+    if (blocks >= (1 << 24)) return ht_set_err(ctx, HT_ESHAPE, "ffn: %lld tiles in one product", (long long)blocks);
+    const unsigned grid = (unsigned)blocks;
+    if (mode == PROJECT) k_ffn_split<PROJECT><<<grid, 256, 0, ctx->stream>>>(a);
+    else if (mode == BACK) k_ffn_split<BACK><<<grid, 256, 0, ctx->stream>>>(a);
+    else if (mode == ROWS) k_ffn_split<ROWS><<<grid, 256, 0, ctx->stream>>>(a);
+    else k_ffn_split<COLS><<<grid, 256, 0, ctx->stream>>>(a);
     HT_LAUNCH_CHECK(ctx);
     return HT_OK;
   }
-  // strides of a weight's inputs and outputs
-  int64_t by_in(const ht_tensor* W) const { return in_out() ? W->ld : 1; }
-  int64_t by_out(const ht_tensor* W) const { return in_out() ? 1 : W->ld; }
-  int project(float* A, int64_t lda, float* B, int64_t ldb) const {
-    HT_TRY(product(X->rows, D->d_hidden, D->d_in, X->ptr, X->ld, 1, Wg->ptr, by_in(Wg), by_out(Wg), A, lda, 1, 0));
-    return product(X->rows, D->d_hidden, D->d_in, X->ptr, X->ld, 1, Wu->ptr, by_in(Wu), by_out(Wu), B, ldb, 1, 0);
-  }
-  int gate(const float* A, int64_t lda, const float* B, int64_t ldb, float* H, float* dA, float* dB) const {
-    const int64_t n = X->rows * D->d_hidden;
-    if (n == 0) return HT_OK;
-    k_ffn_gate<<<(unsigned)std::min<int64_t>(ceil_div64(n, 256), 65536), 256, 0, ctx->stream>>>(D->act, A, lda, B, ldb, X->rows, D->d_hidden, H, dA, dB);
-    HT_LAUNCH_CHECK(ctx);
-    return HT_OK;
-  }
-  int fwd(ht_tensor* Y, ht_tensor* keep_a, ht_tensor* keep_b) const {
-    const int64_t n = X->rows, f = D->d_hidden, e = D->d_out;
-    OpsBlock m;
-    const auto a = m.add<float>(keep_a ? 0 : n * f), b = m.add<float>(keep_b ? 0 : n * f), h = m.add<float>(n * f);
-    HT_TRY(m.take(ctx));
-    float *A = keep_a ? keep_a->ptr : m.at(a), *B = keep_b ? keep_b->ptr : m.at(b);
-    const int64_t lda = keep_a ? keep_a->ld : f, ldb = keep_b ? keep_b->ld : f;
-    HT_TRY(project(A, lda, B, ldb));
-    HT_TRY(gate(A, lda, B, ldb, m.at(h), nullptr, nullptr));
-    return product(n, e, f, m.at(h), f, 1, Wd->ptr, by_in(Wd), by_out(Wd), Y->ptr, Y->ld, 1, D->accumulate);
-  }
-  int bwd(const ht_tensor* kept_a, const ht_tensor* kept_b, const ht_tensor* dY, ht_tensor* dX, ht_tensor* dWg, ht_tensor* dWu, ht_tensor* dWd) const {
-    const int64_t n = X->rows, d = D->d_in, f = D->d_hidden, e = D->d_out;
-    OpsBlock m;
-    const auto a = m.add<float>(kept_a ? 0 : n * f), b = m.add<float>(kept_b ? 0 : n * f), h = m.add<float>(n * f), da = m.add<float>(n * f), db = m.add<float>(n * f);
-    HT_TRY(m.take(ctx));
-    if (!kept_a) HT_TRY(project(m.at(a), f, m.at(b), f));
-    HT_TRY(product(n, f, e, dY->ptr, dY->ld, 1, Wd->ptr, by_out(Wd), by_in(Wd), m.at(db), f, 1, 0));
-    HT_TRY(gate(kept_a ? kept_a->ptr : m.at(a), kept_a ? kept_a->ld : f, kept_b ? kept_b->ptr : m.at(b), kept_b ? kept_b->ld : f, m.at(h), m.at(da), m.at(db)));
-    if (dX) {
-      HT_TRY(product(n, d, f, m.at(da), f, 1, Wg->ptr, by_out(Wg), by_in(Wg), dX->ptr, dX->ld, 1, D->accumulate));
-      HT_TRY(product(n, d, f, m.at(db), f, 1, Wu->ptr, by_out(Wu), by_in(Wu), dX->ptr, dX->ld, 1, 1));
+  int join(Joins& j) const {
+    unsigned grid = 0;
+    for (int k = 0; k < j.n; ++k) {
+      Join& a = j.join[k];
+      a.blocks = (unsigned)ceil_div64(a.rows * (a.pitch / 4), 256);
+      grid += a.blocks;
     }
-    const int add = D->accumulate_dW;
-    if (dWg) HT_TRY(product(d, f, n, X->ptr, 1, X->ld, m.at(da), f, 1, dWg->ptr, by_in(dWg), by_out(dWg), add));
-    if (dWu) HT_TRY(product(d, f, n, X->ptr, 1, X->ld, m.at(db), f, 1, dWu->ptr, by_in(dWu), by_out(dWu), add));
-    if (dWd) HT_TRY(product(f, e, n, m.at(h), 1, f, dY->ptr, dY->ld, 1, dWd->ptr, by_in(dWd), by_out(dWd), add));
+    if (grid == 0) return HT_OK;
+    k_ffn_join<<<grid, 256, 0, ctx->stream>>>(j);
+    HT_LAUNCH_CHECK(ctx);
     return HT_OK;
+  }
+
+  int run(size_t bytes) const {
+    const bool bwd = dY != nullptr, in_out = D->w_form == HT_W_IN_OUT;
+    const int64_t n = X->rows, d = D->d_in, f = D->d_hidden, e = D->d_out;
+    hipStream_t st = ctx->stream;
+    const int64_t fp = up_to(f, 256), dp = up_to(d, TM), ep = up_to(e, TM), KSd = up_to(d, TN) / 16, KSe = up_to(e, TN) / 16, KSH = fp / 16, KSD = fp / 8;
+    const bool remake = bwd && !gate, d_w = dWg || dWu;
+    // a row's share
+    const int64_t own = 4 * (dp + (bwd && d_w ? dp : 0) + (bwd ? ep : 0) + (bwd && dWd ? ep : 0) + fp * (bwd ? 3 : 1) + (remake ? 2 * fp : 0));
+    const int64_t Rp = std::max<int64_t>(TM, std::min<int64_t>((int64_t)bytes / own / TM * TM, up_to(n, TM)));
+    const int64_t KSR = Rp / 16, pieces = ceil_div64(n, Rp);
+    // tiles of the products, and parts of their reductions
+    const int64_t mt = Rp / TM, nte = up_to(e, TN) / TN, ntd = up_to(d, TN) / TN, ntD = ceil_div64(f, 64), ntH = ceil_div64(f, TN);
+    const int64_t pairs_f = ceil_div64(f, PAIR), pairs_2f = ceil_div64(f, HB), pairs_r = ceil_div64(std::min(n, Rp), PAIR);
+    const int sy = parts_of(mt * nte, pairs_f), sx = parts_of(mt * ntd, pairs_2f), sD = parts_of(dp / TM * ntD, pairs_r), sH = parts_of(ep / TM * ntH, pairs_r);
+    const int64_t e4 = up_to(e, 4), d4 = up_to(d, 4), f4 = up_to(f, 4);
+    // a weight's gradient as it lies: rows and pitch of its parts
+    const int64_t wr = in_out ? d : f, wp = in_out ? f4 : d4, vr = in_out ? f : e, vp = in_out ? e4 : f4;
+
+    OpsBlock m;
+    const int64_t n_top = 4 + 5 * Rp + dp + ep + 3 * fp;
+    const auto top = m.add<uint32_t>(n_top);
+    const auto W2 = m.add<_Float16>(2 * fp * KSd * 32), Wf = m.add<_Float16>(fp * KSe * 32);
+    const auto Xr = m.add<_Float16>(Rp * KSd * 32);
+    const auto Xt = m.add<_Float16>(d_w ? dp * KSR * 32 : 0);
+    const auto Gr = m.add<_Float16>(bwd ? Rp * KSe * 32 : 0);
+    const auto Gt = m.add<_Float16>(dWd ? ep * KSR * 32 : 0);
+    const auto A = m.add<float>(remake ? Rp * f4 : 0), B = m.add<float>(remake ? Rp * f4 : 0);
+    const auto H = m.add<float>(Rp * fp), Df = m.add<float>(bwd ? Rp * fp * 2 : 0);
+    const auto sums_y = m.add<float>(!bwd && sy > 1 ? sy * Rp * e4 : 0), sums_x = m.add<float>(dX && sx > 1 ? sx * Rp * d4 : 0);
+    const auto sums_D = m.add<float>(d_w && sD > 1 ? sD * 2 * wr * wp : 0), sums_H = m.add<float>(dWd && sH > 1 ? sH * vr * vp : 0);
+    HT_TRY(bytes > FFN_LEAN ? m.take_if_room(ctx) : m.take(ctx));
+
+    uint32_t *t_g = m.at(top), *t_u = t_g + 1, *t_d = t_g + 2, *t_x = t_g + 4, *t_y = t_x + Rp, *t_h = t_y + Rp, *t_a = t_h + Rp, *t_b = t_a + Rp, *t_xc = t_b + Rp, *t_yc = t_xc + dp,
+             *t_hc = t_yc + ep, *t_ac = t_hc + fp, *t_bc = t_ac + fp;
+    for (int64_t k = 0; k < pieces; ++k) {
+      const int64_t r0 = k * Rp, rows = std::min(Rp, n - r0);
+      HT_TRY(ht_fill_zero(ctx, st, k ? t_x : t_g, (size_t)(k ? n_top - 4 : n_top) * 4));
+      Tops tops{};
+      Packs packs{};
+      unsigned tb = 0, pb = 0;
+      auto operand = [&](const float* p, int64_t ld, int64_t r, int64_t c, uint32_t* rm, uint32_t* cm, uint32_t* all, _Float16* R, int64_t KS, _Float16* T, int64_t KS_t, int mul,
+                         int add, int64_t row_tile, int64_t col_tile) {
+        Top& t = tops.top[tops.n++];
+        t = Top{p, ld, r, c, rm, cm, all, (unsigned)(ceil_div64(r, TOP_ROWS) * ceil_div64(c, 256))};
+        tb += t.blocks;
+        Pack& q = packs.pack[packs.n++];
+        q = Pack{p, ld, r, c, rm, cm, all, R, T, KS, KS_t, mul, add, (unsigned)(up_to(r, row_tile) / 64), (unsigned)(up_to(c, col_tile) / 64)};
+        pb += q.row_tiles * q.col_tiles;
+      };
+      operand(X->ptr + r0 * X->ld, X->ld, rows, d, t_x, d_w ? t_xc : nullptr, nullptr, m.at(Xr), KSd, d_w ? m.at(Xt) : nullptr, KSR, 1, 0, TM, d_w ? TM : TN);
+      if (bwd)
+        operand(dY->ptr + r0 * dY->ld, dY->ld, rows, e, t_y, dWd ? t_yc : nullptr, nullptr, m.at(Gr), KSe, dWd ? m.at(Gt) : nullptr, KSR, 1, 0, TM, dWd ? TM : TN);
+      if (k == 0) {
+        // by hidden columns: the rows of an OUT_IN Wg, the columns of an IN_OUT one
+        const ht_tensor* w[2] = {Wg, Wu};
+        for (int i = 0; i < 2; ++i)
+          operand(w[i]->ptr, w[i]->ld, w[i]->rows, w[i]->cols, nullptr, nullptr, t_g + i, in_out ? nullptr : m.at(W2), KSd, in_out ? m.at(W2) : nullptr, KSd, 2, i, in_out ? TN : TM,
+                  in_out ? TM : TN);
+        operand(Wd->ptr, Wd->ld, Wd->rows, Wd->cols, nullptr, nullptr, t_d, in_out ? m.at(Wf) : nullptr, KSe, in_out ? nullptr : m.at(Wf), KSe, 1, 0, in_out ? TM : TN,
+                in_out ? TN : TM);
+      }
+      k_ffn_top<<<tb, 256, 0, st>>>(tops);
+      HT_LAUNCH_CHECK(ctx);
+      k_ffn_pack<<<pb, 256, 0, st>>>(packs);
+      HT_LAUNCH_CHECK(ctx);
+
+      Args base{};
+      base.act = D->act, base.n = rows, base.f = f, base.splits = 1;
+      base.h_row = t_h, base.a_row = t_a, base.b_row = t_b, base.h_col = t_hc, base.a_col = t_ac, base.b_col = t_bc;
+      base.KSH = KSH, base.KSD = KSD;
+      base.gate = gate ? gate->ptr + r0 * gate->ld : remake ? m.at(A) : nullptr, base.ld_gate = gate ? gate->ld : f4;
+      base.up = up ? up->ptr + r0 * up->ld : remake ? m.at(B) : nullptr, base.ld_up = up ? up->ld : f4;
+      const int64_t row_tiles = ceil_div64(rows, TN);
+      if (!bwd || remake) {
+        Args a = base;
+        a.A = m.at(W2), a.KSA = KSd, a.B = m.at(Xr), a.KSB = KSd;
+        a.mt = ceil_div64(f, TN), a.nt = row_tiles, a.pairs = ceil_div64(d, PAIR);
+        a.w0 = t_g, a.w1 = t_u, a.rows_in = t_x;
+        a.H = bwd ? nullptr : m.at(H);
+        HT_TRY(launch(PROJECT, a));
+      }
+      if (bwd) {
+        Args a = base;
+        a.A = m.at(Wf), a.KSA = KSe, a.B = m.at(Gr), a.KSB = KSe;
+        a.mt = ceil_div64(f, TM), a.nt = row_tiles, a.pairs = ceil_div64(e, PAIR);
+        a.w0 = t_d, a.rows_in = t_y;
+        a.H = m.at(H), a.D = m.at(Df);
+        HT_TRY(launch(BACK, a));
+      }
+      Joins j{};
+      auto by_rows = [&](const ht_tensor* to, const float* P, int64_t KSP, bool two, const _Float16* W, int64_t KSW, const uint32_t* w0, const uint32_t* w1, int64_t cols, int64_t nt,
+                         int64_t pairs, int splits, float* sums, int64_t pitch) -> int {
+        Args a = base;
+        a.A = (const _Float16*)P, a.KSA = KSP, a.B = W, a.KSB = KSW;
+        a.mt = ceil_div64(rows, TM), a.nt = nt, a.pairs = pairs, a.splits = splits, a.two = two, a.w0 = w0, a.w1 = w1;
+        a.m_end = rows, a.n_end = cols;
+        float* out = to->ptr + r0 * to->ld;
+        a.out[0] = splits > 1 ? Out{sums, pitch, 1, Rp * pitch} : Out{out, to->ld, 1, 0};
+        a.add = splits == 1 && D->accumulate;
+        if (splits > 1) j.join[j.n++] = Join{sums, Rp * pitch, pitch, rows, cols, splits, D->accumulate, out, to->ld, 0};
+        return launch(ROWS, a);
+      };
+      if (Y) HT_TRY(by_rows(Y, m.at(H), KSH, false, m.at(Wf), KSe, t_d, nullptr, e, nte, pairs_f, sy, m.at(sums_y), e4));
+      if (dX) HT_TRY(by_rows(dX, m.at(Df), KSD, true, m.at(W2), KSd, t_g, t_u, d, ntd, pairs_2f, sx, m.at(sums_x), d4));
+      HT_TRY(join(j));
+      auto by_cols = [&](const _Float16* At, const uint32_t* m_top, int64_t m_end, const float* P, int64_t KSP, bool two, int64_t tiles_m, int64_t nt, int splits, float* sums,
+                         int64_t r, int64_t pitch, const ht_tensor* o0, const ht_tensor* o1, bool m_is_row) -> int {
+        Args a = base;
+        a.A = At, a.KSA = KSR, a.B = (const _Float16*)P, a.KSB = KSP;
+        a.mt = tiles_m, a.nt = nt, a.pairs = ceil_div64(rows, PAIR), a.splits = splits, a.two = two, a.m_top = m_top;
+        a.m_end = m_end, a.n_end = f;
+        const ht_tensor* o[2] = {o0, o1};
+        for (int i = 0; i < 2; ++i) {
+          if (!o[i]) continue;
+          const int64_t ld = splits > 1 ? pitch : o[i]->ld;
+          a.out[i] = Out{splits > 1 ? sums + i * r * pitch : o[i]->ptr, m_is_row ? ld : 1, m_is_row ? 1 : ld, splits > 1 ? (two ? 2 : 1) * r * pitch : 0};
+        }
+        a.add = k > 0 || (splits == 1 && D->accumulate_dW);
+        return launch(COLS, a);
+      };
+      if (d_w) HT_TRY(by_cols(m.at(Xt), t_xc, d, m.at(Df), KSD, true, dp / TM, ntD, sD, m.at(sums_D), wr, wp, dWg, dWu, in_out));
+      if (dWd) HT_TRY(by_cols(m.at(Gt), t_yc, e, m.at(H), KSH, false, ep / TM, ntH, sH, m.at(sums_H), vr, vp, dWd, nullptr, !in_out));
+      if (k + 1 < pieces) continue;
+      Joins w{};
+      const ht_tensor* dw[2] = {dWg, dWu};
+      for (int i = 0; i < 2; ++i)
+        if (dw[i] && sD > 1) w.join[w.n++] = Join{m.at(sums_D) + i * wr * wp, 2 * wr * wp, wp, dw[i]->rows, dw[i]->cols, sD, D->accumulate_dW, dw[i]->ptr, dw[i]->ld, 0};
+      if (dWd && sH > 1) w.join[w.n++] = Join{m.at(sums_H), vr * vp, vp, dWd->rows, dWd->cols, sH, D->accumulate_dW, dWd->ptr, dWd->ld, 0};
+      HT_TRY(join(w));
+    }
+    return HT_OK;
+  }
+  int call() const {
+    if (X->rows == 0) {                // nothing to add up
+      Joins w{};
+      for (const ht_tensor* t : {dWg, dWu, dWd})
+        if (t && !D->accumulate_dW) w.join[w.n++] = Join{nullptr, 0, up_to(t->cols, 4), t->rows, t->cols, 0, 0, t->ptr, t->ld, 0};
+      return join(w);
+    }
+    const int rc = run(FFN_BYTES);
+    return rc == HT_ENOMEM ? run(FFN_LEAN) : rc;      // (nothing has been launched by a call that is refused memory)
   }
 };
 
@@ -175,8 +808,9 @@ extern "C" int ht_ffn_fwd(ht_ctx* ctx, const ht_ffn_desc* desc, const ht_tensor*
   HT_TRY(check_block(ctx, "ht_ffn_fwd", desc, X, Wg, Wu, Wd, gate, up, Y));
   HT_TRY(check_apart(ctx, "ht_ffn_fwd", {{X, "X"}, {Wg, "Wg"}, {Wu, "Wu"}, {Wd, "Wd"}}, {{Y, "Y"}, {gate, "gate"}, {up, "up"}}));
   HT_HIP(ctx, hipSetDevice(ctx->device));
-  const Ffn op{ctx, desc, X, Wg, Wu, Wd};
-  return ht_with_room(ctx, [&]() -> int { return op.fwd(Y, gate, up); });
+  Ffn op{ctx, desc, X, Wg, Wu, Wd, gate, up};
+  op.Y = Y;
+  return ht_with_room(ctx, [&]() -> int { return op.call(); });
 }
 
 extern "C" int ht_ffn_bwd(ht_ctx* ctx, const ht_ffn_desc* desc, const ht_tensor* X, const ht_tensor* Wg, const ht_tensor* Wu, const ht_tensor* Wd, const ht_tensor* gate,
@@ -190,6 +824,8 @@ extern "C" int ht_ffn_bwd(ht_ctx* ctx, const ht_ffn_desc* desc, const ht_tensor*
   HT_TRY(check_apart(ctx, "ht_ffn_bwd", {{X, "X"}, {Wg, "Wg"}, {Wu, "Wu"}, {Wd, "Wd"}, {gate, "gate"}, {up, "up"}, {dY, "dY"}},
                      {{dX, "dX"}, {dWg, "dWg"}, {dWu, "dWu"}, {dWd, "dWd"}}));
   HT_HIP(ctx, hipSetDevice(ctx->device));
-  const Ffn op{ctx, desc, X, Wg, Wu, Wd};
-  return ht_with_room(ctx, [&]() -> int { return op.bwd(gate, up, dY, dX, dWg, dWu, dWd); });
+  if (!dX && !dWg && !dWu && !dWd) return HT_OK;
+  Ffn op{ctx, desc, X, Wg, Wu, Wd, gate, up};
+  op.dY = dY, op.dX = dX, op.dWg = dWg, op.dWu = dWu, op.dWd = dWd;
+  return ht_with_room(ctx, [&]() -> int { return op.call(); });
 }
