@@ -14,25 +14,30 @@ namespace {
 
 constexpr int HB = 32;                 // hidden columns of a block: [gate, up] of interleaved operands
 
-// act(a) and its derivative.  exp(-|a|) gives s(a) and s(-a) = 1 - s(a) without cancellation.
+// act(a) and its derivative.  Kernels are made for two kinds: s(u) with u = a (k1 + k3 a^2), times a but for the sigmoid itself, and the others.
+enum { LOGISTIC, OTHERS };
+struct Gate {
+  int act;
+  float k1, k3;
+  int alone;                           // s(u) itself
+};
 struct Act {
   float v, s;
 };
-__device__ __forceinline__ Act act_of(int act, float a) {
-  if (act == HT_GATE_RELU) return {a < 0.f ? 0.f : a, a > 0.f ? 1.f : a * 0.f};      // (NaN stays NaN)
-  if (act == HT_GATE_GELU) {
-    const float phi = 0.5f * erfcf(-a * 0.70710678118654752f);
-    return {a * phi, fmaf(a * 0.39894228040143268f, expf(-0.5f * a * a), phi)};
+template <int KIND>
+__device__ __forceinline__ Act act_of(const Gate& g, float a) {
+  constexpr float LOG2E = 1.44269504088896340736f;
+  if constexpr (KIND == LOGISTIC) {
+    // exp(-|u|) gives s(u) and s(-u) = 1 - s(u) without cancellation
+    const float q = fminf(a * a, 1e30f), u = a * fmaf(g.k3, q, g.k1), du = fmaf(3.f * g.k3, q, g.k1);
+    const float e = __builtin_amdgcn_exp2f(-fabsf(u) * LOG2E), hi = __builtin_amdgcn_rcpf(1.f + e), lo = e * hi;
+    const float s = u >= 0.f ? hi : lo, v = a * s;
+    return g.alone ? Act{s, lo * hi} : Act{v, fmaf(v, (u >= 0.f ? lo : hi) * du, s)};
   }
-  const float k = 1.5957691216057308f;              // 2 sqrt(2 / pi)
-  const float u = act == HT_GATE_GELU_TANH ? k * a * fmaf(0.044715f * a, a, 1.f) : a;
-  const float e = expf(-fabsf(u)), r = 1.f / (1.f + e), hi = r, lo = e * r;
-  const float s = u >= 0.f ? hi : lo, t = u >= 0.f ? lo : hi;
-  if (act == HT_GATE_SIGMOID) return {s, s * t};
-  const float du = act == HT_GATE_GELU_TANH ? k * fmaf(3.f * 0.044715f * a, a, 1.f) : 1.f;
-  return {a * s, fmaf(a * s, t * du, s)};
+  if (g.act == HT_GATE_RELU) return {a < 0.f ? 0.f : a, a > 0.f ? 1.f : a * 0.f};      // (NaN stays NaN)
+  const float phi = 0.5f * erfcf(-a * 0.70710678118654752f);
+  return {a * phi, fmaf(a * 0.39894228040143268f, __builtin_amdgcn_exp2f(a * a * (-0.5f * LOG2E)), phi)};
 }
-
 
 // ---------------------------------------------------------------- scales
 
@@ -190,7 +195,7 @@ __global__ void __launch_bounds__(256) k_ffn_pack(Packs packs) {
 // ---------------------------------------------------------------- products
 
 // PROJECT  A's rows: the interleaved hidden columns, B's the rows of X: A and B of the block, H and its largest values
-// BACK     A's rows: the hidden columns of Wd, B's the rows of dY: G, from that and A and B all of H, dA, dB and their largest values
+// BACK     A's rows: 128 hidden columns of Wd, B's the rows of dY: G, from that and A and B all of H, dA, dB and their largest values
 // ROWS     A: H or [dA dB] by rows, B: a weight turned: Y, dX
 // COLS     A: X or dY by columns, B: [dA dB] or H turned: gradients of weights
 enum { PROJECT, BACK, ROWS, COLS };
@@ -205,7 +210,7 @@ struct Args {
   int64_t mt, nt;                      // tiles
   int64_t pairs;                       // of stages, of the reduction
   int splits;                          // parts of it
-  int act;
+  Gate act;
   int two;                             // an operand is [dA dB]
   // largest values: of the weights (gate or only one, up), of the rows of X or dY; of what is made or read by rows and by columns (H; or dA and dB)
   const uint32_t *w0, *w1, *rows_in;
@@ -221,63 +226,292 @@ struct Args {
   int add;
 };
 
-__device__ __forceinline__ V4 as_floats(v8h x) { return __builtin_bit_cast(V4, x); }
-// Eight values (t = 0 .. 3 and 4 .. 7 where the planes will be), each times its factor
+// Eight values (t = 0 .. 3 and 4 .. 7 where the planes will be), each times its factor, a power of two.  Two instructions a value: the compiler rounds each value twice where it
+// is left to itself (a pair's halves once more for themselves).
 template <class F>
 __device__ __forceinline__ void split8(v8h& p0, v8h& p1, F&& factor) {
-  const V4 x = as_floats(p0), y = as_floats(p1);
-  v8h hi, lo;
-#pragma unroll
-  for (int t = 0; t < 8; ++t) {
-    _Float16 u, v;
-    split2((t < 4 ? x[t & 3] : y[t & 3]) * factor(t), &u, &v);
-    hi[t] = u, lo[t] = v;
-  }
-  p0 = hi, p1 = lo;
-}
-
-// Of eight words a lane (of 16, of which each half of a lane's 32 neighbours keeps one half) ... down to one a lane: the largest of each over l32, word e in the
-// lanes whose bits 4, 3, 2, 1 are e's bits 3, 2, 1, 0.
-__device__ __forceinline__ uint32_t max_over_32(const uint32_t (&x)[16]) {
-  const int l32 = threadIdx.x & 31;
-  uint32_t y[8], z[4], w[2], v;
-#pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    const uint32_t keep = l32 & 16 ? x[k + 8] : x[k], give = l32 & 16 ? x[k] : x[k + 8];
-    y[k] = max(keep, (uint32_t)__shfl_xor((int)give, 16, 64));
-  }
+  typedef uint32_t v4i __attribute__((ext_vector_type(4)));
+  const V4 x = __builtin_bit_cast(V4, p0), y = __builtin_bit_cast(V4, p1);
+  v4i hi, lo;
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    const uint32_t keep = l32 & 8 ? y[k + 4] : y[k], give = l32 & 8 ? y[k] : y[k + 4];
-    z[k] = max(keep, (uint32_t)__shfl_xor((int)give, 8, 64));
+    const float a = k < 2 ? x[2 * k] : y[2 * k - 4], b = k < 2 ? x[2 * k + 1] : y[2 * k - 3], fa = factor(2 * k), fb = factor(2 * k + 1);
+    uint32_t h, l;
+    asm("v_fma_mixlo_f16 %0, %2, %3, 0 op_sel_hi:[0,0,0]\n\t"
+        "v_fma_mixhi_f16 %0, %4, %5, 0 op_sel_hi:[0,0,0]\n\t"
+        "v_fma_mixlo_f16 %1, %2, %3, -%0 op_sel_hi:[0,0,1]\n\t"
+        "v_fma_mixhi_f16 %1, %4, %5, -%0 op_sel:[0,0,1] op_sel_hi:[0,0,1]"
+        : "=&v"(h), "=&v"(l)
+        : "v"(a), "v"(fa), "v"(b), "v"(fb));
+    hi[k] = h, lo[k] = l;
   }
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const uint32_t keep = l32 & 4 ? z[k + 2] : z[k], give = l32 & 4 ? z[k] : z[k + 2];
-    w[k] = max(keep, (uint32_t)__shfl_xor((int)give, 4, 64));
-  }
-  const uint32_t keep = l32 & 2 ? w[1] : w[0], give = l32 & 2 ? w[0] : w[1];
-  v = max(keep, (uint32_t)__shfl_xor((int)give, 2, 64));
-  return max(v, (uint32_t)__shfl_xor((int)v, 1, 64));
+  p0 = __builtin_bit_cast(v8h, hi), p1 = __builtin_bit_cast(v8h, lo);
 }
 
-// C = A B^T of fragments, 256 x 128 a block, 64 x 128 a wave.  A wave reads its own rows of A straight into registers, a stage ahead, and the four
-// waves share B through LDS, which is filled a stage ahead as well; two blocks a CU.
-template <int MODE>
+// The largest of each of four over l32: the e-th in the lanes with l32 / 8 = e.
+__device__ __forceinline__ float max_over_32(const float (&x)[4]) {
+  const bool up16 = threadIdx.x & 16, up8 = threadIdx.x & 8;
+  float y[2], v;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) y[k] = fmaxf(up16 ? x[k + 2] : x[k], __shfl_xor(up16 ? x[k] : x[k + 2], 16, 64));
+  v = fmaxf(up8 ? y[1] : y[0], __shfl_xor(up8 ? y[0] : y[1], 8, 64));
+  for (int o = 4; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+  return v;
+}
+
+// acc += A B^T of fragments: NI row blocks of A a wave, NJ of B, which the four waves of a block share.  A wave reads its own rows of A straight into registers,
+// a stage ahead (FAR) or a step, and B goes through LDS, which is filled a stage ahead.
+//   Ap   the wave's first row block, the lane's place in it; a_rows halfs from one row block to the next
+//   Bp   the tile's first row block (TURN: the tile's first 16 of the reduction's first row block); b_rows from one to the next
+//   in_a(x, i, cur)  what is done to a step's planes of row block i before they are used (cur: the stage's parity), in_b(rb): to what a wave brings of B
+template <bool TURN, bool FAR, int NI, int NJ, class InA, class InB>
+__device__ __forceinline__ void multiply(v16f (&acc)[NI][NJ], const _Float16* Ap, const int64_t a_rows, const _Float16* B, const int64_t b_rows, int todo, _Float16* Bs, InA&& in_a, InB&& in_b) {
+  static_assert(!TURN || NJ == 4, "a stage of a turned operand is 32 x 128");
+  constexpr int STAGE = stage_halfs(TURN), RB = TURN ? 4 : NJ * KT * 2 / 4, AHEAD = FAR ? 2 * KT : 2;
+  static_assert(FAR || KT == 2, "steps take turns");
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, half = lane >> 5;
+  // a wave brings NJ of the fragments (row block, step, plane) of a stage, or two of the eight 16s
+  int64_t b_at[RB];
+#pragma unroll
+  for (int u = 0; u < RB; ++u) {
+    const int q = wave * RB + u;
+    b_at[u] = TURN ? (int64_t)q * FRAG : (int64_t)(q / (KT * 2)) * b_rows + q % (KT * 2) * FRAG;
+  }
+  const _Float16* Bp = B + lane * 8;
+  const int64_t b_step = TURN ? b_rows : KT * 2 * FRAG;
+  v8h ra[AHEAD][NI][2], rb[RB];
+  auto fetch_a = [&](int to) {        // the next step
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+      for (int p = 0; p < 2; ++p) ra[to][i][p] = *reinterpret_cast<const v8h*>(Ap + i * a_rows + p * FRAG);
+    Ap += 2 * FRAG;
+  };
+  auto fetch_b = [&]() {              // the next stage
+#pragma unroll
+    for (int u = 0; u < RB; ++u) rb[u] = *reinterpret_cast<const v8h*>(Bp + b_at[u]);
+    Bp += b_step;
+  };
+  auto stash = [&](int to) {
+    in_b(rb);
+#pragma unroll
+    for (int u = 0; u < RB; ++u)
+      *reinterpret_cast<v8h*>(Bs + to * STAGE + (TURN ? ((wave * 4 + u) * 2 + half) * TURN_HALF + l32 * 8 : (wave * RB + u) * FRAG + lane * 8)) = rb[u];
+  };
+  auto read_b = [&](v8h* b, int cur, int k) {          // k: step * NJ + row block
+    const int u = k / NJ, j = k % NJ;
+    if (TURN) {
+      const int i = lane & 15, sixteen = j * 2 + ((lane >> 4) & 1);
+      const _Float16* f = Bs + cur * STAGE + (sixteen * 4 + (i & 1)) * TURN_HALF + (u * 16 + half * 4 + (i >> 2)) * 8 + ((i >> 1) & 1) * 4;
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        const v4h lo = turned(f + p * 2 * TURN_HALF), hi = turned(f + p * 2 * TURN_HALF + 64);
+        b[p] = v8h{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      }
+      return;
+    }
+    const _Float16* f = Bs + cur * STAGE + (j * KT * 2 + u * 2) * FRAG + lane * 8;
+    b[0] = *reinterpret_cast<const v8h*>(f);
+    b[1] = *reinterpret_cast<const v8h*>(f + FRAG);
+  };
+  // (Loads have no condition, so that waits count only the loads that they wait for: the last stage fetches itself again.  The barriers to scheduling
+  // keep them where they stand; they would be moved down to where they are used.)
+  auto stage = [&](int cur, bool more) {
+    if (!more) Bp -= b_step;
+    if (FAR && !more) Ap -= KT * 2 * FRAG;
+    v8h b[2][2];
+    read_b(b[0], cur, 0);
+    fetch_b();
+    if (FAR) {
+#pragma unroll
+      for (int u = 0; u < KT; ++u) fetch_a((cur ^ 1) * KT + u);
+    }
+#pragma unroll
+    for (int k = 0; k < NJ * KT; ++k) {
+      const int u = k / NJ, j = k % NJ;
+      v8h (&x)[NI][2] = ra[FAR ? cur * KT + u : u];
+      const v8h (&y)[2] = b[k & 1];
+      if (j == 0) {
+        if (!FAR) {
+          if (u == KT - 1 && !more) Ap -= KT * 2 * FRAG;
+          fetch_a(u ^ 1);
+        }
+#pragma unroll
+        for (int i = 0; i < NI; ++i) in_a(x[i], i, cur);
+      }
+      if (k + 1 < NJ * KT) read_b(b[(k + 1) & 1], cur, k + 1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < NI; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][1], y[0], acc[i][j], 0, 0, 0);
+#pragma unroll
+      for (int i = 0; i < NI; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][0], y[1], acc[i][j], 0, 0, 0);
+#pragma unroll
+      for (int i = 0; i < NI; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][0], y[0], acc[i][j], 0, 0, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    stash(cur ^ 1);
+    __syncthreads();
+  };
+  if (todo <= 0) return;
+  fetch_b();
+#pragma unroll
+  for (int u = 0; u < (FAR ? KT : 1); ++u) fetch_a(u);
+  stash(0);
+  __syncthreads();
+  do {
+    stage(0, true);
+    stage(1, --todo > 0);
+  } while (todo > 0);
+}
+
+// Where a block's tile is: each XCD takes a contiguous part of the tiles, eight tiles of A over all of B after eight others.
+struct Tile {
+  int64_t split, m, n;                 // m < 0: none
+  __device__ __forceinline__ Tile(int64_t mt, int64_t nt, int splits) {
+    const int64_t tiles = mt * nt, per = (tiles * splits + 7) / 8, ts = (int64_t)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
+    m = -1;
+    if ((int64_t)(blockIdx.x >> 3) >= per || ts >= tiles * splits) return;
+    split = ts / tiles;
+    const int64_t t = ts - split * tiles, g = t / (8 * nt), gm = mt - g * 8 < 8 ? mt - g * 8 : 8, q = t - g * 8 * nt;
+    m = g * 8 + q % gm, n = q / gm;
+  }
+};
+template <int NI, int NJ>
+__device__ __forceinline__ void clear(v16f (&acc)[NI][NJ]) {
+#pragma unroll
+  for (int i = 0; i < NI; ++i)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+}
+
+// Hidden values as they are stored.  Lane l32 + 32 half of a 32 x 32 tile of sums has column l32, a row of X, and the rows 8 k + 4 half + 0 .. 3, hidden columns c .. c + 3.
+struct Hidden {
+  const Args& a;
+  int lane, half;
+  __device__ __forceinline__ Hidden(const Args& args) : a(args), lane(threadIdx.x & 63), half((threadIdx.x & 63) >> 5) {}
+  // four values of hidden columns c .. c + 3 of a row of gate or up
+  __device__ __forceinline__ void put(float* p, int64_t c, V4 x) const {
+    if (c + 4 <= a.f) {
+      *reinterpret_cast<V4*>(p + c) = x;
+      return;
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+      if (c + k < a.f) p[c + k] = x[k];
+  }
+  __device__ __forceinline__ V4 get(const float* p, int64_t c) const {
+    if (c + 4 <= a.f) return *reinterpret_cast<const V4*>(p + c);
+    V4 x{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+      if (c + k < a.f) x[k] = p[c + k];
+    return x;
+  }
+  // four values of a row, in the order of fragments: the k-th four of 16 columns by half
+  __device__ __forceinline__ void put_frag(float* p, int64_t KS, int64_t row_block, int64_t step, int k, V4 x) const {
+    *reinterpret_cast<V4*>(p + ((row_block * KS + step) * 2 + k) * (FRAG / 2) + lane * 4) = x;
+  }
+  // H, dA and dB of NJ row blocks from row block b0 on, of the hidden columns c0 .. c0 + 31.  Largest values: of the rows join ma and mb, of the columns (of H, dA,
+  // dB, 32 each) go to cols.  (An infinite one may be the largest: what is scaled by it is not finite in any case.)  get(j, k, x, y): A and B of four hidden
+  // columns of a row, fetched four columns ahead; sums(j, k, e): G of one.
+  template <int KIND, int NJ, class Get, class Sums>
+  __device__ __forceinline__ void back(int64_t b0, int64_t c0, float (&ma)[NJ], float (&mb)[NJ], float* cols, Get&& get, Sums&& sums) const {
+    const int l32 = lane & 31;
+    const bool edge = (b0 + NJ) * 32 > a.n || c0 + 32 > a.f;
+    V4 x[2][NJ], y[2][NJ];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) get(j, 0, x[0][j], y[0][j]);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (k < 3) {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) get(j, k + 1, x[(k + 1) & 1][j], y[(k + 1) & 1][j]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      const int64_t c = c0 + k * 8 + half * 4, step = c0 / 16 + (k >> 1), step_d = c0 / 8 + (k >> 1);
+      float ch[4] = {}, ca[4] = {}, cb[4] = {};
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        const int64_t v = (b0 + j) * 32 + l32;
+        V4 h, da, db;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const Act s = act_of<KIND>(a.act, x[k & 1][j][e]);
+          const float u = y[k & 1][j][e], g = sums(j, k, e);
+          h[e] = s.v * u, da[e] = g * u * s.s, db[e] = g * s.v;
+        }
+        if (edge) {                    // what is behind the last row and column is 0, whatever the weights are
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (v >= a.n || c + e >= a.f) h[e] = da[e] = db[e] = 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          ch[e] = fmaxf(ch[e], fabsf(h[e])), ca[e] = fmaxf(ca[e], fabsf(da[e])), cb[e] = fmaxf(cb[e], fabsf(db[e]));
+          ma[j] = fmaxf(ma[j], fabsf(da[e])), mb[j] = fmaxf(mb[j], fabsf(db[e]));
+        }
+        put_frag(a.H, a.KSH, b0 + j, step, k & 1, h);
+        put_frag(a.D, a.KSD, b0 + j, step_d, k & 1, da);
+        put_frag(a.D, a.KSD, b0 + j, step_d + 2, k & 1, db);
+        __builtin_amdgcn_sched_barrier(0);      // (one after the other: together they need more registers than there are)
+      }
+      const float th = max_over_32(ch), ta = max_over_32(ca), tb = max_over_32(cb);
+      if (!(l32 & 7)) {
+        float* to = cols + k * 8 + half * 4 + (l32 >> 3);
+        to[0] = th, to[32] = ta, to[64] = tb;
+      }
+    }
+  }
+  // What the four waves found, to where it is kept: cols, of HBS hidden blocks from hidden column c0 on, and ma and mb by way of top (8 NJ 32 words of LDS).  All words are
+  // looked at together: each takes a trip to memory.
+  template <int NJ, int HBS>
+  __device__ __forceinline__ void back_tops(int64_t b0, int64_t c0, const float (&ma)[NJ], const float (&mb)[NJ], const float* cols, float* top) const {
+    constexpr int R = NJ * 32, N = 2 * R + HBS * 96, U = (N + 255) / 256;
+    const int wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const float x = fmaxf(ma[j], __shfl_xor(ma[j], 32, 64)), y = fmaxf(mb[j], __shfl_xor(mb[j], 32, 64));
+      top[(wave * 2 + half) * R + j * 32 + (lane & 31)] = half ? y : x;
+    }
+    __syncthreads();
+    uint32_t *word[U], is[U], was[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = u * 256 + threadIdx.x;
+      word[u] = nullptr;
+      float m = 0.f;
+      if (i < 2 * R) {
+        const int which = i / R, r = i % R;
+        m = fmaxf(fmaxf(top[which * R + r], top[(2 + which) * R + r]), fmaxf(top[(4 + which) * R + r], top[(6 + which) * R + r]));
+        if (b0 * 32 + r < a.n) word[u] = (which ? a.b_row : a.a_row) + b0 * 32 + r;
+      } else if (i < N) {
+        const int q = i - 2 * R, which = q / 32 % 3;
+        const int64_t c = c0 + q / 96 * 32 + q % 32;
+        m = cols[q];
+        if (c < a.f) word[u] = (which == 0 ? a.h_col : which == 1 ? a.a_col : a.b_col) + c;
+      }
+      is[u] = __float_as_uint(m);
+      was[u] = word[u] ? __hip_atomic_load(word[u], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0xffffffffu;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (was[u] < is[u]) atomicMax(word[u], is[u]);
+  }
+};
+
+template <int MODE, int KIND>
 __global__ void __launch_bounds__(256, 2) k_ffn_split(Args a) {
   constexpr bool TURN = MODE == ROWS || MODE == COLS;
-  constexpr int STAGE = stage_halfs(TURN);
-  __shared__ __attribute__((aligned(16))) _Float16 Bs[2 * STAGE];
+  __shared__ __attribute__((aligned(16))) _Float16 Bs[2 * stage_halfs(TURN)];
+  const Tile tile(a.mt, a.nt, a.splits);
+  if (tile.m < 0) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
-  // each XCD takes a contiguous part of the tiles, eight tiles of A over all of B after eight others
-  const int64_t tiles = a.mt * a.nt, per = (tiles * a.splits + 7) / 8, ts = (int64_t)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
-  if ((int64_t)(blockIdx.x >> 3) >= per || ts >= tiles * a.splits) return;
-  const int64_t split = ts / tiles, t = ts - split * tiles;
-  const int64_t g = t / (8 * a.nt), gm = a.mt - g * 8 < 8 ? a.mt - g * 8 : 8, q = t - g * 8 * a.nt;
-  const int64_t m0 = (g * 8 + q % gm) * TM, n0 = q / gm * TN;
+  constexpr int NI = MODE == BACK ? 1 : 2;               // row blocks of A a wave (BACK has much to do with each sum)
+  const int64_t split = tile.split, m0 = tile.m * (NI * 128), n0 = tile.n * TN, mw = m0 + wave * (NI * 32);
   const int64_t s0 = a.pairs * split / a.splits * 2;                 // its first stage
-  int todo = __builtin_amdgcn_readfirstlane((int)(a.pairs * (split + 1) / a.splits - s0 / 2));
-  const int64_t mw = m0 + wave * 64;
+  const int todo = __builtin_amdgcn_readfirstlane((int)(a.pairs * (split + 1) / a.splits - s0 / 2));
 
   // exponents of the weights; of the rows of A (ROWS), of the columns that are split on the way to LDS (COLS)
   const int e0 = exp_or_0(a.w0 ? scale_exp(*a.w0) : NONE), e1 = exp_or_0(a.w1 ? scale_exp(*a.w1) : NONE);
@@ -301,107 +535,32 @@ __global__ void __launch_bounds__(256, 2) k_ffn_split(Args a) {
     if (c >= a.f) return 0u;
     return !a.two ? a.h_col[c] : (n / HB) & 1 ? a.b_col[c] : a.a_col[c];
   };
-  float fr[2][2], fc[2][8];
+  v16f acc[NI][4];
+  clear(acc);
+  const _Float16* Ap = a.A + (mw / 32 * a.KSA + s0 * KT) * 2 * FRAG + lane * 8;
+  const _Float16* B = a.B + (TURN ? s0 * a.KSB + n0 / 16 : n0 / 32 * a.KSB + s0 * KT) * 2 * FRAG;
+  const int64_t a_rows = a.KSA * 2 * FRAG, b_rows = a.KSB * 2 * FRAG;
+  const auto as_it_is = [](v8h (&)[2], int, int) {};
   if constexpr (MODE == ROWS) {
+    float fr[2][2];                    // (a stage's parity is which half of a hidden block [gate, up] it is)
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int e = row_exp(mw + i * 32 + l32);
       fr[i][0] = pow2(e - e0), fr[i][1] = pow2(e - (a.two ? e1 : e0));
     }
-  }
-  if constexpr (MODE == COLS) {
+    multiply<true, true>(acc, Ap, a_rows, B, b_rows, todo, Bs, [&](v8h (&x)[2], int i, int cur) { split8(x[0], x[1], [&](int) { return fr[i][cur]; }); }, [](v8h (&)[4]) {});
+  } else if constexpr (MODE == COLS) {
+    float fc[2][8];
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int k = 0; k < 8; ++k) fc[u][k] = pow2(exp_or_0(scale_exp(col_top(n0 + wave * 32 + u * 16 + (k >> 2) * 8 + half * 4 + (k & 3)))));
-  }
-
-  v16f acc[2][4];
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-
-  const _Float16 *Ap0 = a.A + ((m0 / 32 + wave * 2) * a.KSA + s0 * KT) * 2 * FRAG + lane * 8, *Ap1 = Ap0 + a.KSA * 2 * FRAG;
-  // a wave brings one of the four row blocks, or two of the eight 16s
-  const _Float16* Bp = a.B + (TURN ? s0 * a.KSB + n0 / 16 + wave * 2 : (n0 / 32 + wave) * a.KSB + s0 * KT) * 2 * FRAG + lane * 8;
-  const int64_t b_step = (TURN ? a.KSB : KT) * 2 * FRAG;
-  v8h ra[2][KT][2][2], rb[KT * 2];    // [stage in turn][step][row block][plane]
-  auto fetch = [&](int to) {          // of the stage that the pointers have come to
-#pragma unroll
-    for (int u = 0; u < KT * 2; ++u) rb[u] = *reinterpret_cast<const v8h*>(Bp + u * FRAG);
-#pragma unroll
-    for (int u = 0; u < KT; ++u)
-#pragma unroll
-      for (int p = 0; p < 2; ++p) {
-        ra[to][u][0][p] = *reinterpret_cast<const v8h*>(Ap0 + (u * 2 + p) * FRAG);
-        ra[to][u][1][p] = *reinterpret_cast<const v8h*>(Ap1 + (u * 2 + p) * FRAG);
-      }
-    Ap0 += KT * 2 * FRAG, Ap1 += KT * 2 * FRAG, Bp += b_step;
-  };
-  auto stash = [&](int to) {
-    if constexpr (MODE == COLS) {
+    multiply<true, true>(acc, Ap, a_rows, B, b_rows, todo, Bs, as_it_is, [&](v8h (&rb)[4]) {
 #pragma unroll
       for (int u = 0; u < 2; ++u) split8(rb[u * 2], rb[u * 2 + 1], [&](int t) { return fc[u][t]; });
-    }
-#pragma unroll
-    for (int u = 0; u < KT * 2; ++u)
-      *reinterpret_cast<v8h*>(Bs + to * STAGE + (TURN ? ((wave * 4 + u) * 2 + half) * TURN_HALF + l32 * 8 : (wave * KT * 2 + u) * FRAG + lane * 8)) = rb[u];
-  };
-  auto read_b = [&](v8h* b, int cur, int k) {          // k: step * 4 + row block
-    if (TURN) {
-      const int i = lane & 15, sixteen = (k & 3) * 2 + ((lane >> 4) & 1);
-      const _Float16* f = Bs + cur * STAGE + (sixteen * 4 + (i & 1)) * TURN_HALF + ((k >> 2) * 16 + half * 4 + (i >> 2)) * 8 + ((i >> 1) & 1) * 4;
-#pragma unroll
-      for (int p = 0; p < 2; ++p) {
-        const v4h lo = turned(f + p * 2 * TURN_HALF), hi = turned(f + p * 2 * TURN_HALF + 64);
-        b[p] = v8h{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-      }
-      return;
-    }
-    const _Float16* f = Bs + cur * STAGE + ((k & 3) * KT * 2 + (k >> 2) * 2) * FRAG + lane * 8;
-    b[0] = *reinterpret_cast<const v8h*>(f);
-    b[1] = *reinterpret_cast<const v8h*>(f + FRAG);
-  };
-  // (Loads have no condition, so that waits count only the loads that they wait for: the last stage fetches itself again.  The barriers to scheduling
-  // keep them where they stand; they would be moved down to where they are used.)  cur is also which half of a hidden block [gate, up] the stage is.
-  auto stage = [&](int cur, bool more) {
-    if (!more) Ap0 -= KT * 2 * FRAG, Ap1 -= KT * 2 * FRAG, Bp -= b_step;
-    v8h b[2][2];
-    read_b(b[0], cur, 0);
-    fetch(cur ^ 1);
-#pragma unroll
-    for (int k = 0; k < 4 * KT; ++k) {
-      v8h (&x)[2][2] = ra[cur][k >> 2];
-      const v8h (&y)[2] = b[k & 1];
-      if (MODE == ROWS && (k & 3) == 0) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) split8(x[i][0], x[i][1], [&](int) { return fr[i][cur]; });
-      }
-      if (k + 1 < 4 * KT) read_b(b[(k + 1) & 1], cur, k + 1);
-      __builtin_amdgcn_sched_barrier(0);
-      const int j = k & 3;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][1], y[0], acc[i][j], 0, 0, 0);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][0], y[1], acc[i][j], 0, 0, 0);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][0], y[0], acc[i][j], 0, 0, 0);
-    }
-    __builtin_amdgcn_sched_barrier(0);
-    stash(cur ^ 1);
-    __syncthreads();
-  };
-  if (todo > 0) {
-    fetch(0);
-    stash(0);
-    __syncthreads();
-    do {
-      stage(0, true);
-      stage(1, --todo > 0);
-    } while (todo > 0);
+    });
+  } else {
+    multiply<false, true>(acc, Ap, a_rows, B, b_rows, todo, Bs, as_it_is, [](v8h (&)[4]) {});
   }
 
   // lane l32 + 32 half of a 32 x 32 tile has column l32 and the rows 8 (e / 4) + 4 half + e % 4
@@ -435,29 +594,8 @@ __global__ void __launch_bounds__(256, 2) k_ffn_split(Args a) {
     }
     return;
   }
-  uint32_t* top = reinterpret_cast<uint32_t*>(Bs);      // [wave][which][row]
-  // four values of hidden columns c .. c + 3 to a row of gate or up
-  auto put4 = [&](float* p, int64_t c, V4 x) {
-    if (c + 4 <= a.f) {
-      *reinterpret_cast<V4*>(p + c) = x;
-      return;
-    }
-#pragma unroll
-    for (int k = 0; k < 3; ++k)
-      if (c + k < a.f) p[c + k] = x[k];
-  };
-  auto get4 = [&](const float* p, int64_t c) {
-    if (c + 4 <= a.f) return *reinterpret_cast<const V4*>(p + c);
-    V4 x{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int k = 0; k < 3; ++k)
-      if (c + k < a.f) x[k] = p[c + k];
-    return x;
-  };
-  // four values of a row, in the order of fragments: the k-th four of 16 columns by half
-  auto put_frag = [&](float* p, int64_t KS, int64_t row_block, int64_t step, int k, V4 x) {
-    *reinterpret_cast<V4*>(p + ((row_block * KS + step) * 2 + k) * (FRAG / 2) + lane * 4) = x;
-  };
+  float* top = reinterpret_cast<float*>(Bs);
+  const Hidden at(a);
   if constexpr (MODE == PROJECT) {
     const int64_t c0 = mw / 2;                          // the wave's 32 hidden columns
 #pragma unroll
@@ -465,7 +603,7 @@ __global__ void __launch_bounds__(256, 2) k_ffn_split(Args a) {
       const int64_t v = n0 + j * 32 + l32;
       const bool there = v < a.n;
       const int ex = exp_or_0(scale_exp(there ? a.rows_in[v] : 0u));
-      uint32_t m = 0;
+      float m = 0.f;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const int64_t c = c0 + k * 8 + half * 4;
@@ -473,73 +611,78 @@ __global__ void __launch_bounds__(256, 2) k_ffn_split(Args a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           x[e] = __builtin_amdgcn_ldexpf(acc[0][j][k * 4 + e], -(ex + e0)), y[e] = __builtin_amdgcn_ldexpf(acc[1][j][k * 4 + e], -(ex + e1));
-          h[e] = there ? act_of(a.act, x[e]).v * y[e] : 0.f;
-          m = max(m, size_bits(h[e]));
+          h[e] = act_of<KIND>(a.act, x[e]).v * y[e];
+          m = fmaxf(m, fabsf(h[e]));
         }
-        if (a.gate && there) put4(a.gate + v * a.ld_gate, c, x), put4(a.up + v * a.ld_up, c, y);
-        if (a.H) put_frag(a.H, a.KSH, n0 / 32 + j, c0 / 16 + (k >> 1), k & 1, h);
+        if (a.gate && there) at.put(a.gate + v * a.ld_gate, c, x), at.put(a.up + v * a.ld_up, c, y);
+        at.put_frag(a.H, a.KSH, n0 / 32 + j, c0 / 16 + (k >> 1), k & 1, h);
       }
-      m = max(m, (uint32_t)__shfl_xor((int)m, 32, 64));
+      m = fmaxf(m, __shfl_xor(m, 32, 64));
       if (half == 0) top[wave * TN + j * 32 + l32] = m;
     }
-    if (!a.H) return;
     __syncthreads();
-    if (tid < TN && n0 + tid < a.n) raise(a.h_row + n0 + tid, max(max(top[tid], top[TN + tid]), max(top[2 * TN + tid], top[3 * TN + tid])));
+    if (tid < TN && n0 + tid < a.n) raise(a.h_row + n0 + tid, __float_as_uint(fmaxf(fmaxf(top[tid], top[TN + tid]), fmaxf(top[2 * TN + tid], top[3 * TN + tid]))));
   }
   if constexpr (MODE == BACK) {
-    uint32_t ma[4] = {}, mb[4] = {};
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int64_t c0 = mw + i * 32;
-      uint32_t ch[16] = {}, ca[16] = {}, cb[16] = {};
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int64_t v = n0 + j * 32 + l32;
-        const bool there = v < a.n;
-        const int64_t row = there ? v : a.n - 1;
-        const int ey = exp_or_0(scale_exp(there ? a.rows_in[v] : 0u));
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int64_t c = c0 + k * 8 + half * 4;
-          const V4 x = get4(a.gate + row * a.ld_gate, c), y = get4(a.up + row * a.ld_up, c);
-          V4 h, da, db;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float gr = __builtin_amdgcn_ldexpf(acc[i][j][k * 4 + e], -(ey + e0));
-            const Act s = act_of(a.act, x[e]);
-            const bool in = there && c + e < a.f;
-            h[e] = in ? s.v * y[e] : 0.f;
-            da[e] = in ? gr * y[e] * s.s : 0.f;
-            db[e] = in ? gr * s.v : 0.f;
-            ch[k * 4 + e] = max(ch[k * 4 + e], size_bits(h[e]));
-            ca[k * 4 + e] = max(ca[k * 4 + e], size_bits(da[e]));
-            cb[k * 4 + e] = max(cb[k * 4 + e], size_bits(db[e]));
-            ma[j] = max(ma[j], size_bits(da[e]));
-            mb[j] = max(mb[j], size_bits(db[e]));
-          }
-          const int64_t step = c0 / 16 + (k >> 1);
-          put_frag(a.H, a.KSH, n0 / 32 + j, step, k & 1, h);
-          put_frag(a.D, a.KSD, n0 / 32 + j, c0 / 8 + (k >> 1), k & 1, da);
-          put_frag(a.D, a.KSD, n0 / 32 + j, c0 / 8 + 2 + (k >> 1), k & 1, db);
-        }
-      }
-      const int e = l32 >> 1;
-      const int64_t c = c0 + (e >> 2) * 8 + half * 4 + (e & 3);
-      const uint32_t th = max_over_32(ch), ta = max_over_32(ca), tb = max_over_32(cb);
-      if (!(l32 & 1) && c < a.f) raise(a.h_col + c, th), raise(a.a_col + c, ta), raise(a.b_col + c, tb);
-    }
+    float ma[4] = {}, mb[4] = {};
+    float* cols = top + 8 * TN;
+    int ey[4];
+    const float *gate[4], *up[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const uint32_t x = max(ma[j], (uint32_t)__shfl_xor((int)ma[j], 32, 64)), y = max(mb[j], (uint32_t)__shfl_xor((int)mb[j], 32, 64));
-      top[(wave * 2 + half) * TN + j * 32 + l32] = half ? y : x;
+      const int64_t v = n0 + j * 32 + l32, row = v < a.n ? v : a.n - 1;
+      ey[j] = exp_or_0(scale_exp(a.rows_in[row]));
+      gate[j] = a.gate + row * a.ld_gate, up[j] = a.up + row * a.ld_up;
     }
-    __syncthreads();
-    const int which = tid / TN, r = tid % TN;
-    if (n0 + r < a.n) {
-      const uint32_t m = max(max(top[which * TN + r], top[(2 + which) * TN + r]), max(top[(4 + which) * TN + r], top[(6 + which) * TN + r]));
-      raise((which ? a.b_row : a.a_row) + n0 + r, m);
-    }
+    at.back<KIND, 4>(n0 / 32, mw, ma, mb, cols + wave * 96, [&](int j, int k, V4& x, V4& y) {
+      const int64_t c = mw + k * 8 + half * 4;
+      x = at.get(gate[j], c), y = at.get(up[j], c);
+    }, [&](int j, int k, int e) { return __builtin_amdgcn_ldexpf(acc[0][j][k * 4 + e], -(ey[j] + e0)); });
+    at.back_tops<4, 4>(n0 / 32, m0, ma, mb, cols, top);
   }
+}
+
+// PROJECT and BACK in one where A and B were not kept: 128 hidden columns by 96 rows, 32 by 96 a wave, first A and B, then G.  (With 128 rows the sums alone take
+// 192 registers of 256.)
+constexpr int REMAKE_ROWS = 96;
+struct RemakeArgs {
+  Args a;                              // A, B, KSA, KSB, pairs, w0, w1, rows_in: the projections'
+  const _Float16 *A2, *B2;
+  int64_t KS2, pairs2;
+  const uint32_t *w2, *rows2;
+};
+template <int KIND>
+__global__ void __launch_bounds__(256, 2) k_ffn_remake(RemakeArgs r) {
+  __shared__ __attribute__((aligned(16))) _Float16 Bs[2 * stage_halfs(false)];
+  const Args& a = r.a;
+  const Tile tile(a.mt, a.nt, 1);
+  if (tile.m < 0) return;
+  constexpr int NJ = REMAKE_ROWS / 32;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t hb = tile.m * 4 + wave, b0 = tile.n * NJ;            // the wave's hidden block, the tile's first row block
+  v16f ab[2][NJ], gr[1][NJ];
+  const auto as_it_is = [](v8h (&)[2], int, int) {};
+  const auto as_it_comes = [](v8h (&)[NJ]) {};
+  clear(ab);
+  multiply<false, false>(ab, a.A + hb * 2 * a.KSA * 2 * FRAG + lane * 8, a.KSA * 2 * FRAG, a.B + b0 * a.KSB * 2 * FRAG, a.KSB * 2 * FRAG, (int)a.pairs, Bs, as_it_is, as_it_comes);
+  clear(gr);
+  multiply<false, false>(gr, r.A2 + hb * r.KS2 * 2 * FRAG + lane * 8, 0, r.B2 + b0 * r.KS2 * 2 * FRAG, r.KS2 * 2 * FRAG, (int)r.pairs2, Bs, as_it_is, as_it_comes);
+  const int e0 = exp_or_0(scale_exp(*a.w0)), e1 = exp_or_0(scale_exp(*a.w1)), e2 = exp_or_0(scale_exp(*r.w2));
+  const Hidden at(a);
+  float ma[NJ] = {}, mb[NJ] = {};
+  float *top = reinterpret_cast<float*>(Bs), *cols = top + 8 * NJ * 32;
+  int ex[NJ], ey[NJ];
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    const int64_t v = (b0 + j) * 32 + (lane & 31), row = v < a.n ? v : a.n - 1;
+    ex[j] = exp_or_0(scale_exp(a.rows_in[row])), ey[j] = exp_or_0(scale_exp(r.rows2[row]));
+  }
+  at.back<KIND, NJ>(b0, hb * HB, ma, mb, cols + wave * 96, [&](int j, int k, V4& x, V4& y) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      x[e] = __builtin_amdgcn_ldexpf(ab[0][j][k * 4 + e], -(ex[j] + e0)), y[e] = __builtin_amdgcn_ldexpf(ab[1][j][k * 4 + e], -(ex[j] + e1));
+  }, [&](int j, int k, int e) { return __builtin_amdgcn_ldexpf(gr[0][j][k * 4 + e], -(ey[j] + e2)); });
+  at.back_tops<NJ, 4>(b0, tile.m * 4 * HB, ma, mb, cols, top);
 }
 
 // What products left in parts, added up in their order: out [rows x cols] (+)= the sum of `parts` blocks of [rows x pitch].
@@ -584,6 +727,11 @@ constexpr int64_t LEAST_PAIRS = 4;                 // of a part of a reduction
 
 int parts_of(int64_t tiles, int64_t pairs) { return (int)std::max<int64_t>(1, std::min<int64_t>({SLOTS / tiles, pairs / LEAST_PAIRS, 64})); }
 
+Gate gate_of(int act) {
+  const float k = 1.5957691216057308f;             // 2 sqrt(2 / pi)
+  return act == HT_GATE_GELU_TANH ? Gate{act, k, 0.044715f * k, 0} : Gate{act, 1.f, 0.f, act == HT_GATE_SIGMOID};
+}
+
 // One of ht_ffn_fwd and ht_ffn_bwd
 struct Ffn {
   ht_ctx* ctx;
@@ -597,10 +745,11 @@ struct Ffn {
     const int64_t blocks = up_to(a.mt * a.nt * a.splits, 8);
     if (blocks >= (1 << 24)) return ht_set_err(ctx, HT_ESHAPE, "ffn: %lld tiles in one product", (long long)blocks);
     const unsigned grid = (unsigned)blocks;
-    if (mode == PROJECT) k_ffn_split<PROJECT><<<grid, 256, 0, ctx->stream>>>(a);
-    else if (mode == BACK) k_ffn_split<BACK><<<grid, 256, 0, ctx->stream>>>(a);
-    else if (mode == ROWS) k_ffn_split<ROWS><<<grid, 256, 0, ctx->stream>>>(a);
-    else k_ffn_split<COLS><<<grid, 256, 0, ctx->stream>>>(a);
+    const bool logistic = a.act.act != HT_GATE_GELU && a.act.act != HT_GATE_RELU;
+    if (mode == PROJECT) (logistic ? k_ffn_split<PROJECT, LOGISTIC> : k_ffn_split<PROJECT, OTHERS>)<<<grid, 256, 0, ctx->stream>>>(a);
+    else if (mode == BACK) (logistic ? k_ffn_split<BACK, LOGISTIC> : k_ffn_split<BACK, OTHERS>)<<<grid, 256, 0, ctx->stream>>>(a);
+    else if (mode == ROWS) k_ffn_split<ROWS, OTHERS><<<grid, 256, 0, ctx->stream>>>(a);
+    else k_ffn_split<COLS, OTHERS><<<grid, 256, 0, ctx->stream>>>(a);
     HT_LAUNCH_CHECK(ctx);
     return HT_OK;
   }
@@ -624,8 +773,9 @@ struct Ffn {
     const int64_t fp = up_to(f, 256), dp = up_to(d, TM), ep = up_to(e, TM), KSd = up_to(d, TN) / 16, KSe = up_to(e, TN) / 16, KSH = fp / 16, KSD = fp / 8;
     const bool remake = bwd && !gate, d_w = dWg || dWu;
     // a row's share
-    const int64_t own = 4 * (dp + (bwd && d_w ? dp : 0) + (bwd ? ep : 0) + (bwd && dWd ? ep : 0) + fp * (bwd ? 3 : 1) + (remake ? 2 * fp : 0));
+    const int64_t own = 4 * (dp + (bwd && d_w ? dp : 0) + (bwd ? ep : 0) + (bwd && dWd ? ep : 0) + fp * (bwd ? 3 : 1));
     const int64_t Rp = std::max<int64_t>(TM, std::min<int64_t>((int64_t)bytes / own / TM * TM, up_to(n, TM)));
+    const int64_t Ra = Rp + REMAKE_ROWS;               // (the last tile of k_ffn_remake may go beyond Rp)
     const int64_t KSR = Rp / 16, pieces = ceil_div64(n, Rp);
     // tiles of the products, and parts of their reductions
     const int64_t mt = Rp / TM, nte = up_to(e, TN) / TN, ntd = up_to(d, TN) / TN, ntD = ceil_div64(f, 64), ntH = ceil_div64(f, TN);
@@ -639,12 +789,11 @@ struct Ffn {
     const int64_t n_top = 4 + 5 * Rp + dp + ep + 3 * fp;
     const auto top = m.add<uint32_t>(n_top);
     const auto W2 = m.add<_Float16>(2 * fp * KSd * 32), Wf = m.add<_Float16>(fp * KSe * 32);
-    const auto Xr = m.add<_Float16>(Rp * KSd * 32);
+    const auto Xr = m.add<_Float16>(Ra * KSd * 32);
     const auto Xt = m.add<_Float16>(d_w ? dp * KSR * 32 : 0);
-    const auto Gr = m.add<_Float16>(bwd ? Rp * KSe * 32 : 0);
+    const auto Gr = m.add<_Float16>(bwd ? Ra * KSe * 32 : 0);
     const auto Gt = m.add<_Float16>(dWd ? ep * KSR * 32 : 0);
-    const auto A = m.add<float>(remake ? Rp * f4 : 0), B = m.add<float>(remake ? Rp * f4 : 0);
-    const auto H = m.add<float>(Rp * fp), Df = m.add<float>(bwd ? Rp * fp * 2 : 0);
+    const auto H = m.add<float>(Ra * fp), Df = m.add<float>(bwd ? Ra * fp * 2 : 0);
     const auto sums_y = m.add<float>(!bwd && sy > 1 ? sy * Rp * e4 : 0), sums_x = m.add<float>(dX && sx > 1 ? sx * Rp * d4 : 0);
     const auto sums_D = m.add<float>(d_w && sD > 1 ? sD * 2 * wr * wp : 0), sums_H = m.add<float>(dWd && sH > 1 ? sH * vr * vp : 0);
     HT_TRY(bytes > FFN_LEAN ? m.take_if_room(ctx) : m.take(ctx));
@@ -684,26 +833,31 @@ struct Ffn {
       HT_LAUNCH_CHECK(ctx);
 
       Args base{};
-      base.act = D->act, base.n = rows, base.f = f, base.splits = 1;
+      base.act = gate_of(D->act), base.n = rows, base.f = f, base.splits = 1;
       base.h_row = t_h, base.a_row = t_a, base.b_row = t_b, base.h_col = t_hc, base.a_col = t_ac, base.b_col = t_bc;
       base.KSH = KSH, base.KSD = KSD;
-      base.gate = gate ? gate->ptr + r0 * gate->ld : remake ? m.at(A) : nullptr, base.ld_gate = gate ? gate->ld : f4;
-      base.up = up ? up->ptr + r0 * up->ld : remake ? m.at(B) : nullptr, base.ld_up = up ? up->ld : f4;
+      base.gate = gate ? gate->ptr + r0 * gate->ld : nullptr, base.ld_gate = gate ? gate->ld : 0;
+      base.up = up ? up->ptr + r0 * up->ld : nullptr, base.ld_up = up ? up->ld : 0;
       const int64_t row_tiles = ceil_div64(rows, TN);
+      Args a = base;
+      a.H = m.at(H);
       if (!bwd || remake) {
-        Args a = base;
         a.A = m.at(W2), a.KSA = KSd, a.B = m.at(Xr), a.KSB = KSd;
         a.mt = ceil_div64(f, TN), a.nt = row_tiles, a.pairs = ceil_div64(d, PAIR);
         a.w0 = t_g, a.w1 = t_u, a.rows_in = t_x;
-        a.H = bwd ? nullptr : m.at(H);
-        HT_TRY(launch(PROJECT, a));
+        if (!bwd) HT_TRY(launch(PROJECT, a));
       }
-      if (bwd) {
-        Args a = base;
+      if (remake) {
+        a.D = m.at(Df);
+        a.nt = ceil_div64(up_to(rows, PAIR), REMAKE_ROWS);           // (COLS reads whole pairs of stages)
+        const bool logistic = D->act != HT_GATE_GELU && D->act != HT_GATE_RELU;
+        (logistic ? k_ffn_remake<LOGISTIC> : k_ffn_remake<OTHERS>)<<<(unsigned)up_to(a.mt * a.nt, 8), 256, 0, st>>>(RemakeArgs{a, m.at(Wf), m.at(Gr), KSe, ceil_div64(e, PAIR), t_d, t_y});
+        HT_LAUNCH_CHECK(ctx);
+      } else if (bwd) {
         a.A = m.at(Wf), a.KSA = KSe, a.B = m.at(Gr), a.KSB = KSe;
-        a.mt = ceil_div64(f, TM), a.nt = row_tiles, a.pairs = ceil_div64(e, PAIR);
+        a.mt = ceil_div64(f, TN), a.nt = row_tiles, a.pairs = ceil_div64(e, PAIR);
         a.w0 = t_d, a.rows_in = t_y;
-        a.H = m.at(H), a.D = m.at(Df);
+        a.D = m.at(Df);
         HT_TRY(launch(BACK, a));
       }
       Joins j{};
