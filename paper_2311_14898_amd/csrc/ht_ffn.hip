@@ -565,22 +565,27 @@ __global__ void __launch_bounds__(256, 2) k_ffn_split(Args a) {
 
   // lane l32 + 32 half of a 32 x 32 tile has column l32 and the rows 8 (e / 4) + 4 half + e % 4
   if constexpr (MODE == ROWS || MODE == COLS) {
+    // exponents of the rows and columns of sums, all of them looked up at once (where they are used, one after the other, each would be a trip to memory)
+    int* ends = reinterpret_cast<int*>(Bs);
+    ends[tid] = m0 + tid < a.m_end ? (MODE == COLS ? exp_or_0(scale_exp(a.m_top[m0 + tid])) : row_exp(m0 + tid)) : 0;
+    if (MODE == COLS && tid < TN) ends[TM + tid] = exp_or_0(scale_exp(col_top(n0 + tid)));
+    __syncthreads();
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int64_t n = n0 + j * 32 + l32, c = MODE == COLS ? hidden(n) : n;
       const Out& o = a.out[MODE == COLS && a.two ? j & 1 : 0];
       if (!o.p || c >= a.n_end) continue;
-      const int en = MODE == COLS ? exp_or_0(scale_exp(col_top(n))) : 0;
+      const int en = MODE == COLS ? ends[TM + j * 32 + l32] : 0;
       float* at = o.p + split * o.split_part + c * o.ns;
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const int64_t m = mw + i * 32 + k * 8 + half * 4;
-          V4 x;
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            x[e] = m + e < a.m_end ? __builtin_amdgcn_ldexpf(acc[i][j][k * 4 + e], -(MODE == COLS ? exp_or_0(scale_exp(a.m_top[m + e])) + en : row_exp(m + e))) : 0.f;
+          const int r = wave * 64 + i * 32 + k * 8 + half * 4;
+          const int64_t m = m0 + r;
+          const int4 em = *reinterpret_cast<const int4*>(ends + r);
+          V4 x{__builtin_amdgcn_ldexpf(acc[i][j][k * 4], -(em.x + en)), __builtin_amdgcn_ldexpf(acc[i][j][k * 4 + 1], -(em.y + en)),
+               __builtin_amdgcn_ldexpf(acc[i][j][k * 4 + 2], -(em.z + en)), __builtin_amdgcn_ldexpf(acc[i][j][k * 4 + 3], -(em.w + en))};
           float* to = at + m * o.ms;
           if (o.ms == 1 && m + 4 <= a.m_end) {
             if (a.add) x += *reinterpret_cast<const V4u*>(to);
@@ -598,11 +603,14 @@ __global__ void __launch_bounds__(256, 2) k_ffn_split(Args a) {
   const Hidden at(a);
   if constexpr (MODE == PROJECT) {
     const int64_t c0 = mw / 2;                          // the wave's 32 hidden columns
+    int exps[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) exps[j] = exp_or_0(scale_exp(n0 + j * 32 + l32 < a.n ? a.rows_in[n0 + j * 32 + l32] : 0u));
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int64_t v = n0 + j * 32 + l32;
       const bool there = v < a.n;
-      const int ex = exp_or_0(scale_exp(there ? a.rows_in[v] : 0u));
+      const int ex = exps[j];
       float m = 0.f;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
@@ -664,9 +672,9 @@ __global__ void __launch_bounds__(256, 2) k_ffn_remake(RemakeArgs r) {
   const auto as_it_is = [](v8h (&)[2], int, int) {};
   const auto as_it_comes = [](v8h (&)[NJ]) {};
   clear(ab);
-  multiply<false, false>(ab, a.A + hb * 2 * a.KSA * 2 * FRAG + lane * 8, a.KSA * 2 * FRAG, a.B + b0 * a.KSB * 2 * FRAG, a.KSB * 2 * FRAG, (int)a.pairs, Bs, as_it_is, as_it_comes);
+  multiply<false, true>(ab, a.A + hb * 2 * a.KSA * 2 * FRAG + lane * 8, a.KSA * 2 * FRAG, a.B + b0 * a.KSB * 2 * FRAG, a.KSB * 2 * FRAG, (int)a.pairs, Bs, as_it_is, as_it_comes);
   clear(gr);
-  multiply<false, false>(gr, r.A2 + hb * r.KS2 * 2 * FRAG + lane * 8, 0, r.B2 + b0 * r.KS2 * 2 * FRAG, r.KS2 * 2 * FRAG, (int)r.pairs2, Bs, as_it_is, as_it_comes);
+  multiply<false, true>(gr, r.A2 + hb * r.KS2 * 2 * FRAG + lane * 8, 0, r.B2 + b0 * r.KS2 * 2 * FRAG, r.KS2 * 2 * FRAG, (int)r.pairs2, Bs, as_it_is, as_it_comes);
   const int e0 = exp_or_0(scale_exp(*a.w0)), e1 = exp_or_0(scale_exp(*a.w1)), e2 = exp_or_0(scale_exp(*r.w2));
   const Hidden at(a);
   float ma[NJ] = {}, mb[NJ] = {};
@@ -774,7 +782,8 @@ struct Ffn {
     const bool remake = bwd && !gate, d_w = dWg || dWu;
     // a row's share
     const int64_t own = 4 * (dp + (bwd && d_w ? dp : 0) + (bwd ? ep : 0) + (bwd && dWd ? ep : 0) + fp * (bwd ? 3 : 1));
-    const int64_t Rp = std::max<int64_t>(TM, std::min<int64_t>((int64_t)bytes / own / TM * TM, up_to(n, TM)));
+    static const char* er = getenv("HT_FFN_ROWS");
+    const int64_t Rp = std::max<int64_t>(TM, std::min<int64_t>(er ? atoll(er) : (int64_t)bytes / own / TM * TM, up_to(n, TM)));
     const int64_t Ra = Rp + REMAKE_ROWS;               // (the last tile of k_ffn_remake may go beyond Rp)
     const int64_t KSR = Rp / 16, pieces = ceil_div64(n, Rp);
     // tiles of the products, and parts of their reductions
