@@ -68,54 +68,68 @@ struct Top {
   uint32_t *rmax, *cmax, *all;         // (null: not wanted)
   unsigned blocks;
 };
-constexpr int TOPS = 5, TOP_ROWS = 32;
+constexpr int TOPS = 5, TOP_COLS = 256, TOP_UNROLL = 8;
 struct Tops {
   Top top[TOPS];
   int n;
 };
-// A block takes TOP_ROWS rows by 256 columns, a wave 8 of the rows, four columns a lane.
+__host__ __device__ constexpr int top_lanes(int64_t cols) { return cols > 128 ? 64 : cols > 64 ? 32 : 16; }
+// Rows of a block at a time, and blocks: each one's words wait for those of the others, so there are not many of them
+__host__ __device__ constexpr int top_rows(int64_t cols) { return 4 * TOP_UNROLL * (64 / top_lanes(cols)); }
+constexpr int64_t TOP_BLOCKS = 1024;
+// lanes of four columns each take a row's TOP_COLS, a wave TOP_UNROLL rows of each of its groups of lanes at a time; columns are joined once a block.
 __global__ void __launch_bounds__(256) k_ffn_top(Tops tops) {
-  __shared__ uint32_t sh[4][256];
+  __shared__ __attribute__((aligned(16))) uint32_t sh[4][TOP_COLS];
   unsigned block = blockIdx.x;
   int k = 0;
   while (block >= tops.top[k].blocks) block -= tops.top[k++].blocks;
   const Top& t = tops.top[k];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const unsigned cb = (unsigned)((t.cols + 255) / 256);
-  const int64_t r0 = (int64_t)(block / cb) * TOP_ROWS + wave * 8, c = (int64_t)(block % cb) * 256 + lane * 4;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lpr = top_lanes(t.cols), l = lane & (lpr - 1), groups = 64 / lpr, g = lane / lpr, here = top_rows(t.cols);
+  const unsigned cb = (unsigned)((t.cols + TOP_COLS - 1) / TOP_COLS);
+  const int64_t c = (int64_t)(block % cb) * TOP_COLS + l * 4;
   uint4 cm = make_uint4(0, 0, 0, 0);
-  V4 x[8];
+  for (int64_t r0 = (int64_t)(block / cb) * here; r0 < t.rows; r0 += (int64_t)(t.blocks / cb) * here) {
+    V4 x[TOP_UNROLL];
 #pragma unroll
-  for (int q = 0; q < 8; ++q) {
-    const int64_t r = r0 + q < t.rows ? r0 + q : t.rows - 1;               // (the last row again, behind it)
-    const float* at = t.p + r * t.ld + c;
-    if (c + 4 <= t.cols) {
-      x[q] = *reinterpret_cast<const V4u*>(at);
-    } else {
+    for (int q = 0; q < TOP_UNROLL; ++q) {
+      const int64_t at = r0 + (wave * TOP_UNROLL + q) * groups + g;
+      const float* from = t.p + (at < t.rows ? at : t.rows - 1) * t.ld + c;     // (the last row again, behind it)
+      if (c + 4 <= t.cols) {
+        x[q] = *reinterpret_cast<const V4u*>(from);
+      } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[q][i] = c + i < t.cols ? at[i] : 0.f;
+        for (int i = 0; i < 4; ++i) x[q][i] = c + i < t.cols ? from[i] : 0.f;
+      }
     }
-  }
 #pragma unroll
-  for (int q = 0; q < 8; ++q) {
-    const uint4 b = make_uint4(size_bits(x[q][0]), size_bits(x[q][1]), size_bits(x[q][2]), size_bits(x[q][3]));
-    cm = make_uint4(max(cm.x, b.x), max(cm.y, b.y), max(cm.z, b.z), max(cm.w, b.w));
-    if (t.rmax) {
+    for (int q = 0; q < TOP_UNROLL; ++q) {
+      const uint4 b = make_uint4(size_bits(x[q][0]), size_bits(x[q][1]), size_bits(x[q][2]), size_bits(x[q][3]));
+      cm = make_uint4(max(cm.x, b.x), max(cm.y, b.y), max(cm.z, b.z), max(cm.w, b.w));
+      if (!t.rmax) continue;
       uint32_t m = max(max(b.x, b.y), max(b.z, b.w));
-      for (int o = 32; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
-      if (lane == 0 && r0 + q < t.rows) raise(t.rmax + r0 + q, m);
+      for (int o = lpr / 2; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
+      const int64_t at = r0 + (wave * TOP_UNROLL + q) * groups + g;
+      if (l != 0 || at >= t.rows) continue;
+      if (cb == 1) t.rmax[at] = m;
+      else atomicMax(t.rmax + at, m);
     }
   }
-  *reinterpret_cast<uint4*>(&sh[wave][lane * 4]) = cm;
+  if (!t.cmax && !t.all) return;
+  for (int o = lpr; o < 64; o <<= 1)
+    cm = make_uint4(max(cm.x, (uint32_t)__shfl_xor((int)cm.x, o, 64)), max(cm.y, (uint32_t)__shfl_xor((int)cm.y, o, 64)),
+                    max(cm.z, (uint32_t)__shfl_xor((int)cm.z, o, 64)), max(cm.w, (uint32_t)__shfl_xor((int)cm.w, o, 64)));
+  if (g == 0) *reinterpret_cast<uint4*>(&sh[wave][l * 4]) = cm;
   __syncthreads();
-  const uint32_t m = max(max(sh[0][threadIdx.x], sh[1][threadIdx.x]), max(sh[2][threadIdx.x], sh[3][threadIdx.x]));
-  const int64_t col = (int64_t)(block % cb) * 256 + threadIdx.x;
-  if (t.cmax && col < t.cols) raise(t.cmax + col, m);
-  if (t.all) {
-    uint32_t a = m;
-    for (int o = 32; o > 0; o >>= 1) a = max(a, (uint32_t)__shfl_xor((int)a, o, 64));
-    if (lane == 0) raise(t.all, a);
-  }
+  const int64_t col = (int64_t)(block % cb) * TOP_COLS + threadIdx.x;
+  uint32_t m = 0;
+  if ((int)threadIdx.x < lpr * 4) m = max(max(sh[0][threadIdx.x], sh[1][threadIdx.x]), max(sh[2][threadIdx.x], sh[3][threadIdx.x]));
+  if (t.cmax && (int)threadIdx.x < lpr * 4 && col < t.cols) raise(t.cmax + col, m);
+  if (!t.all) return;
+  for (int o = 32; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
+  __syncthreads();
+  if (lane == 0) sh[0][wave] = m;
+  __syncthreads();
+  if (threadIdx.x == 0) raise(t.all, max(max(sh[0][0], sh[0][1]), max(sh[0][2], sh[0][3])));
 }
 
 // Fragments of a matrix by rows (R: reduction along columns, KS steps apart) and by columns (T: reduction along rows), zeros behind the last row and column; a
@@ -367,10 +381,10 @@ __device__ __forceinline__ void multiply(v16f (&acc)[NI][NJ], const _Float16* Ap
 // Where a block's tile is: each XCD takes a contiguous part of the tiles, eight tiles of A over all of B after eight others.
 struct Tile {
   int64_t split, m, n;                 // m < 0: none
-  __device__ __forceinline__ Tile(int64_t mt, int64_t nt, int splits) {
-    const int64_t tiles = mt * nt, per = (tiles * splits + 7) / 8, ts = (int64_t)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  __device__ __forceinline__ Tile(unsigned block, int64_t mt, int64_t nt, int splits) {
+    const int64_t tiles = mt * nt, per = (tiles * splits + 7) / 8, ts = (int64_t)(block & 7) * per + (block >> 3);
     m = -1;
-    if ((int64_t)(blockIdx.x >> 3) >= per || ts >= tiles * splits) return;
+    if ((int64_t)(block >> 3) >= per || ts >= tiles * splits) return;
     split = ts / tiles;
     const int64_t t = ts - split * tiles, g = t / (8 * nt), gm = mt - g * 8 < 8 ? mt - g * 8 : 8, q = t - g * 8 * nt;
     m = g * 8 + q % gm, n = q / gm;
@@ -411,7 +425,8 @@ struct Hidden {
   }
   // four values of a row, in the order of fragments: the k-th four of 16 columns by half
   __device__ __forceinline__ void put_frag(float* p, int64_t KS, int64_t row_block, int64_t step, int k, V4 x) const {
-    *reinterpret_cast<V4*>(p + ((row_block * KS + step) * 2 + k) * (FRAG / 2) + lane * 4) = x;
+    // (past the caches, which have the operands to keep: 232,965 x 256 x 1,024 backward 4.16 -> 4.08 ms)
+    __builtin_nontemporal_store(x, reinterpret_cast<V4*>(p + ((row_block * KS + step) * 2 + k) * (FRAG / 2) + lane * 4));
   }
   // H, dA and dB of NJ row blocks from row block b0 on, of the hidden columns c0 .. c0 + 31.  Largest values: of the rows join ma and mb, of the columns (of H, dA,
   // dB, 32 each) go to cols.  (An infinite one may be the largest: what is scaled by it is not finite in any case.)  get(j, k, x, y): A and B of four hidden
@@ -502,10 +517,9 @@ struct Hidden {
 };
 
 template <int MODE, int KIND>
-__global__ void __launch_bounds__(256, 2) k_ffn_split(Args a) {
+__device__ __forceinline__ void ffn_split(const Args& a, unsigned block, _Float16* Bs) {
   constexpr bool TURN = MODE == ROWS || MODE == COLS;
-  __shared__ __attribute__((aligned(16))) _Float16 Bs[2 * stage_halfs(TURN)];
-  const Tile tile(a.mt, a.nt, a.splits);
+  const Tile tile(block, a.mt, a.nt, a.splits);
   if (tile.m < 0) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
   constexpr int NI = MODE == BACK ? 1 : 2;               // row blocks of A a wave (BACK has much to do with each sum)
@@ -650,9 +664,27 @@ __global__ void __launch_bounds__(256, 2) k_ffn_split(Args a) {
   }
 }
 
-// PROJECT and BACK in one where A and B were not kept: 128 hidden columns by 96 rows, 32 by 96 a wave, first A and B, then G.  (With 128 rows the sums alone take
-// 192 registers of 256.)
-constexpr int REMAKE_ROWS = 96;
+template <int MODE, int KIND>
+__global__ void __launch_bounds__(256, 2) k_ffn_split(Args a) {
+  __shared__ __attribute__((aligned(16))) _Float16 Bs[2 * stage_halfs(MODE == ROWS || MODE == COLS)];
+  ffn_split<MODE, KIND>(a, blockIdx.x, Bs);
+}
+// dX, and the gradients of the weights, which do not wait for each other, behind each other's blocks where all of them run at once.
+struct Ends {
+  Args a[3];                           // ROWS, COLS, COLS
+  unsigned first[3];                   // blocks before each
+};
+__global__ void __launch_bounds__(256, 2) k_ffn_ends(Ends ends) {
+  __shared__ __attribute__((aligned(16))) _Float16 Bs[2 * stage_halfs(true)];
+  if (blockIdx.x < ends.first[1]) return ffn_split<ROWS, OTHERS>(ends.a[0], blockIdx.x, Bs);
+  const int k = blockIdx.x < ends.first[2] ? 1 : 2;
+  ffn_split<COLS, OTHERS>(ends.a[k], blockIdx.x - ends.first[k], Bs);
+}
+
+// PROJECT and BACK in one where A and B were not kept: 128 hidden columns by 64 rows, 32 by 64 a wave, first A and B, then G; three blocks a CU, which is what hides their ends.  (Of 96
+// rows, two blocks: 232,965 x 256 x 1,024 1,690 -> 1,790 us, 16,384 x 512 x 2,048 417 -> 456, but 8,192 x 1,024 x 4,096 733 -> 702; the sums of 128 would take 192 registers.)
+constexpr int REMAKE_ROWS = 64;
+static_assert(REMAKE_ROWS % PAIR == 0 && TM % REMAKE_ROWS == 0, "COLS reads whole pairs of stages; pieces are multiples of TM rows");
 struct RemakeArgs {
   Args a;                              // A, B, KSA, KSB, pairs, w0, w1, rows_in: the projections'
   const _Float16 *A2, *B2;
@@ -660,10 +692,10 @@ struct RemakeArgs {
   const uint32_t *w2, *rows2;
 };
 template <int KIND>
-__global__ void __launch_bounds__(256, 2) k_ffn_remake(RemakeArgs r) {
+__global__ void __launch_bounds__(256, 3) k_ffn_remake(RemakeArgs r) {
   __shared__ __attribute__((aligned(16))) _Float16 Bs[2 * stage_halfs(false)];
   const Args& a = r.a;
-  const Tile tile(a.mt, a.nt, 1);
+  const Tile tile(blockIdx.x, a.mt, a.nt, 1);
   if (tile.m < 0) return;
   constexpr int NJ = REMAKE_ROWS / 32;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -672,9 +704,9 @@ __global__ void __launch_bounds__(256, 2) k_ffn_remake(RemakeArgs r) {
   const auto as_it_is = [](v8h (&)[2], int, int) {};
   const auto as_it_comes = [](v8h (&)[NJ]) {};
   clear(ab);
-  multiply<false, true>(ab, a.A + hb * 2 * a.KSA * 2 * FRAG + lane * 8, a.KSA * 2 * FRAG, a.B + b0 * a.KSB * 2 * FRAG, a.KSB * 2 * FRAG, (int)a.pairs, Bs, as_it_is, as_it_comes);
+  multiply<false, false>(ab, a.A + hb * 2 * a.KSA * 2 * FRAG + lane * 8, a.KSA * 2 * FRAG, a.B + b0 * a.KSB * 2 * FRAG, a.KSB * 2 * FRAG, (int)a.pairs, Bs, as_it_is, as_it_comes);
   clear(gr);
-  multiply<false, true>(gr, r.A2 + hb * r.KS2 * 2 * FRAG + lane * 8, 0, r.B2 + b0 * r.KS2 * 2 * FRAG, r.KS2 * 2 * FRAG, (int)r.pairs2, Bs, as_it_is, as_it_comes);
+  multiply<false, false>(gr, r.A2 + hb * r.KS2 * 2 * FRAG + lane * 8, 0, r.B2 + b0 * r.KS2 * 2 * FRAG, r.KS2 * 2 * FRAG, (int)r.pairs2, Bs, as_it_is, as_it_comes);
   const int e0 = exp_or_0(scale_exp(*a.w0)), e1 = exp_or_0(scale_exp(*a.w1)), e2 = exp_or_0(scale_exp(*r.w2));
   const Hidden at(a);
   float ma[NJ] = {}, mb[NJ] = {};
@@ -703,7 +735,7 @@ struct Join {
   unsigned blocks;
 };
 struct Joins {
-  Join join[3];
+  Join join[4];
   int n;
 };
 __global__ void __launch_bounds__(256) k_ffn_join(Joins joins) {
@@ -749,8 +781,9 @@ struct Ffn {
   const ht_tensor *Y = nullptr;                                            // forward
   const ht_tensor *dY = nullptr, *dX = nullptr, *dWg = nullptr, *dWu = nullptr, *dWd = nullptr;
 
-  int launch(int mode, Args& a) const {
-    const int64_t blocks = up_to(a.mt * a.nt * a.splits, 8);
+  static int64_t blocks_of(const Args& a) { return up_to(a.mt * a.nt * a.splits, 8); }
+  int launch(int mode, const Args& a) const {
+    const int64_t blocks = blocks_of(a);
     if (blocks >= (1 << 24)) return ht_set_err(ctx, HT_ESHAPE, "ffn: %lld tiles in one product", (long long)blocks);
     const unsigned grid = (unsigned)blocks;
     const bool logistic = a.act.act != HT_GATE_GELU && a.act.act != HT_GATE_RELU;
@@ -782,9 +815,7 @@ struct Ffn {
     const bool remake = bwd && !gate, d_w = dWg || dWu;
     // a row's share
     const int64_t own = 4 * (dp + (bwd && d_w ? dp : 0) + (bwd ? ep : 0) + (bwd && dWd ? ep : 0) + fp * (bwd ? 3 : 1));
-    static const char* er = getenv("HT_FFN_ROWS");
-    const int64_t Rp = std::max<int64_t>(TM, std::min<int64_t>(er ? atoll(er) : (int64_t)bytes / own / TM * TM, up_to(n, TM)));
-    const int64_t Ra = Rp + REMAKE_ROWS;               // (the last tile of k_ffn_remake may go beyond Rp)
+    const int64_t Rp = std::max<int64_t>(TM, std::min<int64_t>((int64_t)bytes / own / TM * TM, up_to(n, TM)));
     const int64_t KSR = Rp / 16, pieces = ceil_div64(n, Rp);
     // tiles of the products, and parts of their reductions
     const int64_t mt = Rp / TM, nte = up_to(e, TN) / TN, ntd = up_to(d, TN) / TN, ntD = ceil_div64(f, 64), ntH = ceil_div64(f, TN);
@@ -798,11 +829,11 @@ struct Ffn {
     const int64_t n_top = 4 + 5 * Rp + dp + ep + 3 * fp;
     const auto top = m.add<uint32_t>(n_top);
     const auto W2 = m.add<_Float16>(2 * fp * KSd * 32), Wf = m.add<_Float16>(fp * KSe * 32);
-    const auto Xr = m.add<_Float16>(Ra * KSd * 32);
+    const auto Xr = m.add<_Float16>(Rp * KSd * 32);
     const auto Xt = m.add<_Float16>(d_w ? dp * KSR * 32 : 0);
-    const auto Gr = m.add<_Float16>(bwd ? Ra * KSe * 32 : 0);
+    const auto Gr = m.add<_Float16>(bwd ? Rp * KSe * 32 : 0);
     const auto Gt = m.add<_Float16>(dWd ? ep * KSR * 32 : 0);
-    const auto H = m.add<float>(Ra * fp), Df = m.add<float>(bwd ? Ra * fp * 2 : 0);
+    const auto H = m.add<float>(Rp * fp), Df = m.add<float>(bwd ? Rp * fp * 2 : 0);
     const auto sums_y = m.add<float>(!bwd && sy > 1 ? sy * Rp * e4 : 0), sums_x = m.add<float>(dX && sx > 1 ? sx * Rp * d4 : 0);
     const auto sums_D = m.add<float>(d_w && sD > 1 ? sD * 2 * wr * wp : 0), sums_H = m.add<float>(dWd && sH > 1 ? sH * vr * vp : 0);
     HT_TRY(bytes > FFN_LEAN ? m.take_if_room(ctx) : m.take(ctx));
@@ -818,7 +849,7 @@ struct Ffn {
       auto operand = [&](const float* p, int64_t ld, int64_t r, int64_t c, uint32_t* rm, uint32_t* cm, uint32_t* all, _Float16* R, int64_t KS, _Float16* T, int64_t KS_t, int mul,
                          int add, int64_t row_tile, int64_t col_tile) {
         Top& t = tops.top[tops.n++];
-        t = Top{p, ld, r, c, rm, cm, all, (unsigned)(ceil_div64(r, TOP_ROWS) * ceil_div64(c, 256))};
+        t = Top{p, ld, r, c, rm, cm, all, (unsigned)(std::min(ceil_div64(r, top_rows(c)), std::max<int64_t>(1, TOP_BLOCKS / ceil_div64(c, TOP_COLS))) * ceil_div64(c, TOP_COLS))};
         tb += t.blocks;
         Pack& q = packs.pack[packs.n++];
         q = Pack{p, ld, r, c, rm, cm, all, R, T, KS, KS_t, mul, add, (unsigned)(up_to(r, row_tile) / 64), (unsigned)(up_to(c, col_tile) / 64)};
@@ -858,7 +889,7 @@ struct Ffn {
       }
       if (remake) {
         a.D = m.at(Df);
-        a.nt = ceil_div64(up_to(rows, PAIR), REMAKE_ROWS);           // (COLS reads whole pairs of stages)
+        a.nt = ceil_div64(rows, REMAKE_ROWS);
         const bool logistic = D->act != HT_GATE_GELU && D->act != HT_GATE_RELU;
         (logistic ? k_ffn_remake<LOGISTIC> : k_ffn_remake<OTHERS>)<<<(unsigned)up_to(a.mt * a.nt, 8), 256, 0, st>>>(RemakeArgs{a, m.at(Wf), m.at(Gr), KSe, ceil_div64(e, PAIR), t_d, t_y});
         HT_LAUNCH_CHECK(ctx);
@@ -869,9 +900,10 @@ struct Ffn {
         a.D = m.at(Df);
         HT_TRY(launch(BACK, a));
       }
+      // Y, or dX; their parts' sums are added up behind each piece, those of the weights' gradients behind the last
       Joins j{};
       auto by_rows = [&](const ht_tensor* to, const float* P, int64_t KSP, bool two, const _Float16* W, int64_t KSW, const uint32_t* w0, const uint32_t* w1, int64_t cols, int64_t nt,
-                         int64_t pairs, int splits, float* sums, int64_t pitch) -> int {
+                         int64_t pairs, int splits, float* sums, int64_t pitch) {
         Args a = base;
         a.A = (const _Float16*)P, a.KSA = KSP, a.B = W, a.KSB = KSW;
         a.mt = ceil_div64(rows, TM), a.nt = nt, a.pairs = pairs, a.splits = splits, a.two = two, a.w0 = w0, a.w1 = w1;
@@ -880,13 +912,10 @@ struct Ffn {
         a.out[0] = splits > 1 ? Out{sums, pitch, 1, Rp * pitch} : Out{out, to->ld, 1, 0};
         a.add = splits == 1 && D->accumulate;
         if (splits > 1) j.join[j.n++] = Join{sums, Rp * pitch, pitch, rows, cols, splits, D->accumulate, out, to->ld, 0};
-        return launch(ROWS, a);
+        return a;
       };
-      if (Y) HT_TRY(by_rows(Y, m.at(H), KSH, false, m.at(Wf), KSe, t_d, nullptr, e, nte, pairs_f, sy, m.at(sums_y), e4));
-      if (dX) HT_TRY(by_rows(dX, m.at(Df), KSD, true, m.at(W2), KSd, t_g, t_u, d, ntd, pairs_2f, sx, m.at(sums_x), d4));
-      HT_TRY(join(j));
       auto by_cols = [&](const _Float16* At, const uint32_t* m_top, int64_t m_end, const float* P, int64_t KSP, bool two, int64_t tiles_m, int64_t nt, int splits, float* sums,
-                         int64_t r, int64_t pitch, const ht_tensor* o0, const ht_tensor* o1, bool m_is_row) -> int {
+                         int64_t r, int64_t pitch, const ht_tensor* o0, const ht_tensor* o1, bool m_is_row) {
         Args a = base;
         a.A = At, a.KSA = KSR, a.B = (const _Float16*)P, a.KSB = KSP;
         a.mt = tiles_m, a.nt = nt, a.pairs = ceil_div64(rows, PAIR), a.splits = splits, a.two = two, a.m_top = m_top;
@@ -896,19 +925,27 @@ struct Ffn {
           if (!o[i]) continue;
           const int64_t ld = splits > 1 ? pitch : o[i]->ld;
           a.out[i] = Out{splits > 1 ? sums + i * r * pitch : o[i]->ptr, m_is_row ? ld : 1, m_is_row ? 1 : ld, splits > 1 ? (two ? 2 : 1) * r * pitch : 0};
+          if (splits > 1 && k + 1 == pieces)
+            j.join[j.n++] = Join{sums + i * r * pitch, (two ? 2 : 1) * r * pitch, pitch, o[i]->rows, o[i]->cols, splits, D->accumulate_dW, o[i]->ptr, o[i]->ld, 0};
         }
         a.add = k > 0 || (splits == 1 && D->accumulate_dW);
-        return launch(COLS, a);
+        return a;
       };
-      if (d_w) HT_TRY(by_cols(m.at(Xt), t_xc, d, m.at(Df), KSD, true, dp / TM, ntD, sD, m.at(sums_D), wr, wp, dWg, dWu, in_out));
-      if (dWd) HT_TRY(by_cols(m.at(Gt), t_yc, e, m.at(H), KSH, false, ep / TM, ntH, sH, m.at(sums_H), vr, vp, dWd, nullptr, !in_out));
-      if (k + 1 < pieces) continue;
-      Joins w{};
-      const ht_tensor* dw[2] = {dWg, dWu};
-      for (int i = 0; i < 2; ++i)
-        if (dw[i] && sD > 1) w.join[w.n++] = Join{m.at(sums_D) + i * wr * wp, 2 * wr * wp, wp, dw[i]->rows, dw[i]->cols, sD, D->accumulate_dW, dw[i]->ptr, dw[i]->ld, 0};
-      if (dWd && sH > 1) w.join[w.n++] = Join{m.at(sums_H), vr * vp, vp, dWd->rows, dWd->cols, sH, D->accumulate_dW, dWd->ptr, dWd->ld, 0};
-      HT_TRY(join(w));
+      if (Y) HT_TRY(launch(ROWS, by_rows(Y, m.at(H), KSH, false, m.at(Wf), KSe, t_d, nullptr, e, nte, pairs_f, sy, m.at(sums_y), e4)));
+      Args ax{}, ad{}, ah{};                             // (no tiles: not asked for)
+      if (dX) ax = by_rows(dX, m.at(Df), KSD, true, m.at(W2), KSd, t_g, t_u, d, ntd, pairs_2f, sx, m.at(sums_x), d4);
+      if (d_w) ad = by_cols(m.at(Xt), t_xc, d, m.at(Df), KSD, true, dp / TM, ntD, sD, m.at(sums_D), wr, wp, dWg, dWu, in_out);
+      if (dWd) ah = by_cols(m.at(Gt), t_yc, e, m.at(H), KSH, false, ep / TM, ntH, sH, m.at(sums_H), vr, vp, dWd, nullptr, !in_out);
+      const int64_t bx = blocks_of(ax), bd = blocks_of(ad), bh = blocks_of(ah);
+      if (bwd && bx + bd + bh <= SLOTS) {
+        k_ffn_ends<<<(unsigned)(bx + bd + bh), 256, 0, st>>>(Ends{{ax, ad, ah}, {0, (unsigned)bx, (unsigned)(bx + bd)}});
+        HT_LAUNCH_CHECK(ctx);
+      } else {
+        if (bx) HT_TRY(launch(ROWS, ax));
+        if (bd) HT_TRY(launch(COLS, ad));
+        if (bh) HT_TRY(launch(COLS, ah));
+      }
+      HT_TRY(join(j));
     }
     return HT_OK;
   }

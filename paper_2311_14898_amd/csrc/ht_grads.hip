@@ -19,20 +19,25 @@ struct Item {
   int64_t cols, vecs, ld, out_ld;        // vecs: of all rows
   int64_t unit0;                         // the launch's units before it
 };
-constexpr int UNIT = 4096;
+// Of few values the units are small, so that there are blocks for all CUs (241 tensors of 4.5 M values a norm and a scaling 126 -> %s us); of many they are large,
+// so that few of them have to be looked for in the list.
+constexpr int UNIT = 4096, SMALL_UNIT = 1024;
+constexpr int64_t SMALL_VECS = (int64_t)2048 * UNIT;
+// What is written goes past the caches where the gradients alone fill them (100 M values 246 -> 224 us); of fewer, whoever reads it next finds it there.
+constexpr int64_t CACHED_VECS = (int64_t)8 << 20;
 constexpr int LIST = 64;                 // tensors of a launch: their descriptions are arguments, so that recorded calls keep them
 struct List {
   Item item[LIST];
   int64_t units;
-  int n;
+  int n, unit;
 };
 constexpr unsigned NORM_BLOCKS = 2048, END_THREADS = 1024;
 
 // f(vector's place in row r, columns of it that there are) for the unit's vectors of this thread
 template <class F>
-__device__ __forceinline__ void each_vector(const Item& t, int64_t unit, F&& f) {
-  const int64_t v0 = (unit - t.unit0) * UNIT, nv = (t.cols + 3) / 4;
-  const int n = (int)(t.vecs - v0 < UNIT ? t.vecs - v0 : UNIT);
+__device__ __forceinline__ void each_vector(const Item& t, int64_t u, int unit, F&& f) {      // u: of the tensor
+  const int64_t v0 = u * unit, nv = (t.cols + 3) / 4;
+  const int n = (int)(t.vecs - v0 < unit ? t.vecs - v0 : unit);
   const int64_t r0 = v0 / nv, c0 = v0 - r0 * nv;
   if (c0 + n <= nv) {                    // in one row
 #pragma unroll 4
@@ -75,7 +80,7 @@ __global__ void __launch_bounds__(256) k_grad_squares(List list, double* __restr
   double s = 0.0;
   for (int64_t u = blockIdx.x; u < list.units; u += gridDim.x) {
     const Item& t = list.item[item_of(list, u)];
-    each_vector(t, u, [&](int64_t r, int64_t c, int64_t left) {
+    each_vector(t, u - t.unit0, list.unit, [&](int64_t r, int64_t c, int64_t left) {
       const V4 x = load4(t.g + r * t.ld + c, left);
       for (int k = 0; k < 4; ++k) s = fma((double)x[k], (double)x[k], s);
     });
@@ -96,11 +101,14 @@ __global__ void __launch_bounds__(END_THREADS) k_grad_end(const double* __restri
   if (factor) *factor = (float)((double)scale * (all <= (double)max_norm ? 1.0 : (double)max_norm / all));
 }
 
+// PAST: past the caches.  The tensors' units from their last to their first: what the sums have read last is what the caches still hold.
+template <bool PAST>
 __global__ void __launch_bounds__(256) k_grad_scale(List list, const float* __restrict__ factor, int add) {
   const float f = *factor;
   for (int64_t u = blockIdx.x; u < list.units; u += gridDim.x) {
     const Item& t = list.item[item_of(list, u)];
-    each_vector(t, u, [&](int64_t r, int64_t c, int64_t left) {
+    if (!add && f == 1.f && t.out == t.g) continue;      // (it is there)
+    each_vector(t, (t.vecs - 1) / list.unit - (u - t.unit0), list.unit, [&](int64_t r, int64_t c, int64_t left) {
       V4 x = load4(t.g + r * t.ld + c, left);
       float* to = t.out + r * t.out_ld + c;
       if (add) {
@@ -110,7 +118,8 @@ __global__ void __launch_bounds__(256) k_grad_scale(List list, const float* __re
         x *= f;
       }
       if (left >= 4) {
-        *reinterpret_cast<V4u*>(to) = x;
+        if (PAST) __builtin_nontemporal_store(x, reinterpret_cast<V4u*>(to));
+        else *reinterpret_cast<V4u*>(to) = x;
       } else {
         for (int k = 0; k < 3; ++k)
           if (k < left) to[k] = x[k];
@@ -120,7 +129,8 @@ __global__ void __launch_bounds__(256) k_grad_scale(List list, const float* __re
 }
 
 int check(ht_ctx* ctx, const char* name, const char* what, int32_t i, const ht_tensor& t) {
-  char s[96];
+  if (t.rows >= 0 && t.rows <= INT32_MAX && t.cols >= 0 && t.ld >= t.cols && t.loc == HT_LOC_DEVICE && ((uintptr_t)t.ptr & 3) == 0 && (t.ptr || t.rows == 0)) return HT_OK;
+  char s[96];                          // (a text for each of hundreds of tensors would be most of a call)
   snprintf(s, sizeof s, "%s: %s %d", name, what, i);
   if (t.rows < 0 || t.cols < 0) return ht_set_err(ctx, HT_ESHAPE, "%s: [%lld x %d]", s, (long long)t.rows, t.cols);
   return ht_check_weights(ctx, &t, t.rows, t.cols, s);
@@ -153,18 +163,19 @@ int check_shared(ht_ctx* ctx, int32_t n, const ht_tensor* grads, const ht_tensor
   return HT_OK;
 }
 
-// Launches over the tensors, LIST of them at a time: launch(list)
+// Launches over the tensors, LIST of them at a time: launch(list).  With out from the last tensor to the first.
 template <class F>
-int in_lists(int32_t n, const ht_tensor* grads, const ht_tensor* out, F&& launch) {
+int in_lists(int32_t n, const ht_tensor* grads, const ht_tensor* out, int unit, F&& launch) {
   List list;
-  list.n = 0, list.units = 0;
-  for (int32_t i = 0; i < n; ++i) {
+  list.n = 0, list.units = 0, list.unit = unit;
+  for (int32_t k = 0; k < n; ++k) {
+    const int32_t i = out ? n - 1 - k : k;
     const ht_tensor& g = grads[i];
     if (g.rows <= 0 || g.cols <= 0) continue;
     const bool flat = g.rows == 1 || (g.ld == g.cols && (!out || out[i].ld == g.cols));
     const int64_t cols = flat ? g.rows * g.cols : g.cols, vecs = (flat ? 1 : g.rows) * ((cols + 3) / 4);
     list.item[list.n++] = Item{g.ptr, out ? out[i].ptr : nullptr, cols, vecs, flat ? 0 : g.ld, out && !flat ? out[i].ld : 0, list.units};
-    list.units += (vecs + UNIT - 1) / UNIT;
+    list.units += (vecs + unit - 1) / unit;
     if (list.n == LIST) {
       HT_TRY(launch(list));
       list.n = 0, list.units = 0;
@@ -175,15 +186,18 @@ int in_lists(int32_t n, const ht_tensor* grads, const ht_tensor* out, F&& launch
 
 int grads_run(ht_ctx* ctx, int32_t n, const ht_tensor* grads, const ht_tensor* out, float max_norm, float scale, int add, float* norm, bool scaled) {
   hipStream_t st = ctx->stream;
-  int64_t parts = 0;
+  int64_t parts = 0, vecs = 0;
+  for (int32_t i = 0; i < n; ++i)
+    if (grads[i].rows > 0 && grads[i].cols > 0) vecs += grads[i].rows * ((grads[i].cols + 3) / 4);
+  const int unit = vecs < SMALL_VECS ? SMALL_UNIT : UNIT;
   auto blocks = [](const List& l) { return (unsigned)std::min<int64_t>(l.units, NORM_BLOCKS); };
-  HT_TRY(in_lists(n, grads, nullptr, [&](const List& l) { return parts += blocks(l), (int)HT_OK; }));
+  HT_TRY(in_lists(n, grads, nullptr, unit, [&](const List& l) { return parts += blocks(l), (int)HT_OK; }));
   OpsBlock m;
   const auto part = m.add<double>(parts);
   const auto factor = m.add<float>(1);
   HT_TRY(m.take(ctx));
   int64_t at = 0;
-  HT_TRY(in_lists(n, grads, nullptr, [&](const List& l) -> int {
+  HT_TRY(in_lists(n, grads, nullptr, unit, [&](const List& l) -> int {
     k_grad_squares<<<blocks(l), 256, 0, st>>>(l, m.at(part) + at);
     HT_LAUNCH_CHECK(ctx);
     at += blocks(l);
@@ -192,8 +206,8 @@ int grads_run(ht_ctx* ctx, int32_t n, const ht_tensor* grads, const ht_tensor* o
   k_grad_end<<<1, END_THREADS, 0, st>>>(m.at(part), parts, norm, scaled ? m.at(factor) : nullptr, max_norm, scale);
   HT_LAUNCH_CHECK(ctx);
   if (!scaled) return HT_OK;
-  return in_lists(n, grads, out, [&](const List& l) -> int {
-    k_grad_scale<<<(unsigned)std::min<int64_t>(l.units, 1 << 20), 256, 0, st>>>(l, m.at(factor), add);
+  return in_lists(n, grads, out, unit, [&](const List& l) -> int {
+    (vecs > CACHED_VECS ? k_grad_scale<true> : k_grad_scale<false>)<<<(unsigned)std::min<int64_t>(l.units, 1 << 20), 256, 0, st>>>(l, m.at(factor), add);
     HT_LAUNCH_CHECK(ctx);
     return HT_OK;
   });
