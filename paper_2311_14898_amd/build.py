@@ -13,7 +13,7 @@ LIB = os.path.join(HERE, "libhongtu.so")
 OBJ = os.path.join(HERE, "_build")
 SOURCES = ["ht_core.hip", "ht_prims.hip", "ht_partition.hip", "ht_spmm.hip", "ht_dense.hip", "ht_gemm.hip", "ht_elem.hip",
            "ht_layer.hip", "ht_gat.hip", "ht_fused.hip", "ht_embed.hip", "ht_head.hip", "ht_head_few.hip", "ht_distill.hip",
-           "ht_ffn.hip", "ht_grads.hip"]
+           "ht_ffn.hip", "ht_ffn_few.hip", "ht_grads.hip"]
 FLAGS = ["-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17", "-Wall",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 

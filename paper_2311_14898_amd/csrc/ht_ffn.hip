@@ -8,36 +8,12 @@
 // read them split them as they load: no pass in between, and either scale as the reduction asks for it.
 #include <algorithm>
 
+#include "ht_ffn.h"
 #include "ht_split.h"
 
 namespace {
 
 constexpr int HB = 32;                 // hidden columns of a block: [gate, up] of interleaved operands
-
-// act(a) and its derivative.  Kernels are made for two kinds: s(u) with u = a (k1 + k3 a^2), times a but for the sigmoid itself, and the others.
-enum { LOGISTIC, OTHERS };
-struct Gate {
-  int act;
-  float k1, k3;
-  int alone;                           // s(u) itself
-};
-struct Act {
-  float v, s;
-};
-template <int KIND>
-__device__ __forceinline__ Act act_of(const Gate& g, float a) {
-  constexpr float LOG2E = 1.44269504088896340736f;
-  if constexpr (KIND == LOGISTIC) {
-    // exp(-|u|) gives s(u) and s(-u) = 1 - s(u) without cancellation
-    const float q = fminf(a * a, 1e30f), u = a * fmaf(g.k3, q, g.k1), du = fmaf(3.f * g.k3, q, g.k1);
-    const float e = __builtin_amdgcn_exp2f(-fabsf(u) * LOG2E), hi = __builtin_amdgcn_rcpf(1.f + e), lo = e * hi;
-    const float s = u >= 0.f ? hi : lo, v = a * s;
-    return g.alone ? Act{s, lo * hi} : Act{v, fmaf(v, (u >= 0.f ? lo : hi) * du, s)};
-  }
-  if (g.act == HT_GATE_RELU) return {a < 0.f ? 0.f : a, a > 0.f ? 1.f : a * 0.f};      // (NaN stays NaN)
-  const float phi = 0.5f * erfcf(-a * 0.70710678118654752f);
-  return {a * phi, fmaf(a * 0.39894228040143268f, __builtin_amdgcn_exp2f(a * a * (-0.5f * LOG2E)), phi)};
-}
 
 // ---------------------------------------------------------------- scales
 
@@ -725,24 +701,11 @@ __global__ void __launch_bounds__(256, 3) k_ffn_remake(RemakeArgs r) {
   at.back_tops<NJ, 4>(b0, tile.m * 4 * HB, ma, mb, cols, top);
 }
 
-// What products left in parts, added up in their order: out [rows x cols] (+)= the sum of `parts` blocks of [rows x pitch].
-struct Join {
-  const float* sums;
-  int64_t part, pitch, rows, cols;
-  int parts, add;
-  float* out;
-  int64_t ld;
-  unsigned blocks;
-};
-struct Joins {
-  Join join[4];
-  int n;
-};
-__global__ void __launch_bounds__(256) k_ffn_join(Joins joins) {
+__global__ void __launch_bounds__(256) k_ffn_join(FfnJoins joins) {
   unsigned block = blockIdx.x;
   int k = 0;
   while (block >= joins.join[k].blocks) block -= joins.join[k++].blocks;
-  const Join& a = joins.join[k];
+  const FfnJoin& a = joins.join[k];
   const int64_t nv = a.pitch / 4, i = (int64_t)block * 256 + threadIdx.x, r = i / nv, c = (i - r * nv) * 4;
   if (r >= a.rows || c >= a.cols) return;
   V4 s{0.f, 0.f, 0.f, 0.f};
@@ -767,26 +730,13 @@ constexpr int64_t LEAST_PAIRS = 4;                 // of a part of a reduction
 
 int parts_of(int64_t tiles, int64_t pairs) { return (int)std::max<int64_t>(1, std::min<int64_t>({SLOTS / tiles, pairs / LEAST_PAIRS, 64})); }
 
-Gate gate_of(int act) {
-  const float k = 1.5957691216057308f;             // 2 sqrt(2 / pi)
-  return act == HT_GATE_GELU_TANH ? Gate{act, k, 0.044715f * k, 0} : Gate{act, 1.f, 0.f, act == HT_GATE_SIGMOID};
-}
-
-// One of ht_ffn_fwd and ht_ffn_bwd
-struct Ffn {
-  ht_ctx* ctx;
-  const ht_ffn_desc* D;
-  const ht_tensor *X, *Wg, *Wu, *Wd;
-  const ht_tensor *gate = nullptr, *up = nullptr;
-  const ht_tensor *Y = nullptr;                                            // forward
-  const ht_tensor *dY = nullptr, *dX = nullptr, *dWg = nullptr, *dWu = nullptr, *dWd = nullptr;
-
+struct Ffn : FfnCall {
   static int64_t blocks_of(const Args& a) { return up_to(a.mt * a.nt * a.splits, 8); }
   int launch(int mode, const Args& a) const {
     const int64_t blocks = blocks_of(a);
     if (blocks >= (1 << 24)) return ht_set_err(ctx, HT_ESHAPE, "ffn: %lld tiles in one product", (long long)blocks);
     const unsigned grid = (unsigned)blocks;
-    const bool logistic = a.act.act != HT_GATE_GELU && a.act.act != HT_GATE_RELU;
+    const bool logistic = a.act.logistic();
     if (mode == PROJECT) (logistic ? k_ffn_split<PROJECT, LOGISTIC> : k_ffn_split<PROJECT, OTHERS>)<<<grid, 256, 0, ctx->stream>>>(a);
     else if (mode == BACK) (logistic ? k_ffn_split<BACK, LOGISTIC> : k_ffn_split<BACK, OTHERS>)<<<grid, 256, 0, ctx->stream>>>(a);
     else if (mode == ROWS) k_ffn_split<ROWS, OTHERS><<<grid, 256, 0, ctx->stream>>>(a);
@@ -794,21 +744,8 @@ struct Ffn {
     HT_LAUNCH_CHECK(ctx);
     return HT_OK;
   }
-  int join(Joins& j) const {
-    unsigned grid = 0;
-    for (int k = 0; k < j.n; ++k) {
-      Join& a = j.join[k];
-      a.blocks = (unsigned)ceil_div64(a.rows * (a.pitch / 4), 256);
-      grid += a.blocks;
-    }
-    if (grid == 0) return HT_OK;
-    k_ffn_join<<<grid, 256, 0, ctx->stream>>>(j);
-    HT_LAUNCH_CHECK(ctx);
-    return HT_OK;
-  }
-
   int run(size_t bytes) const {
-    const bool bwd = dY != nullptr, in_out = D->w_form == HT_W_IN_OUT;
+    const bool bwd = dY != nullptr, in_out = this->in_out();
     const int64_t n = X->rows, d = D->d_in, f = D->d_hidden, e = D->d_out;
     hipStream_t st = ctx->stream;
     const int64_t fp = up_to(f, 256), dp = up_to(d, TM), ep = up_to(e, TM), KSd = up_to(d, TN) / 16, KSe = up_to(e, TN) / 16, KSH = fp / 16, KSD = fp / 8;
@@ -890,7 +827,7 @@ struct Ffn {
       if (remake) {
         a.D = m.at(Df);
         a.nt = ceil_div64(rows, REMAKE_ROWS);
-        const bool logistic = D->act != HT_GATE_GELU && D->act != HT_GATE_RELU;
+        const bool logistic = a.act.logistic();
         (logistic ? k_ffn_remake<LOGISTIC> : k_ffn_remake<OTHERS>)<<<(unsigned)up_to(a.mt * a.nt, 8), 256, 0, st>>>(RemakeArgs{a, m.at(Wf), m.at(Gr), KSe, ceil_div64(e, PAIR), t_d, t_y});
         HT_LAUNCH_CHECK(ctx);
       } else if (bwd) {
@@ -901,7 +838,7 @@ struct Ffn {
         HT_TRY(launch(BACK, a));
       }
       // Y, or dX; their parts' sums are added up behind each piece, those of the weights' gradients behind the last
-      Joins j{};
+      FfnJoins j{};
       auto by_rows = [&](const ht_tensor* to, const float* P, int64_t KSP, bool two, const _Float16* W, int64_t KSW, const uint32_t* w0, const uint32_t* w1, int64_t cols, int64_t nt,
                          int64_t pairs, int splits, float* sums, int64_t pitch) {
         Args a = base;
@@ -911,7 +848,7 @@ struct Ffn {
         float* out = to->ptr + r0 * to->ld;
         a.out[0] = splits > 1 ? Out{sums, pitch, 1, Rp * pitch} : Out{out, to->ld, 1, 0};
         a.add = splits == 1 && D->accumulate;
-        if (splits > 1) j.join[j.n++] = Join{sums, Rp * pitch, pitch, rows, cols, splits, D->accumulate, out, to->ld, 0};
+        if (splits > 1) j.join[j.n++] = FfnJoin{sums, Rp * pitch, pitch, rows, cols, splits, D->accumulate, out, to->ld, 0};
         return a;
       };
       auto by_cols = [&](const _Float16* At, const uint32_t* m_top, int64_t m_end, const float* P, int64_t KSP, bool two, int64_t tiles_m, int64_t nt, int splits, float* sums,
@@ -926,7 +863,7 @@ struct Ffn {
           const int64_t ld = splits > 1 ? pitch : o[i]->ld;
           a.out[i] = Out{splits > 1 ? sums + i * r * pitch : o[i]->ptr, m_is_row ? ld : 1, m_is_row ? 1 : ld, splits > 1 ? (two ? 2 : 1) * r * pitch : 0};
           if (splits > 1 && k + 1 == pieces)
-            j.join[j.n++] = Join{sums + i * r * pitch, (two ? 2 : 1) * r * pitch, pitch, o[i]->rows, o[i]->cols, splits, D->accumulate_dW, o[i]->ptr, o[i]->ld, 0};
+            j.join[j.n++] = FfnJoin{sums + i * r * pitch, (two ? 2 : 1) * r * pitch, pitch, o[i]->rows, o[i]->cols, splits, D->accumulate_dW, o[i]->ptr, o[i]->ld, 0};
         }
         a.add = k > 0 || (splits == 1 && D->accumulate_dW);
         return a;
@@ -945,17 +882,18 @@ struct Ffn {
         if (bd) HT_TRY(launch(COLS, ad));
         if (bh) HT_TRY(launch(COLS, ah));
       }
-      HT_TRY(join(j));
+      HT_TRY(ht_ffn_join(ctx, j));
     }
     return HT_OK;
   }
   int call() const {
     if (X->rows == 0) {                // nothing to add up
-      Joins w{};
+      FfnJoins w{};
       for (const ht_tensor* t : {dWg, dWu, dWd})
-        if (t && !D->accumulate_dW) w.join[w.n++] = Join{nullptr, 0, up_to(t->cols, 4), t->rows, t->cols, 0, 0, t->ptr, t->ld, 0};
-      return join(w);
+        if (t && !D->accumulate_dW) w.join[w.n++] = FfnJoin{nullptr, 0, up_to(t->cols, 4), t->rows, t->cols, 0, 0, t->ptr, t->ld, 0};
+      return ht_ffn_join(ctx, w);
     }
+    if (X->rows <= HT_FFN_FEW) return ht_ffn_few(*this);
     const int rc = run(FFN_BYTES);
     return rc == HT_ENOMEM ? run(FFN_LEAN) : rc;      // (nothing has been launched by a call that is refused memory)
   }
@@ -1002,14 +940,26 @@ int check_block(ht_ctx* ctx, const char* call, const ht_ffn_desc* D, const ht_te
 
 }  // namespace
 
+int ht_ffn_join(ht_ctx* ctx, FfnJoins& j) {
+  unsigned grid = 0;
+  for (int k = 0; k < j.n; ++k) {
+    FfnJoin& a = j.join[k];
+    a.blocks = (unsigned)ceil_div64(a.rows * (a.pitch / 4), 256);
+    grid += a.blocks;
+  }
+  if (grid == 0) return HT_OK;
+  k_ffn_join<<<grid, 256, 0, ctx->stream>>>(j);
+  HT_LAUNCH_CHECK(ctx);
+  return HT_OK;
+}
+
 extern "C" int ht_ffn_fwd(ht_ctx* ctx, const ht_ffn_desc* desc, const ht_tensor* X, const ht_tensor* Wg, const ht_tensor* Wu, const ht_tensor* Wd, ht_tensor* Y, ht_tensor* gate,
                           ht_tensor* up) {
   if (!ctx) return HT_EINVAL;
   HT_TRY(check_block(ctx, "ht_ffn_fwd", desc, X, Wg, Wu, Wd, gate, up, Y));
   HT_TRY(check_apart(ctx, "ht_ffn_fwd", {{X, "X"}, {Wg, "Wg"}, {Wu, "Wu"}, {Wd, "Wd"}}, {{Y, "Y"}, {gate, "gate"}, {up, "up"}}));
   HT_HIP(ctx, hipSetDevice(ctx->device));
-  Ffn op{ctx, desc, X, Wg, Wu, Wd, gate, up};
-  op.Y = Y;
+  const Ffn op{{ctx, desc, X, Wg, Wu, Wd, gate, up, Y, nullptr, nullptr, nullptr, nullptr, nullptr}};
   return ht_with_room(ctx, [&]() -> int { return op.call(); });
 }
 
@@ -1025,7 +975,6 @@ extern "C" int ht_ffn_bwd(ht_ctx* ctx, const ht_ffn_desc* desc, const ht_tensor*
                      {{dX, "dX"}, {dWg, "dWg"}, {dWu, "dWu"}, {dWd, "dWd"}}));
   HT_HIP(ctx, hipSetDevice(ctx->device));
   if (!dX && !dWg && !dWu && !dWd) return HT_OK;
-  Ffn op{ctx, desc, X, Wg, Wu, Wd, gate, up};
-  op.dY = dY, op.dX = dX, op.dWg = dWg, op.dWu = dWu, op.dWd = dWd;
+  const Ffn op{{ctx, desc, X, Wg, Wu, Wd, gate, up, nullptr, dY, dX, dWg, dWu, dWd}};
   return ht_with_room(ctx, [&]() -> int { return op.call(); });
 }
