@@ -1,11 +1,13 @@
 // Gated feed-forward blocks:  A = X Wg ;  B = X Wu ;  H = act(A) * B ;  Y = H Wd, and their gradients:
 //   G = dY Wd^T ;  dA = G * B * act'(A) ;  dB = G * act(A) ;  dX = dA Wg^T + dB Wu^T ;  dWg = X^T dA ;  dWu = X^T dB ;  dWd = H^T dY
 //
-// All products are fp32 products on the fp16 matrix cores (ht_split.h).  X, dY and the weights are packed into fragments of split values first: by
-// rows, scaled by the largest of each row (of all of a weight); for the gradients of weights also by columns, scaled by the largest of each column.
-// The hidden columns of Wg and Wu lie interleaved by 32s, so that one product makes A and B of the same column in the same lane, and dA and dB are one operand
-// with a reduction over both.  H, dA and dB are kept in fp32, in the order of fragments, and with the largest values of their rows and columns; the products that
-// read them split them as they load: no pass in between, and either scale as the reduction asks for it.
+// All products are fp32 products on the fp16 matrix cores (ht_split.h).  X, dY and the weights are packed into fragments of split values first, in one launch that
+// reads them twice: 32 rows (of a weight 32 hidden columns) a block, scaled by the largest of each row (of a weight by that of the block); for the
+// gradients of weights X and dY also turned, scaled by the largest of the 32 rows.  The hidden columns of Wg and Wu lie interleaved by 32s, so that one product makes A and B of the
+// same column in the same lane, and dA and dB are one operand with a reduction over both.  H, dA and dB are kept in fp32, in the order of fragments, and with the largest
+// values of their rows and columns; the products that read them split them as they load, with no pass in between: by rows where the reduction is over
+// hidden columns, by columns where it is over rows.  A scale that changes along a reduction (of the other operand's 32s) is taken off what is split: a stage of a product is
+// 32 values of it.
 #include <algorithm>
 
 #include "ht_ffn.h"
@@ -17,8 +19,7 @@ constexpr int HB = 32;                 // hidden columns of a block: [gate, up] 
 
 // ---------------------------------------------------------------- scales
 
-// The exponent of the power of two that brings what has its largest absolute value in these bits to [2^14, 2^15).  Largest values are those of
-// what is finite: the rest becomes NaN in its split, and takes no bits off the others.  (NONE: there is nothing, or only zeros.)
+// The exponent of the power of two that brings what has its largest absolute value in these bits to [2^14, 2^15).  (NONE: there is nothing, or only zeros.)
 constexpr int NONE = 1 << 20;
 __device__ __forceinline__ int scale_exp(uint32_t bits) {
   if (bits == 0) return NONE;
@@ -27,128 +28,101 @@ __device__ __forceinline__ int scale_exp(uint32_t bits) {
 }
 __device__ __forceinline__ int exp_or_0(int e) { return e >= NONE ? 0 : e; }
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)((e < -126 ? -126 : e > 126 ? 126 : e) + 127) << 23); }
+// Of an operand the largest value is that of what is finite: the rest becomes NaN in its split, and takes no bits off the others.
 __device__ __forceinline__ uint32_t size_bits(float x) {
   const uint32_t b = __float_as_uint(fabsf(x));
   return b < 0x7f800000u ? b : 0u;
 }
-__device__ __forceinline__ void raise(uint32_t* word, uint32_t m) {       // (most find a word as large as it need be)
-  if (__hip_atomic_load(word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) < m) atomicMax(word, m);
-}
+__device__ __forceinline__ uint32_t max4(V4 x) { return max(max(size_bits(x[0]), size_bits(x[1])), max(size_bits(x[2]), size_bits(x[3]))); }
 
 // ---------------------------------------------------------------- operands
 
-// A matrix [rows x cols], pitch ld, of which the largest values are wanted: of each row, of each column, or of all of it (words that hold zeros).
-struct Top {
+// Fragments of a matrix: 32 of its own rows a block (or, turned, of its own columns: `own` and `run` are its rows and columns, or the other way round), zeros behind the last.
+struct Pack {
   const float* p;
-  int64_t ld, rows, cols;
-  uint32_t *rmax, *cmax, *all;         // (null: not wanted)
+  int64_t ld, own, run;
+  int turned;
+  int *e_own, *e_block;                // exponents: of each of the own (null: they have the block's), of the block
+  _Float16* F;                         // by own rows, reduction along run: row block b is number b mul + add, KS steps
+  int64_t KS;
+  int mul, add;
+  _Float16* T;                         // (nullable) by run, scaled by blocks, KS_t steps; own as the reduction
+  int64_t KS_t;
+  int tiles;                           // of PACK_RUN along run
   unsigned blocks;
 };
-constexpr int TOPS = 5, TOP_COLS = 256, TOP_UNROLL = 8;
-struct Tops {
-  Top top[TOPS];
+constexpr int PACKS = 5, PACK_RUN = 128;
+struct Packs {
+  Pack pack[PACKS];
   int n;
+  uint32_t* zero;                      // words that become 0, by the blocks behind
+  int64_t zeros;
 };
-__host__ __device__ constexpr int top_lanes(int64_t cols) { return cols > 128 ? 64 : cols > 64 ? 32 : 16; }
-// Rows of a block at a time, and blocks: each one's words wait for those of the others, so there are not many of them
-__host__ __device__ constexpr int top_rows(int64_t cols) { return 4 * TOP_UNROLL * (64 / top_lanes(cols)); }
-constexpr int64_t TOP_BLOCKS = 1024;
-// lanes of four columns each take a row's TOP_COLS, a wave TOP_UNROLL rows of each of its groups of lanes at a time; columns are joined once a block.
-__global__ void __launch_bounds__(256) k_ffn_top(Tops tops) {
-  __shared__ __attribute__((aligned(16))) uint32_t sh[4][TOP_COLS];
+constexpr unsigned ZEROS = 4096;       // a block
+__global__ void __launch_bounds__(256) k_ffn_pack(Packs packs) {
+  __shared__ float sh[HB][PACK_RUN + 1];
+  __shared__ uint32_t top[HB];
   unsigned block = blockIdx.x;
-  int k = 0;
-  while (block >= tops.top[k].blocks) block -= tops.top[k++].blocks;
-  const Top& t = tops.top[k];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lpr = top_lanes(t.cols), l = lane & (lpr - 1), groups = 64 / lpr, g = lane / lpr, here = top_rows(t.cols);
-  const unsigned cb = (unsigned)((t.cols + TOP_COLS - 1) / TOP_COLS);
-  const int64_t c = (int64_t)(block % cb) * TOP_COLS + l * 4;
-  uint4 cm = make_uint4(0, 0, 0, 0);
-  for (int64_t r0 = (int64_t)(block / cb) * here; r0 < t.rows; r0 += (int64_t)(t.blocks / cb) * here) {
-    V4 x[TOP_UNROLL];
+  int i = 0;
+  while (i < packs.n && block >= packs.pack[i].blocks) block -= packs.pack[i++].blocks;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l32 = lane & 31, half = lane >> 5;
+  if (i == packs.n) {
+    for (int64_t k = (int64_t)block * ZEROS + tid; k < packs.zeros && k < (int64_t)(block + 1) * ZEROS; k += 256) packs.zero[k] = 0;
+    return;
+  }
+  const Pack& a = packs.pack[i];
+  const int64_t own0 = (int64_t)block * HB, left = a.own - own0;               // (left may be <= 0: zeros)
+  if (tid < HB) top[tid] = 0;
+  __syncthreads();
+  if (!a.turned) {
+    // a wave eight rows
+    uint32_t m[8] = {};
+    for (int64_t c0 = 0; c0 < a.run; c0 += 256) {
+      const int64_t c = c0 + lane * 4;
 #pragma unroll
-    for (int q = 0; q < TOP_UNROLL; ++q) {
-      const int64_t at = r0 + (wave * TOP_UNROLL + q) * groups + g;
-      const float* from = t.p + (at < t.rows ? at : t.rows - 1) * t.ld + c;     // (the last row again, behind it)
-      if (c + 4 <= t.cols) {
-        x[q] = *reinterpret_cast<const V4u*>(from);
-      } else {
+      for (int q = 0; q < 8; ++q) {
+        if (wave * 8 + q >= left) continue;
+        const float* from = a.p + (own0 + wave * 8 + q) * a.ld + c;
+        if (c + 4 <= a.run) {
+          m[q] = max(m[q], max4(*reinterpret_cast<const V4u*>(from)));
+        } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[q][i] = c + i < t.cols ? from[i] : 0.f;
+          for (int k = 0; k < 3; ++k)
+            if (c + k < a.run) m[q] = max(m[q], size_bits(from[k]));
+        }
       }
     }
 #pragma unroll
-    for (int q = 0; q < TOP_UNROLL; ++q) {
-      const uint4 b = make_uint4(size_bits(x[q][0]), size_bits(x[q][1]), size_bits(x[q][2]), size_bits(x[q][3]));
-      cm = make_uint4(max(cm.x, b.x), max(cm.y, b.y), max(cm.z, b.z), max(cm.w, b.w));
-      if (!t.rmax) continue;
-      uint32_t m = max(max(b.x, b.y), max(b.z, b.w));
-      for (int o = lpr / 2; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
-      const int64_t at = r0 + (wave * TOP_UNROLL + q) * groups + g;
-      if (l != 0 || at >= t.rows) continue;
-      if (cb == 1) t.rmax[at] = m;
-      else atomicMax(t.rmax + at, m);
+    for (int q = 0; q < 8; ++q) {
+      for (int o = 32; o > 0; o >>= 1) m[q] = max(m[q], (uint32_t)__shfl_xor((int)m[q], o, 64));
+      if (lane == 0) top[wave * 8 + q] = m[q];
     }
-  }
-  if (!t.cmax && !t.all) return;
-  for (int o = lpr; o < 64; o <<= 1)
-    cm = make_uint4(max(cm.x, (uint32_t)__shfl_xor((int)cm.x, o, 64)), max(cm.y, (uint32_t)__shfl_xor((int)cm.y, o, 64)),
-                    max(cm.z, (uint32_t)__shfl_xor((int)cm.z, o, 64)), max(cm.w, (uint32_t)__shfl_xor((int)cm.w, o, 64)));
-  if (g == 0) *reinterpret_cast<uint4*>(&sh[wave][l * 4]) = cm;
-  __syncthreads();
-  const int64_t col = (int64_t)(block % cb) * TOP_COLS + threadIdx.x;
-  uint32_t m = 0;
-  if ((int)threadIdx.x < lpr * 4) m = max(max(sh[0][threadIdx.x], sh[1][threadIdx.x]), max(sh[2][threadIdx.x], sh[3][threadIdx.x]));
-  if (t.cmax && (int)threadIdx.x < lpr * 4 && col < t.cols) raise(t.cmax + col, m);
-  if (!t.all) return;
-  for (int o = 32; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
-  __syncthreads();
-  if (lane == 0) sh[0][wave] = m;
-  __syncthreads();
-  if (threadIdx.x == 0) raise(t.all, max(max(sh[0][0], sh[0][1]), max(sh[0][2], sh[0][3])));
-}
-
-// Fragments of a matrix by rows (R: reduction along columns, KS steps apart) and by columns (T: reduction along rows), zeros behind the last row and column; a
-// 64 x 64 tile a block.  Row block b of R is number b mul + add (so of T: its column blocks).
-struct Pack {
-  const float* p;
-  int64_t ld, rows, cols;
-  const uint32_t *rmax, *cmax, *all;   // scales: `all` of both, or rows for R and columns for T
-  _Float16 *R, *T;
-  int64_t KS, KS_t;
-  int mul, add;
-  unsigned row_tiles, col_tiles;
-};
-struct Packs {
-  Pack pack[TOPS];
-  int n;
-};
-__global__ void __launch_bounds__(256) k_ffn_pack(Packs packs) {
-  __shared__ float sh[64][65];
-  unsigned block = blockIdx.x;
-  int i = 0;
-  while (block >= packs.pack[i].row_tiles * packs.pack[i].col_tiles) block -= packs.pack[i].row_tiles * packs.pack[i].col_tiles, ++i;
-  const Pack& a = packs.pack[i];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, half = lane >> 5;
-  const int64_t r0 = (int64_t)(block / a.col_tiles) * 64, c0 = (int64_t)(block % a.col_tiles) * 64;
-  const int c4 = (lane & 15) * 4, rq = wave * 16 + (lane >> 4);
+  } else {
+    // eight lanes a row of 32 columns
+    uint32_t m = 0;
+    const int64_t c = own0 + (tid & 7) * 4;
+#pragma unroll 4
+    for (int64_t r = tid >> 3; r < a.run; r += 32) {
+      const float* from = a.p + r * a.ld + c;
+      if (c + 4 <= a.own) {
+        m = max(m, max4(*reinterpret_cast<const V4u*>(from)));
+      } else {
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    const int64_t r = r0 + rq + q * 4;
-    const float* at = a.p + (r < a.rows ? r : a.rows - 1) * a.ld + c0 + c4;
-    V4 y;
-    if (c0 + 64 <= a.cols) {
-      y = *reinterpret_cast<const V4u*>(at);
-    } else {
-#pragma unroll
-      for (int k = 0; k < 4; ++k) y[k] = c0 + c4 + k < a.cols ? at[k] : 0.f;
+        for (int k = 0; k < 3; ++k)
+          if (c + k < a.own) m = max(m, size_bits(from[k]));
+      }
     }
-    if (r >= a.rows) y = V4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int k = 0; k < 4; ++k) sh[rq + q * 4][c4 + k] = y[k];
+    for (int o = 32; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
+    if (lane == 0) top[wave] = m;      // (the others stay 0)
   }
   __syncthreads();
-  auto put = [&](_Float16* to, int64_t frag, const float* x) {
+  uint32_t all = top[l32];
+  for (int o = 16; o > 0; o >>= 1) all = max(all, (uint32_t)__shfl_xor((int)all, o, 64));
+  const int eb = exp_or_0(scale_exp(all)), eo = a.e_own ? exp_or_0(scale_exp(top[l32])) : eb;
+  if (tid < HB && a.e_own) a.e_own[own0 + tid] = eo;
+  if (tid == 0 && a.e_block) a.e_block[(int64_t)block * a.mul + a.add] = eb;
+  const float fb = pow2(eb), fo = pow2(eo);
+  auto put = [&](_Float16* to, int64_t frag, const float (&x)[8]) {
     v8h hi, lo;
 #pragma unroll
     for (int t = 0; t < 8; ++t) {
@@ -160,24 +134,49 @@ __global__ void __launch_bounds__(256) k_ffn_pack(Packs packs) {
     *reinterpret_cast<v8h*>(to + frag * 2 * FRAG + lane * 8) = hi;
     *reinterpret_cast<v8h*>(to + frag * 2 * FRAG + FRAG + lane * 8) = lo;
   };
-  const int b = wave >> 1;                        // row block of the tile; a wave takes two of its four steps
+  for (int tile = 0; tile < a.tiles; ++tile) {
+    const int64_t run0 = (int64_t)tile * PACK_RUN;
+    V4 y[4];
 #pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    const int ks = (wave & 1) * 2 + u, k = ks * 16 + half * 4;
-    float x[8];
-    if (a.R && c0 / 16 + ks < a.KS) {
-      const int r = b * 32 + l32;
-      const float f = pow2(exp_or_0(scale_exp(a.all ? *a.all : r0 + r < a.rows ? a.rmax[r0 + r] : 0u)));
+    for (int q = 0; q < 4; ++q) {
+      // 32 lanes a row of PACK_RUN, or eight a row of 32
+      const int r = a.turned ? q * 32 + (tid >> 3) : q * 8 + (tid >> 5), c4 = a.turned ? (tid & 7) * 4 : (tid & 31) * 4;
+      const int64_t row = (a.turned ? run0 : own0) + r, c = (a.turned ? own0 : run0) + c4, cols = a.turned ? a.own : a.run;
+      y[q] = V4{0.f, 0.f, 0.f, 0.f};
+      if (row >= (a.turned ? a.run : a.own)) continue;
+      const float* from = a.p + row * a.ld + c;
+      if (c + 4 <= cols) {
+        y[q] = *reinterpret_cast<const V4u*>(from);
+      } else {
 #pragma unroll
-      for (int t = 0; t < 8; ++t) x[t] = sh[r][k + (t >> 2) * 8 + (t & 3)] * f;
-      put(a.R, ((r0 / 32 + b) * a.mul + a.add) * a.KS + c0 / 16 + ks, x);
+        for (int k = 0; k < 3; ++k)
+          if (c + k < cols) y[q][k] = from[k];
+      }
     }
-    if (a.T && r0 / 16 + ks < a.KS_t) {
-      const int c = b * 32 + l32;
-      const float f = pow2(exp_or_0(scale_exp(a.all ? *a.all : c0 + c < a.cols ? a.cmax[c0 + c] : 0u)));
+    __syncthreads();
 #pragma unroll
-      for (int t = 0; t < 8; ++t) x[t] = sh[k + (t >> 2) * 8 + (t & 3)][c] * f;
-      put(a.T, ((c0 / 32 + b) * a.mul + a.add) * a.KS_t + r0 / 16 + ks, x);
+    for (int q = 0; q < 4; ++q) {
+      const int r = a.turned ? q * 32 + (tid >> 3) : q * 8 + (tid >> 5), c4 = a.turned ? (tid & 7) * 4 : (tid & 31) * 4;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (a.turned) sh[c4 + k][r] = y[q][k];
+        else sh[r][c4 + k] = y[q][k];
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int ks = wave * 2 + u, k = ks * 16 + half * 4;
+      float x[8];
+      if (run0 / 16 + ks < a.KS) {
+#pragma unroll
+        for (int t = 0; t < 8; ++t) x[t] = sh[l32][k + (t >> 2) * 8 + (t & 3)] * fo;
+        put(a.F, ((int64_t)block * a.mul + a.add) * a.KS + run0 / 16 + ks, x);
+      }
+      if (!a.T) continue;
+#pragma unroll
+      for (int t = 0; t < 8; ++t) x[t] = sh[u * 16 + half * 4 + (t >> 2) * 8 + (t & 3)][wave * 32 + l32] * fb;
+      put(a.T, (run0 / 32 + wave) * a.KS_t + (int64_t)block * 2 + u, x);
     }
   }
 }
@@ -202,10 +201,13 @@ struct Args {
   int splits;                          // parts of it
   Gate act;
   int two;                             // an operand is [dA dB]
-  // largest values: of the weights (gate or only one, up), of the rows of X or dY; of what is made or read by rows and by columns (H; or dA and dB)
-  const uint32_t *w0, *w1, *rows_in;
-  uint32_t *h_row, *a_row, *b_row, *h_col, *a_col, *b_col;
-  const uint32_t* m_top;               // COLS: of A's rows
+  // exponents: PROJECT of Wg and Wu by hidden blocks, interleaved, BACK of Wd; ROWS, COLS: of the other operand by stages of the reduction
+  const int* e_w;
+  const int* e_in;                     // PROJECT, BACK: of the rows of X, of dY
+  // largest values of what is made, less the exponents of what it will meet: by rows of H (Wd's: e_d), of dA and dB together (Wg's and Wu's), by columns of H (the rows'
+  // of dY by 32s: e_y), of dA and dB (of X: e_x)
+  uint32_t *h_row, *d_row, *h_col, *a_col, *b_col;
+  const int *e_d, *e_x, *e_y;
   int64_t n, f;                        // rows, hidden columns that there are
   float *H, *D;                        // in the order of fragments (null: not wanted)
   int64_t KSH, KSD;
@@ -216,12 +218,12 @@ struct Args {
   int add;
 };
 
-// Eight values (t = 0 .. 3 and 4 .. 7 where the planes will be), each times its factor, a power of two.  Two instructions a value: the compiler rounds each value twice where it
+// Eight values (t = 0 .. 3 and 4 .. 7 where the planes will be), times `all` and each times its factor, powers of two.  Two instructions a value: the compiler rounds each value twice where it
 // is left to itself (a pair's halves once more for themselves).
 template <class F>
-__device__ __forceinline__ void split8(v8h& p0, v8h& p1, F&& factor) {
+__device__ __forceinline__ void split8(v8h& p0, v8h& p1, float all, F&& factor) {
   typedef uint32_t v4i __attribute__((ext_vector_type(4)));
-  const V4 x = __builtin_bit_cast(V4, p0), y = __builtin_bit_cast(V4, p1);
+  const V4 x = __builtin_bit_cast(V4, p0) * all, y = __builtin_bit_cast(V4, p1) * all;
   v4i hi, lo;
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
@@ -253,9 +255,10 @@ __device__ __forceinline__ float max_over_32(const float (&x)[4]) {
 // a stage ahead (FAR) or a step, and B goes through LDS, which is filled a stage ahead.
 //   Ap   the wave's first row block, the lane's place in it; a_rows halfs from one row block to the next
 //   Bp   the tile's first row block (TURN: the tile's first 16 of the reduction's first row block); b_rows from one to the next
-//   in_a(x, i, cur)  what is done to a step's planes of row block i before they are used (cur: the stage's parity), in_b(rb): to what a wave brings of B
+//   in_a(x, i, e)  what is done to a step's planes of row block i before they are used, in_b(rb, e): to what a wave brings of B; e: the stage's exponent, of e_stage (TURN)
 template <bool TURN, bool FAR, int NI, int NJ, class InA, class InB>
-__device__ __forceinline__ void multiply(v16f (&acc)[NI][NJ], const _Float16* Ap, const int64_t a_rows, const _Float16* B, const int64_t b_rows, int todo, _Float16* Bs, InA&& in_a, InB&& in_b) {
+__device__ __forceinline__ void multiply(v16f (&acc)[NI][NJ], const _Float16* Ap, const int64_t a_rows, const _Float16* B, const int64_t b_rows, const int* e_stage, int todo, _Float16* Bs, InA&& in_a,
+                                         InB&& in_b) {
   static_assert(!TURN || NJ == 4, "a stage of a turned operand is 32 x 128");
   constexpr int STAGE = stage_halfs(TURN), RB = TURN ? 4 : NJ * KT * 2 / 4, AHEAD = FAR ? 2 * KT : 2;
   static_assert(FAR || KT == 2, "steps take turns");
@@ -270,6 +273,7 @@ __device__ __forceinline__ void multiply(v16f (&acc)[NI][NJ], const _Float16* Ap
   const _Float16* Bp = B + lane * 8;
   const int64_t b_step = TURN ? b_rows : KT * 2 * FRAG;
   v8h ra[AHEAD][NI][2], rb[RB];
+  int e = 0, e_next = 0;
   auto fetch_a = [&](int to) {        // the next step
 #pragma unroll
     for (int i = 0; i < NI; ++i)
@@ -281,9 +285,11 @@ __device__ __forceinline__ void multiply(v16f (&acc)[NI][NJ], const _Float16* Ap
 #pragma unroll
     for (int u = 0; u < RB; ++u) rb[u] = *reinterpret_cast<const v8h*>(Bp + b_at[u]);
     Bp += b_step;
+    if (TURN) e_next = *e_stage++;
   };
   auto stash = [&](int to) {
-    in_b(rb);
+    in_b(rb, e_next);
+    e = e_next;
 #pragma unroll
     for (int u = 0; u < RB; ++u)
       *reinterpret_cast<v8h*>(Bs + to * STAGE + (TURN ? ((wave * 4 + u) * 2 + half) * TURN_HALF + l32 * 8 : (wave * RB + u) * FRAG + lane * 8)) = rb[u];
@@ -307,7 +313,7 @@ __device__ __forceinline__ void multiply(v16f (&acc)[NI][NJ], const _Float16* Ap
   // (Loads have no condition, so that waits count only the loads that they wait for: the last stage fetches itself again.  The barriers to scheduling
   // keep them where they stand; they would be moved down to where they are used.)
   auto stage = [&](int cur, bool more) {
-    if (!more) Bp -= b_step;
+    if (!more) Bp -= b_step, e_stage -= TURN;
     if (FAR && !more) Ap -= KT * 2 * FRAG;
     v8h b[2][2];
     read_b(b[0], cur, 0);
@@ -327,7 +333,7 @@ __device__ __forceinline__ void multiply(v16f (&acc)[NI][NJ], const _Float16* Ap
           fetch_a(u ^ 1);
         }
 #pragma unroll
-        for (int i = 0; i < NI; ++i) in_a(x[i], i, cur);
+        for (int i = 0; i < NI; ++i) in_a(x[i], i, e);
       }
       if (k + 1 < NJ * KT) read_b(b[(k + 1) & 1], cur, k + 1);
       __builtin_amdgcn_sched_barrier(0);
@@ -354,6 +360,9 @@ __device__ __forceinline__ void multiply(v16f (&acc)[NI][NJ], const _Float16* Ap
   } while (todo > 0);
 }
 
+__device__ __forceinline__ void raise(uint32_t* word, uint32_t m) {       // (most find a word as large as it need be)
+  if (__hip_atomic_load(word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) < m) atomicMax(word, m);
+}
 // Where a block's tile is: each XCD takes a contiguous part of the tiles, eight tiles of A over all of B after eight others.
 struct Tile {
   int64_t split, m, n;                 // m < 0: none
@@ -404,11 +413,16 @@ struct Hidden {
     // (past the caches, which have the operands to keep: 232,965 x 256 x 1,024 backward 4.16 -> 4.08 ms)
     __builtin_nontemporal_store(x, reinterpret_cast<V4*>(p + ((row_block * KS + step) * 2 + k) * (FRAG / 2) + lane * 4));
   }
-  // H, dA and dB of NJ row blocks from row block b0 on, of the hidden columns c0 .. c0 + 31.  Largest values: of the rows join ma and mb, of the columns (of H, dA,
-  // dB, 32 each) go to cols.  (An infinite one may be the largest: what is scaled by it is not finite in any case.)  get(j, k, x, y): A and B of four hidden
-  // columns of a row, fetched four columns ahead; sums(j, k, e): G of one.
+  // H, dA and dB of NJ row blocks from row block b0 on, of the hidden block hb.  Largest values, less the exponents of what they will meet: of the rows of dA and dB
+  // together in md, of the columns (of H, dA, dB, 32 each) to cols.  (An infinite one may be the largest: what is scaled by it is not finite in any case.)  get(j, k, x, y): A
+  // and B of four hidden columns of a row, fetched four columns ahead; sums(j, k, e): G of one.
   template <int KIND, int NJ, class Get, class Sums>
-  __device__ __forceinline__ void back(int64_t b0, int64_t c0, float (&ma)[NJ], float (&mb)[NJ], float* cols, Get&& get, Sums&& sums) const {
+  __device__ __forceinline__ void back(int64_t b0, int64_t hb, float (&md)[NJ], float* cols, Get&& get, Sums&& sums) const {
+    const int64_t c0 = hb * HB;
+    float fx[NJ], fy[NJ], ma[NJ] = {}, mb[NJ] = {};
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) fx[j] = pow2(-a.e_x[b0 + j]), fy[j] = pow2(-a.e_y[b0 + j]);
+    const int eg = a.e_d[hb * 2], eu = a.e_d[hb * 2 + 1];
     const int l32 = lane & 31;
     const bool edge = (b0 + NJ) * 32 > a.n || c0 + 32 > a.f;
     V4 x[2][NJ], y[2][NJ];
@@ -440,7 +454,7 @@ struct Hidden {
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          ch[e] = fmaxf(ch[e], fabsf(h[e])), ca[e] = fmaxf(ca[e], fabsf(da[e])), cb[e] = fmaxf(cb[e], fabsf(db[e]));
+          ch[e] = fmaxf(ch[e], fabsf(h[e] * fy[j])), ca[e] = fmaxf(ca[e], fabsf(da[e] * fx[j])), cb[e] = fmaxf(cb[e], fabsf(db[e] * fx[j]));
           ma[j] = fmaxf(ma[j], fabsf(da[e])), mb[j] = fmaxf(mb[j], fabsf(db[e]));
         }
         put_frag(a.H, a.KSH, b0 + j, step, k & 1, h);
@@ -454,17 +468,19 @@ struct Hidden {
         to[0] = th, to[32] = ta, to[64] = tb;
       }
     }
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) md[j] = fmaxf(__builtin_amdgcn_ldexpf(ma[j], -eg), __builtin_amdgcn_ldexpf(mb[j], -eu));
   }
-  // What the four waves found, to where it is kept: cols, of HBS hidden blocks from hidden column c0 on, and ma and mb by way of top (8 NJ 32 words of LDS).  All words are
+  // What the four waves found, to where it is kept: cols, of HBS hidden blocks from hidden column c0 on, and md by way of top (4 NJ 32 words of LDS).  All words are
   // looked at together: each takes a trip to memory.
   template <int NJ, int HBS>
-  __device__ __forceinline__ void back_tops(int64_t b0, int64_t c0, const float (&ma)[NJ], const float (&mb)[NJ], const float* cols, float* top) const {
-    constexpr int R = NJ * 32, N = 2 * R + HBS * 96, U = (N + 255) / 256;
+  __device__ __forceinline__ void back_tops(int64_t b0, int64_t c0, const float (&md)[NJ], const float* cols, float* top) const {
+    constexpr int R = NJ * 32, N = R + HBS * 96, U = (N + 255) / 256;
     const int wave = threadIdx.x >> 6;
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
-      const float x = fmaxf(ma[j], __shfl_xor(ma[j], 32, 64)), y = fmaxf(mb[j], __shfl_xor(mb[j], 32, 64));
-      top[(wave * 2 + half) * R + j * 32 + (lane & 31)] = half ? y : x;
+      const float x = fmaxf(md[j], __shfl_xor(md[j], 32, 64));
+      if (half == 0) top[wave * R + j * 32 + lane] = x;
     }
     __syncthreads();
     uint32_t *word[U], is[U], was[U];
@@ -473,12 +489,11 @@ struct Hidden {
       const int i = u * 256 + threadIdx.x;
       word[u] = nullptr;
       float m = 0.f;
-      if (i < 2 * R) {
-        const int which = i / R, r = i % R;
-        m = fmaxf(fmaxf(top[which * R + r], top[(2 + which) * R + r]), fmaxf(top[(4 + which) * R + r], top[(6 + which) * R + r]));
-        if (b0 * 32 + r < a.n) word[u] = (which ? a.b_row : a.a_row) + b0 * 32 + r;
+      if (i < R) {
+        m = fmaxf(fmaxf(top[i], top[R + i]), fmaxf(top[2 * R + i], top[3 * R + i]));
+        if (b0 * 32 + i < a.n) word[u] = a.d_row + b0 * 32 + i;
       } else if (i < N) {
-        const int q = i - 2 * R, which = q / 32 % 3;
+        const int q = i - R, which = q / 32 % 3;
         const int64_t c = c0 + q / 96 * 32 + q % 32;
         m = cols[q];
         if (c < a.f) word[u] = (which == 0 ? a.h_col : which == 1 ? a.a_col : a.b_col) + c;
@@ -503,69 +518,56 @@ __device__ __forceinline__ void ffn_split(const Args& a, unsigned block, _Float1
   const int64_t s0 = a.pairs * split / a.splits * 2;                 // its first stage
   const int todo = __builtin_amdgcn_readfirstlane((int)(a.pairs * (split + 1) / a.splits - s0 / 2));
 
-  // exponents of the weights; of the rows of A (ROWS), of the columns that are split on the way to LDS (COLS)
-  const int e0 = exp_or_0(a.w0 ? scale_exp(*a.w0) : NONE), e1 = exp_or_0(a.w1 ? scale_exp(*a.w1) : NONE);
-  // of a row of H or [dA dB], times the weights that it meets: the smallest that its parts allow
-  auto row_exp = [&](int64_t v) {
-    int e = NONE * 2;
-    if (a.two) {
-      const int x = scale_exp(a.a_row[v]), y = scale_exp(a.b_row[v]);
-      if (x < NONE) e = x + e0;
-      if (y < NONE) e = min(e, y + e1);
-    } else {
-      const int x = scale_exp(a.h_row[v]);
-      if (x < NONE) e = x + e0;
-    }
-    return e >= NONE ? 0 : e;
-  };
-  // hidden column of column n of B, and which of the two
+  // exponents of a row of H or [dA dB] (ROWS), and of a column (COLS); hidden column of column n of B
+  auto row_exp = [&](int64_t v) { return exp_or_0(scale_exp((a.two ? a.d_row : a.h_row)[v])); };
   auto hidden = [&](int64_t n) { return a.two ? n / (2 * HB) * HB + n % HB : n; };
-  auto col_top = [&](int64_t n) -> uint32_t {
+  auto col_exp = [&](int64_t n) {
     const int64_t c = hidden(n);
-    if (c >= a.f) return 0u;
-    return !a.two ? a.h_col[c] : (n / HB) & 1 ? a.b_col[c] : a.a_col[c];
+    return c >= a.f ? 0 : exp_or_0(scale_exp(!a.two ? a.h_col[c] : (n / HB) & 1 ? a.b_col[c] : a.a_col[c]));
   };
   v16f acc[NI][4];
   clear(acc);
   const _Float16* Ap = a.A + (mw / 32 * a.KSA + s0 * KT) * 2 * FRAG + lane * 8;
   const _Float16* B = a.B + (TURN ? s0 * a.KSB + n0 / 16 : n0 / 32 * a.KSB + s0 * KT) * 2 * FRAG;
   const int64_t a_rows = a.KSA * 2 * FRAG, b_rows = a.KSB * 2 * FRAG;
-  const auto as_it_is = [](v8h (&)[2], int, int) {};
+  const auto a_as_it_is = [](v8h (&)[2], int, int) {};
+  const auto b_as_it_is = [](v8h (&)[4], int) {};
   if constexpr (MODE == ROWS) {
-    float fr[2][2];                    // (a stage's parity is which half of a hidden block [gate, up] it is)
+    int er[2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int e = row_exp(mw + i * 32 + l32);
-      fr[i][0] = pow2(e - e0), fr[i][1] = pow2(e - (a.two ? e1 : e0));
-    }
-    multiply<true, true>(acc, Ap, a_rows, B, b_rows, todo, Bs, [&](v8h (&x)[2], int i, int cur) { split8(x[0], x[1], [&](int) { return fr[i][cur]; }); }, [](v8h (&)[4]) {});
+    for (int i = 0; i < 2; ++i) er[i] = row_exp(mw + i * 32 + l32);
+    multiply<true, true>(acc, Ap, a_rows, B, b_rows, a.e_w + s0, todo, Bs, [&](v8h (&x)[2], int i, int e) {
+      const float f = pow2(er[i] - e);
+      split8(x[0], x[1], 1.f, [&](int) { return f; });
+    }, b_as_it_is);
   } else if constexpr (MODE == COLS) {
     float fc[2][8];
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int k = 0; k < 8; ++k) fc[u][k] = pow2(exp_or_0(scale_exp(col_top(n0 + wave * 32 + u * 16 + (k >> 2) * 8 + half * 4 + (k & 3)))));
-    multiply<true, true>(acc, Ap, a_rows, B, b_rows, todo, Bs, as_it_is, [&](v8h (&rb)[4]) {
+      for (int k = 0; k < 8; ++k) fc[u][k] = pow2(col_exp(n0 + wave * 32 + u * 16 + (k >> 2) * 8 + half * 4 + (k & 3)));
+    multiply<true, true>(acc, Ap, a_rows, B, b_rows, a.e_w + s0, todo, Bs, a_as_it_is, [&](v8h (&rb)[4], int e) {
+      const float f = pow2(-e);
 #pragma unroll
-      for (int u = 0; u < 2; ++u) split8(rb[u * 2], rb[u * 2 + 1], [&](int t) { return fc[u][t]; });
+      for (int u = 0; u < 2; ++u) split8(rb[u * 2], rb[u * 2 + 1], f, [&](int t) { return fc[u][t]; });
     });
   } else {
-    multiply<false, true>(acc, Ap, a_rows, B, b_rows, todo, Bs, as_it_is, [](v8h (&)[4]) {});
+    multiply<false, true>(acc, Ap, a_rows, B, b_rows, nullptr, todo, Bs, a_as_it_is, b_as_it_is);
   }
 
   // lane l32 + 32 half of a 32 x 32 tile has column l32 and the rows 8 (e / 4) + 4 half + e % 4
   if constexpr (MODE == ROWS || MODE == COLS) {
     // exponents of the rows and columns of sums, all of them looked up at once (where they are used, one after the other, each would be a trip to memory)
     int* ends = reinterpret_cast<int*>(Bs);
-    ends[tid] = m0 + tid < a.m_end ? (MODE == COLS ? exp_or_0(scale_exp(a.m_top[m0 + tid])) : row_exp(m0 + tid)) : 0;
-    if (MODE == COLS && tid < TN) ends[TM + tid] = exp_or_0(scale_exp(col_top(n0 + tid)));
+    if (MODE == ROWS) ends[tid] = m0 + tid < a.m_end ? row_exp(m0 + tid) : 0;
+    else if (tid < TN) ends[tid] = col_exp(n0 + tid);
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int64_t n = n0 + j * 32 + l32, c = MODE == COLS ? hidden(n) : n;
       const Out& o = a.out[MODE == COLS && a.two ? j & 1 : 0];
       if (!o.p || c >= a.n_end) continue;
-      const int en = MODE == COLS ? ends[TM + j * 32 + l32] : 0;
+      const int en = MODE == COLS ? ends[j * 32 + l32] : 0;
       float* at = o.p + split * o.split_part + c * o.ns;
 #pragma unroll
       for (int i = 0; i < 2; ++i)
@@ -573,7 +575,7 @@ __device__ __forceinline__ void ffn_split(const Args& a, unsigned block, _Float1
         for (int k = 0; k < 4; ++k) {
           const int r = wave * 64 + i * 32 + k * 8 + half * 4;
           const int64_t m = m0 + r;
-          const int4 em = *reinterpret_cast<const int4*>(ends + r);
+          const int4 em = MODE == ROWS ? *reinterpret_cast<const int4*>(ends + r) : make_int4(0, 0, 0, 0);
           V4 x{__builtin_amdgcn_ldexpf(acc[i][j][k * 4], -(em.x + en)), __builtin_amdgcn_ldexpf(acc[i][j][k * 4 + 1], -(em.y + en)),
                __builtin_amdgcn_ldexpf(acc[i][j][k * 4 + 2], -(em.z + en)), __builtin_amdgcn_ldexpf(acc[i][j][k * 4 + 3], -(em.w + en))};
           float* to = at + m * o.ms;
@@ -595,7 +597,8 @@ __device__ __forceinline__ void ffn_split(const Args& a, unsigned block, _Float1
     const int64_t c0 = mw / 2;                          // the wave's 32 hidden columns
     int exps[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) exps[j] = exp_or_0(scale_exp(n0 + j * 32 + l32 < a.n ? a.rows_in[n0 + j * 32 + l32] : 0u));
+    for (int j = 0; j < 4; ++j) exps[j] = a.e_in[n0 + j * 32 + l32];
+    const int e0 = a.e_w[c0 / HB * 2], e1 = a.e_w[c0 / HB * 2 + 1], ed = a.e_d[c0 / HB];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int64_t v = n0 + j * 32 + l32;
@@ -616,27 +619,28 @@ __device__ __forceinline__ void ffn_split(const Args& a, unsigned block, _Float1
         at.put_frag(a.H, a.KSH, n0 / 32 + j, c0 / 16 + (k >> 1), k & 1, h);
       }
       m = fmaxf(m, __shfl_xor(m, 32, 64));
-      if (half == 0) top[wave * TN + j * 32 + l32] = m;
+      if (half == 0) top[wave * TN + j * 32 + l32] = __builtin_amdgcn_ldexpf(m, -ed);
     }
     __syncthreads();
     if (tid < TN && n0 + tid < a.n) raise(a.h_row + n0 + tid, __float_as_uint(fmaxf(fmaxf(top[tid], top[TN + tid]), fmaxf(top[2 * TN + tid], top[3 * TN + tid]))));
   }
   if constexpr (MODE == BACK) {
-    float ma[4] = {}, mb[4] = {};
-    float* cols = top + 8 * TN;
+    float md[4];
+    float* cols = top + 4 * TN;
     int ey[4];
+    const int e0 = a.e_w[mw / HB];
     const float *gate[4], *up[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int64_t v = n0 + j * 32 + l32, row = v < a.n ? v : a.n - 1;
-      ey[j] = exp_or_0(scale_exp(a.rows_in[row]));
+      ey[j] = a.e_in[v];
       gate[j] = a.gate + row * a.ld_gate, up[j] = a.up + row * a.ld_up;
     }
-    at.back<KIND, 4>(n0 / 32, mw, ma, mb, cols + wave * 96, [&](int j, int k, V4& x, V4& y) {
+    at.back<KIND, 4>(n0 / 32, mw / HB, md, cols + wave * 96, [&](int j, int k, V4& x, V4& y) {
       const int64_t c = mw + k * 8 + half * 4;
       x = at.get(gate[j], c), y = at.get(up[j], c);
     }, [&](int j, int k, int e) { return __builtin_amdgcn_ldexpf(acc[0][j][k * 4 + e], -(ey[j] + e0)); });
-    at.back_tops<4, 4>(n0 / 32, m0, ma, mb, cols, top);
+    at.back_tops<4, 4>(n0 / 32, m0, md, cols, top);
   }
 }
 
@@ -662,10 +666,10 @@ __global__ void __launch_bounds__(256, 2) k_ffn_ends(Ends ends) {
 constexpr int REMAKE_ROWS = 64;
 static_assert(REMAKE_ROWS % PAIR == 0 && TM % REMAKE_ROWS == 0, "COLS reads whole pairs of stages; pieces are multiples of TM rows");
 struct RemakeArgs {
-  Args a;                              // A, B, KSA, KSB, pairs, w0, w1, rows_in: the projections'
+  Args a;                              // A, B, KSA, KSB, pairs, e_w, e_in: the projections'
   const _Float16 *A2, *B2;
   int64_t KS2, pairs2;
-  const uint32_t *w2, *rows2;
+  const int *e_w2, *e_in2;
 };
 template <int KIND>
 __global__ void __launch_bounds__(256, 3) k_ffn_remake(RemakeArgs r) {
@@ -677,28 +681,25 @@ __global__ void __launch_bounds__(256, 3) k_ffn_remake(RemakeArgs r) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t hb = tile.m * 4 + wave, b0 = tile.n * NJ;            // the wave's hidden block, the tile's first row block
   v16f ab[2][NJ], gr[1][NJ];
-  const auto as_it_is = [](v8h (&)[2], int, int) {};
-  const auto as_it_comes = [](v8h (&)[NJ]) {};
+  const auto a_as_it_is = [](v8h (&)[2], int, int) {};
+  const auto b_as_it_is = [](v8h (&)[NJ], int) {};
   clear(ab);
-  multiply<false, false>(ab, a.A + hb * 2 * a.KSA * 2 * FRAG + lane * 8, a.KSA * 2 * FRAG, a.B + b0 * a.KSB * 2 * FRAG, a.KSB * 2 * FRAG, (int)a.pairs, Bs, as_it_is, as_it_comes);
+  multiply<false, false>(ab, a.A + hb * 2 * a.KSA * 2 * FRAG + lane * 8, a.KSA * 2 * FRAG, a.B + b0 * a.KSB * 2 * FRAG, a.KSB * 2 * FRAG, nullptr, (int)a.pairs, Bs, a_as_it_is, b_as_it_is);
   clear(gr);
-  multiply<false, false>(gr, r.A2 + hb * r.KS2 * 2 * FRAG + lane * 8, 0, r.B2 + b0 * r.KS2 * 2 * FRAG, r.KS2 * 2 * FRAG, (int)r.pairs2, Bs, as_it_is, as_it_comes);
-  const int e0 = exp_or_0(scale_exp(*a.w0)), e1 = exp_or_0(scale_exp(*a.w1)), e2 = exp_or_0(scale_exp(*r.w2));
+  multiply<false, false>(gr, r.A2 + hb * r.KS2 * 2 * FRAG + lane * 8, 0, r.B2 + b0 * r.KS2 * 2 * FRAG, r.KS2 * 2 * FRAG, nullptr, (int)r.pairs2, Bs, a_as_it_is, b_as_it_is);
+  const int e0 = a.e_w[hb * 2], e1 = a.e_w[hb * 2 + 1], e2 = r.e_w2[hb];
   const Hidden at(a);
-  float ma[NJ] = {}, mb[NJ] = {};
-  float *top = reinterpret_cast<float*>(Bs), *cols = top + 8 * NJ * 32;
+  float md[NJ];
+  float *top = reinterpret_cast<float*>(Bs), *cols = top + 4 * NJ * 32;
   int ex[NJ], ey[NJ];
 #pragma unroll
-  for (int j = 0; j < NJ; ++j) {
-    const int64_t v = (b0 + j) * 32 + (lane & 31), row = v < a.n ? v : a.n - 1;
-    ex[j] = exp_or_0(scale_exp(a.rows_in[row])), ey[j] = exp_or_0(scale_exp(r.rows2[row]));
-  }
-  at.back<KIND, NJ>(b0, hb * HB, ma, mb, cols + wave * 96, [&](int j, int k, V4& x, V4& y) {
+  for (int j = 0; j < NJ; ++j) ex[j] = a.e_in[(b0 + j) * 32 + (lane & 31)], ey[j] = r.e_in2[(b0 + j) * 32 + (lane & 31)];
+  at.back<KIND, NJ>(b0, hb, md, cols + wave * 96, [&](int j, int k, V4& x, V4& y) {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       x[e] = __builtin_amdgcn_ldexpf(ab[0][j][k * 4 + e], -(ex[j] + e0)), y[e] = __builtin_amdgcn_ldexpf(ab[1][j][k * 4 + e], -(ex[j] + e1));
   }, [&](int j, int k, int e) { return __builtin_amdgcn_ldexpf(gr[0][j][k * 4 + e], -(ey[j] + e2)); });
-  at.back_tops<NJ, 4>(b0, tile.m * 4 * HB, ma, mb, cols, top);
+  at.back_tops<NJ, 4>(b0, tile.m * 4 * HB, md, cols, top);
 }
 
 __global__ void __launch_bounds__(256) k_ffn_join(FfnJoins joins) {
@@ -763,8 +764,9 @@ struct Ffn : FfnCall {
     const int64_t wr = in_out ? d : f, wp = in_out ? f4 : d4, vr = in_out ? f : e, vp = in_out ? e4 : f4;
 
     OpsBlock m;
-    const int64_t n_top = 4 + 5 * Rp + dp + ep + 3 * fp;
+    const int64_t n_top = 2 * Rp + 3 * fp;                 // largest values: rows of H, of dA and dB, columns of H, dA, dB
     const auto top = m.add<uint32_t>(n_top);
+    const auto ex = m.add<int>(Rp), ey = m.add<int>(Rp), exb = m.add<int>(Rp / HB), eyb = m.add<int>(Rp / HB), ew2 = m.add<int>(2 * fp / HB), ewd = m.add<int>(fp / HB);
     const auto W2 = m.add<_Float16>(2 * fp * KSd * 32), Wf = m.add<_Float16>(fp * KSe * 32);
     const auto Xr = m.add<_Float16>(Rp * KSd * 32);
     const auto Xt = m.add<_Float16>(d_w ? dp * KSR * 32 : 0);
@@ -775,43 +777,33 @@ struct Ffn : FfnCall {
     const auto sums_D = m.add<float>(d_w && sD > 1 ? sD * 2 * wr * wp : 0), sums_H = m.add<float>(dWd && sH > 1 ? sH * vr * vp : 0);
     HT_TRY(bytes > FFN_LEAN ? m.take_if_room(ctx) : m.take(ctx));
 
-    uint32_t *t_g = m.at(top), *t_u = t_g + 1, *t_d = t_g + 2, *t_x = t_g + 4, *t_y = t_x + Rp, *t_h = t_y + Rp, *t_a = t_h + Rp, *t_b = t_a + Rp, *t_xc = t_b + Rp, *t_yc = t_xc + dp,
-             *t_hc = t_yc + ep, *t_ac = t_hc + fp, *t_bc = t_ac + fp;
+    uint32_t *t_h = m.at(top), *t_d = t_h + Rp, *t_hc = t_d + Rp, *t_ac = t_hc + fp, *t_bc = t_ac + fp;
     for (int64_t k = 0; k < pieces; ++k) {
       const int64_t r0 = k * Rp, rows = std::min(Rp, n - r0);
-      HT_TRY(ht_fill_zero(ctx, st, k ? t_x : t_g, (size_t)(k ? n_top - 4 : n_top) * 4));
-      Tops tops{};
       Packs packs{};
-      unsigned tb = 0, pb = 0;
-      auto operand = [&](const float* p, int64_t ld, int64_t r, int64_t c, uint32_t* rm, uint32_t* cm, uint32_t* all, _Float16* R, int64_t KS, _Float16* T, int64_t KS_t, int mul,
-                         int add, int64_t row_tile, int64_t col_tile) {
-        Top& t = tops.top[tops.n++];
-        t = Top{p, ld, r, c, rm, cm, all, (unsigned)(std::min(ceil_div64(r, top_rows(c)), std::max<int64_t>(1, TOP_BLOCKS / ceil_div64(c, TOP_COLS))) * ceil_div64(c, TOP_COLS))};
-        tb += t.blocks;
-        Pack& q = packs.pack[packs.n++];
-        q = Pack{p, ld, r, c, rm, cm, all, R, T, KS, KS_t, mul, add, (unsigned)(up_to(r, row_tile) / 64), (unsigned)(up_to(c, col_tile) / 64)};
-        pb += q.row_tiles * q.col_tiles;
+      unsigned blocks = 0;
+      auto operand = [&](Pack q, int64_t own, int64_t run) {           // zeros up to so many of either
+        q.tiles = (int)ceil_div64(run, PACK_RUN), q.blocks = (unsigned)(own / HB);
+        blocks += q.blocks;
+        packs.pack[packs.n++] = q;
       };
-      operand(X->ptr + r0 * X->ld, X->ld, rows, d, t_x, d_w ? t_xc : nullptr, nullptr, m.at(Xr), KSd, d_w ? m.at(Xt) : nullptr, KSR, 1, 0, TM, d_w ? TM : TN);
+      operand(Pack{X->ptr + r0 * X->ld, X->ld, rows, d, 0, m.at(ex), m.at(exb), m.at(Xr), KSd, 1, 0, d_w ? m.at(Xt) : nullptr, KSR, 0, 0}, up_to(rows, TM), d_w ? dp : KSd * 16);
       if (bwd)
-        operand(dY->ptr + r0 * dY->ld, dY->ld, rows, e, t_y, dWd ? t_yc : nullptr, nullptr, m.at(Gr), KSe, dWd ? m.at(Gt) : nullptr, KSR, 1, 0, TM, dWd ? TM : TN);
+        operand(Pack{dY->ptr + r0 * dY->ld, dY->ld, rows, e, 0, m.at(ey), m.at(eyb), m.at(Gr), KSe, 1, 0, dWd ? m.at(Gt) : nullptr, KSR, 0, 0}, up_to(rows, TM), dWd ? ep : KSe * 16);
       if (k == 0) {
         // by hidden columns: the rows of an OUT_IN Wg, the columns of an IN_OUT one
-        const ht_tensor* w[2] = {Wg, Wu};
-        for (int i = 0; i < 2; ++i)
-          operand(w[i]->ptr, w[i]->ld, w[i]->rows, w[i]->cols, nullptr, nullptr, t_g + i, in_out ? nullptr : m.at(W2), KSd, in_out ? m.at(W2) : nullptr, KSd, 2, i, in_out ? TN : TM,
-                  in_out ? TM : TN);
-        operand(Wd->ptr, Wd->ld, Wd->rows, Wd->cols, nullptr, nullptr, t_d, in_out ? m.at(Wf) : nullptr, KSe, in_out ? nullptr : m.at(Wf), KSe, 1, 0, in_out ? TM : TN,
-                in_out ? TN : TM);
+        operand(Pack{Wg->ptr, Wg->ld, f, d, in_out, nullptr, m.at(ew2), m.at(W2), KSd, 2, 0, nullptr, 0, 0, 0}, fp, KSd * 16);
+        operand(Pack{Wu->ptr, Wu->ld, f, d, in_out, nullptr, m.at(ew2), m.at(W2), KSd, 2, 1, nullptr, 0, 0, 0}, fp, KSd * 16);
+        operand(Pack{Wd->ptr, Wd->ld, f, e, !in_out, nullptr, m.at(ewd), m.at(Wf), KSe, 1, 0, nullptr, 0, 0, 0}, fp, KSe * 16);
       }
-      k_ffn_top<<<tb, 256, 0, st>>>(tops);
-      HT_LAUNCH_CHECK(ctx);
-      k_ffn_pack<<<pb, 256, 0, st>>>(packs);
+      packs.zero = t_h, packs.zeros = n_top;
+      k_ffn_pack<<<blocks + (unsigned)ceil_div64(n_top, ZEROS), 256, 0, st>>>(packs);
       HT_LAUNCH_CHECK(ctx);
 
       Args base{};
       base.act = gate_of(D->act), base.n = rows, base.f = f, base.splits = 1;
-      base.h_row = t_h, base.a_row = t_a, base.b_row = t_b, base.h_col = t_hc, base.a_col = t_ac, base.b_col = t_bc;
+      base.h_row = t_h, base.d_row = t_d, base.h_col = t_hc, base.a_col = t_ac, base.b_col = t_bc;
+      base.e_x = m.at(exb), base.e_y = m.at(eyb);
       base.KSH = KSH, base.KSD = KSD;
       base.gate = gate ? gate->ptr + r0 * gate->ld : nullptr, base.ld_gate = gate ? gate->ld : 0;
       base.up = up ? up->ptr + r0 * up->ld : nullptr, base.ld_up = up ? up->ld : 0;
@@ -821,29 +813,29 @@ struct Ffn : FfnCall {
       if (!bwd || remake) {
         a.A = m.at(W2), a.KSA = KSd, a.B = m.at(Xr), a.KSB = KSd;
         a.mt = ceil_div64(f, TN), a.nt = row_tiles, a.pairs = ceil_div64(d, PAIR);
-        a.w0 = t_g, a.w1 = t_u, a.rows_in = t_x;
+        a.e_w = m.at(ew2), a.e_in = m.at(ex);
+        a.e_d = m.at(ewd);
         if (!bwd) HT_TRY(launch(PROJECT, a));
       }
+      if (bwd) a.D = m.at(Df), a.e_d = m.at(ew2);
       if (remake) {
-        a.D = m.at(Df);
         a.nt = ceil_div64(rows, REMAKE_ROWS);
         const bool logistic = a.act.logistic();
-        (logistic ? k_ffn_remake<LOGISTIC> : k_ffn_remake<OTHERS>)<<<(unsigned)up_to(a.mt * a.nt, 8), 256, 0, st>>>(RemakeArgs{a, m.at(Wf), m.at(Gr), KSe, ceil_div64(e, PAIR), t_d, t_y});
+        (logistic ? k_ffn_remake<LOGISTIC> : k_ffn_remake<OTHERS>)<<<(unsigned)up_to(a.mt * a.nt, 8), 256, 0, st>>>(RemakeArgs{a, m.at(Wf), m.at(Gr), KSe, ceil_div64(e, PAIR), m.at(ewd), m.at(ey)});
         HT_LAUNCH_CHECK(ctx);
       } else if (bwd) {
         a.A = m.at(Wf), a.KSA = KSe, a.B = m.at(Gr), a.KSB = KSe;
         a.mt = ceil_div64(f, TN), a.nt = row_tiles, a.pairs = ceil_div64(e, PAIR);
-        a.w0 = t_d, a.rows_in = t_y;
-        a.D = m.at(Df);
+        a.e_w = m.at(ewd), a.e_in = m.at(ey);
         HT_TRY(launch(BACK, a));
       }
       // Y, or dX; their parts' sums are added up behind each piece, those of the weights' gradients behind the last
       FfnJoins j{};
-      auto by_rows = [&](const ht_tensor* to, const float* P, int64_t KSP, bool two, const _Float16* W, int64_t KSW, const uint32_t* w0, const uint32_t* w1, int64_t cols, int64_t nt,
+      auto by_rows = [&](const ht_tensor* to, const float* P, int64_t KSP, bool two, const _Float16* W, int64_t KSW, const int* e_w, int64_t cols, int64_t nt,
                          int64_t pairs, int splits, float* sums, int64_t pitch) {
         Args a = base;
         a.A = (const _Float16*)P, a.KSA = KSP, a.B = W, a.KSB = KSW;
-        a.mt = ceil_div64(rows, TM), a.nt = nt, a.pairs = pairs, a.splits = splits, a.two = two, a.w0 = w0, a.w1 = w1;
+        a.mt = ceil_div64(rows, TM), a.nt = nt, a.pairs = pairs, a.splits = splits, a.two = two, a.e_w = e_w;
         a.m_end = rows, a.n_end = cols;
         float* out = to->ptr + r0 * to->ld;
         a.out[0] = splits > 1 ? Out{sums, pitch, 1, Rp * pitch} : Out{out, to->ld, 1, 0};
@@ -851,11 +843,11 @@ struct Ffn : FfnCall {
         if (splits > 1) j.join[j.n++] = FfnJoin{sums, Rp * pitch, pitch, rows, cols, splits, D->accumulate, out, to->ld, 0};
         return a;
       };
-      auto by_cols = [&](const _Float16* At, const uint32_t* m_top, int64_t m_end, const float* P, int64_t KSP, bool two, int64_t tiles_m, int64_t nt, int splits, float* sums,
+      auto by_cols = [&](const _Float16* At, const int* e_rows, int64_t m_end, const float* P, int64_t KSP, bool two, int64_t tiles_m, int64_t nt, int splits, float* sums,
                          int64_t r, int64_t pitch, const ht_tensor* o0, const ht_tensor* o1, bool m_is_row) {
         Args a = base;
         a.A = At, a.KSA = KSR, a.B = (const _Float16*)P, a.KSB = KSP;
-        a.mt = tiles_m, a.nt = nt, a.pairs = ceil_div64(rows, PAIR), a.splits = splits, a.two = two, a.m_top = m_top;
+        a.mt = tiles_m, a.nt = nt, a.pairs = ceil_div64(rows, PAIR), a.splits = splits, a.two = two, a.e_w = e_rows;
         a.m_end = m_end, a.n_end = f;
         const ht_tensor* o[2] = {o0, o1};
         for (int i = 0; i < 2; ++i) {
@@ -868,11 +860,11 @@ struct Ffn : FfnCall {
         a.add = k > 0 || (splits == 1 && D->accumulate_dW);
         return a;
       };
-      if (Y) HT_TRY(launch(ROWS, by_rows(Y, m.at(H), KSH, false, m.at(Wf), KSe, t_d, nullptr, e, nte, pairs_f, sy, m.at(sums_y), e4)));
+      if (Y) HT_TRY(launch(ROWS, by_rows(Y, m.at(H), KSH, false, m.at(Wf), KSe, m.at(ewd), e, nte, pairs_f, sy, m.at(sums_y), e4)));
       Args ax{}, ad{}, ah{};                             // (no tiles: not asked for)
-      if (dX) ax = by_rows(dX, m.at(Df), KSD, true, m.at(W2), KSd, t_g, t_u, d, ntd, pairs_2f, sx, m.at(sums_x), d4);
-      if (d_w) ad = by_cols(m.at(Xt), t_xc, d, m.at(Df), KSD, true, dp / TM, ntD, sD, m.at(sums_D), wr, wp, dWg, dWu, in_out);
-      if (dWd) ah = by_cols(m.at(Gt), t_yc, e, m.at(H), KSH, false, ep / TM, ntH, sH, m.at(sums_H), vr, vp, dWd, nullptr, !in_out);
+      if (dX) ax = by_rows(dX, m.at(Df), KSD, true, m.at(W2), KSd, m.at(ew2), d, ntd, pairs_2f, sx, m.at(sums_x), d4);
+      if (d_w) ad = by_cols(m.at(Xt), m.at(exb), d, m.at(Df), KSD, true, dp / TM, ntD, sD, m.at(sums_D), wr, wp, dWg, dWu, in_out);
+      if (dWd) ah = by_cols(m.at(Gt), m.at(eyb), e, m.at(H), KSH, false, ep / TM, ntH, sH, m.at(sums_H), vr, vp, dWd, nullptr, !in_out);
       const int64_t bx = blocks_of(ax), bd = blocks_of(ad), bh = blocks_of(ah);
       if (bwd && bx + bd + bh <= SLOTS) {
         k_ffn_ends<<<(unsigned)(bx + bd + bh), 256, 0, st>>>(Ends{{ax, ad, ah}, {0, (unsigned)bx, (unsigned)(bx + bd)}});
