@@ -22,23 +22,24 @@ struct FfnJoin {
   int parts, add;
   float* out;
   int64_t ld;
-  unsigned blocks;                     // (set by ht_ffn_join)
 };
+constexpr int FFN_JOINS = 4;
 struct FfnJoins {
-  FfnJoin join[4];
+  unsigned first[FFN_JOINS];           // blocks before each (set by ht_ffn_join)
+  FfnJoin join[FFN_JOINS];
   int n;
 };
 int ht_ffn_join(ht_ctx* ctx, FfnJoins& j);
 
 namespace {
 
-// act(a) and its derivative.  Kernels are made for two kinds: s(u) with u = a (k1 + k3 a^2), times a but for the sigmoid itself, and the others.
-enum { LOGISTIC, OTHERS };
+// act(a) and its derivative.  Kernels are made for three kinds: s(u) with u = a (k1 + k3 a^2), times a but for the sigmoid itself; the normal distribution; max(a, 0).
+enum { LOGISTIC, NORMAL, LINEAR };
 struct Gate {
   int act;
   float k1, k3;
   int alone;                           // s(u) itself
-  __host__ __device__ bool logistic() const { return act != HT_GATE_GELU && act != HT_GATE_RELU; }
+  __host__ __device__ int kind() const { return act == HT_GATE_GELU ? NORMAL : act == HT_GATE_RELU ? LINEAR : LOGISTIC; }
 };
 inline Gate gate_of(int act) {
   const float k = 1.5957691216057308f;             // 2 sqrt(2 / pi)
@@ -57,9 +58,18 @@ __device__ __forceinline__ Act act_of(const Gate& g, float a) {
     const float s = u >= 0.f ? hi : lo, v = a * s;
     return g.alone ? Act{s, lo * hi} : Act{v, fmaf(v, (u >= 0.f ? lo : hi) * du, s)};
   }
-  if (g.act == HT_GATE_RELU) return {a < 0.f ? 0.f : a, a > 0.f ? 1.f : a * 0.f};      // (NaN stays NaN)
-  const float phi = 0.5f * erfcf(-a * 0.70710678118654752f);
-  return {a * phi, fmaf(a * 0.39894228040143268f, __builtin_amdgcn_exp2f(a * a * (-0.5f * LOG2E)), phi)};
+  if constexpr (KIND == NORMAL) {
+    // Phi(-|a|) = e^(-a^2 / 2) / 2 times exp(z^2) erfc(z), z = |a| / sqrt(2), which is t times a polynomial of t = 1 / (1 + 0.4 z) to 6.2e-9 of itself (a least
+    // squares fit to 4,000 values of t in (0, 1], weights raised where it was worst).  A library's erfc takes five times as long: 13 of 28 us of a launch over 1,003 x 1,213.
+    constexpr float R[11] = {-0.0292151887f, 0.14044708f, -0.235528022f, 0.13756232f, -0.0468958393f, 0.0839167088f, 0.119008213f, 0.171739295f, 0.207613721f, 0.225675866f, 0.225675836f};
+    const float e = __builtin_amdgcn_exp2f(a * a * (-0.5f * LOG2E)), t = __builtin_amdgcn_rcpf(fmaf(0.28284271247461901f, fabsf(a), 1.f));
+    float r = R[0];
+#pragma unroll
+    for (int k = 1; k < 11; ++k) r = fmaf(r, t, R[k]);
+    const float tail = 0.5f * e * (t * r), phi = a >= 0.f ? 1.f - tail : tail;
+    return {a * phi, fmaf(a * 0.39894228040143268f, e, phi)};
+  }
+  return {a < 0.f ? 0.f : a, a > 0.f ? 1.f : a * 0.f};      // (NaN stays NaN)
 }
 
 }  // namespace

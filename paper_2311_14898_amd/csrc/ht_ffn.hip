@@ -9,6 +9,7 @@
 // hidden columns, by columns where it is over rows.  A scale that changes along a reduction (of the other operand's 32s) is taken off what is split: a stage of a product is
 // 32 values of it.
 #include <algorithm>
+#include <type_traits>
 
 #include "ht_ffn.h"
 #include "ht_split.h"
@@ -49,10 +50,12 @@ struct Pack {
   _Float16* T;                         // (nullable) by run, scaled by blocks, KS_t steps; own as the reduction
   int64_t KS_t;
   int tiles;                           // of PACK_RUN along run
-  unsigned blocks;
+  unsigned blocks, share;              // (of so many own rows' blocks each takes a part of the tiles, all of them look for the largest values)
 };
 constexpr int PACKS = 5, PACK_RUN = 128;
+constexpr int64_t PACK_BLOCKS = 1024;  // where there are fewer, tiles are shared out
 struct Packs {
+  unsigned first[PACKS + 1];           // blocks before each, and before those that clear words (side by side: one trip to the arguments)
   Pack pack[PACKS];
   int n;
   uint32_t* zero;                      // words that become 0, by the blocks behind
@@ -62,15 +65,18 @@ constexpr unsigned ZEROS = 4096;       // a block
 __global__ void __launch_bounds__(256) k_ffn_pack(Packs packs) {
   __shared__ float sh[HB][PACK_RUN + 1];
   __shared__ uint32_t top[HB];
-  unsigned block = blockIdx.x;
   int i = 0;
-  while (i < packs.n && block >= packs.pack[i].blocks) block -= packs.pack[i++].blocks;
+#pragma unroll
+  for (int k = 1; k <= PACKS; ++k) i += blockIdx.x >= packs.first[k];
+  unsigned block = blockIdx.x - packs.first[i];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l32 = lane & 31, half = lane >> 5;
-  if (i == packs.n) {
+  if (i == PACKS) {
     for (int64_t k = (int64_t)block * ZEROS + tid; k < packs.zeros && k < (int64_t)(block + 1) * ZEROS; k += 256) packs.zero[k] = 0;
     return;
   }
   const Pack& a = packs.pack[i];
+  const unsigned part = block % a.share;
+  block /= a.share;
   const int64_t own0 = (int64_t)block * HB, left = a.own - own0;               // (left may be <= 0: zeros)
   if (tid < HB) top[tid] = 0;
   __syncthreads();
@@ -119,8 +125,8 @@ __global__ void __launch_bounds__(256) k_ffn_pack(Packs packs) {
   uint32_t all = top[l32];
   for (int o = 16; o > 0; o >>= 1) all = max(all, (uint32_t)__shfl_xor((int)all, o, 64));
   const int eb = exp_or_0(scale_exp(all)), eo = a.e_own ? exp_or_0(scale_exp(top[l32])) : eb;
-  if (tid < HB && a.e_own) a.e_own[own0 + tid] = eo;
-  if (tid == 0 && a.e_block) a.e_block[(int64_t)block * a.mul + a.add] = eb;
+  if (tid < HB && a.e_own && part == 0) a.e_own[own0 + tid] = eo;
+  if (tid == 0 && a.e_block && part == 0) a.e_block[(int64_t)block * a.mul + a.add] = eb;
   const float fb = pow2(eb), fo = pow2(eo);
   auto put = [&](_Float16* to, int64_t frag, const float (&x)[8]) {
     v8h hi, lo;
@@ -134,7 +140,7 @@ __global__ void __launch_bounds__(256) k_ffn_pack(Packs packs) {
     *reinterpret_cast<v8h*>(to + frag * 2 * FRAG + lane * 8) = hi;
     *reinterpret_cast<v8h*>(to + frag * 2 * FRAG + FRAG + lane * 8) = lo;
   };
-  for (int tile = 0; tile < a.tiles; ++tile) {
+  for (int tile = part; tile < a.tiles; tile += a.share) {
     const int64_t run0 = (int64_t)tile * PACK_RUN;
     V4 y[4];
 #pragma unroll
@@ -187,7 +193,8 @@ __global__ void __launch_bounds__(256) k_ffn_pack(Packs packs) {
 // BACK     A's rows: 128 hidden columns of Wd, B's the rows of dY: G, from that and A and B all of H, dA, dB and their largest values
 // ROWS     A: H or [dA dB] by rows, B: a weight turned: Y, dX
 // COLS     A: X or dY by columns, B: [dA dB] or H turned: gradients of weights
-enum { PROJECT, BACK, ROWS, COLS };
+// PROJECT_SMALL  PROJECT by 64 rows a block, for calls whose tiles are fewer than there is room for, and three blocks a CU
+enum { PROJECT, BACK, ROWS, COLS, PROJECT_SMALL };
 
 struct Out {                           // value (m, n) at m ms + n ns, split_part floats apart
   float* p;
@@ -513,8 +520,9 @@ __device__ __forceinline__ void ffn_split(const Args& a, unsigned block, _Float1
   const Tile tile(block, a.mt, a.nt, a.splits);
   if (tile.m < 0) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
-  constexpr int NI = MODE == BACK ? 1 : 2;               // row blocks of A a wave (BACK has much to do with each sum)
-  const int64_t split = tile.split, m0 = tile.m * (NI * 128), n0 = tile.n * TN, mw = m0 + wave * (NI * 32);
+  constexpr int NI = MODE == BACK ? 1 : 2, NJ = MODE == PROJECT_SMALL ? 2 : 4;       // row blocks of A a wave (BACK has much to do with each sum), and of B
+  constexpr int NR = NJ * 32;
+  const int64_t split = tile.split, m0 = tile.m * (NI * 128), n0 = tile.n * NR, mw = m0 + wave * (NI * 32);
   const int64_t s0 = a.pairs * split / a.splits * 2;                 // its first stage
   const int todo = __builtin_amdgcn_readfirstlane((int)(a.pairs * (split + 1) / a.splits - s0 / 2));
 
@@ -525,13 +533,13 @@ __device__ __forceinline__ void ffn_split(const Args& a, unsigned block, _Float1
     const int64_t c = hidden(n);
     return c >= a.f ? 0 : exp_or_0(scale_exp(!a.two ? a.h_col[c] : (n / HB) & 1 ? a.b_col[c] : a.a_col[c]));
   };
-  v16f acc[NI][4];
+  v16f acc[NI][NJ];
   clear(acc);
   const _Float16* Ap = a.A + (mw / 32 * a.KSA + s0 * KT) * 2 * FRAG + lane * 8;
   const _Float16* B = a.B + (TURN ? s0 * a.KSB + n0 / 16 : n0 / 32 * a.KSB + s0 * KT) * 2 * FRAG;
   const int64_t a_rows = a.KSA * 2 * FRAG, b_rows = a.KSB * 2 * FRAG;
   const auto a_as_it_is = [](v8h (&)[2], int, int) {};
-  const auto b_as_it_is = [](v8h (&)[4], int) {};
+  const auto b_as_it_is = [](v8h (&)[NJ], int) {};
   if constexpr (MODE == ROWS) {
     int er[2];
 #pragma unroll
@@ -552,7 +560,7 @@ __device__ __forceinline__ void ffn_split(const Args& a, unsigned block, _Float1
       for (int u = 0; u < 2; ++u) split8(rb[u * 2], rb[u * 2 + 1], f, [&](int t) { return fc[u][t]; });
     });
   } else {
-    multiply<false, true>(acc, Ap, a_rows, B, b_rows, nullptr, todo, Bs, a_as_it_is, b_as_it_is);
+    multiply<false, MODE != PROJECT_SMALL>(acc, Ap, a_rows, B, b_rows, nullptr, todo, Bs, a_as_it_is, b_as_it_is);
   }
 
   // lane l32 + 32 half of a 32 x 32 tile has column l32 and the rows 8 (e / 4) + 4 half + e % 4
@@ -593,14 +601,14 @@ __device__ __forceinline__ void ffn_split(const Args& a, unsigned block, _Float1
   }
   float* top = reinterpret_cast<float*>(Bs);
   const Hidden at(a);
-  if constexpr (MODE == PROJECT) {
+  if constexpr (MODE == PROJECT || MODE == PROJECT_SMALL) {
     const int64_t c0 = mw / 2;                          // the wave's 32 hidden columns
-    int exps[4];
+    int exps[NJ];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) exps[j] = a.e_in[n0 + j * 32 + l32];
+    for (int j = 0; j < NJ; ++j) exps[j] = a.e_in[n0 + j * 32 + l32];
     const int e0 = a.e_w[c0 / HB * 2], e1 = a.e_w[c0 / HB * 2 + 1], ed = a.e_d[c0 / HB];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < NJ; ++j) {
       const int64_t v = n0 + j * 32 + l32;
       const bool there = v < a.n;
       const int ex = exps[j];
@@ -619,10 +627,10 @@ __device__ __forceinline__ void ffn_split(const Args& a, unsigned block, _Float1
         at.put_frag(a.H, a.KSH, n0 / 32 + j, c0 / 16 + (k >> 1), k & 1, h);
       }
       m = fmaxf(m, __shfl_xor(m, 32, 64));
-      if (half == 0) top[wave * TN + j * 32 + l32] = __builtin_amdgcn_ldexpf(m, -ed);
+      if (half == 0) top[wave * NR + j * 32 + l32] = __builtin_amdgcn_ldexpf(m, -ed);
     }
     __syncthreads();
-    if (tid < TN && n0 + tid < a.n) raise(a.h_row + n0 + tid, __float_as_uint(fmaxf(fmaxf(top[tid], top[TN + tid]), fmaxf(top[2 * TN + tid], top[3 * TN + tid]))));
+    if (tid < NR && n0 + tid < a.n) raise(a.h_row + n0 + tid, __float_as_uint(fmaxf(fmaxf(top[tid], top[NR + tid]), fmaxf(top[2 * NR + tid], top[3 * NR + tid]))));
   }
   if constexpr (MODE == BACK) {
     float md[4];
@@ -650,15 +658,20 @@ __global__ void __launch_bounds__(256, 2) k_ffn_split(Args a) {
   ffn_split<MODE, KIND>(a, blockIdx.x, Bs);
 }
 // dX, and the gradients of the weights, which do not wait for each other, behind each other's blocks where all of them run at once.
-struct Ends {
+template <int KIND>
+__global__ void __launch_bounds__(256, 3) k_ffn_project_small(Args a) {
+  __shared__ __attribute__((aligned(16))) _Float16 Bs[2 * stage_halfs(false)];
+  ffn_split<PROJECT_SMALL, KIND>(a, blockIdx.x, Bs);
+}
+struct EndsArgs {
   Args a[3];                           // ROWS, COLS, COLS
   unsigned first[3];                   // blocks before each
 };
-__global__ void __launch_bounds__(256, 2) k_ffn_ends(Ends ends) {
+__global__ void __launch_bounds__(256, 2) k_ffn_ends(EndsArgs ends) {
   __shared__ __attribute__((aligned(16))) _Float16 Bs[2 * stage_halfs(true)];
-  if (blockIdx.x < ends.first[1]) return ffn_split<ROWS, OTHERS>(ends.a[0], blockIdx.x, Bs);
+  if (blockIdx.x < ends.first[1]) return ffn_split<ROWS, LINEAR>(ends.a[0], blockIdx.x, Bs);
   const int k = blockIdx.x < ends.first[2] ? 1 : 2;
-  ffn_split<COLS, OTHERS>(ends.a[k], blockIdx.x - ends.first[k], Bs);
+  ffn_split<COLS, LINEAR>(ends.a[k], blockIdx.x - ends.first[k], Bs);
 }
 
 // PROJECT and BACK in one where A and B were not kept: 128 hidden columns by 64 rows, 32 by 64 a wave, first A and B, then G; three blocks a CU, which is what hides their ends.  (Of 96
@@ -703,9 +716,10 @@ __global__ void __launch_bounds__(256, 3) k_ffn_remake(RemakeArgs r) {
 }
 
 __global__ void __launch_bounds__(256) k_ffn_join(FfnJoins joins) {
-  unsigned block = blockIdx.x;
   int k = 0;
-  while (block >= joins.join[k].blocks) block -= joins.join[k++].blocks;
+#pragma unroll
+  for (int i = 1; i < FFN_JOINS; ++i) k += blockIdx.x >= joins.first[i];
+  const unsigned block = blockIdx.x - joins.first[k];
   const FfnJoin& a = joins.join[k];
   const int64_t nv = a.pitch / 4, i = (int64_t)block * 256 + threadIdx.x, r = i / nv, c = (i - r * nv) * 4;
   if (r >= a.rows || c >= a.cols) return;
@@ -727,9 +741,48 @@ __global__ void __launch_bounds__(256) k_ffn_join(FfnJoins joins) {
 
 constexpr size_t FFN_BYTES = (size_t)4 << 30, FFN_LEAN = (size_t)64 << 20;     // of what a piece's rows take
 constexpr int64_t SLOTS = 512;                     // blocks that run together: two a CU
-constexpr int64_t LEAST_PAIRS = 4;                 // of a part of a reduction
+constexpr int64_t LEAST_PAIRS = 4;                 // of a part of a reduction, where a product has a launch for itself
 
-int parts_of(int64_t tiles, int64_t pairs) { return (int)std::max<int64_t>(1, std::min<int64_t>({SLOTS / tiles, pairs / LEAST_PAIRS, 64})); }
+constexpr int64_t SHORT_PAIRS = 8;
+
+// The products behind H, dA and dB: their tiles, pairs of stages of a tile's reduction, and the parts that it is cut into.
+struct Ends {
+  int64_t tiles[3], pairs[3];
+  int parts[3] = {1, 1, 1};
+  bool one = false;                                // one launch for all of them
+  int64_t blocks(int64_t most) const {             // with parts of at most so many pairs
+    int64_t n = 0;
+    for (int k = 0; k < 3; ++k) n += tiles[k] * ceil_div64(pairs[k], most);
+    return n;
+  }
+  int64_t fit(int64_t room) const {                // parts that leave no more blocks than that (0: there are none)
+    if (tiles[0] + tiles[1] + tiles[2] > room) return 0;
+    int64_t most = 1;
+    for (int k = 0; k < 3; ++k) most += tiles[k] * pairs[k] / room;
+    while (blocks(most) > room) most += (most + 15) / 16;
+    return most;
+  }
+  Ends(int64_t t0, int64_t p0, int64_t t1, int64_t p1, int64_t t2, int64_t p2) : tiles{t0, t1, t2}, pairs{p0, p1, p2} {
+    // A CU for each block where its part is short (a block that is alone waits for every stage's loads, but then its sums are few), else two.  us of a call, in one
+    // launch | each in its own: 500 x 128 x 512 backward 54 | 103, 2,048 x 256 x 1,024 78 | 120, 4,096 x 768 x 2,048 378 | 442, 16,384 x 512 x 2,048 965 | 967.
+    int64_t most = fit(SLOTS / 2);
+    if (most == 0 || most > SHORT_PAIRS) most = fit(SLOTS);
+    one = most > 0;
+    for (int k = 0; k < 3; ++k) {
+      const int64_t n = one ? ceil_div64(pairs[k], most) : tiles[k] > 0 ? std::min(SLOTS / tiles[k], pairs[k] / LEAST_PAIRS) : 1;
+      parts[k] = (int)std::max<int64_t>(1, std::min<int64_t>(n, 64));
+    }
+  }
+};
+
+template <class F>
+void of_kind(const Gate& g, F&& launch) {
+  switch (g.kind()) {
+    case LOGISTIC: return launch(std::integral_constant<int, LOGISTIC>());
+    case NORMAL: return launch(std::integral_constant<int, NORMAL>());
+    default: return launch(std::integral_constant<int, LINEAR>());
+  }
+}
 
 struct Ffn : FfnCall {
   static int64_t blocks_of(const Args& a) { return up_to(a.mt * a.nt * a.splits, 8); }
@@ -737,11 +790,13 @@ struct Ffn : FfnCall {
     const int64_t blocks = blocks_of(a);
     if (blocks >= (1 << 24)) return ht_set_err(ctx, HT_ESHAPE, "ffn: %lld tiles in one product", (long long)blocks);
     const unsigned grid = (unsigned)blocks;
-    const bool logistic = a.act.logistic();
-    if (mode == PROJECT) (logistic ? k_ffn_split<PROJECT, LOGISTIC> : k_ffn_split<PROJECT, OTHERS>)<<<grid, 256, 0, ctx->stream>>>(a);
-    else if (mode == BACK) (logistic ? k_ffn_split<BACK, LOGISTIC> : k_ffn_split<BACK, OTHERS>)<<<grid, 256, 0, ctx->stream>>>(a);
-    else if (mode == ROWS) k_ffn_split<ROWS, OTHERS><<<grid, 256, 0, ctx->stream>>>(a);
-    else k_ffn_split<COLS, OTHERS><<<grid, 256, 0, ctx->stream>>>(a);
+    switch (mode) {
+      case PROJECT: of_kind(a.act, [&](auto kind) { k_ffn_split<PROJECT, decltype(kind)::value><<<grid, 256, 0, ctx->stream>>>(a); }); break;
+      case PROJECT_SMALL: of_kind(a.act, [&](auto kind) { k_ffn_project_small<decltype(kind)::value><<<grid, 256, 0, ctx->stream>>>(a); }); break;
+      case BACK: of_kind(a.act, [&](auto kind) { k_ffn_split<BACK, decltype(kind)::value><<<grid, 256, 0, ctx->stream>>>(a); }); break;
+      case ROWS: k_ffn_split<ROWS, LINEAR><<<grid, 256, 0, ctx->stream>>>(a); break;
+      default: k_ffn_split<COLS, LINEAR><<<grid, 256, 0, ctx->stream>>>(a);
+    }
     HT_LAUNCH_CHECK(ctx);
     return HT_OK;
   }
@@ -758,7 +813,8 @@ struct Ffn : FfnCall {
     // tiles of the products, and parts of their reductions
     const int64_t mt = Rp / TM, nte = up_to(e, TN) / TN, ntd = up_to(d, TN) / TN, ntD = ceil_div64(f, 64), ntH = ceil_div64(f, TN);
     const int64_t pairs_f = ceil_div64(f, PAIR), pairs_2f = ceil_div64(f, HB), pairs_r = ceil_div64(std::min(n, Rp), PAIR);
-    const int sy = parts_of(mt * nte, pairs_f), sx = parts_of(mt * ntd, pairs_2f), sD = parts_of(dp / TM * ntD, pairs_r), sH = parts_of(ep / TM * ntH, pairs_r);
+    const Ends ends(Y ? mt * nte : dX ? mt * ntd : 0, Y ? pairs_f : pairs_2f, d_w ? dp / TM * ntD : 0, pairs_r, dWd ? ep / TM * ntH : 0, pairs_r);
+    const int sy = ends.parts[0], sx = sy, sD = ends.parts[1], sH = ends.parts[2];
     const int64_t e4 = up_to(e, 4), d4 = up_to(d, 4), f4 = up_to(f, 4);
     // a weight's gradient as it lies: rows and pitch of its parts
     const int64_t wr = in_out ? d : f, wp = in_out ? f4 : d4, vr = in_out ? f : e, vp = in_out ? e4 : f4;
@@ -777,7 +833,7 @@ struct Ffn : FfnCall {
     const auto sums_D = m.add<float>(d_w && sD > 1 ? sD * 2 * wr * wp : 0), sums_H = m.add<float>(dWd && sH > 1 ? sH * vr * vp : 0);
     HT_TRY(bytes > FFN_LEAN ? m.take_if_room(ctx) : m.take(ctx));
 
-    uint32_t *t_h = m.at(top), *t_d = t_h + Rp, *t_hc = t_d + Rp, *t_ac = t_hc + fp, *t_bc = t_ac + fp;
+    uint32_t *h_row = m.at(top), *d_row = h_row + Rp, *h_col = d_row + Rp, *a_col = h_col + fp, *b_col = a_col + fp;
     for (int64_t k = 0; k < pieces; ++k) {
       const int64_t r0 = k * Rp, rows = std::min(Rp, n - r0);
       Packs packs{};
@@ -796,13 +852,22 @@ struct Ffn : FfnCall {
         operand(Pack{Wu->ptr, Wu->ld, f, d, in_out, nullptr, m.at(ew2), m.at(W2), KSd, 2, 1, nullptr, 0, 0, 0}, fp, KSd * 16);
         operand(Pack{Wd->ptr, Wd->ld, f, e, !in_out, nullptr, m.at(ewd), m.at(Wf), KSe, 1, 0, nullptr, 0, 0, 0}, fp, KSe * 16);
       }
-      packs.zero = t_h, packs.zeros = n_top;
+      const unsigned share = (unsigned)std::max<int64_t>(1, PACK_BLOCKS / blocks);
+      blocks = 0;
+      for (int i = 0; i < packs.n; ++i) {
+        Pack& q = packs.pack[i];
+        q.share = std::min(share, (unsigned)q.tiles);
+        packs.first[i] = blocks;
+        blocks += q.blocks *= q.share;
+      }
+      for (int i = packs.n; i <= PACKS; ++i) packs.first[i] = blocks;
+      packs.zero = h_row, packs.zeros = n_top;
       k_ffn_pack<<<blocks + (unsigned)ceil_div64(n_top, ZEROS), 256, 0, st>>>(packs);
       HT_LAUNCH_CHECK(ctx);
 
       Args base{};
       base.act = gate_of(D->act), base.n = rows, base.f = f, base.splits = 1;
-      base.h_row = t_h, base.d_row = t_d, base.h_col = t_hc, base.a_col = t_ac, base.b_col = t_bc;
+      base.h_row = h_row, base.d_row = d_row, base.h_col = h_col, base.a_col = a_col, base.b_col = b_col;
       base.e_x = m.at(exb), base.e_y = m.at(eyb);
       base.KSH = KSH, base.KSD = KSD;
       base.gate = gate ? gate->ptr + r0 * gate->ld : nullptr, base.ld_gate = gate ? gate->ld : 0;
@@ -815,13 +880,18 @@ struct Ffn : FfnCall {
         a.mt = ceil_div64(f, TN), a.nt = row_tiles, a.pairs = ceil_div64(d, PAIR);
         a.e_w = m.at(ew2), a.e_in = m.at(ex);
         a.e_d = m.at(ewd);
-        if (!bwd) HT_TRY(launch(PROJECT, a));
+        if (!bwd) {
+          const char* sm = getenv("HT_FFN_SMALL");
+          const bool small = a.mt * a.nt < (sm ? atoll(sm) : SLOTS);
+          if (small) a.nt = ceil_div64(rows, TN / 2);
+          HT_TRY(launch(small ? PROJECT_SMALL : PROJECT, a));
+        }
       }
       if (bwd) a.D = m.at(Df), a.e_d = m.at(ew2);
       if (remake) {
         a.nt = ceil_div64(rows, REMAKE_ROWS);
-        const bool logistic = a.act.logistic();
-        (logistic ? k_ffn_remake<LOGISTIC> : k_ffn_remake<OTHERS>)<<<(unsigned)up_to(a.mt * a.nt, 8), 256, 0, st>>>(RemakeArgs{a, m.at(Wf), m.at(Gr), KSe, ceil_div64(e, PAIR), m.at(ewd), m.at(ey)});
+        const RemakeArgs r{a, m.at(Wf), m.at(Gr), KSe, ceil_div64(e, PAIR), m.at(ewd), m.at(ey)};
+        of_kind(a.act, [&](auto kind) { k_ffn_remake<decltype(kind)::value><<<(unsigned)up_to(a.mt * a.nt, 8), 256, 0, st>>>(r); });
         HT_LAUNCH_CHECK(ctx);
       } else if (bwd) {
         a.A = m.at(Wf), a.KSA = KSe, a.B = m.at(Gr), a.KSB = KSe;
@@ -840,7 +910,7 @@ struct Ffn : FfnCall {
         float* out = to->ptr + r0 * to->ld;
         a.out[0] = splits > 1 ? Out{sums, pitch, 1, Rp * pitch} : Out{out, to->ld, 1, 0};
         a.add = splits == 1 && D->accumulate;
-        if (splits > 1) j.join[j.n++] = FfnJoin{sums, Rp * pitch, pitch, rows, cols, splits, D->accumulate, out, to->ld, 0};
+        if (splits > 1) j.join[j.n++] = FfnJoin{sums, Rp * pitch, pitch, rows, cols, splits, D->accumulate, out, to->ld};
         return a;
       };
       auto by_cols = [&](const _Float16* At, const int* e_rows, int64_t m_end, const float* P, int64_t KSP, bool two, int64_t tiles_m, int64_t nt, int splits, float* sums,
@@ -855,7 +925,7 @@ struct Ffn : FfnCall {
           const int64_t ld = splits > 1 ? pitch : o[i]->ld;
           a.out[i] = Out{splits > 1 ? sums + i * r * pitch : o[i]->ptr, m_is_row ? ld : 1, m_is_row ? 1 : ld, splits > 1 ? (two ? 2 : 1) * r * pitch : 0};
           if (splits > 1 && k + 1 == pieces)
-            j.join[j.n++] = FfnJoin{sums + i * r * pitch, (two ? 2 : 1) * r * pitch, pitch, o[i]->rows, o[i]->cols, splits, D->accumulate_dW, o[i]->ptr, o[i]->ld, 0};
+            j.join[j.n++] = FfnJoin{sums + i * r * pitch, (two ? 2 : 1) * r * pitch, pitch, o[i]->rows, o[i]->cols, splits, D->accumulate_dW, o[i]->ptr, o[i]->ld};
         }
         a.add = k > 0 || (splits == 1 && D->accumulate_dW);
         return a;
@@ -866,8 +936,8 @@ struct Ffn : FfnCall {
       if (d_w) ad = by_cols(m.at(Xt), m.at(exb), d, m.at(Df), KSD, true, dp / TM, ntD, sD, m.at(sums_D), wr, wp, dWg, dWu, in_out);
       if (dWd) ah = by_cols(m.at(Gt), m.at(eyb), e, m.at(H), KSH, false, ep / TM, ntH, sH, m.at(sums_H), vr, vp, dWd, nullptr, !in_out);
       const int64_t bx = blocks_of(ax), bd = blocks_of(ad), bh = blocks_of(ah);
-      if (bwd && bx + bd + bh <= SLOTS) {
-        k_ffn_ends<<<(unsigned)(bx + bd + bh), 256, 0, st>>>(Ends{{ax, ad, ah}, {0, (unsigned)bx, (unsigned)(bx + bd)}});
+      if (bwd && ends.one) {
+        k_ffn_ends<<<(unsigned)(bx + bd + bh), 256, 0, st>>>(EndsArgs{{ax, ad, ah}, {0, (unsigned)bx, (unsigned)(bx + bd)}});
         HT_LAUNCH_CHECK(ctx);
       } else {
         if (bx) HT_TRY(launch(ROWS, ax));
@@ -882,7 +952,7 @@ struct Ffn : FfnCall {
     if (X->rows == 0) {                // nothing to add up
       FfnJoins w{};
       for (const ht_tensor* t : {dWg, dWu, dWd})
-        if (t && !D->accumulate_dW) w.join[w.n++] = FfnJoin{nullptr, 0, up_to(t->cols, 4), t->rows, t->cols, 0, 0, t->ptr, t->ld, 0};
+        if (t && !D->accumulate_dW) w.join[w.n++] = FfnJoin{nullptr, 0, up_to(t->cols, 4), t->rows, t->cols, 0, 0, t->ptr, t->ld};
       return ht_ffn_join(ctx, w);
     }
     if (X->rows <= HT_FFN_FEW) return ht_ffn_few(*this);
@@ -936,9 +1006,10 @@ int ht_ffn_join(ht_ctx* ctx, FfnJoins& j) {
   unsigned grid = 0;
   for (int k = 0; k < j.n; ++k) {
     FfnJoin& a = j.join[k];
-    a.blocks = (unsigned)ceil_div64(a.rows * (a.pitch / 4), 256);
-    grid += a.blocks;
+    j.first[k] = grid;
+    grid += (unsigned)ceil_div64(a.rows * (a.pitch / 4), 256);
   }
+  for (int k = j.n; k < FFN_JOINS; ++k) j.first[k] = grid;
   if (grid == 0) return HT_OK;
   k_ffn_join<<<grid, 256, 0, ctx->stream>>>(j);
   HT_LAUNCH_CHECK(ctx);

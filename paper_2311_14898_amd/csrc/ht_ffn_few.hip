@@ -195,7 +195,8 @@ __global__ void __launch_bounds__(WAVES * 64) k_few_hidden(FewArgs a) {
 #pragma unroll
       for (int w = 0; w < WAVES; ++w) s[m] += sh[w][m][k];
     if (!make) s[0] = a.gate[v * a.ld_gate + cc], s[1] = a.up[v * a.ld_up + cc];
-    const Act x = a.act.logistic() ? act_of<LOGISTIC>(a.act, s[0]) : act_of<OTHERS>(a.act, s[0]);
+    const int kind = a.act.kind();
+    const Act x = kind == LOGISTIC ? act_of<LOGISTIC>(a.act, s[0]) : kind == NORMAL ? act_of<NORMAL>(a.act, s[0]) : act_of<LINEAR>(a.act, s[0]);
     h[u] = x.v * s[1];
     if constexpr (!BWD) {
       if (a.gate) a.gate[v * a.ld_gate + cc] = s[0], a.up[v * a.ld_up + cc] = s[1];
@@ -321,7 +322,7 @@ int few(const FfnCall& c) {
   HT_LAUNCH_CHECK(ctx);
   if (splits == 1) return HT_OK;
   FfnJoins j{};
-  j.join[j.n++] = FfnJoin{m.at(sums), n * wp, wp, n, width, splits, c.D->accumulate, to->ptr, to->ld, 0};
+  j.join[j.n++] = FfnJoin{m.at(sums), n * wp, wp, n, width, splits, c.D->accumulate, to->ptr, to->ld};
   return ht_ffn_join(ctx, j);
 }
 

@@ -17,7 +17,6 @@ struct Item {
   const float* g;
   float* out;
   int64_t cols, vecs, ld, out_ld;        // vecs: of all rows
-  int64_t unit0;                         // the launch's units before it
 };
 // Of few values the units are small, so that there are blocks for all CUs (241 tensors of 4.5 M values a norm and a scaling 126 -> %s us); of many they are large,
 // so that few of them have to be looked for in the list.
@@ -27,8 +26,9 @@ constexpr int64_t SMALL_VECS = (int64_t)2048 * UNIT;
 constexpr int64_t CACHED_VECS = (int64_t)8 << 20;
 constexpr int LIST = 64;                 // tensors of a launch: their descriptions are arguments, so that recorded calls keep them
 struct List {
+  uint32_t unit0[LIST];                  // the launch's units before each (side by side: all of them are looked at at once)
   Item item[LIST];
-  int64_t units;
+  uint32_t units;
   int n, unit;
 };
 constexpr unsigned NORM_BLOCKS = 2048, END_THREADS = 1024;
@@ -56,15 +56,18 @@ __device__ __forceinline__ V4 load4(const float* p, int64_t left) {
   if (left >= 4) return *reinterpret_cast<const V4u*>(p);
   return V4{p[0], left > 1 ? p[1] : 0.f, left > 2 ? p[2] : 0.f, 0.f};
 }
-__device__ __forceinline__ int item_of(const List& list, int64_t unit) {
-  int lo = 0, hi = list.n - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) / 2;
-    if (list.item[mid].unit0 <= unit) lo = mid;
-    else hi = mid - 1;
+// The tensor that a unit is of, a lane looks at one each, and its number there.
+struct UnitOf {
+  int i;
+  uint32_t u;
+  __device__ __forceinline__ UnitOf(const List& list, uint32_t unit) {
+    const int lane = threadIdx.x & 63;
+    const uint32_t first = lane < list.n ? list.unit0[lane] : 0xffffffffu;
+    i = __builtin_amdgcn_readfirstlane(__popcll(__ballot(first <= unit)) - 1);
+    u = unit - __builtin_amdgcn_readlane(first, i);
   }
-  return lo;
-}
+};
+static_assert(LIST == 64, "a lane each");
 template <int N>
 __device__ __forceinline__ double block_sum(double s) {
   __shared__ double sh[N / 64];
@@ -78,9 +81,10 @@ __device__ __forceinline__ double block_sum(double s) {
 
 __global__ void __launch_bounds__(256) k_grad_squares(List list, double* __restrict__ part) {
   double s = 0.0;
-  for (int64_t u = blockIdx.x; u < list.units; u += gridDim.x) {
-    const Item& t = list.item[item_of(list, u)];
-    each_vector(t, u - t.unit0, list.unit, [&](int64_t r, int64_t c, int64_t left) {
+  for (uint32_t u = blockIdx.x; u < list.units; u += gridDim.x) {
+    const UnitOf of(list, u);
+    const Item& t = list.item[of.i];
+    each_vector(t, of.u, list.unit, [&](int64_t r, int64_t c, int64_t left) {
       const V4 x = load4(t.g + r * t.ld + c, left);
       for (int k = 0; k < 4; ++k) s = fma((double)x[k], (double)x[k], s);
     });
@@ -105,10 +109,11 @@ __global__ void __launch_bounds__(END_THREADS) k_grad_end(const double* __restri
 template <bool PAST>
 __global__ void __launch_bounds__(256) k_grad_scale(List list, const float* __restrict__ factor, int add) {
   const float f = *factor;
-  for (int64_t u = blockIdx.x; u < list.units; u += gridDim.x) {
-    const Item& t = list.item[item_of(list, u)];
+  for (uint32_t u = blockIdx.x; u < list.units; u += gridDim.x) {
+    const UnitOf of(list, u);
+    const Item& t = list.item[of.i];
     if (!add && f == 1.f && t.out == t.g) continue;      // (it is there)
-    each_vector(t, (t.vecs - 1) / list.unit - (u - t.unit0), list.unit, [&](int64_t r, int64_t c, int64_t left) {
+    each_vector(t, (t.vecs - 1) / list.unit - of.u, list.unit, [&](int64_t r, int64_t c, int64_t left) {
       V4 x = load4(t.g + r * t.ld + c, left);
       float* to = t.out + r * t.out_ld + c;
       if (add) {
@@ -174,8 +179,9 @@ int in_lists(int32_t n, const ht_tensor* grads, const ht_tensor* out, int unit, 
     if (g.rows <= 0 || g.cols <= 0) continue;
     const bool flat = g.rows == 1 || (g.ld == g.cols && (!out || out[i].ld == g.cols));
     const int64_t cols = flat ? g.rows * g.cols : g.cols, vecs = (flat ? 1 : g.rows) * ((cols + 3) / 4);
-    list.item[list.n++] = Item{g.ptr, out ? out[i].ptr : nullptr, cols, vecs, flat ? 0 : g.ld, out && !flat ? out[i].ld : 0, list.units};
-    list.units += (vecs + unit - 1) / unit;
+    list.unit0[list.n] = list.units;
+    list.item[list.n++] = Item{g.ptr, out ? out[i].ptr : nullptr, cols, vecs, flat ? 0 : g.ld, out && !flat ? out[i].ld : 0};
+    list.units += (uint32_t)((vecs + unit - 1) / unit);
     if (list.n == LIST) {
       HT_TRY(launch(list));
       list.n = 0, list.units = 0;
@@ -190,7 +196,7 @@ int grads_run(ht_ctx* ctx, int32_t n, const ht_tensor* grads, const ht_tensor* o
   for (int32_t i = 0; i < n; ++i)
     if (grads[i].rows > 0 && grads[i].cols > 0) vecs += grads[i].rows * ((grads[i].cols + 3) / 4);
   const int unit = vecs < SMALL_VECS ? SMALL_UNIT : UNIT;
-  auto blocks = [](const List& l) { return (unsigned)std::min<int64_t>(l.units, NORM_BLOCKS); };
+  auto blocks = [](const List& l) { return (unsigned)std::min<uint32_t>(l.units, NORM_BLOCKS); };
   HT_TRY(in_lists(n, grads, nullptr, unit, [&](const List& l) { return parts += blocks(l), (int)HT_OK; }));
   OpsBlock m;
   const auto part = m.add<double>(parts);
@@ -207,7 +213,7 @@ int grads_run(ht_ctx* ctx, int32_t n, const ht_tensor* grads, const ht_tensor* o
   HT_LAUNCH_CHECK(ctx);
   if (!scaled) return HT_OK;
   return in_lists(n, grads, out, unit, [&](const List& l) -> int {
-    (vecs > CACHED_VECS ? k_grad_scale<true> : k_grad_scale<false>)<<<(unsigned)std::min<int64_t>(l.units, 1 << 20), 256, 0, st>>>(l, m.at(factor), add);
+    (vecs > CACHED_VECS ? k_grad_scale<true> : k_grad_scale<false>)<<<(unsigned)std::min<uint32_t>(l.units, 1u << 20), 256, 0, st>>>(l, m.at(factor), add);
     HT_LAUNCH_CHECK(ctx);
     return HT_OK;
   });
