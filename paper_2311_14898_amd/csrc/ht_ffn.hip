@@ -397,22 +397,21 @@ struct Hidden {
   const Args& a;
   int lane, half;
   __device__ __forceinline__ Hidden(const Args& args) : a(args), lane(threadIdx.x & 63), half((threadIdx.x & 63) >> 5) {}
-  // four values of hidden columns c .. c + 3 of a row of gate or up
-  __device__ __forceinline__ void put(float* p, int64_t c, V4 x) const {
-    if (c + 4 <= a.f) {
+  // four values of hidden columns c .. c + 3 of a row of gate or up; whole: there are all of the block's
+  __device__ __forceinline__ void put(float* p, int64_t c, V4 x, bool whole) const {
+    if (whole) {
       *reinterpret_cast<V4*>(p + c) = x;
       return;
     }
 #pragma unroll
-    for (int k = 0; k < 3; ++k)
+    for (int k = 0; k < 4; ++k)
       if (c + k < a.f) p[c + k] = x[k];
   }
-  __device__ __forceinline__ V4 get(const float* p, int64_t c) const {
-    if (c + 4 <= a.f) return *reinterpret_cast<const V4*>(p + c);
-    V4 x{0.f, 0.f, 0.f, 0.f};
+  __device__ __forceinline__ V4 get(const float* p, int64_t c, bool whole) const {      // (behind the last column: the last one again)
+    if (whole) return *reinterpret_cast<const V4*>(p + c);
+    V4 x;
 #pragma unroll
-    for (int k = 0; k < 3; ++k)
-      if (c + k < a.f) x[k] = p[c + k];
+    for (int k = 0; k < 4; ++k) x[k] = p[c + k < a.f ? c + k : a.f - 1];
     return x;
   }
   // four values of a row, in the order of fragments: the k-th four of 16 columns by half
@@ -533,6 +532,10 @@ __device__ __forceinline__ void ffn_split(const Args& a, unsigned block, _Float1
     const int64_t c = hidden(n);
     return c >= a.f ? 0 : exp_or_0(scale_exp(!a.two ? a.h_col[c] : (n / HB) & 1 ? a.b_col[c] : a.a_col[c]));
   };
+  // exponents of the rows or columns of the sums, a thread each, for the end (looked up there they would be two trips to memory)
+  int end = 0;
+  if constexpr (MODE == ROWS) end = m0 + tid < a.m_end ? row_exp(m0 + tid) : 0;
+  if constexpr (MODE == COLS) end = tid < TN ? col_exp(n0 + tid) : 0;
   v16f acc[NI][NJ];
   clear(acc);
   const _Float16* Ap = a.A + (mw / 32 * a.KSA + s0 * KT) * 2 * FRAG + lane * 8;
@@ -565,37 +568,71 @@ __device__ __forceinline__ void ffn_split(const Args& a, unsigned block, _Float1
 
   // lane l32 + 32 half of a 32 x 32 tile has column l32 and the rows 8 (e / 4) + 4 half + e % 4
   if constexpr (MODE == ROWS || MODE == COLS) {
-    // exponents of the rows and columns of sums, all of them looked up at once (where they are used, one after the other, each would be a trip to memory)
+    // Exponents of the rows or columns of sums, all of them looked up at once (where they are used, one after the other, each would be a trip to memory).  Sums go by way of LDS, 32
+    // columns at a time, so that what writes them is a short loop: unrolled it is 40 KB of instructions, which a launch that is short waits for (1,003 x 301 x 1,213, Y: 16 -> %s us).
     int* ends = reinterpret_cast<int*>(Bs);
-    if (MODE == ROWS) ends[tid] = m0 + tid < a.m_end ? row_exp(m0 + tid) : 0;
-    else if (tid < TN) ends[tid] = col_exp(n0 + tid);
+    float* sums = reinterpret_cast<float*>(Bs) + TM;
+    constexpr int P = TM + 4;
+    static_assert((TM + 32 * P) * 4 <= 2 * stage_halfs(true) * 2, "sums of 32 columns beside the exponents");
+    ends[tid] = end;
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int64_t n = n0 + j * 32 + l32, c = MODE == COLS ? hidden(n) : n;
-      const Out& o = a.out[MODE == COLS && a.two ? j & 1 : 0];
-      if (!o.p || c >= a.n_end) continue;
+      const bool up = MODE == COLS && a.two && (j & 1);
+      float* out = up ? a.out[1].p : a.out[0].p;
+      const int64_t ms = up ? a.out[1].ms : a.out[0].ms, ns = up ? a.out[1].ns : a.out[0].ns, part = up ? a.out[1].split_part : a.out[0].split_part;
+      if (!out) continue;
+      const int64_t c0 = MODE == COLS && a.two ? n0 / 2 + j / 2 * HB : n0 + j * 32;      // its first column
+      if (c0 >= a.n_end) continue;
+      if (j > 0) __syncthreads();
       const int en = MODE == COLS ? ends[j * 32 + l32] : 0;
-      float* at = o.p + split * o.split_part + c * o.ns;
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const int r = wave * 64 + i * 32 + k * 8 + half * 4;
-          const int64_t m = m0 + r;
           const int4 em = MODE == ROWS ? *reinterpret_cast<const int4*>(ends + r) : make_int4(0, 0, 0, 0);
-          V4 x{__builtin_amdgcn_ldexpf(acc[i][j][k * 4], -(em.x + en)), __builtin_amdgcn_ldexpf(acc[i][j][k * 4 + 1], -(em.y + en)),
-               __builtin_amdgcn_ldexpf(acc[i][j][k * 4 + 2], -(em.z + en)), __builtin_amdgcn_ldexpf(acc[i][j][k * 4 + 3], -(em.w + en))};
-          float* to = at + m * o.ms;
-          if (o.ms == 1 && m + 4 <= a.m_end) {
-            if (a.add) x += *reinterpret_cast<const V4u*>(to);
-            *reinterpret_cast<V4u*>(to) = x;
-            continue;
-          }
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (m + e < a.m_end) to[e * o.ms] = a.add ? to[e * o.ms] + x[e] : x[e];
+          *reinterpret_cast<V4*>(sums + l32 * P + r) =
+              V4{__builtin_amdgcn_ldexpf(acc[i][j][k * 4], -(em.x + en)), __builtin_amdgcn_ldexpf(acc[i][j][k * 4 + 1], -(em.y + en)),
+                 __builtin_amdgcn_ldexpf(acc[i][j][k * 4 + 2], -(em.z + en)), __builtin_amdgcn_ldexpf(acc[i][j][k * 4 + 3], -(em.w + en))};
         }
+      __syncthreads();
+      // fours of neighbours: of a row 32 columns by eight lanes, or of a column 256 rows by a wave
+      const bool along = ns == 1;
+      const int m = along ? tid >> 3 : lane * 4, n = along ? (tid & 7) * 4 : wave, m_step = along ? 32 : 0, n_step = along ? 0 : 4;
+      float* to = out + split * part + (m0 + m) * ms + (c0 + n) * ns;
+      const int64_t step = along ? 32 * ms : 4 * ns;
+      auto four = [&](int it) {
+        const float* from = sums + (n + it * n_step) * P + m + it * m_step;
+        return along ? V4{from[0], from[P], from[2 * P], from[3 * P]} : *reinterpret_cast<const V4*>(from);
+      };
+      if (m0 + TM <= a.m_end && c0 + HB <= a.n_end) {
+        V4 x[8];
+#pragma unroll
+        for (int it = 0; it < 8; ++it) x[it] = four(it);
+        if (a.add) {
+#pragma unroll
+          for (int it = 0; it < 8; ++it) x[it] += *reinterpret_cast<const V4u*>(to + it * step);
+        }
+#pragma unroll
+        for (int it = 0; it < 8; ++it) *reinterpret_cast<V4u*>(to + it * step) = x[it];
+        continue;
+      }
+#pragma unroll 1
+      for (int it = 0; it < 8; ++it, to += step) {
+        V4 x = four(it);
+        const int64_t m_left = a.m_end - (m0 + m + it * m_step), n_left = a.n_end - (c0 + n + it * n_step), left = along ? n_left : m_left;
+        if (m_left <= 0 || n_left <= 0) continue;
+        if (left >= 4) {
+          if (a.add) x += *reinterpret_cast<const V4u*>(to);
+          *reinterpret_cast<V4u*>(to) = x;
+        } else {
+          for (int k = 0; k < left; ++k) {
+            const float v = k == 0 ? x[0] : k == 1 ? x[1] : x[2];
+            to[k] = a.add ? to[k] + v : v;
+          }
+        }
+      }
     }
     return;
   }
@@ -623,7 +660,7 @@ __device__ __forceinline__ void ffn_split(const Args& a, unsigned block, _Float1
           h[e] = act_of<KIND>(a.act, x[e]).v * y[e];
           m = fmaxf(m, fabsf(h[e]));
         }
-        if (a.gate && there) at.put(a.gate + v * a.ld_gate, c, x), at.put(a.up + v * a.ld_up, c, y);
+        if (a.gate && there) at.put(a.gate + v * a.ld_gate, c, x, c0 + HB <= a.f), at.put(a.up + v * a.ld_up, c, y, c0 + HB <= a.f);
         at.put_frag(a.H, a.KSH, n0 / 32 + j, c0 / 16 + (k >> 1), k & 1, h);
       }
       m = fmaxf(m, __shfl_xor(m, 32, 64));
@@ -646,7 +683,7 @@ __device__ __forceinline__ void ffn_split(const Args& a, unsigned block, _Float1
     }
     at.back<KIND, 4>(n0 / 32, mw / HB, md, cols + wave * 96, [&](int j, int k, V4& x, V4& y) {
       const int64_t c = mw + k * 8 + half * 4;
-      x = at.get(gate[j], c), y = at.get(up[j], c);
+      x = at.get(gate[j], c, mw + HB <= a.f), y = at.get(up[j], c, mw + HB <= a.f);
     }, [&](int j, int k, int e) { return __builtin_amdgcn_ldexpf(acc[0][j][k * 4 + e], -(ey[j] + e0)); });
     at.back_tops<4, 4>(n0 / 32, m0, md, cols, top);
   }
