@@ -33,32 +33,28 @@ int ht_ffn_join(ht_ctx* ctx, FfnJoins& j);
 
 namespace {
 
-// act(a) and its derivative.  Kernels are made for three kinds: s(u) with u = a (k1 + k3 a^2), times a but for the sigmoid itself; the normal distribution; max(a, 0).
-enum { LOGISTIC, NORMAL, LINEAR };
-struct Gate {
-  int act;
-  float k1, k3;
-  int alone;                           // s(u) itself
-  __host__ __device__ int kind() const { return act == HT_GATE_GELU ? NORMAL : act == HT_GATE_RELU ? LINEAR : LOGISTIC; }
-};
-inline Gate gate_of(int act) {
-  const float k = 1.5957691216057308f;             // 2 sqrt(2 / pi)
-  return act == HT_GATE_GELU_TANH ? Gate{act, k, 0.044715f * k, 0} : Gate{act, 1.f, 0.f, act == HT_GATE_SIGMOID};
-}
+// act(a) and its derivative; kernels are made for each (HT_GATE_*): what is made of a product's sums takes the vector units as long as the product takes the matrix cores.
 struct Act {
   float v, s;
 };
-template <int KIND>
-__device__ __forceinline__ Act act_of(const Gate& g, float a) {
+template <int ACT>
+__device__ __forceinline__ Act act_of(float a) {
   constexpr float LOG2E = 1.44269504088896340736f;
-  if constexpr (KIND == LOGISTIC) {
-    // exp(-|u|) gives s(u) and s(-u) = 1 - s(u) without cancellation
-    const float q = fminf(a * a, 1e30f), u = a * fmaf(g.k3, q, g.k1), du = fmaf(3.f * g.k3, q, g.k1);
-    const float e = __builtin_amdgcn_exp2f(-fabsf(u) * LOG2E), hi = __builtin_amdgcn_rcpf(1.f + e), lo = e * hi;
-    const float s = u >= 0.f ? hi : lo, v = a * s;
-    return g.alone ? Act{s, lo * hi} : Act{v, fmaf(v, (u >= 0.f ? lo : hi) * du, s)};
+  if constexpr (ACT == HT_GATE_SILU) {
+    // s(-a) = 1 - s(a) is off by half a step of 1 where it is small, and so is the derivative, which is near 1 there
+    const float s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(a * -LOG2E)), v = a * s;
+    return {v, fmaf(v, 1.f - s, s)};
   }
-  if constexpr (KIND == NORMAL) {
+  if constexpr (ACT == HT_GATE_GELU_TANH) {        // s(u), u = 2 sqrt(2 / pi) (a + 0.044715 a^3)
+    constexpr float K1 = 1.5957691216057308f, K3 = 0.044715f * K1;
+    const float q = fminf(a * a, 1e30f), s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(a * fmaf(q, -LOG2E * K3, -LOG2E * K1))), v = a * s;
+    return {v, fmaf(v * (1.f - s), fmaf(q, 3.f * K3, K1), s)};
+  }
+  if constexpr (ACT == HT_GATE_SIGMOID) {          // exp(-|a|) gives s(a) and s(-a) without cancellation
+    const float e = __builtin_amdgcn_exp2f(fabsf(a) * -LOG2E), hi = __builtin_amdgcn_rcpf(1.f + e), lo = e * hi;
+    return {a >= 0.f ? hi : lo, lo * hi};
+  }
+  if constexpr (ACT == HT_GATE_GELU) {
     // Phi(-|a|) = e^(-a^2 / 2) / 2 times exp(z^2) erfc(z), z = |a| / sqrt(2), which is t times a polynomial of t = 1 / (1 + 0.4 z) to 6.2e-9 of itself (a least
     // squares fit to 4,000 values of t in (0, 1], weights raised where it was worst).  A library's erfc takes five times as long: 13 of 28 us of a launch over 1,003 x 1,213.
     constexpr float R[11] = {-0.0292151887f, 0.14044708f, -0.235528022f, 0.13756232f, -0.0468958393f, 0.0839167088f, 0.119008213f, 0.171739295f, 0.207613721f, 0.225675866f, 0.225675836f};

@@ -206,7 +206,6 @@ struct Args {
   int64_t mt, nt;                      // tiles
   int64_t pairs;                       // of stages, of the reduction
   int splits;                          // parts of it
-  Gate act;
   int two;                             // an operand is [dA dB]
   // exponents: PROJECT of Wg and Wu by hidden blocks, interleaved, BACK of Wd; ROWS, COLS: of the other operand by stages of the reduction
   const int* e_w;
@@ -421,8 +420,8 @@ struct Hidden {
   }
   // H, dA and dB of NJ row blocks from row block b0 on, of the hidden block hb.  Largest values, less the exponents of what they will meet: of the rows of dA and dB
   // together in md, of the columns (of H, dA, dB, 32 each) to cols.  (An infinite one may be the largest: what is scaled by it is not finite in any case.)  get(j, k, x, y): A
-  // and B of four hidden columns of a row, fetched four columns ahead; sums(j, k, e): G of one.
-  template <int KIND, int NJ, class Get, class Sums>
+  // and B of four hidden columns of a row, fetched four columns ahead; sums(j, k, e): G of one.  Behind the last row and column G is 0, and so is A or B.
+  template <int ACT, int NJ, class Get, class Sums>
   __device__ __forceinline__ void back(int64_t b0, int64_t hb, float (&md)[NJ], float* cols, Get&& get, Sums&& sums) const {
     const int64_t c0 = hb * HB;
     float fx[NJ], fy[NJ], ma[NJ] = {}, mb[NJ] = {};
@@ -430,7 +429,6 @@ struct Hidden {
     for (int j = 0; j < NJ; ++j) fx[j] = pow2(-a.e_x[b0 + j]), fy[j] = pow2(-a.e_y[b0 + j]);
     const int eg = a.e_d[hb * 2], eu = a.e_d[hb * 2 + 1];
     const int l32 = lane & 31;
-    const bool edge = (b0 + NJ) * 32 > a.n || c0 + 32 > a.f;
     V4 x[2][NJ], y[2][NJ];
 #pragma unroll
     for (int j = 0; j < NJ; ++j) get(j, 0, x[0][j], y[0][j]);
@@ -441,22 +439,16 @@ struct Hidden {
         for (int j = 0; j < NJ; ++j) get(j, k + 1, x[(k + 1) & 1][j], y[(k + 1) & 1][j]);
         __builtin_amdgcn_sched_barrier(0);
       }
-      const int64_t c = c0 + k * 8 + half * 4, step = c0 / 16 + (k >> 1), step_d = c0 / 8 + (k >> 1);
+      const int64_t step = c0 / 16 + (k >> 1), step_d = c0 / 8 + (k >> 1);
       float ch[4] = {}, ca[4] = {}, cb[4] = {};
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
-        const int64_t v = (b0 + j) * 32 + l32;
         V4 h, da, db;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const Act s = act_of<KIND>(a.act, x[k & 1][j][e]);
+          const Act s = act_of<ACT>(x[k & 1][j][e]);
           const float u = y[k & 1][j][e], g = sums(j, k, e);
           h[e] = s.v * u, da[e] = g * u * s.s, db[e] = g * s.v;
-        }
-        if (edge) {                    // what is behind the last row and column is 0, whatever the weights are
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (v >= a.n || c + e >= a.f) h[e] = da[e] = db[e] = 0.f;
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -513,7 +505,7 @@ struct Hidden {
   }
 };
 
-template <int MODE, int KIND>
+template <int MODE, int ACT>
 __device__ __forceinline__ void ffn_split(const Args& a, unsigned block, _Float16* Bs) {
   constexpr bool TURN = MODE == ROWS || MODE == COLS;
   const Tile tile(block, a.mt, a.nt, a.splits);
@@ -657,7 +649,7 @@ __device__ __forceinline__ void ffn_split(const Args& a, unsigned block, _Float1
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           x[e] = __builtin_amdgcn_ldexpf(acc[0][j][k * 4 + e], -(ex + e0)), y[e] = __builtin_amdgcn_ldexpf(acc[1][j][k * 4 + e], -(ex + e1));
-          h[e] = act_of<KIND>(a.act, x[e]).v * y[e];
+          h[e] = act_of<ACT>(x[e]).v * y[e];
           m = fmaxf(m, fabsf(h[e]));
         }
         if (a.gate && there) at.put(a.gate + v * a.ld_gate, c, x, c0 + HB <= a.f), at.put(a.up + v * a.ld_up, c, y, c0 + HB <= a.f);
@@ -675,30 +667,32 @@ __device__ __forceinline__ void ffn_split(const Args& a, unsigned block, _Float1
     int ey[4];
     const int e0 = a.e_w[mw / HB];
     const float *gate[4], *up[4];
+    const bool last = n0 + TN > a.n;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int64_t v = n0 + j * 32 + l32, row = v < a.n ? v : a.n - 1;
       ey[j] = a.e_in[v];
       gate[j] = a.gate + row * a.ld_gate, up[j] = a.up + row * a.ld_up;
     }
-    at.back<KIND, 4>(n0 / 32, mw / HB, md, cols + wave * 96, [&](int j, int k, V4& x, V4& y) {
+    at.back<ACT, 4>(n0 / 32, mw / HB, md, cols + wave * 96, [&](int j, int k, V4& x, V4& y) {
       const int64_t c = mw + k * 8 + half * 4;
       x = at.get(gate[j], c, mw + HB <= a.f), y = at.get(up[j], c, mw + HB <= a.f);
+      if (last && n0 + j * 32 + l32 >= a.n) x = y = V4{0.f, 0.f, 0.f, 0.f};
     }, [&](int j, int k, int e) { return __builtin_amdgcn_ldexpf(acc[0][j][k * 4 + e], -(ey[j] + e0)); });
     at.back_tops<4, 4>(n0 / 32, m0, md, cols, top);
   }
 }
 
-template <int MODE, int KIND>
+template <int MODE, int ACT>
 __global__ void __launch_bounds__(256, 2) k_ffn_split(Args a) {
   __shared__ __attribute__((aligned(16))) _Float16 Bs[2 * stage_halfs(MODE == ROWS || MODE == COLS)];
-  ffn_split<MODE, KIND>(a, blockIdx.x, Bs);
+  ffn_split<MODE, ACT>(a, blockIdx.x, Bs);
 }
 // dX, and the gradients of the weights, which do not wait for each other, behind each other's blocks where all of them run at once.
-template <int KIND>
+template <int ACT>
 __global__ void __launch_bounds__(256, 3) k_ffn_project_small(Args a) {
   __shared__ __attribute__((aligned(16))) _Float16 Bs[2 * stage_halfs(false)];
-  ffn_split<PROJECT_SMALL, KIND>(a, blockIdx.x, Bs);
+  ffn_split<PROJECT_SMALL, ACT>(a, blockIdx.x, Bs);
 }
 struct EndsArgs {
   Args a[3];                           // ROWS, COLS, COLS
@@ -706,9 +700,9 @@ struct EndsArgs {
 };
 __global__ void __launch_bounds__(256, 2) k_ffn_ends(EndsArgs ends) {
   __shared__ __attribute__((aligned(16))) _Float16 Bs[2 * stage_halfs(true)];
-  if (blockIdx.x < ends.first[1]) return ffn_split<ROWS, LINEAR>(ends.a[0], blockIdx.x, Bs);
+  if (blockIdx.x < ends.first[1]) return ffn_split<ROWS, 0>(ends.a[0], blockIdx.x, Bs);
   const int k = blockIdx.x < ends.first[2] ? 1 : 2;
-  ffn_split<COLS, LINEAR>(ends.a[k], blockIdx.x - ends.first[k], Bs);
+  ffn_split<COLS, 0>(ends.a[k], blockIdx.x - ends.first[k], Bs);
 }
 
 // PROJECT and BACK in one where A and B were not kept: 128 hidden columns by 64 rows, 32 by 64 a wave, first A and B, then G; three blocks a CU, which is what hides their ends.  (Of 96
@@ -721,7 +715,7 @@ struct RemakeArgs {
   int64_t KS2, pairs2;
   const int *e_w2, *e_in2;
 };
-template <int KIND>
+template <int ACT>
 __global__ void __launch_bounds__(256, 3) k_ffn_remake(RemakeArgs r) {
   __shared__ __attribute__((aligned(16))) _Float16 Bs[2 * stage_halfs(false)];
   const Args& a = r.a;
@@ -744,7 +738,7 @@ __global__ void __launch_bounds__(256, 3) k_ffn_remake(RemakeArgs r) {
   int ex[NJ], ey[NJ];
 #pragma unroll
   for (int j = 0; j < NJ; ++j) ex[j] = a.e_in[(b0 + j) * 32 + (lane & 31)], ey[j] = r.e_in2[(b0 + j) * 32 + (lane & 31)];
-  at.back<KIND, NJ>(b0, hb, md, cols + wave * 96, [&](int j, int k, V4& x, V4& y) {
+  at.back<ACT, NJ>(b0, hb, md, cols + wave * 96, [&](int j, int k, V4& x, V4& y) {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       x[e] = __builtin_amdgcn_ldexpf(ab[0][j][k * 4 + e], -(ex[j] + e0)), y[e] = __builtin_amdgcn_ldexpf(ab[1][j][k * 4 + e], -(ex[j] + e1));
@@ -813,11 +807,13 @@ struct Ends {
 };
 
 template <class F>
-void of_kind(const Gate& g, F&& launch) {
-  switch (g.kind()) {
-    case LOGISTIC: return launch(std::integral_constant<int, LOGISTIC>());
-    case NORMAL: return launch(std::integral_constant<int, NORMAL>());
-    default: return launch(std::integral_constant<int, LINEAR>());
+void with_act(int act, F&& launch) {   // launch(std::integral_constant<int, act>())
+  switch (act) {
+    case HT_GATE_SILU: return launch(std::integral_constant<int, HT_GATE_SILU>());
+    case HT_GATE_GELU: return launch(std::integral_constant<int, HT_GATE_GELU>());
+    case HT_GATE_GELU_TANH: return launch(std::integral_constant<int, HT_GATE_GELU_TANH>());
+    case HT_GATE_RELU: return launch(std::integral_constant<int, HT_GATE_RELU>());
+    default: return launch(std::integral_constant<int, HT_GATE_SIGMOID>());
   }
 }
 
@@ -828,11 +824,11 @@ struct Ffn : FfnCall {
     if (blocks >= (1 << 24)) return ht_set_err(ctx, HT_ESHAPE, "ffn: %lld tiles in one product", (long long)blocks);
     const unsigned grid = (unsigned)blocks;
     switch (mode) {
-      case PROJECT: of_kind(a.act, [&](auto kind) { k_ffn_split<PROJECT, decltype(kind)::value><<<grid, 256, 0, ctx->stream>>>(a); }); break;
-      case PROJECT_SMALL: of_kind(a.act, [&](auto kind) { k_ffn_project_small<decltype(kind)::value><<<grid, 256, 0, ctx->stream>>>(a); }); break;
-      case BACK: of_kind(a.act, [&](auto kind) { k_ffn_split<BACK, decltype(kind)::value><<<grid, 256, 0, ctx->stream>>>(a); }); break;
-      case ROWS: k_ffn_split<ROWS, LINEAR><<<grid, 256, 0, ctx->stream>>>(a); break;
-      default: k_ffn_split<COLS, LINEAR><<<grid, 256, 0, ctx->stream>>>(a);
+      case PROJECT: with_act(D->act, [&](auto act) { k_ffn_split<PROJECT, decltype(act)::value><<<grid, 256, 0, ctx->stream>>>(a); }); break;
+      case PROJECT_SMALL: with_act(D->act, [&](auto act) { k_ffn_project_small<decltype(act)::value><<<grid, 256, 0, ctx->stream>>>(a); }); break;
+      case BACK: with_act(D->act, [&](auto act) { k_ffn_split<BACK, decltype(act)::value><<<grid, 256, 0, ctx->stream>>>(a); }); break;
+      case ROWS: k_ffn_split<ROWS, 0><<<grid, 256, 0, ctx->stream>>>(a); break;
+      default: k_ffn_split<COLS, 0><<<grid, 256, 0, ctx->stream>>>(a);
     }
     HT_LAUNCH_CHECK(ctx);
     return HT_OK;
@@ -903,7 +899,7 @@ struct Ffn : FfnCall {
       HT_LAUNCH_CHECK(ctx);
 
       Args base{};
-      base.act = gate_of(D->act), base.n = rows, base.f = f, base.splits = 1;
+      base.n = rows, base.f = f, base.splits = 1;
       base.h_row = h_row, base.d_row = d_row, base.h_col = h_col, base.a_col = a_col, base.b_col = b_col;
       base.e_x = m.at(exb), base.e_y = m.at(eyb);
       base.KSH = KSH, base.KSD = KSD;
@@ -928,7 +924,7 @@ struct Ffn : FfnCall {
       if (remake) {
         a.nt = ceil_div64(rows, REMAKE_ROWS);
         const RemakeArgs r{a, m.at(Wf), m.at(Gr), KSe, ceil_div64(e, PAIR), m.at(ewd), m.at(ey)};
-        of_kind(a.act, [&](auto kind) { k_ffn_remake<decltype(kind)::value><<<(unsigned)up_to(a.mt * a.nt, 8), 256, 0, st>>>(r); });
+        with_act(D->act, [&](auto act) { k_ffn_remake<decltype(act)::value><<<(unsigned)up_to(a.mt * a.nt, 8), 256, 0, st>>>(r); });
         HT_LAUNCH_CHECK(ctx);
       } else if (bwd) {
         a.A = m.at(Wf), a.KSA = KSe, a.B = m.at(Gr), a.KSB = KSe;

@@ -88,9 +88,19 @@ __device__ __forceinline__ void few_products(v4f (&acc)[M][NB], const float* con
   }
 }
 
+__device__ __forceinline__ Act few_act(int act, float a) {
+  switch (act) {
+    case HT_GATE_SILU: return act_of<HT_GATE_SILU>(a);
+    case HT_GATE_GELU: return act_of<HT_GATE_GELU>(a);
+    case HT_GATE_GELU_TANH: return act_of<HT_GATE_GELU_TANH>(a);
+    case HT_GATE_RELU: return act_of<HT_GATE_RELU>(a);
+    default: return act_of<HT_GATE_SIGMOID>(a);
+  }
+}
+
 struct FewArgs {
   int64_t n, d, f, e;
-  Gate act;
+  int act;
   const float *X, *Wg, *Wu, *Wd, *dY;
   int64_t ldx, ldg, ldu, ldd, ldy;
   float *gate, *up;                    // forward: where A and B go (null: nowhere); backward: where they are (null: they are made)
@@ -195,8 +205,7 @@ __global__ void __launch_bounds__(WAVES * 64) k_few_hidden(FewArgs a) {
 #pragma unroll
       for (int w = 0; w < WAVES; ++w) s[m] += sh[w][m][k];
     if (!make) s[0] = a.gate[v * a.ld_gate + cc], s[1] = a.up[v * a.ld_up + cc];
-    const int kind = a.act.kind();
-    const Act x = kind == LOGISTIC ? act_of<LOGISTIC>(a.act, s[0]) : kind == NORMAL ? act_of<NORMAL>(a.act, s[0]) : act_of<LINEAR>(a.act, s[0]);
+    const Act x = few_act(a.act, s[0]);
     h[u] = x.v * s[1];
     if constexpr (!BWD) {
       if (a.gate) a.gate[v * a.ld_gate + cc] = s[0], a.up[v * a.ld_up + cc] = s[1];
@@ -295,7 +304,7 @@ int few(const FfnCall& c) {
   const auto sums = m.add<float>(to && splits > 1 ? splits * n * wp : 0);
   HT_TRY(m.take(ctx));
   FewArgs a{};
-  a.n = n, a.d = d, a.f = f, a.e = e, a.act = gate_of(c.D->act);
+  a.n = n, a.d = d, a.f = f, a.e = e, a.act = c.D->act;
   a.X = c.X->ptr, a.ldx = c.X->ld, a.Wg = c.Wg->ptr, a.ldg = c.Wg->ld, a.Wu = c.Wu->ptr, a.ldu = c.Wu->ld, a.Wd = c.Wd->ptr, a.ldd = c.Wd->ld;
   if (bwd) a.dY = c.dY->ptr, a.ldy = c.dY->ld;
   if (c.gate) a.gate = c.gate->ptr, a.ld_gate = c.gate->ld, a.up = c.up->ptr, a.ld_up = c.up->ld;
