@@ -561,7 +561,7 @@ __device__ __forceinline__ void ffn_split(const Args& a, unsigned block, _Float1
   // lane l32 + 32 half of a 32 x 32 tile has column l32 and the rows 8 (e / 4) + 4 half + e % 4
   if constexpr (MODE == ROWS || MODE == COLS) {
     // Exponents of the rows or columns of sums, all of them looked up at once (where they are used, one after the other, each would be a trip to memory).  Sums go by way of LDS, 32
-    // columns at a time, so that what writes them is a short loop: unrolled it is 40 KB of instructions, which a launch that is short waits for (1,003 x 301 x 1,213, Y: 16 -> %s us).
+    // columns at a time, so that what writes them is a short loop: unrolled it is 4,000 instructions a wave (1,003 x 301 x 1,213, Y: 16.2 -> 15.3 us, 8,192 x 1,024 x 4,096, dX: 463 -> 447).
     int* ends = reinterpret_cast<int*>(Bs);
     float* sums = reinterpret_cast<float*>(Bs) + TM;
     constexpr int P = TM + 4;

@@ -18,7 +18,7 @@ struct Item {
   float* out;
   int64_t cols, vecs, ld, out_ld;        // vecs: of all rows
 };
-// Of few values the units are small, so that there are blocks for all CUs (241 tensors of 4.5 M values a norm and a scaling 126 -> %s us); of many they are large,
+// Of few values the units are small, so that there are blocks for all CUs (241 tensors of 4.5 M values a norm and a scaling 126 -> 103 us); of many they are large,
 // so that few of them have to be looked for in the list.
 constexpr int UNIT = 4096, SMALL_UNIT = 1024;
 constexpr int64_t SMALL_VECS = (int64_t)2048 * UNIT;

@@ -1,0 +1,347 @@
+"""Gated blocks and clipped steps as a program uses them: together with tables, layers and heads, on streams of its own, recorded and replayed, with little memory.
+
+Tolerances of the composed step: assert_close's and assert_close_grad's, as for the other calls together; of single calls those of test_gpu_ffn and test_gpu_grads."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import oracle as orc
+from paper_2311_14898_amd import binding as B
+from paper_2311_14898_amd import inputs
+from tests.test_gpu_ffn import activation, check, reference
+from tests.test_gpu_ffn import _inputs as ffn_inputs
+from tests.test_gpu_ffn import call as ffn_call
+from tests.util import assert_close, assert_close_grad
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("V", [50, 1500])
+def test_a_training_step(V):
+    """Ids -> table -> layer -> h + block(h) -> head; backwards; the norm of all gradients; one clipped step of everything."""
+    E, items, d, f, C = 12 * V, 300, 36, 88, 70
+    src, dst = inputs.rmat_edges(V, E, seed=7)
+    rng = np.random.default_rng(V)
+    r = lambda a, b, s: (rng.standard_normal((a, b)) * s).astype(np.float32)
+    P = dict(T=r(items, d, 1.0), W=r(d, d, 1 / math.sqrt(d)), Wg=r(d, f, 1.5 / math.sqrt(d)), Wu=r(d, f, 1 / math.sqrt(d)), Wd=r(f, d, 1 / math.sqrt(f)), Wh=r(d, C, 0.3))
+    ids, y = rng.integers(0, items, V).astype(np.int32), rng.integers(0, C, V).astype(np.int32)
+    # in 64 bits
+    Q = {k: v.astype(np.float64) for k, v in P.items()}
+    indptr, col = orc.csc_build(V, src.numpy(), dst.numpy())
+    h0 = Q["T"][ids]
+    a = orc.aggregate(indptr, col, h0)
+    h1 = a @ Q["W"]
+    A, U = h1 @ Q["Wg"], h1 @ Q["Wu"]
+    v, s = activation(A, "silu")[:2]
+    Y = h1 + (v * U) @ Q["Wd"]
+    x = Y @ Q["Wh"]
+    m = x.max(axis=1, keepdims=True)
+    lse = np.log(np.exp(x - m).sum(axis=1)) + m[:, 0]
+    loss = (lse - x[np.arange(V), y]).mean()
+    g = np.exp(x - lse[:, None])
+    g[np.arange(V), y] -= 1.0
+    g /= V
+    G = dict(Wh=Y.T @ g)
+    dY = g @ Q["Wh"].T
+    back = dY @ Q["Wd"].T
+    dA, dU = back * U * s, back * v
+    G.update(Wd=(v * U).T @ dY, Wg=h1.T @ dA, Wu=h1.T @ dU)
+    dh1 = dY + dA @ Q["Wg"].T + dU @ Q["Wu"].T
+    G["W"] = a.T @ dh1
+    da = dh1 @ Q["W"].T
+    deg = np.diff(indptr).astype(np.float64)
+    dh0 = np.zeros_like(h0)
+    rows = np.repeat(np.arange(V), np.diff(indptr))
+    np.add.at(dh0, col, da[rows] / np.sqrt(deg[rows] * deg[col])[:, None])
+    G["T"] = np.zeros_like(Q["T"])
+    np.add.at(G["T"], ids, dh0)
+    norm = math.sqrt(sum((t ** 2).sum() for t in G.values()))
+    max_norm, lr = 0.5 * norm, 0.1
+
+    ctx = B.ht_ctx_create(0)
+    try:
+        graph = B.ht_partition(ctx, V, src.cuda(), dst.cuda(), 2)
+        p = {k: torch.from_numpy(t).cuda() for k, t in P.items()}
+        grads = {k: torch.empty_like(t) for k, t in p.items()}
+        ids_d, y_d, l, got_norm = torch.from_numpy(ids).cuda(), torch.from_numpy(y).cuda(), torch.zeros(1, device="cuda"), torch.zeros(1, device="cuda")
+        new = lambda c: torch.zeros(V, c, device="cuda")
+        H0, Ag, H1, Yd, dYd, dH1, dH0, gate, up = new(d), new(d), new(d), new(d), new(d), new(d), new(d), new(f), new(f)
+        B.ht_embed_fwd(ctx, d, p["T"], ids_d, H0)
+        B.ht_layer_fwd(ctx, graph, d, d, B.HT_ACT_NONE, H0, p["W"], H1, Ag)
+        B.ht_sync(ctx)
+        Yd.copy_(H1)                                           # the residual stream
+        B.ht_ffn_fwd(ctx, d, f, d, H1, p["Wg"], p["Wu"], p["Wd"], Yd, gate=gate, up=up, accumulate=True)
+        head = torch.zeros(d, (C + 3) // 4 * 4, device="cuda")
+        head[:, :C] = p["Wh"]
+        dhead = torch.zeros_like(head)
+        B.ht_head_loss(ctx, d, C, Yd, head, y_d, l, dH=dYd, dW=dhead)
+        B.ht_sync(ctx)
+        dH1.copy_(dYd)
+        B.ht_ffn_bwd(ctx, d, f, d, H1, p["Wg"], p["Wu"], p["Wd"], dYd, dX=dH1, dWg=grads["Wg"], dWu=grads["Wu"], dWd=grads["Wd"], gate=gate, up=up, accumulate=True)
+        B.ht_layer_bwd(ctx, graph, d, d, B.HT_ACT_NONE, Ag, p["W"], dH1, grads["W"], dH_in=dH0)
+        B.ht_embed_bwd(ctx, d, dH0, ids_d, grads["T"])
+        B.ht_sync(ctx)
+        grads["Wh"].copy_(dhead[:, :C])
+        torch.cuda.synchronize()
+        names = sorted(p)
+        B.ht_grad_clip(ctx, [grads[k] for k in names], max_norm, out=[p[k] for k in names], scale=-lr, accumulate=True, norm=got_norm)
+        B.ht_sync(ctx)
+        assert abs(float(l) - loss) <= 1e-5 * abs(loss)
+        assert_close(Yd.cpu().numpy(), Y, "Y")
+        for k in names:
+            assert_close_grad(grads[k].cpu().numpy(), G[k], "d" + k)
+            step = P[k] - lr * 0.5 * grads[k].cpu().numpy().astype(np.float64)
+            # the norm is off by 1e-5 of itself at most (assert_close_grad's rows are closer than that), and so is the step; one rounding of the sum
+            assert (np.abs(p[k].cpu().numpy() - step) <= 2e-5 * lr * 0.5 * np.abs(G[k]) + 1e-7 * np.abs(G[k]).max() * lr + 2.0 ** -23 * np.abs(step)).all(), k
+        assert abs(float(got_norm) - norm) <= 1e-5 * norm
+        B.ht_graph_destroy(graph)
+    finally:
+        B.ht_ctx_destroy(ctx)
+
+
+class Work:
+    """Calls of each kind on a context, of few rows and of many, kept and made again; their inputs and outputs."""
+
+    def __init__(self, ctx, big=1, seed=0):
+        self.ctx, self.g = ctx, torch.Generator(device="cuda")
+        self.g.manual_seed(seed)
+        self.n, self.few, self.d, self.f, self.e = 90 * big, 40, 36, 100, 28
+        r = lambda *s: torch.randn(*s, generator=self.g, device="cuda")
+        z = lambda *s: torch.zeros(*s, device="cuda")
+        n, d, f, e = self.n, self.d, self.f, self.e
+        self.ins = dict(X=r(n, d), Wg=r(f, d) * 0.2, Wu=r(f, d) * 0.2, Wd=r(e, f) * 0.1, dY=r(n, e))
+        self.small = [r(1 + i % 3, 5 + i) for i in range(70)]
+        self.outs = {}
+        for k, rows in (("many", n), ("few", self.few)):
+            self.outs[k] = dict(Y=z(rows, e), gate=z(rows, f), up=z(rows, f), dX=z(rows, d), dWg=z(f, d), dWu=z(f, d), dWd=z(e, f), dX2=z(rows, d))
+        self.clipped, self.norm, self.norm2 = [torch.zeros_like(t) for t in self.small], z(1), z(1)
+        torch.cuda.synchronize()
+
+    def outputs(self):
+        return [t for o in self.outs.values() for t in o.values()] + self.clipped + [self.norm, self.norm2]
+
+    def run(self, sync=False):
+        x, c = self.ins, self.ctx
+        size = (self.d, self.f, self.e)
+        for k, o in self.outs.items():
+            rows = o["Y"].shape[0]
+            args = (c, *size, x["X"][:rows], x["Wg"], x["Wu"], x["Wd"])
+            kw = dict(act=B.HT_GATE_GELU, w_form=B.HT_W_OUT_IN, sync=sync)
+            B.ht_ffn_fwd(*args, o["Y"], gate=o["gate"], up=o["up"], **kw)
+            B.ht_ffn_bwd(*args, x["dY"][:rows], dX=o["dX"], dWg=o["dWg"], dWu=o["dWu"], dWd=o["dWd"], gate=o["gate"], up=o["up"], **kw)
+            B.ht_ffn_bwd(*args, x["dY"][:rows], dX=o["dX2"], **kw)
+        B.ht_grad_clip(c, self.small, 3.0, out=self.clipped, norm=self.norm, sync=sync)
+        B.ht_grad_norm(c, self.clipped, self.norm2, sync=sync)
+
+    def renew(self, seed):
+        self.g.manual_seed(seed)
+        for t in list(self.ins.values()) + self.small:
+            t.copy_(torch.randn(t.shape, generator=self.g, device="cuda") * 0.3)
+
+    def eager(self):
+        """Results of an unrecorded pass on a context of its own."""
+        other = Work.__new__(Work)
+        other.__dict__.update(self.__dict__)
+        other.outs = {k: {m: torch.zeros_like(t) for m, t in o.items()} for k, o in self.outs.items()}
+        other.clipped, other.norm, other.norm2 = [torch.zeros_like(t) for t in self.clipped], torch.zeros_like(self.norm), torch.zeros_like(self.norm)
+        other.ctx = B.ht_ctx_create(0)
+        torch.cuda.synchronize()
+        other.run(sync=True)
+        B.ht_sync(other.ctx)
+        B.ht_ctx_destroy(other.ctx)
+        return other.outputs()
+
+
+def _same(w, want):
+    for a, b in zip(w.outputs(), want):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("big", [1, 20])
+def test_recorded_and_replayed(big):
+    s = torch.cuda.Stream()
+    ctx = B.ht_ctx_create(0, s.cuda_stream)
+    try:
+        w = Work(ctx, big)
+        w.run()
+        s.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            w.run()
+        for k in range(4):
+            w.renew(100 + k)
+            want = w.eager()                               # the program's own work and synchronizations between the replays
+            for o in w.outputs():
+                o.fill_(float(k))
+            torch.cuda.synchronize()
+            with torch.cuda.stream(s):
+                graph.replay()
+            s.synchronize()
+            _same(w, want)
+        # a larger call outgrows the scratch memory; the graph keeps what it works in
+        Work(ctx, big * 3, seed=9).run()
+        s.synchronize()
+        hog = torch.full((64 << 20,), float("nan"), device="cuda")        # (whoever gets memory that was given back writes into it)
+        w.renew(200)
+        want = w.eager()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(s):
+            graph.replay()
+        s.synchronize()
+        _same(w, want)
+        assert bool(torch.isnan(hog).all())
+        del graph
+    finally:
+        B.ht_ctx_destroy(ctx)
+
+
+def test_a_recorded_first_call_is_refused():
+    s = torch.cuda.Stream()
+    ctx = B.ht_ctx_create(0, s.cuda_stream)
+    try:
+        w = Work(ctx)
+        x, o = torch.zeros(8, device="cuda"), w.outs["many"]
+        i, size = w.ins, (w.d, w.f, w.e)
+        codes = []
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            x.add_(1.0)
+            kw = dict(w_form=B.HT_W_OUT_IN, sync=False)
+            for call in (lambda: B.ht_ffn_fwd(ctx, *size, i["X"], i["Wg"], i["Wu"], i["Wd"], o["Y"], **kw),
+                         lambda: B.ht_ffn_fwd(ctx, *size, i["X"][:2], i["Wg"], i["Wu"], i["Wd"], o["Y"][:2], **kw),
+                         lambda: B.ht_ffn_bwd(ctx, *size, i["X"], i["Wg"], i["Wu"], i["Wd"], i["dY"], dX=o["dX"], **kw),
+                         lambda: B.ht_grad_norm(ctx, w.small, w.norm, sync=False), lambda: B.ht_grad_clip(ctx, w.small, 1.0, sync=False)):
+                try:
+                    call()
+                    codes.append(0)
+                except B.HongtuError as e:
+                    codes.append(e.code)
+        assert codes == [B.HT_ESTATE] * 5
+        with torch.cuda.stream(s):
+            graph.replay()
+            graph.replay()
+        s.synchronize()
+        assert float(x[0]) == 2.0
+        w.run()                                            # and the context works on
+        s.synchronize()
+        _same(w, w.eager())
+        del graph
+    finally:
+        B.ht_ctx_destroy(ctx)
+
+
+def test_two_contexts_at_once():
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    ctxs = [B.ht_ctx_create(0, s.cuda_stream) for s in streams]
+    try:
+        work = [Work(c, big=1 + 15 * i, seed=i) for i, c in enumerate(ctxs)]
+        want = [w.eager() for w in work]
+        for _ in range(5):
+            for w in work:
+                w.run()
+        torch.cuda.synchronize()
+        for w, e in zip(work, want):
+            _same(w, e)
+    finally:
+        for c in ctxs:
+            B.ht_ctx_destroy(c)
+
+
+def test_refused_memory_is_said_and_gone_again():
+    ctx = B.ht_ctx_create(0)
+    try:
+        B.ht_ctx_set_hbm_budget(ctx, 64)
+        w = Work(ctx)
+        o, i, size, kw = w.outs["many"], w.ins, (w.d, w.f, w.e), dict(w_form=B.HT_W_OUT_IN)
+        for call in (lambda: B.ht_ffn_fwd(ctx, *size, i["X"], i["Wg"], i["Wu"], i["Wd"], o["Y"], **kw),
+                     lambda: B.ht_ffn_bwd(ctx, *size, i["X"][:3], i["Wg"], i["Wu"], i["Wd"], i["dY"][:3], dX=o["dX"][:3], **kw),
+                     lambda: B.ht_grad_clip(ctx, w.small, 1.0)):
+            before = [t.clone() for t in w.outputs() + w.small]
+            with pytest.raises(B.HongtuError) as err:
+                call()
+            assert err.value.code == B.HT_ENOMEM
+            B.ht_sync(ctx)
+            assert all(torch.equal(a, b) for a, b in zip(before, w.outputs() + w.small))
+        B.ht_ctx_set_hbm_budget(ctx, 1 << 30)
+        w.run(sync=True)
+        B.ht_sync(ctx)
+        _same(w, w.eager())
+    finally:
+        B.ht_ctx_destroy(ctx)
+
+
+@pytest.mark.parametrize("refused", [1, 2, 3, -1, -2])
+def test_each_allocation_refused(refused, monkeypatch):
+    """The call gets through all the same, or says so and the next one does."""
+    want = Work(None).eager()
+    monkeypatch.setenv("HT_REFUSE_ALLOC", str(refused))
+    ctx = B.ht_ctx_create(0)
+    try:
+        w = Work(ctx)
+        try:
+            w.run(sync=True)
+        except B.HongtuError as e:
+            assert e.code == B.HT_ENOMEM
+            w.run(sync=True)
+        B.ht_sync(ctx)
+        _same(w, want)
+    finally:
+        B.ht_ctx_destroy(ctx)
+
+
+@pytest.mark.parametrize("form", [B.HT_W_IN_OUT, B.HT_W_OUT_IN])
+def test_rows_in_pieces(form):
+    """Under a byte budget the rows go in three pieces (28 KB of scratch memory a row, 64 MiB a piece): forward, backward, added to what is there."""
+    n, d, f, e = 5_000, 60, 2_020, 36
+    X, Wg, Wu, Wd, dY = ffn_inputs(n, d, f, e)
+    ref, tol = reference(X, Wg, Wu, Wd, "silu", dY)
+    ctx = B.ht_ctx_create(0)
+    try:
+        B.ht_ctx_set_hbm_budget(ctx, 120 << 20)
+        check(ffn_call(ctx, X, Wg, Wu, Wd, dY=dY, form=form), ref, tol)
+        check(ffn_call(ctx, X, Wg, Wu, Wd, dY=dY, form=form, keep=True), ref, tol)
+        check(ffn_call(ctx, X, Wg, Wu, Wd, dY=dY, form=form, add=True), ref, tol, add=True)
+        B.ht_ctx_set_hbm_budget(ctx, 0)
+        check(ffn_call(ctx, X, Wg, Wu, Wd, dY=dY, form=form), ref, tol)
+    finally:
+        B.ht_ctx_destroy(ctx)
+
+
+def test_more_than_2_31_hidden_values():
+    """gate and up of 300,000 x 8,192: rows beyond 2^31 values from the first, against the same rows alone."""
+    n, d, f, e, at = 300_000, 16, 8_192, 16, 299_800
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    r = lambda a, b, s: torch.randn(a, b, generator=g, device="cuda") * s
+    X, Wg, Wu, Wd, dY = r(n, d, 1.0), r(d, f, 0.3), r(d, f, 0.25), r(f, e, 0.01), r(n, e, 1e-2)
+    ctx = B.ht_ctx_create(0)
+    try:
+        Y, dX, gate, up = (torch.empty(n, c, device="cuda") for c in (e, d, f, f))
+        B.ht_ffn_fwd(ctx, d, f, e, X, Wg, Wu, Wd, Y, gate=gate, up=up)
+        B.ht_ffn_bwd(ctx, d, f, e, X, Wg, Wu, Wd, dY, dX=dX, gate=gate, up=up)
+        B.ht_sync(ctx)
+        host = [t.cpu().numpy() for t in (X[at:], Wg, Wu, Wd)]
+        ref, tol = reference(*host, "silu", dY[at:].cpu().numpy())
+        check({k: t[at:].cpu().numpy() for k, t in dict(Y=Y, dX=dX, gate=gate, up=up).items()}, ref, tol)
+    finally:
+        B.ht_ctx_destroy(ctx)
+
+
+def test_a_tensor_of_more_than_2_31_values():
+    n = (1 << 31) + 1_003
+    t, norm = torch.ones(n, device="cuda"), torch.zeros(1, device="cuda")
+    ctx = B.ht_ctx_create(0)
+    with pytest.raises(AssertionError):                        # (columns are counted in 32 bits: as a matrix it goes)
+        B.ht_grad_clip(ctx, [t], 1.0, norm=norm)
+    try:
+        m = t[:1 << 31].view(1 << 16, 1 << 15)
+        B.ht_grad_clip(ctx, [m, t[1 << 31:]], 1.0, norm=norm)
+        B.ht_sync(ctx)
+        assert abs(float(norm) - math.sqrt(n)) <= 2.0 ** -23 * math.sqrt(n)
+        want = np.float32(1.0 / math.sqrt(n))
+        for part in (t[:4], t[1 << 30:(1 << 30) + 4], t[(1 << 31) - 2:(1 << 31) + 2], t[-4:]):
+            assert (np.abs(part.cpu().numpy() - want) <= 2.0 ** -22 * want).all()
+    finally:
+        B.ht_ctx_destroy(ctx)
