@@ -57,7 +57,7 @@ constexpr int64_t PACK_BLOCKS = 1024;  // where there are fewer, tiles are share
 struct Packs {
   unsigned first[PACKS + 1];           // blocks before each, and before those that clear words (side by side: one trip to the arguments)
   Pack pack[PACKS];
-  int n;
+  int n = 0;
   uint32_t* zero;                      // words that become 0, by the blocks behind
   int64_t zeros;
 };
@@ -688,12 +688,12 @@ __global__ void __launch_bounds__(256, 2) k_ffn_split(Args a) {
   __shared__ __attribute__((aligned(16))) _Float16 Bs[2 * stage_halfs(MODE == ROWS || MODE == COLS)];
   ffn_split<MODE, ACT>(a, blockIdx.x, Bs);
 }
-// dX, and the gradients of the weights, which do not wait for each other, behind each other's blocks where all of them run at once.
 template <int ACT>
 __global__ void __launch_bounds__(256, 3) k_ffn_project_small(Args a) {
   __shared__ __attribute__((aligned(16))) _Float16 Bs[2 * stage_halfs(false)];
   ffn_split<PROJECT_SMALL, ACT>(a, blockIdx.x, Bs);
 }
+// dX, and the gradients of the weights, which do not wait for each other, behind each other's blocks where all of them run at once.
 struct EndsArgs {
   Args a[3];                           // ROWS, COLS, COLS
   unsigned first[3];                   // blocks before each
@@ -914,8 +914,9 @@ struct Ffn : FfnCall {
         a.e_w = m.at(ew2), a.e_in = m.at(ex);
         a.e_d = m.at(ewd);
         if (!bwd) {
-          const char* sm = getenv("HT_FFN_SMALL");
-          const bool small = a.mt * a.nt < (sm ? atoll(sm) : SLOTS);
+          // (half tiles where whole ones leave room for more blocks: 1,003 x 301 x 1,213 56 -> 49 us, 300 x 256 x 688 44 -> 39; of more tiles they only read more: 16,384 x
+          // 1,024 x 4,096 1,114 -> 1,192)
+          const bool small = a.mt * a.nt < SLOTS;
           if (small) a.nt = ceil_div64(rows, TN / 2);
           HT_TRY(launch(small ? PROJECT_SMALL : PROJECT, a));
         }
