@@ -577,10 +577,10 @@ int ht_grad_norm(ht_ctx *ctx, int32_t n, const ht_tensor *grads, float *norm);
  * step with clipped gradients in one pass).  out: n tensors of the same shapes, or
  * null for grads themselves; one of them may be its gradient (in place: the same
  * pointer and pitch), otherwise out shares no memory with grads or with itself.
- * norm: device float, nullable: the norm before.  c is taken from the norm in 64
- * bits.  With a gradient that is NaN all of out is; with infinite ones c is 0, and
+ * norm: device float, nullable: the norm before.  scale c is made of the norm in 64
+ * bits and rounded once.  With a gradient that is NaN all of out is; with infinite ones c is 0, and
  * out NaN where they are. */
-int ht_grad_clip(ht_ctx *ctx, int32_t n, const ht_tensor *grads, float max_norm, float scale, int32_t accumulate, ht_tensor *out, float *norm);
+int ht_grad_clip(ht_ctx *ctx, int32_t n, const ht_tensor *grads, double max_norm, double scale, int32_t accumulate, ht_tensor *out, float *norm);
 
 /* -------------------------------------------------------------------- epoch */
 

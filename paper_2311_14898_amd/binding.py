@@ -210,7 +210,7 @@ def load():
     lib.ht_ffn_fwd.argtypes = [C.c_void_p, C.POINTER(ht_ffn_desc)] + [C.POINTER(ht_tensor)] * 7
     lib.ht_ffn_bwd.argtypes = [C.c_void_p, C.POINTER(ht_ffn_desc)] + [C.POINTER(ht_tensor)] * 11
     lib.ht_grad_norm.argtypes = [C.c_void_p, C.c_int32, C.POINTER(ht_tensor), C.c_void_p]
-    lib.ht_grad_clip.argtypes = [C.c_void_p, C.c_int32, C.POINTER(ht_tensor), C.c_float, C.c_float, C.c_int32, C.POINTER(ht_tensor), C.c_void_p]
+    lib.ht_grad_clip.argtypes = [C.c_void_p, C.c_int32, C.POINTER(ht_tensor), C.c_double, C.c_double, C.c_int32, C.POINTER(ht_tensor), C.c_void_p]
     _lib = lib
     return lib
 

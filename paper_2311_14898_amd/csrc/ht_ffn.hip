@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(256) k_ffn_pack(Packs packs) {
 // ---------------------------------------------------------------- products
 
 // PROJECT  A's rows: the interleaved hidden columns, B's the rows of X: A and B of the block, H and its largest values
-// BACK     A's rows: 128 hidden columns of Wd, B's the rows of dY: G, from that and A and B all of H, dA, dB and their largest values
+// BACK     A's rows: hidden columns of Wd, B's 64 the rows of dY: G, from that and A and B all of H, dA, dB and their largest values
 // ROWS     A: H or [dA dB] by rows, B: a weight turned: Y, dX
 // COLS     A: X or dY by columns, B: [dA dB] or H turned: gradients of weights
 // PROJECT_SMALL  PROJECT by 64 rows a block, for calls whose tiles are fewer than there is room for, and three blocks a CU
@@ -511,7 +511,7 @@ __device__ __forceinline__ void ffn_split(const Args& a, unsigned block, _Float1
   const Tile tile(block, a.mt, a.nt, a.splits);
   if (tile.m < 0) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
-  constexpr int NI = MODE == BACK ? 1 : 2, NJ = MODE == PROJECT_SMALL ? 2 : 4;       // row blocks of A a wave (BACK has much to do with each sum), and of B
+  constexpr int NI = 2, NJ = MODE == PROJECT_SMALL || MODE == BACK ? 2 : 4;       // row blocks of A a wave, and of B (BACK has much to do with each sum)
   constexpr int NR = NJ * 32;
   const int64_t split = tile.split, m0 = tile.m * (NI * 128), n0 = tile.n * NR, mw = m0 + wave * (NI * 32);
   const int64_t s0 = a.pairs * split / a.splits * 2;                 // its first stage
@@ -555,7 +555,7 @@ __device__ __forceinline__ void ffn_split(const Args& a, unsigned block, _Float1
       for (int u = 0; u < 2; ++u) split8(rb[u * 2], rb[u * 2 + 1], f, [&](int t) { return fc[u][t]; });
     });
   } else {
-    multiply<false, MODE != PROJECT_SMALL>(acc, Ap, a_rows, B, b_rows, nullptr, todo, Bs, a_as_it_is, b_as_it_is);
+    multiply<false, NJ == 4>(acc, Ap, a_rows, B, b_rows, nullptr, todo, Bs, a_as_it_is, b_as_it_is);
   }
 
   // lane l32 + 32 half of a 32 x 32 tile has column l32 and the rows 8 (e / 4) + 4 half + e % 4
@@ -662,24 +662,32 @@ __device__ __forceinline__ void ffn_split(const Args& a, unsigned block, _Float1
     if (tid < NR && n0 + tid < a.n) raise(a.h_row + n0 + tid, __float_as_uint(fmaxf(fmaxf(top[tid], top[NR + tid]), fmaxf(top[2 * NR + tid], top[3 * NR + tid]))));
   }
   if constexpr (MODE == BACK) {
-    float md[4];
-    float* cols = top + 4 * TN;
-    int ey[4];
-    const int e0 = a.e_w[mw / HB];
-    const float *gate[4], *up[4];
-    const bool last = n0 + TN > a.n;
+    float md[NJ] = {};
+    float* cols = top + 4 * NR;
+    int ey[NJ];
+    const float *gate[NJ], *up[NJ];
+    const bool last = n0 + NR > a.n;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < NJ; ++j) {
       const int64_t v = n0 + j * 32 + l32, row = v < a.n ? v : a.n - 1;
       ey[j] = a.e_in[v];
       gate[j] = a.gate + row * a.ld_gate, up[j] = a.up + row * a.ld_up;
     }
-    at.back<ACT, 4>(n0 / 32, mw / HB, md, cols + wave * 96, [&](int j, int k, V4& x, V4& y) {
-      const int64_t c = mw + k * 8 + half * 4;
-      x = at.get(gate[j], c, mw + HB <= a.f), y = at.get(up[j], c, mw + HB <= a.f);
-      if (last && n0 + j * 32 + l32 >= a.n) x = y = V4{0.f, 0.f, 0.f, 0.f};
-    }, [&](int j, int k, int e) { return __builtin_amdgcn_ldexpf(acc[0][j][k * 4 + e], -(ey[j] + e0)); });
-    at.back_tops<4, 4>(n0 / 32, m0, md, cols, top);
+    auto part = [&](const v16f (&sums)[NJ], int i) __attribute__((always_inline)) {
+      const int64_t c0 = mw + i * HB;
+      const int e0 = a.e_w[c0 / HB];
+      float m[NJ];
+      at.back<ACT, NJ>(n0 / 32, c0 / HB, m, cols + (wave * 2 + i) * 96, [&](int j, int k, V4& x, V4& y) {
+        const int64_t c = c0 + k * 8 + half * 4;
+        x = at.get(gate[j], c, c0 + HB <= a.f), y = at.get(up[j], c, c0 + HB <= a.f);
+        if (last && n0 + j * 32 + l32 >= a.n) x = y = V4{0.f, 0.f, 0.f, 0.f};
+      }, [&](int j, int k, int e) { return __builtin_amdgcn_ldexpf(sums[j][k * 4 + e], -(ey[j] + e0)); });
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) md[j] = fmaxf(md[j], m[j]);
+    };
+    part(acc[0], 0);
+    part(acc[1], 1);
+    at.back_tops<NJ, 8>(n0 / 32, m0, md, cols, top);
   }
 }
 
@@ -688,10 +696,12 @@ __global__ void __launch_bounds__(256, 2) k_ffn_split(Args a) {
   __shared__ __attribute__((aligned(16))) _Float16 Bs[2 * stage_halfs(MODE == ROWS || MODE == COLS)];
   ffn_split<MODE, ACT>(a, blockIdx.x, Bs);
 }
-template <int ACT>
-__global__ void __launch_bounds__(256, 3) k_ffn_project_small(Args a) {
+// By 64 rows.  BACK has 199 registers: three blocks a CU would keep 35 of them in memory (30,000 x 128 x 512 91 -> 117 us, 8,192 x 1,024 x 4,096 341 -> 353); half as many hidden columns
+// by 128 rows take as long (356).
+template <int MODE, int ACT>
+__global__ void __launch_bounds__(256, MODE == BACK ? 2 : 3) k_ffn_narrow(Args a) {
   __shared__ __attribute__((aligned(16))) _Float16 Bs[2 * stage_halfs(false)];
-  ffn_split<PROJECT_SMALL, ACT>(a, blockIdx.x, Bs);
+  ffn_split<MODE, ACT>(a, blockIdx.x, Bs);
 }
 // dX, and the gradients of the weights, which do not wait for each other, behind each other's blocks where all of them run at once.
 struct EndsArgs {
@@ -825,8 +835,8 @@ struct Ffn : FfnCall {
     const unsigned grid = (unsigned)blocks;
     switch (mode) {
       case PROJECT: with_act(D->act, [&](auto act) { k_ffn_split<PROJECT, decltype(act)::value><<<grid, 256, 0, ctx->stream>>>(a); }); break;
-      case PROJECT_SMALL: with_act(D->act, [&](auto act) { k_ffn_project_small<decltype(act)::value><<<grid, 256, 0, ctx->stream>>>(a); }); break;
-      case BACK: with_act(D->act, [&](auto act) { k_ffn_split<BACK, decltype(act)::value><<<grid, 256, 0, ctx->stream>>>(a); }); break;
+      case PROJECT_SMALL: with_act(D->act, [&](auto act) { k_ffn_narrow<PROJECT_SMALL, decltype(act)::value><<<grid, 256, 0, ctx->stream>>>(a); }); break;
+      case BACK: with_act(D->act, [&](auto act) { k_ffn_narrow<BACK, decltype(act)::value><<<grid, 256, 0, ctx->stream>>>(a); }); break;
       case ROWS: k_ffn_split<ROWS, 0><<<grid, 256, 0, ctx->stream>>>(a); break;
       default: k_ffn_split<COLS, 0><<<grid, 256, 0, ctx->stream>>>(a);
     }
@@ -929,7 +939,7 @@ struct Ffn : FfnCall {
         HT_LAUNCH_CHECK(ctx);
       } else if (bwd) {
         a.A = m.at(Wf), a.KSA = KSe, a.B = m.at(Gr), a.KSB = KSe;
-        a.mt = ceil_div64(f, TN), a.nt = row_tiles, a.pairs = ceil_div64(e, PAIR);
+        a.mt = ceil_div64(f, TM), a.nt = ceil_div64(rows, TN / 2), a.pairs = ceil_div64(e, PAIR);
         a.e_w = m.at(ewd), a.e_in = m.at(ey);
         HT_TRY(launch(BACK, a));
       }

@@ -94,15 +94,15 @@ __global__ void __launch_bounds__(256) k_grad_squares(List list, double* __restr
 }
 
 // factor (nullable) = scale c
-__global__ void __launch_bounds__(END_THREADS) k_grad_end(const double* __restrict__ part, int64_t n, float* __restrict__ norm, float* __restrict__ factor, float max_norm,
-                                                          float scale) {
+__global__ void __launch_bounds__(END_THREADS) k_grad_end(const double* __restrict__ part, int64_t n, float* __restrict__ norm, float* __restrict__ factor, double max_norm,
+                                                          double scale) {
   double s = 0.0;
   for (int64_t i = threadIdx.x; i < n; i += END_THREADS) s += part[i];
   s = block_sum<END_THREADS>(s);
   if (threadIdx.x != 0) return;
   const double all = sqrt(s);
   if (norm) *norm = (float)all;
-  if (factor) *factor = (float)((double)scale * (all <= (double)max_norm ? 1.0 : (double)max_norm / all));
+  if (factor) *factor = (float)(scale * (all <= max_norm ? 1.0 : max_norm / all));
 }
 
 // PAST: past the caches.  The tensors' units from their last to their first: what the sums have read last is what the caches still hold.
@@ -190,7 +190,7 @@ int in_lists(int32_t n, const ht_tensor* grads, const ht_tensor* out, int unit, 
   return list.n > 0 ? launch(list) : HT_OK;
 }
 
-int grads_run(ht_ctx* ctx, int32_t n, const ht_tensor* grads, const ht_tensor* out, float max_norm, float scale, int add, float* norm, bool scaled) {
+int grads_run(ht_ctx* ctx, int32_t n, const ht_tensor* grads, const ht_tensor* out, double max_norm, double scale, int add, float* norm, bool scaled) {
   hipStream_t st = ctx->stream;
   int64_t parts = 0, vecs = 0;
   for (int32_t i = 0; i < n; ++i)
@@ -226,13 +226,13 @@ extern "C" int ht_grad_norm(ht_ctx* ctx, int32_t n, const ht_tensor* grads, floa
   if (n < 0 || (n > 0 && !grads) || !norm) return ht_set_err(ctx, HT_EINVAL, "ht_grad_norm: %s", n < 0 ? "a negative number of tensors" : "null argument");
   for (int32_t i = 0; i < n; ++i) HT_TRY(check(ctx, "ht_grad_norm", "gradient", i, grads[i]));
   HT_HIP(ctx, hipSetDevice(ctx->device));
-  return ht_with_room(ctx, [&]() -> int { return grads_run(ctx, n, grads, nullptr, 1.f, 1.f, 0, norm, false); });
+  return ht_with_room(ctx, [&]() -> int { return grads_run(ctx, n, grads, nullptr, 1.0, 1.0, 0, norm, false); });
 }
 
-extern "C" int ht_grad_clip(ht_ctx* ctx, int32_t n, const ht_tensor* grads, float max_norm, float scale, int32_t accumulate, ht_tensor* out, float* norm) {
+extern "C" int ht_grad_clip(ht_ctx* ctx, int32_t n, const ht_tensor* grads, double max_norm, double scale, int32_t accumulate, ht_tensor* out, float* norm) {
   if (!ctx) return HT_EINVAL;
   if (n < 0 || (n > 0 && !grads)) return ht_set_err(ctx, HT_EINVAL, "ht_grad_clip: %s", n < 0 ? "a negative number of tensors" : "null argument");
-  if (!(max_norm > 0.f)) return ht_set_err(ctx, HT_EINVAL, "ht_grad_clip: max_norm %g, must be positive", (double)max_norm);
+  if (!(max_norm > 0.0)) return ht_set_err(ctx, HT_EINVAL, "ht_grad_clip: max_norm %g, must be positive", max_norm);
   const ht_tensor* to = out ? out : grads;
   for (int32_t i = 0; i < n; ++i) {
     HT_TRY(check(ctx, "ht_grad_clip", "gradient", i, grads[i]));

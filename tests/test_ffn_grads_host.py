@@ -21,7 +21,7 @@ int main(void) {
   if (ht_ffn_fwd(NULL, NULL, NULL, NULL, NULL, NULL, NULL, NULL, NULL) != HT_EINVAL) return 1;
   if (ht_ffn_bwd(NULL, NULL, NULL, NULL, NULL, NULL, NULL, NULL, NULL, NULL, NULL, NULL, NULL) != HT_EINVAL) return 2;
   if (ht_grad_norm(NULL, 1, NULL, NULL) != HT_EINVAL) return 3;
-  if (ht_grad_clip(NULL, 1, NULL, 1.0f, 1.0f, 0, NULL, NULL) != HT_EINVAL) return 4;
+  if (ht_grad_clip(NULL, 1, NULL, 1.0, 1.0, 0, NULL, NULL) != HT_EINVAL) return 4;
   return 0;
 }
 """
