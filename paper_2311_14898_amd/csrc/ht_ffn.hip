@@ -50,6 +50,7 @@ struct Pack {
   _Float16* T;                         // (nullable) by run, scaled by blocks, KS_t steps; own as the reduction
   int64_t KS_t;
   int tiles;                           // of PACK_RUN along run
+  int steps, blocks_t;                 // of F and of T that are written: whole pairs of stages of a reduction; what a tile has beyond its operand's rows reaches no sum that is kept
   unsigned blocks, share;              // (of so many own rows' blocks each takes a part of the tiles, all of them look for the largest values)
 };
 constexpr int PACKS = 5, PACK_RUN = 128;
@@ -174,12 +175,12 @@ __global__ void __launch_bounds__(256) k_ffn_pack(Packs packs) {
     for (int u = 0; u < 2; ++u) {
       const int ks = wave * 2 + u, k = ks * 16 + half * 4;
       float x[8];
-      if (run0 / 16 + ks < a.KS) {
+      if (run0 / 16 + ks < a.steps) {
 #pragma unroll
         for (int t = 0; t < 8; ++t) x[t] = sh[l32][k + (t >> 2) * 8 + (t & 3)] * fo;
         put(a.F, ((int64_t)block * a.mul + a.add) * a.KS + run0 / 16 + ks, x);
       }
-      if (!a.T) continue;
+      if (!a.T || run0 / 32 + wave >= a.blocks_t) continue;
 #pragma unroll
       for (int t = 0; t < 8; ++t) x[t] = sh[u * 16 + half * 4 + (t >> 2) * 8 + (t & 3)][wave * 32 + l32] * fb;
       put(a.T, (run0 / 32 + wave) * a.KS_t + (int64_t)block * 2 + u, x);
@@ -194,7 +195,9 @@ __global__ void __launch_bounds__(256) k_ffn_pack(Packs packs) {
 // ROWS     A: H or [dA dB] by rows, B: a weight turned: Y, dX
 // COLS     A: X or dY by columns, B: [dA dB] or H turned: gradients of weights
 // PROJECT_SMALL  PROJECT by 64 rows a block, for calls whose tiles are fewer than there is room for, and three blocks a CU
-enum { PROJECT, BACK, ROWS, COLS, PROJECT_SMALL };
+// COLS_SMALL     COLS of at most 128 rows of A
+enum { PROJECT, BACK, ROWS, COLS, PROJECT_SMALL, COLS_SMALL };
+constexpr bool is_cols(int mode) { return mode == COLS || mode == COLS_SMALL; }
 
 struct Out {                           // value (m, n) at m ms + n ns, split_part floats apart
   float* p;
@@ -507,13 +510,13 @@ struct Hidden {
 
 template <int MODE, int ACT>
 __device__ __forceinline__ void ffn_split(const Args& a, unsigned block, _Float16* Bs) {
-  constexpr bool TURN = MODE == ROWS || MODE == COLS;
+  constexpr bool BY_COLS = is_cols(MODE), TURN = MODE == ROWS || BY_COLS;
   const Tile tile(block, a.mt, a.nt, a.splits);
   if (tile.m < 0) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
-  constexpr int NI = 2, NJ = MODE == PROJECT_SMALL || MODE == BACK ? 2 : 4;       // row blocks of A a wave, and of B (BACK has much to do with each sum)
-  constexpr int NR = NJ * 32;
-  const int64_t split = tile.split, m0 = tile.m * (NI * 128), n0 = tile.n * NR, mw = m0 + wave * (NI * 32);
+  constexpr int NI = MODE == COLS_SMALL ? 1 : 2, NJ = MODE == PROJECT_SMALL || MODE == BACK ? 2 : 4;       // row blocks of A a wave, and of B (BACK has much to do with each sum)
+  constexpr int NR = NJ * 32, MT = NI * 128;
+  const int64_t split = tile.split, m0 = tile.m * MT, n0 = tile.n * NR, mw = m0 + wave * (NI * 32);
   const int64_t s0 = a.pairs * split / a.splits * 2;                 // its first stage
   const int todo = __builtin_amdgcn_readfirstlane((int)(a.pairs * (split + 1) / a.splits - s0 / 2));
 
@@ -527,7 +530,7 @@ __device__ __forceinline__ void ffn_split(const Args& a, unsigned block, _Float1
   // exponents of the rows or columns of the sums, a thread each, for the end (looked up there they would be two trips to memory)
   int end = 0;
   if constexpr (MODE == ROWS) end = m0 + tid < a.m_end ? row_exp(m0 + tid) : 0;
-  if constexpr (MODE == COLS) end = tid < TN ? col_exp(n0 + tid) : 0;
+  if constexpr (BY_COLS) end = tid < TN ? col_exp(n0 + tid) : 0;
   v16f acc[NI][NJ];
   clear(acc);
   const _Float16* Ap = a.A + (mw / 32 * a.KSA + s0 * KT) * 2 * FRAG + lane * 8;
@@ -543,7 +546,7 @@ __device__ __forceinline__ void ffn_split(const Args& a, unsigned block, _Float1
       const float f = pow2(er[i] - e);
       split8(x[0], x[1], 1.f, [&](int) { return f; });
     }, b_as_it_is);
-  } else if constexpr (MODE == COLS) {
+  } else if constexpr (BY_COLS) {
     float fc[2][8];
 #pragma unroll
     for (int u = 0; u < 2; ++u)
@@ -559,59 +562,60 @@ __device__ __forceinline__ void ffn_split(const Args& a, unsigned block, _Float1
   }
 
   // lane l32 + 32 half of a 32 x 32 tile has column l32 and the rows 8 (e / 4) + 4 half + e % 4
-  if constexpr (MODE == ROWS || MODE == COLS) {
+  if constexpr (TURN) {
     // Exponents of the rows or columns of sums, all of them looked up at once (where they are used, one after the other, each would be a trip to memory).  Sums go by way of LDS, 32
     // columns at a time, so that what writes them is a short loop: unrolled it is 4,000 instructions a wave (1,003 x 301 x 1,213, Y: 16.2 -> 15.3 us, 8,192 x 1,024 x 4,096, dX: 463 -> 447).
     int* ends = reinterpret_cast<int*>(Bs);
     float* sums = reinterpret_cast<float*>(Bs) + TM;
-    constexpr int P = TM + 4;
+    constexpr int P = MT + 4;
     static_assert((TM + 32 * P) * 4 <= 2 * stage_halfs(true) * 2, "sums of 32 columns beside the exponents");
     ends[tid] = end;
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const bool up = MODE == COLS && a.two && (j & 1);
+      const bool up = BY_COLS && a.two && (j & 1);
       float* out = up ? a.out[1].p : a.out[0].p;
       const int64_t ms = up ? a.out[1].ms : a.out[0].ms, ns = up ? a.out[1].ns : a.out[0].ns, part = up ? a.out[1].split_part : a.out[0].split_part;
       if (!out) continue;
-      const int64_t c0 = MODE == COLS && a.two ? n0 / 2 + j / 2 * HB : n0 + j * 32;      // its first column
+      const int64_t c0 = BY_COLS && a.two ? n0 / 2 + j / 2 * HB : n0 + j * 32;      // its first column
       if (c0 >= a.n_end) continue;
       if (j > 0) __syncthreads();
-      const int en = MODE == COLS ? ends[j * 32 + l32] : 0;
+      const int en = BY_COLS ? ends[j * 32 + l32] : 0;
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < NI; ++i)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const int r = wave * 64 + i * 32 + k * 8 + half * 4;
+          const int r = wave * (NI * 32) + i * 32 + k * 8 + half * 4;
           const int4 em = MODE == ROWS ? *reinterpret_cast<const int4*>(ends + r) : make_int4(0, 0, 0, 0);
           *reinterpret_cast<V4*>(sums + l32 * P + r) =
               V4{__builtin_amdgcn_ldexpf(acc[i][j][k * 4], -(em.x + en)), __builtin_amdgcn_ldexpf(acc[i][j][k * 4 + 1], -(em.y + en)),
                  __builtin_amdgcn_ldexpf(acc[i][j][k * 4 + 2], -(em.z + en)), __builtin_amdgcn_ldexpf(acc[i][j][k * 4 + 3], -(em.w + en))};
         }
       __syncthreads();
-      // fours of neighbours: of a row 32 columns by eight lanes, or of a column 256 rows by a wave
+      // fours of neighbours: of a row 32 columns by eight lanes, or of a column all rows by a wave or half of one
       const bool along = ns == 1;
-      const int m = along ? tid >> 3 : lane * 4, n = along ? (tid & 7) * 4 : wave, m_step = along ? 32 : 0, n_step = along ? 0 : 4;
+      constexpr int LANES = MT / 4, COLUMNS = 256 / LANES, TIMES = MT / 32;      // of a column, columns at a time, how often
+      const int m = along ? tid >> 3 : (tid % LANES) * 4, n = along ? (tid & 7) * 4 : tid / LANES, m_step = along ? 32 : 0, n_step = along ? 0 : COLUMNS;
       float* to = out + split * part + (m0 + m) * ms + (c0 + n) * ns;
-      const int64_t step = along ? 32 * ms : 4 * ns;
+      const int64_t step = along ? 32 * ms : COLUMNS * ns;
       auto four = [&](int it) {
         const float* from = sums + (n + it * n_step) * P + m + it * m_step;
         return along ? V4{from[0], from[P], from[2 * P], from[3 * P]} : *reinterpret_cast<const V4*>(from);
       };
-      if (m0 + TM <= a.m_end && c0 + HB <= a.n_end) {
-        V4 x[8];
+      if (m0 + MT <= a.m_end && c0 + HB <= a.n_end) {
+        V4 x[TIMES];
 #pragma unroll
-        for (int it = 0; it < 8; ++it) x[it] = four(it);
+        for (int it = 0; it < TIMES; ++it) x[it] = four(it);
         if (a.add) {
 #pragma unroll
-          for (int it = 0; it < 8; ++it) x[it] += *reinterpret_cast<const V4u*>(to + it * step);
+          for (int it = 0; it < TIMES; ++it) x[it] += *reinterpret_cast<const V4u*>(to + it * step);
         }
 #pragma unroll
-        for (int it = 0; it < 8; ++it) *reinterpret_cast<V4u*>(to + it * step) = x[it];
+        for (int it = 0; it < TIMES; ++it) *reinterpret_cast<V4u*>(to + it * step) = x[it];
         continue;
       }
 #pragma unroll 1
-      for (int it = 0; it < 8; ++it, to += step) {
+      for (int it = 0; it < TIMES; ++it, to += step) {
         V4 x = four(it);
         const int64_t m_left = a.m_end - (m0 + m + it * m_step), n_left = a.n_end - (c0 + n + it * n_step), left = along ? n_left : m_left;
         if (m_left <= 0 || n_left <= 0) continue;
@@ -693,7 +697,7 @@ __device__ __forceinline__ void ffn_split(const Args& a, unsigned block, _Float1
 
 template <int MODE, int ACT>
 __global__ void __launch_bounds__(256, 2) k_ffn_split(Args a) {
-  __shared__ __attribute__((aligned(16))) _Float16 Bs[2 * stage_halfs(MODE == ROWS || MODE == COLS)];
+  __shared__ __attribute__((aligned(16))) _Float16 Bs[2 * stage_halfs(MODE == ROWS || is_cols(MODE))];
   ffn_split<MODE, ACT>(a, blockIdx.x, Bs);
 }
 // By 64 rows.  BACK has 199 registers: three blocks a CU would keep 35 of them in memory (30,000 x 128 x 512 91 -> 117 us, 8,192 x 1,024 x 4,096 341 -> 353); half as many hidden columns
@@ -708,11 +712,16 @@ struct EndsArgs {
   Args a[3];                           // ROWS, COLS, COLS
   unsigned first[3];                   // blocks before each
 };
+template <int COLS_D, int COLS_H>
 __global__ void __launch_bounds__(256, 2) k_ffn_ends(EndsArgs ends) {
   __shared__ __attribute__((aligned(16))) _Float16 Bs[2 * stage_halfs(true)];
   if (blockIdx.x < ends.first[1]) return ffn_split<ROWS, 0>(ends.a[0], blockIdx.x, Bs);
-  const int k = blockIdx.x < ends.first[2] ? 1 : 2;
-  ffn_split<COLS, 0>(ends.a[k], blockIdx.x - ends.first[k], Bs);
+  if constexpr (COLS_D == COLS_H) {
+    const int k = blockIdx.x < ends.first[2] ? 1 : 2;
+    return ffn_split<COLS_D, 0>(ends.a[k], blockIdx.x - ends.first[k], Bs);
+  }
+  if (blockIdx.x < ends.first[2]) ffn_split<COLS_D, 0>(ends.a[1], blockIdx.x - ends.first[1], Bs);
+  else ffn_split<COLS_H, 0>(ends.a[2], blockIdx.x - ends.first[2], Bs);
 }
 
 // PROJECT and BACK in one where A and B were not kept: 128 hidden columns by 64 rows, 32 by 64 a wave, first A and B, then G; three blocks a CU, which is what hides their ends.  (Of 96
@@ -756,17 +765,24 @@ __global__ void __launch_bounds__(256, 3) k_ffn_remake(RemakeArgs r) {
   at.back_tops<NJ, 4>(b0, tile.m * 4 * HB, md, cols, top);
 }
 
+constexpr int JOIN_MANY = 32;
 __global__ void __launch_bounds__(256) k_ffn_join(FfnJoins joins) {
   int k = 0;
 #pragma unroll
   for (int i = 1; i < FFN_JOINS; ++i) k += blockIdx.x >= joins.first[i];
   const unsigned block = blockIdx.x - joins.first[k];
   const FfnJoin& a = joins.join[k];
-  const int64_t nv = a.pitch / 4, i = (int64_t)block * 256 + threadIdx.x, r = i / nv, c = (i - r * nv) * 4;
-  if (r >= a.rows || c >= a.cols) return;
+  // eight lanes a value where there are many parts of few values
+  const int sub = a.parts >= JOIN_MANY ? threadIdx.x & 7 : 0, subs = a.parts >= JOIN_MANY ? 8 : 1;
+  const int64_t nv = a.pitch / 4, i = ((int64_t)block * 256 + threadIdx.x) / subs, r = i / nv, c = (i - r * nv) * 4;
+  if (r >= a.rows || c >= a.cols) return;      // (all eight of them)
   V4 s{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
-  for (int p = 0; p < a.parts; ++p) s += *reinterpret_cast<const V4*>(a.sums + p * a.part + r * a.pitch + c);
+  for (int p = sub; p < a.parts; p += subs) s += *reinterpret_cast<const V4*>(a.sums + p * a.part + r * a.pitch + c);
+  if (subs > 1) {
+    for (int o = 1; o < 8; o <<= 1) s += V4{__shfl_xor(s[0], o, 64), __shfl_xor(s[1], o, 64), __shfl_xor(s[2], o, 64), __shfl_xor(s[3], o, 64)};
+    if (sub > 0) return;
+  }
   float* to = a.out + r * a.ld + c;
   if (c + 4 <= a.cols) {
     if (a.add) s += *reinterpret_cast<const V4u*>(to);
@@ -811,7 +827,7 @@ struct Ends {
     one = most > 0;
     for (int k = 0; k < 3; ++k) {
       const int64_t n = one ? ceil_div64(pairs[k], most) : tiles[k] > 0 ? std::min(SLOTS / tiles[k], pairs[k] / LEAST_PAIRS) : 1;
-      parts[k] = (int)std::max<int64_t>(1, std::min<int64_t>(n, 64));
+      parts[k] = (int)std::max<int64_t>(1, std::min<int64_t>(n, 512));
     }
   }
 };
@@ -838,7 +854,8 @@ struct Ffn : FfnCall {
       case PROJECT_SMALL: with_act(D->act, [&](auto act) { k_ffn_narrow<PROJECT_SMALL, decltype(act)::value><<<grid, 256, 0, ctx->stream>>>(a); }); break;
       case BACK: with_act(D->act, [&](auto act) { k_ffn_narrow<BACK, decltype(act)::value><<<grid, 256, 0, ctx->stream>>>(a); }); break;
       case ROWS: k_ffn_split<ROWS, 0><<<grid, 256, 0, ctx->stream>>>(a); break;
-      default: k_ffn_split<COLS, 0><<<grid, 256, 0, ctx->stream>>>(a);
+      case COLS: k_ffn_split<COLS, 0><<<grid, 256, 0, ctx->stream>>>(a); break;
+      default: k_ffn_split<COLS_SMALL, 0><<<grid, 256, 0, ctx->stream>>>(a);
     }
     HT_LAUNCH_CHECK(ctx);
     return HT_OK;
@@ -856,7 +873,9 @@ struct Ffn : FfnCall {
     // tiles of the products, and parts of their reductions
     const int64_t mt = Rp / TM, nte = up_to(e, TN) / TN, ntd = up_to(d, TN) / TN, ntD = ceil_div64(f, 64), ntH = ceil_div64(f, TN);
     const int64_t pairs_f = ceil_div64(f, PAIR), pairs_2f = ceil_div64(f, HB), pairs_r = ceil_div64(std::min(n, Rp), PAIR);
-    const Ends ends(Y ? mt * nte : dX ? mt * ntd : 0, Y ? pairs_f : pairs_2f, d_w ? dp / TM * ntD : 0, pairs_r, dWd ? ep / TM * ntH : 0, pairs_r);
+    const int cols_D = d <= TN ? COLS_SMALL : COLS, cols_H = e <= TN ? COLS_SMALL : COLS;
+    const int64_t mtD = cols_D == COLS ? dp / TM : 1, mtH = cols_H == COLS ? ep / TM : 1;
+    const Ends ends(Y ? mt * nte : dX ? mt * ntd : 0, Y ? pairs_f : pairs_2f, d_w ? mtD * ntD : 0, pairs_r, dWd ? mtH * ntH : 0, pairs_r);
     const int sy = ends.parts[0], sx = sy, sD = ends.parts[1], sH = ends.parts[2];
     const int64_t e4 = up_to(e, 4), d4 = up_to(d, 4), f4 = up_to(f, 4);
     // a weight's gradient as it lies: rows and pitch of its parts
@@ -881,19 +900,20 @@ struct Ffn : FfnCall {
       const int64_t r0 = k * Rp, rows = std::min(Rp, n - r0);
       Packs packs{};
       unsigned blocks = 0;
-      auto operand = [&](Pack q, int64_t own, int64_t run) {           // zeros up to so many of either
-        q.tiles = (int)ceil_div64(run, PACK_RUN), q.blocks = (unsigned)(own / HB);
+      auto operand = [&](Pack q, int64_t own) {                         // (zeros up to so many of its own)
+        q.tiles = (int)ceil_div64(q.run, PACK_RUN), q.blocks = (unsigned)(own / HB);
+        q.steps = (int)(up_to(q.run, PAIR) / 16), q.blocks_t = (int)ceil_div64(q.run, 32);
         blocks += q.blocks;
         packs.pack[packs.n++] = q;
       };
-      operand(Pack{X->ptr + r0 * X->ld, X->ld, rows, d, 0, m.at(ex), m.at(exb), m.at(Xr), KSd, 1, 0, d_w ? m.at(Xt) : nullptr, KSR, 0, 0}, up_to(rows, TM), d_w ? dp : KSd * 16);
+      operand(Pack{X->ptr + r0 * X->ld, X->ld, rows, d, 0, m.at(ex), m.at(exb), m.at(Xr), KSd, 1, 0, d_w ? m.at(Xt) : nullptr, KSR}, up_to(rows, TM));
       if (bwd)
-        operand(Pack{dY->ptr + r0 * dY->ld, dY->ld, rows, e, 0, m.at(ey), m.at(eyb), m.at(Gr), KSe, 1, 0, dWd ? m.at(Gt) : nullptr, KSR, 0, 0}, up_to(rows, TM), dWd ? ep : KSe * 16);
+        operand(Pack{dY->ptr + r0 * dY->ld, dY->ld, rows, e, 0, m.at(ey), m.at(eyb), m.at(Gr), KSe, 1, 0, dWd ? m.at(Gt) : nullptr, KSR}, up_to(rows, TM));
       if (k == 0) {
         // by hidden columns: the rows of an OUT_IN Wg, the columns of an IN_OUT one
-        operand(Pack{Wg->ptr, Wg->ld, f, d, in_out, nullptr, m.at(ew2), m.at(W2), KSd, 2, 0, nullptr, 0, 0, 0}, fp, KSd * 16);
-        operand(Pack{Wu->ptr, Wu->ld, f, d, in_out, nullptr, m.at(ew2), m.at(W2), KSd, 2, 1, nullptr, 0, 0, 0}, fp, KSd * 16);
-        operand(Pack{Wd->ptr, Wd->ld, f, e, !in_out, nullptr, m.at(ewd), m.at(Wf), KSe, 1, 0, nullptr, 0, 0, 0}, fp, KSe * 16);
+        operand(Pack{Wg->ptr, Wg->ld, f, d, in_out, nullptr, m.at(ew2), m.at(W2), KSd, 2, 0, nullptr, 0}, fp);
+        operand(Pack{Wu->ptr, Wu->ld, f, d, in_out, nullptr, m.at(ew2), m.at(W2), KSd, 2, 1, nullptr, 0}, fp);
+        operand(Pack{Wd->ptr, Wd->ld, f, e, !in_out, nullptr, m.at(ewd), m.at(Wf), KSe, 1, 0, nullptr, 0}, fp);
       }
       const unsigned share = (unsigned)std::max<int64_t>(1, PACK_BLOCKS / blocks);
       blocks = 0;
@@ -977,16 +997,18 @@ struct Ffn : FfnCall {
       if (Y) HT_TRY(launch(ROWS, by_rows(Y, m.at(H), KSH, false, m.at(Wf), KSe, m.at(ewd), e, nte, pairs_f, sy, m.at(sums_y), e4)));
       Args ax{}, ad{}, ah{};                             // (no tiles: not asked for)
       if (dX) ax = by_rows(dX, m.at(Df), KSD, true, m.at(W2), KSd, m.at(ew2), d, ntd, pairs_2f, sx, m.at(sums_x), d4);
-      if (d_w) ad = by_cols(m.at(Xt), m.at(exb), d, m.at(Df), KSD, true, dp / TM, ntD, sD, m.at(sums_D), wr, wp, dWg, dWu, in_out);
-      if (dWd) ah = by_cols(m.at(Gt), m.at(eyb), e, m.at(H), KSH, false, ep / TM, ntH, sH, m.at(sums_H), vr, vp, dWd, nullptr, !in_out);
+      if (d_w) ad = by_cols(m.at(Xt), m.at(exb), d, m.at(Df), KSD, true, mtD, ntD, sD, m.at(sums_D), wr, wp, dWg, dWu, in_out);
+      if (dWd) ah = by_cols(m.at(Gt), m.at(eyb), e, m.at(H), KSH, false, mtH, ntH, sH, m.at(sums_H), vr, vp, dWd, nullptr, !in_out);
       const int64_t bx = blocks_of(ax), bd = blocks_of(ad), bh = blocks_of(ah);
       if (bwd && ends.one) {
-        k_ffn_ends<<<(unsigned)(bx + bd + bh), 256, 0, st>>>(EndsArgs{{ax, ad, ah}, {0, (unsigned)bx, (unsigned)(bx + bd)}});
+        const auto kernel = cols_D == COLS ? (cols_H == COLS ? k_ffn_ends<COLS, COLS> : k_ffn_ends<COLS, COLS_SMALL>)
+                                           : (cols_H == COLS ? k_ffn_ends<COLS_SMALL, COLS> : k_ffn_ends<COLS_SMALL, COLS_SMALL>);
+        kernel<<<(unsigned)(bx + bd + bh), 256, 0, st>>>(EndsArgs{{ax, ad, ah}, {0, (unsigned)bx, (unsigned)(bx + bd)}});
         HT_LAUNCH_CHECK(ctx);
       } else {
         if (bx) HT_TRY(launch(ROWS, ax));
-        if (bd) HT_TRY(launch(COLS, ad));
-        if (bh) HT_TRY(launch(COLS, ah));
+        if (bd) HT_TRY(launch(cols_D, ad));
+        if (bh) HT_TRY(launch(cols_H, ah));
       }
       HT_TRY(ht_ffn_join(ctx, j));
     }
@@ -1051,7 +1073,7 @@ int ht_ffn_join(ht_ctx* ctx, FfnJoins& j) {
   for (int k = 0; k < j.n; ++k) {
     FfnJoin& a = j.join[k];
     j.first[k] = grid;
-    grid += (unsigned)ceil_div64(a.rows * (a.pitch / 4), 256);
+    grid += (unsigned)ceil_div64(a.rows * (a.pitch / 4) * (a.parts >= JOIN_MANY ? 8 : 1), 256);
   }
   for (int k = j.n; k < FFN_JOINS; ++k) j.first[k] = grid;
   if (grid == 0) return HT_OK;

@@ -309,6 +309,20 @@ def test_rows_in_pieces(form):
         B.ht_ctx_destroy(ctx)
 
 
+def test_scratch_memory_that_holds_nan():
+    """What an earlier call left in the scratch memory reaches nothing: NaN all over it, then widths and rows that end inside every kind of tile."""
+    ctx = B.ht_ctx_create(0)
+    try:
+        for n, d, f, e in [(70, 10, 20, 12), (100, 65, 33, 129), (300, 130, 70, 20), (65, 257, 129, 64), (1000, 16, 300, 100), (40, 17, 50, 9), (2, 300, 90, 70)]:
+            X, Wg, Wu, Wd, dY = ffn_inputs(1500, 330, 600, 270)
+            ffn_call(ctx, X * np.nan, Wg, Wu, Wd * np.nan, dY=dY * np.nan)
+            X, Wg, Wu, Wd, dY = ffn_inputs(n, d, f, e)
+            ref, tol = reference(X, Wg, Wu, Wd, "gelu_tanh", dY)
+            check(ffn_call(ctx, X, Wg, Wu, Wd, act="gelu_tanh", dY=dY, keep=n % 3 == 1), ref, tol)
+    finally:
+        B.ht_ctx_destroy(ctx)
+
+
 def test_more_than_2_31_hidden_values():
     """gate and up of 300,000 x 8,192: rows beyond 2^31 values from the first, against the same rows alone."""
     n, d, f, e, at = 300_000, 16, 8_192, 16, 299_800
