@@ -578,10 +578,11 @@ int ht_ffn_bwd(ht_ctx *ctx, const ht_ffn_desc *desc, const ht_tensor *X, const h
 
 /* The norm of the values of n tensors together, in HBM and of any row pitch:
  *   *norm = sqrt(sum of the squares of them all)
- * norm: device float.  Squares are added up in 64 bits: no value is too small or
- * too large for its square, but a norm above the largest float is +inf.  grads is
- * an array of n on the host, which the call is done with when it returns; n may be
- * 0 (a norm of 0).  A tensor that is named twice counts twice. */
+ * norm: device float, none of the tensors' values.  Squares are added up in 64 bits:
+ * no value is too small or too large for its square, but a norm above the largest
+ * float is +inf.  grads is an array of n on the host, which the call is done with
+ * when it returns; n may be 0 (a norm of 0).  A tensor that is named twice counts
+ * twice. */
 int ht_grad_norm(ht_ctx *ctx, int32_t n, const ht_tensor *grads, float *norm);
 /* The same norm, and every tensor scaled so that it is at most max_norm > 0 (+inf: as
  * it is):
@@ -590,9 +591,9 @@ int ht_grad_norm(ht_ctx *ctx, int32_t n, const ht_tensor *grads, float *norm);
  * step with clipped gradients in one pass).  out: n tensors of the same shapes, or
  * null for grads themselves; one of them may be its gradient (in place: the same
  * pointer and pitch), otherwise out shares no memory with grads or with itself.
- * norm: device float, nullable: the norm before.  scale c is made of the norm in 64
- * bits and rounded once.  With a gradient that is NaN all of out is; with infinite ones c is 0, and
- * out NaN where they are. */
+ * norm: device float, nullable, none of the tensors' values: the norm before.  scale c
+ * is made of the norm in 64 bits and rounded once.  With a gradient that is NaN all
+ * of out is; with infinite ones c is 0, and out NaN where they are. */
 int ht_grad_clip(ht_ctx *ctx, int32_t n, const ht_tensor *grads, double max_norm, double scale, int32_t accumulate, ht_tensor *out, float *norm);
 
 /* -------------------------------------------------------------------- epoch */

@@ -168,6 +168,18 @@ int check_shared(ht_ctx* ctx, int32_t n, const ht_tensor* grads, const ht_tensor
   return HT_OK;
 }
 
+// norm is none of a tensor's values (it may lie between its rows): scaled with them it would be no norm, and the norm written over a gradient would be scaled.
+int check_norm(ht_ctx* ctx, const char* name, const char* what, int32_t n, const ht_tensor* t, const float* norm) {
+  const uintptr_t p = (uintptr_t)norm;
+  if (p & 3) return ht_set_err(ctx, HT_EINVAL, "%s: norm must be 4-byte aligned", name);
+  for (int32_t i = 0; norm && i < n; ++i) {
+    const uintptr_t a = (uintptr_t)t[i].ptr, row = (uintptr_t)t[i].ld * 4;
+    if (p < a || t[i].rows == 0 || t[i].cols == 0 || (p - a) / row >= (uintptr_t)t[i].rows || (p - a) % row >= (uintptr_t)t[i].cols * 4) continue;
+    return ht_set_err(ctx, HT_EINVAL, "%s: norm shares memory with %s %d", name, what, i);
+  }
+  return HT_OK;
+}
+
 // Launches over the tensors, LIST of them at a time: launch(list).  With out from the last tensor to the first.
 template <class F>
 int in_lists(int32_t n, const ht_tensor* grads, const ht_tensor* out, int unit, F&& launch) {
@@ -225,6 +237,7 @@ extern "C" int ht_grad_norm(ht_ctx* ctx, int32_t n, const ht_tensor* grads, floa
   if (!ctx) return HT_EINVAL;
   if (n < 0 || (n > 0 && !grads) || !norm) return ht_set_err(ctx, HT_EINVAL, "ht_grad_norm: %s", n < 0 ? "a negative number of tensors" : "null argument");
   for (int32_t i = 0; i < n; ++i) HT_TRY(check(ctx, "ht_grad_norm", "gradient", i, grads[i]));
+  HT_TRY(check_norm(ctx, "ht_grad_norm", "gradient", n, grads, norm));
   HT_HIP(ctx, hipSetDevice(ctx->device));
   return ht_with_room(ctx, [&]() -> int { return grads_run(ctx, n, grads, nullptr, 1.0, 1.0, 0, norm, false); });
 }
@@ -246,6 +259,8 @@ extern "C" int ht_grad_clip(ht_ctx* ctx, int32_t n, const ht_tensor* grads, doub
   } catch (const std::bad_alloc&) {
     return ht_set_err(ctx, HT_ENOMEM, "ht_grad_clip: no host memory for %d tensors", n);
   }
+  HT_TRY(check_norm(ctx, "ht_grad_clip", "gradient", n, grads, norm));
+  if (out) HT_TRY(check_norm(ctx, "ht_grad_clip", "out", n, out, norm));
   HT_HIP(ctx, hipSetDevice(ctx->device));
   return ht_with_room(ctx, [&]() -> int { return grads_run(ctx, n, grads, to, max_norm, scale, accumulate, norm, true); });
 }

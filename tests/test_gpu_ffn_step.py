@@ -309,6 +309,22 @@ def test_rows_in_pieces(form):
         B.ht_ctx_destroy(ctx)
 
 
+@pytest.mark.parametrize("form", [B.HT_W_IN_OUT, B.HT_W_OUT_IN])
+def test_a_last_piece_of_one_row(form):
+    """Of the parts that the gradients' sums are cut into most have nothing of the last piece."""
+    d, f, e, piece = 60, 2_020, 36, 2_304                 # (64 MiB of 28,672 bytes a row, in 256s)
+    n = 2 * piece + 1
+    X, Wg, Wu, Wd, dY = ffn_inputs(n, d, f, e)
+    ref, tol = reference(X, Wg, Wu, Wd, "silu", dY)
+    ctx = B.ht_ctx_create(0)
+    try:
+        B.ht_ctx_set_hbm_budget(ctx, 120 << 20)
+        check(ffn_call(ctx, X, Wg, Wu, Wd, dY=dY, form=form), ref, tol)
+        check(ffn_call(ctx, X, Wg, Wu, Wd, dY=dY, form=form, keep=True, add=True), ref, tol, add=True)
+    finally:
+        B.ht_ctx_destroy(ctx)
+
+
 def test_scratch_memory_that_holds_nan():
     """What an earlier call left in the scratch memory reaches nothing: NaN all over it, then widths and rows that end inside every kind of tile."""
     ctx = B.ht_ctx_create(0)

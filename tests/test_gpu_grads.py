@@ -205,3 +205,23 @@ def test_refusals(ctx):
     B.ht_grad_norm(ctx, [b, b], norm)                                                                # a norm may count a tensor twice
     B.ht_sync(ctx)
     assert abs(float(norm) - np.sqrt(96)) < 1e-5
+
+
+def test_a_norm_lies_in_no_tensor(ctx):
+    """Written over a gradient it would be scaled with it, written over an output it would be none; between a tensor's rows it may lie."""
+    whole, out = torch.ones(6, 8, device="cuda"), torch.zeros(6, 8, device="cuda")
+    norm = whole.view(-1)
+    for at in (0, 4, 43, 44):                                       # the first value, the first row's last, the last row's
+        for call in (lambda: B.ht_grad_norm(ctx, [out, whole], norm[at:at + 1], cols=[8, 5]),
+                     lambda: B.ht_grad_clip(ctx, [out, whole], 1.0, norm=norm[at:at + 1], cols=[8, 5]),
+                     lambda: B.ht_grad_clip(ctx, [out], 1.0, out=[whole], norm=norm[at:at + 1], cols=[5])):
+            with pytest.raises(B.HongtuError) as err:
+                call()
+            assert err.value.code == -1 and "norm shares memory" in str(err.value)
+    assert (whole == 1).all() and (out == 0).all()
+    for at in (5, 15, 45, 47):                                      # behind a row's five values
+        whole.fill_(1.0)
+        B.ht_grad_clip(ctx, [whole], 1.0, norm=norm[at:at + 1], cols=[5])
+        B.ht_sync(ctx)
+        assert float(norm[at]) == np.float32(np.sqrt(30.0))
+        assert (np.abs(whole[:, :5].cpu().numpy() - 1 / np.sqrt(30.0)) <= 2 * HALF).all()
