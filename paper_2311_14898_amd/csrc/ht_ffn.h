@@ -11,8 +11,10 @@ struct FfnCall {
   const ht_tensor *Y, *dY, *dX, *dWg, *dWu, *dWd;
   bool in_out() const { return D->w_form == HT_W_IN_OUT; }
 };
-// Of 1 .. HT_FFN_FEW rows (ht_ffn_few.hip).
+// Of 1 .. HT_FFN_FEW rows (ht_ffn_few.hip); with FEW_WEIGHTS values of weights, of at most 16: more multiply longer there than they read (2,048 x 8,192, us there | with weights split: forward
+// of 16 rows 51 | 59, 17 66 | 58, 64 112 | 62, backward 176 | 188, 192 | 195, 316 | 204; 1,024 x 4,096: forward of 48 rows 30 | 36, 64 39 | 36, backward 68 | 77, 82 | 79).
 constexpr int HT_FFN_FEW = 64;
+constexpr int64_t FEW_WEIGHTS = (int64_t)1 << 24;
 int ht_ffn_few(const FfnCall& c);
 
 // out [rows x cols] (+)= the sum of `parts` blocks of [rows x pitch], added up in their order; all of them in one launch.
@@ -66,6 +68,15 @@ __device__ __forceinline__ Act act_of(float a) {
     return {a * phi, fmaf(a * 0.39894228040143268f, e, phi)};
   }
   return {a < 0.f ? 0.f : a, a > 0.f ? 1.f : a * 0.f};      // (NaN stays NaN)
+}
+__device__ __forceinline__ Act any_act(int act, float a) {
+  switch (act) {
+    case HT_GATE_SILU: return act_of<HT_GATE_SILU>(a);
+    case HT_GATE_GELU: return act_of<HT_GATE_GELU>(a);
+    case HT_GATE_GELU_TANH: return act_of<HT_GATE_GELU_TANH>(a);
+    case HT_GATE_RELU: return act_of<HT_GATE_RELU>(a);
+    default: return act_of<HT_GATE_SIGMOID>(a);
+  }
 }
 
 }  // namespace

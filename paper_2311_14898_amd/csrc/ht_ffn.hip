@@ -81,43 +81,59 @@ __global__ void __launch_bounds__(256) k_ffn_pack(Packs packs) {
   const int64_t own0 = (int64_t)block * HB, left = a.own - own0;               // (left may be <= 0: zeros)
   if (tid < HB) top[tid] = 0;
   __syncthreads();
+  // What is there at (row, c .. c + 3); the others are 0.  Loads have no condition (rows and columns behind the last are the last again), so that they go together: with one each, 128 x
+  // 1,024 rows took 17 us.  whole: all of the columns that the block looks at are there.
+  auto four = [&](int64_t row, int64_t c, int64_t rows, int64_t cols, bool whole) __attribute__((always_inline)) {
+    const float* from = a.p + (row < rows ? row : rows - 1) * a.ld;
+    V4 x;
+    if (whole) {
+      x = *reinterpret_cast<const V4u*>(from + c);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[k] = from[c + k < cols ? c + k : cols - 1];
+    }
+    return x;
+  };
+  auto there = [&](V4 x, int64_t row, int64_t c, int64_t rows, int64_t cols) __attribute__((always_inline)) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = row < rows && c + k < cols ? x[k] : 0.f;
+    return x;
+  };
   if (!a.turned) {
     // a wave eight rows
     uint32_t m[8] = {};
-    for (int64_t c0 = 0; c0 < a.run; c0 += 256) {
-      const int64_t c = c0 + lane * 4;
+    auto look = [&](int64_t c0, bool whole) __attribute__((always_inline)) {
+      V4 x[8];
 #pragma unroll
-      for (int q = 0; q < 8; ++q) {
-        if (wave * 8 + q >= left) continue;
-        const float* from = a.p + (own0 + wave * 8 + q) * a.ld + c;
-        if (c + 4 <= a.run) {
-          m[q] = max(m[q], max4(*reinterpret_cast<const V4u*>(from)));
-        } else {
+      for (int q = 0; q < 8; ++q) x[q] = four(own0 + wave * 8 + q, c0 + lane * 4, a.own, a.run, whole);
 #pragma unroll
-          for (int k = 0; k < 3; ++k)
-            if (c + k < a.run) m[q] = max(m[q], size_bits(from[k]));
-        }
-      }
-    }
+      for (int q = 0; q < 8; ++q) m[q] = max(m[q], max4(x[q]));                // (the last column again is no larger)
+    };
+    int64_t c0 = 0;
+#pragma unroll 2
+    for (; c0 + 256 <= a.run; c0 += 256) look(c0, true);
+    if (c0 < a.run) look(c0, false);
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
       for (int o = 32; o > 0; o >>= 1) m[q] = max(m[q], (uint32_t)__shfl_xor((int)m[q], o, 64));
-      if (lane == 0) top[wave * 8 + q] = m[q];
+      if (lane == 0) top[wave * 8 + q] = wave * 8 + q < left ? m[q] : 0;
     }
   } else {
     // eight lanes a row of 32 columns
     uint32_t m = 0;
-    const int64_t c = own0 + (tid & 7) * 4;
-#pragma unroll 4
-    for (int64_t r = tid >> 3; r < a.run; r += 32) {
-      const float* from = a.p + r * a.ld + c;
-      if (c + 4 <= a.own) {
-        m = max(m, max4(*reinterpret_cast<const V4u*>(from)));
-      } else {
+    auto look = [&](int64_t r0, bool whole) __attribute__((always_inline)) {
+      V4 x[4];
 #pragma unroll
-        for (int k = 0; k < 3; ++k)
-          if (c + k < a.own) m = max(m, size_bits(from[k]));
-      }
+      for (int q = 0; q < 4; ++q) x[q] = four(r0 + q * 32 + (tid >> 3), own0 + (tid & 7) * 4, a.run, a.own, whole);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) m = max(m, max4(x[q]));
+    };
+    const bool whole = left >= HB;
+    if (whole) {
+#pragma unroll 2
+      for (int64_t r0 = 0; r0 < a.run; r0 += 128) look(r0, true);
+    } else if (left > 0) {
+      for (int64_t r0 = 0; r0 < a.run; r0 += 128) look(r0, false);
     }
     for (int o = 32; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
     if (lane == 0) top[wave] = m;      // (the others stay 0)
@@ -144,22 +160,23 @@ __global__ void __launch_bounds__(256) k_ffn_pack(Packs packs) {
   for (int tile = part; tile < a.tiles; tile += a.share) {
     const int64_t run0 = (int64_t)tile * PACK_RUN;
     V4 y[4];
+    // 32 lanes a row of PACK_RUN, or eight a row of 32
+    const int64_t rows = a.turned ? a.run : a.own, cols = a.turned ? a.own : a.run;
+    auto fetch = [&](bool whole) __attribute__((always_inline)) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      // 32 lanes a row of PACK_RUN, or eight a row of 32
-      const int r = a.turned ? q * 32 + (tid >> 3) : q * 8 + (tid >> 5), c4 = a.turned ? (tid & 7) * 4 : (tid & 31) * 4;
-      const int64_t row = (a.turned ? run0 : own0) + r, c = (a.turned ? own0 : run0) + c4, cols = a.turned ? a.own : a.run;
-      y[q] = V4{0.f, 0.f, 0.f, 0.f};
-      if (row >= (a.turned ? a.run : a.own)) continue;
-      const float* from = a.p + row * a.ld + c;
-      if (c + 4 <= cols) {
-        y[q] = *reinterpret_cast<const V4u*>(from);
-      } else {
-#pragma unroll
-        for (int k = 0; k < 3; ++k)
-          if (c + k < cols) y[q][k] = from[k];
+      for (int q = 0; q < 4; ++q) {
+        const int r = a.turned ? q * 32 + (tid >> 3) : q * 8 + (tid >> 5), c4 = a.turned ? (tid & 7) * 4 : (tid & 31) * 4;
+        y[q] = four((a.turned ? run0 : own0) + r, (a.turned ? own0 : run0) + c4, rows, cols, whole);
       }
-    }
+      if (whole && left >= HB && run0 + PACK_RUN <= a.run) return;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int r = a.turned ? q * 32 + (tid >> 3) : q * 8 + (tid >> 5), c4 = a.turned ? (tid & 7) * 4 : (tid & 31) * 4;
+        y[q] = there(y[q], (a.turned ? run0 : own0) + r, (a.turned ? own0 : run0) + c4, rows, cols);
+      }
+    };
+    if (a.turned ? left >= HB : run0 + PACK_RUN <= a.run) fetch(true);
+    else fetch(false);
     __syncthreads();
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
@@ -765,6 +782,8 @@ __global__ void __launch_bounds__(256, 3) k_ffn_remake(RemakeArgs r) {
   at.back_tops<NJ, 4>(b0, tile.m * 4 * HB, md, cols, top);
 }
 
+#include "ht_ffn_stream.h"
+
 constexpr int JOIN_MANY = 32;
 __global__ void __launch_bounds__(256) k_ffn_join(FfnJoins joins) {
   int k = 0;
@@ -801,6 +820,10 @@ constexpr int64_t SLOTS = 512;                     // blocks that run together: 
 constexpr int64_t LEAST_PAIRS = 4;                 // of a part of a reduction, where a product has a launch for itself
 
 constexpr int64_t SHORT_PAIRS = 8;
+// Weights that are read once (ht_ffn_stream.h) against packed ones, us: forward 128 x 1,024 x 4,096 41 | 89, 512 x 512 x 2,048 43 | 53, 512 x 2,048 x 8,192 284 | 301, 1,024 x 512 x 2,048
+// 64 | 60; backward 128 x 1,024 x 4,096 91 | 130, 256 x 512 x 2,048 73 | 75, 128 x 256 x 1,024 53 | 52, 384 x 1,024 x 4,096 186 | 160 (both have a launch more).
+constexpr int64_t STREAM_ROWS = 512, STREAM_ROWS_BWD = 256, STREAM_WEIGHTS_BWD = (int64_t)1 << 21;
+constexpr int64_t STREAM_BLOCKS = 256;             // of Y or dX, at most: one a CU
 
 // The products behind H, dA and dB: their tiles, pairs of stages of a tile's reduction, and the parts that it is cut into.
 struct Ends {
@@ -860,6 +883,25 @@ struct Ffn : FfnCall {
     HT_LAUNCH_CHECK(ctx);
     return HT_OK;
   }
+  int stream_hidden(const StreamHidden& s) const {
+    const unsigned grid = (unsigned)up_to(s.row_tiles * ceil_div64(s.a.f, HB), 8);
+    if (dY) (in_out() ? k_stream_hidden<true, true> : k_stream_hidden<false, true>)<<<grid, STREAM_WAVES * 64, 0, ctx->stream>>>(s);
+    else (in_out() ? k_stream_hidden<true, false> : k_stream_hidden<false, false>)<<<grid, STREAM_WAVES * 64, 0, ctx->stream>>>(s);
+    HT_LAUNCH_CHECK(ctx);
+    return HT_OK;
+  }
+  int stream_out(const StreamOut& s) const {
+    const unsigned grid = (unsigned)up_to(s.row_tiles * ceil_div64(s.width, 32) * s.splits, 8);
+    if (dY) (in_out() ? k_stream_out<2, true> : k_stream_out<2, false>)<<<grid, STREAM_WAVES * 64, 0, ctx->stream>>>(s);
+    else (in_out() ? k_stream_out<1, false> : k_stream_out<1, true>)<<<grid, STREAM_WAVES * 64, 0, ctx->stream>>>(s);
+    HT_LAUNCH_CHECK(ctx);
+    return HT_OK;
+  }
+  int64_t weights() const { return (int64_t)D->d_hidden * (2 * (int64_t)D->d_in + D->d_out); }
+  bool streamed() const {
+    if (std::max({Wg->ld, Wu->ld, Wd->ld}) > STREAM_LD) return false;
+    return dY ? X->rows <= STREAM_ROWS_BWD && weights() >= STREAM_WEIGHTS_BWD : X->rows <= STREAM_ROWS;
+  }
   int run(size_t bytes) const {
     const bool bwd = dY != nullptr, in_out = this->in_out();
     const int64_t n = X->rows, d = D->d_in, f = D->d_hidden, e = D->d_out;
@@ -875,8 +917,11 @@ struct Ffn : FfnCall {
     const int64_t pairs_f = ceil_div64(f, PAIR), pairs_2f = ceil_div64(f, HB), pairs_r = ceil_div64(std::min(n, Rp), PAIR);
     const int cols_D = d <= TN ? COLS_SMALL : COLS, cols_H = e <= TN ? COLS_SMALL : COLS;
     const int64_t mtD = cols_D == COLS ? dp / TM : 1, mtH = cols_H == COLS ? ep / TM : 1;
-    const Ends ends(Y ? mt * nte : dX ? mt * ntd : 0, Y ? pairs_f : pairs_2f, d_w ? mtD * ntD : 0, pairs_r, dWd ? mtH * ntH : 0, pairs_r);
-    const int sy = ends.parts[0], sx = sy, sD = ends.parts[1], sH = ends.parts[2];
+    const bool streamed = this->streamed();
+    const Ends ends(streamed ? 0 : Y ? mt * nte : dX ? mt * ntd : 0, Y ? pairs_f : pairs_2f, d_w ? mtD * ntD : 0, pairs_r, dWd ? mtH * ntH : 0, pairs_r);
+    const int64_t tiles = ceil_div64(std::min(n, Rp), STREAM_TILE), out_tiles = tiles * ceil_div64(Y ? e : d, 32);
+    const int64_t out_parts = std::max<int64_t>(1, std::min(STREAM_BLOCKS / out_tiles, f / (STREAM_WAVES * 32)));
+    const int sy = streamed ? (int)out_parts : ends.parts[0], sx = sy, sD = ends.parts[1], sH = ends.parts[2];
     const int64_t e4 = up_to(e, 4), d4 = up_to(d, 4), f4 = up_to(f, 4);
     // a weight's gradient as it lies: rows and pitch of its parts
     const int64_t wr = in_out ? d : f, wp = in_out ? f4 : d4, vr = in_out ? f : e, vp = in_out ? e4 : f4;
@@ -885,7 +930,7 @@ struct Ffn : FfnCall {
     const int64_t n_top = 2 * Rp + 3 * fp;                 // largest values: rows of H, of dA and dB, columns of H, dA, dB
     const auto top = m.add<uint32_t>(n_top);
     const auto ex = m.add<int>(Rp), ey = m.add<int>(Rp), exb = m.add<int>(Rp / HB), eyb = m.add<int>(Rp / HB), ew2 = m.add<int>(2 * fp / HB), ewd = m.add<int>(fp / HB);
-    const auto W2 = m.add<_Float16>(2 * fp * KSd * 32), Wf = m.add<_Float16>(fp * KSe * 32);
+    const auto W2 = m.add<_Float16>(streamed ? 0 : 2 * fp * KSd * 32), Wf = m.add<_Float16>(streamed ? 0 : fp * KSe * 32);
     const auto Xr = m.add<_Float16>(Rp * KSd * 32);
     const auto Xt = m.add<_Float16>(d_w ? dp * KSR * 32 : 0);
     const auto Gr = m.add<_Float16>(bwd ? Rp * KSe * 32 : 0);
@@ -909,7 +954,7 @@ struct Ffn : FfnCall {
       operand(Pack{X->ptr + r0 * X->ld, X->ld, rows, d, 0, m.at(ex), m.at(exb), m.at(Xr), KSd, 1, 0, d_w ? m.at(Xt) : nullptr, KSR}, up_to(rows, TM));
       if (bwd)
         operand(Pack{dY->ptr + r0 * dY->ld, dY->ld, rows, e, 0, m.at(ey), m.at(eyb), m.at(Gr), KSe, 1, 0, dWd ? m.at(Gt) : nullptr, KSR}, up_to(rows, TM));
-      if (k == 0) {
+      if (k == 0 && !streamed) {
         // by hidden columns: the rows of an OUT_IN Wg, the columns of an IN_OUT one
         operand(Pack{Wg->ptr, Wg->ld, f, d, in_out, nullptr, m.at(ew2), m.at(W2), KSd, 2, 0, nullptr, 0}, fp);
         operand(Pack{Wu->ptr, Wu->ld, f, d, in_out, nullptr, m.at(ew2), m.at(W2), KSd, 2, 1, nullptr, 0}, fp);
@@ -938,7 +983,21 @@ struct Ffn : FfnCall {
       const int64_t row_tiles = ceil_div64(rows, TN);
       Args a = base;
       a.H = m.at(H);
-      if (!bwd || remake) {
+      FfnJoins j{};
+      if (streamed) {
+        a.D = bwd ? m.at(Df) : nullptr;
+        HT_TRY(stream_hidden(StreamHidden{a, {Wg->ptr, Wu->ptr, Wd->ptr}, {Wg->ld, Wu->ld, Wd->ld}, d, e, m.at(Xr), bwd ? m.at(Gr) : nullptr, KSd, KSe, m.at(ex),
+                                          m.at(ey), D->act, !gate, (int)ceil_div64(rows, STREAM_TILE)}));
+        if (const ht_tensor* to = Y ? Y : dX) {
+          const int64_t cols = Y ? e : d, pitch = up_to(cols, 4);
+          float *out = to->ptr + r0 * to->ld, *sums = Y ? m.at(sums_y) : m.at(sums_x);
+          const bool parts = sy > 1;
+          StreamOut o{rows, f, cols, {Y ? Wd->ptr : Wg->ptr, Wu->ptr}, {Y ? Wd->ld : Wg->ld, Wu->ld}, (const _Float16*)(Y ? m.at(H) : m.at(Df)), Y ? KSH : KSD, {h_row, d_row},
+                      sy, (int)ceil_div64(rows, STREAM_TILE), parts ? sums : out, parts ? pitch : to->ld, Rp * pitch, !parts && D->accumulate};
+          if (parts) j.join[j.n++] = FfnJoin{sums, Rp * pitch, pitch, rows, cols, sy, D->accumulate, out, to->ld};
+          HT_TRY(stream_out(o));
+        }
+      } else if (!bwd || remake) {
         a.A = m.at(W2), a.KSA = KSd, a.B = m.at(Xr), a.KSB = KSd;
         a.mt = ceil_div64(f, TN), a.nt = row_tiles, a.pairs = ceil_div64(d, PAIR);
         a.e_w = m.at(ew2), a.e_in = m.at(ex);
@@ -952,7 +1011,8 @@ struct Ffn : FfnCall {
         }
       }
       if (bwd) a.D = m.at(Df), a.e_d = m.at(ew2);
-      if (remake) {
+      if (streamed) {
+      } else if (remake) {
         a.nt = ceil_div64(rows, REMAKE_ROWS);
         const RemakeArgs r{a, m.at(Wf), m.at(Gr), KSe, ceil_div64(e, PAIR), m.at(ewd), m.at(ey)};
         with_act(D->act, [&](auto act) { k_ffn_remake<decltype(act)::value><<<(unsigned)up_to(a.mt * a.nt, 8), 256, 0, st>>>(r); });
@@ -964,7 +1024,6 @@ struct Ffn : FfnCall {
         HT_TRY(launch(BACK, a));
       }
       // Y, or dX; their parts' sums are added up behind each piece, those of the weights' gradients behind the last
-      FfnJoins j{};
       auto by_rows = [&](const ht_tensor* to, const float* P, int64_t KSP, bool two, const _Float16* W, int64_t KSW, const int* e_w, int64_t cols, int64_t nt,
                          int64_t pairs, int splits, float* sums, int64_t pitch) {
         Args a = base;
@@ -994,16 +1053,16 @@ struct Ffn : FfnCall {
         a.add = k > 0 || (splits == 1 && D->accumulate_dW);
         return a;
       };
-      if (Y) HT_TRY(launch(ROWS, by_rows(Y, m.at(H), KSH, false, m.at(Wf), KSe, m.at(ewd), e, nte, pairs_f, sy, m.at(sums_y), e4)));
+      if (Y && !streamed) HT_TRY(launch(ROWS, by_rows(Y, m.at(H), KSH, false, m.at(Wf), KSe, m.at(ewd), e, nte, pairs_f, sy, m.at(sums_y), e4)));
       Args ax{}, ad{}, ah{};                             // (no tiles: not asked for)
-      if (dX) ax = by_rows(dX, m.at(Df), KSD, true, m.at(W2), KSd, m.at(ew2), d, ntd, pairs_2f, sx, m.at(sums_x), d4);
+      if (dX && !streamed) ax = by_rows(dX, m.at(Df), KSD, true, m.at(W2), KSd, m.at(ew2), d, ntd, pairs_2f, sx, m.at(sums_x), d4);
       if (d_w) ad = by_cols(m.at(Xt), m.at(exb), d, m.at(Df), KSD, true, mtD, ntD, sD, m.at(sums_D), wr, wp, dWg, dWu, in_out);
       if (dWd) ah = by_cols(m.at(Gt), m.at(eyb), e, m.at(H), KSH, false, mtH, ntH, sH, m.at(sums_H), vr, vp, dWd, nullptr, !in_out);
       const int64_t bx = blocks_of(ax), bd = blocks_of(ad), bh = blocks_of(ah);
       if (bwd && ends.one) {
         const auto kernel = cols_D == COLS ? (cols_H == COLS ? k_ffn_ends<COLS, COLS> : k_ffn_ends<COLS, COLS_SMALL>)
                                            : (cols_H == COLS ? k_ffn_ends<COLS_SMALL, COLS> : k_ffn_ends<COLS_SMALL, COLS_SMALL>);
-        kernel<<<(unsigned)(bx + bd + bh), 256, 0, st>>>(EndsArgs{{ax, ad, ah}, {0, (unsigned)bx, (unsigned)(bx + bd)}});
+        if (bx + bd + bh > 0) kernel<<<(unsigned)(bx + bd + bh), 256, 0, st>>>(EndsArgs{{ax, ad, ah}, {0, (unsigned)bx, (unsigned)(bx + bd)}});
         HT_LAUNCH_CHECK(ctx);
       } else {
         if (bx) HT_TRY(launch(ROWS, ax));
@@ -1021,7 +1080,7 @@ struct Ffn : FfnCall {
         if (t && !D->accumulate_dW) w.join[w.n++] = FfnJoin{nullptr, 0, up_to(t->cols, 4), t->rows, t->cols, 0, 0, t->ptr, t->ld};
       return ht_ffn_join(ctx, w);
     }
-    if (X->rows <= HT_FFN_FEW) return ht_ffn_few(*this);
+    if (X->rows <= (weights() < FEW_WEIGHTS || !streamed() ? HT_FFN_FEW : 16)) return ht_ffn_few(*this);
     const int rc = run(FFN_BYTES);
     return rc == HT_ENOMEM ? run(FFN_LEAN) : rc;      // (nothing has been launched by a call that is refused memory)
   }

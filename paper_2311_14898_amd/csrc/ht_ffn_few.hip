@@ -88,16 +88,6 @@ __device__ __forceinline__ void few_products(v4f (&acc)[M][NB], const float* con
   }
 }
 
-__device__ __forceinline__ Act few_act(int act, float a) {
-  switch (act) {
-    case HT_GATE_SILU: return act_of<HT_GATE_SILU>(a);
-    case HT_GATE_GELU: return act_of<HT_GATE_GELU>(a);
-    case HT_GATE_GELU_TANH: return act_of<HT_GATE_GELU_TANH>(a);
-    case HT_GATE_RELU: return act_of<HT_GATE_RELU>(a);
-    default: return act_of<HT_GATE_SIGMOID>(a);
-  }
-}
-
 struct FewArgs {
   int64_t n, d, f, e;
   int act;
@@ -205,7 +195,7 @@ __global__ void __launch_bounds__(WAVES * 64) k_few_hidden(FewArgs a) {
 #pragma unroll
       for (int w = 0; w < WAVES; ++w) s[m] += sh[w][m][k];
     if (!make) s[0] = a.gate[v * a.ld_gate + cc], s[1] = a.up[v * a.ld_up + cc];
-    const Act x = few_act(a.act, s[0]);
+    const Act x = any_act(a.act, s[0]);
     h[u] = x.v * s[1];
     if constexpr (!BWD) {
       if (a.gate) a.gate[v * a.ld_gate + cc] = s[0], a.up[v * a.ld_up + cc] = s[1];

@@ -297,6 +297,70 @@ def test_what_is_not_finite_stays_where_it_reaches(ctx, n, bad):
     check({"dWd": got["dWd"]}, ref, tol)
 
 
+# (few rows, and weights that are most of what there is to read)
+STREAMED = [(65, 301, 2_405, 300), (128, 300, 2_400, 300), (130, 513, 1_366, 514), (256, 130, 8_200, 47), (500, 61, 130, 37), (17, 1_001, 5_603, 1_003), (64, 1_024, 5_600, 1_000), (16, 1_001, 5_603, 1_003)]
+
+
+@pytest.mark.parametrize("form", [B.HT_W_IN_OUT, B.HT_W_OUT_IN])
+@pytest.mark.parametrize("n,d,f,e", STREAMED)
+def test_weights_that_are_read_once(ctx, n, d, f, e, form):
+    X, Wg, Wu, Wd, dY = _inputs(n, d, f, e)
+    ref, tol = reference(X, Wg, Wu, Wd, "silu", dY)
+    check(call(ctx, X, Wg, Wu, Wd, dY=dY, form=form, ld_w=n % 3), ref, tol)
+    check(call(ctx, X, Wg, Wu, Wd, dY=dY, form=form, keep=True, add=True), ref, tol, add=True)
+
+
+@pytest.mark.parametrize("only", [("dX",), ("dWg",), ("dWd",), ("dWu", "dX")])
+def test_some_gradients_of_weights_that_are_read_once(ctx, only):
+    X, Wg, Wu, Wd, dY = _inputs(70, 301, 2_405, 300)
+    ref, tol = reference(X, Wg, Wu, Wd, "gelu", dY)
+    check(call(ctx, X, Wg, Wu, Wd, act="gelu", dY=dY, only=only), ref, tol)
+
+
+@pytest.mark.parametrize("form", [B.HT_W_IN_OUT, B.HT_W_OUT_IN])
+def test_weights_that_grow_along_a_reduction(ctx, form):
+    """Each step of a reduction meets a larger value than those before it: what was added up with a smaller scale comes with; zeros before them have no scale at all."""
+    X, Wg, Wu, Wd, dY = _inputs(100, 320, 2_240, 320)
+    grow = lambda n, top: np.exp2(np.linspace(-top, 0, n)).astype(np.float32)[:, None]
+    Wg, Wu = Wg * grow(320, 30), Wu * grow(320, 60)
+    Wg[:40] = 0.0
+    Wd = Wd * grow(2_240, 50)
+    ref, tol = reference(X, Wg, Wu, Wd, "silu", dY)
+    check(call(ctx, X, Wg, Wu, Wd, dY=dY, form=form), ref, tol)
+    Wd = np.ascontiguousarray(Wd[:, ::-1]) * grow(320, 40).T
+    Wg, Wu = (w * np.float32(2.0 ** s) * grow(2_240, 20).T for w, s in ((Wg, -20), (Wu, 40)))      # (dX: two products whose factors are far apart, and whose sums are not)
+    ref, tol = reference(X, Wg, Wu, Wd, "silu", dY)
+    check(call(ctx, X, Wg, Wu, Wd, dY=dY, form=form, keep=True), ref, tol)
+    tiny = [w * np.float32(2.0 ** -110) for w in (Wg, Wu)]
+    ref, tol = reference(X, *tiny, Wd, "sigmoid", dY)
+    got = call(ctx, X, *tiny, Wd, act="sigmoid", dY=dY, form=form, only=("dWu",))
+    check({"dWu": got["dWu"]}, ref, tol)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+def test_what_is_not_finite_in_weights_that_are_read_once(ctx, bad):
+    n, d, f, e = 100, 300, 2_405, 290
+    X, Wg, Wu, Wd, dY = _inputs(n, d, f, e)
+    ref, tol = reference(X, Wg, Wu, Wd, "silu", dY)
+    Wb = Wd.copy()
+    Wb[2_401, 289] = bad                     # in the last steps of both reductions
+    got = call(ctx, X, Wg, Wu, Wb, dY=dY)
+    assert not np.isfinite(got["Y"][:, 289]).any() and not np.isfinite(got["dX"]).any()
+    check({"Y": got["Y"][:, :289]}, {"Y": ref["Y"][:, :289]}, {"Y": tol["Y"][:, :289]})
+    rest = np.arange(f) != 2_401
+    for k in ("dWg", "dWu"):
+        assert not np.isfinite(got[k][:, 2_401]).any()
+        check({k: got[k][:, rest]}, {k: ref[k][:, rest]}, {k: tol[k][:, rest]})
+    check({"dWd": got["dWd"]}, ref, tol)
+    Xb = X.copy()
+    Xb[77, 299] = bad
+    got = call(ctx, Xb, Wg, Wu, Wd, dY=dY)
+    rest = np.arange(n) != 77
+    for k in ("Y", "dX"):
+        assert not np.isfinite(got[k][77]).any(), k
+        check({k: got[k][rest]}, {k: ref[k][rest]}, {k: tol[k][rest]})
+
+
 def test_no_rows(ctx):
     d, f, e = 12, 20, 8
     z = lambda r, c: torch.zeros(r, c, device="cuda")
