@@ -553,18 +553,19 @@ typedef struct {
  * one matrix beside each other do not).  Asynchronous, recorded, and the same bits
  * from call to call (of more than 64 rows as long as memory allows the same
  * pieces), as the calls above.
- *   Products are added up in fp32.  With at most 64 rows their factors are fp32 too;
- * with more they keep 22 bits, fewer of values below 2^-17 of the largest that they
- * are scaled with, none below 2^-39: of the row for X, dY and, between the products,
- * H, dA and dB (for the weights' gradients of the hidden column for those, of 32
- * rows for X and dY), of the 32 hidden columns for the weights.  Where a factor is not
- * finite, what it reaches is NaN.
+ *   Products are added up in fp32.  With at most 64 rows (16, where the weights are
+ * 2^24 values or more) their factors are fp32 too; with more they keep 22 bits, fewer
+ * of values below 2^-17 of the largest that they are scaled with, none below 2^-39: of
+ * the row for X, dY and, between the products, H, dA and dB (for the weights'
+ * gradients of the hidden column for those, of 32 rows for X and dY), for the weights
+ * of 32 hidden columns, or of 32 columns of what is made of them.  Where a factor is
+ * not finite, what it reaches is NaN.
  *   Scratch memory: 4 bytes a weight (hidden columns counted in 256s, others in
- * 128s) and up to 4 GiB for the rows of a piece, 4 bytes each for d and hidden
- * columns, with gradients for 2 d + 2 e and three times the hidden columns, all
- * counted in 256s (pieces are smaller where memory is scarce), and up to some 200 MB
- * for parts of sums; with at most 64 rows 8 bytes a hidden value, and 4 for each value
- * of Y or dX up to 512 / (their columns / 16) times. */
+ * 128s; none with few rows) and up to 4 GiB for the rows of a piece, 4 bytes each for
+ * d and hidden columns, with gradients for 2 d + 2 e and three times the hidden
+ * columns, all counted in 256s (pieces are smaller where memory is scarce), and up to
+ * some 200 MB for parts of sums; with fp32 factors 8 bytes a hidden value, and 4 for
+ * each value of Y or dX up to 512 / (their columns / 16) times. */
 int ht_ffn_fwd(ht_ctx *ctx, const ht_ffn_desc *desc, const ht_tensor *X, const ht_tensor *Wg, const ht_tensor *Wu, const ht_tensor *Wd,
                ht_tensor *Y, ht_tensor *gate, ht_tensor *up);
 /* Its gradients from dY: with G = dY Wd^T,

@@ -1,7 +1,7 @@
 // Gated feed-forward blocks:  A = X Wg ;  B = X Wu ;  H = act(A) * B ;  Y = H Wd, and their gradients:
 //   G = dY Wd^T ;  dA = G * B * act'(A) ;  dB = G * act(A) ;  dX = dA Wg^T + dB Wu^T ;  dWg = X^T dA ;  dWu = X^T dB ;  dWd = H^T dY
 //
-// All products are fp32 products on the fp16 matrix cores (ht_split.h).  X, dY and the weights are packed into fragments of split values first, in one launch that
+// All products are fp32 products on the fp16 matrix cores (ht_split.h).  X, dY and the weights are packed into fragments of split values first (weights that few rows meet are not: ht_ffn_stream.h), in one launch that
 // reads them twice: 32 rows (of a weight 32 hidden columns) a block, scaled by the largest of each row (of a weight by that of the block); for the
 // gradients of weights X and dY also turned, scaled by the largest of the 32 rows.  The hidden columns of Wg and Wu lie interleaved by 32s, so that one product makes A and B of the
 // same column in the same lane, and dA and dB are one operand with a reduction over both.  H, dA and dB are kept in fp32, in the order of fragments, and with the largest
@@ -820,9 +820,9 @@ constexpr int64_t SLOTS = 512;                     // blocks that run together: 
 constexpr int64_t LEAST_PAIRS = 4;                 // of a part of a reduction, where a product has a launch for itself
 
 constexpr int64_t SHORT_PAIRS = 8;
-// Weights that are read once (ht_ffn_stream.h) against packed ones, us: forward 128 x 1,024 x 4,096 41 | 89, 512 x 512 x 2,048 43 | 53, 512 x 2,048 x 8,192 284 | 301, 1,024 x 512 x 2,048
-// 64 | 60; backward 128 x 1,024 x 4,096 91 | 130, 256 x 512 x 2,048 73 | 75, 128 x 256 x 1,024 53 | 52, 384 x 1,024 x 4,096 186 | 160 (both have a launch more).
-constexpr int64_t STREAM_ROWS = 512, STREAM_ROWS_BWD = 256, STREAM_WEIGHTS_BWD = (int64_t)1 << 21;
+// Weights that are read once (ht_ffn_stream.h) against packed ones, us: forward 128 x 1,024 x 4,096 41 | 89, 512 x 512 x 2,048 43 | 53, 1,003 x 301 x 1,213 36 | 44, 2,048 x 256 x 1,024 38 | 42, 1,003 x 512 x 2,048 53 | 60,
+// 2,048 x 512 x 1,024 55 | 56, 1,024 x 1,024 x 4,096 142 | 140; backward 128 x 1,024 x 4,096 90 | 130, 256 x 512 x 2,048 72 | 75, 256 x 256 x 1,024 59 | 52, 384 x 1,024 x 4,096 186 | 160.
+constexpr int64_t STREAM_ROWS = 512, STREAM_ROWS_MOST = 2048, STREAM_WORK = (int64_t)7 << 29, STREAM_ROWS_BWD = 256, STREAM_WEIGHTS_BWD = (int64_t)1 << 21;
 constexpr int64_t STREAM_BLOCKS = 256;             // of Y or dX, at most: one a CU
 
 // The products behind H, dA and dB: their tiles, pairs of stages of a tile's reduction, and the parts that it is cut into.
@@ -885,22 +885,23 @@ struct Ffn : FfnCall {
   }
   int stream_hidden(const StreamHidden& s) const {
     const unsigned grid = (unsigned)up_to(s.row_tiles * ceil_div64(s.a.f, HB), 8);
-    if (dY) (in_out() ? k_stream_hidden<true, true> : k_stream_hidden<false, true>)<<<grid, STREAM_WAVES * 64, 0, ctx->stream>>>(s);
-    else (in_out() ? k_stream_hidden<true, false> : k_stream_hidden<false, false>)<<<grid, STREAM_WAVES * 64, 0, ctx->stream>>>(s);
+    if (dY) (in_out() ? k_stream_hidden<true, true> : k_stream_hidden<false, true>)<<<grid, HIDDEN_WAVES * 64, 0, ctx->stream>>>(s);
+    else (in_out() ? k_stream_hidden<true, false> : k_stream_hidden<false, false>)<<<grid, HIDDEN_WAVES * 64, 0, ctx->stream>>>(s);
     HT_LAUNCH_CHECK(ctx);
     return HT_OK;
   }
   int stream_out(const StreamOut& s) const {
     const unsigned grid = (unsigned)up_to(s.row_tiles * ceil_div64(s.width, 32) * s.splits, 8);
-    if (dY) (in_out() ? k_stream_out<2, true> : k_stream_out<2, false>)<<<grid, STREAM_WAVES * 64, 0, ctx->stream>>>(s);
-    else (in_out() ? k_stream_out<1, false> : k_stream_out<1, true>)<<<grid, STREAM_WAVES * 64, 0, ctx->stream>>>(s);
+    if (dY) (in_out() ? k_stream_out<2, true> : k_stream_out<2, false>)<<<grid, OUT_WAVES * 64, 0, ctx->stream>>>(s);
+    else (in_out() ? k_stream_out<1, false> : k_stream_out<1, true>)<<<grid, OUT_WAVES * 64, 0, ctx->stream>>>(s);
     HT_LAUNCH_CHECK(ctx);
     return HT_OK;
   }
   int64_t weights() const { return (int64_t)D->d_hidden * (2 * (int64_t)D->d_in + D->d_out); }
   bool streamed() const {
     if (std::max({Wg->ld, Wu->ld, Wd->ld}) > STREAM_LD) return false;
-    return dY ? X->rows <= STREAM_ROWS_BWD && weights() >= STREAM_WEIGHTS_BWD : X->rows <= STREAM_ROWS;
+    const int64_t n = X->rows;
+    return dY ? n <= STREAM_ROWS_BWD && weights() >= STREAM_WEIGHTS_BWD : n <= STREAM_ROWS || (n <= STREAM_ROWS_MOST && n * weights() <= STREAM_WORK);
   }
   int run(size_t bytes) const {
     const bool bwd = dY != nullptr, in_out = this->in_out();
@@ -920,7 +921,7 @@ struct Ffn : FfnCall {
     const bool streamed = this->streamed();
     const Ends ends(streamed ? 0 : Y ? mt * nte : dX ? mt * ntd : 0, Y ? pairs_f : pairs_2f, d_w ? mtD * ntD : 0, pairs_r, dWd ? mtH * ntH : 0, pairs_r);
     const int64_t tiles = ceil_div64(std::min(n, Rp), STREAM_TILE), out_tiles = tiles * ceil_div64(Y ? e : d, 32);
-    const int64_t out_parts = std::max<int64_t>(1, std::min(STREAM_BLOCKS / out_tiles, f / (STREAM_WAVES * 32)));
+    const int64_t out_parts = std::max<int64_t>(1, std::min(STREAM_BLOCKS / out_tiles, f / (OUT_WAVES * 32)));
     const int sy = streamed ? (int)out_parts : ends.parts[0], sx = sy, sD = ends.parts[1], sH = ends.parts[2];
     const int64_t e4 = up_to(e, 4), d4 = up_to(d, 4), f4 = up_to(f, 4);
     // a weight's gradient as it lies: rows and pitch of its parts

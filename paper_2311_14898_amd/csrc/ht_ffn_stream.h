@@ -1,12 +1,14 @@
-// Blocks of more than 64 rows whose weights are most of what there is to read: the weights go as they lie straight from memory into the registers of the one block that multiplies them
-// (of two, where its rows are two tiles), and are split there; only rows are packed.
-//   k_stream_hidden  32 hidden columns and 64 rows a block: A and B (and G) over all of the reduction, an eighth a wave; of their sums H, or H, dA and dB, in the order of
+// Blocks of more rows than ht_ffn_few.hip has, but not many: most of what there is to read are the weights.  They go as they lie straight from memory into the registers of the block that
+// multiplies them (of one for every 64 rows; the others find them in the caches), and are split there; only rows are packed.
+//   k_stream_hidden  32 hidden columns and 64 rows a block: A and B (and G) over all of the reduction, a quarter a wave; of their sums H, or H, dA and dB, in the order of
 //                    fragments, with their largest values
 //   k_stream_out     32 columns of Y or dX and 64 rows, by a part of the hidden columns a block; the parts are added up behind it
 // A wave scales the weights by the largest that it has met, and its sums with them where a larger one comes: no pass looks for it before.
 #pragma once
 
-constexpr int STREAM_WAVES = 8, NJ = 2, STREAM_TILE = NJ * 32;      // waves of a block, its row blocks and rows
+// Waves of a block of either; row blocks and rows of a tile.  (k_stream_hidden with eight waves: 1,003 x 512 x 2,048 forward 53 -> 64 us, 256 x 2,048 x 8,192 141 -> 157; with tiles of 128 rows
+// 128 x 1,024 x 4,096 51 -> 66, for the rows are read from the caches as often, but by half as many blocks.)
+constexpr int HIDDEN_WAVES = 4, OUT_WAVES = 8, NJ = 2, STREAM_TILE = NJ * 32;
 
 // Eight values of a weight's column (lane l32) along the reduction from k0 on, in the order of fragments.  w: the block's first column (the same in all lanes); off: the lane's place
 // behind it, floats.  BYK: the reduction lies in a row, else ld floats apart.
@@ -144,10 +146,9 @@ struct StreamHidden {
   int act, make, row_tiles;
 };
 template <bool IN_OUT, bool BWD>
-__global__ void __launch_bounds__(STREAM_WAVES * 64, 2) k_stream_hidden(StreamHidden s) {
-  constexpr int SUMS = BWD ? 3 : 2, JR = BWD ? 1 : 2;          // row blocks that LDS takes at once
-  static_assert(NJ % JR == 0, "");
-  __shared__ __attribute__((aligned(16))) float sh[STREAM_WAVES][JR][SUMS][1024];
+__global__ void __launch_bounds__(HIDDEN_WAVES * 64, 2) k_stream_hidden(StreamHidden s) {
+  constexpr int SUMS = BWD ? 3 : 2;
+  __shared__ __attribute__((aligned(16))) float sh[HIDDEN_WAVES][SUMS][1024];
   __shared__ float tops[BWD ? 2 : 1][4][NJ * 32], cols[BWD ? 3 : 1][NJ][32];
   const Args& a = s.a;
   const Tile tile(blockIdx.x, s.row_tiles, (a.f + HB - 1) / HB, 1);
@@ -161,7 +162,7 @@ __global__ void __launch_bounds__(STREAM_WAVES * 64, 2) k_stream_hidden(StreamHi
     const uint32_t off[2] = {raw_off<!IN_OUT>(s.ld[0], a.f - c0), raw_off<!IN_OUT>(s.ld[1], a.f - c0)};
     const _Float16* X = s.X + b0 * s.KSX * 2 * FRAG + lane * 8;
     const int64_t rows = s.KSX * 2 * FRAG;
-    const Steps at(s.d, wave, STREAM_WAVES);
+    const Steps at(s.d, wave, HIDDEN_WAVES);
     stream<2, 1>(ab, at.s0, at.s1, [&](int k, v8h (&x)[2][2], v8h (&y)[1][NJ][2]) {
 #pragma unroll
       for (int m = 0; m < 2; ++m) raw8<!IN_OUT>(x[m], w[m], s.ld[m], off[m], (int64_t)k * 16);
@@ -181,7 +182,7 @@ __global__ void __launch_bounds__(STREAM_WAVES * 64, 2) k_stream_hidden(StreamHi
     const uint32_t off = raw_off<IN_OUT>(s.ld[2], a.f - c0);
     const _Float16* G = s.G + b0 * s.KSG * 2 * FRAG + lane * 8;
     const int64_t rows = s.KSG * 2 * FRAG;
-    const Steps at(s.e, wave, STREAM_WAVES);
+    const Steps at(s.e, wave, HIDDEN_WAVES);
     stream<1, 1>(g, at.s0, at.s1, [&](int k, v8h (&x)[1][2], v8h (&y)[1][NJ][2]) {
       raw8<IN_OUT>(x[0], w, s.ld[2], off, (int64_t)k * 16);
       fragments(y[0], G + (int64_t)k * 2 * FRAG, rows);
@@ -193,33 +194,31 @@ __global__ void __launch_bounds__(STREAM_WAVES * 64, 2) k_stream_hidden(StreamHi
       g[0].split(x), g[0].add(x, y);
     }
   }
-  // the waves' sums: thread (k, lane) of 256 has four columns of a row
+  // the waves' sums, a row block after the other: a lane has four columns of a row, 8 k + 4 half + 0 .. 3
   const Hidden at(a);
-  const int k = (tid >> 6) & 3, group = tid >> 8;
+  static_assert(HIDDEN_WAVES == 4, "a wave for each k");
+  const int k = wave;
   int ex[NJ], ey[NJ];
 #pragma unroll
   for (int j = 0; j < NJ; ++j) ex[j] = s.ex[(b0 + j) * 32 + l32], ey[j] = BWD ? s.ey[(b0 + j) * 32 + l32] : 0;
 #pragma unroll
-  for (int j0 = 0; j0 < NJ; j0 += JR) {
-    if (j0 > 0) __syncthreads();
+  for (int j = 0; j < NJ; ++j) {
+    if (j > 0) __syncthreads();
 #pragma unroll
-    for (int j = 0; j < JR; ++j)
+    for (int q = 0; q < 4; ++q) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-#pragma unroll
-        for (int m = 0; m < 2; ++m) *reinterpret_cast<V4*>(&sh[wave][j][m][(q * 64 + lane) * 4]) = ab[m].four(j0 + j, q, ex[j0 + j]);
-        if (BWD) *reinterpret_cast<V4*>(&sh[wave][j][SUMS - 1][(q * 64 + lane) * 4]) = g[0].four(j0 + j, q, ey[j0 + j]);
-      }
+      for (int m = 0; m < 2; ++m) *reinterpret_cast<V4*>(&sh[wave][m][(q * 64 + lane) * 4]) = ab[m].four(j, q, ex[j]);
+      if (BWD) *reinterpret_cast<V4*>(&sh[wave][SUMS - 1][(q * 64 + lane) * 4]) = g[0].four(j, q, ey[j]);
+    }
     __syncthreads();
-    if (group >= JR) continue;
     V4 x[SUMS];
 #pragma unroll
     for (int m = 0; m < SUMS; ++m) {
       x[m] = V4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int w = 0; w < STREAM_WAVES; ++w) x[m] += *reinterpret_cast<const V4*>(&sh[w][group][m][(k * 64 + lane) * 4]);
+      for (int w = 0; w < HIDDEN_WAVES; ++w) x[m] += *reinterpret_cast<const V4*>(&sh[w][m][(k * 64 + lane) * 4]);
     }
-    const int64_t block = b0 + j0 + group, v = block * 32 + l32, c = c0 + k * 8 + half * 4;
+    const int64_t block = b0 + j, v = block * 32 + l32, c = c0 + k * 8 + half * 4;
     const bool there = v < a.n, whole = c0 + HB <= a.f;
     if (BWD && !s.make) {
       const int64_t row = there ? v : a.n - 1;
@@ -244,7 +243,7 @@ __global__ void __launch_bounds__(STREAM_WAVES * 64, 2) k_stream_hidden(StreamHi
     at.put_frag(a.H, a.KSH, block, step, k & 1, h);
     auto row_top = [&](int which, float m) {
       m = fmaxf(m, __shfl_xor(m, 32, 64));
-      if (half == 0) tops[which][k][(j0 + group) * 32 + l32] = m;
+      if (half == 0) tops[which][k][j * 32 + l32] = m;
     };
     row_top(0, BWD ? ma : mh);
     if constexpr (BWD) {
@@ -257,13 +256,13 @@ __global__ void __launch_bounds__(STREAM_WAVES * 64, 2) k_stream_hidden(StreamHi
       for (int i = 0; i < 4; ++i) ch[i] = fabsf(h[i] * fy), ca[i] = fabsf(da[i] * fx), cb[i] = fabsf(db[i] * fx);
       const float th = max_over_32(ch), ta = max_over_32(ca), tb = max_over_32(cb);
       const int col = k * 8 + half * 4 + (l32 >> 3);
-      if (!(l32 & 7)) cols[0][j0][col] = th, cols[1][j0][col] = ta, cols[2][j0][col] = tb;
+      if (!(l32 & 7)) cols[0][j][col] = th, cols[1][j][col] = ta, cols[2][j][col] = tb;
     }
   }
   // largest values, to where they are kept: a thread each, so that all of them take one trip to memory
   __syncthreads();
   constexpr int R = NJ * 32, ROWS_OF = BWD ? 2 : 1;
-  static_assert(ROWS_OF * R + 96 <= STREAM_WAVES * 64, "a thread each");
+  static_assert(ROWS_OF * R + 96 <= HIDDEN_WAVES * 64, "a thread each");
   if (tid < ROWS_OF * R) {
     const int which = tid / R, r = tid % R;
     const float m = fmaxf(fmaxf(tops[which][0][r], tops[which][1][r]), fmaxf(tops[which][2][r], tops[which][3][r]));
@@ -291,9 +290,9 @@ struct StreamOut {
 };
 // M: Y's weight, or the two of dX.
 template <int M, bool BYK>
-__global__ void __launch_bounds__(STREAM_WAVES * 64, 2) k_stream_out(StreamOut s) {
+__global__ void __launch_bounds__(OUT_WAVES * 64, 2) k_stream_out(StreamOut s) {
   constexpr int GROUP = 32 * 4 + 4, BLOCK = 8 * GROUP;         // floats: four columns of 32 rows, a row block (what a store's lanes read lies in other banks)
-  __shared__ __attribute__((aligned(16))) float sh[STREAM_WAVES][NJ][BLOCK];
+  __shared__ __attribute__((aligned(16))) float sh[OUT_WAVES][NJ][BLOCK];
   const Tile tile(blockIdx.x, s.row_tiles, (s.width + 31) / 32, s.splits);
   if (tile.m < 0) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
@@ -320,7 +319,7 @@ __global__ void __launch_bounds__(STREAM_WAVES * 64, 2) k_stream_out(StreamOut s
       }
   };
   Scaled sums[M];
-  const Steps at(s.f, (int)tile.split * STREAM_WAVES + wave, s.splits * STREAM_WAVES);
+  const Steps at(s.f, (int)tile.split * OUT_WAVES + wave, s.splits * OUT_WAVES);
   stream<M, M>(sums, at.s0, at.s1, [&](int k, v8h (&x)[M][2], v8h (&y)[M][NJ][2]) {
 #pragma unroll
     for (int m = 0; m < M; ++m) {
@@ -350,12 +349,12 @@ __global__ void __launch_bounds__(STREAM_WAVES * 64, 2) k_stream_out(StreamOut s
   __syncthreads();
 #pragma unroll
   for (int u = 0; u < NJ / 2; ++u) {
-    const int i = u * STREAM_WAVES * 64 + tid, j = i >> 8, row = (i >> 3) & 31, g = i & 7;
+    const int i = u * OUT_WAVES * 64 + tid, j = i >> 8, row = (i >> 3) & 31, g = i & 7;
     const int64_t v = (b0 + j) * 32 + row, c = c0 + g * 4;
     if (v >= s.n || c >= s.width) continue;
     V4 x{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int q = 0; q < STREAM_WAVES; ++q) x += *reinterpret_cast<const V4*>(&sh[q][j][g * GROUP + row * 4]);
+    for (int q = 0; q < OUT_WAVES; ++q) x += *reinterpret_cast<const V4*>(&sh[q][j][g * GROUP + row * 4]);
     float* to = s.out + tile.split * s.part + v * s.pitch + c;
     if (c + 4 <= s.width) {
       if (s.add) x += *reinterpret_cast<const V4*>(to);
