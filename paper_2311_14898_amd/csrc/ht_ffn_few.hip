@@ -38,7 +38,7 @@ __device__ __forceinline__ v4f load4(const float* p, int64_t left) {
 // in a row, else k_ld floats apart.  x[b]: row l of the b-th 16.
 template <int NB, int M, bool BYK>
 __device__ __forceinline__ void few_products(v4f (&acc)[M][NB], const float* const (&w)[M], const int64_t (&k_ld)[M], const float* const (&x)[NB], int64_t K, int s0, int s1) {
-  constexpr int U = NB * M <= 2 ? 4 : 2;       // steps loaded together
+  constexpr int U = NB * M <= 4 ? 4 : 2;       // steps loaded together
   const int q = (threadIdx.x & 63) >> 4;
   auto multiply = [&](const v4f (&a)[M], const v4f (&b)[NB]) {
 #pragma unroll
@@ -67,6 +67,8 @@ __device__ __forceinline__ void few_products(v4f (&acc)[M][NB], const float* con
 #pragma unroll
       for (int c = 0; c < NB; ++c) b[u][c] = *reinterpret_cast<const v4f*>(x[c] + k);
     }
+    // (all loads before the first product: 24 x 1,024 x 4,096 forward 32 -> 23 us, 1 x 4,096 x 16,384 205 -> 197, backward 682 -> 628; of 64 rows backward 82 -> 85)
+    if (NB < 4) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int u = 0; u < U; ++u) multiply(a[u], b[u]);
   }
