@@ -12,7 +12,7 @@ struct FfnCall {
   bool in_out() const { return D->w_form == HT_W_IN_OUT; }
 };
 // Of 1 .. HT_FFN_FEW rows (ht_ffn_few.hip); with FEW_WEIGHTS values of weights, of at most 16: more multiply longer there than they read (2,048 x 8,192, us there | with weights split: forward
-// of 16 rows 51 | 59, 17 66 | 58, 64 112 | 62, backward 176 | 188, 192 | 195, 316 | 204; 1,024 x 4,096: forward of 48 rows 30 | 36, 64 39 | 36, backward 68 | 77, 82 | 79).
+// of 16 rows 49 | 59, 17 68 | 59, 64 107 | 61, backward 171 | 188, 209 | 192, 313 | 198; 1,024 x 4,096: forward of 48 rows 30 | 36, 64 38 | 36, backward 68 | 77, 81 | 79).
 constexpr int HT_FFN_FEW = 64;
 constexpr int64_t FEW_WEIGHTS = (int64_t)1 << 24;
 int ht_ffn_few(const FfnCall& c);

@@ -197,6 +197,46 @@ def test_recorded_and_replayed(big):
         B.ht_ctx_destroy(ctx)
 
 
+def test_weights_that_are_read_once_recorded():
+    """Few rows and wide weights, forward and backward, over inputs that change between the replays; largest values are found anew in each."""
+    n, d, f, e = 100, 301, 2_405, 300
+    s = torch.cuda.Stream()
+    ctx = B.ht_ctx_create(0, s.cuda_stream)
+    try:
+        ins = [torch.from_numpy(t).cuda() for t in ffn_inputs(n, 304, f + 3, e)]
+        X, Wg, Wu, Wd, dY = ins
+        outs = [torch.zeros(n, e, device="cuda"), torch.zeros(n, 304, device="cuda")] + [torch.zeros_like(w) for w in (Wg[:d], Wu[:d], Wd[:f])]
+
+        def run():
+            B.ht_ffn_fwd(ctx, d, f, e, X, Wg[:d], Wu[:d], Wd[:f], outs[0], sync=False)
+            B.ht_ffn_bwd(ctx, d, f, e, X, Wg[:d], Wu[:d], Wd[:f], dY, dX=outs[1], dWg=outs[2], dWu=outs[3], dWd=outs[4], sync=False)
+
+        torch.cuda.synchronize()
+        run()
+        s.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            run()
+        for k, scale in enumerate((1.0, 1e-4, 30.0, 0.0, 1.0)):
+            for t, new in zip(ins, ffn_inputs(n, 304, f + 3, e, seed=k)):
+                t.copy_(torch.from_numpy(new) * scale)
+            torch.cuda.synchronize()
+            run()
+            s.synchronize()
+            want = [o.clone() for o in outs]
+            for o in outs:
+                o.fill_(float(k))
+            torch.cuda.synchronize()
+            with torch.cuda.stream(s):
+                graph.replay()
+            s.synchronize()
+            for o, w, cols in zip(outs, want, (e, d, f, f, e)):
+                assert torch.isfinite(w[:, :cols]).all() and (o[:, :cols] == w[:, :cols]).all()
+        del graph
+    finally:
+        B.ht_ctx_destroy(ctx)
+
+
 def test_a_recorded_first_call_is_refused():
     s = torch.cuda.Stream()
     ctx = B.ht_ctx_create(0, s.cuda_stream)
