@@ -1004,9 +1004,9 @@ struct Ffn : FfnCall {
         a.e_w = m.at(ew2), a.e_in = m.at(ex);
         a.e_d = m.at(ewd);
         if (!bwd) {
-          // (half tiles where whole ones leave room for more blocks: 1,003 x 301 x 1,213 56 -> 49 us, 300 x 256 x 688 44 -> 39; of more tiles they only read more: 16,384 x
-          // 1,024 x 4,096 1,114 -> 1,192)
-          const bool small = a.mt * a.nt < SLOTS;
+          // (half tiles where whole ones are on half of the CUs at most: 1,024 x 1,024 x 2,048 102 -> 90 us, 4,096 x 128 x 512 41 -> 39; of more tiles they only read more: 1,024 x 1,024 x
+          // 4,096 135 -> 138, 16,384 x 1,024 x 4,096 1,114 -> 1,192)
+          const bool small = a.mt * a.nt < SLOTS / 2;
           if (small) a.nt = ceil_div64(rows, TN / 2);
           HT_TRY(launch(small ? PROJECT_SMALL : PROJECT, a));
         }

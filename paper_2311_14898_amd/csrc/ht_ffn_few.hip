@@ -1,4 +1,4 @@
-// Gated feed-forward blocks of at most 64 rows, where all there is to do is read the weights (and write their gradients): fp32 matrix instructions on the weights as they lie,
+// Gated feed-forward blocks of at most 64 rows (16 of very wide weights), where all there is to do is read the weights (and write their gradients): fp32 matrix instructions on the weights as they lie,
 // no copies of them.
 //   k_few_hidden  16 hidden columns a block: A and B (and G) over all of the reduction, an eighth a wave; H, or H, dA and dB; and of the gradients of the weights all that these
 //                 columns have, which is whole: their reduction is over the rows

@@ -365,6 +365,20 @@ def test_a_last_piece_of_one_row(form):
         B.ht_ctx_destroy(ctx)
 
 
+@pytest.mark.parametrize("form", [B.HT_W_IN_OUT, B.HT_W_OUT_IN])
+def test_pieces_of_rows_that_meet_weights_as_they_lie(form):
+    """Hidden rows of 161 KB: 64 MiB hold 256 of 600, which go in three pieces."""
+    X, Wg, Wu, Wd, _ = ffn_inputs(600, 9, 40_007, 6)
+    ref, tol = reference(X, Wg, Wu, Wd, "sigmoid")
+    ctx = B.ht_ctx_create(0)
+    try:
+        B.ht_ctx_set_hbm_budget(ctx, 100 << 20)
+        check(ffn_call(ctx, X, Wg, Wu, Wd, act="sigmoid", form=form), ref, tol)
+        check(ffn_call(ctx, X, Wg, Wu, Wd, act="sigmoid", form=form, keep=True, add=True), ref, tol, add=True)
+    finally:
+        B.ht_ctx_destroy(ctx)
+
+
 def test_scratch_memory_that_holds_nan():
     """What an earlier call left in the scratch memory reaches nothing: NaN all over it, then widths and rows that end inside every kind of tile."""
     ctx = B.ht_ctx_create(0)
