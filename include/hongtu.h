@@ -557,9 +557,10 @@ typedef struct {
  * 2^24 values or more) their factors are fp32 too; with more they keep 22 bits, fewer
  * of values below 2^-17 of the largest that they are scaled with, none below 2^-39: of
  * the row for X, dY and, between the products, H, dA and dB (for the weights'
- * gradients of the hidden column for those, of 32 rows for X and dY), for the weights
- * of 32 hidden columns, or of 32 columns of what is made of them.  Where a factor is
- * not finite, what it reaches is NaN.
+ * gradients of 32 rows for X and dY, of the hidden column for those, each value times
+ * the largest of the 32 rows that it meets: rows of zeros take nothing off it), for
+ * the weights of 32 hidden columns, or of 32 columns of what is made of them.  Where a
+ * factor is not finite, what it reaches is NaN.
  *   Scratch memory: 4 bytes a weight (hidden columns counted in 256s, others in
  * 128s; none with few rows) and up to 4 GiB for the rows of a piece, 4 bytes each for
  * d and hidden columns, with gradients for 2 d + 2 e and three times the hidden

@@ -29,6 +29,8 @@ __device__ __forceinline__ int scale_exp(uint32_t bits) {
 }
 __device__ __forceinline__ int exp_or_0(int e) { return e >= NONE ? 0 : e; }
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)((e < -126 ? -126 : e > 126 ? 126 : e) + 127) << 23); }
+// What a block of zeros (its exponent is NONE) meets is scaled by 0: it adds nothing, and takes no bits off what the other blocks meet.  (What is not finite becomes NaN there, as 0 times it is.)
+__device__ __forceinline__ float pow2_or_0(int e) { return e < -NONE / 2 ? 0.f : pow2(e); }
 // Of an operand the largest value is that of what is finite: the rest becomes NaN in its split, and takes no bits off the others.
 __device__ __forceinline__ uint32_t size_bits(float x) {
   const uint32_t b = __float_as_uint(fabsf(x));
@@ -43,7 +45,7 @@ struct Pack {
   const float* p;
   int64_t ld, own, run;
   int turned;
-  int *e_own, *e_block;                // exponents: of each of the own (null: they have the block's), of the block
+  int *e_own, *e_block;                // exponents: of each of the own (null: they have the block's), of the block (with e_own NONE where it is all zeros)
   _Float16* F;                         // by own rows, reduction along run: row block b is number b mul + add, KS steps
   int64_t KS;
   int mul, add;
@@ -141,9 +143,9 @@ __global__ void __launch_bounds__(256) k_ffn_pack(Packs packs) {
   __syncthreads();
   uint32_t all = top[l32];
   for (int o = 16; o > 0; o >>= 1) all = max(all, (uint32_t)__shfl_xor((int)all, o, 64));
-  const int eb = exp_or_0(scale_exp(all)), eo = a.e_own ? exp_or_0(scale_exp(top[l32])) : eb;
+  const int e_all = scale_exp(all), eb = exp_or_0(e_all), eo = a.e_own ? exp_or_0(scale_exp(top[l32])) : eb;
   if (tid < HB && a.e_own && part == 0) a.e_own[own0 + tid] = eo;
-  if (tid == 0 && a.e_block && part == 0) a.e_block[(int64_t)block * a.mul + a.add] = eb;
+  if (tid == 0 && a.e_block && part == 0) a.e_block[(int64_t)block * a.mul + a.add] = a.e_own ? e_all : eb;
   const float fb = pow2(eb), fo = pow2(eo);
   auto put = [&](_Float16* to, int64_t frag, const float (&x)[8]) {
     v8h hi, lo;
@@ -446,7 +448,7 @@ struct Hidden {
     const int64_t c0 = hb * HB;
     float fx[NJ], fy[NJ], ma[NJ] = {}, mb[NJ] = {};
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) fx[j] = pow2(-a.e_x[b0 + j]), fy[j] = pow2(-a.e_y[b0 + j]);
+    for (int j = 0; j < NJ; ++j) fx[j] = pow2_or_0(-a.e_x[b0 + j]), fy[j] = pow2_or_0(-a.e_y[b0 + j]);
     const int eg = a.e_d[hb * 2], eu = a.e_d[hb * 2 + 1];
     const int l32 = lane & 31;
     V4 x[2][NJ], y[2][NJ];
@@ -570,7 +572,7 @@ __device__ __forceinline__ void ffn_split(const Args& a, unsigned block, _Float1
 #pragma unroll
       for (int k = 0; k < 8; ++k) fc[u][k] = pow2(col_exp(n0 + wave * 32 + u * 16 + (k >> 2) * 8 + half * 4 + (k & 3)));
     multiply<true, true>(acc, Ap, a_rows, B, b_rows, a.e_w + s0, todo, Bs, a_as_it_is, [&](v8h (&rb)[4], int e) {
-      const float f = pow2(-e);
+      const float f = pow2_or_0(-e);
 #pragma unroll
       for (int u = 0; u < 2; ++u) split8(rb[u * 2], rb[u * 2 + 1], f, [&](int t) { return fc[u][t]; });
     });

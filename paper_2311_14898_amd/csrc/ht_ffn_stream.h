@@ -250,7 +250,7 @@ __global__ void __launch_bounds__(HIDDEN_WAVES * 64, 2) k_stream_hidden(StreamHi
       at.put_frag(a.D, a.KSD, block, step_d, k & 1, da);
       at.put_frag(a.D, a.KSD, block, step_d + 2, k & 1, db);
       row_top(1, mb);
-      const float fx = pow2(-a.e_x[block]), fy = pow2(-a.e_y[block]);
+      const float fx = pow2_or_0(-a.e_x[block]), fy = pow2_or_0(-a.e_y[block]);
       float ch[4], ca[4], cb[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) ch[i] = fabsf(h[i] * fy), ca[i] = fabsf(da[i] * fx), cb[i] = fabsf(db[i] * fx);

@@ -1,0 +1,70 @@
+"""Gated blocks: where what a factor is scaled by is nothing, or at the ends of the range.  Against 64 bits, with the tolerances of test_gpu_ffn.
+
+A reduction over rows scales X and dY by the largest value of 32 rows, and one over hidden columns the weights by that of 32 hidden columns.  Where those are all zeros they add
+nothing, whatever the other factor is there, and so they may take no bits of it elsewhere: the same tolerances hold."""
+import numpy as np
+import pytest
+
+from paper_2311_14898_amd import binding as B
+from tests.test_gpu_ffn import _inputs, call, check, reference
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = B.ht_ctx_create(0)
+    yield c
+    B.ht_ctx_destroy(c)
+
+
+# (packed; packed with narrow widths on both sides of it; weights that are read once)
+ROWS = [(140, 30, 60, 20), (330, 150, 200, 140), (100, 301, 2_405, 300)]
+
+
+@pytest.mark.parametrize("keep", [False, True])
+@pytest.mark.parametrize("tiny", [1e-3, 1e-5, 1e-8])
+@pytest.mark.parametrize("n,d,f,e", ROWS)
+def test_blocks_of_rows_without_gradients(ctx, n, d, f, e, tiny, keep):
+    """dY of 32 and of 64 rows beside each other is zero, as that of rows without a label is."""
+    X, Wg, Wu, Wd, dY = _inputs(n, d, f, e)
+    dY *= np.float32(tiny * 100)
+    for first, last in ((0, 32), (32, 96)):
+        masked = dY.copy()
+        masked[first:last] = 0.0
+        ref, tol = reference(X, Wg, Wu, Wd, "silu", masked)
+        check(call(ctx, X, Wg, Wu, Wd, dY=masked, keep=keep), ref, tol)
+
+
+@pytest.mark.parametrize("keep", [False, True])
+@pytest.mark.parametrize("tiny", [1e-3, 1e-5, 1e-8])
+@pytest.mark.parametrize("n,d,f,e", ROWS)
+def test_blocks_of_rows_of_zeros(ctx, n, d, f, e, tiny, keep):
+    """X of such rows is zero, and their gates are open: dB of them is not zero, and adds nothing to dWu."""
+    X, Wg, Wu, Wd, dY = _inputs(n, d, f, e)
+    X *= np.float32(tiny)
+    for first, last in ((0, 32), (32, 96)):
+        padded = X.copy()
+        padded[first:last] = 0.0
+        ref, tol = reference(padded, Wg, Wu, Wd, "sigmoid", dY)
+        check(call(ctx, padded, Wg, Wu, Wd, act="sigmoid", dY=dY, keep=keep), ref, tol)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("n,d,f,e", ROWS)
+def test_what_is_not_finite_meets_blocks_of_zeros(ctx, n, d, f, e, bad):
+    """A zero times what is not finite is NaN, on either side."""
+    X, Wg, Wu, Wd, dY = _inputs(n, d, f, e)
+    dY[32:64] = 0.0
+    Xb = X.copy()
+    Xb[40, 3] = bad                          # a row without gradients
+    got = call(ctx, Xb, Wg, Wu, Wd, dY=dY)
+    assert np.isnan(got["dWd"]).all() and np.isnan(got["dWg"]).all() and np.isnan(got["dWu"]).all()
+    db = dY.copy()
+    db[50, 7] = bad                          # and one whose block's other gradients are zeros: column 7 of dWd, and all that G reaches
+    ref, tol = reference(X, Wg, Wu, Wd, "silu", dY)
+    got = call(ctx, X, Wg, Wu, Wd, dY=db)
+    assert np.isnan(got["dWd"][:, 7]).all() and np.isnan(got["dWg"]).all() and np.isnan(got["dWu"]).all() and np.isnan(got["dX"][50]).all()
+    rest, rows = np.arange(e) != 7, np.arange(n) != 50
+    check({"dWd": got["dWd"][:, rest]}, {"dWd": ref["dWd"][:, rest]}, {"dWd": tol["dWd"][:, rest]})
+    check({"dX": got["dX"][rows]}, {"dX": ref["dX"][rows]}, {"dX": tol["dX"][rows]})
