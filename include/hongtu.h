@@ -556,11 +556,12 @@ typedef struct {
  *   Products are added up in fp32.  With at most 64 rows (16, where the weights are
  * 2^24 values or more) their factors are fp32 too; with more they keep 22 bits, fewer
  * of values below 2^-17 of the largest that they are scaled with, none below 2^-39: of
- * the row for X, dY and, between the products, H, dA and dB (for the weights'
- * gradients of 32 rows for X and dY, of the hidden column for those, each value times
- * the largest of the 32 rows that it meets: rows of zeros take nothing off it), for
- * the weights of 32 hidden columns, or of 32 columns of what is made of them.  Where a
- * factor is not finite, what it reaches is NaN.
+ * the row for X and dY (for the weights' gradients of 32 rows), for the weights of 32
+ * hidden columns, or of 32 columns of what is made of them.  H, dA and dB, between the
+ * products, are scaled with their row, for the weights' gradients with their column,
+ * each value times the largest of the 32 rows of X or dY that it meets or, in large
+ * calls, of the weights of the 32 hidden columns: where those are zeros it takes
+ * nothing off the others.  Where a factor is not finite, what it reaches is NaN.
  *   Scratch memory: 4 bytes a weight (hidden columns counted in 256s, others in
  * 128s; none with few rows) and up to 4 GiB for the rows of a piece, 4 bytes each for
  * d and hidden columns, with gradients for 2 d + 2 e and three times the hidden

@@ -29,7 +29,8 @@ __device__ __forceinline__ int scale_exp(uint32_t bits) {
 }
 __device__ __forceinline__ int exp_or_0(int e) { return e >= NONE ? 0 : e; }
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)((e < -126 ? -126 : e > 126 ? 126 : e) + 127) << 23); }
-// What a block of zeros (its exponent is NONE) meets is scaled by 0: it adds nothing, and takes no bits off what the other blocks meet.  (What is not finite becomes NaN there, as 0 times it is.)
+// What a block of zeros (its exponent is NONE) meets is scaled by 0: it adds nothing, and takes no bits off what the other blocks meet.  (What is not finite becomes NaN there, as 0 times it is.
+// ldexp takes NONE as it is: sums of zeros stay 0, and largest values less it are 0.)
 __device__ __forceinline__ float pow2_or_0(int e) { return e < -NONE / 2 ? 0.f : pow2(e); }
 // Of an operand the largest value is that of what is finite: the rest becomes NaN in its split, and takes no bits off the others.
 __device__ __forceinline__ uint32_t size_bits(float x) {
@@ -45,7 +46,7 @@ struct Pack {
   const float* p;
   int64_t ld, own, run;
   int turned;
-  int *e_own, *e_block;                // exponents: of each of the own (null: they have the block's), of the block (with e_own NONE where it is all zeros)
+  int *e_own, *e_block;                // exponents: of each of the own (null: they have the block's), of the block (NONE where it is all zeros)
   _Float16* F;                         // by own rows, reduction along run: row block b is number b mul + add, KS steps
   int64_t KS;
   int mul, add;
@@ -145,7 +146,7 @@ __global__ void __launch_bounds__(256) k_ffn_pack(Packs packs) {
   for (int o = 16; o > 0; o >>= 1) all = max(all, (uint32_t)__shfl_xor((int)all, o, 64));
   const int e_all = scale_exp(all), eb = exp_or_0(e_all), eo = a.e_own ? exp_or_0(scale_exp(top[l32])) : eb;
   if (tid < HB && a.e_own && part == 0) a.e_own[own0 + tid] = eo;
-  if (tid == 0 && a.e_block && part == 0) a.e_block[(int64_t)block * a.mul + a.add] = a.e_own ? e_all : eb;
+  if (tid == 0 && a.e_block && part == 0) a.e_block[(int64_t)block * a.mul + a.add] = e_all;
   const float fb = pow2(eb), fo = pow2(eo);
   auto put = [&](_Float16* to, int64_t frag, const float (&x)[8]) {
     v8h hi, lo;
@@ -562,7 +563,7 @@ __device__ __forceinline__ void ffn_split(const Args& a, unsigned block, _Float1
 #pragma unroll
     for (int i = 0; i < 2; ++i) er[i] = row_exp(mw + i * 32 + l32);
     multiply<true, true>(acc, Ap, a_rows, B, b_rows, a.e_w + s0, todo, Bs, [&](v8h (&x)[2], int i, int e) {
-      const float f = pow2(er[i] - e);
+      const float f = pow2_or_0(er[i] - e);
       split8(x[0], x[1], 1.f, [&](int) { return f; });
     }, b_as_it_is);
   } else if constexpr (BY_COLS) {

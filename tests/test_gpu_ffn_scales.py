@@ -68,3 +68,44 @@ def test_what_is_not_finite_meets_blocks_of_zeros(ctx, n, d, f, e, bad):
     rest, rows = np.arange(e) != 7, np.arange(n) != 50
     check({"dWd": got["dWd"][:, rest]}, {"dWd": ref["dWd"][:, rest]}, {"dWd": tol["dWd"][:, rest]})
     check({"dX": got["dX"][rows]}, {"dX": ref["dX"][rows]}, {"dX": tol["dX"][rows]})
+
+
+# (weights are packed from 65 rows on backward, and from 2,049 on forward)
+HIDDEN = [(140, 30, 100, 20), (330, 150, 200, 140), (2_100, 40, 97, 24)]
+
+
+@pytest.mark.parametrize("form", [B.HT_W_IN_OUT, B.HT_W_OUT_IN])
+@pytest.mark.parametrize("tiny", [1e-2, 1e-4, 1e-7])
+@pytest.mark.parametrize("n,d,f,e", HIDDEN)
+def test_blocks_of_hidden_columns_without_weights(ctx, n, d, f, e, tiny, form):
+    """32 hidden columns' rows of Wd, or columns of Wg and of Wu, are zeros, as pruned ones are."""
+    X, Wg, Wu, Wd, dY = _inputs(n, d, f, e)
+    Wz = Wd * np.float32(tiny)
+    Wz[32:64] = 0.0
+    ref, tol = reference(X, Wg, Wu, Wz, "silu", dY)
+    check(call(ctx, X, Wg, Wu, Wz, dY=dY, form=form), ref, tol)
+    gates = [w * np.float32(tiny) for w in (Wg, Wu)]
+    for which in ((0,), (1,), (0, 1)):
+        zeros = [w.copy() for w in gates]
+        for k in which:
+            zeros[k][:, 64:96] = 0.0
+        ref, tol = reference(X, *zeros, Wd, "sigmoid", dY)
+        check(call(ctx, X, *zeros, Wd, act="sigmoid", dY=dY, form=form), ref, tol)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("n", [140, 2_100])
+def test_what_is_not_finite_meets_hidden_columns_of_zeros(ctx, n, bad):
+    X, Wg, Wu, Wd, dY = _inputs(n, 30, 100, 20)
+    Wd[32:64] = 0.0
+    Wb = Wu.copy()
+    Wb[5, 40] = bad                          # hidden column 40 is not finite, its weights behind are zeros: so is Y
+    got = call(ctx, X, Wg, Wb, Wd, dY=dY)
+    assert np.isnan(got["Y"]).all()
+    Wb = Wd.copy()
+    Wb[33, 4] = bad                          # column 4 of Y
+    ref, tol = reference(X, Wg, Wu, Wd, "silu")
+    got = call(ctx, X, Wg, Wu, Wb)
+    assert np.isnan(got["Y"][:, 4]).all()
+    rest = np.arange(20) != 4
+    check({"Y": got["Y"][:, rest]}, {"Y": ref["Y"][:, rest]}, {"Y": tol["Y"][:, rest]})
