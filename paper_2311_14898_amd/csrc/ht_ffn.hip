@@ -31,7 +31,7 @@ __device__ __forceinline__ int exp_or_0(int e) { return e >= NONE ? 0 : e; }
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)((e < -126 ? -126 : e > 126 ? 126 : e) + 127) << 23); }
 // What a block of zeros (its exponent is NONE) meets is scaled by 0: it adds nothing, and takes no bits off what the other blocks meet.  (What is not finite becomes NaN there, as 0 times it is.
 // ldexp takes NONE as it is: sums of zeros stay 0, and largest values less it are 0.)
-__device__ __forceinline__ float pow2_or_0(int e) { return e < -NONE / 2 ? 0.f : pow2(e); }
+__device__ __forceinline__ float pow2_or_0(int e) { return e < -NONE / 4 ? 0.f : pow2(e); }
 // Of an operand the largest value is that of what is finite: the rest becomes NaN in its split, and takes no bits off the others.
 __device__ __forceinline__ uint32_t size_bits(float x) {
   const uint32_t b = __float_as_uint(fabsf(x));
@@ -563,8 +563,10 @@ __device__ __forceinline__ void ffn_split(const Args& a, unsigned block, _Float1
 #pragma unroll
     for (int i = 0; i < 2; ++i) er[i] = row_exp(mw + i * 32 + l32);
     multiply<true, true>(acc, Ap, a_rows, B, b_rows, a.e_w + s0, todo, Bs, [&](v8h (&x)[2], int i, int e) {
-      const float f = pow2_or_0(er[i] - e);
-      split8(x[0], x[1], 1.f, [&](int) { return f; });
+      // (in two powers: the row's exponent has the weights' in it, and less this stage's it may lie outside the range of floats)
+      const int t = er[i] - e, u = t >> 1;
+      const float f = pow2_or_0(t - u);
+      split8(x[0], x[1], pow2(u), [&](int) { return f; });
     }, b_as_it_is);
   } else if constexpr (BY_COLS) {
     float fc[2][8];

@@ -109,3 +109,30 @@ def test_what_is_not_finite_meets_hidden_columns_of_zeros(ctx, n, bad):
     assert np.isnan(got["Y"][:, 4]).all()
     rest = np.arange(20) != 4
     check({"Y": got["Y"][:, rest]}, {"Y": ref["Y"][:, rest]}, {"Y": tol["Y"][:, rest]})
+
+
+@pytest.mark.parametrize("form", [B.HT_W_IN_OUT, B.HT_W_OUT_IN])
+@pytest.mark.parametrize("small,large", [(-114, 16), (-116, 30), (-118, 100), (-60, 60)])
+def test_small_hidden_values_and_large_weights(ctx, small, large, form):
+    """Hidden values near the least of all floats, and weights that bring what is made of them back: each power of two may lie outside the range of floats, their products do not.
+    (Floats have no finer step than 2^-149: half of it for each rounding on the way to hidden values, times what they meet, is added to what these may be off.)"""
+    half = 2.0 ** -150
+    n, d, f, e = 2_100, 40, 96, 24
+    X, Wg, Wu, Wd, dY = _inputs(n, d, f, e)
+    Wu, Wd = Wu * np.float32(2.0 ** small), Wd * np.float32(2.0 ** large)
+    ref, tol = reference(X, Wg, Wu, Wd, "silu")
+    a = np.abs(X.astype(np.float64) @ Wg)    # (H = v B, |v| <= |a|)
+    tol["Y"] = tol["Y"] + 1.01 * half * ((1.0 + a) @ np.abs(Wd).astype(np.float64))
+    got = call(ctx, X, Wg, Wu, Wd, form=form)
+    check({"Y": got["Y"]}, ref, tol)
+    n = 140
+    X, Wg, Wu, Wd, dY = _inputs(n, d, f, e)
+    back = np.float32(2.0 ** -large)
+    X, Wg, Wu, dY = X * back, Wg / back, Wu / back, dY * np.float32(2.0 ** (small + 7))
+    ref, tol = reference(X, Wg, Wu, Wd, "silu", dY)
+    a, u = (np.abs(X.astype(np.float64) @ w) for w in (Wg, Wu))
+    # (dA = G u s, |s| < 1.1, with roundings of G, of G u and of the whole; dB = G v)
+    tol["dX"] = tol["dX"] + 1.01 * half * ((2.1 + 1.1 * u) @ np.abs(Wg).T.astype(np.float64) + (1.0 + a) @ np.abs(Wu).T.astype(np.float64))
+    for keep in (False, True):
+        got = call(ctx, X, Wg, Wu, Wd, dY=dY, form=form, keep=keep, only=("dX",))
+        check({"dX": got["dX"]}, ref, tol)
