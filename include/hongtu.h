@@ -584,8 +584,8 @@ int ht_ffn_bwd(ht_ctx *ctx, const ht_ffn_desc *desc, const ht_tensor *X, const h
  * norm: device float, none of the tensors' values.  Squares are added up in 64 bits:
  * no value is too small or too large for its square, but a norm above the largest
  * float is +inf.  grads is an array of n on the host, which the call is done with
- * when it returns; n may be 0 (a norm of 0).  A tensor that is named twice counts
- * twice. */
+ * when it returns; n may be 0 (a norm of 0).  Tensors without rows or columns count
+ * nothing, and need no memory; one that is named twice counts twice. */
 int ht_grad_norm(ht_ctx *ctx, int32_t n, const ht_tensor *grads, float *norm);
 /* The same norm, and every tensor scaled so that it is at most max_norm > 0 (+inf: as
  * it is):

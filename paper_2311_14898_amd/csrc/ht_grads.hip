@@ -134,7 +134,7 @@ __global__ void __launch_bounds__(256) k_grad_scale(List list, const float* __re
 }
 
 int check(ht_ctx* ctx, const char* name, const char* what, int32_t i, const ht_tensor& t) {
-  if (t.rows >= 0 && t.rows <= INT32_MAX && t.cols >= 0 && t.ld >= t.cols && t.loc == HT_LOC_DEVICE && ((uintptr_t)t.ptr & 3) == 0 && (t.ptr || t.rows == 0)) return HT_OK;
+  if (t.rows >= 0 && t.rows <= INT32_MAX && t.cols >= 0 && t.ld >= t.cols && t.loc == HT_LOC_DEVICE && ((uintptr_t)t.ptr & 3) == 0 && (t.ptr || t.rows == 0 || t.cols == 0)) return HT_OK;
   char s[96];                          // (a text for each of hundreds of tensors would be most of a call)
   snprintf(s, sizeof s, "%s: %s %d", name, what, i);
   if (t.rows < 0 || t.cols < 0) return ht_set_err(ctx, HT_ESHAPE, "%s: [%lld x %d]", s, (long long)t.rows, t.cols);
