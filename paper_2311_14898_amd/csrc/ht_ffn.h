@@ -57,8 +57,8 @@ __device__ __forceinline__ Act act_of(float a) {
     return {a >= 0.f ? hi : lo, lo * hi};
   }
   if constexpr (ACT == HT_GATE_GELU) {
-    // Phi(-|a|) = e^(-a^2 / 2) / 2 times exp(z^2) erfc(z), z = |a| / sqrt(2), which is t times a polynomial of t = 1 / (1 + 0.4 z) to 6.2e-9 of itself (a least
-    // squares fit to 4,000 values of t in (0, 1], weights raised where it was worst).  A library's erfc takes five times as long: 13 of 28 us of k_ffn_narrow over 1,003 x 1,213.
+    // Phi(-|a|) = e^(-a^2 / 2) / 2 times exp(z^2) erfc(z), z = |a| / sqrt(2), which is t times a polynomial of t = 1 / (1 + 0.4 z) to 1.4e-8 of itself (a least
+    // squares fit to 4,000 values of t in (0, 1], weights raised where it was worst, its coefficients rounded to floats).  The rounding of a^2 in the exponent counts a^2 / 2 fold.  A library's erfc takes five times as long: 13 of 28 us of k_ffn_narrow over 1,003 x 1,213.
     constexpr float R[11] = {-0.0292151887f, 0.14044708f, -0.235528022f, 0.13756232f, -0.0468958393f, 0.0839167088f, 0.119008213f, 0.171739295f, 0.207613721f, 0.225675866f, 0.225675836f};
     const float e = __builtin_amdgcn_exp2f(a * a * (-0.5f * LOG2E)), t = __builtin_amdgcn_rcpf(fmaf(0.28284271247461901f, fabsf(a), 1.f));
     float r = R[0];

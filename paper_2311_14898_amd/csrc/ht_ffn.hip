@@ -3,7 +3,7 @@
 //
 // All products are fp32 products on the fp16 matrix cores (ht_split.h).  X, dY and the weights are packed into fragments of split values first (weights that few rows meet are not: ht_ffn_stream.h), in one launch that
 // reads them twice: 32 rows (of a weight 32 hidden columns) a block, scaled by the largest of each row (of a weight by that of the block); for the
-// gradients of weights X and dY also turned, scaled by the largest of the 32 rows.  The hidden columns of Wg and Wu lie interleaved by 32s, so that one product makes A and B of the
+// gradients of weights X and dY also turned, scaled by the largest of the 32 rows.  (A block of zeros has no scale, and what meets it counts in none.)  The hidden columns of Wg and Wu lie interleaved by 32s, so that one product makes A and B of the
 // same column in the same lane, and dA and dB are one operand with a reduction over both.  H, dA and dB are kept in fp32, in the order of fragments, and with the largest
 // values of their rows and columns; the products that read them split them as they load, with no pass in between: by rows where the reduction is over
 // hidden columns, by columns where it is over rows.  A scale that changes along a reduction (of the other operand's 32s) is taken off what is split: a stage of a product is
@@ -443,7 +443,8 @@ struct Hidden {
   }
   // H, dA and dB of NJ row blocks from row block b0 on, of the hidden block hb.  Largest values, less the exponents of what they will meet: of the rows of dA and dB
   // together in md, of the columns (of H, dA, dB, 32 each) to cols.  (An infinite one may be the largest: what is scaled by it is not finite in any case.)  get(j, k, x, y): A
-  // and B of four hidden columns of a row, fetched four columns ahead; sums(j, k, e): G of one.  Behind the last row and column G is 0, and so is A or B.
+  // and B of four hidden columns of a row, fetched four columns ahead; sums(j, k, e): G of one.  Behind the last row and column G is 0, and with it dA and dB; H is 0
+  // behind the last row, and behind the last column what get() gives there, which nothing reads that is kept.
   template <int ACT, int NJ, class Get, class Sums>
   __device__ __forceinline__ void back(int64_t b0, int64_t hb, float (&md)[NJ], float* cols, Get&& get, Sums&& sums) const {
     const int64_t c0 = hb * HB;
@@ -826,7 +827,8 @@ constexpr int64_t LEAST_PAIRS = 4;                 // of a part of a reduction, 
 
 constexpr int64_t SHORT_PAIRS = 8;
 // Weights that are read once (ht_ffn_stream.h) against packed ones, us: forward 128 x 1,024 x 4,096 41 | 89, 512 x 512 x 2,048 43 | 53, 1,003 x 301 x 1,213 36 | 44, 2,048 x 256 x 1,024 38 | 42, 1,003 x 512 x 2,048 53 | 60,
-// 2,048 x 512 x 1,024 55 | 56, 1,024 x 1,024 x 4,096 142 | 140; backward 128 x 1,024 x 4,096 90 | 130, 256 x 512 x 2,048 72 | 75, 256 x 256 x 1,024 59 | 52, 384 x 1,024 x 4,096 186 | 160.
+// 2,048 x 512 x 1,024 55 | 56, 1,024 x 1,024 x 4,096 142 | 140; with more work, 256 x 2,048 x 8,192 136 | 245, 512 x 1,024 x 4,096 79 | 96, 512 x 2,048 x 8,192 251 | 287, 512 x 4,096 x 16,384
+// 1,039 | 1,042; backward 128 x 1,024 x 4,096 90 | 130, 256 x 512 x 2,048 72 | 75, 256 x 256 x 1,024 59 | 52, 384 x 1,024 x 4,096 186 | 160.
 constexpr int64_t STREAM_ROWS = 512, STREAM_ROWS_MOST = 2048, STREAM_WORK = (int64_t)7 << 29, STREAM_ROWS_BWD = 256, STREAM_WEIGHTS_BWD = (int64_t)1 << 21;
 constexpr int64_t STREAM_BLOCKS = 256;             // of Y or dX, at most: one a CU
 
@@ -1009,8 +1011,9 @@ struct Ffn : FfnCall {
         a.e_w = m.at(ew2), a.e_in = m.at(ex);
         a.e_d = m.at(ewd);
         if (!bwd) {
-          // (half tiles where whole ones are on half of the CUs at most: 1,024 x 1,024 x 2,048 102 -> 90 us, 4,096 x 128 x 512 41 -> 39; of more tiles they only read more: 1,024 x 1,024 x
-          // 4,096 135 -> 138, 16,384 x 1,024 x 4,096 1,114 -> 1,192)
+          // (half tiles where whole ones fill less than half of the places, us of whole ones -> of half ones: 128 tiles, 1,024 x 1,024 x 2,048 101 -> 89, 4,096 x 512 x 512 62 -> 56, 4,096 x 128 x
+          // 512 41 -> 38; 192, 4,096 x 512 x 768 67.2 -> 66.7; 216, 2,304 x 512 x 1,536 68.6 -> 68.4; 240, 1,024 x 1,024 x 3,840 123 -> 126.  Of more tiles they only read more: 16,384 x 1,024 x
+          // 4,096 1,114 -> 1,192)
           const bool small = a.mt * a.nt < SLOTS / 2;
           if (small) a.nt = ceil_div64(rows, TN / 2);
           HT_TRY(launch(small ? PROJECT_SMALL : PROJECT, a));

@@ -101,7 +101,7 @@ struct FewArgs {
   int64_t pitch;
   float *dWg, *dWu, *dWd;              // (null: not wanted)
   int64_t ld_dWg, ld_dWu, ld_dWd;
-  int in_out, add;
+  int add;
 };
 
 // The gradient of a weight: of its 16 columns l from c0 on (of f), for features of P [n x width] by 16s; t: [NB * 16][16] in LDS, 0 behind the last row and column.  A feature's value
@@ -306,7 +306,7 @@ int few(const FfnCall& c) {
   if (c.dWg) a.dWg = c.dWg->ptr, a.ld_dWg = c.dWg->ld;
   if (c.dWu) a.dWu = c.dWu->ptr, a.ld_dWu = c.dWu->ld;
   if (c.dWd) a.dWd = c.dWd->ptr, a.ld_dWd = c.dWd->ld;
-  a.in_out = in_out, a.add = c.D->accumulate_dW;
+  a.add = c.D->accumulate_dW;
   const unsigned grid = (unsigned)((ceil_div64(f, OUTS) + 7) / 8 * 8);
   if (bwd) (in_out ? k_few_hidden<NB, true, true> : k_few_hidden<NB, false, true>)<<<grid, WAVES * 64, 0, st>>>(a);
   else (in_out ? k_few_hidden<NB, true, false> : k_few_hidden<NB, false, false>)<<<grid, WAVES * 64, 0, st>>>(a);

@@ -95,7 +95,7 @@ struct Scaled {
   }
 };
 // Products of the columns of M weights with rows, over the steps s0 .. s1 - 1; a step's operands are fetched two steps ahead: fetch(s, a, b), and what is done to b before it is
-// used: in_b(b).  TWO: each weight has rows of its own (b[1]).
+// used: in_b(b).  NB = 2: each weight has rows of its own (b[1]).
 template <int M, int NB, class Fetch, class InB>
 __device__ __forceinline__ void stream(Scaled (&sums)[M], int s0, int s1, Fetch&& fetch, InB&& in_b) {
   if (s0 >= s1) return;
